@@ -436,6 +436,75 @@ convbn_status convbn_aux_maxpool_fwd(int dtype, const void *x, void *y, void *id
 convbn_status convbn_aux_maxpool_bwd(int dtype, const void *dy, const void *idx, void *dx,
                                      int32_t N, int32_t H, int32_t W, int32_t C, void *stream);
 
+/* ---- 8-bit rows: activation checkpoints, and a Linear block on integer products ----------------------------
+ * What a Tune block keeps between its passes is its input.  These calls hold it in 8 bits, and run a Linear block (a
+ * pointwise convolution whose pixels are the rows; a projection whose tokens are) on the very same codes.
+ *
+ * A row of channels -- a token, a pixel of a channels-last tensor, an output channel's weights -- is held as
+ *     a = max |x|,   s = a / 127,   code = rint(x (127 / a))  in fp32, ties to even:  -127 .. 127,
+ * so that x is about s code (s the next smaller fp32 where 127 s would overflow).  A row with a < 2^-119 (all zeros: padding) has s = 0 and codes 0; a row that holds an infinity
+ * or a NaN has s = NaN and codes 0: what is computed from it is NaN.  Codes are dense rows of convbn_qrow_bytes(K)
+ * bytes (K rounded up to 16; the bytes past K are zero, writers leave them so and readers rely on it), scales one fp32 a row.
+ *
+ *   forward    z[m,n]  = sx[m] sw[n] sum_k qx[m,k] qw[n,k] + b[n]            (the integer sum is exact)
+ *   backward   dx[m,k] = sum_n dz[m,n] sw[n] qw[n,k]     dW[n,k] = sum_m dz[m,n] sx[m] qx[m,k]     db[n] = sum_m dz[m,n]
+ * Backward is the gradient of the product of the two rounded operands; the rounding itself passes it on unchanged.  With dtype
+ * BF16 the products s q are rounded to bf16 before they meet the bf16 gradients (sums in fp32); with F32 nothing is
+ * rounded below fp32.
+ *
+ * Rows may be strided (ldx, ldz); codes, scales, W and vectors are dense.  M == 0 is no error: nothing is read, dW and db
+ * become zero.  A sum over the channels is exact up to K = 131072 (longer: CONVBN_ERR_UNSUPPORTED).  codes and workspace are
+ * 16-byte aligned; rows of x, z, dx, dz, h, y, dy, dh need the alignment of their element only (16 bytes are faster). */
+typedef struct {
+  int64_t M;                  /* rows of x, z, dx, dz (a gate: of h, y, dy, dh)                                      */
+  int64_t ldx, ldz;           /* elements from a row of x / dx (a gate: h / dh) and of z / dz (y / dy) to the next;  */
+                              /* 0 = dense                                                                           */
+  int32_t K, N;               /* channels in and out (pack, unpack: of a row; a gate: of each half; N unused there) */
+  int32_t dtype;              /* convbn_dtype of x, z, dx, dz, W, dW, h, y, dy, dh                                   */
+  int32_t act;                /* CONVBN_ACT_ADD_OUT and / or _ADD_IN, 0 = none                                       */
+  int32_t gate;               /* convbn_gate (the gate calls)                                                        */
+  int32_t reserved;           /* 0                                                                                   */
+  const void *add_out;        /* CONVBN_ACT_ADD_OUT: forward returns z + add_out, laid out like z (it may be z)      */
+  const void *add_in;         /* CONVBN_ACT_ADD_IN: backward returns dx + add_in, laid out like dx (it may be dx)    */
+} convbn_qdesc;
+
+typedef enum { CONVBN_GATE_SILU = 0, CONVBN_GATE_GELU = 1 } convbn_gate;   /* g / (1 + e^-g);  g (1 + erf(g / sqrt 2)) / 2 */
+
+/* Bytes from one row of codes to the next (0 for channels < 1). */
+size_t convbn_qrow_bytes(int32_t channels);
+
+/* Rows x [M][K] (ldx apart) to codes and scales, and back (x = s code, rounded to dtype).  Any block whose input was kept this
+ * way reads it back for its backward call; a weight [N][K] is packed with M = N (a scale for each output channel). */
+convbn_status convbn_qpack(const convbn_qdesc *desc, const void *x, void *codes, float *scales,
+                           void *stream);
+convbn_status convbn_qunpack(const convbn_qdesc *desc, const void *codes, const float *scales, void *x,
+                             void *stream);
+
+/* Bytes of device workspace that convbn_qlinear_fwd / _bwd need (pass: convbn_pass); 0 for an invalid descriptor. */
+size_t convbn_qlinear_workspace_bytes(const convbn_qdesc *desc, int pass);
+
+/* Forward.  x != NULL: its rows are packed into codes and scales (what backward needs; both NULL = not kept).  x == NULL: codes
+ * and scales are given.  w_codes, w_scales: the weight packed by output channel.  b: [N] fp32, nullable. */
+convbn_status convbn_qlinear_fwd(const convbn_qdesc *desc, const void *x, void *codes, float *scales,
+                                 const void *w_codes, const float *w_scales, const float *b,
+                                 void *z, void *ws, size_t ws_bytes, void *stream);
+
+/* Backward from the kept codes.  dx, dW, db nullable, each = not wanted (codes and scales are read for dW only, w_codes and
+ * w_scales for dx only).  dW: [N][K] of dtype. */
+convbn_status convbn_qlinear_bwd(const convbn_qdesc *desc, const void *codes, const float *scales,
+                                 const void *w_codes, const float *w_scales, const void *dz,
+                                 void *dx, void *dW, float *db, void *ws, size_t ws_bytes,
+                                 void *stream);
+
+/* Gate: y = f(g) u for rows h = [g | u] of 2 K channels, ldx apart.  h_codes, h_scales: both NULL (nothing is kept) or h packed by
+ * halves, i.e. as 2 M rows of K channels, g's before u's.  y: nullable; y_codes, y_scales: y packed (from the fp32 value), both
+ * NULL = not wanted; one of the two forms is asked for.
+ * Backward: dh = [dy u f'(g) | dy f(g)] at the g and u that the codes stand for. */
+convbn_status convbn_qgate_fwd(const convbn_qdesc *desc, const void *h, void *h_codes, float *h_scales,
+                               void *y, void *y_codes, float *y_scales, void *stream);
+convbn_status convbn_qgate_bwd(const convbn_qdesc *desc, const void *h_codes, const float *h_scales,
+                               const void *dy, void *dh, void *stream);
+
 /* Bytes a block must keep alive between its forward and its backward call in
  * addition to X (App. K.1): Eval keeps Y (N Cout Hout Wout elements); Tune keeps
  * w' (kH kW Cin Cout elements), or nothing when `refold` is non-zero. */

@@ -34,7 +34,9 @@ EXPORTS = ["convbn_hout", "convbn_wout", "convbn_workspace_bytes", "convbn_saved
            "convbn_tune_fwd_scale_epilogue", "convbn_grouped_workspace_bytes", "convbn_grouped_saved_bytes",
            "convbn_grouped_tune_fwd", "convbn_grouped_tune_bwd", "convbn_grouped_eval_fwd", "convbn_grouped_eval_bwd",
            "convbn_tune_fwd_static", "convbn_static_workspace_limit", "convbn_fold_back_group_table_bytes",
-           "convbn_fold_back_group_plan", "convbn_fold_back_group", "convbn_tune_bwd_is_fused", "convbn_tune_route"]
+           "convbn_fold_back_group_plan", "convbn_fold_back_group", "convbn_tune_bwd_is_fused", "convbn_tune_route",
+           "convbn_qrow_bytes", "convbn_qpack", "convbn_qunpack", "convbn_qlinear_workspace_bytes", "convbn_qlinear_fwd",
+           "convbn_qlinear_bwd", "convbn_qgate_fwd", "convbn_qgate_bwd"]
 
 
 class Desc(C.Structure):
@@ -44,6 +46,13 @@ class Desc(C.Structure):
                 ("stride_h", C.c_int32), ("stride_w", C.c_int32),
                 ("pad_h", C.c_int32), ("pad_w", C.c_int32),
                 ("eps", C.c_float), ("dtype", C.c_int32), ("layout", C.c_int32), ("act", C.c_int32),
+                ("add_out", C.c_void_p), ("add_in", C.c_void_p)]
+
+
+class QDesc(C.Structure):
+    """Mirror of convbn_qdesc."""
+    _fields_ = [("M", C.c_int64), ("ldx", C.c_int64), ("ldz", C.c_int64), ("K", C.c_int32), ("N", C.c_int32),
+                ("dtype", C.c_int32), ("act", C.c_int32), ("gate", C.c_int32), ("reserved", C.c_int32),
                 ("add_out", C.c_void_p), ("add_in", C.c_void_p)]
 
 
@@ -68,6 +77,7 @@ class ConvBNError(RuntimeError):
 
 
 _lib = None
+_call_rows = None
 _call = _at = _NO_WS = None   # the extension's `call`, the entry points' addresses by name, its "no workspace" marker
 _pointer = _stream_handle = None
 
@@ -87,7 +97,7 @@ def _load():
 
 def lib():
     """The loaded library.  Raises if it has not been built (no silent fallback)."""
-    global _lib, _call, _at, _NO_WS, _pointer, _stream_handle
+    global _lib, _call, _call_rows, _at, _NO_WS, _pointer, _stream_handle
     if _lib is None:
         missing = [p for p in (LIB_PATH, CALL_PATH) if not os.path.exists(p)]
         if missing:
@@ -195,9 +205,19 @@ def lib():
         L.convbn_tune_fwd_static.argtypes = [dp, vp, vp, fp, fp, fp, fp, fp, vp, vp, vp]
         L.convbn_static_workspace_limit.restype = C.c_size_t
         L.convbn_static_workspace_limit.argtypes = []
+        L.convbn_qrow_bytes.restype = C.c_size_t
+        L.convbn_qrow_bytes.argtypes = [C.c_int32]
+        qp = C.POINTER(QDesc)
+        L.convbn_qlinear_workspace_bytes.restype = C.c_size_t
+        L.convbn_qlinear_workspace_bytes.argtypes = [qp, C.c_int]
+        for name, tensors, ws in (("convbn_qpack", 3, 0), ("convbn_qunpack", 3, 0), ("convbn_qlinear_fwd", 7, 1),
+                                  ("convbn_qlinear_bwd", 8, 1), ("convbn_qgate_fwd", 6, 0), ("convbn_qgate_bwd", 4, 0)):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = [qp] + [vp] * tensors + [vp, C.c_size_t] * ws + [vp]
         from . import _call as ext
         # another thread may be in its first call: what a call reads behind `_call` or `_lib` is there before they are
         _at, _NO_WS, _pointer, _stream_handle = _Addresses(L), ext.NO_WS, ext.pointer, ext.stream
+        _call_rows = ext.call_rows
         _call = ext.call
         _lib = L
     return _lib
@@ -618,6 +638,61 @@ def convbn_grouped_eval_bwd(desc, groups, x, W, b, gamma, mean, var, y_saved, dz
                             stream=None, check=True):
     return _gblock_bwd("convbn_grouped_eval_bwd", desc, groups, x, W, b, gamma, mean, var, y_saved, dz, dx, dW, db,
                        dgamma, dbeta, ws, stream, check)
+
+
+# ---- 8-bit rows ---------------------------------------------------------------
+
+GATE_SILU, GATE_GELU = 0, 1
+
+
+def make_qdesc(M, K, N=0, dtype=BF16, ldx=0, ldz=0, act=0, gate=GATE_SILU) -> QDesc:
+    return QDesc(M, ldx, ldz, K, N, dtype, act, gate)
+
+
+def convbn_qrow_bytes(channels: int) -> int:
+    return lib().convbn_qrow_bytes(channels)
+
+
+def convbn_qlinear_workspace_bytes(desc: QDesc, pass_: int) -> int:
+    return lib().convbn_qlinear_workspace_bytes(C.byref(desc), pass_)
+
+
+def _rows_call(address, desc, *tensors_and_ws, stream, check):
+    st = _call_rows(address, desc, *tensors_and_ws, None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+def convbn_qpack(desc, x, codes, scales, stream=None, check=True):
+    _call or _load()
+    return _rows_call(_at.convbn_qpack, desc, x, codes, scales, _NO_WS, stream=stream, check=check)
+
+
+def convbn_qunpack(desc, codes, scales, x, stream=None, check=True):
+    _call or _load()
+    return _rows_call(_at.convbn_qunpack, desc, codes, scales, x, _NO_WS, stream=stream, check=check)
+
+
+def convbn_qlinear_fwd(desc, x, codes, scales, w_codes, w_scales, b, z, ws=None, stream=None, check=True):
+    _call or _load()
+    return _rows_call(_at.convbn_qlinear_fwd, desc, x, codes, scales, w_codes, w_scales, b, z, ws, stream=stream, check=check)
+
+
+def convbn_qlinear_bwd(desc, codes, scales, w_codes, w_scales, dz, dx, dW, db, ws=None, stream=None, check=True):
+    _call or _load()
+    return _rows_call(_at.convbn_qlinear_bwd, desc, codes, scales, w_codes, w_scales, dz, dx, dW, db, ws, stream=stream,
+                      check=check)
+
+
+def convbn_qgate_fwd(desc, h, h_codes, h_scales, y, y_codes, y_scales, stream=None, check=True):
+    _call or _load()
+    return _rows_call(_at.convbn_qgate_fwd, desc, h, h_codes, h_scales, y, y_codes, y_scales, _NO_WS, stream=stream, check=check)
+
+
+def convbn_qgate_bwd(desc, h_codes, h_scales, dy, dh, stream=None, check=True):
+    _call or _load()
+    return _rows_call(_at.convbn_qgate_bwd, desc, h_codes, h_scales, dy, dh, _NO_WS, stream=stream, check=check)
 
 
 # ---- channels-last device buffers (pure permutes and casts) -------------------

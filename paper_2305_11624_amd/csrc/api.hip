@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "fold_back_t_tile.h"
+#include "quant.h"
 
 using namespace convbn;
 
@@ -14,13 +15,19 @@ namespace {
 
 thread_local char g_err[256] = "no error";
 
-convbn_status fail(convbn_status code, const char* fmt, ...) {
+}  // namespace
+
+convbn_status convbn::set_error(convbn_status code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return code;
 }
+
+namespace {
+
+convbn_status (&fail)(convbn_status, const char*, ...) = set_error;
 
 int out_size(int in, int k, int s, int p) { return (in + 2 * p - k) / s + 1; }
 

@@ -5,11 +5,12 @@
 // 5-7 us a call; here it takes well under one.
 //
 //   call(address, desc, groups, tensors..., ws, stream) -> status
+//   call_rows(address, desc, tensors..., ws, stream) -> status     (the 8-bit rows: desc is a convbn_qdesc)
 //
 // `address` is the entry point's address, `desc` a convbn_desc (any object with the buffer protocol), groups None
 // means that the entry point takes none; a tensor is None, a device tensor or an int (a raw address); ws is None or a
 // device tensor, passed on as pointer and size (NO_WS: the entry point takes none); stream is None (the current
-// stream) or a raw handle.
+// stream) or a raw handle.  Tensors are dense; call_rows also takes matrices whose rows are ldx or ldz of the descriptor apart.
 #include <Python.h>
 
 #include <c10/hip/HIPStream.h>
@@ -19,6 +20,8 @@
 #include <exception>
 
 #include "../../include/convbn.h"
+
+static_assert(sizeof(convbn_desc) != sizeof(convbn_qdesc), "the calls tell the descriptors apart by their size");
 
 namespace {
 
@@ -40,13 +43,19 @@ bool guarded(F&& f) {
   return false;
 }
 
-// Address of a tensor argument; false (with a Python error set) where it is neither None, an int nor a dense device tensor.
-bool pointer_of(PyObject* o, void** out) {
+// Whether a tensor is a matrix with the row stride of the descriptor's.
+bool has_rows_of(const at::Tensor& t, const convbn_qdesc* d) {
+  return d && t.dim() == 2 && t.stride(1) == 1 && (t.stride(0) == d->ldx || t.stride(0) == d->ldz);
+}
+
+// Address of a tensor argument; false (with a Python error set) where it is neither None, an int nor a device tensor that is dense or has
+// the rows of `rows`.
+bool pointer_of(PyObject* o, void** out, const convbn_qdesc* rows = nullptr) {
   if (o == Py_None) { *out = nullptr; return true; }
   if (THPVariable_Check(o)) return guarded([&] {
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || !t.is_contiguous()) {
-      PyErr_SetString(PyExc_AssertionError, "device, dense tensors only");
+    if (!t.is_cuda() || !(t.is_contiguous() || has_rows_of(t, rows))) {
+      PyErr_SetString(PyExc_AssertionError, rows ? "device tensors only, dense or with the descriptor's row stride" : "device, dense tensors only");
       return false;
     }
     *out = t.data_ptr();
@@ -81,6 +90,8 @@ int dispatch(void* f, int n, void* const* p, bool* known, const void* d, T... ta
   switch (n) {
     case 3: return invoke(f, d, p[0], p[1], p[2], tail...);
     case 4: return invoke(f, d, P4, tail...);
+    case 6: return invoke(f, d, P4, p[4], p[5], tail...);
+    case 7: return invoke(f, d, P4, p[4], p[5], p[6], tail...);
     case 8: return invoke(f, d, P8, tail...);
     case 9: return invoke(f, d, P8, p[8], tail...);
     case 11: return invoke(f, d, P8, p[8], p[9], p[10], tail...);
@@ -99,6 +110,49 @@ int dispatch_groups(void* f, int n, void* const* p, bool* known, const void* d, 
   return 0;
 }
 
+// The descriptor's bytes for the length of a call.
+struct DescView {
+  Py_buffer b;
+  bool held = false;
+  bool get(PyObject* o, size_t size, const char* name) {
+    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) return false;
+    held = true;
+    if (b.len == (Py_ssize_t)size) return true;
+    PyErr_Format(PyExc_TypeError, "expected a %s", name);
+    return false;
+  }
+  ~DescView() { if (held) PyBuffer_Release(&b); }
+};
+
+// args: `n` tensors, ws, stream
+PyObject* call_with(void* f, const DescView& d, const convbn_qdesc* rows, bool has_groups, int groups, PyObject* const* args, Py_ssize_t n) {
+  void* p[kMaxPtr];
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (!pointer_of(args[i], &p[i], rows)) return nullptr;
+  PyObject* ws_o = args[n];
+  const bool has_ws = ws_o != g_no_ws;
+  void* ws = nullptr;
+  size_t ws_bytes = 0;
+  if (has_ws) {
+    if (!pointer_of(ws_o, &ws)) return nullptr;
+    if (THPVariable_Check(ws_o) && !guarded([&] { ws_bytes = THPVariable_Unpack(ws_o).nbytes(); return true; })) return nullptr;
+  }
+  void* stream = nullptr;
+  if (!stream_of(args[n + 1], &stream)) return nullptr;
+  bool known = true;
+  int st = 0;
+  Py_BEGIN_ALLOW_THREADS
+  if (has_groups) st = dispatch_groups(f, (int)n, p, &known, d.b.buf, groups, ws, ws_bytes, stream);
+  else if (has_ws) st = dispatch(f, (int)n, p, &known, d.b.buf, ws, ws_bytes, stream);
+  else st = dispatch(f, (int)n, p, &known, d.b.buf, stream);
+  Py_END_ALLOW_THREADS
+  if (!known) {
+    PyErr_SetString(PyExc_TypeError, "no entry point takes this number of tensors");
+    return nullptr;
+  }
+  return PyLong_FromLong(st);
+}
+
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const Py_ssize_t n = nargs - 5;   // tensors
   if (n < 1 || n > kMaxPtr) {
@@ -109,39 +163,22 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const bool has_groups = args[2] != Py_None;
   const long groups = has_groups ? PyLong_AsLong(args[2]) : 0;
   if (PyErr_Occurred()) return nullptr;
-  void* p[kMaxPtr];
-  for (Py_ssize_t i = 0; i < n; ++i)
-    if (!pointer_of(args[3 + i], &p[i])) return nullptr;
-  PyObject* ws_o = args[3 + n];
-  const bool has_ws = ws_o != g_no_ws;
-  void* ws = nullptr;
-  size_t ws_bytes = 0;
-  if (has_ws) {
-    if (!pointer_of(ws_o, &ws)) return nullptr;
-    if (THPVariable_Check(ws_o) && !guarded([&] { ws_bytes = THPVariable_Unpack(ws_o).nbytes(); return true; })) return nullptr;
-  }
-  void* stream = nullptr;
-  if (!stream_of(args[4 + n], &stream)) return nullptr;
-  Py_buffer d;
-  if (PyObject_GetBuffer(args[1], &d, PyBUF_SIMPLE) != 0) return nullptr;
-  if (d.len != (Py_ssize_t)sizeof(convbn_desc)) {
-    PyBuffer_Release(&d);
-    PyErr_SetString(PyExc_TypeError, "expected a convbn_desc");
+  DescView d;
+  if (!d.get(args[1], sizeof(convbn_desc), "convbn_desc")) return nullptr;
+  return call_with(f, d, nullptr, has_groups, (int)groups, args + 3, n);
+}
+
+PyObject* call_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  const Py_ssize_t n = nargs - 4;
+  if (n < 1 || n > kMaxPtr) {
+    PyErr_SetString(PyExc_TypeError, "call_rows(address, desc, tensors..., ws, stream)");
     return nullptr;
   }
-  bool known = true;
-  int st = 0;
-  Py_BEGIN_ALLOW_THREADS
-  if (has_groups) st = dispatch_groups(f, (int)n, p, &known, d.buf, (int)groups, ws, ws_bytes, stream);
-  else if (has_ws) st = dispatch(f, (int)n, p, &known, d.buf, ws, ws_bytes, stream);
-  else st = dispatch(f, (int)n, p, &known, d.buf, stream);
-  Py_END_ALLOW_THREADS
-  PyBuffer_Release(&d);
-  if (!known) {
-    PyErr_SetString(PyExc_TypeError, "no entry point takes this number of tensors");
-    return nullptr;
-  }
-  return PyLong_FromLong(st);
+  void* f = PyLong_AsVoidPtr(args[0]);
+  if (PyErr_Occurred()) return nullptr;
+  DescView d;
+  if (!d.get(args[1], sizeof(convbn_qdesc), "convbn_qdesc")) return nullptr;
+  return call_with(f, d, static_cast<const convbn_qdesc*>(d.b.buf), false, 0, args + 2, n);
 }
 
 // pointer(tensor) -> address or None, stream(None or handle) -> handle: for the entry points that take no descriptor.
@@ -159,6 +196,7 @@ PyObject* stream(PyObject*, PyObject* o) {
 
 PyMethodDef methods[] = {
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL, nullptr},
+    {"call_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call_rows)), METH_FASTCALL, nullptr},
     {"pointer", pointer, METH_O, nullptr},
     {"stream", stream, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,369 @@
+// Rows in 8 bits: packing, reading back, and the gate between two products with its backward pass.
+//
+// A row is taken by a group of LPR lanes (a part of a wave, a wave, or the workgroup), each holding VPL pieces of 8 channels in
+// registers from the one read of the row to the store of its codes: the maximum has to be known before the first code is.  Rows that
+// are too long for that (VPL = 0) are read twice, the second time from the caches.  All of it is bound by memory.
+#include "quant.h"
+
+namespace convbn {
+
+namespace {
+
+constexpr int NT = 256;
+constexpr float TINY = 1.504632769e-36f;   // 2^-119: below, 127 / a and a / 127 leave the normal range; the row counts as zeros
+constexpr unsigned ABS = 0x7fffffffu, INF = 0x7f800000u;
+
+struct F8 { float v[8]; };
+
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16_t> { uint4 a; };
+template <> struct Raw8<float> { uint4 a, b; };
+
+__device__ __forceinline__ F8 widen(const Raw8<bf16_t>& r) {
+  return {{bf16_lo(r.a.x), bf16_hi(r.a.x), bf16_lo(r.a.y), bf16_hi(r.a.y), bf16_lo(r.a.z), bf16_hi(r.a.z), bf16_lo(r.a.w), bf16_hi(r.a.w)}};
+}
+__device__ __forceinline__ F8 widen(const Raw8<float>& r) {
+  return {{__uint_as_float(r.a.x), __uint_as_float(r.a.y), __uint_as_float(r.a.z), __uint_as_float(r.a.w), __uint_as_float(r.b.x),
+           __uint_as_float(r.b.y), __uint_as_float(r.b.z), __uint_as_float(r.b.w)}};
+}
+
+// Channels k .. k+7 of a row of K (zeros past the end).  AL: every row starts on 16 bytes.
+template <typename T, bool AL> __device__ __forceinline__ F8 load8(const T* __restrict__ row, int k, int K) {
+  if (AL && k + 8 <= K) {
+    const Raw8<T> r = *reinterpret_cast<const Raw8<T>*>(row + k);
+    return widen(r);
+  }
+  F8 f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.v[i] = k + i < K ? to_f32(row[k + i]) : 0.f;
+  return f;
+}
+template <typename T, bool AL> __device__ __forceinline__ void store8(T* __restrict__ row, int k, int K, const F8& f) {
+  if (AL && k + 8 <= K) {
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4*>(row + k) = make_uint4(pack_bf16x2(f.v[0], f.v[1]), pack_bf16x2(f.v[2], f.v[3]),
+                                                      pack_bf16x2(f.v[4], f.v[5]), pack_bf16x2(f.v[6], f.v[7]));
+    } else {
+      float4* p = reinterpret_cast<float4*>(row + k);
+      p[0] = make_float4(f.v[0], f.v[1], f.v[2], f.v[3]);
+      p[1] = make_float4(f.v[4], f.v[5], f.v[6], f.v[7]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (k + i < K) row[k + i] = from_f32<T>(f.v[i]);
+}
+
+__device__ __forceinline__ unsigned amax8(const F8& f) {   // (compared as whole numbers: a NaN is the largest of all)
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f.v[i]) & ABS);
+  return m;
+}
+
+// Scale and 127 / a of a row from its maximum's bits
+struct Scale { float s, r; };
+__device__ __forceinline__ Scale scale_of(unsigned bits) {
+  if (bits >= INF) return {__uint_as_float(0x7fc00000u), 0.f};
+  const float a = __uint_as_float(bits);
+  if (a < TINY) return {0.f, 0.f};
+  float s = a / 127.f;
+  if (s * 127.f >= INFINITY) s = __uint_as_float(__float_as_uint(s) - 1);   // (rounded up at the very top: a row's maximum reads back finite)
+  return {s, 127.f / a};
+}
+
+// 8 codes: adding 1.5 * 2^23 to |v| <= 127.0001 rounds it to a whole number, ties to even, and leaves it in the low byte.  The
+// product is rounded before that (the definition): no fused multiply-add here.
+__device__ __forceinline__ uint2 codes8(const F8& f, float r) {
+#pragma clang fp contract(off)
+  unsigned q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = f.v[i] * r;
+    q[i] = __float_as_uint(v + 12582912.f);
+  }
+  if (r == 0.f) return make_uint2(0, 0);
+  auto four = [](unsigned a, unsigned b, unsigned c, unsigned d) {
+    return (a & 255u) | (b & 255u) << 8 | (c & 255u) << 16 | d << 24;
+  };
+  return make_uint2(four(q[0], q[1], q[2], q[3]), four(q[4], q[5], q[6], q[7]));
+}
+__device__ __forceinline__ F8 decode8(uint2 c, float s) {
+  F8 f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f.v[i] = (float)(int8_t)(c.x >> (8 * i)) * s;
+    f.v[4 + i] = (float)(int8_t)(c.y >> (8 * i)) * s;
+  }
+  return f;
+}
+
+// Maximum over the LPR lanes of a row (all of them call this together).
+template <int LPR> __device__ __forceinline__ unsigned group_max(unsigned m, unsigned* lds) {
+#pragma unroll
+  for (int off = (LPR < 64 ? LPR : 64) / 2; off > 0; off >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, off, 64));
+  if constexpr (LPR > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) m = max(m, lds[w]);
+    __syncthreads();   // (the next row's maxima go to the same place)
+  }
+  return m;
+}
+
+// f(g) and f'(g)
+template <int KIND> __device__ __forceinline__ void gate_of(float g, float* f, float* df) {
+  if constexpr (KIND == CONVBN_GATE_SILU) {
+    const float p = 1.f / (1.f + expf(-g));
+    *f = g * p;
+    *df = p * (1.f + g * (1.f - p));
+  } else {
+    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+    *f = g * p;
+    *df = p + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+  }
+}
+
+struct RowArgs { i64 rows, ld; int K; const void* x; void* out; uint8_t* codes; float* scales; };
+
+template <typename T, int LPR, int VPL, bool AL>
+__global__ __launch_bounds__(NT) void qpack_kernel(RowArgs p) {
+  __shared__ unsigned lds[NT / 64];
+  constexpr int RPB = NT / LPR;
+  const int lane = threadIdx.x % LPR, row0 = threadIdx.x / LPR;
+  const int K = p.K, Kp = qrow(K);
+  for (i64 b = blockIdx.x; b * RPB < p.rows; b += gridDim.x) {   // (whole groups: every lane reaches group_max)
+    const i64 row = b * RPB + row0;
+    const bool in = row < p.rows;
+    const T* x = static_cast<const T*>(p.x) + (in ? row : 0) * p.ld;
+    uint8_t* codes = p.codes + (in ? row : 0) * Kp;
+    F8 f[VPL ? VPL : 1];
+    unsigned m = 0;
+    if constexpr (VPL > 0) {
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) f[v] = load8<T, AL>(x, (v * LPR + lane) * 8, in ? K : 0);
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) m = max(m, amax8(f[v]));
+    } else {
+      for (int k = lane * 8; k < K; k += LPR * 8) m = max(m, amax8(load8<T, AL>(x, k, K)));
+    }
+    const Scale sc = scale_of(group_max<LPR>(m, lds));
+    if (!in) continue;
+    if (lane == 0) p.scales[row] = sc.s;
+    if constexpr (VPL > 0) {
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        const int k = (v * LPR + lane) * 8;
+        if (k < Kp) *reinterpret_cast<uint2*>(codes + k) = codes8(f[v], sc.r);
+      }
+    } else {
+      for (int k = lane * 8; k < Kp; k += LPR * 8) *reinterpret_cast<uint2*>(codes + k) = codes8(load8<T, AL>(x, k, K), sc.r);
+    }
+  }
+}
+
+template <typename T, bool AL>
+__global__ __launch_bounds__(NT) void qunpack_kernel(RowArgs p, unsigned pieces) {
+  const int K = p.K, Kp = qrow(K);
+  const i64 total = p.rows * pieces;
+  for (i64 i = (i64)blockIdx.x * NT + threadIdx.x; i < total; i += (i64)gridDim.x * NT) {
+    const i64 row = i / pieces;
+    const int k = (int)(i - row * pieces) * 8;
+    const uint2 c = *reinterpret_cast<const uint2*>(p.codes + row * Kp + k);
+    store8<T, AL>(static_cast<T*>(p.out) + row * p.ld, k, K, decode8(c, p.scales[row]));
+  }
+}
+
+struct GateArgs {
+  i64 rows, ldh, ldy;
+  int K;
+  const void* h; void* y; uint8_t* hc; float* hs; uint8_t* yc; float* ys;   // forward
+  const void* dy; void* dh;                                                  // backward
+};
+
+template <typename T, int KIND, int LPR, int VPL, bool AL>
+__global__ __launch_bounds__(NT) void qgate_fwd_kernel(GateArgs p) {
+  __shared__ unsigned lds[NT / 64];
+  constexpr int RPB = NT / LPR, NV = VPL ? VPL : 1;
+  const int lane = threadIdx.x % LPR, row0 = threadIdx.x / LPR;
+  const int K = p.K, Kp = qrow(K);
+  for (i64 b = blockIdx.x; b * RPB < p.rows; b += gridDim.x) {
+    const i64 row = b * RPB + row0;
+    const bool in = row < p.rows;
+    const i64 at = in ? row : 0;
+    const T* h = static_cast<const T*>(p.h) + at * p.ldh;
+    auto make = [](const F8& g, const F8& u) {
+      F8 y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float f, df;
+        gate_of<KIND>(g.v[i], &f, &df);
+        y.v[i] = f * u.v[i];
+      }
+      return y;
+    };
+    F8 g[NV], u[NV], y[NV];
+    unsigned mg = 0, mu = 0, my = 0;
+    auto look = [&](const F8& a, const F8& b2, const F8& c) {
+      mg = max(mg, amax8(a)); mu = max(mu, amax8(b2)); my = max(my, amax8(c));
+    };
+    if constexpr (VPL > 0) {
+      const int Kin = in ? K : 0;
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        g[v] = load8<T, AL>(h, (v * LPR + lane) * 8, Kin);
+        u[v] = load8<T, AL>(h + K, (v * LPR + lane) * 8, Kin);
+      }
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        y[v] = make(g[v], u[v]);
+        look(g[v], u[v], y[v]);
+      }
+    } else {
+      for (int k = lane * 8; k < K; k += LPR * 8) {
+        g[0] = load8<T, AL>(h, k, K);
+        u[0] = load8<T, AL>(h + K, k, K);
+        look(g[0], u[0], make(g[0], u[0]));
+      }
+    }
+    Scale sg = {0, 0}, su = {0, 0}, sy = {0, 0};
+    if (p.hc) { sg = scale_of(group_max<LPR>(mg, lds)); su = scale_of(group_max<LPR>(mu, lds)); }
+    if (p.yc) sy = scale_of(group_max<LPR>(my, lds));
+    if (!in) continue;
+    if (lane == 0) {
+      if (p.hc) { p.hs[2 * row] = sg.s; p.hs[2 * row + 1] = su.s; }
+      if (p.yc) p.ys[row] = sy.s;
+    }
+    auto out = [&](int k, const F8& a, const F8& b2, const F8& c) {
+      if (k >= Kp) return;
+      if (p.hc) {
+        *reinterpret_cast<uint2*>(p.hc + 2 * row * Kp + k) = codes8(a, sg.r);
+        *reinterpret_cast<uint2*>(p.hc + (2 * row + 1) * Kp + k) = codes8(b2, su.r);
+      }
+      if (p.yc) *reinterpret_cast<uint2*>(p.yc + row * Kp + k) = codes8(c, sy.r);
+      if (p.y) store8<T, AL>(static_cast<T*>(p.y) + row * p.ldy, k, K, c);
+    };
+    if constexpr (VPL > 0) {
+#pragma unroll
+      for (int v = 0; v < VPL; ++v) out((v * LPR + lane) * 8, g[v], u[v], y[v]);
+    } else {
+      for (int k = lane * 8; k < Kp; k += LPR * 8) {
+        g[0] = load8<T, AL>(h, k, K);
+        u[0] = load8<T, AL>(h + K, k, K);
+        out(k, g[0], u[0], make(g[0], u[0]));
+      }
+    }
+  }
+}
+
+template <typename T, int KIND, bool AL>
+__global__ __launch_bounds__(NT) void qgate_bwd_kernel(GateArgs p, unsigned pieces) {
+  const int K = p.K, Kp = qrow(K);
+  const i64 total = p.rows * pieces;
+  for (i64 i = (i64)blockIdx.x * NT + threadIdx.x; i < total; i += (i64)gridDim.x * NT) {
+    const i64 row = i / pieces;
+    const int k = (int)(i - row * pieces) * 8;
+    const F8 g = decode8(*reinterpret_cast<const uint2*>(p.hc + 2 * row * Kp + k), p.hs[2 * row]);
+    const F8 u = decode8(*reinterpret_cast<const uint2*>(p.hc + (2 * row + 1) * Kp + k), p.hs[2 * row + 1]);
+    const F8 dy = load8<T, AL>(static_cast<const T*>(p.dy) + row * p.ldy, k, K);
+    F8 dg, du;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float f, df;
+      gate_of<KIND>(g.v[e], &f, &df);
+      dg.v[e] = dy.v[e] * u.v[e] * df;
+      du.v[e] = dy.v[e] * f;
+    }
+    T* dh = static_cast<T*>(p.dh) + row * p.ldh;
+    store8<T, AL>(dh, k, K, dg);
+    store8<T, AL>(dh + K, k, K, du);
+  }
+}
+
+bool aligned16(const void* p, i64 bytes_apart) { return ((uintptr_t)p | (uintptr_t)bytes_apart) % 16 == 0; }
+
+int blocks_of(i64 work) { return (int)(work < 1 << 20 ? work : 1 << 20); }   // (launches stay below 2^32 threads)
+
+}  // namespace
+
+// Calls f(LPR, VPL) with the narrowest group that holds a row of K channels.
+template <class F> static hipError_t by_row_length(int K, F&& f) {
+  const int pieces = ceil_div(K, 8);
+  using std::integral_constant;
+#define QROW(LPR, VPL) \
+  if (pieces <= (LPR) * (VPL)) return f(integral_constant<int, LPR>{}, integral_constant<int, VPL>{})
+  QROW(8, 1); QROW(16, 1); QROW(32, 1); QROW(64, 1); QROW(64, 2); QROW(256, 1); QROW(256, 2); QROW(256, 4);
+#undef QROW
+  return f(integral_constant<int, 256>{}, integral_constant<int, 0>{});
+}
+
+template <typename T> static hipError_t pack_t(const RowArgs& a, bool al, hipStream_t st) {
+  return by_row_length(a.K, [&](auto lpr, auto vpl) {
+    const int grid = blocks_of((a.rows + NT / lpr.value - 1) / (NT / lpr.value));
+    if (al) qpack_kernel<T, lpr.value, vpl.value, true><<<grid, NT, 0, st>>>(a);
+    else qpack_kernel<T, lpr.value, vpl.value, false><<<grid, NT, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_qpack(int dtype, i64 rows, int K, i64 ld, const void* x, void* codes, float* scales, hipStream_t st) {
+  if (!rows) return hipSuccess;
+  const RowArgs a = {rows, ld, K, x, nullptr, (uint8_t*)codes, scales};
+  if (dtype == CONVBN_BF16) return pack_t<bf16_t>(a, aligned16(x, ld * 2), st);
+  return pack_t<float>(a, aligned16(x, ld * 4), st);
+}
+
+hipError_t launch_qunpack(int dtype, i64 rows, int K, i64 ld, const void* codes, const float* scales, void* x, hipStream_t st) {
+  if (!rows) return hipSuccess;
+  const RowArgs a = {rows, ld, K, nullptr, x, (uint8_t*)codes, (float*)scales};
+  const unsigned pieces = ceil_div(K, 8);
+  const int grid = blocks_of((rows * pieces + NT - 1) / NT);
+  const bool al = aligned16(x, ld * (dtype == CONVBN_BF16 ? 2 : 4));
+  if (dtype == CONVBN_BF16 && al) qunpack_kernel<bf16_t, true><<<grid, NT, 0, st>>>(a, pieces);
+  else if (dtype == CONVBN_BF16) qunpack_kernel<bf16_t, false><<<grid, NT, 0, st>>>(a, pieces);
+  else if (al) qunpack_kernel<float, true><<<grid, NT, 0, st>>>(a, pieces);
+  else qunpack_kernel<float, false><<<grid, NT, 0, st>>>(a, pieces);
+  return hipGetLastError();
+}
+
+template <typename T, int KIND, bool AL> static hipError_t gate_fwd_t(const GateArgs& a, hipStream_t st) {
+  return by_row_length(a.K, [&](auto lpr, auto vpl) {
+    const int grid = blocks_of((a.rows + NT / lpr.value - 1) / (NT / lpr.value));
+    qgate_fwd_kernel<T, KIND, lpr.value, vpl.value, AL><<<grid, NT, 0, st>>>(a);
+    return hipGetLastError();
+  });
+}
+template <typename T, int KIND, bool AL> static hipError_t gate_bwd_t(const GateArgs& a, hipStream_t st) {
+  const unsigned pieces = ceil_div(a.K, 8);
+  qgate_bwd_kernel<T, KIND, AL><<<blocks_of((a.rows * pieces + NT - 1) / NT), NT, 0, st>>>(a, pieces);
+  return hipGetLastError();
+}
+// Calls f(T, KIND, AL) with the gate's types; al: every row it touches starts on 16 bytes
+template <class F> static hipError_t by_gate(int dtype, int kind, bool al, F&& f) {
+  auto with = [&](auto t) {
+    if (kind == CONVBN_GATE_SILU) return al ? f(t, std::integral_constant<int, 0>{}, std::true_type{}) : f(t, std::integral_constant<int, 0>{}, std::false_type{});
+    return al ? f(t, std::integral_constant<int, 1>{}, std::true_type{}) : f(t, std::integral_constant<int, 1>{}, std::false_type{});
+  };
+  return dtype == CONVBN_BF16 ? with(bf16_t{}) : with(float{});
+}
+
+hipError_t launch_qgate_fwd(int dtype, int kind, i64 rows, int K, i64 ldh, i64 ldy, const void* h, void* h_codes, float* h_scales,
+                            void* y, void* y_codes, float* y_scales, hipStream_t st) {
+  if (!rows) return hipSuccess;
+  GateArgs a = {rows, ldh, ldy, K, h, y, (uint8_t*)h_codes, h_scales, (uint8_t*)y_codes, y_scales, nullptr, nullptr};
+  const i64 e = dtype == CONVBN_BF16 ? 2 : 4;
+  const bool al = aligned16(h, ldh * e) && K * e % 16 == 0 && (!y || aligned16(y, ldy * e));
+  return by_gate(dtype, kind, al, [&](auto t, auto k, auto v) { return gate_fwd_t<decltype(t), k.value, v.value>(a, st); });
+}
+hipError_t launch_qgate_bwd(int dtype, int kind, i64 rows, int K, i64 ldh, i64 ldy, const void* h_codes, const float* h_scales,
+                            const void* dy, void* dh, hipStream_t st) {
+  if (!rows) return hipSuccess;
+  GateArgs a = {rows, ldh, ldy, K, nullptr, nullptr, (uint8_t*)h_codes, (float*)h_scales, nullptr, nullptr, dy, dh};
+  const i64 e = dtype == CONVBN_BF16 ? 2 : 4;
+  const bool al = aligned16(dh, ldh * e) && K * e % 16 == 0 && aligned16(dy, ldy * e);
+  return by_gate(dtype, kind, al, [&](auto t, auto k, auto v) { return gate_bwd_t<decltype(t), k.value, v.value>(a, st); });
+}
+
+}  // namespace convbn

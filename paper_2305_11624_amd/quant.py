@@ -1,0 +1,217 @@
+"""The 8-bit rows for a PyTorch program: an activation kept in 8 bits, a Linear block on integer products that keeps its input
+that way, the gate between two of them, and the gated block that they make up.
+
+Each object holds the codes, scales, outputs and workspace of one layer, allocated once; its calls enqueue on the current
+stream (or the one they are given) and allocate nothing.  What they return are the object's own buffers, overwritten by the
+next call.  Arguments are checked before anything is launched.
+"""
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+_DTYPES = {torch.bfloat16: B.BF16, torch.float32: B.F32}
+_GATES = {"silu": B.GATE_SILU, "gelu": B.GATE_GELU}
+
+
+def _dtype(dt):
+    if dt not in _DTYPES:
+        raise TypeError(f"{dt}: bfloat16 or float32")
+    return _DTYPES[dt]
+
+
+def _rows(t: torch.Tensor, M: int, width: int, dt, ld: int, name: str):
+    if t.dtype is not dt or t.dim() != 2 or t.shape[0] != M or t.shape[1] != width:
+        raise ValueError(f"{name}: expected {dt} [{M}, {width}], got {t.dtype} {list(t.shape)}")
+    if M > 1 and t.stride(0) != ld or t.stride(1) != 1 and width > 1:
+        raise ValueError(f"{name}: expected rows {ld} elements apart, got strides {t.stride()}")
+    return t
+
+
+def _vector(t: Optional[torch.Tensor], n: int, name: str):
+    if t is not None and (t.dtype is not torch.float32 or t.numel() != n):
+        raise ValueError(f"{name}: expected float32 [{n}], got {t.dtype} {list(t.shape)}")
+    return t
+
+
+def _codes(t: torch.Tensor, rows: int, K: int, name: str):
+    if t.element_size() != 1 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != B.convbn_qrow_bytes(K):
+        raise ValueError(f"{name}: expected bytes [{rows}, {B.convbn_qrow_bytes(K)}], got {t.dtype} {list(t.shape)}")
+    return t
+
+
+def _new_rows(M, width, ld, dt, device):
+    return torch.empty(M, ld, dtype=dt, device=device)[:, :width]
+
+
+def new_codes(rows: int, K: int, device="cuda"):
+    """Buffers for `rows` packed rows of K channels: (codes, scales)."""
+    return (torch.empty(rows, B.convbn_qrow_bytes(K), dtype=torch.int8, device=device),
+            torch.empty(rows, dtype=torch.float32, device=device))
+
+
+class Checkpoint:
+    """[M, K] rows kept in 8 bits between a block's forward and its backward (a channels-last activation is [pixels,
+    channels]): 1 byte a value and 4 a row in place of 2 or 4 a value."""
+
+    def __init__(self, M: int, K: int, dtype=torch.bfloat16, device="cuda"):
+        self.M, self.K, self.dtype = M, K, dtype
+        self.desc = B.make_qdesc(M, K, dtype=_dtype(dtype))
+        self.codes, self.scales = new_codes(M, K, device)
+        self.out = None
+
+    def pack(self, x: torch.Tensor, stream=None):
+        self.desc.ldx = ld = x.stride(0) if self.M > 1 else self.K
+        B.convbn_qpack(self.desc, _rows(x, self.M, self.K, self.dtype, ld, "x"), self.codes, self.scales, stream)
+
+    def unpack(self, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        if out is None:
+            if self.out is None:
+                self.out = torch.empty(self.M, self.K, dtype=self.dtype, device=self.codes.device)
+            out = self.out
+        self.desc.ldx = ld = out.stride(0) if self.M > 1 else self.K
+        B.convbn_qunpack(self.desc, self.codes, self.scales, _rows(out, self.M, self.K, self.dtype, ld, "out"), stream)
+        return out
+
+    def saved_bytes(self) -> int:
+        return self.codes.numel() + 4 * self.M
+
+
+class Linear:
+    """z = x w^T + b on M rows: x and w in 8 bits with a scale for each row of x and each output channel, integer sums.
+
+    train: the codes of x are kept for `backward`, which works from them (x itself may be dropped after `forward`).
+    gap: x, dx, z and dz are rows of buffers with `gap` elements between the rows."""
+
+    def __init__(self, M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0, device="cuda"):
+        self.M, self.K, self.N, self.dtype, self.train = M, K, N, dtype, train
+        self.ldx, self.ldz = K + gap, N + gap
+        self.desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)
+        self.codes, self.scales = new_codes(M, K, device) if train else (None, None)
+        self.w_codes = self.w_scales = None
+        self._w_desc = B.make_qdesc(N, K, dtype=_dtype(dtype))
+        self.z = _new_rows(M, N, self.ldz, dtype, device)
+        self.dx = _new_rows(M, K, self.ldx, dtype, device) if train else None
+        self.dW = torch.empty(N, K, dtype=dtype, device=device) if train else None
+        self.db = torch.empty(N, dtype=torch.float32, device=device) if train else None
+        need = B.convbn_qlinear_workspace_bytes(self.desc, B.PASS_FWD) if not train else 0
+        if train:
+            need = max(need, B.convbn_qlinear_workspace_bytes(self.desc, B.PASS_BWD))
+        self.ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+    def set_weight(self, codes: torch.Tensor, scales: torch.Tensor):
+        """A weight that is packed already (`new_codes(N, K)`, `convbn_qpack`): kept, not copied."""
+        self.w_codes, self.w_scales = _codes(codes, self.N, self.K, "codes"), _vector(scales, self.N, "scales")
+
+    def pack_weight(self, W: torch.Tensor, stream=None):
+        """Pack W [N, K] by output channel."""
+        if self.w_codes is None:
+            self.w_codes, self.w_scales = new_codes(self.N, self.K, W.device)
+        B.convbn_qpack(self._w_desc, _rows(W, self.N, self.K, self.dtype, self.K, "W"), self.w_codes, self.w_scales, stream)
+
+    def _weight(self):
+        if self.w_codes is None:
+            raise RuntimeError("no weight: call pack_weight or set_weight first")
+        return self.w_codes, self.w_scales
+
+    def _add(self, bit: int, field: str, add, width: int, ld: int):
+        d = self.desc
+        d.act = 0 if add is None else bit
+        setattr(d, field, None if add is None else _rows(add, self.M, width, self.dtype, ld, "add").data_ptr())
+
+    def forward(self, x: torch.Tensor, b: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None, stream=None):
+        """z = x w^T + b (+ add)."""
+        w, ws = self._weight()
+        _rows(x, self.M, self.K, self.dtype, self.ldx, "x")
+        self._add(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
+        B.convbn_qlinear_fwd(self.desc, x, self.codes, self.scales, w, ws, _vector(b, self.N, "b"), self.z, self.ws, stream)
+        return self.z
+
+    def forward_packed(self, codes: torch.Tensor, scales: torch.Tensor, b: Optional[torch.Tensor] = None,
+                       add: Optional[torch.Tensor] = None, stream=None):
+        """The same for rows that are packed already; with `train` they are what `backward` reads, so keep them until then."""
+        w, ws = self._weight()
+        _codes(codes, self.M, self.K, "codes")
+        _vector(scales, self.M, "scales")
+        self._add(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
+        if self.train:
+            self.codes, self.scales = codes, scales
+        B.convbn_qlinear_fwd(self.desc, None, codes, scales, w, ws, _vector(b, self.N, "b"), self.z, self.ws, stream)
+        return self.z
+
+    def backward(self, dz: torch.Tensor, need_dx: bool = True, need_dW: bool = True, bias: bool = False,
+                 add: Optional[torch.Tensor] = None, stream=None):
+        """(dx (+ add), dW, db) from the kept codes; None for what is not asked for."""
+        if not self.train:
+            raise RuntimeError("this layer keeps no codes (train=False)")
+        w, ws = self._weight()
+        _rows(dz, self.M, self.N, self.dtype, self.ldz, "dz")
+        self._add(B.ACT_ADD_IN, "add_in", add, self.K, self.ldx)
+        dx, dW, db = self.dx if need_dx else None, self.dW if need_dW else None, self.db if bias else None
+        B.convbn_qlinear_bwd(self.desc, self.codes, self.scales, w, ws, dz, dx, dW, db, self.ws, stream)
+        return dx, dW, db
+
+    def saved_bytes(self) -> int:
+        """What stays alive between forward and backward."""
+        return self.codes.numel() + 4 * self.M if self.train else 0
+
+
+class Gate:
+    """y = f(g) u for rows h = [g | u] of 2 K channels, f = "silu" or "gelu".
+
+    train: the codes of g and u are kept for `backward`.  packed: y comes as codes and scales (`codes_y`, `scales_y`), the form that the
+    next Linear takes, and not as a tensor.  gap: as in Linear."""
+
+    def __init__(self, M: int, K: int, dtype=torch.bfloat16, kind: str = "silu", train: bool = True, packed: bool = False, gap: int = 0,
+                 device="cuda"):
+        self.M, self.K, self.dtype = M, K, dtype
+        self.ldh, self.ldy = 2 * K + gap, K + gap
+        self.desc = B.make_qdesc(M, K, dtype=_dtype(dtype), ldx=self.ldh, ldz=self.ldy, gate=_GATES[kind])
+        self.codes, self.scales = new_codes(2 * M, K, device) if train else (None, None)
+        self.codes_y, self.scales_y = new_codes(M, K, device) if packed else (None, None)
+        self.y = None if packed else _new_rows(M, K, self.ldy, dtype, device)
+        self.dh = _new_rows(M, 2 * K, self.ldh, dtype, device) if train else None
+
+    def forward(self, h: torch.Tensor, stream=None):
+        _rows(h, self.M, 2 * self.K, self.dtype, self.ldh, "h")
+        B.convbn_qgate_fwd(self.desc, h, self.codes, self.scales, self.y, self.codes_y, self.scales_y, stream)
+        return self.y
+
+    def backward(self, dy: torch.Tensor, stream=None):
+        if self.codes is None:
+            raise RuntimeError("this gate keeps no codes (train=False)")
+        _rows(dy, self.M, self.K, self.dtype, self.ldy, "dy")
+        B.convbn_qgate_bwd(self.desc, self.codes, self.scales, dy, self.dh, stream)
+        return self.dh
+
+    def saved_bytes(self) -> int:
+        return 0 if self.codes is None else self.codes.numel() + 8 * self.M
+
+
+class GatedBlock:
+    """out = x + down(f(up_g(x)) up_u(x)): the gated two-layer block on M rows of C channels with F hidden ones, on a backbone's last
+    feature map (rows = pixels) or a token stream.  Between forward and backward it keeps x, h and y in 8 bits only."""
+
+    def __init__(self, M: int, C: int, F: int, dtype=torch.bfloat16, kind: str = "silu", train: bool = True, device="cuda"):
+        self.up = Linear(M, C, 2 * F, dtype, train, device=device)
+        self.gate = Gate(M, F, dtype, kind, train, packed=True, device=device)
+        self.down = Linear(M, F, C, dtype, train, device=device)
+
+    def pack_weights(self, W_up: torch.Tensor, W_down: torch.Tensor, stream=None):
+        """W_up [2 F, C] (g's rows before u's), W_down [C, F]: once for serving, every step in training."""
+        self.up.pack_weight(W_up, stream)
+        self.down.pack_weight(W_down, stream)
+
+    def forward(self, x: torch.Tensor, stream=None):
+        self.gate.forward(self.up.forward(x, stream=stream), stream)
+        return self.down.forward_packed(self.gate.codes_y, self.gate.scales_y, add=x, stream=stream)
+
+    def backward(self, dout: torch.Tensor, stream=None):
+        """(dx, dW_up, dW_down)."""
+        dy, dW_down, _ = self.down.backward(dout, stream=stream)
+        dx, dW_up, _ = self.up.backward(self.gate.backward(dy, stream), add=dout, stream=stream)
+        return dx, dW_up, dW_down
+
+    def saved_bytes(self) -> int:
+        return self.up.saved_bytes() + self.gate.saved_bytes() + self.down.saved_bytes()

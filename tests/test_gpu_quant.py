@@ -1,0 +1,437 @@
+"""The 8-bit rows on the GPU against plain implementations in 64 bits.
+
+Two kinds of comparison.  Exact: where the values are small whole numbers (rows whose maximum is 127, so that the scale is 1) every sum
+fits 24 bits, and the result has to be the exact one, rounded once.  Bounded: elsewhere an output may be off by what the stated roundings
+allow, element by element: with u = 2^-24 and R summed terms t, (R + 8) u sum |t| for the sums and scales, 2^-8 |result| for a bf16
+result, and in the bf16 gradients 2^-8 sum |t| for the rounding of s q."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2305_11624_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U, H = 2.0 ** -24, 2.0 ** -8
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _q():
+    from paper_2305_11624_amd import quant
+    return quant
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _rows(x, gap, dt):
+    """x on the device, as rows of a buffer with `gap` poisoned elements behind each."""
+    buf = torch.full((x.shape[0], x.shape[1] + gap), float("nan"), dtype=dt, device="cuda")
+    buf[:, :x.shape[1]] = x.to("cuda", dt)
+    return buf[:, :x.shape[1]]
+
+
+def _np(t):
+    return t.detach().to("cpu", torch.float64).numpy()
+
+
+def _pack_ref(x32):
+    """Codes and scales by the definition, in numpy's fp32; NaN rows where a value is not finite."""
+    x = np.asarray(x32, dtype=np.float32)
+    a = np.abs(x).max(axis=1) if x.shape[0] else np.zeros(0, np.float32)
+    bad = ~np.isfinite(x).all(axis=1)
+    live = ~bad & (a >= np.float32(2.0 ** -119))
+    s, r = np.zeros_like(a), np.zeros_like(a)
+    s[live] = a[live] / np.float32(127)
+    r[live] = np.float32(127) / a[live]
+    with np.errstate(over="ignore"):
+        s = np.where(live & ~np.isfinite(s * np.float32(127)), np.nextafter(s, np.float32(0)), s)
+    s[bad] = np.nan
+    q = np.where(live[:, None], np.rint(np.where(live[:, None], x, 0) * r[:, None]), 0).astype(np.int8)
+    return q, s
+
+
+def _activations(M, K, dt, seed):
+    x = torch.randn(M, K, generator=_gen(seed))
+    x[:, ::17] *= 9
+    if M > 2:
+        x[M // 2] = 0
+    return x.to(dt).float()
+
+
+SIZES = [(1, 1), (2, 7), (3, 16), (5, 65), (33, 72), (7, 128), (4, 255), (9, 256), (3, 513), (2, 1000), (2, 1024), (3, 2048), (2, 2056),
+         (2, 4096), (3, 4100), (2, 8192), (1, 8200), (2, 20001), (1300, 24)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gap", [0, 8, 5])
+@pytest.mark.parametrize("M,K", SIZES)
+def test_pack_and_unpack(M, K, gap, dtype):
+    Q, dt = _q(), DT[dtype]
+    x = _activations(M, K, dt, M * 1000 + K)
+    ck = Q.Checkpoint(M, K, dt)
+    ck.codes.fill_(77)
+    ck.scales.fill_(float("nan"))
+    ck.pack(_rows(x, gap, dt))
+    q, s = _pack_ref(x)
+    assert np.array_equal(ck.codes.cpu().numpy()[:, :K], q) and (ck.codes.cpu().numpy()[:, K:] == 0).all()
+    assert np.array_equal(ck.scales.cpu().numpy(), s)
+    out = _rows(torch.zeros(M, K), gap, dt)
+    full = out.as_strided((M * out.stride(0) - gap,), (1,)) if M else out
+    ck.unpack(out)
+    want = torch.from_numpy(q.astype(np.float32) * s[:, None]).to(dt)      # one fp32 product, one rounding
+    assert torch.equal(out.cpu(), want)
+    if gap and M > 1:
+        assert torch.isnan(full.as_strided((M - 1, gap), (out.stride(0), 1), K)).all()      # nothing between the rows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [40, 3000, 9001])
+def test_pack_special_rows(dtype, K):
+    Q, dt = _q(), DT[dtype]
+    x = torch.randn(9, K, generator=_gen(5))
+    x[0] = 0
+    x[1] *= 2.0 ** -122                              # below the smallest row that is kept
+    x[2] *= 2.0 ** -110
+    x[3, K // 2] = float("inf")
+    x[4, K - 1] = float("nan")
+    x[5, 0] = torch.finfo(dt).max
+    x[6] = torch.arange(K) % 255 - 127               # every code, and halves below
+    x[7] = (torch.arange(K) % 254 - 127) + 0.5
+    x[7, 0] = 127
+    x[8, 1] = -torch.finfo(dt).max                   # a mask's lowest value
+    x = x.to(dt).float()
+    ck = Q.Checkpoint(9, K, dt)
+    ck.pack(x.to("cuda", dt))
+    q, s = _pack_ref(x)
+    assert np.array_equal(ck.codes.cpu().numpy()[:, :K], q)
+    assert np.array_equal(ck.scales.cpu().numpy(), s, equal_nan=True)
+    back = ck.unpack().float().cpu()
+    assert torch.isnan(back[3]).all() and torch.isnan(back[4]).all() and (back[0] == 0).all() and (back[1] == 0).all()
+    assert torch.isfinite(back[[2, 5, 6, 7, 8]]).all()
+
+
+def _whole(rows, K, seed, most=127):
+    """Whole numbers with a maximum of 127 in every row: packed exactly, with the scale 1."""
+    x = torch.randint(-most, most + 1, (rows, K), generator=_gen(seed)).float()
+    if rows:
+        x[torch.arange(rows), torch.arange(rows) % K] = 127
+    return x
+
+
+LINEAR = [(1, 64, 64), (1, 1, 1), (2, 16, 33), (5, 100, 72), (13, 1000, 24), (16, 512, 130), (17, 72, 16), (31, 40, 257), (33, 136, 72),
+          (64, 128, 64), (65, 2048, 48), (100, 264, 200), (129, 64, 129), (200, 33, 65), (257, 320, 256), (300, 1032, 128),
+          (513, 192, 520), (1100, 88, 40), (1568, 256, 64), (3000, 64, 264), (70, 64, 5000), (24, 5000, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gap", [0, 8, 5])
+@pytest.mark.parametrize("M,K,N", LINEAR)
+def test_linear_is_exact_on_whole_numbers(M, K, N, gap, dtype):
+    """Forward with and without kept codes, and all gradients, with the two addends; nothing outside the rows is written."""
+    Q, dt = _q(), DT[dtype]
+    x, W = _whole(M, K, 1), _whole(N, K, 2, 8)      # |sums| stay below 2^24: 127 * 8 * 5000 < 2^23, and rows that hold one 127
+    W[:, 0] = 0
+    W[torch.arange(N), torch.arange(N) % K] = 127
+    dz = torch.randint(-2, 3, (M, N), generator=_gen(3)).float()
+    b, add, add_in = torch.randint(-50, 51, (N,), generator=_gen(4)).float(), torch.randint(-9, 10, (M, N), generator=_gen(6)).float(), \
+        torch.randint(-9, 10, (M, K), generator=_gen(7)).float()
+    lin = Q.Linear(M, K, N, dt, train=True, gap=gap)
+    for t in (lin.z, lin.dx):
+        t.as_strided((t.shape[0] * t.stride(0) - gap,), (1,)).fill_(float("nan"))
+    lin.dW.fill_(float("nan"))
+    lin.db.fill_(float("nan"))
+    if lin.ws is not None:
+        lin.ws.fill_(255)
+    lin.pack_weight(W.to("cuda", dt))
+    z = lin.forward(_rows(x, gap, dt), b.cuda())
+    xd, wd = x.double(), W.double()
+    assert torch.equal(z.cpu(), (xd @ wd.t() + b).to(dt))
+    z = lin.forward(_rows(x, gap, dt), b.cuda(), add=_rows(add, gap, dt))
+    assert torch.equal(z.cpu(), (xd @ wd.t() + b + add).to(dt))
+    dzr = _rows(dz, gap, dt)
+    dx, dW, db = lin.backward(dzr, bias=True)
+    assert torch.equal(dx.cpu(), (dz.double() @ wd).to(dt))
+    assert torch.equal(dW.cpu(), (dz.double().t() @ xd).to(dt))
+    assert torch.equal(db.cpu(), dz.sum(0))
+    dx, _, _ = lin.backward(dzr, need_dW=False, add=_rows(add_in, gap, dt))
+    assert torch.equal(dx.cpu(), (dz.double() @ wd + add_in).to(dt))
+    if gap and M > 1:
+        for t in (lin.z, lin.dx):
+            assert torch.isnan(t.as_strided((M - 1, gap), (t.stride(0), 1), t.shape[1])).all()
+    serve = Q.Linear(M, K, N, dt, train=False, gap=gap)
+    serve.set_weight(lin.w_codes, lin.w_scales)
+    assert torch.equal(serve.forward(_rows(x, gap, dt), b.cuda()).cpu(), (xd @ wd.t() + b).to(dt))
+    assert torch.equal(serve.forward_packed(lin.codes, lin.scales).cpu(), (xd @ wd.t()).to(dt))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N,gap", [(1, 2048, 300, 0), (3, 8192, 64, 0), (19, 640, 96, 0), (50, 72, 136, 5), (333, 256, 512, 0),
+                                       (2000, 136, 72, 8), (9000, 64, 64, 0)])
+def test_linear_within_its_roundings(M, K, N, gap, dtype):
+    Q, dt = _q(), DT[dtype]
+    x, W = _activations(M, K, dt, 11), (torch.randn(N, K, generator=_gen(12)) * K ** -0.5).to(dt).float()
+    dz = (torch.randn(M, N, generator=_gen(13)) * 1e-3).to(dt).float()
+    b = torch.randn(N, generator=_gen(14))
+    lin = Q.Linear(M, K, N, dt, gap=gap)
+    lin.pack_weight(W.to("cuda", dt))
+    z = lin.forward(_rows(x, gap, dt), b.cuda())
+    dx, dW, db = lin.backward(_rows(dz, gap, dt), bias=True)
+    (qx, sx), (qw, sw) = _pack_ref(x), _pack_ref(W)
+    xt, wt, g = qx.astype(np.float64) * sx[:, None], qw.astype(np.float64) * sw[:, None], _np(dz)
+    half = H if dtype == "bf16" else 0.0
+
+    def within(got, ref, terms, R, operand):
+        bound = ((R + 8) * U + operand) * terms + half * np.abs(ref) + 1e-37
+        worst = (np.abs(_np(got) - ref) / bound).max()
+        assert worst <= 1, worst
+
+    within(z, xt @ wt.T + _np(b), np.abs(xt @ wt.T) + np.abs(_np(b)), 0, 0.0)      # (the sum itself is exact)
+    within(dx, g @ wt, np.abs(g) @ np.abs(wt), N, half)
+    within(dW, g.T @ xt, np.abs(g).T @ np.abs(xt), M, half)
+    ref = g.sum(0)
+    assert (np.abs(_np(db) - ref) <= (M + 8) * U * np.abs(g).sum(0)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_gradients_against_differences(dtype):
+    """One code moved by one either way: the outputs' change against dz is 2 s times the gradient there."""
+    Q, dt = _q(), DT[dtype]
+    M, K, N = 21, 80, 40
+    lin = Q.Linear(M, K, N, dt)
+    f32 = Q.Linear(M, K, N, torch.float32)           # (outputs of the differences unrounded)
+    x, W = _activations(M, K, dt, 21) + 0.5, torch.randn(N, K, generator=_gen(22)) * 0.1
+    dz = (torch.randn(M, N, generator=_gen(23))).to(dt)
+    lin.pack_weight(W.to("cuda", dt))
+    lin.forward(x.to("cuda", dt))
+    dx, dW, _ = lin.backward(dz.cuda())
+    f32.set_weight(lin.w_codes, lin.w_scales)
+    g = _np(dz)
+    for m, k, n in [(0, 0, 0), (M - 1, K - 1, N - 1), (7, 33, 12), (20, 64, 39)]:
+        for codes, scales, at, grad in ((lin.codes, lin.scales, (m, k), dx), (lin.w_codes, lin.w_scales, (n, k), dW)):
+            outs = []
+            for step in (1, -1):
+                old = codes[at].item()
+                codes[at] = max(-127, min(127, old + step))
+                moved = codes[at].item() - old
+                outs.append((_np(f32.forward_packed(lin.codes, lin.scales)).copy(), moved))
+                codes[at] = old
+            (zp, up), (zm, down) = outs
+            want = ((zp - zm) * g).sum()
+            have = float(grad[at]) * float(scales[at[0]]) * (up - down)
+            size = (np.abs(zp - zm) * np.abs(g)).sum()
+            noise = 4 * U * (np.abs(zp) * np.abs(g)).sum()
+            assert abs(want - have) <= (2 * H if dtype == "bf16" else 100 * U) * size + noise
+
+
+def test_non_finite_rows_stay_in_their_row():
+    Q = _q()
+    M, K, N = 40, 96, 48
+    x = torch.randn(M, K, generator=_gen(31))
+    x[3, 5], x[39, 95] = float("inf"), float("nan")
+    lin = Q.Linear(M, K, N)
+    lin.pack_weight(torch.randn(N, K, generator=_gen(32)).to("cuda", torch.bfloat16))
+    z = lin.forward(x.to("cuda", torch.bfloat16)).cpu()
+    assert torch.isnan(z[3]).all() and torch.isnan(z[39]).all()
+    ok = [i for i in range(M) if i not in (3, 39)]
+    assert torch.isfinite(z[ok]).all()
+    dz = torch.randn(M, N, generator=_gen(33))
+    dz[17, 4] = float("inf")
+    dx, dW, _ = lin.backward(dz.to("cuda", torch.bfloat16))
+    assert not torch.isfinite(dx.cpu()[17]).any() and torch.isfinite(dx.cpu()[[i for i in range(M) if i != 17]]).all()
+    assert torch.isnan(dW.cpu()).all()               # a NaN row reaches every sum over the rows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_rows(dtype):
+    Q, dt = _q(), DT[dtype]
+    lin = Q.Linear(0, 64, 40, dt)
+    lin.pack_weight(torch.ones(40, 64, dtype=dt, device="cuda"))
+    assert lin.forward(torch.empty(0, 64, dtype=dt, device="cuda")).shape == (0, 40)
+    lin.dW.fill_(7)
+    lin.db.fill_(7)
+    dx, dW, db = lin.backward(torch.empty(0, 40, dtype=dt, device="cuda"), bias=True)
+    assert dx.shape == (0, 64) and (dW == 0).all() and (db == 0).all()
+    ck = Q.Checkpoint(0, 24, dt)
+    ck.pack(torch.empty(0, 24, dtype=dt, device="cuda"))
+    assert ck.unpack().shape == (0, 24)
+    gate = Q.Gate(0, 24, dt)
+    assert gate.forward(torch.empty(0, 48, dtype=dt, device="cuda")).shape == (0, 24)
+    assert gate.backward(torch.empty(0, 24, dtype=dt, device="cuda")).shape == (0, 48)
+
+
+def _act64(kind, g):
+    if kind == "silu":
+        p = 1 / (1 + np.exp(-g))
+        return g * p, p + g * p * (1 - p)
+    p = 0.5 * (1 + np.vectorize(math.erf)(g / math.sqrt(2)))
+    return g * p, p + g * np.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,gap", [(1, 8, 0), (1, 8192, 0), (3, 33, 5), (37, 72, 8), (5, 130, 0), (4, 1000, 0), (9, 2048, 0), (2, 4104, 5),
+                                     (2, 9000, 0)])
+def test_gate(M, K, gap, dtype, kind):
+    """f and f' are a few fp32 operations on library functions that are right to 2 ulp: 16 u of the terms; bf16 results are rounded once."""
+    Q, dt = _q(), DT[dtype]
+    h = _activations(M, 2 * K, dt, 41)
+    dy = torch.randn(M, K, generator=_gen(42)).to(dt).float()
+    gate = Q.Gate(M, K, dt, kind=kind, gap=gap)
+    gate.codes.fill_(77)
+    y = gate.forward(_rows(h, gap, dt))
+    half = H if dtype == "bf16" else 0.0
+    g, u = _np(h)[:, :K], _np(h)[:, K:]
+    f, _ = _act64(kind, g)
+    # (1 + erf) and 1 + e^-g cancel or round at the scale of 1: the error of f is relative to |g| there
+    assert (np.abs(_np(y) - f * u) <= 16 * U * np.abs(g * u) + half * np.abs(f * u) + 1e-37).all()
+    q, s = _pack_ref(np.stack([h.numpy()[:, :K], h.numpy()[:, K:]], 1).reshape(2 * M, K))
+    assert np.array_equal(gate.codes.cpu().numpy()[:, :K], q) and np.array_equal(gate.scales.cpu().numpy(), s)
+    assert (gate.codes.cpu().numpy()[:, K:] == 0).all()
+    dh = gate.backward(_rows(dy, gap, dt))
+    back = (q.astype(np.float32) * s[:, None]).astype(np.float64).reshape(M, 2, K)
+    gt, ut = back[:, 0], back[:, 1]
+    f, df = _act64(kind, gt)
+    want = np.concatenate([_np(dy) * ut * df, _np(dy) * f], 1)
+    room = np.concatenate([np.abs(_np(dy) * ut) * (1 + np.abs(gt)), np.abs(_np(dy) * gt)], 1)
+    assert (np.abs(_np(dh) - want) <= 32 * U * room + half * np.abs(want) + 1e-37).all()
+    # the same derivative by differences of f in 64 bits
+    e = 1e-5
+    diff = (_act64(kind, gt + e)[0] - _act64(kind, gt - e)[0]) / (2 * e)
+    assert (np.abs(_np(dh)[:, :K] - _np(dy) * ut * diff) <= 1e-5 * np.abs(_np(dy) * ut) + 32 * U * room[:, :K] + half * np.abs(want[:, :K])).all()
+    # y packed: the fp32 value's codes, at most one step from those of the 64-bit value
+    packed = Q.Gate(M, K, dt, kind=kind, train=False, packed=True, gap=gap)
+    packed.codes_y.fill_(77)
+    assert packed.forward(_rows(h, gap, dt)) is None
+    yc, ys = packed.codes_y.cpu().numpy(), packed.scales_y.cpu().numpy()
+    assert (yc[:, K:] == 0).all()
+    y64 = _act64(kind, g)[0] * u
+    a = np.abs(y64).max(1)
+    assert (np.abs(ys * 127 - a) <= 32 * U * np.maximum(a, np.abs(g * u).max(1))).all()
+    assert (np.abs(yc[:, :K] * ys[:, None].astype(np.float64) - y64) <= (0.5 + 1e-4) * ys[:, None]).all()
+
+
+def test_gate_of_non_finite_rows():
+    Q = _q()
+    h = torch.randn(6, 64, generator=_gen(51))
+    h[1, 3], h[4, 40] = float("inf"), float("nan")
+    h[2, 5] = torch.finfo(torch.float32).min         # a mask's lowest value: f = -0 there
+    gate = Q.Gate(6, 32, torch.float32)
+    y = gate.forward(h.cuda()).cpu()
+    s = gate.scales.cpu().view(6, 2)
+    assert torch.isnan(s[1, 0]) and torch.isnan(s[4, 1]) and torch.isfinite(s[[0, 2, 3, 5]]).all()
+    assert torch.isfinite(s[1, 1]) and torch.isfinite(s[4, 0])
+    assert y[2, 5] == 0 and torch.isfinite(y[[0, 2, 3, 5]]).all()
+    dh = gate.backward(torch.ones(6, 32, device="cuda")).cpu()
+    assert torch.isnan(dh[1]).all() and torch.isnan(dh[4, :32]).all() and torch.isfinite(dh[[0, 3, 5]]).all()
+
+
+def test_offsets_beyond_32_bits():
+    """Codes and rows past 2^31 bytes and elements: the last rows are as they are in a small tensor."""
+    Q = _q()
+    M, K, N, last = (1 << 20) + 77, 2064, 16, 301
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    tail = _activations(last, K, torch.bfloat16, 61).to("cuda", torch.bfloat16)
+    x[-last:] = tail
+    W = torch.randn(N, K, generator=_gen(62)).to("cuda", torch.bfloat16)
+    dz = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    dz[-last:] = torch.randn(last, N, generator=_gen(63)).to("cuda", torch.bfloat16)
+    big, small = Q.Linear(M, K, N), Q.Linear(last, K, N)
+    for lin, xx, d in ((big, x, dz), (small, tail, dz[-last:].contiguous())):
+        lin.pack_weight(W)
+        lin.forward(xx)
+        lin.backward(d)
+    assert torch.equal(big.codes[-last:], small.codes) and torch.equal(big.z[-last:], small.z) and (big.z[:-last] == 0).all()
+    assert torch.equal(big.dx[-last:], small.dx) and (big.dx[:-last] == 0).all()
+    assert (big.dW.float() - small.dW.float()).abs().max() <= 2 * H * small.dW.float().abs().max()
+    ck = Q.Checkpoint(M, K)
+    ck.codes, ck.scales = big.codes, big.scales
+    assert torch.equal(ck.unpack()[-last:], Q.Checkpoint.unpack(_of(Q, small, last, K)))
+
+
+def _of(Q, lin, M, K):
+    ck = Q.Checkpoint(M, K)
+    ck.codes, ck.scales = lin.codes, lin.scales
+    return ck
+
+
+def test_results_do_not_depend_on_the_run_or_the_stream():
+    Q = _q()
+    M, K, N = 900, 520, 264
+    x, W = _activations(M, K, torch.bfloat16, 71).to("cuda", torch.bfloat16), torch.randn(N, K, generator=_gen(72)).to("cuda", torch.bfloat16)
+    dz = torch.randn(M, N, generator=_gen(73)).to("cuda", torch.bfloat16)
+    lin = Q.Linear(M, K, N)
+
+    def step(stream=None):
+        lin.pack_weight(W, stream)
+        lin.forward(x, stream=stream)
+        lin.backward(dz, bias=True, stream=stream)
+        return [t.clone() for t in (lin.z, lin.dx, lin.dW, lin.db)]
+
+    first = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t in (lin.z, lin.dx, lin.dW, lin.db):
+        t.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        again = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    lin.z.zero_()
+    torch.cuda.synchronize()
+    B.convbn_qlinear_fwd(lin.desc, x, lin.codes, lin.scales, lin.w_codes, lin.w_scales, None, lin.z, lin.ws, side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(lin.z, first[0])
+
+
+def test_captured_step_replays():
+    """A captured forward and backward step of a gated block, replayed over changing inputs, against the eager one."""
+    Q = _q()
+    M, C, F = 130, 64, 96
+    blk, ref = Q.GatedBlock(M, C, F), Q.GatedBlock(M, C, F)
+    x, dout = torch.zeros(M, C, dtype=torch.bfloat16, device="cuda"), torch.zeros(M, C, dtype=torch.bfloat16, device="cuda")
+    wu = (torch.randn(2 * F, C, generator=_gen(81)) * 0.1).to("cuda", torch.bfloat16)
+    wd = (torch.randn(C, F, generator=_gen(82)) * 0.1).to("cuda", torch.bfloat16)
+
+    def step(b):
+        b.pack_weights(wu, wd)
+        return (b.forward(x), *b.backward(dout))
+
+    step(blk)
+    step(ref)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step(blk)
+    for seed in range(3):
+        x.copy_(torch.randn(M, C, generator=_gen(90 + seed)))
+        dout.copy_(torch.randn(M, C, generator=_gen(95 + seed)))
+        want = [t.clone() for t in step(ref)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,C,F", [(1, 64, 128), (50, 72, 200), (196, 256, 512)])
+def test_gated_block(M, C, F, dtype):
+    """The chain against the same chain in 64 bits without any code: what 8 bits leave, 1/254 of a row's maximum an operand.  Three codes
+    stand between x and the gradients; their errors are independent, so a tenth of the norm is several times what they add up to."""
+    Q, dt = _q(), DT[dtype]
+    blk = Q.GatedBlock(M, C, F, dt)
+    x, dout = torch.randn(M, C, generator=_gen(101)).to(dt), torch.randn(M, C, generator=_gen(102)).to(dt)
+    wu, wd = (torch.randn(2 * F, C, generator=_gen(103)) * C ** -0.5).to(dt), (torch.randn(C, F, generator=_gen(104)) * F ** -0.5).to(dt)
+    blk.pack_weights(wu.cuda(), wd.cuda())
+    out = blk.forward(x.cuda())
+    dx, dwu, dwd = blk.backward(dout.cuda())
+    xr, ur, dr = (t.double().requires_grad_() for t in (x, wu, wd))
+    h = xr @ ur.t()
+    ref = xr + (torch.nn.functional.silu(h[:, :F]) * h[:, F:]) @ dr.t()
+    ref.backward(dout.double())
+    for got, want in ((out, ref.detach()), (dx, xr.grad), (dwu, ur.grad), (dwd, dr.grad)):
+        assert (got.cpu().double() - want).norm() <= 0.1 * want.norm()
+    assert blk.saved_bytes() < 1.4 * M * (C + 3 * F)      # x, both halves of h, and y: a byte each, and the rows' scales and padding

@@ -1,0 +1,138 @@
+"""The 8-bit rows, CPU only: sizes, and every refusal before anything is launched."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2305_11624_amd import binding as B
+
+OKP = C.c_void_p(4096)      # never dereferenced: validation fails first
+NEED = 1 << 40
+
+
+def _qdesc(**change):
+    kw = dict(M=8, K=64, N=32, dtype=B.BF16)
+    kw.update(change)
+    return B.make_qdesc(**kw)
+
+
+def _fwd(d, x=OKP, codes=OKP, scales=OKP, w=OKP, ws=OKP, b=None, z=OKP, work=OKP, nbytes=NEED):
+    return B.lib().convbn_qlinear_fwd(C.byref(d), x, codes, scales, w, ws, b, z, work, nbytes, None)
+
+
+def _bwd(d, codes=OKP, scales=OKP, w=OKP, ws=OKP, dz=OKP, dx=OKP, dW=OKP, db=OKP, work=OKP, nbytes=NEED):
+    return B.lib().convbn_qlinear_bwd(C.byref(d), codes, scales, w, ws, dz, dx, dW, db, work, nbytes, None)
+
+
+def _gate(d, h=OKP, hc=OKP, hs=OKP, y=OKP, yc=OKP, ys=OKP):
+    return B.lib().convbn_qgate_fwd(C.byref(d), h, hc, hs, y, yc, ys, None)
+
+
+def test_row_bytes_are_whole_16_byte_pieces():
+    assert [B.convbn_qrow_bytes(k) for k in (-1, 0, 1, 15, 16, 17, 72, 4096)] == [0, 0, 16, 16, 16, 32, 80, 4096]
+
+
+def test_descriptor_mirror_has_the_size_of_the_struct():
+    assert C.sizeof(B.QDesc) == 64 and C.sizeof(B.Desc) != C.sizeof(B.QDesc)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(M=-1), B.ERR_SHAPE), (dict(K=0), B.ERR_SHAPE), (dict(N=0), B.ERR_SHAPE), (dict(dtype=2), B.ERR_UNSUPPORTED),
+    (dict(ldx=63), B.ERR_SHAPE), (dict(ldz=31), B.ERR_SHAPE), (dict(ldx=-64), B.ERR_SHAPE), (dict(act=1), B.ERR_UNSUPPORTED),
+    (dict(act=16), B.ERR_UNSUPPORTED), (dict(act=4), B.ERR_NULL), (dict(act=8), B.ERR_NULL), (dict(K=131073), B.ERR_UNSUPPORTED),
+    (dict(M=(1 << 30) + 1), B.ERR_UNSUPPORTED), (dict(ldx=1 << 41), B.ERR_UNSUPPORTED)])
+def test_bad_descriptors_of_a_linear_block(change, code):
+    d = _qdesc(**change)
+    assert _fwd(d) == code and _bwd(d) == code
+    assert B.convbn_qlinear_workspace_bytes(d, B.PASS_FWD) == 0 == B.convbn_qlinear_workspace_bytes(d, B.PASS_BWD)
+    assert len(B.convbn_last_error()) > 4
+
+
+def test_reserved_field_and_missing_descriptor():
+    d = _qdesc()
+    d.reserved = 1
+    assert _fwd(d) == B.ERR_UNSUPPORTED and _gate(d) == B.ERR_UNSUPPORTED
+    L = B.lib()
+    assert L.convbn_qpack(None, OKP, OKP, OKP, None) == B.ERR_NULL
+    assert L.convbn_qunpack(None, OKP, OKP, OKP, None) == B.ERR_NULL
+    assert L.convbn_qlinear_fwd(None, OKP, OKP, OKP, OKP, OKP, None, OKP, OKP, NEED, None) == B.ERR_NULL
+    assert L.convbn_qlinear_bwd(None, OKP, OKP, OKP, OKP, OKP, OKP, OKP, OKP, OKP, NEED, None) == B.ERR_NULL
+    assert L.convbn_qgate_fwd(None, OKP, None, None, OKP, None, None, None) == B.ERR_NULL
+    assert L.convbn_qgate_bwd(None, OKP, OKP, OKP, OKP, None) == B.ERR_NULL
+
+
+def test_missing_and_misaligned_pointers():
+    d = _qdesc()
+    assert _fwd(d, x=None, codes=None, scales=None) == B.ERR_NULL      # neither rows nor codes
+    assert _fwd(d, scales=None) == B.ERR_NULL and "together" in B.convbn_last_error()
+    assert _fwd(d, w=None) == B.ERR_NULL and _fwd(d, ws=None) == B.ERR_NULL and _fwd(d, z=None) == B.ERR_NULL
+    assert _fwd(d, codes=C.c_void_p(4104)) == B.ERR_UNSUPPORTED and _fwd(d, w=C.c_void_p(4104)) == B.ERR_UNSUPPORTED
+    assert _fwd(d, x=C.c_void_p(4097)) == B.ERR_UNSUPPORTED and _fwd(d, z=C.c_void_p(4097)) == B.ERR_UNSUPPORTED
+    assert _bwd(d, dz=None) == B.ERR_NULL and _bwd(d, dx=None, dW=None, db=None) == B.ERR_NULL
+    assert _bwd(d, codes=None) == B.ERR_NULL and _bwd(d, w=None) == B.ERR_NULL
+    assert _bwd(_qdesc(dtype=B.F32), dz=C.c_void_p(4098)) == B.ERR_UNSUPPORTED
+    for name in ("convbn_qpack", "convbn_qunpack"):
+        f = getattr(B.lib(), name)
+        for i in range(3):
+            p = [OKP] * 3
+            p[i] = None
+            assert f(C.byref(d), *p, None) == B.ERR_NULL
+    assert B.lib().convbn_qpack(C.byref(d), C.c_void_p(4097), OKP, OKP, None) == B.ERR_UNSUPPORTED
+
+
+def test_gate_refusals():
+    assert _gate(_qdesc(gate=2)) == B.ERR_UNSUPPORTED
+    assert _gate(_qdesc(ldx=127)) == B.ERR_SHAPE and _gate(_qdesc(ldz=63)) == B.ERR_SHAPE
+    d = _qdesc()
+    assert _gate(d, h=None) == B.ERR_NULL and _gate(d, hs=None) == B.ERR_NULL and _gate(d, ys=None) == B.ERR_NULL
+    assert _gate(d, y=None, yc=None, ys=None) == B.ERR_NULL
+    assert _gate(d, h=C.c_void_p(4097)) == B.ERR_UNSUPPORTED
+    assert B.lib().convbn_qgate_bwd(C.byref(d), OKP, OKP, OKP, None, None) == B.ERR_NULL
+
+
+def test_workspace_is_asked_for_and_checked():
+    d = _qdesc()
+    need = B.convbn_qlinear_workspace_bytes(d, B.PASS_FWD)
+    assert need >= 8 * 64 + 8 * 4
+    assert _fwd(d, codes=None, scales=None, work=None, nbytes=0) == B.ERR_WORKSPACE
+    assert _fwd(d, codes=None, scales=None, nbytes=need - 1) == B.ERR_WORKSPACE
+    assert _fwd(d, codes=None, scales=None, work=C.c_void_p(4104)) == B.ERR_UNSUPPORTED
+
+
+def test_native_call_takes_the_descriptors_rows_only():
+    B.lib()
+    call, at = B._call_rows, B._at.convbn_qpack
+    assert call(at, _qdesc(), None, None, None, B._NO_WS, 0) == B.ERR_NULL
+    for bad in (None, b"\0" * 8, B.Desc()):
+        with pytest.raises(TypeError):
+            call(at, bad, None, None, None, B._NO_WS, 0)
+    with pytest.raises(TypeError):
+        B._call(at, _qdesc(), None, None, None, None, B._NO_WS, 0)
+    with pytest.raises(AssertionError):
+        call(at, _qdesc(), torch.zeros(8, 64), None, None, B._NO_WS, 0)
+    with pytest.raises(TypeError):
+        call(at, _qdesc(), *[None] * 5, B._NO_WS, 0)   # (no entry point takes five)
+
+
+def test_objects_check_their_arguments():
+    from paper_2305_11624_amd import quant as Q
+    with pytest.raises(TypeError):
+        Q.Checkpoint(4, 8, torch.float16, device="cpu")
+    with pytest.raises(KeyError):
+        Q.Gate(4, 8, kind="relu", device="cpu")
+    lin = Q.Linear(4, 24, 8, torch.float32, train=False, device="cpu")
+    x = torch.zeros(4, 24)
+    with pytest.raises(RuntimeError):
+        lin.forward(x)                                   # no weight yet
+    with pytest.raises(ValueError):
+        lin.set_weight(torch.zeros(8, 24, dtype=torch.int8), torch.zeros(8))      # rows are 32 bytes
+    lin.set_weight(*Q.new_codes(8, 24, "cpu"))
+    for bad in (x[:, :23], x.bfloat16(), torch.zeros(4, 32)[:, :24], x[:3]):
+        with pytest.raises(ValueError):
+            lin.forward(bad)
+    with pytest.raises(ValueError):
+        lin.forward(x, b=torch.zeros(7))
+    with pytest.raises(RuntimeError):
+        lin.backward(torch.zeros(4, 8))
+    with pytest.raises(AssertionError):
+        lin.forward(x)                                   # right in everything, but on the host
