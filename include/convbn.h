@@ -453,7 +453,8 @@ convbn_status convbn_aux_maxpool_bwd(int dtype, const void *dy, const void *idx,
  * rounded below fp32.
  *
  * Rows may be strided (ldx, ldz); codes, scales, W and vectors are dense.  M == 0 is no error: nothing is read, dW and db
- * become zero.  A sum over the channels is exact up to K = 131072 (longer: CONVBN_ERR_UNSUPPORTED).  codes and workspace are
+ * become zero.  A sum over the channels is exact up to K = 131072 (longer, or N above 2^20, M above 2^30:
+ * CONVBN_ERR_UNSUPPORTED).  codes and workspace are
  * 16-byte aligned; rows of x, z, dx, dz, h, y, dy, dh need the alignment of their element only (16 bytes are faster). */
 typedef struct {
   int64_t M;                  /* rows of x, z, dx, dz (a gate: of h, y, dy, dh)                                      */

@@ -6,6 +6,7 @@ using namespace convbn;
 namespace {
 
 constexpr int32_t MAX_SUM = 131072;   // products of two codes stay below 2^14: that many of them fit 32 bits
+constexpr int32_t MAX_OUT = 1 << 20;
 
 bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
@@ -57,6 +58,7 @@ convbn_status check_linear(const convbn_qdesc* d, i64* ldx, i64* ldz) {
   if (d->N < 1) return set_error(CONVBN_ERR_SHAPE, "N must be >= 1");
   TRY_STATUS(check(d, d->K, d->N, ldx, ldz));
   if (d->K > MAX_SUM) return set_error(CONVBN_ERR_UNSUPPORTED, "a sum over more than %d channels", (int)MAX_SUM);
+  if (d->N > MAX_OUT) return set_error(CONVBN_ERR_UNSUPPORTED, "more than %d output channels", (int)MAX_OUT);
   if (d->act & ~(CONVBN_ACT_ADD_OUT | CONVBN_ACT_ADD_IN))
     return set_error(CONVBN_ERR_UNSUPPORTED, "act %d: only the two addends", d->act);
   if (((d->act & CONVBN_ACT_ADD_OUT) && !d->add_out) || ((d->act & CONVBN_ACT_ADD_IN) && !d->add_in))

@@ -1,71 +1,441 @@
 // Gradients of the 8-bit product from the kept codes: dx = dz . (sw qw) + add, dW = dz^T . (sx qx), db = column sums of dz.
+//
+// Both products are C[i][j] = sum_r A(i, r) s[r] q[r][j] with codes that run along j: the input gradient reduces over the output
+// channels (A = dz), the weight gradient over the rows (A = dz^T).  Codes become bf16 numbers s q on their way into LDS, once for
+// all waves of a workgroup; q alone is exact there, s q is rounded to bf16 (as the activation it stands for would be).
+//
+// F32: A s is split into three bf16 parts that add up to all 24 bits, the codes stay whole numbers, and the three products are
+// summed in fp32: nothing is rounded below that.
 #include "quant.h"
 
 namespace convbn {
 
 namespace {
 
-// C[i][j] = sum_r A(i, r) s[r] q[r][j], 32 x 32 outputs a workgroup, 32 of the reduced index at a time.  TRANS: A(i, r) = dz[r][i].
-template <typename T, bool TRANS>
-__global__ __launch_bounds__(256) void qgrad_kernel(i64 I, int J, i64 R, const T* __restrict__ dz, i64 ldz, const int8_t* __restrict__ q,
-                                                    const float* __restrict__ s, T* C, i64 ldc, const T* add) {
-  __shared__ float A[32][33], Bq[32][33];
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const i64 i0 = (i64)blockIdx.x * 32;
-  const int j0 = blockIdx.y * 32, Jp = qrow(J);
-  float acc[4] = {};
-  for (i64 r0 = 0; r0 < R; r0 += 32) {
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr unsigned OOB = 0x80000000u;   // beyond any buffer: the load returns zeros
+constexpr int RC = 64;                  // of the reduced index at a time
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, i64 bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000);
+}
+
+struct GradParams {
+  const bf16_t* A;      // [planes][rows][lda]; aligned, zeros between the last channel and a multiple of 8
+  i64 plane;            // elements of a plane
+  i64 lda;
+  const uint8_t* q;     // [R][Jp]
+  const float* s;       // [R], null: 1
+  void* C;              // [I][ldc] of the output type, or [splits][I][J] fp32
+  const void* add;      // laid out like C
+  i64 ldc;
+  i64 I, R;             // (I: rows of C)
+  int J, Jp, Aw;        // Aw: channels of A's rows, a multiple of 8
+  int planes, nch;      // chunks of RC of a plane
+  int splits, per;      // chunks of a split
+  int nti, ntj;
+};
+
+template <int TI, int TJ, int WI, int WJ> struct GradCfg {
+  static constexpr int WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;
+  static constexpr int A_BYTES = TI * RC * 2, B_BYTES = TJ * RC * 2, STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
+};
+
+// Two codes to bf16 numbers s q
+__device__ __forceinline__ uint32_t code2(uint32_t w, int at, float s) {
+  return pack_bf16x2((float)(int8_t)(w >> (8 * at)) * s, (float)(int8_t)(w >> (8 * at + 8)) * s);
+}
+
+__device__ __forceinline__ bf16x8 read_tr8(const unsigned char* p, int rows4) {   // 8 rows of this lane's column; rows4: bytes of 4 rows
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + rows4));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(bf16x8, (s16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+}
+
+// OUT: float or bf16_t.  TRANS: A(i, r) = A[r][i].
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ>
+__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradParams p) {
+  using Cfg = GradCfg<TI, TJ, WI, WJ>;
+  constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
+  constexpr int PA = TI * 8 / NT, PB = TJ * 8 / NT;   // 16-byte pieces of A and 8-code pieces of q that a thread moves per chunk
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+  // contiguous runs of tiles to each XCD
+  const int total = p.nti * p.ntj * p.splits, run = (total + 7) >> 3;
+  const int id = ((int)blockIdx.x & 7) * run + ((int)blockIdx.x >> 3);
+  if (((int)blockIdx.x >> 3) >= run || id >= total) return;
+  const int split = id / (p.nti * p.ntj), tile = id - split * (p.nti * p.ntj);
+  const int ti = tile % p.nti, tj = tile / p.nti;
+  const i64 i0 = (i64)ti * TI;
+  const int j0 = tj * TJ;
+  const int c_beg = split * p.per, c_end = min(p.planes * p.nch, c_beg + p.per);
+
+  // ---- this thread's pieces
+  unsigned a_off[PA], b_off[PB];   // byte offsets of the first chunk's pieces
+  unsigned a_lds[PA], b_lds[PB], s_off[PB];
+  int a_col[PA];                   // direct: channel within the chunk
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int y = ty + 8 * t;
-      if (TRANS) A[y][tx] = r0 + y < R && i0 + tx < I ? to_f32(dz[(r0 + y) * ldz + i0 + tx]) : 0.f;   // [r][i]
-      else A[tx][y] = i0 + y < I && r0 + tx < R ? to_f32(dz[(i0 + y) * ldz + r0 + tx]) : 0.f;
-      Bq[y][tx] = r0 + y < R && j0 + tx < J ? (float)q[(r0 + y) * Jp + j0 + tx] * s[r0 + y] : 0.f;
+  for (int t = 0; t < PA; ++t) {
+    const int w = t * NT + tid;
+    if constexpr (TRANS) {
+      const int r = w / (TI / 8), g = w % (TI / 8);
+      a_off[t] = i0 + g * 8 < p.Aw ? (unsigned)(r * (int)p.lda + g * 8) * 2u : OOB;
+      a_lds[t] = r * (TI * 2) + (((g >> 2) ^ (r & 3)) << 6) + (g & 3) * 16;
+      a_col[t] = 0;
+    } else {
+      const int r = w >> 3, g = w & 7;
+      a_off[t] = (unsigned)(r * (int)p.lda + g * 8) * 2u;
+      a_lds[t] = r * 128 + ((g ^ (r & 7)) << 4);
+      a_col[t] = g * 8;
     }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 32; ++r)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] += A[r][ty + 8 * t] * Bq[r][tx];
-    __syncthreads();
   }
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const i64 i = i0 + ty + 8 * t;
-    if (i >= I || j0 + tx >= J) continue;
-    const i64 o = i * ldc + j0 + tx;
-    C[o] = from_f32<T>(acc[t] + (add ? to_f32(add[o]) : 0.f));
+  for (int t = 0; t < PB; ++t) {
+    const int w = t * NT + tid;
+    const int r = w / (TJ / 8), g = w % (TJ / 8);
+    b_off[t] = j0 + g * 8 < p.Jp ? (unsigned)(r * p.Jp + g * 8) : OOB;
+    b_lds[t] = r * (TJ * 2) + (((g >> 2) ^ (r & 3)) << 6) + (g & 3) * 16;
+    s_off[t] = r * 4;
+  }
+
+  i32x4 a_reg[PA];
+  i32x2 b_reg[PB];
+  float s_reg[PB];
+  auto fetch = [&](int c) {
+    const int plane = c / p.nch;
+    const i64 r0 = (i64)(c - plane * p.nch) * RC;
+    const i64 left = p.R - r0 < RC ? p.R - r0 : RC;
+    const bf16_t* A = p.A + plane * p.plane;
+    if constexpr (TRANS) {
+      const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + r0 * p.lda + i0, ((left - 1) * p.lda + p.Aw - i0) * 2);
+#pragma unroll
+      for (int t = 0; t < PA; ++t) a_reg[t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)a_off[t], 0, 0);
+    } else {
+      const i64 rows = p.I - i0 < TI ? p.I - i0 : TI;
+      const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + i0 * p.lda + r0, ((rows - 1) * p.lda + p.Aw - r0) * 2);
+#pragma unroll
+      for (int t = 0; t < PA; ++t)
+        a_reg[t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(r0 + a_col[t] < p.Aw ? a_off[t] : OOB), 0, 0);
+    }
+    const __amdgpu_buffer_rsrc_t rq = make_rsrc(p.q + r0 * p.Jp + j0, left * p.Jp - j0);
+#pragma unroll
+    for (int t = 0; t < PB; ++t) b_reg[t] = __builtin_amdgcn_raw_buffer_load_b64(rq, (int)b_off[t], 0, 0);
+    if (p.s) {
+      const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.s + r0, left * 4);
+#pragma unroll
+      for (int t = 0; t < PB; ++t) s_reg[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
+    } else {
+#pragma unroll
+      for (int t = 0; t < PB; ++t) s_reg[t] = 1.f;
+    }
+  };
+  auto put = [&](unsigned char* stage) {
+#pragma unroll
+    for (int t = 0; t < PA; ++t) *reinterpret_cast<i32x4*>(stage + a_lds[t]) = a_reg[t];
+#pragma unroll
+    for (int t = 0; t < PB; ++t) {
+      const uint32_t lo = b_reg[t][0], hi = b_reg[t][1];
+      const float s = s_reg[t];
+      *reinterpret_cast<uint4*>(stage + Cfg::A_BYTES + b_lds[t]) = make_uint4(code2(lo, 0, s), code2(lo, 2, s), code2(hi, 0, s), code2(hi, 2, s));
+    }
+  };
+
+  // ---- operands of this wave
+  const int wi = (wave % (TI / WI)) * WI, wj = (wave / (TI / WI)) * WJ;
+  const int kb = lane >> 5, ep = (lane & 15) >> 2;
+  // transposing reads: this lane addresses row kb * 8 + ep (+ 4) of a 16-row step, channels (l / 16 % 2) * 16 + (l % 4) * 4 of 32
+  const int tr_row = kb * 8 + ep, tr_col = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  auto b_at = [&](int step, int f) {
+    return Cfg::A_BYTES + (step * 16 + tr_row) * (TJ * 2) + (((((wj >> 5) + f)) ^ ep) << 6) + tr_col;
+  };
+  auto a_at = [&](int step, int f) {
+    if constexpr (TRANS) return (step * 16 + tr_row) * (TI * 2) + ((((wi >> 5) + f) ^ ep) << 6) + tr_col;
+    const int row = wi + f * 32 + (lane & 31);
+    return row * 128 + (((step * 2 + kb) ^ (row & 7)) << 4);
+  };
+
+  f32x16 acc[FI][FJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  if (c_beg < c_end) {
+    fetch(c_beg);
+    put(smem);
+    if (c_beg + 1 < c_end) fetch(c_beg + 1);
+    __syncthreads();
+    for (int c = c_beg; c < c_end; ++c) {
+      const unsigned char* cur = smem + ((c - c_beg) & 1) * Cfg::STAGE;
+      if (c + 1 < c_end) {
+        put(smem + ((c - c_beg + 1) & 1) * Cfg::STAGE);
+        if (c + 2 < c_end) fetch(c + 2);
+      }
+#pragma unroll
+      for (int step = 0; step < RC / 16; ++step) {
+        bf16x8 af[FI], bf[FJ];
+#pragma unroll
+        for (int f = 0; f < FI; ++f) {
+          if constexpr (TRANS) af[f] = read_tr8(cur + a_at(step, f), 4 * TI * 2);
+          else af[f] = *reinterpret_cast<const bf16x8*>(cur + a_at(step, f));
+        }
+#pragma unroll
+        for (int f = 0; f < FJ; ++f) bf[f] = read_tr8(cur + b_at(step, f), 4 * TJ * 2);
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+          for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
+      }
+      __syncthreads();
+    }
+  }
+
+  // ---- a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..
+  OUT* C = static_cast<OUT*>(p.C);
+  const OUT* add = static_cast<const OUT*>(p.add);
+  i64 ldc = p.ldc;
+  if (p.splits > 1) { C += (i64)split * p.I * ldc; }
+  const bool vec = ((uintptr_t)C | (uintptr_t)(ldc * sizeof(OUT)) | (uintptr_t)add) % (4 * sizeof(OUT)) == 0;
+#pragma unroll
+  for (int i = 0; i < FI; ++i) {
+    const i64 row = i0 + wi + i * 32 + (lane & 31);
+    if (row >= p.I) continue;
+#pragma unroll
+    for (int j = 0; j < FJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int col = j0 + wj + j * 32 + 8 * (e >> 2) + 4 * kb;
+        if (col >= p.J) continue;
+        float v[4] = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        OUT* o = C + row * ldc + col;
+        const OUT* a = add ? add + row * ldc + col : nullptr;
+        if (vec && col + 4 <= p.J) {
+          if constexpr (sizeof(OUT) == 2) {
+            if (a) {
+              const uint2 w = *reinterpret_cast<const uint2*>(a);
+              v[0] += bf16_lo(w.x); v[1] += bf16_hi(w.x); v[2] += bf16_lo(w.y); v[3] += bf16_hi(w.y);
+            }
+            *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+          } else {
+            if (a) {
+              const float4 w = *reinterpret_cast<const float4*>(a);
+              v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+            }
+            *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (col + x < p.J) o[x] = from_f32<OUT>(v[x] + (a ? to_f32(a[x]) : 0.f));
+        }
+      }
   }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void qcolsum_kernel(i64 M, int N, const T* __restrict__ dz, i64 ldz, float* db) {
-  __shared__ float part[4][64];
+// C = the sum of the splits + add, in the order of the splits
+template <typename OUT>
+__global__ __launch_bounds__(256) void qjoin_kernel(i64 I, int J, int splits, const float* __restrict__ part, OUT* C, i64 ldc, const OUT* add) {
+  const i64 total = I * J;
+  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
+    float v = 0.f;
+    for (int s = 0; s < splits; ++s) v += part[s * total + x];
+    const i64 o = x / J * ldc + x % J;
+    C[o] = from_f32<OUT>(v + (add ? to_f32(add[o]) : 0.f));
+  }
+}
+
+// dz as the products want it: rows of a multiple of 8 channels, zeros past the last.  F32: A = dz s in three parts, s by row or by column.
+__global__ __launch_bounds__(256) void qcopy_kernel(i64 M, int N, int N8, const bf16_t* __restrict__ dz, i64 ldz, bf16_t* __restrict__ out) {
+  const i64 total = M * N8;
+  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
+    const i64 m = x / N8;
+    const int n = (int)(x - m * N8);
+    out[x] = n < N ? dz[m * ldz + n] : (bf16_t)0.f;
+  }
+}
+template <bool BY_ROW>
+__global__ __launch_bounds__(256) void qsplit_kernel(i64 M, int N, int N8, const float* __restrict__ dz, i64 ldz, const float* __restrict__ s,
+                                                     bf16_t* __restrict__ out) {
+  const i64 total = M * N8;
+  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
+    const i64 m = x / N8;
+    const int n = (int)(x - m * N8);
+    float v = n < N ? dz[m * ldz + n] * s[BY_ROW ? m : n] : 0.f;
+    bf16_t part[3] = {(bf16_t)v, (bf16_t)0.f, (bf16_t)0.f};   // (infinities and NaN: whole)
+    if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {   // the 8 leading bits, what is left of it, and the rest of that: each exact
+        const float t = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+        part[i] = (bf16_t)t;
+        v -= t;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) out[i * total + x] = part[i];
+  }
+}
+
+// Column sums: a workgroup takes 64 columns and a slice of the rows; slices are added in order by the second launch.
+template <typename T>
+__global__ __launch_bounds__(256) void qcolsum_kernel(i64 M, int N, i64 per, const T* __restrict__ dz, i64 ldz, float* __restrict__ part) {
+  __shared__ float sum[4][64];
   const int n = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+  const i64 beg = (i64)blockIdx.y * per, end = beg + per < M ? beg + per : M;
   float s = 0.f;
   if (n < N)
-    for (i64 m = w; m < M; m += 4) s += to_f32(dz[m * ldz + n]);
-  part[w][threadIdx.x & 63] = s;
+    for (i64 m = beg + w; m < end; m += 4) s += to_f32(dz[m * ldz + n]);
+  sum[w][threadIdx.x & 63] = s;
   __syncthreads();
-  if (w == 0 && n < N) db[n] = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
+  if (w == 0 && n < N)
+    part[(i64)blockIdx.y * N + n] = sum[0][threadIdx.x] + sum[1][threadIdx.x] + sum[2][threadIdx.x] + sum[3][threadIdx.x];
+}
+__global__ __launch_bounds__(256) void qcolsum_join_kernel(int N, int slices, const float* __restrict__ part, float* __restrict__ db) {
+  const int n = blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  float s = 0.f;
+  for (int i = 0; i < slices; ++i) s += part[(i64)i * N + n];
+  db[n] = s;
 }
 
-template <typename T> hipError_t grad_t(const QGrad& p, hipStream_t st) {
+int grid_of(i64 work) { const i64 b = (work + 255) / 256; return (int)(b < 1 ? 1 : b < 65536 ? b : 65536); }
+
+constexpr int CUS = 256;
+
+struct Plan { int ti, tj, splits, per; };
+Plan plan_of(i64 I, int J, i64 R, int planes) {
+  Plan pl;
+  const int nch = (int)((R + RC - 1) / RC) * planes;
+  const i64 big = ((I + 255) / 256) * ((J + 255) / 256), small = ((I + 127) / 128) * ((J + 127) / 128);
+  const bool large = big >= CUS;
+  pl.ti = pl.tj = large ? 256 : 128;
+  const i64 tiles = large ? big : small;
+  pl.splits = pl.per = 1;
+  if (!tiles || !nch) return pl;   // (no rows)
+  int s = 1;
+  if (tiles < CUS) s = (int)(CUS / tiles);
+  if (s > nch / 4) s = nch / 4;
+  if (s < 1) s = 1;
+  pl.per = (nch + s - 1) / s;
+  pl.splits = (nch + pl.per - 1) / pl.per;
+  return pl;
+}
+
+int colsum_slices(i64 M, int N) {
+  const int cols = ceil_div(N, 64);
+  i64 s = 1024 / cols;
+  if (s > M / 64) s = M / 64;
+  return (int)(s < 1 ? 1 : s);
+}
+
+// Whether the products read dz where it is
+bool direct(const QGrad& p) {
+  return p.dtype == CONVBN_BF16 && p.N % 8 == 0 && p.ldz % 8 == 0 && (uintptr_t)p.dz % 16 == 0 && p.ldz <= 1 << 20;
+}
+
+struct Scratch { size_t copy, part, cols, total; };
+Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outputs)
+  Scratch s;
+  const int N8 = (p.N + 7) & ~7;
+  const int planes = p.dtype == CONVBN_BF16 ? 1 : 3;
+  s.copy = 0;
+  if (p.dtype != CONVBN_BF16) s.copy = (size_t)3 * p.M * N8 * 2;
+  else s.copy = (size_t)p.M * N8 * 2;
+  const Plan dx = plan_of(p.M, p.K, p.N, planes), dw = plan_of(p.N, p.K, p.M, planes);
+  const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * p.K * 4 : 0;
+  s.copy = align_up(s.copy, 256);
+  s.part = align_up(px > pw ? px : pw, 256);
+  s.cols = align_up((size_t)colsum_slices(p.M, p.N) * p.N * 4, 256);
+  s.total = s.copy + s.part + s.cols;
+  return s;
+}
+
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ>
+hipError_t launch_tiles(const GradParams& g, hipStream_t st) {
+  using Cfg = GradCfg<TI, TJ, WI, WJ>;
+  static LdsLimitOnce once;
+  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ>;
+  const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
+  if (e != hipSuccess) return e;
+  const int total = g.nti * g.ntj * g.splits;
+  k<<<((total + 7) / 8) * 8, Cfg::NT, Cfg::LDS, st>>>(g);
+  return hipGetLastError();
+}
+
+template <typename T, bool TRANS>
+hipError_t product(const QGrad& p, const bf16_t* A, i64 lda, float* part, hipStream_t st) {
+  GradParams g = {};
+  const bool f32 = p.dtype != CONVBN_BF16;
+  const int N8 = (p.N + 7) & ~7;
+  g.planes = f32 ? 3 : 1;
+  g.A = A; g.lda = lda; g.plane = p.M * (i64)N8; g.Aw = N8;
+  g.q = static_cast<const uint8_t*>(TRANS ? p.qx : p.qw);
+  g.s = f32 ? nullptr : TRANS ? p.sx : p.sw;
+  g.J = p.K; g.Jp = qrow(p.K);
+  g.I = TRANS ? p.N : p.M;
+  g.R = TRANS ? p.M : p.N;
+  g.nch = (int)((g.R + RC - 1) / RC);
+  const Plan pl = plan_of(g.I, g.J, g.R, g.planes);
+  g.splits = pl.splits; g.per = pl.per;
+  g.nti = (int)((g.I + pl.ti - 1) / pl.ti); g.ntj = ceil_div(g.J, pl.tj);
+  T* C = static_cast<T*>(TRANS ? p.dW : p.dx);
+  const i64 ldc = TRANS ? p.K : p.ldx;
+  const T* add = TRANS ? nullptr : static_cast<const T*>(p.add);
+  if (pl.splits > 1) {
+    g.C = part; g.ldc = g.J;
+    const hipError_t e = pl.ti == 256 ? launch_tiles<float, TRANS, 256, 256, 64, 128>(g, st) : launch_tiles<float, TRANS, 128, 128, 64, 64>(g, st);
+    if (e != hipSuccess) return e;
+    qjoin_kernel<T><<<grid_of(g.I * g.J), 256, 0, st>>>(g.I, g.J, pl.splits, part, C, ldc, add);
+    return hipGetLastError();
+  }
+  g.C = C; g.ldc = ldc; g.add = add;
+  return pl.ti == 256 ? launch_tiles<T, TRANS, 256, 256, 64, 128>(g, st) : launch_tiles<T, TRANS, 128, 128, 64, 64>(g, st);
+}
+
+template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st) {
   const T* dz = static_cast<const T*>(p.dz);
-  if (p.dx && p.M)
-    qgrad_kernel<T, false><<<dim3((unsigned)((p.M + 31) / 32), ceil_div(p.K, 32)), 256, 0, st>>>(
-        p.M, p.K, p.N, dz, p.ldz, (const int8_t*)p.qw, p.sw, (T*)p.dx, p.ldx, (const T*)p.add);
-  if (p.dW)
-    qgrad_kernel<T, true><<<dim3(ceil_div(p.N, 32), ceil_div(p.K, 32)), 256, 0, st>>>(
-        p.N, p.K, p.M, dz, p.ldz, (const int8_t*)p.qx, p.sx, (T*)p.dW, p.K, nullptr);
-  if (p.db) qcolsum_kernel<T><<<ceil_div(p.N, 64), 256, 0, st>>>(p.M, p.N, dz, p.ldz, p.db);
+  const Scratch sc = scratch_of(p);
+  bf16_t* copy = static_cast<bf16_t*>(ws);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(ws) + sc.copy);
+  float* cols = reinterpret_cast<float*>(static_cast<char*>(ws) + sc.copy + sc.part);
+  const int N8 = (p.N + 7) & ~7;
+  const bf16_t* A = copy;
+  i64 lda = N8;
+  if constexpr (sizeof(T) == 2) {
+    if (direct(p)) { A = dz; lda = p.ldz; }
+    else if (p.M && (p.dx || p.dW)) qcopy_kernel<<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, copy);
+  }
+  if (p.dx && p.M) {
+    if constexpr (sizeof(T) == 4) qsplit_kernel<false><<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, copy);
+    const hipError_t e = product<T, false>(p, A, lda, part, st);
+    if (e != hipSuccess) return e;
+  }
+  if (p.dW) {
+    if constexpr (sizeof(T) == 4)
+      if (p.M) qsplit_kernel<true><<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sx, copy);
+    const hipError_t e = product<T, true>(p, A, lda, part, st);
+    if (e != hipSuccess) return e;
+  }
+  if (p.db) {
+    const int slices = colsum_slices(p.M, p.N);
+    const i64 per = (p.M + slices - 1) / slices;
+    qcolsum_kernel<T><<<dim3(ceil_div(p.N, 64), slices), 256, 0, st>>>(p.M, p.N, per, dz, p.ldz, cols);
+    qcolsum_join_kernel<<<ceil_div(p.N, 256), 256, 0, st>>>(p.N, slices, cols, p.db);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t qgrad_scratch(const QGrad&) { return 0; }
-hipError_t launch_qgrad(const QGrad& p, void*, hipStream_t st) {
-  return p.dtype == CONVBN_BF16 ? grad_t<bf16_t>(p, st) : grad_t<float>(p, st);
+size_t qgrad_scratch(const QGrad& p) { return scratch_of(p).total; }
+hipError_t launch_qgrad(const QGrad& p, void* ws, hipStream_t st) {
+  return p.dtype == CONVBN_BF16 ? grad_t<bf16_t>(p, ws, st) : grad_t<float>(p, ws, st);
 }
 
 }  // namespace convbn

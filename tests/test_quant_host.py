@@ -39,7 +39,7 @@ def test_descriptor_mirror_has_the_size_of_the_struct():
 @pytest.mark.parametrize("change,code", [
     (dict(M=-1), B.ERR_SHAPE), (dict(K=0), B.ERR_SHAPE), (dict(N=0), B.ERR_SHAPE), (dict(dtype=2), B.ERR_UNSUPPORTED),
     (dict(ldx=63), B.ERR_SHAPE), (dict(ldz=31), B.ERR_SHAPE), (dict(ldx=-64), B.ERR_SHAPE), (dict(act=1), B.ERR_UNSUPPORTED),
-    (dict(act=16), B.ERR_UNSUPPORTED), (dict(act=4), B.ERR_NULL), (dict(act=8), B.ERR_NULL), (dict(K=131073), B.ERR_UNSUPPORTED),
+    (dict(act=16), B.ERR_UNSUPPORTED), (dict(act=4), B.ERR_NULL), (dict(act=8), B.ERR_NULL), (dict(K=131073), B.ERR_UNSUPPORTED), (dict(N=(1 << 20) + 1), B.ERR_UNSUPPORTED),
     (dict(M=(1 << 30) + 1), B.ERR_UNSUPPORTED), (dict(ldx=1 << 41), B.ERR_UNSUPPORTED)])
 def test_bad_descriptors_of_a_linear_block(change, code):
     d = _qdesc(**change)
@@ -97,6 +97,14 @@ def test_workspace_is_asked_for_and_checked():
     assert _fwd(d, codes=None, scales=None, work=None, nbytes=0) == B.ERR_WORKSPACE
     assert _fwd(d, codes=None, scales=None, nbytes=need - 1) == B.ERR_WORKSPACE
     assert _fwd(d, codes=None, scales=None, work=C.c_void_p(4104)) == B.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("M,K,N", [(0, 64, 40), (1, 1, 1), (0, 1, 1), (1 << 30, 16, 1), (1, 131072, 1 << 20), (4097, 4096, 4096)])
+def test_workspace_query_of_any_size(M, K, N, dtype):
+    d = _qdesc(M=M, K=K, N=N, dtype=dtype)
+    for p in (B.PASS_FWD, B.PASS_BWD):
+        assert B.convbn_qlinear_workspace_bytes(d, p) % 256 == 0
 
 
 def test_native_call_takes_the_descriptors_rows_only():
