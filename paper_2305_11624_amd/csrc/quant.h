@@ -26,7 +26,8 @@ struct QMul {
   const void* qx; const float* sx; const void* qw; const float* sw; const float* b; const void* add;
   void* z;
 };
-hipError_t launch_qmul(const QMul& p, hipStream_t st);
+size_t qmul_scratch(i64 M, int N, int K);
+hipError_t launch_qmul(const QMul& p, void* ws, hipStream_t st);
 
 // dx [M][K] = dz . (sw qw) + add, dW [N][K] = dz^T . (sx qx), db = column sums of dz; dx, dW, db nullable
 struct QGrad {

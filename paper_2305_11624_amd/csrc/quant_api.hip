@@ -59,6 +59,8 @@ convbn_status check_linear(const convbn_qdesc* d, i64* ldx, i64* ldz) {
   TRY_STATUS(check(d, d->K, d->N, ldx, ldz));
   if (d->K > MAX_SUM) return set_error(CONVBN_ERR_UNSUPPORTED, "a sum over more than %d channels", (int)MAX_SUM);
   if (d->N > MAX_OUT) return set_error(CONVBN_ERR_UNSUPPORTED, "more than %d output channels", (int)MAX_OUT);
+  const i64 most = 1LL << 38;   // (more than the card holds; tile counts stay far below 2^31)
+  if (d->M * d->N > most || d->M * d->K > most) return set_error(CONVBN_ERR_UNSUPPORTED, "a tensor of more than 2^38 elements");
   if (d->act & ~(CONVBN_ACT_ADD_OUT | CONVBN_ACT_ADD_IN))
     return set_error(CONVBN_ERR_UNSUPPORTED, "act %d: only the two addends", d->act);
   if (((d->act & CONVBN_ACT_ADD_OUT) && !d->add_out) || ((d->act & CONVBN_ACT_ADD_IN) && !d->add_in))
@@ -91,9 +93,10 @@ QGrad grad_of(const convbn_qdesc* d, i64 ldx, i64 ldz) {
   g.add = (d->act & CONVBN_ACT_ADD_IN) ? d->add_in : nullptr;
   return g;
 }
-// Codes and scales that a forward call does not hand out
-size_t own_codes(const convbn_qdesc* d) { return align_up((size_t)d->M * qrow(d->K), 256); }
-size_t fwd_ws(const convbn_qdesc* d) { return own_codes(d) + align_up((size_t)d->M * 4, 256); }
+// Forward workspace: the product's, then codes and scales that the call does not hand out
+size_t mul_ws(const convbn_qdesc* d) { return qmul_scratch(d->M, d->N, d->K); }
+size_t codes_ws(const convbn_qdesc* d) { return align_up((size_t)d->M * qrow(d->K), 256); }
+size_t fwd_ws(const convbn_qdesc* d) { return mul_ws(d) + codes_ws(d) + align_up((size_t)d->M * 4, 256); }
 
 }  // namespace
 
@@ -134,10 +137,10 @@ convbn_status convbn_qlinear_fwd(const convbn_qdesc* desc, const void* x, void* 
   REQUIRE(w_codes, 16); REQUIRE(w_scales, 4); OPTIONAL(b, 4); REQUIRE_ROWS(z, elem(desc));
   OPTIONAL(desc->add_out, elem(desc));
   if (!desc->M) return CONVBN_OK;
+  TRY_STATUS(check_ws(codes ? mul_ws(desc) : fwd_ws(desc), ws, ws_bytes));
   if (!codes) {
-    TRY_STATUS(check_ws(fwd_ws(desc), ws, ws_bytes));
-    codes = ws;
-    scales = reinterpret_cast<float*>(static_cast<char*>(ws) + own_codes(desc));
+    codes = static_cast<char*>(ws) + mul_ws(desc);
+    scales = reinterpret_cast<float*>(static_cast<char*>(codes) + codes_ws(desc));
   }
   const hipStream_t st = (hipStream_t)stream;
   if (x) LAUNCH(launch_qpack(desc->dtype, desc->M, desc->K, ldx, x, codes, scales, st));
@@ -145,7 +148,7 @@ convbn_status convbn_qlinear_fwd(const convbn_qdesc* desc, const void* x, void* 
   m.M = desc->M; m.ldz = ldz; m.K = desc->K; m.N = desc->N; m.dtype = desc->dtype;
   m.qx = codes; m.sx = scales; m.qw = w_codes; m.sw = w_scales; m.b = b; m.z = z;
   m.add = (desc->act & CONVBN_ACT_ADD_OUT) ? desc->add_out : nullptr;
-  LAUNCH(launch_qmul(m, st));
+  LAUNCH(launch_qmul(m, ws, st));
   return CONVBN_OK;
 }
 

@@ -95,7 +95,7 @@ class Linear:
         self.dx = _new_rows(M, K, self.ldx, dtype, device) if train else None
         self.dW = torch.empty(N, K, dtype=dtype, device=device) if train else None
         self.db = torch.empty(N, dtype=torch.float32, device=device) if train else None
-        need = B.convbn_qlinear_workspace_bytes(self.desc, B.PASS_FWD) if not train else 0
+        need = B.convbn_qlinear_workspace_bytes(self.desc, B.PASS_FWD)
         if train:
             need = max(need, B.convbn_qlinear_workspace_bytes(self.desc, B.PASS_BWD))
         self.ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None

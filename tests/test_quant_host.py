@@ -40,7 +40,8 @@ def test_descriptor_mirror_has_the_size_of_the_struct():
     (dict(M=-1), B.ERR_SHAPE), (dict(K=0), B.ERR_SHAPE), (dict(N=0), B.ERR_SHAPE), (dict(dtype=2), B.ERR_UNSUPPORTED),
     (dict(ldx=63), B.ERR_SHAPE), (dict(ldz=31), B.ERR_SHAPE), (dict(ldx=-64), B.ERR_SHAPE), (dict(act=1), B.ERR_UNSUPPORTED),
     (dict(act=16), B.ERR_UNSUPPORTED), (dict(act=4), B.ERR_NULL), (dict(act=8), B.ERR_NULL), (dict(K=131073), B.ERR_UNSUPPORTED), (dict(N=(1 << 20) + 1), B.ERR_UNSUPPORTED),
-    (dict(M=(1 << 30) + 1), B.ERR_UNSUPPORTED), (dict(ldx=1 << 41), B.ERR_UNSUPPORTED)])
+    (dict(M=(1 << 30) + 1), B.ERR_UNSUPPORTED), (dict(ldx=1 << 41), B.ERR_UNSUPPORTED), (dict(M=1 << 30, K=257), B.ERR_UNSUPPORTED),
+    (dict(M=1 << 30, N=257), B.ERR_UNSUPPORTED)])
 def test_bad_descriptors_of_a_linear_block(change, code):
     d = _qdesc(**change)
     assert _fwd(d) == code and _bwd(d) == code
@@ -100,7 +101,7 @@ def test_workspace_is_asked_for_and_checked():
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("M,K,N", [(0, 64, 40), (1, 1, 1), (0, 1, 1), (1 << 30, 16, 1), (1, 131072, 1 << 20), (4097, 4096, 4096)])
+@pytest.mark.parametrize("M,K,N", [(0, 64, 40), (1, 1, 1), (0, 1, 1), (1 << 30, 16, 1), (1 << 30, 256, 256), (1, 131072, 1 << 20), (4097, 4096, 4096)])
 def test_workspace_query_of_any_size(M, K, N, dtype):
     d = _qdesc(M=M, K=K, N=N, dtype=dtype)
     for p in (B.PASS_FWD, B.PASS_BWD):
