@@ -9,6 +9,44 @@ typedef long long i64;
 // Bytes from one row of codes to the next: whole 16-byte pieces, zero past the last channel.
 inline __host__ __device__ int qrow(int channels) { return (channels + 15) & ~15; }
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// ---- copies from memory into LDS.  Inline asm: what the compiler knows to be such a copy it waits for before every LDS read.
+// `bytes` from p on as a buffer; loads past it return zeros
+__device__ __forceinline__ i32x4 make_desc(const void* p, i64 bytes) {
+  const uint64_t a = (uint64_t)p;
+  const i32x4 d = {(int)(uint32_t)a, (int)(uint32_t)(a >> 32) & 0xffff, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000};
+  return (i32x4){__builtin_amdgcn_readfirstlane(d[0]), __builtin_amdgcn_readfirstlane(d[1]), __builtin_amdgcn_readfirstlane(d[2]),
+                 __builtin_amdgcn_readfirstlane(d[3])};
+}
+__device__ __forceinline__ unsigned lds_off(const void* p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p; }
+// 16 bytes a lane, lane l's to lds + 16 l (lds: the same for the whole wave)
+__device__ __forceinline__ void dma16(i32x4 desc, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(desc));   // (m0 holds nothing between instructions that need it)
+}
+// Until at most N of this wave's copies and loads are in flight; then the workgroup's barrier
+template <int N> __device__ __forceinline__ void landed() {
+  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// Tile (i, j) of nti x ntj and split of a workgroup; false: none.  Workgroups go to the eight XCDs in turn, so each gets a contiguous run
+// of the order, and the order walks bands of 8 rows of tiles: the 32 workgroups that an XCD runs at a time are about 8 x 4 tiles, which
+// share what they read in its cache.
+struct TileAt { int i, j, split; };
+__device__ __forceinline__ bool tile_at(int nti, int ntj, int splits, TileAt* at) {
+  const int total = nti * ntj * splits, run = (total + 7) >> 3, slot = (int)blockIdx.x >> 3;
+  const int id = ((int)blockIdx.x & 7) * run + slot;
+  if (slot >= run || id >= total) return false;
+  at->split = id / (nti * ntj);
+  const int tile = id - at->split * (nti * ntj), band = tile / (8 * ntj), in = tile - band * 8 * ntj;
+  const int h = min(8, nti - band * 8);
+  at->j = in / h;
+  at->i = band * 8 + in - at->j * h;
+  return true;
+}
+
 // ---- rows (quant_rows.hip): ld* in elements ----
 hipError_t launch_qpack(int dtype, i64 rows, int K, i64 ld, const void* x, void* codes, float* scales, hipStream_t st);
 hipError_t launch_qunpack(int dtype, i64 rows, int K, i64 ld, const void* codes, const float* scales, void* x, hipStream_t st);

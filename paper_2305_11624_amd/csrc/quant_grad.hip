@@ -65,14 +65,10 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-  // contiguous runs of tiles to each XCD
-  const int total = p.nti * p.ntj * p.splits, run = (total + 7) >> 3;
-  const int id = ((int)blockIdx.x & 7) * run + ((int)blockIdx.x >> 3);
-  if (((int)blockIdx.x >> 3) >= run || id >= total) return;
-  const int split = id / (p.nti * p.ntj), tile = id - split * (p.nti * p.ntj);
-  const int ti = tile % p.nti, tj = tile / p.nti;
-  const i64 i0 = (i64)ti * TI;
-  const int j0 = tj * TJ;
+  TileAt t;
+  if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
+  const int split = t.split, j0 = t.j * TJ;
+  const i64 i0 = (i64)t.i * TI;
   const int c_beg = split * p.per, c_end = min(p.planes * p.nch, c_beg + p.per);
 
   // ---- this thread's pieces
@@ -90,7 +86,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     } else {
       const int r = w >> 3, g = w & 7;
       a_off[t] = (unsigned)(r * (int)p.lda + g * 8) * 2u;
-      a_lds[t] = r * 128 + ((g ^ (r & 7)) << 4);
+      a_lds[t] = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
       a_col[t] = g * 8;
     }
   }
@@ -156,7 +152,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   auto a_at = [&](int step, int f) {
     if constexpr (TRANS) return (step * 16 + tr_row) * (TI * 2) + ((((wi >> 5) + f) ^ ep) << 6) + tr_col;
     const int row = wi + f * 32 + (lane & 31);
-    return row * 128 + (((step * 2 + kb) ^ (row & 7)) << 4);
+    return row * 128 + (((step * 2 + kb) ^ ((row >> 1) & 7)) << 4);
   };
 
   f32x16 acc[FI][FJ];

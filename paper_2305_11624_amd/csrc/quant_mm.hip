@@ -1,7 +1,7 @@
 // z = sx sw (qx . qw) + b + add: the product of 8-bit integers with a scale for each row of either operand.
 //
 // Both operands' channels run together, which is what the matrix instruction wants; they pass through LDS as rows of 128 codes whose
-// 16-byte pieces are exchanged by the row's low bits, so that 16 lanes reading a column of pieces meet distinct banks.  Sums over
+// 16-byte pieces are exchanged by bits 1-3 of the row, so that 16 lanes reading a column of pieces meet distinct banks.  Sums over
 // channels that are split between workgroups stay whole numbers: any order gives the same.
 #include "quant.h"
 
@@ -9,15 +9,10 @@ namespace convbn {
 
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr unsigned OOB = 0x80000000u;   // beyond any buffer: the load returns zeros
-constexpr int KC = 128;                 // channels at a time
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, i64 bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000);
-}
+constexpr int KC = 128;                 // channels at a time: a whole cache line a row
 
 struct MulParams {
   QMul m;
@@ -26,87 +21,86 @@ struct MulParams {
   int* part;                  // [splits][M][N], where there are several
 };
 
-// Four channels n .. n+3 of row m: scaled, with bias and addend, rounded once
-template <typename T> __device__ __forceinline__ void finish4(const QMul& q, i64 m, int n, const int (&acc)[4], float sx, bool vec) {
+// Eight channels n .. n+7 of row m: scaled, with bias and addend, rounded once.  vec: 16-byte accesses
+template <typename T>
+__device__ __forceinline__ void finish8(const QMul& q, i64 m, int n, const int (&acc)[8], float sx, const float (&sw)[8], const float (&b)[8], bool vec) {
   T* z = static_cast<T*>(q.z) + m * q.ldz + n;
   const T* add = q.add ? static_cast<const T*>(q.add) + m * q.ldz + n : nullptr;
-  float v[4];
+  float v[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool in = n + i < q.N;
-    v[i] = (float)acc[i] * (sx * (in ? q.sw[n + i] : 0.f)) + (q.b && in ? q.b[n + i] : 0.f);
-  }
-  if (vec && n + 4 <= q.N) {
+  for (int i = 0; i < 8; ++i) v[i] = (float)acc[i] * (sx * sw[i]) + b[i];
+  if (vec && n + 8 <= q.N) {
     if constexpr (sizeof(T) == 2) {
       if (add) {
-        const uint2 w = *reinterpret_cast<const uint2*>(add);
+        const uint4 w = *reinterpret_cast<const uint4*>(add);
         v[0] += bf16_lo(w.x); v[1] += bf16_hi(w.x); v[2] += bf16_lo(w.y); v[3] += bf16_hi(w.y);
+        v[4] += bf16_lo(w.z); v[5] += bf16_hi(w.z); v[6] += bf16_lo(w.w); v[7] += bf16_hi(w.w);
       }
-      *reinterpret_cast<uint2*>(z) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      *reinterpret_cast<uint4*>(z) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
     } else {
-      if (add) {
-        const float4 w = *reinterpret_cast<const float4*>(add);
-        v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+#pragma unroll
+      for (int h = 0; h < 8; h += 4) {
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (add) w = *reinterpret_cast<const float4*>(add + h);
+        *reinterpret_cast<float4*>(z + h) = make_float4(v[h] + w.x, v[h + 1] + w.y, v[h + 2] + w.z, v[h + 3] + w.w);
       }
-      *reinterpret_cast<float4*>(z) = make_float4(v[0], v[1], v[2], v[3]);
     }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 8; ++i)
     if (n + i < q.N) z[i] = from_f32<T>(v[i] + (add ? to_f32(add[i]) : 0.f));
 }
 template <typename T> __device__ __forceinline__ bool vectors(const QMul& q) {
-  return ((uintptr_t)q.z | (uintptr_t)(q.ldz * sizeof(T)) | (uintptr_t)q.add) % (4 * sizeof(T)) == 0;
+  return ((uintptr_t)q.z | (uintptr_t)(q.ldz * sizeof(T)) | (uintptr_t)q.add) % 16 == 0;
 }
 
-template <int TI, int TJ, int WI, int WJ> struct MulCfg {
-  static constexpr int NT = 64 * (TI / WI) * (TJ / WJ), STAGE = (TI + TJ) * KC, LDS = 2 * STAGE;
+// A ring of NST stages of KC channels of TI + TJ rows
+template <int TI, int TJ, int WI, int WJ, int NST_> struct MulCfg {
+  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES, STAGE = (TI + TJ) * KC;
+  static constexpr int CPW = (TI + TJ) / 8 / WAVES;   // copies a wave, 8 rows each
+  static constexpr int PITCH = WJ * 4 + 16, OUT = WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
+  static constexpr int LDS = NST * STAGE > OUT ? NST * STAGE : OUT;
+  static_assert((TI + TJ) % (16 * WAVES) == 0 && TI % 16 == 0, "whole pairs of copies");
 };
 
-template <typename T, int TI, int TJ, int WI, int WJ, bool SPLIT>
+template <typename T, int TI, int TJ, int WI, int WJ, int NST, bool SPLIT>
 __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulParams p) {
-  using Cfg = MulCfg<TI, TJ, WI, WJ>;
-  constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32, PA = TI * 8 / NT, PB = TJ * 8 / NT;
+  using Cfg = MulCfg<TI, TJ, WI, WJ, NST>;
+  constexpr int FI = WI / 32, FJ = WJ / 32, CPW = Cfg::CPW;
   extern __shared__ __align__(16) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int total = p.nti * p.ntj * p.splits, run = (total + 7) >> 3;   // contiguous runs of tiles to each XCD
-  const int id = ((int)blockIdx.x & 7) * run + ((int)blockIdx.x >> 3);
-  if (((int)blockIdx.x >> 3) >= run || id >= total) return;
-  const int split = id / (p.nti * p.ntj), tile = id - split * (p.nti * p.ntj);
-  const i64 i0 = (i64)(tile % p.nti) * TI;
-  const int j0 = tile / p.nti * TJ;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  TileAt t;
+  if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
+  const int split = t.split, j0 = t.j * TJ;
+  const i64 i0 = (i64)t.i * TI;
   const int c_beg = split * p.per, c_end = min(p.nch, c_beg + p.per);
 
+  // ---- copies: lane l puts 16 codes into piece l % 8 of row l / 8; rows past the end lie past the buffer
   const i64 rows_a = p.m.M - i0 < TI ? p.m.M - i0 : TI;
   const int rows_b = min(p.m.N - j0, TJ);
-  const __amdgpu_buffer_rsrc_t ra = make_rsrc(static_cast<const uint8_t*>(p.m.qx) + i0 * p.Kp, rows_a * p.Kp);
-  const __amdgpu_buffer_rsrc_t rb = make_rsrc(static_cast<const uint8_t*>(p.m.qw) + (i64)j0 * p.Kp, (i64)rows_b * p.Kp);
-  // piece w of a chunk: row w / 8, 16 codes from 16 (w % 8); rows past the end lie past the buffer
-  const int g = tid & 7, row0 = tid >> 3;
-  const unsigned off0 = (unsigned)(row0 * p.Kp + g * 16), step = (unsigned)(NT / 8) * (unsigned)p.Kp;
-  const unsigned lds0 = row0 * KC + ((g ^ (row0 & 7)) << 4);
-  static_assert(NT / 8 % 8 == 0, "a thread's pieces are exchanged alike");
-  i32x4 a_reg[PA], b_reg[PB];
-  auto fetch = [&](int c) {
+  const i32x4 ra = make_desc(static_cast<const uint8_t*>(p.m.qx) + i0 * p.Kp, rows_a * p.Kp);
+  const i32x4 rb = make_desc(static_cast<const uint8_t*>(p.m.qw) + (i64)j0 * p.Kp, (i64)rows_b * p.Kp);
+  const int g16 = ((lane & 7) ^ (lane >> 4)) * 16;   // (a wave's odd copies: ^ 64)
+  unsigned off[CPW];
+#pragma unroll
+  for (int i = 0; i < CPW; ++i) {
+    const int copy = wave * CPW + i, row = copy < TI / 8 ? copy * 8 : copy * 8 - TI;
+    off[i] = (unsigned)(row + (lane >> 3)) * (unsigned)p.Kp + (g16 ^ (i & 1) * 64);
+  }
+  const unsigned lds0 = lds_off(smem) + wave * CPW * 1024;
+  auto issue = [&](int c, int slot) {   // (chunks past the end are copied as zeros: every wave has the same copies in flight)
     const unsigned k = (unsigned)c * KC;
-    const bool in = (int)k + g * 16 < p.Kp;
+    const bool in[2] = {c < c_end && (int)k + g16 < p.Kp, c < c_end && (int)k + (g16 ^ 64) < p.Kp};
 #pragma unroll
-    for (int t = 0; t < PA; ++t) a_reg[t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(in ? off0 + t * step + k : OOB), 0, 0);
-#pragma unroll
-    for (int t = 0; t < PB; ++t) b_reg[t] = __builtin_amdgcn_raw_buffer_load_b128(rb, (int)(in ? off0 + t * step + k : OOB), 0, 0);
-  };
-  auto put = [&](unsigned char* stage) {
-#pragma unroll
-    for (int t = 0; t < PA; ++t) *reinterpret_cast<i32x4*>(stage + lds0 + t * (NT / 8) * KC) = a_reg[t];
-#pragma unroll
-    for (int t = 0; t < PB; ++t) *reinterpret_cast<i32x4*>(stage + TI * KC + lds0 + t * (NT / 8) * KC) = b_reg[t];
+    for (int i = 0; i < CPW; ++i)
+      dma16(wave * CPW + i < TI / 8 ? ra : rb, in[i & 1] ? off[i] + k : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
   };
 
   const int wi = (wave % (TI / WI)) * WI, wj = (wave / (TI / WI)) * WJ, kb = lane >> 5;
-  auto at = [&](int first, int step_, int f) {   // 16 codes of row l % 32, from 32 step + 16 (l / 32)
+  auto at = [&](int first, int step, int f) {   // 16 codes of row l % 32, from 32 step + 16 (l / 32)
     const int row = first + f * 32 + (lane & 31);
-    return row * KC + (((step_ * 2 + kb) ^ (row & 7)) << 4);
+    return row * KC + (((step * 2 + kb) ^ ((row >> 1) & 7)) << 4);
   };
   i32x16 acc[FI][FJ];
 #pragma unroll
@@ -116,16 +110,14 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
-  fetch(c_beg);
-  put(smem);
-  if (c_beg + 1 < c_end) fetch(c_beg + 1);
-  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < NST - 1; ++s) issue(c_beg + s, s);
+  int slot = 0;
   for (int c = c_beg; c < c_end; ++c) {
-    const unsigned char* cur = smem + ((c - c_beg) & 1) * Cfg::STAGE;
-    if (c + 1 < c_end) {
-      put(smem + ((c - c_beg + 1) & 1) * Cfg::STAGE);
-      if (c + 2 < c_end) fetch(c + 2);
-    }
+    landed<CPW * (NST - 2)>();   // this chunk's copies, for all waves; and all have read the chunk before
+    issue(c + NST - 1, slot ? slot - 1 : NST - 1);
+    const unsigned char* cur = smem + slot * Cfg::STAGE;
+    slot = slot + 1 == NST ? 0 : slot + 1;
 #pragma unroll
     for (int s = 0; s < KC / 32; ++s) {
       i32x4 af[FI], bf[FJ];
@@ -138,59 +130,87 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
 #pragma unroll
         for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[j], af[i], acc[i][j], 0, 0, 0);
     }
-    __syncthreads();
   }
+  landed<0>();
 
-  // a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..
+  // ---- out, 32 rows of this wave at a time: a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..;
+  // through LDS they become whole rows (8 bytes a row straight from the registers: 30 % of the pass at 8192 x 4096 x 8192)
+  constexpr int LPR = WJ / 8;   // lanes a row, 8 channels each
+  unsigned char* mine = smem + wave * 32 * Cfg::PITCH;
+  const int col = (lane % LPR) * 8, n = j0 + wj + col;
+  float sw[8], b[8];
+  if constexpr (!SPLIT) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      sw[x] = n + x < p.m.N ? p.m.sw[n + x] : 0.f;
+      b[x] = p.m.b && n + x < p.m.N ? p.m.b[n + x] : 0.f;
+    }
+  }
   const bool vec = SPLIT ? p.m.N % 4 == 0 : vectors<T>(p.m);
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
-    const i64 m = i0 + wi + i * 32 + (lane & 31);
-    if (m >= p.m.M) continue;
-    const float sx = SPLIT ? 0.f : p.m.sx[m];
 #pragma unroll
     for (int j = 0; j < FJ; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int n = j0 + wj + j * 32 + 8 * (e >> 2) + 4 * kb;
-        if (n >= p.m.N) continue;
-        const int v[4] = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        if constexpr (SPLIT) {
-          int* o = p.part + (split * p.m.M + m) * p.m.N + n;
-          if (vec) {
-            *reinterpret_cast<int4*>(o) = make_int4(v[0], v[1], v[2], v[3]);
-          } else {
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<i32x4*>(mine + (lane & 31) * Cfg::PITCH + (j * 32 + 8 * (e >> 2) + 4 * kb) * 4) =
+            (i32x4){acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (n + x < p.m.N) o[x] = v[x];
-          }
-        } else {
-          finish4<T>(p.m, m, n, v, sx, vec);
-        }
+    for (int r = 0; r < 32; r += 64 / LPR) {
+      const int row = r + lane / LPR;
+      const i64 m = i0 + wi + i * 32 + row;
+      int v[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const i32x4 w = *reinterpret_cast<const i32x4*>(mine + row * Cfg::PITCH + col * 4 + h * 16);
+        v[4 * h] = w[0]; v[4 * h + 1] = w[1]; v[4 * h + 2] = w[2]; v[4 * h + 3] = w[3];
       }
+      if (m >= p.m.M || n >= p.m.N) continue;
+      if constexpr (SPLIT) {
+        int* o = p.part + (split * p.m.M + m) * p.m.N + n;
+        if (vec && n + 8 <= p.m.N) {
+          *reinterpret_cast<int4*>(o) = make_int4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<int4*>(o + 4) = make_int4(v[4], v[5], v[6], v[7]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            if (n + x < p.m.N) o[x] = v[x];
+        }
+      } else {
+        finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b, vec);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
 template <typename T> __global__ __launch_bounds__(256) void qmul_join_kernel(MulParams p) {
-  const int quads = (p.m.N + 3) >> 2;
-  const i64 total = p.m.M * quads;
-  const bool vec = vectors<T>(p.m), pvec = p.m.N % 4 == 0;
+  const int oct = (p.m.N + 7) >> 3;
+  const i64 total = p.m.M * oct;
+  const bool vec = vectors<T>(p.m), pvec = p.m.N % 8 == 0;
   for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
-    const i64 m = x / quads;
-    const int n = (int)(x - m * quads) * 4;
-    int v[4] = {0, 0, 0, 0};
+    const i64 m = x / oct;
+    const int n = (int)(x - m * oct) * 8;
+    int v[8] = {};
     for (int s = 0; s < p.splits; ++s) {
       const int* o = p.part + (s * p.m.M + m) * p.m.N + n;
       if (pvec) {
-        const int4 w = *reinterpret_cast<const int4*>(o);
-        v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+        const int4 w = *reinterpret_cast<const int4*>(o), u = *reinterpret_cast<const int4*>(o + 4);
+        v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w; v[4] += u.x; v[5] += u.y; v[6] += u.z; v[7] += u.w;
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
           if (n + i < p.m.N) v[i] += o[i];
       }
     }
-    finish4<T>(p.m, m, n, v, p.m.sx[m], vec);
+    float sw[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sw[i] = n + i < p.m.N ? p.m.sw[n + i] : 0.f;
+      b[i] = p.m.b && n + i < p.m.N ? p.m.b[n + i] : 0.f;
+    }
+    finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b, vec);
   }
 }
 
@@ -214,25 +234,25 @@ Plan plan_of(i64 M, int N, int K) {
   return pl;
 }
 
-template <typename T, int TI, int TJ, int WI, int WJ, bool SPLIT> hipError_t launch_tiles(const MulParams& p, hipStream_t st) {
-  using Cfg = MulCfg<TI, TJ, WI, WJ>;
+template <typename T, int TI, int TJ, int WI, int WJ, int NST, bool SPLIT> hipError_t launch_tiles(const MulParams& p, hipStream_t st) {
+  using Cfg = MulCfg<TI, TJ, WI, WJ, NST>;
   static LdsLimitOnce once;
-  auto* k = &qmul_kernel<T, TI, TJ, WI, WJ, SPLIT>;
+  auto* k = &qmul_kernel<T, TI, TJ, WI, WJ, NST, SPLIT>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   k<<<(p.nti * p.ntj * p.splits + 7) / 8 * 8, Cfg::NT, Cfg::LDS, st>>>(p);
   return hipGetLastError();
 }
 template <typename T, bool SPLIT> hipError_t by_tile(int tile, const MulParams& p, hipStream_t st) {
-  if (tile == 256) return launch_tiles<T, 256, 256, 64, 128, SPLIT>(p, st);
-  if (tile == 128) return launch_tiles<T, 128, 128, 64, 64, SPLIT>(p, st);
-  return launch_tiles<T, 64, 64, 32, 32, SPLIT>(p, st);
+  if (tile == 256) return launch_tiles<T, 256, 256, 64, 128, 2, SPLIT>(p, st);
+  if (tile == 128) return launch_tiles<T, 128, 128, 64, 64, 2, SPLIT>(p, st);
+  return launch_tiles<T, 64, 64, 32, 32, 4, SPLIT>(p, st);
 }
 template <typename T> hipError_t mul_t(const MulParams& p, int tile, hipStream_t st) {
   if (p.splits == 1) return by_tile<T, false>(tile, p, st);
   const hipError_t e = by_tile<int, true>(tile, p, st);
   if (e != hipSuccess) return e;
-  const i64 blocks = (p.m.M * ((p.m.N + 3) >> 2) + 255) / 256;
+  const i64 blocks = (p.m.M * ((p.m.N + 7) >> 3) + 255) / 256;
   qmul_join_kernel<T><<<(int)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(p);
   return hipGetLastError();
 }
