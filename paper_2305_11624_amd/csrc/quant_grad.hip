@@ -13,7 +13,6 @@ namespace convbn {
 namespace {
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr unsigned OOB = 0x80000000u;   // beyond any buffer: the load returns zeros
@@ -41,7 +40,11 @@ struct GradParams {
 
 template <int TI, int TJ, int WI, int WJ> struct GradCfg {
   static constexpr int WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;
-  static constexpr int A_BYTES = TI * RC * 2, B_BYTES = TJ * RC * 2, STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
+  static constexpr int A_BYTES = TI * RC * 2, STAGE = A_BYTES + TJ * RC * 2;
+  static constexpr int CPW = A_BYTES / 1024 / WAVES;   // copies a wave
+  static constexpr int PITCH = WJ * 4 + 16, OUT_BYTES = WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
+  static constexpr int LDS = 2 * STAGE > OUT_BYTES ? 2 * STAGE : OUT_BYTES;
+  static_assert(A_BYTES % (2048 * WAVES) == 0, "whole pairs of copies");
 };
 
 // Two codes to bf16 numbers s q
@@ -56,40 +59,80 @@ __device__ __forceinline__ bf16x8 read_tr8(const unsigned char* p, int rows4) { 
   return __builtin_bit_cast(bf16x8, (s16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
 }
 
+// Eight channels of a row (`left` of them inside), with the addend; vec: 16-byte accesses
+template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT* add, float (&v)[8], bool vec, int left) {
+  if (vec && left >= 8) {
+    if constexpr (sizeof(OUT) == 2) {
+      if (add) {
+        const uint4 w = *reinterpret_cast<const uint4*>(add);
+        v[0] += bf16_lo(w.x); v[1] += bf16_hi(w.x); v[2] += bf16_lo(w.y); v[3] += bf16_hi(w.y);
+        v[4] += bf16_lo(w.z); v[5] += bf16_hi(w.z); v[6] += bf16_lo(w.w); v[7] += bf16_hi(w.w);
+      }
+      *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 8; h += 4) {
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (add) w = *reinterpret_cast<const float4*>(add + h);
+        *reinterpret_cast<float4*>(o + h) = make_float4(v[h] + w.x, v[h + 1] + w.y, v[h + 2] + w.z, v[h + 3] + w.w);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int x = 0; x < 8; ++x)
+    if (x < left) o[x] = from_f32<OUT>(v[x] + (add ? to_f32(add[x]) : 0.f));
+}
+
 // OUT: float or bf16_t.  TRANS: A(i, r) = A[r][i].
 template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ>
 __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradParams p) {
   using Cfg = GradCfg<TI, TJ, WI, WJ>;
   constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
-  constexpr int PA = TI * 8 / NT, PB = TJ * 8 / NT;   // 16-byte pieces of A and 8-code pieces of q that a thread moves per chunk
   extern __shared__ __align__(16) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   TileAt t;
   if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
   const int split = t.split, j0 = t.j * TJ;
   const i64 i0 = (i64)t.i * TI;
   const int c_beg = split * p.per, c_end = min(p.planes * p.nch, c_beg + p.per);
 
-  // ---- this thread's pieces
-  unsigned a_off[PA], b_off[PB];   // byte offsets of the first chunk's pieces
-  unsigned a_lds[PA], b_lds[PB], s_off[PB];
-  int a_col[PA];                   // direct: channel within the chunk
+  // ---- copies of A: 8 rows of 64 channels (direct) or 1 KB of rows of TI channels
+  constexpr int CPW = Cfg::CPW, RPC = TRANS ? 512 / TI : 8;   // rows a copy
+  unsigned a_off[CPW];
+  const int dg = ((lane & 7) ^ (lane >> 4)) * 8;   // direct: this lane's channels in a chunk (a wave's odd copies: ^ 32)
 #pragma unroll
-  for (int t = 0; t < PA; ++t) {
-    const int w = t * NT + tid;
+  for (int i = 0; i < CPW; ++i) {
+    const int r = (wave * CPW + i) * RPC + lane / (64 / RPC);
     if constexpr (TRANS) {
-      const int r = w / (TI / 8), g = w % (TI / 8);
-      a_off[t] = i0 + g * 8 < p.Aw ? (unsigned)(r * (int)p.lda + g * 8) * 2u : OOB;
-      a_lds[t] = r * (TI * 2) + (((g >> 2) ^ (r & 3)) << 6) + (g & 3) * 16;
-      a_col[t] = 0;
+      const int l = lane % (TI / 8), g = ((((l >> 2) ^ (r & 3)) << 2) | (l & 3)) * 8;   // 64-byte pieces are exchanged by the row's low bits
+      a_off[i] = i0 + g < p.Aw ? (unsigned)(r * (int)p.lda + g) * 2u : OOB;
     } else {
-      const int r = w >> 3, g = w & 7;
-      a_off[t] = (unsigned)(r * (int)p.lda + g * 8) * 2u;
-      a_lds[t] = r * 128 + ((g ^ ((r >> 1) & 7)) << 4);
-      a_col[t] = g * 8;
+      a_off[i] = (unsigned)(r * (int)p.lda + (dg ^ (i & 1) * 32)) * 2u;
     }
   }
+  const unsigned lds0 = lds_off(smem) + wave * CPW * 1024;
+  struct Source { i32x4 desc; i64 r0; };
+  auto source = [&](int c) {
+    const int plane = c / p.nch;
+    Source s;
+    s.r0 = (i64)(c - plane * p.nch) * RC;
+    const i64 left = p.R - s.r0 < RC ? p.R - s.r0 : RC, rows = p.I - i0 < TI ? p.I - i0 : TI;
+    const bf16_t* A = p.A + plane * p.plane;
+    s.desc = TRANS ? make_desc(A + s.r0 * p.lda + i0, ((left - 1) * p.lda + p.Aw - i0) * 2)
+                   : make_desc(A + i0 * p.lda + s.r0, ((rows - 1) * p.lda + p.Aw - s.r0) * 2);
+    return s;
+  };
+  auto issue = [&](const Source& s, int slot, int from, int to) {
+    const bool in[2] = {TRANS || s.r0 + dg < p.Aw, TRANS || s.r0 + (dg ^ 32) < p.Aw};
+#pragma unroll
+    for (int i = 0; i < CPW; ++i)
+      if (i >= from && i < to) dma16(s.desc, in[i & 1] ? a_off[i] : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
+  };
+
+  // ---- codes: 8 a piece
+  constexpr int PB = TJ * 8 / NT;
+  unsigned b_off[PB], b_lds[PB], s_off[PB];
 #pragma unroll
   for (int t = 0; t < PB; ++t) {
     const int w = t * NT + tid;
@@ -98,46 +141,32 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     b_lds[t] = r * (TJ * 2) + (((g >> 2) ^ (r & 3)) << 6) + (g & 3) * 16;
     s_off[t] = r * 4;
   }
-
-  i32x4 a_reg[PA];
-  i32x2 b_reg[PB];
-  float s_reg[PB];
+  struct Codes { i32x2 q[PB]; float s[PB]; };
   auto fetch = [&](int c) {
-    const int plane = c / p.nch;
-    const i64 r0 = (i64)(c - plane * p.nch) * RC;
+    Codes b;
+    const i64 r0 = (i64)(c % p.nch) * RC;
     const i64 left = p.R - r0 < RC ? p.R - r0 : RC;
-    const bf16_t* A = p.A + plane * p.plane;
-    if constexpr (TRANS) {
-      const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + r0 * p.lda + i0, ((left - 1) * p.lda + p.Aw - i0) * 2);
-#pragma unroll
-      for (int t = 0; t < PA; ++t) a_reg[t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)a_off[t], 0, 0);
-    } else {
-      const i64 rows = p.I - i0 < TI ? p.I - i0 : TI;
-      const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + i0 * p.lda + r0, ((rows - 1) * p.lda + p.Aw - r0) * 2);
-#pragma unroll
-      for (int t = 0; t < PA; ++t)
-        a_reg[t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(r0 + a_col[t] < p.Aw ? a_off[t] : OOB), 0, 0);
-    }
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(p.q + r0 * p.Jp + j0, left * p.Jp - j0);
 #pragma unroll
-    for (int t = 0; t < PB; ++t) b_reg[t] = __builtin_amdgcn_raw_buffer_load_b64(rq, (int)b_off[t], 0, 0);
+    for (int t = 0; t < PB; ++t) b.q[t] = __builtin_amdgcn_raw_buffer_load_b64(rq, (int)b_off[t], 0, 0);
     if (p.s) {
       const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.s + r0, left * 4);
 #pragma unroll
-      for (int t = 0; t < PB; ++t) s_reg[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
+      for (int t = 0; t < PB; ++t) b.s[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
     } else {
 #pragma unroll
-      for (int t = 0; t < PB; ++t) s_reg[t] = 1.f;
+      for (int t = 0; t < PB; ++t) b.s[t] = 1.f;
     }
+    return b;
   };
-  auto put = [&](unsigned char* stage) {
-#pragma unroll
-    for (int t = 0; t < PA; ++t) *reinterpret_cast<i32x4*>(stage + a_lds[t]) = a_reg[t];
+  auto put = [&](const Codes& b, int slot, int from, int to) {
 #pragma unroll
     for (int t = 0; t < PB; ++t) {
-      const uint32_t lo = b_reg[t][0], hi = b_reg[t][1];
-      const float s = s_reg[t];
-      *reinterpret_cast<uint4*>(stage + Cfg::A_BYTES + b_lds[t]) = make_uint4(code2(lo, 0, s), code2(lo, 2, s), code2(hi, 0, s), code2(hi, 2, s));
+      if (t < from || t >= to) continue;
+      const uint32_t lo = b.q[t][0], hi = b.q[t][1];
+      const float s = b.s[t];
+      *reinterpret_cast<uint4*>(smem + slot * Cfg::STAGE + Cfg::A_BYTES + b_lds[t]) =
+          make_uint4(code2(lo, 0, s), code2(lo, 2, s), code2(hi, 0, s), code2(hi, 2, s));
     }
   };
 
@@ -164,18 +193,20 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
   if (c_beg < c_end) {
-    fetch(c_beg);
-    put(smem);
-    if (c_beg + 1 < c_end) fetch(c_beg + 1);
-    __syncthreads();
+    issue(source(c_beg), 0, 0, CPW);
+    put(fetch(c_beg), 0, 0, PB);
+    Codes next = fetch(c_beg + 1 < c_end ? c_beg + 1 : c_beg);
     for (int c = c_beg; c < c_end; ++c) {
-      const unsigned char* cur = smem + ((c - c_beg) & 1) * Cfg::STAGE;
-      if (c + 1 < c_end) {
-        put(smem + ((c - c_beg + 1) & 1) * Cfg::STAGE);
-        if (c + 2 < c_end) fetch(c + 2);
-      }
+      landed<0>();   // this chunk is in place for all waves, and all have read the one before
+      const int slot = (c - c_beg) & 1;
+      const unsigned char* cur = smem + slot * Cfg::STAGE;
+      const Codes b = next;
+      const bool more = c + 1 < c_end;
+      if (c + 2 < c_end) next = fetch(c + 2);
+      const Source src = source(more ? c + 1 : c);
 #pragma unroll
       for (int step = 0; step < RC / 16; ++step) {
+        if (more) issue(src, slot ^ 1, step * CPW / 2, (step + 1) * CPW / 2);
         bf16x8 af[FI], bf[FJ];
 #pragma unroll
         for (int f = 0; f < FI; ++f) {
@@ -184,54 +215,48 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
         }
 #pragma unroll
         for (int f = 0; f < FJ; ++f) bf[f] = read_tr8(cur + b_at(step, f), 4 * TJ * 2);
+        if (more) put(b, slot ^ 1, step * PB / 4, (step + 1) * PB / 4);
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
           for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
       }
-      __syncthreads();
     }
+    landed<0>();
   }
 
-  // ---- a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..
-  OUT* C = static_cast<OUT*>(p.C);
+  // ---- out, 32 rows of this wave at a time: a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..;
+  // through LDS they become whole rows
+  constexpr int LPR = WJ / 8;   // lanes a row, 8 channels each
+  unsigned char* mine = smem + wave * 32 * Cfg::PITCH;
+  const int col = (lane % LPR) * 8, n = j0 + wj + col;
+  OUT* C = static_cast<OUT*>(p.C) + (p.splits > 1 ? (i64)split * p.I * p.ldc : 0);
   const OUT* add = static_cast<const OUT*>(p.add);
-  i64 ldc = p.ldc;
-  if (p.splits > 1) { C += (i64)split * p.I * ldc; }
-  const bool vec = ((uintptr_t)C | (uintptr_t)(ldc * sizeof(OUT)) | (uintptr_t)add) % (4 * sizeof(OUT)) == 0;
+  const bool vec = ((uintptr_t)C | (uintptr_t)(p.ldc * sizeof(OUT)) | (uintptr_t)add) % 16 == 0;
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
-    const i64 row = i0 + wi + i * 32 + (lane & 31);
-    if (row >= p.I) continue;
 #pragma unroll
     for (int j = 0; j < FJ; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        const int col = j0 + wj + j * 32 + 8 * (e >> 2) + 4 * kb;
-        if (col >= p.J) continue;
-        float v[4] = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        OUT* o = C + row * ldc + col;
-        const OUT* a = add ? add + row * ldc + col : nullptr;
-        if (vec && col + 4 <= p.J) {
-          if constexpr (sizeof(OUT) == 2) {
-            if (a) {
-              const uint2 w = *reinterpret_cast<const uint2*>(a);
-              v[0] += bf16_lo(w.x); v[1] += bf16_hi(w.x); v[2] += bf16_lo(w.y); v[3] += bf16_hi(w.y);
-            }
-            *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-          } else {
-            if (a) {
-              const float4 w = *reinterpret_cast<const float4*>(a);
-              v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
-            }
-            *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-          }
-        } else {
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<float4*>(mine + (lane & 31) * Cfg::PITCH + (j * 32 + 8 * (e >> 2) + 4 * kb) * 4) =
+            make_float4(acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]);
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (col + x < p.J) o[x] = from_f32<OUT>(v[x] + (a ? to_f32(a[x]) : 0.f));
-        }
+    for (int r = 0; r < 32; r += 64 / LPR) {
+      const int at = r + lane / LPR;
+      const i64 row = i0 + wi + i * 32 + at;
+      float v[8];
+#pragma unroll
+      for (int h = 0; h < 8; h += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(mine + at * Cfg::PITCH + (col + h) * 4);
+        v[h] = w.x; v[h + 1] = w.y; v[h + 2] = w.z; v[h + 3] = w.w;
       }
+      if (row >= p.I || n >= p.J) continue;
+      OUT* o = C + row * p.ldc + n;
+      store8<OUT>(o, add ? add + row * p.ldc + n : nullptr, v, vec, p.J - n);
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 

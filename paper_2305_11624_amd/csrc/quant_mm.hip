@@ -89,12 +89,12 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
     off[i] = (unsigned)(row + (lane >> 3)) * (unsigned)p.Kp + (g16 ^ (i & 1) * 64);
   }
   const unsigned lds0 = lds_off(smem) + wave * CPW * 1024;
-  auto issue = [&](int c, int slot) {   // (chunks past the end are copied as zeros: every wave has the same copies in flight)
+  auto issue = [&](int c, int slot, int from, int to) {   // (chunks past the end are copied as zeros: every wave has the same copies in flight)
     const unsigned k = (unsigned)c * KC;
     const bool in[2] = {c < c_end && (int)k + g16 < p.Kp, c < c_end && (int)k + (g16 ^ 64) < p.Kp};
 #pragma unroll
     for (int i = 0; i < CPW; ++i)
-      dma16(wave * CPW + i < TI / 8 ? ra : rb, in[i & 1] ? off[i] + k : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
+      if (i >= from && i < to) dma16(wave * CPW + i < TI / 8 ? ra : rb, in[i & 1] ? off[i] + k : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
   };
 
   const int wi = (wave % (TI / WI)) * WI, wj = (wave / (TI / WI)) * WJ, kb = lane >> 5;
@@ -111,15 +111,18 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
 #pragma unroll
-  for (int s = 0; s < NST - 1; ++s) issue(c_beg + s, s);
+  for (int s = 0; s < NST - 1; ++s) issue(c_beg + s, s, 0, CPW);
   int slot = 0;
   for (int c = c_beg; c < c_end; ++c) {
     landed<CPW * (NST - 2)>();   // this chunk's copies, for all waves; and all have read the chunk before
-    issue(c + NST - 1, slot ? slot - 1 : NST - 1);
+    const int fill = slot ? slot - 1 : NST - 1;
     const unsigned char* cur = smem + slot * Cfg::STAGE;
     slot = slot + 1 == NST ? 0 : slot + 1;
 #pragma unroll
     for (int s = 0; s < KC / 32; ++s) {
+      // the copies, spread over half of the chunk's multiplies: all of them behind the barrier keep the waves from their first
+      // multiplies (8192 x 4096 x 8192: 246 us; over the first half 240, over all of it 237, but 1568 x 8192 x 2048 43, 42 and 45)
+      issue(c + NST - 1, fill, s * CPW / 2, (s + 1) * CPW / 2);
       i32x4 af[FI], bf[FJ];
 #pragma unroll
       for (int f = 0; f < FI; ++f) af[f] = *reinterpret_cast<const i32x4*>(cur + at(wi, s, f));
@@ -223,7 +226,7 @@ Plan plan_of(i64 M, int N, int K) {
   const int nch = ceil_div(qrow(K), KC);
   pl.per = nch;
   if (M == 0) return pl;
-  pl.tile = tiles(256) >= CUS ? 256 : M > 64 && tiles(128) >= CUS / 4 ? 128 : 64;
+  pl.tile = tiles(256) >= CUS && N > 128 ? 256 : M > 64 && tiles(128) >= CUS / 4 ? 128 : 64;
   const i64 t = tiles(pl.tile);
   const i64 want = pl.tile == 64 ? 2 * CUS : CUS;
   i64 s = t < want ? want / t : 1;
