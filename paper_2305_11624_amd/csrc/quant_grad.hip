@@ -112,22 +112,31 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     }
   }
   const unsigned lds0 = lds_off(smem) + wave * CPW * 1024;
-  struct Source { i32x4 desc; i64 r0; };
-  auto source = [&](int c) {
-    const int plane = c / p.nch;
-    Source s;
-    s.r0 = (i64)(c - plane * p.nch) * RC;
-    const i64 left = p.R - s.r0 < RC ? p.R - s.r0 : RC, rows = p.I - i0 < TI ? p.I - i0 : TI;
-    const bf16_t* A = p.A + plane * p.plane;
-    s.desc = TRANS ? make_desc(A + s.r0 * p.lda + i0, ((left - 1) * p.lda + p.Aw - i0) * 2)
-                   : make_desc(A + i0 * p.lda + s.r0, ((rows - 1) * p.lda + p.Aw - s.r0) * 2);
-    return s;
+  // Where the next chunk of A starts; past the last one (c >= c_end) nothing is in bounds and zeros are copied: the loop has no branch
+  const int R = (int)p.R;
+  int a_r0 = (c_beg % p.nch) * RC, a_c = c_beg;
+  const bf16_t* a_plane = p.A + (c_beg / p.nch) * p.plane + (TRANS ? i0 : i0 * p.lda);
+  const i64 a_rows = p.I - i0 < TI ? p.I - i0 : TI;
+  const i64 a_step = TRANS ? RC * p.lda : RC, a_full = TRANS ? ((RC - 1) * p.lda + p.Aw - i0) * 2 : ((a_rows - 1) * p.lda + p.Aw) * 2;
+  const int left_last = R - (p.nch - 1) * RC;
+  const i64 a_last = TRANS ? ((left_last - 1) * p.lda + p.Aw - i0) * 2 : 0;
+  const bf16_t* a_ptr = a_plane + (c_beg % p.nch) * a_step;
+  i32x4 a_desc;
+  bool a_in[2];
+  auto next_a = [&]() {
+    const bool last = a_r0 + RC >= R, live = a_c < c_end;
+    a_desc = make_desc(a_ptr, !live ? 0 : TRANS ? (last ? a_last : a_full) : a_full - a_r0 * 2);
+    a_in[0] = TRANS || a_r0 + dg < p.Aw;
+    a_in[1] = TRANS || a_r0 + (dg ^ 32) < p.Aw;
+    ++a_c;
+    a_r0 = last ? 0 : a_r0 + RC;
+    a_plane = last ? a_plane + p.plane : a_plane;
+    a_ptr = last ? a_plane : a_ptr + a_step;
   };
-  auto issue = [&](const Source& s, int slot, int from, int to) {
-    const bool in[2] = {TRANS || s.r0 + dg < p.Aw, TRANS || s.r0 + (dg ^ 32) < p.Aw};
+  auto issue = [&](int slot, int from, int to) {
 #pragma unroll
     for (int i = 0; i < CPW; ++i)
-      if (i >= from && i < to) dma16(s.desc, in[i & 1] ? a_off[i] : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
+      if (i >= from && i < to) dma16(a_desc, a_in[i & 1] ? a_off[i] : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
   };
 
   // ---- codes: 8 a piece
@@ -142,21 +151,22 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     s_off[t] = r * 4;
   }
   struct Codes { i32x2 q[PB]; float s[PB]; };
-  auto fetch = [&](int c) {
+  int q_r0 = (c_beg % p.nch) * RC, q_c = c_beg;
+  const uint8_t* q_ptr = p.q + j0 + (i64)q_r0 * p.Jp;
+  auto fetch = [&]() {
     Codes b;
-    const i64 r0 = (i64)(c % p.nch) * RC;
-    const i64 left = p.R - r0 < RC ? p.R - r0 : RC;
-    const __amdgpu_buffer_rsrc_t rq = make_rsrc(p.q + r0 * p.Jp + j0, left * p.Jp - j0);
+    const bool last = q_r0 + RC >= R;
+    const int left = q_c < c_end ? last ? left_last : RC : 0;
+    const __amdgpu_buffer_rsrc_t rq = make_rsrc(q_ptr, left ? left * p.Jp - j0 : 0);
 #pragma unroll
     for (int t = 0; t < PB; ++t) b.q[t] = __builtin_amdgcn_raw_buffer_load_b64(rq, (int)b_off[t], 0, 0);
-    if (p.s) {
-      const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.s + r0, left * 4);
+    // (no scales: the codes themselves; the buffer is empty then and what it returns is replaced)
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.s + q_r0, p.s ? left * 4 : 0);
 #pragma unroll
-      for (int t = 0; t < PB; ++t) b.s[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
-    } else {
-#pragma unroll
-      for (int t = 0; t < PB; ++t) b.s[t] = 1.f;
-    }
+    for (int t = 0; t < PB; ++t) b.s[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
+    ++q_c;
+    q_r0 = last ? 0 : q_r0 + RC;
+    q_ptr = last ? p.q + j0 : q_ptr + RC * p.Jp;
     return b;
   };
   auto put = [&](const Codes& b, int slot, int from, int to) {
@@ -164,7 +174,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     for (int t = 0; t < PB; ++t) {
       if (t < from || t >= to) continue;
       const uint32_t lo = b.q[t][0], hi = b.q[t][1];
-      const float s = b.s[t];
+      const float s = p.s ? b.s[t] : 1.f;
       *reinterpret_cast<uint4*>(smem + slot * Cfg::STAGE + Cfg::A_BYTES + b_lds[t]) =
           make_uint4(code2(lo, 0, s), code2(lo, 2, s), code2(hi, 0, s), code2(hi, 2, s));
     }
@@ -193,34 +203,40 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
   if (c_beg < c_end) {
-    issue(source(c_beg), 0, 0, CPW);
-    put(fetch(c_beg), 0, 0, PB);
-    Codes next = fetch(c_beg + 1 < c_end ? c_beg + 1 : c_beg);
+    next_a();
+    issue(0, 0, CPW);
+    put(fetch(), 0, 0, PB);
+    Codes next = fetch();
+    next_a();
     for (int c = c_beg; c < c_end; ++c) {
       landed<0>();   // this chunk is in place for all waves, and all have read the one before
       const int slot = (c - c_beg) & 1;
       const unsigned char* cur = smem + slot * Cfg::STAGE;
-      const Codes b = next;
-      const bool more = c + 1 < c_end;
-      if (c + 2 < c_end) next = fetch(c + 2);
-      const Source src = source(more ? c + 1 : c);
-#pragma unroll
-      for (int step = 0; step < RC / 16; ++step) {
-        if (more) issue(src, slot ^ 1, step * CPW / 2, (step + 1) * CPW / 2);
-        bf16x8 af[FI], bf[FJ];
+      bf16x8 af[2][FI], bf[2][FJ];
+      auto read = [&](int step) {
 #pragma unroll
         for (int f = 0; f < FI; ++f) {
-          if constexpr (TRANS) af[f] = read_tr8(cur + a_at(step, f), 4 * TI * 2);
-          else af[f] = *reinterpret_cast<const bf16x8*>(cur + a_at(step, f));
+          if constexpr (TRANS) af[step & 1][f] = read_tr8(cur + a_at(step, f), 4 * TI * 2);
+          else af[step & 1][f] = *reinterpret_cast<const bf16x8*>(cur + a_at(step, f));
         }
 #pragma unroll
-        for (int f = 0; f < FJ; ++f) bf[f] = read_tr8(cur + b_at(step, f), 4 * TJ * 2);
-        if (more) put(b, slot ^ 1, step * PB / 4, (step + 1) * PB / 4);
+        for (int f = 0; f < FJ; ++f) bf[step & 1][f] = read_tr8(cur + b_at(step, f), 4 * TJ * 2);
+      };
+      read(0);
+      const Codes b = next;
+      next = fetch();
+#pragma unroll
+      for (int step = 0; step < RC / 16; ++step) {
+        if (step + 1 < RC / 16) read(step + 1);
+        issue(slot ^ 1, step * CPW / 2, (step + 1) * CPW / 2);
+        put(b, slot ^ 1, step * PB / 4, (step + 1) * PB / 4);
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
-          for (int j = 0; j < FJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[j], af[i], acc[i][j], 0, 0, 0);
+          for (int j = 0; j < FJ; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[step & 1][j], af[step & 1][i], acc[i][j], 0, 0, 0);
       }
+      next_a();
     }
     landed<0>();
   }
