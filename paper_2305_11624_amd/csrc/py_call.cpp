@@ -5,12 +5,14 @@
 // 5-7 us a call; here it takes well under one.
 //
 //   call(address, desc, groups, tensors..., ws, stream) -> status
-//   call_rows(address, desc, tensors..., ws, stream) -> status     (the 8-bit rows: desc is a convbn_qdesc)
+//   call_rows(address, desc, kinds, tensors..., ws, stream) -> status     (the 8-bit rows: desc is a convbn_qdesc)
 //
 // `address` is the entry point's address, `desc` a convbn_desc (any object with the buffer protocol), groups None
 // means that the entry point takes none; a tensor is None, a device tensor or an int (a raw address); ws is None or a
 // device tensor, passed on as pointer and size (NO_WS: the entry point takes none); stream is None (the current
-// stream) or a raw handle.  Tensors are dense; call_rows also takes matrices whose rows are ldx or ldz of the descriptor apart.
+// stream) or a raw handle.  Tensors are dense.  call_rows checks each against the descriptor, by one letter of `kinds`:
+//   x z h y  rows of desc's type, [M, K] ldx apart, [M, N] ldz, [M, 2 K] ldx, [M, K] ldz;   W  a dense weight [N, K]
+//   c d e    codes of M, N, 2 M rows of K channels;   s n t  fp32 vectors of M, N, 2 M
 #include <Python.h>
 
 #include <c10/hip/HIPStream.h>
@@ -43,19 +45,14 @@ bool guarded(F&& f) {
   return false;
 }
 
-// Whether a tensor is a matrix with the row stride of the descriptor's.
-bool has_rows_of(const at::Tensor& t, const convbn_qdesc* d) {
-  return d && t.dim() == 2 && t.stride(1) == 1 && (t.stride(0) == d->ldx || t.stride(0) == d->ldz);
-}
-
-// Address of a tensor argument; false (with a Python error set) where it is neither None, an int nor a device tensor that is dense or has
-// the rows of `rows`.
-bool pointer_of(PyObject* o, void** out, const convbn_qdesc* rows = nullptr) {
+// Address of a tensor argument; false (with a Python error set) where it is neither None, an int nor a device tensor, dense unless it
+// has been looked at already.
+bool pointer_of(PyObject* o, void** out, bool dense = true) {
   if (o == Py_None) { *out = nullptr; return true; }
   if (THPVariable_Check(o)) return guarded([&] {
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.is_cuda() || !(t.is_contiguous() || has_rows_of(t, rows))) {
-      PyErr_SetString(PyExc_AssertionError, rows ? "device tensors only, dense or with the descriptor's row stride" : "device, dense tensors only");
+    if (!t.is_cuda() || (dense && !t.is_contiguous())) {
+      PyErr_SetString(PyExc_AssertionError, "device, dense tensors only");
       return false;
     }
     *out = t.data_ptr();
@@ -67,6 +64,41 @@ bool pointer_of(PyObject* o, void** out, const convbn_qdesc* rows = nullptr) {
   }
   PyErr_Format(PyExc_TypeError, "expected a tensor, an address or None, got %s", Py_TYPE(o)->tp_name);
   return false;
+}
+
+// Whether a tensor is what an entry point of the 8-bit rows reads or writes in its place; false with a Python error set.
+bool fits(PyObject* o, char kind, const convbn_qdesc* d, int at) {
+  if (!THPVariable_Check(o)) return true;   // (None and addresses: the library's own checks)
+  return guarded([&] {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const int64_t M = d->M, K = d->K, N = d->N, Kp = (K + 15) / 16 * 16;
+    int64_t rows = M, width = 1, ld = 0;
+    bool bytes = false, vector = false;
+    switch (kind) {
+      case 'x': width = K; ld = d->ldx; break;
+      case 'z': width = N; ld = d->ldz; break;
+      case 'h': width = 2 * K; ld = d->ldx; break;
+      case 'y': width = K; ld = d->ldz; break;
+      case 'W': rows = N; width = K; break;
+      case 'c': width = Kp; bytes = true; break;
+      case 'd': rows = N; width = Kp; bytes = true; break;
+      case 'e': rows = 2 * M; width = Kp; bytes = true; break;
+      case 's': vector = true; break;
+      case 'n': rows = N; vector = true; break;
+      case 't': rows = 2 * M; vector = true; break;
+    }
+    if (ld == 0) ld = width;
+    bool ok;
+    if (vector) ok = t.scalar_type() == at::kFloat && t.numel() == rows && t.is_contiguous();
+    else
+      ok = (bytes ? t.element_size() == 1 : t.scalar_type() == (d->dtype == CONVBN_BF16 ? at::kBFloat16 : at::kFloat)) && t.dim() == 2 &&
+           t.size(0) == rows && t.size(1) == width && (rows <= 1 || t.stride(0) == ld) && (width <= 1 || t.stride(1) == 1 || rows == 0);
+    if (!ok)
+      PyErr_Format(PyExc_ValueError, "tensor %d: expected %s%s [%lld, %lld], rows %lld elements apart", at,
+                   vector ? "float32 vector" : bytes ? "bytes" : d->dtype == CONVBN_BF16 ? "bfloat16" : "float32", vector ? ", as" : "",
+                   (long long)rows, (long long)width, (long long)ld);
+    return ok;
+  });
 }
 
 bool stream_of(PyObject* o, void** out) {
@@ -125,10 +157,13 @@ struct DescView {
 };
 
 // args: `n` tensors, ws, stream
-PyObject* call_with(void* f, const DescView& d, const convbn_qdesc* rows, bool has_groups, int groups, PyObject* const* args, Py_ssize_t n) {
+PyObject* call_with(void* f, const DescView& d, const char* kinds, bool has_groups, int groups, PyObject* const* args, Py_ssize_t n) {
   void* p[kMaxPtr];
+  if (kinds)
+    for (Py_ssize_t i = 0; i < n; ++i)
+      if (!fits(args[i], kinds[i], static_cast<const convbn_qdesc*>(d.b.buf), (int)i)) return nullptr;
   for (Py_ssize_t i = 0; i < n; ++i)
-    if (!pointer_of(args[i], &p[i], rows)) return nullptr;
+    if (!pointer_of(args[i], &p[i], !kinds)) return nullptr;
   PyObject* ws_o = args[n];
   const bool has_ws = ws_o != g_no_ws;
   void* ws = nullptr;
@@ -169,16 +204,23 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 PyObject* call_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  const Py_ssize_t n = nargs - 4;
+  const Py_ssize_t n = nargs - 5;
   if (n < 1 || n > kMaxPtr) {
-    PyErr_SetString(PyExc_TypeError, "call_rows(address, desc, tensors..., ws, stream)");
+    PyErr_SetString(PyExc_TypeError, "call_rows(address, desc, kinds, tensors..., ws, stream)");
     return nullptr;
   }
   void* f = PyLong_AsVoidPtr(args[0]);
   if (PyErr_Occurred()) return nullptr;
   DescView d;
   if (!d.get(args[1], sizeof(convbn_qdesc), "convbn_qdesc")) return nullptr;
-  return call_with(f, d, static_cast<const convbn_qdesc*>(d.b.buf), false, 0, args + 2, n);
+  Py_ssize_t length = 0;
+  const char* kinds = PyUnicode_AsUTF8AndSize(args[2], &length);
+  if (!kinds) return nullptr;
+  if (length != n) {
+    PyErr_SetString(PyExc_TypeError, "one kind for each tensor");
+    return nullptr;
+  }
+  return call_with(f, d, kinds, false, 0, args + 3, n);
 }
 
 // pointer(tensor) -> address or None, stream(None or handle) -> handle: for the entry points that take no descriptor.

@@ -1,4 +1,4 @@
-// 8-bit rows: what the kernels of quant_rows.hip, quant_mm.hip and quant_grad.hip share, and their launchers.
+// 8-bit rows: what the kernels of quant_rows.hip, quant_mm.hip, quant_few.hip and quant_grad.hip share, and their launchers.
 #pragma once
 #include "common.h"
 
@@ -66,6 +66,11 @@ struct QMul {
 };
 size_t qmul_scratch(i64 M, int N, int K);
 hipError_t launch_qmul(const QMul& p, void* ws, hipStream_t st);
+
+// The same for few rows (quant_few.hip), which it can pack itself where qfew_packs(): x != null, codes and scales null = not kept
+bool qfew_taken(i64 M, int N, int K);
+bool qfew_packs(i64 M, int N, int K);
+hipError_t launch_qfew(const QMul& p, const void* x, i64 ldx, void* codes, float* scales, hipStream_t st);
 
 // dx [M][K] = dz . (sw qw) + add, dW [N][K] = dz^T . (sx qx), db = column sums of dz; dx, dW, db nullable
 struct QGrad {

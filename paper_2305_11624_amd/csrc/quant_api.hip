@@ -94,9 +94,12 @@ QGrad grad_of(const convbn_qdesc* d, i64 ldx, i64 ldz) {
   return g;
 }
 // Forward workspace: the product's, then codes and scales that the call does not hand out
-size_t mul_ws(const convbn_qdesc* d) { return qmul_scratch(d->M, d->N, d->K); }
+size_t mul_ws(const convbn_qdesc* d) { return qfew_taken(d->M, d->N, d->K) ? 0 : qmul_scratch(d->M, d->N, d->K); }
 size_t codes_ws(const convbn_qdesc* d) { return align_up((size_t)d->M * qrow(d->K), 256); }
-size_t fwd_ws(const convbn_qdesc* d) { return mul_ws(d) + codes_ws(d) + align_up((size_t)d->M * 4, 256); }
+size_t fwd_ws(const convbn_qdesc* d) {
+  if (qfew_taken(d->M, d->N, d->K) && qfew_packs(d->M, d->N, d->K)) return 0;
+  return mul_ws(d) + codes_ws(d) + align_up((size_t)d->M * 4, 256);
+}
 
 }  // namespace
 
@@ -137,18 +140,25 @@ convbn_status convbn_qlinear_fwd(const convbn_qdesc* desc, const void* x, void* 
   REQUIRE(w_codes, 16); REQUIRE(w_scales, 4); OPTIONAL(b, 4); REQUIRE_ROWS(z, elem(desc));
   OPTIONAL(desc->add_out, elem(desc));
   if (!desc->M) return CONVBN_OK;
-  TRY_STATUS(check_ws(codes ? mul_ws(desc) : fwd_ws(desc), ws, ws_bytes));
+  const bool few = qfew_taken(desc->M, desc->N, desc->K), packs = few && x && qfew_packs(desc->M, desc->N, desc->K);
+  if (!packs) TRY_STATUS(check_ws(codes ? mul_ws(desc) : fwd_ws(desc), ws, ws_bytes));
+  const hipStream_t st = (hipStream_t)stream;
+  QMul m = {};
+  m.M = desc->M; m.ldz = ldz; m.K = desc->K; m.N = desc->N; m.dtype = desc->dtype;
+  m.qw = w_codes; m.sw = w_scales; m.b = b; m.z = z;
+  m.add = (desc->act & CONVBN_ACT_ADD_OUT) ? desc->add_out : nullptr;
+  if (packs) {
+    LAUNCH(launch_qfew(m, x, ldx, codes, scales, st));
+    return CONVBN_OK;
+  }
   if (!codes) {
     codes = static_cast<char*>(ws) + mul_ws(desc);
     scales = reinterpret_cast<float*>(static_cast<char*>(codes) + codes_ws(desc));
   }
-  const hipStream_t st = (hipStream_t)stream;
+  m.qx = codes; m.sx = scales;
   if (x) LAUNCH(launch_qpack(desc->dtype, desc->M, desc->K, ldx, x, codes, scales, st));
-  QMul m = {};
-  m.M = desc->M; m.ldz = ldz; m.K = desc->K; m.N = desc->N; m.dtype = desc->dtype;
-  m.qx = codes; m.sx = scales; m.qw = w_codes; m.sw = w_scales; m.b = b; m.z = z;
-  m.add = (desc->act & CONVBN_ACT_ADD_OUT) ? desc->add_out : nullptr;
-  LAUNCH(launch_qmul(m, ws, st));
+  if (few) LAUNCH(launch_qfew(m, nullptr, 0, nullptr, nullptr, st));
+  else LAUNCH(launch_qmul(m, ws, st));
   return CONVBN_OK;
 }
 

@@ -247,9 +247,10 @@ template <typename T, int TI, int TJ, int WI, int WJ, int NST, bool SPLIT> hipEr
   return hipGetLastError();
 }
 template <typename T, bool SPLIT> hipError_t by_tile(int tile, const MulParams& p, hipStream_t st) {
+  const bool alone = p.nti * p.ntj * p.splits <= CUS;   // one workgroup a compute unit: its copies are all that hides the way to memory
   if (tile == 256) return launch_tiles<T, 256, 256, 64, 128, 2, SPLIT>(p, st);
-  if (tile == 128) return launch_tiles<T, 128, 128, 64, 64, 2, SPLIT>(p, st);
-  return launch_tiles<T, 64, 64, 32, 32, 4, SPLIT>(p, st);
+  if (tile == 128) return alone ? launch_tiles<T, 128, 128, 64, 64, 4, SPLIT>(p, st) : launch_tiles<T, 128, 128, 64, 64, 2, SPLIT>(p, st);
+  return alone ? launch_tiles<T, 64, 64, 32, 32, 8, SPLIT>(p, st) : launch_tiles<T, 64, 64, 32, 32, 4, SPLIT>(p, st);
 }
 template <typename T> hipError_t mul_t(const MulParams& p, int tile, hipStream_t st) {
   if (p.splits == 1) return by_tile<T, false>(tile, p, st);

@@ -3,7 +3,7 @@ that way, the gate between two of them, and the gated block that they make up.
 
 Each object holds the codes, scales, outputs and workspace of one layer, allocated once; its calls enqueue on the current
 stream (or the one they are given) and allocate nothing.  What they return are the object's own buffers, overwritten by the
-next call.  Arguments are checked before anything is launched.
+next call.  Types, sizes and strides of the arguments are checked before anything is launched (ValueError).
 """
 from typing import Optional
 
@@ -19,14 +19,6 @@ def _dtype(dt):
     if dt not in _DTYPES:
         raise TypeError(f"{dt}: bfloat16 or float32")
     return _DTYPES[dt]
-
-
-def _rows(t: torch.Tensor, M: int, width: int, dt, ld: int, name: str):
-    if t.dtype is not dt or t.dim() != 2 or t.shape[0] != M or t.shape[1] != width:
-        raise ValueError(f"{name}: expected {dt} [{M}, {width}], got {t.dtype} {list(t.shape)}")
-    if M > 1 and t.stride(0) != ld or t.stride(1) != 1 and width > 1:
-        raise ValueError(f"{name}: expected rows {ld} elements apart, got strides {t.stride()}")
-    return t
 
 
 def _vector(t: Optional[torch.Tensor], n: int, name: str):
@@ -62,16 +54,17 @@ class Checkpoint:
         self.out = None
 
     def pack(self, x: torch.Tensor, stream=None):
-        self.desc.ldx = ld = x.stride(0) if self.M > 1 else self.K
-        B.convbn_qpack(self.desc, _rows(x, self.M, self.K, self.dtype, ld, "x"), self.codes, self.scales, stream)
+        """The rows of x may be strided."""
+        self.desc.ldx = x.stride(0) if self.M > 1 else self.K
+        B.convbn_qpack(self.desc, x, self.codes, self.scales, stream)
 
     def unpack(self, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         if out is None:
             if self.out is None:
                 self.out = torch.empty(self.M, self.K, dtype=self.dtype, device=self.codes.device)
             out = self.out
-        self.desc.ldx = ld = out.stride(0) if self.M > 1 else self.K
-        B.convbn_qunpack(self.desc, self.codes, self.scales, _rows(out, self.M, self.K, self.dtype, ld, "out"), stream)
+        self.desc.ldx = out.stride(0) if self.M > 1 else self.K
+        B.convbn_qunpack(self.desc, self.codes, self.scales, out, stream)
         return out
 
     def saved_bytes(self) -> int:
@@ -88,6 +81,7 @@ class Linear:
         self.M, self.K, self.N, self.dtype, self.train = M, K, N, dtype, train
         self.ldx, self.ldz = K + gap, N + gap
         self.desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)
+        self._add_desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)   # (with an addend)
         self.codes, self.scales = new_codes(M, K, device) if train else (None, None)
         self.w_codes = self.w_scales = None
         self._w_desc = B.make_qdesc(N, K, dtype=_dtype(dtype))
@@ -108,36 +102,37 @@ class Linear:
         """Pack W [N, K] by output channel."""
         if self.w_codes is None:
             self.w_codes, self.w_scales = new_codes(self.N, self.K, W.device)
-        B.convbn_qpack(self._w_desc, _rows(W, self.N, self.K, self.dtype, self.K, "W"), self.w_codes, self.w_scales, stream)
+        B.convbn_qpack(self._w_desc, W, self.w_codes, self.w_scales, stream)
 
-    def _weight(self):
+    def _desc_with(self, bit: int, field: str, add, width: int, ld: int):
+        if add is None:
+            return self.desc
+        if add.dtype is not self.dtype or add.shape != (self.M, width) or self.M > 1 and add.stride() != (ld, 1):
+            raise ValueError(f"add: expected {self.dtype} [{self.M}, {width}] with rows {ld} elements apart")
+        d = self._add_desc
+        d.act = bit
+        setattr(d, field, add.data_ptr())
+        return d
+
+    def _ready(self):
         if self.w_codes is None:
             raise RuntimeError("no weight: call pack_weight or set_weight first")
-        return self.w_codes, self.w_scales
-
-    def _add(self, bit: int, field: str, add, width: int, ld: int):
-        d = self.desc
-        d.act = 0 if add is None else bit
-        setattr(d, field, None if add is None else _rows(add, self.M, width, self.dtype, ld, "add").data_ptr())
 
     def forward(self, x: torch.Tensor, b: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None, stream=None):
         """z = x w^T + b (+ add)."""
-        w, ws = self._weight()
-        _rows(x, self.M, self.K, self.dtype, self.ldx, "x")
-        self._add(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
-        B.convbn_qlinear_fwd(self.desc, x, self.codes, self.scales, w, ws, _vector(b, self.N, "b"), self.z, self.ws, stream)
+        self._ready()
+        d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
+        B.convbn_qlinear_fwd(d, x, self.codes, self.scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         return self.z
 
     def forward_packed(self, codes: torch.Tensor, scales: torch.Tensor, b: Optional[torch.Tensor] = None,
                        add: Optional[torch.Tensor] = None, stream=None):
         """The same for rows that are packed already; with `train` they are what `backward` reads, so keep them until then."""
-        w, ws = self._weight()
-        _codes(codes, self.M, self.K, "codes")
-        _vector(scales, self.M, "scales")
-        self._add(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
+        self._ready()
+        d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
+        B.convbn_qlinear_fwd(d, None, codes, scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         if self.train:
             self.codes, self.scales = codes, scales
-        B.convbn_qlinear_fwd(self.desc, None, codes, scales, w, ws, _vector(b, self.N, "b"), self.z, self.ws, stream)
         return self.z
 
     def backward(self, dz: torch.Tensor, need_dx: bool = True, need_dW: bool = True, bias: bool = False,
@@ -145,11 +140,10 @@ class Linear:
         """(dx (+ add), dW, db) from the kept codes; None for what is not asked for."""
         if not self.train:
             raise RuntimeError("this layer keeps no codes (train=False)")
-        w, ws = self._weight()
-        _rows(dz, self.M, self.N, self.dtype, self.ldz, "dz")
-        self._add(B.ACT_ADD_IN, "add_in", add, self.K, self.ldx)
+        self._ready()
+        d = self._desc_with(B.ACT_ADD_IN, "add_in", add, self.K, self.ldx)
         dx, dW, db = self.dx if need_dx else None, self.dW if need_dW else None, self.db if bias else None
-        B.convbn_qlinear_bwd(self.desc, self.codes, self.scales, w, ws, dz, dx, dW, db, self.ws, stream)
+        B.convbn_qlinear_bwd(d, self.codes, self.scales, self.w_codes, self.w_scales, dz, dx, dW, db, self.ws, stream)
         return dx, dW, db
 
     def saved_bytes(self) -> int:
@@ -174,14 +168,12 @@ class Gate:
         self.dh = _new_rows(M, 2 * K, self.ldh, dtype, device) if train else None
 
     def forward(self, h: torch.Tensor, stream=None):
-        _rows(h, self.M, 2 * self.K, self.dtype, self.ldh, "h")
         B.convbn_qgate_fwd(self.desc, h, self.codes, self.scales, self.y, self.codes_y, self.scales_y, stream)
         return self.y
 
     def backward(self, dy: torch.Tensor, stream=None):
         if self.codes is None:
             raise RuntimeError("this gate keeps no codes (train=False)")
-        _rows(dy, self.M, self.K, self.dtype, self.ldy, "dy")
         B.convbn_qgate_bwd(self.desc, self.codes, self.scales, dy, self.dh, stream)
         return self.dh
 

@@ -92,9 +92,9 @@ def test_gate_refusals():
 
 
 def test_workspace_is_asked_for_and_checked():
-    d = _qdesc()
+    d = _qdesc(M=100)      # (few rows are packed by the product itself)
     need = B.convbn_qlinear_workspace_bytes(d, B.PASS_FWD)
-    assert need >= 8 * 64 + 8 * 4
+    assert need >= 100 * 64 + 100 * 4
     assert _fwd(d, codes=None, scales=None, work=None, nbytes=0) == B.ERR_WORKSPACE
     assert _fwd(d, codes=None, scales=None, nbytes=need - 1) == B.ERR_WORKSPACE
     assert _fwd(d, codes=None, scales=None, work=C.c_void_p(4104)) == B.ERR_UNSUPPORTED
@@ -111,16 +111,56 @@ def test_workspace_query_of_any_size(M, K, N, dtype):
 def test_native_call_takes_the_descriptors_rows_only():
     B.lib()
     call, at = B._call_rows, B._at.convbn_qpack
-    assert call(at, _qdesc(), None, None, None, B._NO_WS, 0) == B.ERR_NULL
+    assert call(at, _qdesc(), "xcs", None, None, None, B._NO_WS, 0) == B.ERR_NULL
     for bad in (None, b"\0" * 8, B.Desc()):
         with pytest.raises(TypeError):
-            call(at, bad, None, None, None, B._NO_WS, 0)
+            call(at, bad, "xcs", None, None, None, B._NO_WS, 0)
+    for kinds in ("xc", None):
+        with pytest.raises(TypeError):
+            call(at, _qdesc(), kinds, None, None, None, B._NO_WS, 0)
     with pytest.raises(TypeError):
         B._call(at, _qdesc(), None, None, None, None, B._NO_WS, 0)
     with pytest.raises(AssertionError):
-        call(at, _qdesc(), torch.zeros(8, 64), None, None, B._NO_WS, 0)
+        call(at, _qdesc(), "xcs", torch.zeros(8, 64, dtype=torch.bfloat16), None, None, B._NO_WS, 0)
     with pytest.raises(TypeError):
-        call(at, _qdesc(), *[None] * 5, B._NO_WS, 0)   # (no entry point takes five)
+        call(at, _qdesc(), "xxxxx", *[None] * 5, B._NO_WS, 0)   # (no entry point takes five)
+
+
+GOOD = dict(x=(torch.bfloat16, 8, 64), z=(torch.bfloat16, 8, 32), h=(torch.bfloat16, 8, 128), y=(torch.bfloat16, 8, 64),
+            W=(torch.bfloat16, 32, 64), c=(torch.int8, 8, 64), d=(torch.uint8, 32, 64), e=(torch.int8, 16, 64))
+
+
+@pytest.mark.parametrize("kind", sorted(GOOD))
+def test_tensors_are_checked_against_the_descriptor(kind):
+    """A tensor of the wrong type, size or stride is a ValueError; the right one gets as far as the check for the device."""
+    B.lib()
+    call, at, d = B._call_rows, B._at.convbn_qpack, _qdesc()
+    dt, rows, width = GOOD[kind]
+    other = torch.float32 if dt is torch.bfloat16 else torch.int16
+    good = torch.zeros(rows, width, dtype=dt)
+    for bad in (good[:-1], good[:, :-1], good.to(other), torch.zeros(rows, width + 8, dtype=dt)[:, :width], torch.zeros(width, rows, dtype=dt).t(),
+                good.view(1, rows, width), good.view(-1)):
+        with pytest.raises(ValueError):
+            call(at, d, kind + "cs", bad, None, None, B._NO_WS, 0)
+    with pytest.raises(AssertionError):
+        call(at, d, kind + "cs", good, None, None, B._NO_WS, 0)
+    if kind in "xzhy":      # rows of a wider buffer, where the descriptor says so
+        d.ldx, d.ldz = (width + 8, 0) if kind in "xh" else (0, width + 8)
+        with pytest.raises(AssertionError):
+            call(at, d, kind + "cs", torch.zeros(rows, width + 8, dtype=dt)[:, :width], None, None, B._NO_WS, 0)
+        with pytest.raises(ValueError):
+            call(at, d, kind + "cs", good, None, None, B._NO_WS, 0)
+
+
+@pytest.mark.parametrize("kind,n", [("s", 8), ("n", 32), ("t", 16)])
+def test_vectors_are_checked_against_the_descriptor(kind, n):
+    B.lib()
+    call, at, d = B._call_rows, B._at.convbn_qpack, _qdesc()
+    for bad in (torch.zeros(n + 1), torch.zeros(n - 1), torch.zeros(n, dtype=torch.float64), torch.zeros(2 * n)[::2]):
+        with pytest.raises(ValueError):
+            call(at, d, "xc" + kind, None, None, bad, B._NO_WS, 0)
+    with pytest.raises(AssertionError):
+        call(at, d, "xc" + kind, None, None, torch.zeros(n), B._NO_WS, 0)
 
 
 def test_objects_check_their_arguments():
