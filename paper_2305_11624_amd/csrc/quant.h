@@ -25,6 +25,11 @@ __device__ __forceinline__ void dma16(i32x4 desc, unsigned voff, unsigned lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(desc));   // (m0 holds nothing between instructions that need it)
 }
+// ... 4 bytes a lane
+__device__ __forceinline__ void dma4(i32x4 desc, unsigned voff, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(desc));
+}
 // Until at most N of this wave's copies and loads are in flight; then the workgroup's barrier
 template <int N> __device__ __forceinline__ void landed() {
   static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");

@@ -36,16 +36,27 @@ struct GradParams {
   int planes, nch;      // chunks of RC of a plane
   int splits, per;      // chunks of a split
   int nti, ntj;
+  float* db;            // TRANS: column sums of A, [splits][I]; null: not wanted
 };
 
-template <int TI, int TJ, int WI, int WJ> struct GradCfg {
-  static constexpr int WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;
-  static constexpr int A_BYTES = TI * RC * 2, STAGE = A_BYTES + TJ * RC * 2;
-  static constexpr int CPW = A_BYTES / 1024 / WAVES;   // copies a wave
+// NST stages of A; two of the codes as bf16 numbers.  Up to two stages the codes come through registers, a chunk ahead; with more they
+// have a ring of their own, as they are in memory, and a copy of the scales for each wave.
+template <int TI, int TJ, int WI, int WJ, int NST_> struct GradCfg {
+  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;
+  static constexpr bool DEEP = NST > 2;
+  static constexpr int A_BYTES = TI * RC * 2, B_BYTES = TJ * RC * 2, Q_BYTES = TJ * RC;
+  static constexpr int B_AT = NST * A_BYTES, Q_AT = B_AT + 2 * B_BYTES, S_AT = Q_AT + (DEEP ? NST * Q_BYTES : 0);
+  static constexpr int RING = S_AT + (DEEP ? NST * WAVES * 256 : 0);
+  static constexpr int CPW = A_BYTES / 1024 / WAVES, QPW = Q_BYTES / 1024 / WAVES;   // copies a wave
+  static constexpr int GROUP = CPW + QPW + 1;                                        // DEEP: of a chunk of A, the next one's codes and scales
   static constexpr int PITCH = WJ * 4 + 16, OUT_BYTES = WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
-  static constexpr int LDS = 2 * STAGE > OUT_BYTES ? 2 * STAGE : OUT_BYTES;
-  static_assert(A_BYTES % (2048 * WAVES) == 0, "whole pairs of copies");
+  static constexpr int LDS = RING > OUT_BYTES ? RING : OUT_BYTES;
+  static_assert(A_BYTES % (2048 * WAVES) == 0 && Q_BYTES % (1024 * WAVES) == 0 && LDS <= 160 * 1024, "whole pairs of copies");
 };
+
+// 64-byte pieces of a row of W channels in LDS are exchanged by the row's low bits, so that the pieces of four rows that half a wave reads
+// with the transposing load lie on distinct banks
+template <int W> __device__ __forceinline__ int turn(int r) { return W >= 128 ? r & 3 : (r >> 1) & 1; }
 
 // Two codes to bf16 numbers s q
 __device__ __forceinline__ uint32_t code2(uint32_t w, int at, float s) {
@@ -85,9 +96,9 @@ template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT
 }
 
 // OUT: float or bf16_t.  TRANS: A(i, r) = A[r][i].
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ>
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST>
 __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradParams p) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ>;
+  using Cfg = GradCfg<TI, TJ, WI, WJ, NST>;
   constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -105,7 +116,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   for (int i = 0; i < CPW; ++i) {
     const int r = (wave * CPW + i) * RPC + lane / (64 / RPC);
     if constexpr (TRANS) {
-      const int l = lane % (TI / 8), g = ((((l >> 2) ^ (r & 3)) << 2) | (l & 3)) * 8;   // 64-byte pieces are exchanged by the row's low bits
+      const int l = lane % (TI / 8), g = (((l >> 2) ^ turn<TI>(r)) * 4 + (l & 3)) * 8;
       a_off[i] = i0 + g < p.Aw ? (unsigned)(r * (int)p.lda + g) * 2u : OOB;
     } else {
       a_off[i] = (unsigned)(r * (int)p.lda + (dg ^ (i & 1) * 32)) * 2u;
@@ -136,19 +147,26 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   auto issue = [&](int slot, int from, int to) {
 #pragma unroll
     for (int i = 0; i < CPW; ++i)
-      if (i >= from && i < to) dma16(a_desc, a_in[i & 1] ? a_off[i] : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
+      if (i >= from && i < to) dma16(a_desc, a_in[i & 1] ? a_off[i] : OOB, lds0 + slot * Cfg::A_BYTES + i * 1024);
   };
 
   // ---- codes: 8 a piece
   constexpr int PB = TJ * 8 / NT;
-  unsigned b_off[PB], b_lds[PB], s_off[PB];
+  unsigned b_off[PB], b_lds[PB], s_off[PB];   // where they come from (DEEP: in the ring) and go
 #pragma unroll
   for (int t = 0; t < PB; ++t) {
     const int w = t * NT + tid;
     const int r = w / (TJ / 8), g = w % (TJ / 8);
-    b_off[t] = j0 + g * 8 < p.Jp ? (unsigned)(r * p.Jp + g * 8) : OOB;
-    b_lds[t] = r * (TJ * 2) + (((g >> 2) ^ (r & 3)) << 6) + (g & 3) * 16;
+    b_off[t] = Cfg::DEEP ? r * TJ + g * 8 : j0 + g * 8 < p.Jp ? (unsigned)(r * p.Jp + g * 8) : OOB;
+    b_lds[t] = r * (TJ * 2) + ((g >> 2) ^ turn<TJ>(r)) * 64 + (g & 3) * 16;
     s_off[t] = r * 4;
+  }
+  constexpr int QPW = Cfg::QPW, LPQ = TJ / 16;   // DEEP: copies a wave, lanes a row
+  unsigned q_off[QPW];
+#pragma unroll
+  for (int i = 0; i < QPW; ++i) {
+    const int r = (wave * QPW + i) * (64 / LPQ) + lane / LPQ, c = (lane % LPQ) * 16;
+    q_off[i] = j0 + c < p.Jp ? (unsigned)(r * p.Jp + c) : OOB;
   }
   struct Codes { i32x2 q[PB]; float s[PB]; };
   int q_r0 = (c_beg % p.nch) * RC, q_c = c_beg;
@@ -169,13 +187,33 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     q_ptr = last ? p.q + j0 : q_ptr + RC * p.Jp;
     return b;
   };
+  auto issue_q = [&](int slot) {   // DEEP: the next chunk's codes and scales
+    const bool last = q_r0 + RC >= R;
+    const int left = q_c < c_end ? last ? left_last : RC : 0;
+    const i32x4 dq = make_desc(q_ptr, left ? left * p.Jp - j0 : 0), ds = make_desc(p.s + q_r0, p.s ? left * 4 : 0);
+#pragma unroll
+    for (int i = 0; i < QPW; ++i) dma16(dq, q_off[i], lds_off(smem) + Cfg::Q_AT + slot * Cfg::Q_BYTES + (wave * QPW + i) * 1024);
+    dma4(ds, lane * 4, lds_off(smem) + Cfg::S_AT + (slot * Cfg::WAVES + wave) * 256);
+    ++q_c;
+    q_r0 = last ? 0 : q_r0 + RC;
+    q_ptr = last ? p.q + j0 : q_ptr + RC * p.Jp;
+  };
+  auto from_ring = [&](int slot) {
+    Codes b;
+#pragma unroll
+    for (int t = 0; t < PB; ++t) {
+      b.q[t] = *reinterpret_cast<const i32x2*>(smem + Cfg::Q_AT + slot * Cfg::Q_BYTES + b_off[t]);
+      b.s[t] = *reinterpret_cast<const float*>(smem + Cfg::S_AT + (slot * Cfg::WAVES + wave) * 256 + s_off[t]);
+    }
+    return b;
+  };
   auto put = [&](const Codes& b, int slot, int from, int to) {
 #pragma unroll
     for (int t = 0; t < PB; ++t) {
       if (t < from || t >= to) continue;
       const uint32_t lo = b.q[t][0], hi = b.q[t][1];
       const float s = p.s ? b.s[t] : 1.f;
-      *reinterpret_cast<uint4*>(smem + slot * Cfg::STAGE + Cfg::A_BYTES + b_lds[t]) =
+      *reinterpret_cast<uint4*>(smem + Cfg::B_AT + slot * Cfg::B_BYTES + b_lds[t]) =
           make_uint4(code2(lo, 0, s), code2(lo, 2, s), code2(hi, 0, s), code2(hi, 2, s));
     }
   };
@@ -186,10 +224,10 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   // transposing reads: this lane addresses row kb * 8 + ep (+ 4) of a 16-row step, channels (l / 16 % 2) * 16 + (l % 4) * 4 of 32
   const int tr_row = kb * 8 + ep, tr_col = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   auto b_at = [&](int step, int f) {
-    return Cfg::A_BYTES + (step * 16 + tr_row) * (TJ * 2) + (((((wj >> 5) + f)) ^ ep) << 6) + tr_col;
+    return (step * 16 + tr_row) * (TJ * 2) + (((wj >> 5) + f) ^ turn<TJ>(ep)) * 64 + tr_col;
   };
   auto a_at = [&](int step, int f) {
-    if constexpr (TRANS) return (step * 16 + tr_row) * (TI * 2) + ((((wi >> 5) + f) ^ ep) << 6) + tr_col;
+    if constexpr (TRANS) return (step * 16 + tr_row) * (TI * 2) + (((wi >> 5) + f) ^ turn<TI>(ep)) * 64 + tr_col;
     const int row = wi + f * 32 + (lane & 31);
     return row * 128 + (((step * 2 + kb) ^ ((row >> 1) & 7)) << 4);
   };
@@ -202,16 +240,38 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
+  // Column sums of A on the side, by the workgroups of the first tile column: two columns and a share of the rows a thread
+  const bool sums = TRANS && p.db && t.j == 0;
+  constexpr int SHARE = NT / (TI / 2), ROWS = RC / SHARE;   // threads a pair of columns, rows each
+  const int pair = tid % (TI / 2), share = tid / (TI / 2);
+  float sum0 = 0.f, sum1 = 0.f;
+
   if (c_beg < c_end) {
+    Codes next;
+    if constexpr (Cfg::DEEP) {
+      issue_q(0);
+#pragma unroll
+      for (int s = 0; s < NST - 1; ++s) {
+        next_a();
+        issue(s, 0, CPW);
+        issue_q(s + 1);
+      }
+      landed<Cfg::GROUP * (NST - 1)>();
+      put(from_ring(0), 0, 0, PB);
+    } else {
+      next_a();
+      issue(0, 0, CPW);
+      put(fetch(), 0, 0, PB);
+      next = fetch();
+    }
     next_a();
-    issue(0, 0, CPW);
-    put(fetch(), 0, 0, PB);
-    Codes next = fetch();
-    next_a();
+    int slot = 0;   // of A (and, of the ring of codes, this chunk's, which is free again)
     for (int c = c_beg; c < c_end; ++c) {
-      landed<0>();   // this chunk is in place for all waves, and all have read the one before
-      const int slot = (c - c_beg) & 1;
-      const unsigned char* cur = smem + slot * Cfg::STAGE;
+      landed<Cfg::DEEP ? Cfg::GROUP * (NST - 2) : 0>();   // this chunk is in place for all waves, and all have read the one before
+      const unsigned char* cur = smem + slot * Cfg::A_BYTES;
+      const unsigned char* curb = smem + Cfg::B_AT + ((c - c_beg) & 1) * Cfg::B_BYTES;
+      const int fill = slot ? slot - 1 : NST - 1;
+      const int putb = (c - c_beg + 1) & 1;
       bf16x8 af[2][FI], bf[2][FJ];
       auto read = [&](int step) {
 #pragma unroll
@@ -220,25 +280,56 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
           else af[step & 1][f] = *reinterpret_cast<const bf16x8*>(cur + a_at(step, f));
         }
 #pragma unroll
-        for (int f = 0; f < FJ; ++f) bf[step & 1][f] = read_tr8(cur + b_at(step, f), 4 * TJ * 2);
+        for (int f = 0; f < FJ; ++f) bf[step & 1][f] = read_tr8(curb + b_at(step, f), 4 * TJ * 2);
       };
       read(0);
-      const Codes b = next;
-      next = fetch();
+      Codes b;
+      const int after = slot + 1 == NST ? 0 : slot + 1;
+      if constexpr (Cfg::DEEP) {
+        b = from_ring(after);
+      } else {
+        b = next;
+        next = fetch();
+      }
 #pragma unroll
       for (int step = 0; step < RC / 16; ++step) {
         if (step + 1 < RC / 16) read(step + 1);
-        issue(slot ^ 1, step * CPW / 2, (step + 1) * CPW / 2);
-        put(b, slot ^ 1, step * PB / 4, (step + 1) * PB / 4);
+        issue(fill, step * CPW / 2, (step + 1) * CPW / 2);
+        if constexpr (Cfg::DEEP)
+          if (step == 1) issue_q(slot);
+        put(b, putb, step * PB / 4, (step + 1) * PB / 4);
 #pragma unroll
         for (int i = 0; i < FI; ++i)
 #pragma unroll
           for (int j = 0; j < FJ; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[step & 1][j], af[step & 1][i], acc[i][j], 0, 0, 0);
       }
+      if (sums) {
+#pragma unroll
+        for (int x = 0; x < ROWS; ++x) {
+          const int r = share * ROWS + x;
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(cur + r * (TI * 2) + ((pair >> 4) ^ turn<TI>(r)) * 64 + (pair & 15) * 4);
+          sum0 += bf16_lo(w);
+          sum1 += bf16_hi(w);
+        }
+      }
       next_a();
+      slot = after;
     }
     landed<0>();
+  }
+  if (sums) {
+    float* part = reinterpret_cast<float*>(smem);
+    part[share * TI + 2 * pair] = sum0;
+    part[share * TI + 2 * pair + 1] = sum1;
+    __syncthreads();
+    if (tid < TI && i0 + tid < p.I) {
+      float v = 0.f;
+#pragma unroll
+      for (int x = 0; x < SHARE; ++x) v += part[x * TI + tid];
+      p.db[split * p.I + i0 + tid] = v;
+    }
+    __syncthreads();
   }
 
   // ---- out, 32 rows of this wave at a time: a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..;
@@ -276,15 +367,50 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   }
 }
 
-// C = the sum of the splits + add, in the order of the splits
+// C = the sum of the splits + add; likewise the column sums.  Four threads share eight channels (or one, where J is no multiple of 8), each
+// adds every fourth split, and the four sums meet in LDS: the order is the same in every run.
+constexpr int JOIN = 4;
 template <typename OUT>
-__global__ __launch_bounds__(256) void qjoin_kernel(i64 I, int J, int splits, const float* __restrict__ part, OUT* C, i64 ldc, const OUT* add) {
-  const i64 total = I * J;
-  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
-    float v = 0.f;
-    for (int s = 0; s < splits; ++s) v += part[s * total + x];
-    const i64 o = x / J * ldc + x % J;
-    C[o] = from_f32<OUT>(v + (add ? to_f32(add[o]) : 0.f));
+__global__ __launch_bounds__(256) void qjoin_kernel(i64 I, int J, int splits, const float* __restrict__ part, OUT* C, i64 ldc, const OUT* add,
+                                                    const float* __restrict__ db_part, float* __restrict__ db) {
+  __shared__ float meet[JOIN][8][64];
+  const int at = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const bool vec = ((uintptr_t)C | (uintptr_t)(ldc * sizeof(OUT)) | (uintptr_t)add) % 16 == 0;
+  const int width = J % 8 ? 1 : 8;
+  const i64 mine = I * (J / width), total = mine + (db ? I : 0);   // the column sums come last, one a thread
+  for (i64 x0 = (i64)blockIdx.x * 64; x0 < total; x0 += (i64)gridDim.x * 64) {
+    const i64 x = x0 + at;
+    float v[8] = {};
+    if (x < mine && width == 8) {
+#pragma unroll 4
+      for (int s = q; s < splits; s += JOIN) {
+        const float4* f = reinterpret_cast<const float4*>(part + s * I * J + x * 8);
+        const float4 a = f[0], b = f[1];
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+      }
+    } else if (x < total) {
+      const float* f = x < mine ? part + x : db_part + (x - mine);
+      const i64 apart = x < mine ? I * J : I;
+#pragma unroll 4
+      for (int s = q; s < splits; s += JOIN) v[0] += f[s * apart];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) meet[q][e][at] = v[e];
+    __syncthreads();
+    if (q == 0 && x < total) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (meet[0][e][at] + meet[1][e][at]) + (meet[2][e][at] + meet[3][e][at]);
+      if (x >= mine) {
+        db[x - mine] = v[0];
+      } else if (width == 8) {
+        const i64 row = x / (J / 8), o = row * ldc + (x - row * (J / 8)) * 8;
+        store8<OUT>(C + o, add ? add + o : nullptr, v, vec, 8);
+      } else {
+        const i64 o = x / J * ldc + x % J;
+        C[o] = from_f32<OUT>(v[0] + (add ? to_f32(add[o]) : 0.f));
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -319,24 +445,31 @@ __global__ __launch_bounds__(256) void qsplit_kernel(i64 M, int N, int N8, const
   }
 }
 
-// Column sums: a workgroup takes 64 columns and a slice of the rows; slices are added in order by the second launch.
+// Column sums on their own: a workgroup takes 64 columns and a slice of the rows; several slices are added in order by a second launch.
+constexpr int SUM_WAVES = 16;
 template <typename T>
-__global__ __launch_bounds__(256) void qcolsum_kernel(i64 M, int N, i64 per, const T* __restrict__ dz, i64 ldz, float* __restrict__ part) {
-  __shared__ float sum[4][64];
+__global__ __launch_bounds__(64 * SUM_WAVES) void qcolsum_kernel(i64 M, int N, i64 per, const T* __restrict__ dz, i64 ldz, float* __restrict__ part) {
+  __shared__ float sum[SUM_WAVES][64];
   const int n = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
   const i64 beg = (i64)blockIdx.y * per, end = beg + per < M ? beg + per : M;
   float s = 0.f;
-  if (n < N)
-    for (i64 m = beg + w; m < end; m += 4) s += to_f32(dz[m * ldz + n]);
+  if (n < N) {
+#pragma unroll 8
+    for (i64 m = beg + w; m < end; m += SUM_WAVES) s += to_f32(dz[m * ldz + n]);
+  }
   sum[w][threadIdx.x & 63] = s;
   __syncthreads();
-  if (w == 0 && n < N)
-    part[(i64)blockIdx.y * N + n] = sum[0][threadIdx.x] + sum[1][threadIdx.x] + sum[2][threadIdx.x] + sum[3][threadIdx.x];
+  if (w == 0 && n < N) {
+    float v = 0.f;
+    for (int i = 0; i < SUM_WAVES; ++i) v += sum[i][threadIdx.x];
+    part[(i64)blockIdx.y * N + n] = v;
+  }
 }
 __global__ __launch_bounds__(256) void qcolsum_join_kernel(int N, int slices, const float* __restrict__ part, float* __restrict__ db) {
   const int n = blockIdx.x * 256 + threadIdx.x;
   if (n >= N) return;
   float s = 0.f;
+#pragma unroll 8
   for (int i = 0; i < slices; ++i) s += part[(i64)i * N + n];
   db[n] = s;
 }
@@ -345,29 +478,40 @@ int grid_of(i64 work) { const i64 b = (work + 255) / 256; return (int)(b < 1 ? 1
 
 constexpr int CUS = 256;
 
-struct Plan { int ti, tj, splits, per; };
+// Tiles of 256 where they are a round; below that the cheaper of 64 (as long as they are a round themselves) and 128, and of 1 to 256 parts of
+// the sum, by what a launch was measured to take in us: 4.8 (64) or 5.3 (128) and, for each chunk, 0.5 or 0.76 with a workgroup alone on
+// its compute unit, 1.4 a round of two; parts cost another launch and their sums' way through memory.  dW of 1568 x 2048 x 512: 64 whole
+// 17.3, in two parts 28, 128 whole 24.2, in two 22.7, in four 22.5; dx of 64 x 2048 x 512: 64 8.0, 128 9.8; dx of 200 x 1024 x 4096: 64 whole
+// 32.8, in four 16.7, 128 whole 47, in eight 17.8.
+struct Plan { int tile, splits, per; };
 Plan plan_of(i64 I, int J, i64 R, int planes) {
-  Plan pl;
   const int nch = (int)((R + RC - 1) / RC) * planes;
-  const i64 big = ((I + 255) / 256) * ((J + 255) / 256), small = ((I + 127) / 128) * ((J + 127) / 128);
-  const bool large = big >= CUS;
-  pl.ti = pl.tj = large ? 256 : 128;
-  const i64 tiles = large ? big : small;
-  pl.splits = pl.per = 1;
-  if (!tiles || !nch) return pl;   // (no rows)
-  int s = 1;
-  if (tiles < CUS) s = (int)(CUS / tiles);
-  if (s > nch / 4) s = nch / 4;
-  if (s < 1) s = 1;
-  pl.per = (nch + s - 1) / s;
-  pl.splits = (nch + pl.per - 1) / pl.per;
+  Plan pl = {128, 1, nch};
+  auto tiles = [&](i64 t) { return ((I + t - 1) / t) * ((J + t - 1) / t); };
+  if (!I || !nch) return pl;   // (no rows)
+  if (tiles(256) >= CUS && I > 128 && J > 128) {
+    pl.tile = 256;
+    return pl;
+  }
+  double best = 1e30;
+  for (int tile = 64; tile <= 128; tile *= 2)
+    for (int s = 1; s <= 256 && s <= nch; s *= 2) {
+      const int per = ceil_div(nch, s), parts = ceil_div(nch, per);
+      const double w = (double)tiles(tile) * parts;
+      if (tile == 64 && w > CUS) break;
+      const double chunk = w <= CUS ? (tile == 64 ? 0.5 : 0.76) : 1.4 * (double)(i64)((w + 511) / 512);
+      const double us = (tile == 64 ? 4.8 : 5.3) + chunk * per + (parts > 1 ? 4 + 2e-6 * parts * (double)I * J : 0);
+      if (us < best) {
+        best = us;
+        pl = {tile, parts, per};
+      }
+    }
   return pl;
 }
 
 int colsum_slices(i64 M, int N) {
-  const int cols = ceil_div(N, 64);
-  i64 s = 1024 / cols;
-  if (s > M / 64) s = M / 64;
+  i64 s = 512 / ceil_div(N, 64);
+  if (s > M / 512) s = M / 512;
   return (int)(s < 1 ? 1 : s);
 }
 
@@ -385,7 +529,7 @@ Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outp
   if (p.dtype != CONVBN_BF16) s.copy = (size_t)3 * p.M * N8 * 2;
   else s.copy = (size_t)p.M * N8 * 2;
   const Plan dx = plan_of(p.M, p.K, p.N, planes), dw = plan_of(p.N, p.K, p.M, planes);
-  const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * p.K * 4 : 0;
+  const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * (p.K + 1) * 4 : 0;
   s.copy = align_up(s.copy, 256);
   s.part = align_up(px > pw ? px : pw, 256);
   s.cols = align_up((size_t)colsum_slices(p.M, p.N) * p.N * 4, 256);
@@ -393,20 +537,28 @@ Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outp
   return s;
 }
 
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ>
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST>
 hipError_t launch_tiles(const GradParams& g, hipStream_t st) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ>;
+  using Cfg = GradCfg<TI, TJ, WI, WJ, NST>;
   static LdsLimitOnce once;
-  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ>;
+  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ, NST>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   const int total = g.nti * g.ntj * g.splits;
   k<<<((total + 7) / 8) * 8, Cfg::NT, Cfg::LDS, st>>>(g);
   return hipGetLastError();
 }
+template <typename OUT, bool TRANS> hipError_t by_tile(int tile, const GradParams& g, hipStream_t st) {
+  if (tile == 256) return launch_tiles<OUT, TRANS, 256, 256, 64, 128, 2>(g, st);
+  if (tile == 64) return launch_tiles<OUT, TRANS, 64, 64, 32, 32, 8>(g, st);
+  // one workgroup a compute unit: its copies are all that hides the way to memory
+  if (g.nti * g.ntj * g.splits <= CUS) return launch_tiles<OUT, TRANS, 128, 128, 64, 32, 4>(g, st);
+  return launch_tiles<OUT, TRANS, 128, 128, 64, 64, 2>(g, st);
+}
 
+// sums: column sums of A as well (TRANS, A = dz itself); their partial sums lie behind those of the product
 template <typename T, bool TRANS>
-hipError_t product(const QGrad& p, const bf16_t* A, i64 lda, float* part, hipStream_t st) {
+hipError_t product(const QGrad& p, const bf16_t* A, i64 lda, float* part, bool sums, hipStream_t st) {
   GradParams g = {};
   const bool f32 = p.dtype != CONVBN_BF16;
   const int N8 = (p.N + 7) & ~7;
@@ -420,19 +572,20 @@ hipError_t product(const QGrad& p, const bf16_t* A, i64 lda, float* part, hipStr
   g.nch = (int)((g.R + RC - 1) / RC);
   const Plan pl = plan_of(g.I, g.J, g.R, g.planes);
   g.splits = pl.splits; g.per = pl.per;
-  g.nti = (int)((g.I + pl.ti - 1) / pl.ti); g.ntj = ceil_div(g.J, pl.tj);
+  g.nti = (int)((g.I + pl.tile - 1) / pl.tile); g.ntj = ceil_div(g.J, pl.tile);
   T* C = static_cast<T*>(TRANS ? p.dW : p.dx);
   const i64 ldc = TRANS ? p.K : p.ldx;
   const T* add = TRANS ? nullptr : static_cast<const T*>(p.add);
   if (pl.splits > 1) {
-    g.C = part; g.ldc = g.J;
-    const hipError_t e = pl.ti == 256 ? launch_tiles<float, TRANS, 256, 256, 64, 128>(g, st) : launch_tiles<float, TRANS, 128, 128, 64, 64>(g, st);
+    float* db_part = part + (i64)pl.splits * g.I * g.J;
+    g.C = part; g.ldc = g.J; g.db = sums ? db_part : nullptr;
+    const hipError_t e = by_tile<float, TRANS>(pl.tile, g, st);
     if (e != hipSuccess) return e;
-    qjoin_kernel<T><<<grid_of(g.I * g.J), 256, 0, st>>>(g.I, g.J, pl.splits, part, C, ldc, add);
+    qjoin_kernel<T><<<grid_of(4 * (g.I * (g.J % 8 ? g.J : g.J / 8) + (sums ? g.I : 0))), 256, 0, st>>>(g.I, g.J, pl.splits, part, C, ldc, add, db_part, sums ? p.db : nullptr);
     return hipGetLastError();
   }
-  g.C = C; g.ldc = ldc; g.add = add;
-  return pl.ti == 256 ? launch_tiles<T, TRANS, 256, 256, 64, 128>(g, st) : launch_tiles<T, TRANS, 128, 128, 64, 64>(g, st);
+  g.C = C; g.ldc = ldc; g.add = add; g.db = sums ? p.db : nullptr;
+  return by_tile<T, TRANS>(pl.tile, g, st);
 }
 
 template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st) {
@@ -450,20 +603,21 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
   }
   if (p.dx && p.M) {
     if constexpr (sizeof(T) == 4) qsplit_kernel<false><<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, copy);
-    const hipError_t e = product<T, false>(p, A, lda, part, st);
+    const hipError_t e = product<T, false>(p, A, lda, part, false, st);
     if (e != hipSuccess) return e;
   }
+  const bool aside = p.db && p.dW && p.M && sizeof(T) == 2;   // the column sums ride in the weight gradient
   if (p.dW) {
     if constexpr (sizeof(T) == 4)
       if (p.M) qsplit_kernel<true><<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sx, copy);
-    const hipError_t e = product<T, true>(p, A, lda, part, st);
+    const hipError_t e = product<T, true>(p, A, lda, part, aside, st);
     if (e != hipSuccess) return e;
   }
-  if (p.db) {
+  if (p.db && !aside) {
     const int slices = colsum_slices(p.M, p.N);
     const i64 per = (p.M + slices - 1) / slices;
-    qcolsum_kernel<T><<<dim3(ceil_div(p.N, 64), slices), 256, 0, st>>>(p.M, p.N, per, dz, p.ldz, cols);
-    qcolsum_join_kernel<<<ceil_div(p.N, 256), 256, 0, st>>>(p.N, slices, cols, p.db);
+    qcolsum_kernel<T><<<dim3(ceil_div(p.N, 64), slices), 64 * SUM_WAVES, 0, st>>>(p.M, p.N, per, dz, p.ldz, slices > 1 ? cols : p.db);
+    if (slices > 1) qcolsum_join_kernel<<<ceil_div(p.N, 256), 256, 0, st>>>(p.N, slices, cols, p.db);
   }
   return hipGetLastError();
 }

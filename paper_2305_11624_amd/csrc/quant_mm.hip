@@ -219,21 +219,32 @@ template <typename T> __global__ __launch_bounds__(256) void qmul_join_kernel(Mu
 
 constexpr int CUS = 256;
 
-struct Plan { int tile, splits, per; };   // tile: 256, 128 or 64 rows and channels
+// Tiles of 256 where they are a round; below that the cheaper of 64 and 128, and of 1 to 64 parts of the channel sum, by what a launch
+// was measured to take in us: 4 (64) or 5 (128) and, for each chunk, 0.27 or 0.5 with a workgroup alone on its compute unit, 0.37 or 0.8
+// a round of two of them; parts cost another launch and their sums' way through memory.  1568 x 2048 x 512: 64 whole 8.6, in two parts
+// 14.1, 128 whole 13.3; 64 x 8192 x 2048: 64 whole 20.6, in four parts 13.3; 1568 x 8192 x 2048: 64 51.9, 128 39.5.
+struct Plan { int tile, splits, per; };
 Plan plan_of(i64 M, int N, int K) {
-  Plan pl = {64, 1, 1};
-  auto tiles = [&](i64 t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
   const int nch = ceil_div(qrow(K), KC);
-  pl.per = nch;
+  Plan pl = {64, 1, nch};
   if (M == 0) return pl;
-  pl.tile = tiles(256) >= CUS && N > 128 ? 256 : M > 64 && tiles(128) >= CUS / 4 ? 128 : 64;
-  const i64 t = tiles(pl.tile);
-  const i64 want = pl.tile == 64 ? 2 * CUS : CUS;
-  i64 s = t < want ? want / t : 1;
-  if (s > nch / 2) s = nch / 2;
-  if (s < 1) s = 1;
-  pl.per = (int)((nch + s - 1) / s);
-  pl.splits = ceil_div(nch, pl.per);
+  auto tiles = [&](i64 t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+  if (tiles(256) >= CUS && M > 128 && N > 128) {
+    pl.tile = 256;
+    return pl;
+  }
+  double best = 1e30;
+  for (int tile = 64; tile <= 128; tile *= 2)
+    for (int s = 1; s <= 64 && s <= nch; s *= 2) {
+      const int per = ceil_div(nch, s), parts = ceil_div(nch, per);
+      const double w = (double)tiles(tile) * parts, rounds = (double)(i64)((w + 511) / 512);
+      const double chunk = w <= CUS ? (tile == 64 ? 0.27 : 0.5) : rounds * (tile == 64 ? 0.37 : 0.8);
+      const double us = (tile == 64 ? 4 : 5) + chunk * per + (parts > 1 ? 4.2 + 2e-6 * parts * (double)M * N : 0);
+      if (us < best) {
+        best = us;
+        pl = {tile, parts, per};
+      }
+    }
   return pl;
 }
 
