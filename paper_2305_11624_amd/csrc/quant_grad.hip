@@ -478,29 +478,27 @@ int grid_of(i64 work) { const i64 b = (work + 255) / 256; return (int)(b < 1 ? 1
 
 constexpr int CUS = 256;
 
-// Tiles of 256 where they are a round; below that the cheaper of 64 (as long as they are a round themselves) and 128, and of 1 to 256 parts of
-// the sum, by what a launch was measured to take in us: 4.8 (64) or 5.3 (128) and, for each chunk, 0.5 or 0.76 with a workgroup alone on
-// its compute unit, 1.4 a round of two; parts cost another launch and their sums' way through memory.  dW of 1568 x 2048 x 512: 64 whole
-// 17.3, in two parts 28, 128 whole 24.2, in two 22.7, in four 22.5; dx of 64 x 2048 x 512: 64 8.0, 128 9.8; dx of 200 x 1024 x 4096: 64 whole
-// 32.8, in four 16.7, 128 whole 47, in eight 17.8.
+// The cheapest of tiles of 64 (as long as they are a round), 128 and 256, and of 1 to 256 parts of the sum, by what was measured in us: a
+// launch 2.5, every round of workgroups 2.3, 2.8 or 7 and, for each chunk, 0.5, 0.76 or 1.85 with a workgroup alone on its compute unit,
+// 1.4 with two (128); parts cost another launch and their sums' way through memory.  dW of 1568 x 2048 x 512: 64 whole 17.3, in two parts
+// 28, 128 whole 24.2, in two 22.7, in four 22.5; dx of 64 x 2048 x 512: 64 8.0, 128 9.8; of 200 x 1024 x 4096: 64 whole 32.8, in four 16.7,
+// 128 whole 47, in eight 17.8; of 1568 x 8192 x 2048: 128 82, 256 59.5; of 100352 x 256 x 64: 128 19.4, 256 20.3.
 struct Plan { int tile, splits, per; };
 Plan plan_of(i64 I, int J, i64 R, int planes) {
   const int nch = (int)((R + RC - 1) / RC) * planes;
   Plan pl = {128, 1, nch};
   auto tiles = [&](i64 t) { return ((I + t - 1) / t) * ((J + t - 1) / t); };
   if (!I || !nch) return pl;   // (no rows)
-  if (tiles(256) >= CUS && I > 128 && J > 128) {
-    pl.tile = 256;
-    return pl;
-  }
   double best = 1e30;
-  for (int tile = 64; tile <= 128; tile *= 2)
+  for (int tile = 64; tile <= 256; tile *= 2)
     for (int s = 1; s <= 256 && s <= nch; s *= 2) {
       const int per = ceil_div(nch, s), parts = ceil_div(nch, per);
       const double w = (double)tiles(tile) * parts;
       if (tile == 64 && w > CUS) break;
-      const double chunk = w <= CUS ? (tile == 64 ? 0.5 : 0.76) : 1.4 * (double)(i64)((w + 511) / 512);
-      const double us = (tile == 64 ? 4.8 : 5.3) + chunk * per + (parts > 1 ? 4 + 2e-6 * parts * (double)I * J : 0);
+      const bool alone = w <= CUS;
+      const double rounds = (double)(i64)(tile == 256 ? (w + 255) / 256 : (w + 511) / 512);
+      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.76 : 1.4) : 0.5;
+      const double us = 2.5 + rounds * ((tile == 256 ? 7 : tile == 128 ? 2.8 : 2.3) + chunk * per) + (parts > 1 ? 4 + 2e-6 * parts * (double)I * J : 0);
       if (us < best) {
         best = us;
         pl = {tile, parts, per};

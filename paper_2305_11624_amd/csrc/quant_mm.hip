@@ -219,27 +219,26 @@ template <typename T> __global__ __launch_bounds__(256) void qmul_join_kernel(Mu
 
 constexpr int CUS = 256;
 
-// Tiles of 256 where they are a round; below that the cheaper of 64 and 128, and of 1 to 64 parts of the channel sum, by what a launch
-// was measured to take in us: 4 (64) or 5 (128) and, for each chunk, 0.27 or 0.5 with a workgroup alone on its compute unit, 0.37 or 0.8
-// a round of two of them; parts cost another launch and their sums' way through memory.  1568 x 2048 x 512: 64 whole 8.6, in two parts
-// 14.1, 128 whole 13.3; 64 x 8192 x 2048: 64 whole 20.6, in four parts 13.3; 1568 x 8192 x 2048: 64 51.9, 128 39.5.
+// The cheapest of tiles of 64, 128 and 256, and of 1 to 64 parts of the channel sum, by what was measured in us: a launch 2, every round of
+// workgroups 2, 3 or 6 and, for each chunk, 0.27, 0.5 or 1.85 with a workgroup alone on its compute unit, 0.37 or 1.2 with two (64, 128);
+// parts cost another launch and their sums' way through memory.  1568 x 2048 x 512: 64 whole 8.6, in two parts 14.1, 128 whole 13.3;
+// 64 x 8192 x 2048: 64 whole 20.6, in four parts 13.3; 1568 x 8192 x 2048: 64 51.9, 128 39.5; 100352 x 64 x 256: 64 39.4, 128 23.3;
+// 16384 x 1024 x 1024: 128 30.3, 256 26.
 struct Plan { int tile, splits, per; };
 Plan plan_of(i64 M, int N, int K) {
   const int nch = ceil_div(qrow(K), KC);
   Plan pl = {64, 1, nch};
   if (M == 0) return pl;
   auto tiles = [&](i64 t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-  if (tiles(256) >= CUS && M > 128 && N > 128) {
-    pl.tile = 256;
-    return pl;
-  }
   double best = 1e30;
-  for (int tile = 64; tile <= 128; tile *= 2)
+  for (int tile = 64; tile <= 256; tile *= 2)
     for (int s = 1; s <= 64 && s <= nch; s *= 2) {
       const int per = ceil_div(nch, s), parts = ceil_div(nch, per);
-      const double w = (double)tiles(tile) * parts, rounds = (double)(i64)((w + 511) / 512);
-      const double chunk = w <= CUS ? (tile == 64 ? 0.27 : 0.5) : rounds * (tile == 64 ? 0.37 : 0.8);
-      const double us = (tile == 64 ? 4 : 5) + chunk * per + (parts > 1 ? 4.2 + 2e-6 * parts * (double)M * N : 0);
+      const double w = (double)tiles(tile) * parts;
+      const bool alone = w <= CUS;
+      const double rounds = (double)(i64)(tile == 256 ? (w + 255) / 256 : (w + 511) / 512);
+      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.5 : 1.2) : alone ? 0.27 : 0.37;
+      const double us = 2 + rounds * ((tile == 256 ? 6 : tile == 128 ? 3 : 2) + chunk * per) + (parts > 1 ? 4.2 + 2e-6 * parts * (double)M * N : 0);
       if (us < best) {
         best = us;
         pl = {tile, parts, per};
