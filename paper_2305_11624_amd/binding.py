@@ -95,11 +95,6 @@ def _load():
     return _call
 
 
-def _no_ws():
-    lib()
-    return _NO_WS
-
-
 def lib():
     """The loaded library.  Raises if it has not been built (no silent fallback)."""
     global _lib, _call, _call_rows, _at, _NO_WS, _pointer, _stream_handle
@@ -662,37 +657,57 @@ def convbn_qlinear_workspace_bytes(desc: QDesc, pass_: int) -> int:
     return lib().convbn_qlinear_workspace_bytes(C.byref(desc), pass_)
 
 
-def _rows_call(name, desc, kinds, args, stream, check):
-    if _call is None:
-        _load()
-    st = _call_rows(getattr(_at, name), desc, kinds, *args, None if stream is None else _handle(stream))
+def _load_rows():
+    lib()
+    return _call_rows
+
+
+def convbn_qpack(desc, x, codes, scales, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_qpack, desc, "xcs", x, codes, scales, _NO_WS,
+                                      None if stream is None else _handle(stream))
     if st and check:
         _check(st)
     return st
 
 
-def convbn_qpack(desc, x, codes, scales, stream=None, check=True):
-    return _rows_call("convbn_qpack", desc, "xcs", (x, codes, scales, _NO_WS or _no_ws()), stream, check)
-
-
 def convbn_qunpack(desc, codes, scales, x, stream=None, check=True):
-    return _rows_call("convbn_qunpack", desc, "csx", (codes, scales, x, _NO_WS or _no_ws()), stream, check)
+    st = (_call_rows or _load_rows())(_at.convbn_qunpack, desc, "csx", codes, scales, x, _NO_WS,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
 
 
 def convbn_qlinear_fwd(desc, x, codes, scales, w_codes, w_scales, b, z, ws=None, stream=None, check=True):
-    return _rows_call("convbn_qlinear_fwd", desc, "xcsdnnz", (x, codes, scales, w_codes, w_scales, b, z, ws), stream, check)
+    st = (_call_rows or _load_rows())(_at.convbn_qlinear_fwd, desc, "xcsdnnz", x, codes, scales, w_codes, w_scales, b, z, ws,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
 
 
 def convbn_qlinear_bwd(desc, codes, scales, w_codes, w_scales, dz, dx, dW, db, ws=None, stream=None, check=True):
-    return _rows_call("convbn_qlinear_bwd", desc, "csdnzxWn", (codes, scales, w_codes, w_scales, dz, dx, dW, db, ws), stream, check)
+    st = (_call_rows or _load_rows())(_at.convbn_qlinear_bwd, desc, "csdnzxWn", codes, scales, w_codes, w_scales, dz, dx, dW, db,
+                                      ws, None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
 
 
 def convbn_qgate_fwd(desc, h, h_codes, h_scales, y, y_codes, y_scales, stream=None, check=True):
-    return _rows_call("convbn_qgate_fwd", desc, "hetycs", (h, h_codes, h_scales, y, y_codes, y_scales, _NO_WS or _no_ws()), stream, check)
+    st = (_call_rows or _load_rows())(_at.convbn_qgate_fwd, desc, "hetycs", h, h_codes, h_scales, y, y_codes, y_scales, _NO_WS,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
 
 
 def convbn_qgate_bwd(desc, h_codes, h_scales, dy, dh, stream=None, check=True):
-    return _rows_call("convbn_qgate_bwd", desc, "etyh", (h_codes, h_scales, dy, dh, _NO_WS or _no_ws()), stream, check)
+    st = (_call_rows or _load_rows())(_at.convbn_qgate_bwd, desc, "etyh", h_codes, h_scales, dy, dh, _NO_WS,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
 
 
 # ---- channels-last device buffers (pure permutes and casts) -------------------
