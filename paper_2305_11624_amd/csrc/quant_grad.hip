@@ -41,16 +41,18 @@ struct GradParams {
 
 // NST stages of A; two of the codes as bf16 numbers.  Up to two stages the codes come through registers, a chunk ahead; with more they
 // have a ring of their own, as they are in memory, and a copy of the scales for each wave.
-template <int TI, int TJ, int WI, int WJ, int NST_> struct GradCfg {
-  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;
+// G groups of waves divide the workgroup's part of the sum, each with rings of its own (one wave on a SIMD waits for its own reads and
+// copies most of the time); their sums meet on the way out.
+template <int TI, int TJ, int WI, int WJ, int NST_, int G> struct GradCfg {
+  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;   // of a group
   static constexpr bool DEEP = NST > 2;
   static constexpr int A_BYTES = TI * RC * 2, B_BYTES = TJ * RC * 2, Q_BYTES = TJ * RC;
   static constexpr int B_AT = NST * A_BYTES, Q_AT = B_AT + 2 * B_BYTES, S_AT = Q_AT + (DEEP ? NST * Q_BYTES : 0);
   static constexpr int RING = S_AT + (DEEP ? NST * WAVES * 256 : 0);
   static constexpr int CPW = A_BYTES / 1024 / WAVES, QPW = Q_BYTES / 1024 / WAVES;   // copies a wave
   static constexpr int GROUP = CPW + QPW + 1;                                        // DEEP: of a chunk of A, the next one's codes and scales
-  static constexpr int PITCH = WJ * 4 + 16, OUT_BYTES = WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
-  static constexpr int LDS = RING > OUT_BYTES ? RING : OUT_BYTES;
+  static constexpr int PITCH = WJ * 4 + 16, OUT_BYTES = G * WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
+  static constexpr int LDS = G * RING > OUT_BYTES ? G * RING : OUT_BYTES;
   static_assert(A_BYTES % (2048 * WAVES) == 0 && Q_BYTES % (1024 * WAVES) == 0 && LDS <= 160 * 1024, "whole pairs of copies");
 };
 
@@ -96,17 +98,20 @@ template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT
 }
 
 // OUT: float or bf16_t.  TRANS: A(i, r) = A[r][i].
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST>
-__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradParams p) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ, NST>;
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, int G>
+__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qgrad_kernel(GradParams p) {
+  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, G>;
   constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
-  extern __shared__ __align__(16) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  extern __shared__ __align__(16) unsigned char shared[];
+  const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = all / Cfg::WAVES, wave = all % Cfg::WAVES, tid = wave * 64 + lane;
+  unsigned char* const smem = shared + group * Cfg::RING;
   TileAt t;
   if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
   const int split = t.split, j0 = t.j * TJ;
   const i64 i0 = (i64)t.i * TI;
-  const int c_beg = split * p.per, c_end = min(p.planes * p.nch, c_beg + p.per);
+  const int w_beg = split * p.per, w_end = min(p.planes * p.nch, w_beg + p.per), turns = (w_end - w_beg + G - 1) / G;
+  const int c_beg = w_beg + group * turns, c_end = min(w_end, c_beg + turns);   // (all groups take as many turns)
 
   // ---- copies of A: 8 rows of 64 channels (direct) or 1 KB of rows of TI channels
   constexpr int CPW = Cfg::CPW, RPC = TRANS ? 512 / TI : 8;   // rows a copy
@@ -246,7 +251,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   const int pair = tid % (TI / 2), share = tid / (TI / 2);
   float sum0 = 0.f, sum1 = 0.f;
 
-  if (c_beg < c_end) {
+  if (turns > 0) {
     Codes next;
     if constexpr (Cfg::DEEP) {
       issue_q(0);
@@ -266,7 +271,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     }
     next_a();
     int slot = 0;   // of A (and, of the ring of codes, this chunk's, which is free again)
-    for (int c = c_beg; c < c_end; ++c) {
+    for (int c = c_beg; c < c_beg + turns; ++c) {
       landed<Cfg::DEEP ? Cfg::GROUP * (NST - 2) : 0>();   // this chunk is in place for all waves, and all have read the one before
       const unsigned char* cur = smem + slot * Cfg::A_BYTES;
       const unsigned char* curb = smem + Cfg::B_AT + ((c - c_beg) & 1) * Cfg::B_BYTES;
@@ -319,14 +324,14 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
     landed<0>();
   }
   if (sums) {
-    float* part = reinterpret_cast<float*>(smem);
-    part[share * TI + 2 * pair] = sum0;
-    part[share * TI + 2 * pair + 1] = sum1;
+    float* part = reinterpret_cast<float*>(shared);
+    part[(group * SHARE + share) * TI + 2 * pair] = sum0;
+    part[(group * SHARE + share) * TI + 2 * pair + 1] = sum1;
     __syncthreads();
-    if (tid < TI && i0 + tid < p.I) {
+    if (group == 0 && tid < TI && i0 + tid < p.I) {
       float v = 0.f;
 #pragma unroll
-      for (int x = 0; x < SHARE; ++x) v += part[x * TI + tid];
+      for (int x = 0; x < G * SHARE; ++x) v += part[x * TI + tid];
       p.db[split * p.I + i0 + tid] = v;
     }
     __syncthreads();
@@ -335,7 +340,11 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
   // ---- out, 32 rows of this wave at a time: a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..;
   // through LDS they become whole rows
   constexpr int LPR = WJ / 8;   // lanes a row, 8 channels each
-  unsigned char* mine = smem + wave * 32 * Cfg::PITCH;
+  unsigned char* mine = shared + all * 32 * Cfg::PITCH;
+  auto meet = [] {
+    if constexpr (G > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+  };
   const int col = (lane % LPR) * 8, n = j0 + wj + col;
   OUT* C = static_cast<OUT*>(p.C) + (p.splits > 1 ? (i64)split * p.I * p.ldc : 0);
   const OUT* add = static_cast<const OUT*>(p.add);
@@ -348,22 +357,25 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qgrad_kernel(GradP
       for (int e = 0; e < 16; e += 4)
         *reinterpret_cast<float4*>(mine + (lane & 31) * Cfg::PITCH + (j * 32 + 8 * (e >> 2) + 4 * kb) * 4) =
             make_float4(acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]);
-    __builtin_amdgcn_wave_barrier();
+    meet();
+    constexpr int RPI = 64 / LPR;   // rows at a time, a group after the other
 #pragma unroll
-    for (int r = 0; r < 32; r += 64 / LPR) {
-      const int at = r + lane / LPR;
+    for (int r0 = 0; r0 < 32; r0 += RPI * G) {
+      const int at = r0 + group * RPI + lane / LPR;
       const i64 row = i0 + wi + i * 32 + at;
-      float v[8];
+      float v[8] = {};
 #pragma unroll
-      for (int h = 0; h < 8; h += 4) {
-        const float4 w = *reinterpret_cast<const float4*>(mine + at * Cfg::PITCH + (col + h) * 4);
-        v[h] = w.x; v[h + 1] = w.y; v[h + 2] = w.z; v[h + 3] = w.w;
-      }
+      for (int o = 0; o < G; ++o)
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+          const float4 w = *reinterpret_cast<const float4*>(shared + ((o * Cfg::WAVES + wave) * 32 + at) * Cfg::PITCH + (col + h) * 4);
+          v[h] += w.x; v[h + 1] += w.y; v[h + 2] += w.z; v[h + 3] += w.w;
+        }
       if (row >= p.I || n >= p.J) continue;
       OUT* o = C + row * p.ldc + n;
       store8<OUT>(o, add ? add + row * p.ldc + n : nullptr, v, vec, p.J - n);
     }
-    __builtin_amdgcn_wave_barrier();
+    meet();
   }
 }
 
@@ -423,25 +435,35 @@ __global__ __launch_bounds__(256) void qcopy_kernel(i64 M, int N, int N8, const 
     out[x] = n < N ? dz[m * ldz + n] : (bf16_t)0.f;
   }
 }
-template <bool BY_ROW>
-__global__ __launch_bounds__(256) void qsplit_kernel(i64 M, int N, int N8, const float* __restrict__ dz, i64 ldz, const float* __restrict__ s,
-                                                     bf16_t* __restrict__ out) {
+__device__ __forceinline__ void split3(float v, bf16_t (&part)[3]) {
+  part[0] = (bf16_t)v; part[1] = part[2] = (bf16_t)0.f;   // (infinities and NaN: whole)
+  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {   // the 8 leading bits, what is left of it, and the rest of that: each exact
+    const float t = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+    part[i] = (bf16_t)t;
+    v -= t;
+  }
+}
+// by_col: dz sw, by_row: dz sx; null = not wanted
+__global__ __launch_bounds__(256) void qsplit_kernel(i64 M, int N, int N8, const float* __restrict__ dz, i64 ldz, const float* __restrict__ sw,
+                                                     const float* __restrict__ sx, bf16_t* __restrict__ by_col, bf16_t* __restrict__ by_row) {
   const i64 total = M * N8;
   for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
     const i64 m = x / N8;
     const int n = (int)(x - m * N8);
-    float v = n < N ? dz[m * ldz + n] * s[BY_ROW ? m : n] : 0.f;
-    bf16_t part[3] = {(bf16_t)v, (bf16_t)0.f, (bf16_t)0.f};   // (infinities and NaN: whole)
-    if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) {
+    const float v = n < N ? dz[m * ldz + n] : 0.f;
+    bf16_t part[3];
+    if (by_col) {
+      split3(n < N ? v * sw[n] : 0.f, part);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) {   // the 8 leading bits, what is left of it, and the rest of that: each exact
-        const float t = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-        part[i] = (bf16_t)t;
-        v -= t;
-      }
+      for (int i = 0; i < 3; ++i) by_col[i * total + x] = part[i];
     }
+    if (by_row) {
+      split3(n < N ? v * sx[m] : 0.f, part);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) out[i * total + x] = part[i];
+      for (int i = 0; i < 3; ++i) by_row[i * total + x] = part[i];
+    }
   }
 }
 
@@ -479,9 +501,9 @@ int grid_of(i64 work) { const i64 b = (work + 255) / 256; return (int)(b < 1 ? 1
 constexpr int CUS = 256;
 
 // The cheapest of tiles of 64 (as long as they are a round), 128 and 256, and of 1 to 256 parts of the sum, by what was measured in us: a
-// launch 2.5, every round of workgroups 2.3, 2.8 or 7 and, for each chunk, 0.5, 0.76 or 1.85 with a workgroup alone on its compute unit,
-// 1.4 with two (128); parts cost another launch and their sums' way through memory.  dW of 1568 x 2048 x 512: 64 whole 17.3, in two parts
-// 28, 128 whole 24.2, in two 22.7, in four 22.5; dx of 64 x 2048 x 512: 64 8.0, 128 9.8; of 200 x 1024 x 4096: 64 whole 32.8, in four 16.7,
+// launch 2.5, every round of workgroups 2.3, 3.2 or 7 and, for each chunk, 0.36, 0.76 or 1.85 with a workgroup alone on its compute unit,
+// 1.4 with two (128); parts cost another launch and their sums' way through memory.  With one group of waves a tile, dW of 1568 x
+// 2048 x 512: 64 whole 17.3 (with two 14.3), in two parts 28, 128 whole 24.2, in two 22.7, in four 22.5; dx of 64 x 2048 x 512: 64 8.0, 128 9.8; of 200 x 1024 x 4096: 64 whole 32.8, in four 16.7,
 // 128 whole 47, in eight 17.8; of 1568 x 8192 x 2048: 128 82, 256 59.5; of 100352 x 256 x 64: 128 19.4, 256 20.3.
 struct Plan { int tile, splits, per; };
 Plan plan_of(i64 I, int J, i64 R, int planes) {
@@ -497,8 +519,8 @@ Plan plan_of(i64 I, int J, i64 R, int planes) {
       if (tile == 64 && w > CUS) break;
       const bool alone = w <= CUS;
       const double rounds = (double)(i64)(tile == 256 ? (w + 255) / 256 : (w + 511) / 512);
-      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.76 : 1.4) : 0.5;
-      const double us = 2.5 + rounds * ((tile == 256 ? 7 : tile == 128 ? 2.8 : 2.3) + chunk * per) + (parts > 1 ? 4 + 2e-6 * parts * (double)I * J : 0);
+      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.76 : 1.4) : 0.36;
+      const double us = 2.5 + rounds * ((tile == 256 ? 7 : tile == 128 ? 3.2 : 2.3) + chunk * per) + (parts > 1 ? 4 + 2e-6 * parts * (double)I * J : 0);
       if (us < best) {
         best = us;
         pl = {tile, parts, per};
@@ -524,7 +546,7 @@ Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outp
   const int N8 = (p.N + 7) & ~7;
   const int planes = p.dtype == CONVBN_BF16 ? 1 : 3;
   s.copy = 0;
-  if (p.dtype != CONVBN_BF16) s.copy = (size_t)3 * p.M * N8 * 2;
+  if (p.dtype != CONVBN_BF16) s.copy = (size_t)6 * p.M * N8 * 2;   // three parts, for either product
   else s.copy = (size_t)p.M * N8 * 2;
   const Plan dx = plan_of(p.M, p.K, p.N, planes), dw = plan_of(p.N, p.K, p.M, planes);
   const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * (p.K + 1) * 4 : 0;
@@ -535,23 +557,23 @@ Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outp
   return s;
 }
 
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST>
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, int G>
 hipError_t launch_tiles(const GradParams& g, hipStream_t st) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ, NST>;
+  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, G>;
   static LdsLimitOnce once;
-  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ, NST>;
+  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ, NST, G>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   const int total = g.nti * g.ntj * g.splits;
-  k<<<((total + 7) / 8) * 8, Cfg::NT, Cfg::LDS, st>>>(g);
+  k<<<((total + 7) / 8) * 8, Cfg::NT * G, Cfg::LDS, st>>>(g);
   return hipGetLastError();
 }
 template <typename OUT, bool TRANS> hipError_t by_tile(int tile, const GradParams& g, hipStream_t st) {
-  if (tile == 256) return launch_tiles<OUT, TRANS, 256, 256, 64, 128, 2>(g, st);
-  if (tile == 64) return launch_tiles<OUT, TRANS, 64, 64, 32, 32, 8>(g, st);
+  if (tile == 256) return launch_tiles<OUT, TRANS, 256, 256, 64, 128, 2, 1>(g, st);
+  if (tile == 64) return launch_tiles<OUT, TRANS, 64, 64, 32, 32, 4, 2>(g, st);
   // one workgroup a compute unit: its copies are all that hides the way to memory
-  if (g.nti * g.ntj * g.splits <= CUS) return launch_tiles<OUT, TRANS, 128, 128, 64, 32, 4>(g, st);
-  return launch_tiles<OUT, TRANS, 128, 128, 64, 64, 2>(g, st);
+  if (g.nti * g.ntj * g.splits <= CUS) return launch_tiles<OUT, TRANS, 128, 128, 64, 32, 4, 1>(g, st);
+  return launch_tiles<OUT, TRANS, 128, 128, 64, 64, 2, 1>(g, st);
 }
 
 // sums: column sums of A as well (TRANS, A = dz itself); their partial sums lie behind those of the product
@@ -599,16 +621,17 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
     if (direct(p)) { A = dz; lda = p.ldz; }
     else if (p.M && (p.dx || p.dW)) qcopy_kernel<<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, copy);
   }
+  bf16_t* by_row = copy + 3 * p.M * N8;
+  if constexpr (sizeof(T) == 4)
+    if (p.M && (p.dx || p.dW))
+      qsplit_kernel<<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, p.sx, p.dx ? copy : nullptr, p.dW ? by_row : nullptr);
   if (p.dx && p.M) {
-    if constexpr (sizeof(T) == 4) qsplit_kernel<false><<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, copy);
     const hipError_t e = product<T, false>(p, A, lda, part, false, st);
     if (e != hipSuccess) return e;
   }
   const bool aside = p.db && p.dW && p.M && sizeof(T) == 2;   // the column sums ride in the weight gradient
   if (p.dW) {
-    if constexpr (sizeof(T) == 4)
-      if (p.M) qsplit_kernel<true><<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sx, copy);
-    const hipError_t e = product<T, true>(p, A, lda, part, aside, st);
+    const hipError_t e = product<T, true>(p, sizeof(T) == 4 ? by_row : A, lda, part, aside, st);
     if (e != hipSuccess) return e;
   }
   if (p.db && !aside) {

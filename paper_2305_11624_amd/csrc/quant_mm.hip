@@ -55,26 +55,30 @@ template <typename T> __device__ __forceinline__ bool vectors(const QMul& q) {
   return ((uintptr_t)q.z | (uintptr_t)(q.ldz * sizeof(T)) | (uintptr_t)q.add) % 16 == 0;
 }
 
-// A ring of NST stages of KC channels of TI + TJ rows
-template <int TI, int TJ, int WI, int WJ, int NST_> struct MulCfg {
-  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES, STAGE = (TI + TJ) * KC;
+// G groups of waves divide the workgroup's channels, each with a ring of NST stages of KC channels of TI + TJ rows (one wave on a SIMD waits for
+// its own reads and copies most of the time); their sums meet on the way out.
+template <int TI, int TJ, int WI, int WJ, int NST_, int G> struct MulCfg {
+  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES * G, STAGE = (TI + TJ) * KC;   // WAVES: of a group
   static constexpr int CPW = (TI + TJ) / 8 / WAVES;   // copies a wave, 8 rows each
-  static constexpr int PITCH = WJ * 4 + 16, OUT = WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
-  static constexpr int LDS = NST * STAGE > OUT ? NST * STAGE : OUT;
-  static_assert((TI + TJ) % (16 * WAVES) == 0 && TI % 16 == 0, "whole pairs of copies");
+  static constexpr int PITCH = WJ * 4 + 16, OUT = G * WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
+  static constexpr int LDS = G * NST * STAGE > OUT ? G * NST * STAGE : OUT;
+  static_assert((TI + TJ) % (16 * WAVES) == 0 && TI % 16 == 0 && LDS <= 160 * 1024, "whole pairs of copies");
 };
 
-template <typename T, int TI, int TJ, int WI, int WJ, int NST, bool SPLIT>
-__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulParams p) {
-  using Cfg = MulCfg<TI, TJ, WI, WJ, NST>;
+template <typename T, int TI, int TJ, int WI, int WJ, int NST, int G, bool SPLIT>
+__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qmul_kernel(MulParams p) {
+  using Cfg = MulCfg<TI, TJ, WI, WJ, NST, G>;
   constexpr int FI = WI / 32, FJ = WJ / 32, CPW = Cfg::CPW;
   extern __shared__ __align__(16) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = all / Cfg::WAVES, wave = all % Cfg::WAVES;
+  unsigned char* const ring = smem + group * NST * Cfg::STAGE;
   TileAt t;
   if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
   const int split = t.split, j0 = t.j * TJ;
   const i64 i0 = (i64)t.i * TI;
-  const int c_beg = split * p.per, c_end = min(p.nch, c_beg + p.per);
+  const int w_beg = split * p.per, w_end = min(p.nch, w_beg + p.per), share = (w_end - w_beg + G - 1) / G;
+  const int c_beg = w_beg + group * share, c_end = min(w_end, c_beg + share);   // (all groups take `share` turns)
 
   // ---- copies: lane l puts 16 codes into piece l % 8 of row l / 8; rows past the end lie past the buffer
   const i64 rows_a = p.m.M - i0 < TI ? p.m.M - i0 : TI;
@@ -88,7 +92,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
     const int copy = wave * CPW + i, row = copy < TI / 8 ? copy * 8 : copy * 8 - TI;
     off[i] = (unsigned)(row + (lane >> 3)) * (unsigned)p.Kp + (g16 ^ (i & 1) * 64);
   }
-  const unsigned lds0 = lds_off(smem) + wave * CPW * 1024;
+  const unsigned lds0 = lds_off(ring) + wave * CPW * 1024;
   auto issue = [&](int c, int slot, int from, int to) {   // (chunks past the end are copied as zeros: every wave has the same copies in flight)
     const unsigned k = (unsigned)c * KC;
     const bool in[2] = {c < c_end && (int)k + g16 < p.Kp, c < c_end && (int)k + (g16 ^ 64) < p.Kp};
@@ -113,10 +117,10 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
 #pragma unroll
   for (int s = 0; s < NST - 1; ++s) issue(c_beg + s, s, 0, CPW);
   int slot = 0;
-  for (int c = c_beg; c < c_end; ++c) {
+  for (int c = c_beg; c < c_beg + share; ++c) {
     landed<CPW * (NST - 2)>();   // this chunk's copies, for all waves; and all have read the chunk before
     const int fill = slot ? slot - 1 : NST - 1;
-    const unsigned char* cur = smem + slot * Cfg::STAGE;
+    const unsigned char* cur = ring + slot * Cfg::STAGE;
     slot = slot + 1 == NST ? 0 : slot + 1;
 #pragma unroll
     for (int s = 0; s < KC / 32; ++s) {
@@ -139,7 +143,11 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
   // ---- out, 32 rows of this wave at a time: a lane holds row l % 32 and, for each e / 4, four channels 8 (e / 4) + 4 (l / 32) ..;
   // through LDS they become whole rows (8 bytes a row straight from the registers: 30 % of the pass at 8192 x 4096 x 8192)
   constexpr int LPR = WJ / 8;   // lanes a row, 8 channels each
-  unsigned char* mine = smem + wave * 32 * Cfg::PITCH;
+  unsigned char* mine = smem + all * 32 * Cfg::PITCH;
+  auto meet = [] {
+    if constexpr (G > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+  };
   const int col = (lane % LPR) * 8, n = j0 + wj + col;
   float sw[8], b[8];
   if constexpr (!SPLIT) {
@@ -158,17 +166,20 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
       for (int e = 0; e < 16; e += 4)
         *reinterpret_cast<i32x4*>(mine + (lane & 31) * Cfg::PITCH + (j * 32 + 8 * (e >> 2) + 4 * kb) * 4) =
             (i32x4){acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-    __builtin_amdgcn_wave_barrier();
+    meet();
+    constexpr int RPI = 64 / LPR;   // rows at a time, a group after the other
 #pragma unroll
-    for (int r = 0; r < 32; r += 64 / LPR) {
-      const int row = r + lane / LPR;
+    for (int r0 = 0; r0 < 32; r0 += RPI * G) {
+      const int row = r0 + group * RPI + lane / LPR;
       const i64 m = i0 + wi + i * 32 + row;
-      int v[8];
+      int v[8] = {};
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const i32x4 w = *reinterpret_cast<const i32x4*>(mine + row * Cfg::PITCH + col * 4 + h * 16);
-        v[4 * h] = w[0]; v[4 * h + 1] = w[1]; v[4 * h + 2] = w[2]; v[4 * h + 3] = w[3];
-      }
+      for (int o = 0; o < G; ++o)
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+          const i32x4 w = *reinterpret_cast<const i32x4*>(smem + ((o * Cfg::WAVES + wave) * 32 + row) * Cfg::PITCH + (col + h) * 4);
+          v[h] += w[0]; v[h + 1] += w[1]; v[h + 2] += w[2]; v[h + 3] += w[3];
+        }
       if (m >= p.m.M || n >= p.m.N) continue;
       if constexpr (SPLIT) {
         int* o = p.part + (split * p.m.M + m) * p.m.N + n;
@@ -184,7 +195,7 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64) void qmul_kernel(MulPar
         finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b, vec);
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    meet();
   }
 }
 
@@ -220,9 +231,10 @@ template <typename T> __global__ __launch_bounds__(256) void qmul_join_kernel(Mu
 constexpr int CUS = 256;
 
 // The cheapest of tiles of 64, 128 and 256, and of 1 to 64 parts of the channel sum, by what was measured in us: a launch 2, every round of
-// workgroups 2, 3 or 6 and, for each chunk, 0.27, 0.5 or 1.85 with a workgroup alone on its compute unit, 0.37 or 1.2 with two (64, 128);
-// parts cost another launch and their sums' way through memory.  1568 x 2048 x 512: 64 whole 8.6, in two parts 14.1, 128 whole 13.3;
-// 64 x 8192 x 2048: 64 whole 20.6, in four parts 13.3; 1568 x 8192 x 2048: 64 51.9, 128 39.5; 100352 x 64 x 256: 64 39.4, 128 23.3;
+// workgroups 2, 3 or 6 and, for each chunk, 0.18, 0.47 or 1.85 with a workgroup alone on its compute unit, 0.37 or 1.2 with two (64, 128);
+// parts cost another launch and their sums' way through memory.  With one group of waves a tile,
+// 1568 x 2048 x 512: 64 whole 8.6 (with two 6.7), in two parts 14.1, 128 whole 13.3; 64 x 8192 x 2048: 64 whole 20.6, in four parts 13.3;
+// 1568 x 8192 x 2048: 64 51.9, 128 39.5 (36.2 with twice the waves); 100352 x 64 x 256: 64 39.4, 128 23.3;
 // 16384 x 1024 x 1024: 128 30.3, 256 26.
 struct Plan { int tile, splits, per; };
 Plan plan_of(i64 M, int N, int K) {
@@ -237,7 +249,7 @@ Plan plan_of(i64 M, int N, int K) {
       const double w = (double)tiles(tile) * parts;
       const bool alone = w <= CUS;
       const double rounds = (double)(i64)(tile == 256 ? (w + 255) / 256 : (w + 511) / 512);
-      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.5 : 1.2) : alone ? 0.27 : 0.37;
+      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.47 : 1.2) : alone ? 0.18 : 0.37;
       const double us = 2 + rounds * ((tile == 256 ? 6 : tile == 128 ? 3 : 2) + chunk * per) + (parts > 1 ? 4.2 + 2e-6 * parts * (double)M * N : 0);
       if (us < best) {
         best = us;
@@ -247,10 +259,10 @@ Plan plan_of(i64 M, int N, int K) {
   return pl;
 }
 
-template <typename T, int TI, int TJ, int WI, int WJ, int NST, bool SPLIT> hipError_t launch_tiles(const MulParams& p, hipStream_t st) {
-  using Cfg = MulCfg<TI, TJ, WI, WJ, NST>;
+template <typename T, int TI, int TJ, int WI, int WJ, int NST, int G, bool SPLIT> hipError_t launch_tiles(const MulParams& p, hipStream_t st) {
+  using Cfg = MulCfg<TI, TJ, WI, WJ, NST, G>;
   static LdsLimitOnce once;
-  auto* k = &qmul_kernel<T, TI, TJ, WI, WJ, NST, SPLIT>;
+  auto* k = &qmul_kernel<T, TI, TJ, WI, WJ, NST, G, SPLIT>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   k<<<(p.nti * p.ntj * p.splits + 7) / 8 * 8, Cfg::NT, Cfg::LDS, st>>>(p);
@@ -258,9 +270,9 @@ template <typename T, int TI, int TJ, int WI, int WJ, int NST, bool SPLIT> hipEr
 }
 template <typename T, bool SPLIT> hipError_t by_tile(int tile, const MulParams& p, hipStream_t st) {
   const bool alone = p.nti * p.ntj * p.splits <= CUS;   // one workgroup a compute unit: its copies are all that hides the way to memory
-  if (tile == 256) return launch_tiles<T, 256, 256, 64, 128, 2, SPLIT>(p, st);
-  if (tile == 128) return alone ? launch_tiles<T, 128, 128, 64, 64, 4, SPLIT>(p, st) : launch_tiles<T, 128, 128, 64, 64, 2, SPLIT>(p, st);
-  return alone ? launch_tiles<T, 64, 64, 32, 32, 8, SPLIT>(p, st) : launch_tiles<T, 64, 64, 32, 32, 4, SPLIT>(p, st);
+  if (tile == 256) return launch_tiles<T, 256, 256, 64, 128, 2, 1, SPLIT>(p, st);
+  if (tile == 128) return alone ? launch_tiles<T, 128, 128, 32, 64, 4, 1, SPLIT>(p, st) : launch_tiles<T, 128, 128, 64, 64, 2, 1, SPLIT>(p, st);
+  return alone ? launch_tiles<T, 64, 64, 32, 32, 4, 2, SPLIT>(p, st) : launch_tiles<T, 64, 64, 32, 32, 4, 1, SPLIT>(p, st);
 }
 template <typename T> hipError_t mul_t(const MulParams& p, int tile, hipStream_t st) {
   if (p.splits == 1) return by_tile<T, false>(tile, p, st);
