@@ -39,13 +39,13 @@ struct GradParams {
   float* db;            // TRANS: column sums of A, [splits][I]; null: not wanted
 };
 
-// NST stages of A; two of the codes as bf16 numbers.  Up to two stages the codes come through registers, a chunk ahead; with more they
-// have a ring of their own, as they are in memory, and a copy of the scales for each wave.
+// NST stages of A; two of the codes as bf16 numbers.  The codes come through registers, a chunk ahead, or (DEEP) have a ring of their own,
+// as they are in memory, and a copy of the scales for each wave.
 // G groups of waves divide the workgroup's part of the sum, each with rings of its own (one wave on a SIMD waits for its own reads and
 // copies most of the time); their sums meet on the way out.
-template <int TI, int TJ, int WI, int WJ, int NST_, int G> struct GradCfg {
+template <int TI, int TJ, int WI, int WJ, int NST_, bool DEEP_, int G> struct GradCfg {
   static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;   // of a group
-  static constexpr bool DEEP = NST > 2;
+  static constexpr bool DEEP = DEEP_;
   static constexpr int A_BYTES = TI * RC * 2, B_BYTES = TJ * RC * 2, Q_BYTES = TJ * RC;
   static constexpr int B_AT = NST * A_BYTES, Q_AT = B_AT + 2 * B_BYTES, S_AT = Q_AT + (DEEP ? NST * Q_BYTES : 0);
   static constexpr int RING = S_AT + (DEEP ? NST * WAVES * 256 : 0);
@@ -98,9 +98,9 @@ template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT
 }
 
 // OUT: float or bf16_t.  TRANS: A(i, r) = A[r][i].
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, int G>
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, bool DEEP, int G>
 __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qgrad_kernel(GradParams p) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, G>;
+  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, DEEP, G>;
   constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
   extern __shared__ __align__(16) unsigned char shared[];
   const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -264,15 +264,18 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qgrad_kernel(G
       landed<Cfg::GROUP * (NST - 1)>();
       put(from_ring(0), 0, 0, PB);
     } else {
-      next_a();
-      issue(0, 0, CPW);
+#pragma unroll
+      for (int s = 0; s < NST - 1; ++s) {
+        next_a();
+        issue(s, 0, CPW);
+      }
       put(fetch(), 0, 0, PB);
       next = fetch();
     }
     next_a();
     int slot = 0;   // of A (and, of the ring of codes, this chunk's, which is free again)
     for (int c = c_beg; c < c_beg + turns; ++c) {
-      landed<Cfg::DEEP ? Cfg::GROUP * (NST - 2) : 0>();   // this chunk is in place for all waves, and all have read the one before
+      landed<(Cfg::DEEP ? Cfg::GROUP : CPW) * (NST - 2)>();   // this chunk is in place for all waves, and all have read the one before
       const unsigned char* cur = smem + slot * Cfg::A_BYTES;
       const unsigned char* curb = smem + Cfg::B_AT + ((c - c_beg) & 1) * Cfg::B_BYTES;
       const int fill = slot ? slot - 1 : NST - 1;
@@ -557,11 +560,11 @@ Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outp
   return s;
 }
 
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, int G>
+template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, bool DEEP, int G>
 hipError_t launch_tiles(const GradParams& g, hipStream_t st) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, G>;
+  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, DEEP, G>;
   static LdsLimitOnce once;
-  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ, NST, G>;
+  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ, NST, DEEP, G>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   const int total = g.nti * g.ntj * g.splits;
@@ -569,11 +572,11 @@ hipError_t launch_tiles(const GradParams& g, hipStream_t st) {
   return hipGetLastError();
 }
 template <typename OUT, bool TRANS> hipError_t by_tile(int tile, const GradParams& g, hipStream_t st) {
-  if (tile == 256) return launch_tiles<OUT, TRANS, 256, 256, 64, 128, 2, 1>(g, st);
-  if (tile == 64) return launch_tiles<OUT, TRANS, 64, 64, 32, 32, 4, 2>(g, st);
+  if (tile == 256) return launch_tiles<OUT, TRANS, 256, 256, TRANS ? 64 : 128, TRANS ? 128 : 64, 3, false, 1>(g, st);
+  if (tile == 64) return launch_tiles<OUT, TRANS, 64, 64, 32, 32, 4, true, 2>(g, st);
   // one workgroup a compute unit: its copies are all that hides the way to memory
-  if (g.nti * g.ntj * g.splits <= CUS) return launch_tiles<OUT, TRANS, 128, 128, 64, 32, 4, 1>(g, st);
-  return launch_tiles<OUT, TRANS, 128, 128, 64, 64, 2, 1>(g, st);
+  if (g.nti * g.ntj * g.splits <= CUS) return launch_tiles<OUT, TRANS, 128, 128, 64, 32, 4, true, 1>(g, st);
+  return launch_tiles<OUT, TRANS, 128, 128, 64, 64, 2, false, 1>(g, st);
 }
 
 // sums: column sums of A as well (TRANS, A = dz itself); their partial sums lie behind those of the product

@@ -55,24 +55,26 @@ template <typename T> __device__ __forceinline__ bool vectors(const QMul& q) {
   return ((uintptr_t)q.z | (uintptr_t)(q.ldz * sizeof(T)) | (uintptr_t)q.add) % 16 == 0;
 }
 
-// G groups of waves divide the workgroup's channels, each with a ring of NST stages of KC channels of TI + TJ rows (one wave on a SIMD waits for
-// its own reads and copies most of the time); their sums meet on the way out.
-template <int TI, int TJ, int WI, int WJ, int NST_, int G> struct MulCfg {
-  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES * G, STAGE = (TI + TJ) * KC;   // WAVES: of a group
-  static constexpr int CPW = (TI + TJ) / 8 / WAVES;   // copies a wave, 8 rows each
+// G groups of waves divide the workgroup's channels (one wave on a SIMD waits for its own reads and copies most of the time); their sums meet
+// on the way out.  Each has a ring of NB halves, a half being KC channels of its tile's rows of x or of the weight: chunk c's are halves 2 c and
+// 2 c + 1 of the sequence, and while it is multiplied halves 2 c + NB - 2 and 2 c + NB - 1 are copied.  (Five halves for 256 x 256 tiles, all of LDS, so
+// that copies are in flight across the barrier: 8192 x 4096 x 8192 240.7 us, with four 237.7.)
+template <int TI_, int WI, int WJ, int NB_, int G> struct MulCfg {
+  static constexpr int NB = NB_, WAVES = (TI_ / WI) * (TI_ / WJ), NT = 64 * WAVES * G, HALF = TI_ * KC;   // WAVES: of a group
+  static constexpr int CPH = TI_ / 8 / WAVES;   // copies a wave and half, 8 rows each
   static constexpr int PITCH = WJ * 4 + 16, OUT = G * WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
-  static constexpr int LDS = G * NST * STAGE > OUT ? G * NST * STAGE : OUT;
-  static_assert((TI + TJ) % (16 * WAVES) == 0 && TI % 16 == 0 && LDS <= 160 * 1024, "whole pairs of copies");
+  static constexpr int LDS = G * NB * HALF > OUT ? G * NB * HALF : OUT;
+  static_assert(TI_ % (16 * WAVES) == 0 && NB >= 4 && NB % 2 == 0 && LDS <= 160 * 1024, "whole pairs of copies");
 };
 
-template <typename T, int TI, int TJ, int WI, int WJ, int NST, int G, bool SPLIT>
-__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qmul_kernel(MulParams p) {
-  using Cfg = MulCfg<TI, TJ, WI, WJ, NST, G>;
-  constexpr int FI = WI / 32, FJ = WJ / 32, CPW = Cfg::CPW;
+template <typename T, int TI, int WI, int WJ, int NB, int G, bool SPLIT>
+__global__ __launch_bounds__((TI / WI) * (TI / WJ) * 64 * G) void qmul_kernel(MulParams p) {
+  using Cfg = MulCfg<TI, WI, WJ, NB, G>;
+  constexpr int TJ = TI, FI = WI / 32, FJ = WJ / 32, CPH = Cfg::CPH;
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, all = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = all / Cfg::WAVES, wave = all % Cfg::WAVES;
-  unsigned char* const ring = smem + group * NST * Cfg::STAGE;
+  unsigned char* const ring = smem + group * NB * Cfg::HALF;
   TileAt t;
   if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
   const int split = t.split, j0 = t.j * TJ;
@@ -86,19 +88,17 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qmul_kernel(Mu
   const i32x4 ra = make_desc(static_cast<const uint8_t*>(p.m.qx) + i0 * p.Kp, rows_a * p.Kp);
   const i32x4 rb = make_desc(static_cast<const uint8_t*>(p.m.qw) + (i64)j0 * p.Kp, (i64)rows_b * p.Kp);
   const int g16 = ((lane & 7) ^ (lane >> 4)) * 16;   // (a wave's odd copies: ^ 64)
-  unsigned off[CPW];
+  unsigned off[CPH];
 #pragma unroll
-  for (int i = 0; i < CPW; ++i) {
-    const int copy = wave * CPW + i, row = copy < TI / 8 ? copy * 8 : copy * 8 - TI;
-    off[i] = (unsigned)(row + (lane >> 3)) * (unsigned)p.Kp + (g16 ^ (i & 1) * 64);
-  }
-  const unsigned lds0 = lds_off(ring) + wave * CPW * 1024;
-  auto issue = [&](int c, int slot, int from, int to) {   // (chunks past the end are copied as zeros: every wave has the same copies in flight)
+  for (int i = 0; i < CPH; ++i) off[i] = (unsigned)((wave * CPH + i) * 8 + (lane >> 3)) * (unsigned)p.Kp + (g16 ^ (i & 1) * 64);
+  const unsigned lds0 = lds_off(ring) + wave * CPH * 1024;
+  // (chunks past the end are copied as zeros: every wave has the same copies in flight)
+  auto issue = [&](bool weight, int c, int slot, int from, int to) {
     const unsigned k = (unsigned)c * KC;
     const bool in[2] = {c < c_end && (int)k + g16 < p.Kp, c < c_end && (int)k + (g16 ^ 64) < p.Kp};
 #pragma unroll
-    for (int i = 0; i < CPW; ++i)
-      if (i >= from && i < to) dma16(wave * CPW + i < TI / 8 ? ra : rb, in[i & 1] ? off[i] + k : OOB, lds0 + slot * Cfg::STAGE + i * 1024);
+    for (int i = 0; i < CPH; ++i)
+      if (i >= from && i < to) dma16(weight ? rb : ra, in[i & 1] ? off[i] + k : OOB, lds0 + slot * Cfg::HALF + i * 1024);
   };
 
   const int wi = (wave % (TI / WI)) * WI, wj = (wave / (TI / WI)) * WJ, kb = lane >> 5;
@@ -115,23 +115,28 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qmul_kernel(Mu
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
 #pragma unroll
-  for (int s = 0; s < NST - 1; ++s) issue(c_beg + s, s, 0, CPW);
-  int slot = 0;
+  for (int h = 0; h < NB - 2; ++h) issue(h & 1, c_beg + h / 2, h, 0, CPH);
+  int slot = 0;   // of this chunk's rows of x
   for (int c = c_beg; c < c_beg + share; ++c) {
-    landed<CPW * (NST - 2)>();   // this chunk's copies, for all waves; and all have read the chunk before
-    const int fill = slot ? slot - 1 : NST - 1;
-    const unsigned char* cur = ring + slot * Cfg::STAGE;
-    slot = slot + 1 == NST ? 0 : slot + 1;
+    landed<CPH * (NB - 4)>();   // this chunk's copies, for all waves; and all have read the chunk before
+    auto wrap = [](int s) { return s >= NB ? s - NB : s; };
+    const unsigned char* cura = ring + slot * Cfg::HALF;
+    const unsigned char* curb = ring + wrap(slot + 1) * Cfg::HALF;
+    const int first = wrap(slot + NB - 2), second = wrap(slot + NB - 1);
+    slot = wrap(slot + 2);
 #pragma unroll
     for (int s = 0; s < KC / 32; ++s) {
-      // the copies, spread over half of the chunk's multiplies: all of them behind the barrier keep the waves from their first
-      // multiplies (8192 x 4096 x 8192: 246 us; over the first half 240, over all of it 237, but 1568 x 8192 x 2048 43, 42 and 45)
-      issue(c + NST - 1, fill, s * CPW / 2, (s + 1) * CPW / 2);
+      // the copies, spread over the chunk's multiplies: all of them behind the barrier keep the waves from their first multiplies
+      // (8192 x 4096 x 8192: 246 us; over the first half of the chunk 240, over all of it 237; 128 x 128 tiles, 1568 x 8192 x 2048:
+      // 43, 42 and 45)
+      constexpr int OVER = TI == 256 ? 2 : 1;   // steps that a half's copies take
+      if (s < OVER) issue(false, c + NB / 2 - 1, first, s * CPH / OVER, (s + 1) * CPH / OVER);
+      else if (s < 2 * OVER) issue(true, c + NB / 2 - 1, second, (s - OVER) * CPH / OVER, (s - OVER + 1) * CPH / OVER);
       i32x4 af[FI], bf[FJ];
 #pragma unroll
-      for (int f = 0; f < FI; ++f) af[f] = *reinterpret_cast<const i32x4*>(cur + at(wi, s, f));
+      for (int f = 0; f < FI; ++f) af[f] = *reinterpret_cast<const i32x4*>(cura + at(wi, s, f));
 #pragma unroll
-      for (int f = 0; f < FJ; ++f) bf[f] = *reinterpret_cast<const i32x4*>(cur + TI * KC + at(wj, s, f));
+      for (int f = 0; f < FJ; ++f) bf[f] = *reinterpret_cast<const i32x4*>(curb + at(wj, s, f));
 #pragma unroll
       for (int i = 0; i < FI; ++i)
 #pragma unroll
@@ -259,10 +264,10 @@ Plan plan_of(i64 M, int N, int K) {
   return pl;
 }
 
-template <typename T, int TI, int TJ, int WI, int WJ, int NST, int G, bool SPLIT> hipError_t launch_tiles(const MulParams& p, hipStream_t st) {
-  using Cfg = MulCfg<TI, TJ, WI, WJ, NST, G>;
+template <typename T, int TI, int WI, int WJ, int NB, int G, bool SPLIT> hipError_t launch_tiles(const MulParams& p, hipStream_t st) {
+  using Cfg = MulCfg<TI, WI, WJ, NB, G>;
   static LdsLimitOnce once;
-  auto* k = &qmul_kernel<T, TI, TJ, WI, WJ, NST, G, SPLIT>;
+  auto* k = &qmul_kernel<T, TI, WI, WJ, NB, G, SPLIT>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   k<<<(p.nti * p.ntj * p.splits + 7) / 8 * 8, Cfg::NT, Cfg::LDS, st>>>(p);
@@ -270,9 +275,9 @@ template <typename T, int TI, int TJ, int WI, int WJ, int NST, int G, bool SPLIT
 }
 template <typename T, bool SPLIT> hipError_t by_tile(int tile, const MulParams& p, hipStream_t st) {
   const bool alone = p.nti * p.ntj * p.splits <= CUS;   // one workgroup a compute unit: its copies are all that hides the way to memory
-  if (tile == 256) return launch_tiles<T, 256, 256, 64, 128, 2, 1, SPLIT>(p, st);
-  if (tile == 128) return alone ? launch_tiles<T, 128, 128, 32, 64, 4, 1, SPLIT>(p, st) : launch_tiles<T, 128, 128, 64, 64, 2, 1, SPLIT>(p, st);
-  return alone ? launch_tiles<T, 64, 64, 32, 32, 4, 2, SPLIT>(p, st) : launch_tiles<T, 64, 64, 32, 32, 4, 1, SPLIT>(p, st);
+  if (tile == 256) return launch_tiles<T, 256, 64, 128, 4, 1, SPLIT>(p, st);
+  if (tile == 128) return alone ? launch_tiles<T, 128, 32, 64, 8, 1, SPLIT>(p, st) : launch_tiles<T, 128, 64, 64, 4, 1, SPLIT>(p, st);
+  return alone ? launch_tiles<T, 64, 32, 32, 8, 2, SPLIT>(p, st) : launch_tiles<T, 64, 32, 32, 8, 1, SPLIT>(p, st);
 }
 template <typename T> hipError_t mul_t(const MulParams& p, int tile, hipStream_t st) {
   if (p.splits == 1) return by_tile<T, false>(tile, p, st);
