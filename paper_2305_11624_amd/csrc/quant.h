@@ -36,13 +36,13 @@ template <int N> __device__ __forceinline__ void landed() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// Tile (i, j) of nti x ntj and split of a workgroup; false: none.  Workgroups go to the eight XCDs in turn, so each gets a contiguous run
+// Tile (i, j) of nti x ntj and split of workgroup wg; false: none.  Workgroups go to the eight XCDs in turn, so each gets a contiguous run
 // of the order, and the order walks bands of 8 rows of tiles: the 32 workgroups that an XCD runs at a time are about 8 x 4 tiles, which
 // share what they read in its cache.
 struct TileAt { int i, j, split; };
-__device__ __forceinline__ bool tile_at(int nti, int ntj, int splits, TileAt* at) {
-  const int total = nti * ntj * splits, run = (total + 7) >> 3, slot = (int)blockIdx.x >> 3;
-  const int id = ((int)blockIdx.x & 7) * run + slot;
+__device__ __forceinline__ bool tile_at(int wg, int nti, int ntj, int splits, TileAt* at) {
+  const int total = nti * ntj * splits, run = (total + 7) >> 3, slot = wg >> 3;
+  const int id = (wg & 7) * run + slot;
   if (slot >= run || id >= total) return false;
   at->split = id / (nti * ntj);
   const int tile = id - at->split * (nti * ntj), band = tile / (8 * ntj), in = tile - band * 8 * ntj;

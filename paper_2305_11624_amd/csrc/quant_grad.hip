@@ -6,6 +6,8 @@
 //
 // F32: A s is split into three bf16 parts that add up to all 24 bits, the codes stay whole numbers, and the three products are
 // summed in fp32: nothing is rounded below that.
+#include <type_traits>
+
 #include "quant.h"
 
 namespace convbn {
@@ -28,8 +30,9 @@ struct GradParams {
   i64 lda;
   const uint8_t* q;     // [R][Jp]
   const float* s;       // [R], null: 1
-  void* C;              // [I][ldc] of the output type, or [splits][I][J] fp32
-  const void* add;      // laid out like C
+  void* C;              // [I][ldc], bf16 or fp32; several splits: [splits][I][J] fp32
+  const void* add;      // laid out like C, of its type
+  int c_bf16;
   i64 ldc;
   i64 I, R;             // (I: rows of C)
   int J, Jp, Aw;        // Aw: channels of A's rows, a multiple of 8
@@ -43,8 +46,8 @@ struct GradParams {
 // as they are in memory, and a copy of the scales for each wave.
 // G groups of waves divide the workgroup's part of the sum, each with rings of its own (one wave on a SIMD waits for its own reads and
 // copies most of the time); their sums meet on the way out.
-template <int TI, int TJ, int WI, int WJ, int NST_, bool DEEP_, int G> struct GradCfg {
-  static constexpr int NST = NST_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;   // of a group
+template <int TI_, int TJ_, int WI_, int WJ_, int NST_, bool DEEP_, int G_> struct GradCfg {
+  static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, NST = NST_, G = G_, WAVES = (TI / WI) * (TJ / WJ), NT = 64 * WAVES;   // of a group
   static constexpr bool DEEP = DEEP_;
   static constexpr int A_BYTES = TI * RC * 2, B_BYTES = TJ * RC * 2, Q_BYTES = TJ * RC;
   static constexpr int B_AT = NST * A_BYTES, Q_AT = B_AT + 2 * B_BYTES, S_AT = Q_AT + (DEEP ? NST * Q_BYTES : 0);
@@ -97,17 +100,15 @@ template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT
     if (x < left) o[x] = from_f32<OUT>(v[x] + (add ? to_f32(add[x]) : 0.f));
 }
 
-// OUT: float or bf16_t.  TRANS: A(i, r) = A[r][i].
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, bool DEEP, int G>
-__global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qgrad_kernel(GradParams p) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, DEEP, G>;
+// Workgroup wg of a product.  TRANS: A(i, r) = A[r][i].
+template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const GradParams& p, const int wg, unsigned char* const shared) {
+  constexpr int TI = Cfg::TI, TJ = Cfg::TJ, WI = Cfg::WI, WJ = Cfg::WJ, NST = Cfg::NST, G = Cfg::G;
   constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
-  extern __shared__ __align__(16) unsigned char shared[];
   const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = all / Cfg::WAVES, wave = all % Cfg::WAVES, tid = wave * 64 + lane;
   unsigned char* const smem = shared + group * Cfg::RING;
   TileAt t;
-  if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
+  if (!tile_at(wg, p.nti, p.ntj, p.splits, &t)) return;
   const int split = t.split, j0 = t.j * TJ;
   const i64 i0 = (i64)t.i * TI;
   const int w_beg = split * p.per, w_end = min(p.planes * p.nch, w_beg + p.per), turns = (w_end - w_beg + G - 1) / G;
@@ -349,9 +350,8 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qgrad_kernel(G
     else __builtin_amdgcn_wave_barrier();
   };
   const int col = (lane % LPR) * 8, n = j0 + wj + col;
-  OUT* C = static_cast<OUT*>(p.C) + (p.splits > 1 ? (i64)split * p.I * p.ldc : 0);
-  const OUT* add = static_cast<const OUT*>(p.add);
-  const bool vec = ((uintptr_t)C | (uintptr_t)(p.ldc * sizeof(OUT)) | (uintptr_t)add) % 16 == 0;
+  const i64 c0 = p.splits > 1 ? (i64)split * p.I * p.ldc : 0;
+  const bool vec = ((uintptr_t)p.C | (uintptr_t)p.add | (uintptr_t)((p.c_bf16 ? 2 : 4) * p.ldc)) % 16 == 0 && (p.splits == 1 || p.J % 4 == 0);
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
 #pragma unroll
@@ -375,39 +375,63 @@ __global__ __launch_bounds__((TI / WI) * (TJ / WJ) * 64 * G) void qgrad_kernel(G
           v[h] += w.x; v[h + 1] += w.y; v[h + 2] += w.z; v[h + 3] += w.w;
         }
       if (row >= p.I || n >= p.J) continue;
-      OUT* o = C + row * p.ldc + n;
-      store8<OUT>(o, add ? add + row * p.ldc + n : nullptr, v, vec, p.J - n);
+      const i64 o = c0 + row * p.ldc + n;
+      if (p.c_bf16) store8<bf16_t>(static_cast<bf16_t*>(p.C) + o, p.add ? static_cast<const bf16_t*>(p.add) + o : nullptr, v, vec, p.J - n);
+      else store8<float>(static_cast<float*>(p.C) + o, p.add ? static_cast<const float*>(p.add) + o : nullptr, v, vec, p.J - n);
     }
     meet();
   }
 }
 
+using Big = GradCfg<256, 256, 128, 64, 3, false, 1>;
+using BigT = GradCfg<256, 256, 64, 128, 3, false, 1>;       // (dW; dx with these waves: 1096 TFLOP/s at 8192 x 4096 x 4096 and not 1129)
+using Mid = GradCfg<128, 128, 64, 64, 2, false, 1>;
+using MidAlone = GradCfg<128, 128, 64, 32, 4, true, 1>;     // one workgroup a compute unit: its copies are all that hides the way to memory
+using Small = GradCfg<64, 64, 32, 32, 4, true, 2>;
+
+template <bool TRANS, class Cfg> __global__ __launch_bounds__(Cfg::NT * Cfg::G) void qgrad_kernel(GradParams p) {
+  extern __shared__ __align__(16) unsigned char shared[];
+  grad_body<TRANS, Cfg>(p, (int)blockIdx.x, shared);
+}
+// Both gradients in one launch: where neither fills the chip for long, the second need not wait for the last workgroup of the first.
+template <class X, class W> __global__ __launch_bounds__(X::NT * X::G) void qgrad_pair_kernel(GradParams x, GradParams w, int first) {
+  static_assert(X::NT * X::G == W::NT * W::G, "one launch");
+  extern __shared__ __align__(16) unsigned char shared[];
+  if ((int)blockIdx.x < first) grad_body<false, X>(x, (int)blockIdx.x, shared);
+  else grad_body<true, W>(w, (int)blockIdx.x - first, shared);
+}
+
 // C = the sum of the splits + add; likewise the column sums.  Four threads share eight channels (or one, where J is no multiple of 8), each
 // adds every fourth split, and the four sums meet in LDS: the order is the same in every run.
 constexpr int JOIN = 4;
-template <typename OUT>
-__global__ __launch_bounds__(256) void qjoin_kernel(i64 I, int J, int splits, const float* __restrict__ part, OUT* C, i64 ldc, const OUT* add,
-                                                    const float* __restrict__ db_part, float* __restrict__ db) {
+struct JoinParams {
+  i64 I, ldc;
+  int J, splits, blocks;
+  const float* part; void* C; const void* add; const float* db_part; float* db;
+};
+template <typename OUT> __device__ __forceinline__ void join_body(const JoinParams& p, const int wg) {
   __shared__ float meet[JOIN][8][64];
-  const int at = threadIdx.x & 63, q = threadIdx.x >> 6;
-  const bool vec = ((uintptr_t)C | (uintptr_t)(ldc * sizeof(OUT)) | (uintptr_t)add) % 16 == 0;
+  OUT* C = static_cast<OUT*>(p.C);
+  const OUT* add = static_cast<const OUT*>(p.add);
+  const int at = threadIdx.x & 63, q = threadIdx.x >> 6, J = p.J;
+  const bool vec = ((uintptr_t)C | (uintptr_t)(p.ldc * sizeof(OUT)) | (uintptr_t)add) % 16 == 0;
   const int width = J % 8 ? 1 : 8;
-  const i64 mine = I * (J / width), total = mine + (db ? I : 0);   // the column sums come last, one a thread
-  for (i64 x0 = (i64)blockIdx.x * 64; x0 < total; x0 += (i64)gridDim.x * 64) {
+  const i64 mine = p.I * (J / width), total = mine + (p.db ? p.I : 0);   // the column sums come last, one a thread
+  for (i64 x0 = (i64)wg * 64; x0 < total; x0 += (i64)p.blocks * 64) {
     const i64 x = x0 + at;
     float v[8] = {};
     if (x < mine && width == 8) {
 #pragma unroll 4
-      for (int s = q; s < splits; s += JOIN) {
-        const float4* f = reinterpret_cast<const float4*>(part + s * I * J + x * 8);
+      for (int s = q; s < p.splits; s += JOIN) {
+        const float4* f = reinterpret_cast<const float4*>(p.part + s * p.I * J + x * 8);
         const float4 a = f[0], b = f[1];
         v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
       }
     } else if (x < total) {
-      const float* f = x < mine ? part + x : db_part + (x - mine);
-      const i64 apart = x < mine ? I * J : I;
+      const float* f = x < mine ? p.part + x : p.db_part + (x - mine);
+      const i64 apart = x < mine ? p.I * J : p.I;
 #pragma unroll 4
-      for (int s = q; s < splits; s += JOIN) v[0] += f[s * apart];
+      for (int s = q; s < p.splits; s += JOIN) v[0] += f[s * apart];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) meet[q][e][at] = v[e];
@@ -416,17 +440,22 @@ __global__ __launch_bounds__(256) void qjoin_kernel(i64 I, int J, int splits, co
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (meet[0][e][at] + meet[1][e][at]) + (meet[2][e][at] + meet[3][e][at]);
       if (x >= mine) {
-        db[x - mine] = v[0];
+        p.db[x - mine] = v[0];
       } else if (width == 8) {
-        const i64 row = x / (J / 8), o = row * ldc + (x - row * (J / 8)) * 8;
+        const i64 row = x / (J / 8), o = row * p.ldc + (x - row * (J / 8)) * 8;
         store8<OUT>(C + o, add ? add + o : nullptr, v, vec, 8);
       } else {
-        const i64 o = x / J * ldc + x % J;
+        const i64 o = x / J * p.ldc + x % J;
         C[o] = from_f32<OUT>(v[0] + (add ? to_f32(add[o]) : 0.f));
       }
     }
     __syncthreads();
   }
+}
+// (of both gradients, or of one: the other has no blocks)
+template <typename OUT> __global__ __launch_bounds__(256) void qjoin_kernel(JoinParams x, JoinParams w) {
+  if ((int)blockIdx.x < x.blocks) join_body<OUT>(x, (int)blockIdx.x);
+  else join_body<OUT>(w, (int)blockIdx.x - x.blocks);
 }
 
 // dz as the products want it: rows of a multiple of 8 channels, zeros past the last.  F32: A = dz s in three parts, s by row or by column.
@@ -554,37 +583,49 @@ Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outp
   const Plan dx = plan_of(p.M, p.K, p.N, planes), dw = plan_of(p.N, p.K, p.M, planes);
   const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * (p.K + 1) * 4 : 0;
   s.copy = align_up(s.copy, 256);
-  s.part = align_up(px > pw ? px : pw, 256);
+  s.part = align_up(px + pw, 256);
   s.cols = align_up((size_t)colsum_slices(p.M, p.N) * p.N * 4, 256);
   s.total = s.copy + s.part + s.cols;
   return s;
 }
 
-template <typename OUT, bool TRANS, int TI, int TJ, int WI, int WJ, int NST, bool DEEP, int G>
-hipError_t launch_tiles(const GradParams& g, hipStream_t st) {
-  using Cfg = GradCfg<TI, TJ, WI, WJ, NST, DEEP, G>;
+int grid_of(const GradParams& g) { return (g.nti * g.ntj * g.splits + 7) / 8 * 8; }
+
+template <bool TRANS, class Cfg> hipError_t launch_one(const GradParams& g, hipStream_t st) {
   static LdsLimitOnce once;
-  auto* k = &qgrad_kernel<OUT, TRANS, TI, TJ, WI, WJ, NST, DEEP, G>;
+  auto* k = &qgrad_kernel<TRANS, Cfg>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
-  const int total = g.nti * g.ntj * g.splits;
-  k<<<((total + 7) / 8) * 8, Cfg::NT * G, Cfg::LDS, st>>>(g);
+  k<<<grid_of(g), Cfg::NT * Cfg::G, Cfg::LDS, st>>>(g);
   return hipGetLastError();
 }
-template <typename OUT, bool TRANS> hipError_t by_tile(int tile, const GradParams& g, hipStream_t st) {
-  if (tile == 256) return launch_tiles<OUT, TRANS, 256, 256, TRANS ? 64 : 128, TRANS ? 128 : 64, 3, false, 1>(g, st);
-  if (tile == 64) return launch_tiles<OUT, TRANS, 64, 64, 32, 32, 4, true, 2>(g, st);
-  // one workgroup a compute unit: its copies are all that hides the way to memory
-  if (g.nti * g.ntj * g.splits <= CUS) return launch_tiles<OUT, TRANS, 128, 128, 64, 32, 4, true, 1>(g, st);
-  return launch_tiles<OUT, TRANS, 128, 128, 64, 64, 2, false, 1>(g, st);
+template <class X, class W> hipError_t launch_pair(const GradParams& x, const GradParams& w, hipStream_t st) {
+  constexpr int LDS = X::LDS > W::LDS ? X::LDS : W::LDS;
+  static LdsLimitOnce once;
+  auto* k = &qgrad_pair_kernel<X, W>;
+  const hipError_t e = set_lds_limit_once(once, (const void*)k, LDS);
+  if (e != hipSuccess) return e;
+  k<<<grid_of(x) + grid_of(w), X::NT * X::G, LDS, st>>>(x, w, grid_of(x));
+  return hipGetLastError();
 }
 
-// sums: column sums of A as well (TRANS, A = dz itself); their partial sums lie behind those of the product
-template <typename T, bool TRANS>
-hipError_t product(const QGrad& p, const bf16_t* A, i64 lda, float* part, bool sums, hipStream_t st) {
-  GradParams g = {};
+// A product as it is launched, and what joins it
+struct Product { bool on = false; int tile = 0; GradParams g; JoinParams join; };
+bool alone(const Product& r) { return r.tile <= 128 && r.g.nti * r.g.ntj * r.g.splits <= CUS; }
+
+template <bool TRANS> hipError_t launch_product(const Product& r, hipStream_t st) {
+  if (r.tile == 256) return launch_one<TRANS, std::conditional_t<TRANS, BigT, Big>>(r.g, st);
+  if (r.tile == 64) return launch_one<TRANS, Small>(r.g, st);
+  return alone(r) ? launch_one<TRANS, MidAlone>(r.g, st) : launch_one<TRANS, Mid>(r.g, st);
+}
+
+// sums: column sums of A as well (A = dz itself)
+template <bool TRANS> Product product(const QGrad& p, const bf16_t* A, i64 lda, float* part, bool sums) {
+  Product r;
+  GradParams& g = r.g = {};
   const bool f32 = p.dtype != CONVBN_BF16;
   const int N8 = (p.N + 7) & ~7;
+  r.on = true;
   g.planes = f32 ? 3 : 1;
   g.A = A; g.lda = lda; g.plane = p.M * (i64)N8; g.Aw = N8;
   g.q = static_cast<const uint8_t*>(TRANS ? p.qx : p.qw);
@@ -594,21 +635,21 @@ hipError_t product(const QGrad& p, const bf16_t* A, i64 lda, float* part, bool s
   g.R = TRANS ? p.M : p.N;
   g.nch = (int)((g.R + RC - 1) / RC);
   const Plan pl = plan_of(g.I, g.J, g.R, g.planes);
+  r.tile = pl.tile;
   g.splits = pl.splits; g.per = pl.per;
   g.nti = (int)((g.I + pl.tile - 1) / pl.tile); g.ntj = ceil_div(g.J, pl.tile);
-  T* C = static_cast<T*>(TRANS ? p.dW : p.dx);
+  void* C = TRANS ? p.dW : p.dx;
   const i64 ldc = TRANS ? p.K : p.ldx;
-  const T* add = TRANS ? nullptr : static_cast<const T*>(p.add);
+  const void* add = TRANS ? nullptr : p.add;
+  r.join = {};
   if (pl.splits > 1) {
     float* db_part = part + (i64)pl.splits * g.I * g.J;
     g.C = part; g.ldc = g.J; g.db = sums ? db_part : nullptr;
-    const hipError_t e = by_tile<float, TRANS>(pl.tile, g, st);
-    if (e != hipSuccess) return e;
-    qjoin_kernel<T><<<grid_of(4 * (g.I * (g.J % 8 ? g.J : g.J / 8) + (sums ? g.I : 0))), 256, 0, st>>>(g.I, g.J, pl.splits, part, C, ldc, add, db_part, sums ? p.db : nullptr);
-    return hipGetLastError();
+    r.join = {g.I, ldc, g.J, pl.splits, grid_of(4 * (g.I * (g.J % 8 ? g.J : g.J / 8) + (sums ? g.I : 0))), part, C, add, db_part, sums ? p.db : nullptr};
+  } else {
+    g.C = C; g.ldc = ldc; g.add = add; g.c_bf16 = !f32; g.db = sums ? p.db : nullptr;
   }
-  g.C = C; g.ldc = ldc; g.add = add; g.db = sums ? p.db : nullptr;
-  return by_tile<T, TRANS>(pl.tile, g, st);
+  return r;
 }
 
 template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st) {
@@ -628,15 +669,24 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
   if constexpr (sizeof(T) == 4)
     if (p.M && (p.dx || p.dW))
       qsplit_kernel<<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, p.sx, p.dx ? copy : nullptr, p.dW ? by_row : nullptr);
-  if (p.dx && p.M) {
-    const hipError_t e = product<T, false>(p, A, lda, part, false, st);
-    if (e != hipSuccess) return e;
+  // The column sums ride in the weight gradient, except with the largest tiles: the workgroups that add them up would keep the others
+  // waiting (8192 x 4096 x 4096: 26 us more, a launch of their own 14; 1568 x 2048 x 512: 1 us more, a launch 6)
+  const bool aside = p.db && p.dW && p.M && sizeof(T) == 2 && plan_of(p.N, p.K, p.M, 1).tile < 256;
+  Product x, w;
+  if (p.dx && p.M) x = product<false>(p, A, lda, part, false);
+  if (p.dW) w = product<true>(p, sizeof(T) == 4 ? by_row : A, lda, part + (x.on && x.g.splits > 1 ? (i64)x.g.splits * x.g.I * x.g.J : 0), aside);
+  hipError_t e = hipSuccess;
+  if (x.on && w.on && alone(x) && alone(w)) {
+    if (x.tile == 64) e = w.tile == 64 ? launch_pair<Small, Small>(x.g, w.g, st) : launch_pair<Small, MidAlone>(x.g, w.g, st);
+    else e = w.tile == 64 ? launch_pair<MidAlone, Small>(x.g, w.g, st) : launch_pair<MidAlone, MidAlone>(x.g, w.g, st);
+  } else {
+    if (x.on) e = launch_product<false>(x, st);
+    if (e == hipSuccess && w.on) e = launch_product<true>(w, st);
   }
-  const bool aside = p.db && p.dW && p.M && sizeof(T) == 2;   // the column sums ride in the weight gradient
-  if (p.dW) {
-    const hipError_t e = product<T, true>(p, sizeof(T) == 4 ? by_row : A, lda, part, aside, st);
-    if (e != hipSuccess) return e;
-  }
+  if (e != hipSuccess) return e;
+  if (!x.on) x.join = {};
+  if (!w.on) w.join = {};
+  if (x.join.blocks + w.join.blocks) qjoin_kernel<T><<<x.join.blocks + w.join.blocks, 256, 0, st>>>(x.join, w.join);
   if (p.db && !aside) {
     const int slices = colsum_slices(p.M, p.N);
     const i64 per = (p.M + slices - 1) / slices;

@@ -76,7 +76,7 @@ __global__ __launch_bounds__((TI / WI) * (TI / WJ) * 64 * G) void qmul_kernel(Mu
   const int group = all / Cfg::WAVES, wave = all % Cfg::WAVES;
   unsigned char* const ring = smem + group * NB * Cfg::HALF;
   TileAt t;
-  if (!tile_at(p.nti, p.ntj, p.splits, &t)) return;
+  if (!tile_at((int)blockIdx.x, p.nti, p.ntj, p.splits, &t)) return;
   const int split = t.split, j0 = t.j * TJ;
   const i64 i0 = (i64)t.i * TI;
   const int w_beg = split * p.per, w_end = min(p.nch, w_beg + p.per), share = (w_end - w_beg + G - 1) / G;

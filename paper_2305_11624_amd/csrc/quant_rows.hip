@@ -11,19 +11,25 @@ namespace convbn {
 namespace {
 
 constexpr int NT = 256;
-// Maximum over the LPR lanes of a row (all of them call this together).
+// N maxima over the LPR lanes of a row (all of them call this together).
 constexpr int threads_of(int LPR) { return LPR > NT ? LPR : NT; }
-template <int LPR> __device__ __forceinline__ unsigned group_max(unsigned m, unsigned* lds) {
+template <int LPR, int N> __device__ __forceinline__ void group_max(unsigned (&m)[N], unsigned (&lds)[N][16]) {
 #pragma unroll
-  for (int off = (LPR < 64 ? LPR : 64) / 2; off > 0; off >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, off, 64));
+  for (int off = (LPR < 64 ? LPR : 64) / 2; off > 0; off >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) m[i] = max(m[i], (unsigned)__shfl_xor((int)m[i], off, 64));
   if constexpr (LPR > 64) {
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) lds[i][threadIdx.x >> 6] = m[i];
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < LPR / 64; ++w) m = max(m, lds[w]);
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int w = 0; w < LPR / 64; ++w) m[i] = max(m[i], lds[i][w]);
     __syncthreads();   // (the next row's maxima go to the same place)
   }
-  return m;
 }
 
 // f(g) and f'(g)
@@ -44,7 +50,7 @@ struct RowArgs { i64 rows, ld; int K; const void* x; void* out; uint8_t* codes; 
 
 template <typename T, int LPR, int VPL, bool AL>
 __global__ __launch_bounds__(threads_of(LPR)) void qpack_kernel(RowArgs p) {
-  __shared__ unsigned lds[16];
+  __shared__ unsigned lds[1][16];
   constexpr int RPB = threads_of(LPR) / LPR;
   const int lane = threadIdx.x % LPR, row0 = threadIdx.x / LPR;
   const int K = p.K, Kp = qrow(K);
@@ -54,16 +60,17 @@ __global__ __launch_bounds__(threads_of(LPR)) void qpack_kernel(RowArgs p) {
     const T* x = static_cast<const T*>(p.x) + (in ? row : 0) * p.ld;
     uint8_t* codes = p.codes + (in ? row : 0) * Kp;
     F8 f[VPL ? VPL : 1];
-    unsigned m = 0;
+    unsigned m[1] = {0};
     if constexpr (VPL > 0) {
 #pragma unroll
       for (int v = 0; v < VPL; ++v) f[v] = load8<T, AL>(x, (v * LPR + lane) * 8, in ? K : 0);
 #pragma unroll
-      for (int v = 0; v < VPL; ++v) m = max(m, amax8(f[v]));
+      for (int v = 0; v < VPL; ++v) m[0] = max(m[0], amax8(f[v]));
     } else {
-      for (int k = lane * 8; k < K; k += LPR * 8) m = max(m, amax8(load8<T, AL>(x, k, K)));
+      for (int k = lane * 8; k < K; k += LPR * 8) m[0] = max(m[0], amax8(load8<T, AL>(x, k, K)));
     }
-    const Scale sc = scale_of(group_max<LPR>(m, lds));
+    group_max<LPR>(m, lds);
+    const Scale sc = scale_of(m[0]);
     if (!in) continue;
     if (lane == 0) p.scales[row] = sc.s;
     if constexpr (VPL > 0) {
@@ -99,7 +106,7 @@ struct GateArgs {
 
 template <typename T, int KIND, int LPR, int VPL, bool AL>
 __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) {
-  __shared__ unsigned lds[16];
+  __shared__ unsigned lds_h[2][16], lds_y[1][16];
   constexpr int RPB = threads_of(LPR) / LPR, NV = VPL ? VPL : 1;
   const int lane = threadIdx.x % LPR, row0 = threadIdx.x / LPR;
   const int K = p.K, Kp = qrow(K);
@@ -119,9 +126,10 @@ __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) 
       return y;
     };
     F8 g[NV], u[NV], y[NV];
-    unsigned mg = 0, mu = 0, my = 0;
+    unsigned mh[2] = {0, 0}, my[1] = {0};
     auto look = [&](const F8& a, const F8& b2, const F8& c) {
-      mg = max(mg, amax8(a)); mu = max(mu, amax8(b2)); my = max(my, amax8(c));
+      if (p.hc) { mh[0] = max(mh[0], amax8(a)); mh[1] = max(mh[1], amax8(b2)); }
+      if (p.yc) my[0] = max(my[0], amax8(c));
     };
     if constexpr (VPL > 0) {
       const int Kin = in ? K : 0;
@@ -142,9 +150,9 @@ __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) 
         look(g[0], u[0], make(g[0], u[0]));
       }
     }
-    Scale sg = {0, 0}, su = {0, 0}, sy = {0, 0};
-    if (p.hc) { sg = scale_of(group_max<LPR>(mg, lds)); su = scale_of(group_max<LPR>(mu, lds)); }
-    if (p.yc) sy = scale_of(group_max<LPR>(my, lds));
+    if (p.hc) group_max<LPR>(mh, lds_h);
+    if (p.yc) group_max<LPR>(my, lds_y);
+    const Scale sg = scale_of(mh[0]), su = scale_of(mh[1]), sy = scale_of(my[0]);
     if (!in) continue;
     if (lane == 0) {
       if (p.hc) { p.hs[2 * row] = sg.s; p.hs[2 * row + 1] = su.s; }
@@ -203,7 +211,8 @@ int blocks_of(i64 work) { return (int)(work < 1 << 20 ? work : 1 << 20); }   // 
 }  // namespace
 
 // Calls f(LPR, VPL) with the group for rows of K channels: with few rows (at most two a compute unit) one piece a lane as far as that goes, else
-// few lanes and more pieces in flight for each.  us for 4 rows of 8192, forward gate: 256 lanes 7.0, 1024 lanes 3.9.
+// few lanes and more pieces in flight for each.  us, forward gate: 4 rows of 8192 with 256 lanes 7.0,
+// with 1024 4.9; 8192 rows of 8192 with 256 lanes of four pieces 121, with 512 of two 113, with 1024 of one 149.
 template <class F> static hipError_t by_row_length(i64 rows, int K, F&& f) {
   const int pieces = ceil_div(K, 8);
   using std::integral_constant;
@@ -211,7 +220,7 @@ template <class F> static hipError_t by_row_length(i64 rows, int K, F&& f) {
   if (pieces <= (LPR) * (VPL)) return f(integral_constant<int, LPR>{}, integral_constant<int, VPL>{})
   QROW(8, 1); QROW(16, 1); QROW(32, 1); QROW(64, 1);
   if (rows <= 512) { QROW(256, 1); QROW(512, 1); QROW(1024, 1); }
-  QROW(64, 2); QROW(256, 1); QROW(256, 2); QROW(256, 4);
+  QROW(64, 2); QROW(256, 1); QROW(256, 2); QROW(512, 2); QROW(1024, 2);
 #undef QROW
   return f(integral_constant<int, 256>{}, integral_constant<int, 0>{});
 }
