@@ -455,7 +455,9 @@ convbn_status convbn_aux_maxpool_bwd(int dtype, const void *dy, const void *idx,
  * Rows may be strided (ldx, ldz); codes, scales, W and vectors are dense.  M == 0 is no error: nothing is read, dW and db
  * become zero.  A sum over the channels is exact up to K = 131072 (longer, or N above 2^20, M above 2^30:
  * CONVBN_ERR_UNSUPPORTED).  codes and workspace are
- * 16-byte aligned; rows of x, z, dx, dz, h, y, dy, dh need the alignment of their element only (16 bytes are faster). */
+ * 16-byte aligned; rows of x, z, dx, dz, h, y, dy, dh need the alignment of their element only (16 bytes are faster), except
+ * that bf16 gradients dz whose N and ldz are multiples of 8 start on 16 bytes (they are read where they are, others from a copy
+ * in the workspace).  Outputs overlap no input, but for the addends below. */
 typedef struct {
   int64_t M;                  /* rows of x, z, dx, dz (a gate: of h, y, dy, dh)                                      */
   int64_t ldx, ldz;           /* elements from a row of x / dx (a gate: h / dh) and of z / dz (y / dy) to the next;  */

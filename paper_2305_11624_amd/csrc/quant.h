@@ -11,7 +11,9 @@ inline __host__ __device__ int qrow(int channels) { return (channels + 15) & ~15
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// ---- copies from memory into LDS.  Inline asm: what the compiler knows to be such a copy it waits for before every LDS read.
+// ---- copies from memory into LDS.  Inline asm: what the compiler knows to be such a copy it waits for before every LDS read.  Nothing is
+// returned in registers.  Five wait states in front: a vector memory instruction must not follow sooner where a vector instruction wrote one
+// of its scalar registers, and inside asm nobody else counts them (0.3 - 1 % of a pass).
 // `bytes` from p on as a buffer; loads past it return zeros
 __device__ __forceinline__ i32x4 make_desc(const void* p, i64 bytes) {
   const uint64_t a = (uint64_t)p;
@@ -22,12 +24,12 @@ __device__ __forceinline__ i32x4 make_desc(const void* p, i64 bytes) {
 __device__ __forceinline__ unsigned lds_off(const void* p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p; }
 // 16 bytes a lane, lane l's to lds + 16 l (lds: the same for the whole wave)
 __device__ __forceinline__ void dma16(i32x4 desc, unsigned voff, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(desc));   // (m0 holds nothing between instructions that need it)
 }
 // ... 4 bytes a lane
 __device__ __forceinline__ void dma4(i32x4 desc, unsigned voff, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(desc));
 }
 // Until at most N of this wave's copies and loads are in flight; then the workgroup's barrier
@@ -84,6 +86,7 @@ struct QGrad {
   const void* qx; const float* sx; const void* qw; const float* sw; const void* dz; const void* add;
   void* dx; void* dW; float* db;
 };
+bool qgrad_reads_in_place(int dtype, int N, i64 ldz);   // dz on 16 bytes then
 size_t qgrad_scratch(const QGrad& p);
 hipError_t launch_qgrad(const QGrad& p, void* ws, hipStream_t st);
 

@@ -167,7 +167,7 @@ convbn_status convbn_qlinear_bwd(const convbn_qdesc* desc, const void* codes, co
                                  void* stream) {
   i64 ldx, ldz;
   TRY_STATUS(check_linear(desc, &ldx, &ldz));
-  REQUIRE_ROWS(dz, elem(desc));
+  REQUIRE_ROWS(dz, qgrad_reads_in_place(desc->dtype, desc->N, ldz) && (dx || dW) ? 16 : elem(desc));
   OPTIONAL(dx, elem(desc)); OPTIONAL(dW, elem(desc)); OPTIONAL(db, 4);
   if (!dx && !dW && !db && desc->M) return set_error(CONVBN_ERR_NULL, "no output is asked for");
   if (dW) { REQUIRE_ROWS(codes, 16); REQUIRE_ROWS(scales, 4); }

@@ -567,19 +567,16 @@ int colsum_slices(i64 M, int N) {
   return (int)(s < 1 ? 1 : s);
 }
 
-// Whether the products read dz where it is
-bool direct(const QGrad& p) {
-  return p.dtype == CONVBN_BF16 && p.N % 8 == 0 && p.ldz % 8 == 0 && (uintptr_t)p.dz % 16 == 0 && p.ldz <= 1 << 20;
-}
+// Whether the products read dz where it is (its first row on 16 bytes then: qgrad_reads_in_place); else a copy, or the three parts
+bool direct(const QGrad& p) { return qgrad_reads_in_place(p.dtype, p.N, p.ldz); }
 
 struct Scratch { size_t copy, part, cols, total; };
-Scratch scratch_of(const QGrad& p) {   // (for any alignment of dz, and all outputs)
+Scratch scratch_of(const QGrad& p) {   // (for all outputs)
   Scratch s;
   const int N8 = (p.N + 7) & ~7;
   const int planes = p.dtype == CONVBN_BF16 ? 1 : 3;
-  s.copy = 0;
   if (p.dtype != CONVBN_BF16) s.copy = (size_t)6 * p.M * N8 * 2;   // three parts, for either product
-  else s.copy = (size_t)p.M * N8 * 2;
+  else s.copy = direct(p) ? 0 : (size_t)p.M * N8 * 2;
   const Plan dx = plan_of(p.M, p.K, p.N, planes), dw = plan_of(p.N, p.K, p.M, planes);
   const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * (p.K + 1) * 4 : 0;
   s.copy = align_up(s.copy, 256);
@@ -698,6 +695,7 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
 
 }  // namespace
 
+bool qgrad_reads_in_place(int dtype, int N, i64 ldz) { return dtype == CONVBN_BF16 && N % 8 == 0 && ldz % 8 == 0 && ldz <= 1 << 20; }
 size_t qgrad_scratch(const QGrad& p) { return scratch_of(p).total; }
 hipError_t launch_qgrad(const QGrad& p, void* ws, hipStream_t st) {
   return p.dtype == CONVBN_BF16 ? grad_t<bf16_t>(p, ws, st) : grad_t<float>(p, ws, st);

@@ -72,6 +72,7 @@ def test_missing_and_misaligned_pointers():
     assert _bwd(d, dz=None) == B.ERR_NULL and _bwd(d, dx=None, dW=None, db=None) == B.ERR_NULL
     assert _bwd(d, codes=None) == B.ERR_NULL and _bwd(d, w=None) == B.ERR_NULL
     assert _bwd(_qdesc(dtype=B.F32), dz=C.c_void_p(4098)) == B.ERR_UNSUPPORTED
+    assert _bwd(d, dz=C.c_void_p(4104)) == B.ERR_UNSUPPORTED and "16-byte" in B.convbn_last_error()   # read in place: N, ldz multiples of 8
     for name in ("convbn_qpack", "convbn_qunpack"):
         f = getattr(B.lib(), name)
         for i in range(3):
@@ -106,6 +107,12 @@ def test_workspace_query_of_any_size(M, K, N, dtype):
     d = _qdesc(M=M, K=K, N=N, dtype=dtype)
     for p in (B.PASS_FWD, B.PASS_BWD):
         assert B.convbn_qlinear_workspace_bytes(d, p) % 256 == 0
+
+
+def test_gradients_that_are_read_in_place_need_no_copy():
+    n = {N: B.convbn_qlinear_workspace_bytes(_qdesc(M=100000, K=64, N=N), B.PASS_BWD) for N in (32, 31)}
+    assert n[31] >= n[32] + 100000 * 30 * 2      # (less other scratch, which goes by N)
+    assert B.convbn_qlinear_workspace_bytes(_qdesc(M=100000, K=64, N=32, ldz=37), B.PASS_BWD) == n[32] + 100000 * 32 * 2
 
 
 def test_native_call_takes_the_descriptors_rows_only():
