@@ -15,11 +15,10 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // returned in registers.  Five wait states in front: a vector memory instruction must not follow sooner where a vector instruction wrote one
 // of its scalar registers, and inside asm nobody else counts them (0.3 - 1 % of a pass).
 // `bytes` from p on as a buffer; loads past it return zeros
-__device__ __forceinline__ i32x4 make_desc(const void* p, i64 bytes) {
+__device__ __forceinline__ i32x4 make_desc(const void* p, int bytes) {
   const uint64_t a = (uint64_t)p;
-  const i32x4 d = {(int)(uint32_t)a, (int)(uint32_t)(a >> 32) & 0xffff, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000};
-  return (i32x4){__builtin_amdgcn_readfirstlane(d[0]), __builtin_amdgcn_readfirstlane(d[1]), __builtin_amdgcn_readfirstlane(d[2]),
-                 __builtin_amdgcn_readfirstlane(d[3])};
+  return (i32x4){__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xffff),
+                 __builtin_amdgcn_readfirstlane(bytes), 0x00020000};
 }
 __device__ __forceinline__ unsigned lds_off(const void* p) { return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p; }
 // 16 bytes a lane, lane l's to lds + 16 l (lds: the same for the whole wave)

@@ -29,7 +29,7 @@ struct GradParams {
   i64 plane;            // elements of a plane
   i64 lda;
   const uint8_t* q;     // [R][Jp]
-  const float* s;       // [R], null: 1
+  const float* s;       // [R]; null with parts, which hold them
   void* C;              // [I][ldc], bf16 or fp32; several splits: [splits][I][J] fp32
   const void* add;      // laid out like C, of its type
   int c_bf16;
@@ -53,7 +53,7 @@ template <int TI_, int TJ_, int WI_, int WJ_, int NST_, bool DEEP_, int G_> stru
   static constexpr int B_AT = NST * A_BYTES, Q_AT = B_AT + 2 * B_BYTES, S_AT = Q_AT + (DEEP ? NST * Q_BYTES : 0);
   static constexpr int RING = S_AT + (DEEP ? NST * WAVES * 256 : 0);
   static constexpr int CPW = A_BYTES / 1024 / WAVES, QPW = Q_BYTES / 1024 / WAVES;   // copies a wave
-  static constexpr int GROUP = CPW + QPW + 1;                                        // DEEP: of a chunk of A, the next one's codes and scales
+  static constexpr int group(bool parts) { return CPW + QPW + (parts ? 0 : 1); }   // DEEP: copies of a chunk of A, the next one's codes and scales
   static constexpr int PITCH = WJ * 4 + 16, OUT_BYTES = G * WAVES * 32 * PITCH;   // sums of 32 rows a wave on their way out
   static constexpr int LDS = G * RING > OUT_BYTES ? G * RING : OUT_BYTES;
   static_assert(A_BYTES % (2048 * WAVES) == 0 && Q_BYTES % (1024 * WAVES) == 0 && LDS <= 160 * 1024, "whole pairs of copies");
@@ -100,8 +100,8 @@ template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT
     if (x < left) o[x] = from_f32<OUT>(v[x] + (add ? to_f32(add[x]) : 0.f));
 }
 
-// Workgroup wg of a product.  TRANS: A(i, r) = A[r][i].
-template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const GradParams& p, const int wg, unsigned char* const shared) {
+// Workgroup wg of a product.  TRANS: A(i, r) = A[r][i].  PARTS: A comes in p.planes parts with the scales in it (fp32); else in one.
+template <bool TRANS, bool PARTS, class Cfg> __device__ __forceinline__ void grad_body(const GradParams& p, const int wg, unsigned char* const shared) {
   constexpr int TI = Cfg::TI, TJ = Cfg::TJ, WI = Cfg::WI, WJ = Cfg::WJ, NST = Cfg::NST, G = Cfg::G;
   constexpr int NT = Cfg::NT, FI = WI / 32, FJ = WJ / 32;
   const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -129,26 +129,36 @@ template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const
     }
   }
   const unsigned lds0 = lds_off(smem) + wave * CPW * 1024;
-  // Where the next chunk of A starts; past the last one (c >= c_end) nothing is in bounds and zeros are copied: the loop has no branch
-  const int R = (int)p.R;
-  int a_r0 = (c_beg % p.nch) * RC, a_c = c_beg;
-  const bf16_t* a_plane = p.A + (c_beg / p.nch) * p.plane + (TRANS ? i0 : i0 * p.lda);
-  const i64 a_rows = p.I - i0 < TI ? p.I - i0 : TI;
-  const i64 a_step = TRANS ? RC * p.lda : RC, a_full = TRANS ? ((RC - 1) * p.lda + p.Aw - i0) * 2 : ((a_rows - 1) * p.lda + p.Aw) * 2;
-  const int left_last = R - (p.nch - 1) * RC;
-  const i64 a_last = TRANS ? ((left_last - 1) * p.lda + p.Aw - i0) * 2 : 0;
-  const bf16_t* a_ptr = a_plane + (c_beg % p.nch) * a_step;
+  // Where the next chunk of A starts, and how many there are: past the last one nothing is in bounds and zeros are copied, so the loop has
+  // no branch.  In one part every chunk is a step further and only the slice's last can be short; parts start over at the first row.
+  const int R = (int)p.R, left_last = R - (p.nch - 1) * RC, c_in = PARTS ? c_beg % max(p.nch, 1) : c_beg;
+  const bool ends = c_end == p.nch;   // (one part: this slice holds the last chunk)
+  int a_r0 = c_in * RC, a_left = c_end - c_beg;
+  const int a_rows = (int)(p.I - i0 < TI ? p.I - i0 : TI);
+  const int a_full = TRANS ? (int)((RC - 1) * p.lda + p.Aw - i0) * 2 : (int)((a_rows - 1) * p.lda + p.Aw) * 2;
+  const int a_last = TRANS ? (int)((left_last - 1) * p.lda + p.Aw - i0) * 2 : 0;
+  const i64 a_step = TRANS ? RC * p.lda : RC;
+  const bf16_t* a_plane = p.A + (PARTS ? (c_beg / max(p.nch, 1)) * p.plane : 0) + (TRANS ? i0 : i0 * p.lda);
+  const bf16_t* a_ptr = a_plane + c_in * a_step;
   i32x4 a_desc;
   bool a_in[2];
   auto next_a = [&]() {
-    const bool last = a_r0 + RC >= R, live = a_c < c_end;
-    a_desc = make_desc(a_ptr, !live ? 0 : TRANS ? (last ? a_last : a_full) : a_full - a_r0 * 2);
+    int bytes = a_full;
+    if constexpr (!TRANS) bytes -= a_r0 * 2;
+    else if (PARTS ? a_r0 + RC >= R : ends && a_left == 1) bytes = a_last;
+    a_desc = make_desc(a_ptr, a_left > 0 ? bytes : 0);
     a_in[0] = TRANS || a_r0 + dg < p.Aw;
     a_in[1] = TRANS || a_r0 + (dg ^ 32) < p.Aw;
-    ++a_c;
-    a_r0 = last ? 0 : a_r0 + RC;
-    a_plane = last ? a_plane + p.plane : a_plane;
-    a_ptr = last ? a_plane : a_ptr + a_step;
+    --a_left;
+    if constexpr (PARTS) {
+      const bool wrap = a_r0 + RC >= R;
+      a_r0 = wrap ? 0 : a_r0 + RC;
+      a_plane = wrap ? a_plane + p.plane : a_plane;
+      a_ptr = wrap ? a_plane : a_ptr + a_step;
+    } else {
+      a_r0 += RC;
+      a_ptr += a_step;
+    }
   };
   auto issue = [&](int slot, int from, int to) {
 #pragma unroll
@@ -175,41 +185,54 @@ template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const
     q_off[i] = j0 + c < p.Jp ? (unsigned)(r * p.Jp + c) : OOB;
   }
   struct Codes { i32x2 q[PB]; float s[PB]; };
-  int q_r0 = (c_beg % p.nch) * RC, q_c = c_beg;
+  // ... of the codes and (one part) the scales
+  int q_r0 = c_in * RC, q_left = c_end - c_beg;
   const uint8_t* q_ptr = p.q + j0 + (i64)q_r0 * p.Jp;
+  const float* s_ptr = p.s + (PARTS ? 0 : q_r0);
+  const int q_step = RC * p.Jp;
+  auto rows_left = [&]() {
+    const bool last = PARTS ? q_r0 + RC >= R : ends && q_left == 1;
+    return q_left > 0 ? last ? left_last : RC : 0;
+  };
+  auto next_q = [&]() {
+    --q_left;
+    if constexpr (PARTS) {
+      const bool wrap = q_r0 + RC >= R;
+      q_r0 = wrap ? 0 : q_r0 + RC;
+      q_ptr = wrap ? p.q + j0 : q_ptr + q_step;
+    } else {
+      q_ptr += q_step;
+      s_ptr += RC;
+    }
+  };
   auto fetch = [&]() {
     Codes b;
-    const bool last = q_r0 + RC >= R;
-    const int left = q_c < c_end ? last ? left_last : RC : 0;
+    const int left = rows_left();
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(q_ptr, left ? left * p.Jp - j0 : 0);
 #pragma unroll
     for (int t = 0; t < PB; ++t) b.q[t] = __builtin_amdgcn_raw_buffer_load_b64(rq, (int)b_off[t], 0, 0);
-    // (no scales: the codes themselves; the buffer is empty then and what it returns is replaced)
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(p.s + q_r0, p.s ? left * 4 : 0);
+    if constexpr (!PARTS) {
+      const __amdgpu_buffer_rsrc_t rs = make_rsrc(s_ptr, left * 4);
 #pragma unroll
-    for (int t = 0; t < PB; ++t) b.s[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
-    ++q_c;
-    q_r0 = last ? 0 : q_r0 + RC;
-    q_ptr = last ? p.q + j0 : q_ptr + RC * p.Jp;
+      for (int t = 0; t < PB; ++t) b.s[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, (int)s_off[t], 0, 0));
+    }
+    next_q();
     return b;
   };
   auto issue_q = [&](int slot) {   // DEEP: the next chunk's codes and scales
-    const bool last = q_r0 + RC >= R;
-    const int left = q_c < c_end ? last ? left_last : RC : 0;
-    const i32x4 dq = make_desc(q_ptr, left ? left * p.Jp - j0 : 0), ds = make_desc(p.s + q_r0, p.s ? left * 4 : 0);
+    const int left = rows_left();
+    const i32x4 dq = make_desc(q_ptr, left ? left * p.Jp - j0 : 0);
 #pragma unroll
     for (int i = 0; i < QPW; ++i) dma16(dq, q_off[i], lds_off(smem) + Cfg::Q_AT + slot * Cfg::Q_BYTES + (wave * QPW + i) * 1024);
-    dma4(ds, lane * 4, lds_off(smem) + Cfg::S_AT + (slot * Cfg::WAVES + wave) * 256);
-    ++q_c;
-    q_r0 = last ? 0 : q_r0 + RC;
-    q_ptr = last ? p.q + j0 : q_ptr + RC * p.Jp;
+    if constexpr (!PARTS) dma4(make_desc(s_ptr, left * 4), lane * 4, lds_off(smem) + Cfg::S_AT + (slot * Cfg::WAVES + wave) * 256);
+    next_q();
   };
   auto from_ring = [&](int slot) {
     Codes b;
 #pragma unroll
     for (int t = 0; t < PB; ++t) {
       b.q[t] = *reinterpret_cast<const i32x2*>(smem + Cfg::Q_AT + slot * Cfg::Q_BYTES + b_off[t]);
-      b.s[t] = *reinterpret_cast<const float*>(smem + Cfg::S_AT + (slot * Cfg::WAVES + wave) * 256 + s_off[t]);
+      if constexpr (!PARTS) b.s[t] = *reinterpret_cast<const float*>(smem + Cfg::S_AT + (slot * Cfg::WAVES + wave) * 256 + s_off[t]);
     }
     return b;
   };
@@ -218,7 +241,7 @@ template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const
     for (int t = 0; t < PB; ++t) {
       if (t < from || t >= to) continue;
       const uint32_t lo = b.q[t][0], hi = b.q[t][1];
-      const float s = p.s ? b.s[t] : 1.f;
+      const float s = PARTS ? 1.f : b.s[t];
       *reinterpret_cast<uint4*>(smem + Cfg::B_AT + slot * Cfg::B_BYTES + b_lds[t]) =
           make_uint4(code2(lo, 0, s), code2(lo, 2, s), code2(hi, 0, s), code2(hi, 2, s));
     }
@@ -262,7 +285,7 @@ template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const
         issue(s, 0, CPW);
         issue_q(s + 1);
       }
-      landed<Cfg::GROUP * (NST - 1)>();
+      landed<Cfg::group(PARTS) * (NST - 1)>();
       put(from_ring(0), 0, 0, PB);
     } else {
 #pragma unroll
@@ -276,7 +299,7 @@ template <bool TRANS, class Cfg> __device__ __forceinline__ void grad_body(const
     next_a();
     int slot = 0;   // of A (and, of the ring of codes, this chunk's, which is free again)
     for (int c = c_beg; c < c_beg + turns; ++c) {
-      landed<(Cfg::DEEP ? Cfg::GROUP : CPW) * (NST - 2)>();   // this chunk is in place for all waves, and all have read the one before
+      landed<(Cfg::DEEP ? Cfg::group(PARTS) : CPW) * (NST - 2)>();   // this chunk is in place for all waves, and all have read the one before
       const unsigned char* cur = smem + slot * Cfg::A_BYTES;
       const unsigned char* curb = smem + Cfg::B_AT + ((c - c_beg) & 1) * Cfg::B_BYTES;
       const int fill = slot ? slot - 1 : NST - 1;
@@ -389,16 +412,16 @@ using Mid = GradCfg<128, 128, 64, 64, 2, false, 1>;
 using MidAlone = GradCfg<128, 128, 64, 32, 4, true, 1>;     // one workgroup a compute unit: its copies are all that hides the way to memory
 using Small = GradCfg<64, 64, 32, 32, 4, true, 2>;
 
-template <bool TRANS, class Cfg> __global__ __launch_bounds__(Cfg::NT * Cfg::G) void qgrad_kernel(GradParams p) {
+template <bool TRANS, bool PARTS, class Cfg> __global__ __launch_bounds__(Cfg::NT * Cfg::G) void qgrad_kernel(GradParams p) {
   extern __shared__ __align__(16) unsigned char shared[];
-  grad_body<TRANS, Cfg>(p, (int)blockIdx.x, shared);
+  grad_body<TRANS, PARTS, Cfg>(p, (int)blockIdx.x, shared);
 }
 // Both gradients in one launch: where neither fills the chip for long, the second need not wait for the last workgroup of the first.
-template <class X, class W> __global__ __launch_bounds__(X::NT * X::G) void qgrad_pair_kernel(GradParams x, GradParams w, int first) {
+template <bool PARTS, class X, class W> __global__ __launch_bounds__(X::NT * X::G) void qgrad_pair_kernel(GradParams x, GradParams w, int first) {
   static_assert(X::NT * X::G == W::NT * W::G, "one launch");
   extern __shared__ __align__(16) unsigned char shared[];
-  if ((int)blockIdx.x < first) grad_body<false, X>(x, (int)blockIdx.x, shared);
-  else grad_body<true, W>(w, (int)blockIdx.x - first, shared);
+  if ((int)blockIdx.x < first) grad_body<false, PARTS, X>(x, (int)blockIdx.x, shared);
+  else grad_body<true, PARTS, W>(w, (int)blockIdx.x - first, shared);
 }
 
 // C = the sum of the splits + add; likewise the column sums.  Four threads share eight channels (or one, where J is no multiple of 8), each
@@ -588,18 +611,18 @@ Scratch scratch_of(const QGrad& p) {   // (for all outputs)
 
 int grid_of(const GradParams& g) { return (g.nti * g.ntj * g.splits + 7) / 8 * 8; }
 
-template <bool TRANS, class Cfg> hipError_t launch_one(const GradParams& g, hipStream_t st) {
+template <bool TRANS, bool PARTS, class Cfg> hipError_t launch_one(const GradParams& g, hipStream_t st) {
   static LdsLimitOnce once;
-  auto* k = &qgrad_kernel<TRANS, Cfg>;
+  auto* k = &qgrad_kernel<TRANS, PARTS, Cfg>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
   k<<<grid_of(g), Cfg::NT * Cfg::G, Cfg::LDS, st>>>(g);
   return hipGetLastError();
 }
-template <class X, class W> hipError_t launch_pair(const GradParams& x, const GradParams& w, hipStream_t st) {
+template <bool PARTS, class X, class W> hipError_t launch_pair(const GradParams& x, const GradParams& w, hipStream_t st) {
   constexpr int LDS = X::LDS > W::LDS ? X::LDS : W::LDS;
   static LdsLimitOnce once;
-  auto* k = &qgrad_pair_kernel<X, W>;
+  auto* k = &qgrad_pair_kernel<PARTS, X, W>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, LDS);
   if (e != hipSuccess) return e;
   k<<<grid_of(x) + grid_of(w), X::NT * X::G, LDS, st>>>(x, w, grid_of(x));
@@ -610,10 +633,10 @@ template <class X, class W> hipError_t launch_pair(const GradParams& x, const Gr
 struct Product { bool on = false; int tile = 0; GradParams g; JoinParams join; };
 bool alone(const Product& r) { return r.tile <= 128 && r.g.nti * r.g.ntj * r.g.splits <= CUS; }
 
-template <bool TRANS> hipError_t launch_product(const Product& r, hipStream_t st) {
-  if (r.tile == 256) return launch_one<TRANS, std::conditional_t<TRANS, BigT, Big>>(r.g, st);
-  if (r.tile == 64) return launch_one<TRANS, Small>(r.g, st);
-  return alone(r) ? launch_one<TRANS, MidAlone>(r.g, st) : launch_one<TRANS, Mid>(r.g, st);
+template <bool TRANS, bool PARTS> hipError_t launch_product(const Product& r, hipStream_t st) {
+  if (r.tile == 256) return launch_one<TRANS, PARTS, std::conditional_t<TRANS, BigT, Big>>(r.g, st);
+  if (r.tile == 64) return launch_one<TRANS, PARTS, Small>(r.g, st);
+  return alone(r) ? launch_one<TRANS, PARTS, MidAlone>(r.g, st) : launch_one<TRANS, PARTS, Mid>(r.g, st);
 }
 
 // sums: column sums of A as well (A = dz itself)
@@ -650,6 +673,7 @@ template <bool TRANS> Product product(const QGrad& p, const bf16_t* A, i64 lda, 
 }
 
 template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st) {
+  constexpr bool PARTS = sizeof(T) == 4;
   const T* dz = static_cast<const T*>(p.dz);
   const Scratch sc = scratch_of(p);
   bf16_t* copy = static_cast<bf16_t*>(ws);
@@ -674,11 +698,11 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
   if (p.dW) w = product<true>(p, sizeof(T) == 4 ? by_row : A, lda, part + (x.on && x.g.splits > 1 ? (i64)x.g.splits * x.g.I * x.g.J : 0), aside);
   hipError_t e = hipSuccess;
   if (x.on && w.on && alone(x) && alone(w)) {
-    if (x.tile == 64) e = w.tile == 64 ? launch_pair<Small, Small>(x.g, w.g, st) : launch_pair<Small, MidAlone>(x.g, w.g, st);
-    else e = w.tile == 64 ? launch_pair<MidAlone, Small>(x.g, w.g, st) : launch_pair<MidAlone, MidAlone>(x.g, w.g, st);
+    if (x.tile == 64) e = w.tile == 64 ? launch_pair<PARTS, Small, Small>(x.g, w.g, st) : launch_pair<PARTS, Small, MidAlone>(x.g, w.g, st);
+    else e = w.tile == 64 ? launch_pair<PARTS, MidAlone, Small>(x.g, w.g, st) : launch_pair<PARTS, MidAlone, MidAlone>(x.g, w.g, st);
   } else {
-    if (x.on) e = launch_product<false>(x, st);
-    if (e == hipSuccess && w.on) e = launch_product<true>(w, st);
+    if (x.on) e = launch_product<false, PARTS>(x, st);
+    if (e == hipSuccess && w.on) e = launch_product<true, PARTS>(w, st);
   }
   if (e != hipSuccess) return e;
   if (!x.on) x.join = {};

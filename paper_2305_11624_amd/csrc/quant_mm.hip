@@ -83,10 +83,10 @@ __global__ __launch_bounds__((TI / WI) * (TI / WJ) * 64 * G) void qmul_kernel(Mu
   const int c_beg = w_beg + group * share, c_end = min(w_end, c_beg + share);   // (all groups take `share` turns)
 
   // ---- copies: lane l puts 16 codes into piece l % 8 of row l / 8; rows past the end lie past the buffer
-  const i64 rows_a = p.m.M - i0 < TI ? p.m.M - i0 : TI;
+  const int rows_a = (int)(p.m.M - i0 < TI ? p.m.M - i0 : TI);
   const int rows_b = min(p.m.N - j0, TJ);
   const i32x4 ra = make_desc(static_cast<const uint8_t*>(p.m.qx) + i0 * p.Kp, rows_a * p.Kp);
-  const i32x4 rb = make_desc(static_cast<const uint8_t*>(p.m.qw) + (i64)j0 * p.Kp, (i64)rows_b * p.Kp);
+  const i32x4 rb = make_desc(static_cast<const uint8_t*>(p.m.qw) + (i64)j0 * p.Kp, rows_b * p.Kp);
   const int g16 = ((lane & 7) ^ (lane >> 4)) * 16;   // (a wave's odd copies: ^ 64)
   unsigned off[CPH];
 #pragma unroll
