@@ -6,8 +6,6 @@
 //
 // F32: A s is split into three bf16 parts that add up to all 24 bits, the codes stay whole numbers, and the three products are
 // summed in fp32: nothing is rounded below that.
-#include <type_traits>
-
 #include "quant.h"
 
 namespace convbn {
@@ -326,7 +324,9 @@ template <bool TRANS, bool PARTS, class Cfg> __device__ __forceinline__ void gra
 #pragma unroll
       for (int step = 0; step < RC / 16; ++step) {
         if (step + 1 < RC / 16) read(step + 1);
-        issue(fill, step * CPW / 2, (step + 1) * CPW / 2);
+        // (8192 x 4096 x 4096, dx: over half of the chunk's multiplies 241 us, over all of them 232; 1568 x 2048 x 512: 10.8 and 11.1)
+        constexpr int OVER = TI == 256 ? 4 : 2;
+        issue(fill, step * CPW / OVER, (step + 1) * CPW / OVER);
         if constexpr (Cfg::DEEP)
           if (step == 1) issue_q(slot);
         put(b, putb, step * PB / 4, (step + 1) * PB / 4);
@@ -406,8 +406,7 @@ template <bool TRANS, bool PARTS, class Cfg> __device__ __forceinline__ void gra
   }
 }
 
-using Big = GradCfg<256, 256, 128, 64, 3, false, 1>;
-using BigT = GradCfg<256, 256, 64, 128, 3, false, 1>;       // (dW; dx with these waves: 1096 TFLOP/s at 8192 x 4096 x 4096 and not 1129)
+using Big = GradCfg<256, 256, 128, 64, 3, false, 1>;        // (waves of 64 x 128: dW of 8192 x 4096 x 4096 240 us and not 235)
 using Mid = GradCfg<128, 128, 64, 64, 2, false, 1>;
 using MidAlone = GradCfg<128, 128, 64, 32, 4, true, 1>;     // one workgroup a compute unit: its copies are all that hides the way to memory
 using Small = GradCfg<64, 64, 32, 32, 4, true, 2>;
@@ -634,7 +633,7 @@ struct Product { bool on = false; int tile = 0; GradParams g; JoinParams join; }
 bool alone(const Product& r) { return r.tile <= 128 && r.g.nti * r.g.ntj * r.g.splits <= CUS; }
 
 template <bool TRANS, bool PARTS> hipError_t launch_product(const Product& r, hipStream_t st) {
-  if (r.tile == 256) return launch_one<TRANS, PARTS, std::conditional_t<TRANS, BigT, Big>>(r.g, st);
+  if (r.tile == 256) return launch_one<TRANS, PARTS, Big>(r.g, st);
   if (r.tile == 64) return launch_one<TRANS, PARTS, Small>(r.g, st);
   return alone(r) ? launch_one<TRANS, PARTS, MidAlone>(r.g, st) : launch_one<TRANS, PARTS, Mid>(r.g, st);
 }
