@@ -9,44 +9,64 @@ constexpr unsigned ABS = 0x7fffffffu, INF = 0x7f800000u;
 
 struct F8 { float v[8]; };
 
+// Eight channels of a row wherever it starts: one or two 16-byte accesses that need the alignment of an element only (the hardware takes
+// any; rows of odd length cost little more than aligned ones)
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> struct Raw8;
-template <> struct Raw8<bf16_t> { uint4 a; };
-template <> struct Raw8<float> { uint4 a, b; };
+template <> struct __attribute__((packed, aligned(2), may_alias)) Raw8<bf16_t> { u32x4 a; };
+template <> struct __attribute__((packed, aligned(4), may_alias)) Raw8<float> { u32x4 a, b; };
 
 __device__ __forceinline__ F8 widen(const Raw8<bf16_t>& r) {
-  return {{bf16_lo(r.a.x), bf16_hi(r.a.x), bf16_lo(r.a.y), bf16_hi(r.a.y), bf16_lo(r.a.z), bf16_hi(r.a.z), bf16_lo(r.a.w), bf16_hi(r.a.w)}};
+  const u32x4 a = r.a;
+  return {{bf16_lo(a[0]), bf16_hi(a[0]), bf16_lo(a[1]), bf16_hi(a[1]), bf16_lo(a[2]), bf16_hi(a[2]), bf16_lo(a[3]), bf16_hi(a[3])}};
 }
 __device__ __forceinline__ F8 widen(const Raw8<float>& r) {
-  return {{__uint_as_float(r.a.x), __uint_as_float(r.a.y), __uint_as_float(r.a.z), __uint_as_float(r.a.w), __uint_as_float(r.b.x),
-           __uint_as_float(r.b.y), __uint_as_float(r.b.z), __uint_as_float(r.b.w)}};
+  const u32x4 a = r.a, b = r.b;
+  return {{__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[2]), __uint_as_float(a[3]), __uint_as_float(b[0]),
+           __uint_as_float(b[1]), __uint_as_float(b[2]), __uint_as_float(b[3])}};
+}
+template <typename T> __device__ __forceinline__ Raw8<T> narrow(const F8& f) {
+  Raw8<T> r;
+  if constexpr (sizeof(T) == 2) {
+    r.a = (u32x4){pack_bf16x2(f.v[0], f.v[1]), pack_bf16x2(f.v[2], f.v[3]), pack_bf16x2(f.v[4], f.v[5]), pack_bf16x2(f.v[6], f.v[7])};
+  } else {
+    r.a = (u32x4){__float_as_uint(f.v[0]), __float_as_uint(f.v[1]), __float_as_uint(f.v[2]), __float_as_uint(f.v[3])};
+    r.b = (u32x4){__float_as_uint(f.v[4]), __float_as_uint(f.v[5]), __float_as_uint(f.v[6]), __float_as_uint(f.v[7])};
+  }
+  return r;
 }
 
-// Channels k .. k+7 of a row of K (zeros past the end).  AL: every row starts on 16 bytes.
-template <typename T, bool AL> __device__ __forceinline__ F8 load8(const T* __restrict__ row, int k, int K) {
-  if (AL && k + 8 <= K) {
-    const Raw8<T> r = *reinterpret_cast<const Raw8<T>*>(row + k);
-    return widen(r);
-  }
+// Channels k .. k+7 of a row of K (zeros past the end)
+template <typename T> __device__ __forceinline__ F8 load8(const T* __restrict__ row, int k, int K) {
+  if (k + 8 <= K) return widen(*reinterpret_cast<const Raw8<T>*>(row + k));
   F8 f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) f.v[i] = k + i < K ? to_f32(row[k + i]) : 0.f;
   return f;
 }
-template <typename T, bool AL> __device__ __forceinline__ void store8(T* __restrict__ row, int k, int K, const F8& f) {
-  if (AL && k + 8 <= K) {
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(row + k) = make_uint4(pack_bf16x2(f.v[0], f.v[1]), pack_bf16x2(f.v[2], f.v[3]),
-                                                      pack_bf16x2(f.v[4], f.v[5]), pack_bf16x2(f.v[6], f.v[7]));
-    } else {
-      float4* p = reinterpret_cast<float4*>(row + k);
-      p[0] = make_float4(f.v[0], f.v[1], f.v[2], f.v[3]);
-      p[1] = make_float4(f.v[4], f.v[5], f.v[6], f.v[7]);
-    }
+template <typename T> __device__ __forceinline__ void store8(T* __restrict__ row, int k, int K, const F8& f) {
+  if (k + 8 <= K) {
+    *reinterpret_cast<Raw8<T>*>(row + k) = narrow<T>(f);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (k + i < K) row[k + i] = from_f32<T>(f.v[i]);
+}
+// ... a product's result: the addend, if any, comes on top (it may be the same memory)
+template <typename T> __device__ __forceinline__ void store8_plus(T* row, const T* add, int k, int K, F8 f) {
+  if (add) {
+    if (k + 8 <= K) {
+      const F8 a = widen(*reinterpret_cast<const Raw8<T>*>(add + k));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f.v[i] += a.v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + i < K) f.v[i] += to_f32(add[k + i]);
+    }
+  }
+  store8<T>(row, k, K, f);
 }
 
 __device__ __forceinline__ unsigned amax8(const F8& f) {   // (compared as whole numbers: a NaN is the largest of all)

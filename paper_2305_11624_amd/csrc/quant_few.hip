@@ -64,7 +64,7 @@ __global__ __launch_bounds__(1024) void qfew_kernel(FewParams p) {
     const int group = wave / per, first = ((wave % per) * 64 + lane) * 8, hop = per * 512;
     auto piece = [&](int m, int k) {
       const T* x = static_cast<const T*>(p.x) + m * p.ldx;
-      return ((uintptr_t)x & 15) == 0 ? load8<T, true>(x, k, p.m.K) : load8<T, false>(x, k, p.m.K);
+      return load8<T>(x, k, p.m.K);
     };
     if (group < groups)
       for (int m = group; m < M; m += groups) {

@@ -6,7 +6,7 @@
 //
 // F32: A s is split into three bf16 parts that add up to all 24 bits, the codes stay whole numbers, and the three products are
 // summed in fp32: nothing is rounded below that.
-#include "quant.h"
+#include "quant_code.h"
 
 namespace convbn {
 
@@ -71,31 +71,6 @@ __device__ __forceinline__ bf16x8 read_tr8(const unsigned char* p, int rows4) { 
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + rows4));
   typedef short s16x8 __attribute__((ext_vector_type(8)));
   return __builtin_bit_cast(bf16x8, (s16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
-}
-
-// Eight channels of a row (`left` of them inside), with the addend; vec: 16-byte accesses
-template <typename OUT> __device__ __forceinline__ void store8(OUT* o, const OUT* add, float (&v)[8], bool vec, int left) {
-  if (vec && left >= 8) {
-    if constexpr (sizeof(OUT) == 2) {
-      if (add) {
-        const uint4 w = *reinterpret_cast<const uint4*>(add);
-        v[0] += bf16_lo(w.x); v[1] += bf16_hi(w.x); v[2] += bf16_lo(w.y); v[3] += bf16_hi(w.y);
-        v[4] += bf16_lo(w.z); v[5] += bf16_hi(w.z); v[6] += bf16_lo(w.w); v[7] += bf16_hi(w.w);
-      }
-      *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-    } else {
-#pragma unroll
-      for (int h = 0; h < 8; h += 4) {
-        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (add) w = *reinterpret_cast<const float4*>(add + h);
-        *reinterpret_cast<float4*>(o + h) = make_float4(v[h] + w.x, v[h + 1] + w.y, v[h + 2] + w.z, v[h + 3] + w.w);
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int x = 0; x < 8; ++x)
-    if (x < left) o[x] = from_f32<OUT>(v[x] + (add ? to_f32(add[x]) : 0.f));
 }
 
 // Workgroup wg of a product.  TRANS: A(i, r) = A[r][i].  PARTS: A comes in p.planes parts with the scales in it (fp32); else in one.
@@ -374,7 +349,6 @@ template <bool TRANS, bool PARTS, class Cfg> __device__ __forceinline__ void gra
   };
   const int col = (lane % LPR) * 8, n = j0 + wj + col;
   const i64 c0 = p.splits > 1 ? (i64)split * p.I * p.ldc : 0;
-  const bool vec = ((uintptr_t)p.C | (uintptr_t)p.add | (uintptr_t)((p.c_bf16 ? 2 : 4) * p.ldc)) % 16 == 0 && (p.splits == 1 || p.J % 4 == 0);
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
 #pragma unroll
@@ -389,18 +363,18 @@ template <bool TRANS, bool PARTS, class Cfg> __device__ __forceinline__ void gra
     for (int r0 = 0; r0 < 32; r0 += RPI * G) {
       const int at = r0 + group * RPI + lane / LPR;
       const i64 row = i0 + wi + i * 32 + at;
-      float v[8] = {};
+      F8 v = {};
 #pragma unroll
       for (int o = 0; o < G; ++o)
 #pragma unroll
         for (int h = 0; h < 8; h += 4) {
           const float4 w = *reinterpret_cast<const float4*>(shared + ((o * Cfg::WAVES + wave) * 32 + at) * Cfg::PITCH + (col + h) * 4);
-          v[h] += w.x; v[h + 1] += w.y; v[h + 2] += w.z; v[h + 3] += w.w;
+          v.v[h] += w.x; v.v[h + 1] += w.y; v.v[h + 2] += w.z; v.v[h + 3] += w.w;
         }
       if (row >= p.I || n >= p.J) continue;
-      const i64 o = c0 + row * p.ldc + n;
-      if (p.c_bf16) store8<bf16_t>(static_cast<bf16_t*>(p.C) + o, p.add ? static_cast<const bf16_t*>(p.add) + o : nullptr, v, vec, p.J - n);
-      else store8<float>(static_cast<float*>(p.C) + o, p.add ? static_cast<const float*>(p.add) + o : nullptr, v, vec, p.J - n);
+      const i64 o = c0 + row * p.ldc;
+      if (p.c_bf16) store8_plus<bf16_t>(static_cast<bf16_t*>(p.C) + o, p.add ? static_cast<const bf16_t*>(p.add) + o : nullptr, n, p.J, v);
+      else store8_plus<float>(static_cast<float*>(p.C) + o, p.add ? static_cast<const float*>(p.add) + o : nullptr, n, p.J, v);
     }
     meet();
   }
@@ -436,7 +410,6 @@ template <typename OUT> __device__ __forceinline__ void join_body(const JoinPara
   OUT* C = static_cast<OUT*>(p.C);
   const OUT* add = static_cast<const OUT*>(p.add);
   const int at = threadIdx.x & 63, q = threadIdx.x >> 6, J = p.J;
-  const bool vec = ((uintptr_t)C | (uintptr_t)(p.ldc * sizeof(OUT)) | (uintptr_t)add) % 16 == 0;
   const int width = J % 8 ? 1 : 8;
   const i64 mine = p.I * (J / width), total = mine + (p.db ? p.I : 0);   // the column sums come last, one a thread
   for (i64 x0 = (i64)wg * 64; x0 < total; x0 += (i64)p.blocks * 64) {
@@ -464,8 +437,11 @@ template <typename OUT> __device__ __forceinline__ void join_body(const JoinPara
       if (x >= mine) {
         p.db[x - mine] = v[0];
       } else if (width == 8) {
-        const i64 row = x / (J / 8), o = row * p.ldc + (x - row * (J / 8)) * 8;
-        store8<OUT>(C + o, add ? add + o : nullptr, v, vec, 8);
+        const i64 row = x / (J / 8), o = row * p.ldc;
+        F8 f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] = v[e];
+        store8_plus<OUT>(C + o, add ? add + o : nullptr, (int)(x - row * (J / 8)) * 8, J, f);
       } else {
         const i64 o = x / J * p.ldc + x % J;
         C[o] = from_f32<OUT>(v[0] + (add ? to_f32(add[o]) : 0.f));
@@ -482,41 +458,53 @@ template <typename OUT> __global__ __launch_bounds__(256) void qjoin_kernel(Join
 
 // dz as the products want it: rows of a multiple of 8 channels, zeros past the last.  F32: A = dz s in three parts, s by row or by column.
 __global__ __launch_bounds__(256) void qcopy_kernel(i64 M, int N, int N8, const bf16_t* __restrict__ dz, i64 ldz, bf16_t* __restrict__ out) {
-  const i64 total = M * N8;
-  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
-    const i64 m = x / N8;
-    const int n = (int)(x - m * N8);
-    out[x] = n < N ? dz[m * ldz + n] : (bf16_t)0.f;
+  const unsigned pieces = N8 >> 3;
+  const i64 total = M * pieces;
+  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < total; i += (i64)gridDim.x * 256) {
+    const i64 m = i >> 32 ? i / pieces : (i64)((unsigned)i / pieces);
+    const int n = (int)(i - m * pieces) * 8;
+    store8<bf16_t>(out + m * N8, n, N8, load8<bf16_t>(dz + m * ldz, n, N));
   }
 }
-__device__ __forceinline__ void split3(float v, bf16_t (&part)[3]) {
-  part[0] = (bf16_t)v; part[1] = part[2] = (bf16_t)0.f;   // (infinities and NaN: whole)
-  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) return;
+// v in three parts of 8 bits each, which add up to it; infinities and NaN are the first whole
+__device__ __forceinline__ void split3(const F8& f, F8 (&part)[3]) {
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {   // the 8 leading bits, what is left of it, and the rest of that: each exact
-    const float t = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-    part[i] = (bf16_t)t;
-    v -= t;
+  for (int e = 0; e < 8; ++e) {
+    float v = f.v[e];
+    const bool whole = (__float_as_uint(v) & INF) == INF;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {   // the 8 leading bits, what is left of it, and the rest of that: each exact
+      const float t = whole ? (i ? 0.f : v) : __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+      part[i].v[e] = t;
+      v -= t;
+    }
   }
 }
 // by_col: dz sw, by_row: dz sx; null = not wanted
 __global__ __launch_bounds__(256) void qsplit_kernel(i64 M, int N, int N8, const float* __restrict__ dz, i64 ldz, const float* __restrict__ sw,
                                                      const float* __restrict__ sx, bf16_t* __restrict__ by_col, bf16_t* __restrict__ by_row) {
-  const i64 total = M * N8;
-  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
-    const i64 m = x / N8;
-    const int n = (int)(x - m * N8);
-    const float v = n < N ? dz[m * ldz + n] : 0.f;
-    bf16_t part[3];
+  const unsigned pieces = N8 >> 3;
+  const i64 total = M * pieces, plane = M * N8;
+  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < total; i += (i64)gridDim.x * 256) {
+    const i64 m = i >> 32 ? i / pieces : (i64)((unsigned)i / pieces);
+    const int n = (int)(i - m * pieces) * 8;
+    const F8 v = load8<float>(dz + m * ldz, n, N);
+    F8 scaled, part[3];
     if (by_col) {
-      split3(n < N ? v * sw[n] : 0.f, part);
+      const F8 s = load8<float>(sw, n, N);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) by_col[i * total + x] = part[i];
+      for (int e = 0; e < 8; ++e) scaled.v[e] = n + e < N ? v.v[e] * s.v[e] : 0.f;
+      split3(scaled, part);
+#pragma unroll
+      for (int x = 0; x < 3; ++x) store8<bf16_t>(by_col + x * plane + m * N8, n, N8, part[x]);
     }
     if (by_row) {
-      split3(n < N ? v * sx[m] : 0.f, part);
+      const float s = sx[m];
 #pragma unroll
-      for (int i = 0; i < 3; ++i) by_row[i * total + x] = part[i];
+      for (int e = 0; e < 8; ++e) scaled.v[e] = n + e < N ? v.v[e] * s : 0.f;
+      split3(scaled, part);
+#pragma unroll
+      for (int x = 0; x < 3; ++x) store8<bf16_t>(by_row + x * plane + m * N8, n, N8, part[x]);
     }
   }
 }
@@ -683,12 +671,12 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
   i64 lda = N8;
   if constexpr (sizeof(T) == 2) {
     if (direct(p)) { A = dz; lda = p.ldz; }
-    else if (p.M && (p.dx || p.dW)) qcopy_kernel<<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, copy);
+    else if (p.M && (p.dx || p.dW)) qcopy_kernel<<<grid_of(p.M * (N8 / 8)), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, copy);
   }
   bf16_t* by_row = copy + 3 * p.M * N8;
   if constexpr (sizeof(T) == 4)
     if (p.M && (p.dx || p.dW))
-      qsplit_kernel<<<grid_of(p.M * N8), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, p.sx, p.dx ? copy : nullptr, p.dW ? by_row : nullptr);
+      qsplit_kernel<<<grid_of(p.M * (N8 / 8)), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, p.sx, p.dx ? copy : nullptr, p.dW ? by_row : nullptr);
   // The column sums ride in the weight gradient, except with the largest tiles: the workgroups that add them up would keep the others
   // waiting (8192 x 4096 x 4096: 26 us more, a launch of their own 14; 1568 x 2048 x 512: 1 us more, a launch 6)
   const bool aside = p.db && p.dW && p.M && sizeof(T) == 2 && plan_of(p.N, p.K, p.M, 1).tile < 256;

@@ -3,7 +3,7 @@
 // Both operands' channels run together, which is what the matrix instruction wants; they pass through LDS as rows of 128 codes whose
 // 16-byte pieces are exchanged by bits 1-3 of the row, so that 16 lanes reading a column of pieces meet distinct banks.  Sums over
 // channels that are split between workgroups stay whole numbers: any order gives the same.
-#include "quant.h"
+#include "quant_code.h"
 
 namespace convbn {
 
@@ -21,38 +21,13 @@ struct MulParams {
   int* part;                  // [splits][M][N], where there are several
 };
 
-// Eight channels n .. n+7 of row m: scaled, with bias and addend, rounded once.  vec: 16-byte accesses
+// Eight channels n .. n+7 of row m: scaled, with bias and addend, rounded once
 template <typename T>
-__device__ __forceinline__ void finish8(const QMul& q, i64 m, int n, const int (&acc)[8], float sx, const float (&sw)[8], const float (&b)[8], bool vec) {
-  T* z = static_cast<T*>(q.z) + m * q.ldz + n;
-  const T* add = q.add ? static_cast<const T*>(q.add) + m * q.ldz + n : nullptr;
-  float v[8];
+__device__ __forceinline__ void finish8(const QMul& q, i64 m, int n, const int (&acc)[8], float sx, const float (&sw)[8], const float (&b)[8]) {
+  F8 f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (float)acc[i] * (sx * sw[i]) + b[i];
-  if (vec && n + 8 <= q.N) {
-    if constexpr (sizeof(T) == 2) {
-      if (add) {
-        const uint4 w = *reinterpret_cast<const uint4*>(add);
-        v[0] += bf16_lo(w.x); v[1] += bf16_hi(w.x); v[2] += bf16_lo(w.y); v[3] += bf16_hi(w.y);
-        v[4] += bf16_lo(w.z); v[5] += bf16_hi(w.z); v[6] += bf16_lo(w.w); v[7] += bf16_hi(w.w);
-      }
-      *reinterpret_cast<uint4*>(z) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-    } else {
-#pragma unroll
-      for (int h = 0; h < 8; h += 4) {
-        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (add) w = *reinterpret_cast<const float4*>(add + h);
-        *reinterpret_cast<float4*>(z + h) = make_float4(v[h] + w.x, v[h + 1] + w.y, v[h + 2] + w.z, v[h + 3] + w.w);
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (n + i < q.N) z[i] = from_f32<T>(v[i] + (add ? to_f32(add[i]) : 0.f));
-}
-template <typename T> __device__ __forceinline__ bool vectors(const QMul& q) {
-  return ((uintptr_t)q.z | (uintptr_t)(q.ldz * sizeof(T)) | (uintptr_t)q.add) % 16 == 0;
+  for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * (sx * sw[i]) + b[i];
+  store8_plus<T>(static_cast<T*>(q.z) + m * q.ldz, q.add ? static_cast<const T*>(q.add) + m * q.ldz : nullptr, n, q.N, f);
 }
 
 // G groups of waves divide the workgroup's channels (one wave on a SIMD waits for its own reads and copies most of the time); their sums meet
@@ -162,7 +137,7 @@ __global__ __launch_bounds__((TI / WI) * (TI / WJ) * 64 * G) void qmul_kernel(Mu
       b[x] = p.m.b && n + x < p.m.N ? p.m.b[n + x] : 0.f;
     }
   }
-  const bool vec = SPLIT ? p.m.N % 4 == 0 : vectors<T>(p.m);
+  const bool vec = p.m.N % 4 == 0;   // (of the partial sums)
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
 #pragma unroll
@@ -197,7 +172,7 @@ __global__ __launch_bounds__((TI / WI) * (TI / WJ) * 64 * G) void qmul_kernel(Mu
             if (n + x < p.m.N) o[x] = v[x];
         }
       } else {
-        finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b, vec);
+        finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b);
       }
     }
     meet();
@@ -207,7 +182,7 @@ __global__ __launch_bounds__((TI / WI) * (TI / WJ) * 64 * G) void qmul_kernel(Mu
 template <typename T> __global__ __launch_bounds__(256) void qmul_join_kernel(MulParams p) {
   const int oct = (p.m.N + 7) >> 3;
   const i64 total = p.m.M * oct;
-  const bool vec = vectors<T>(p.m), pvec = p.m.N % 8 == 0;
+  const bool pvec = p.m.N % 8 == 0;
   for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
     const i64 m = x / oct;
     const int n = (int)(x - m * oct) * 8;
@@ -229,7 +204,7 @@ template <typename T> __global__ __launch_bounds__(256) void qmul_join_kernel(Mu
       sw[i] = n + i < p.m.N ? p.m.sw[n + i] : 0.f;
       b[i] = p.m.b && n + i < p.m.N ? p.m.b[n + i] : 0.f;
     }
-    finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b, vec);
+    finish8<T>(p.m, m, n, v, p.m.sx[m], sw, b);
   }
 }
 

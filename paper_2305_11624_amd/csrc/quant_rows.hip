@@ -48,7 +48,7 @@ template <int KIND> __device__ __forceinline__ void gate_of(float g, float* f, f
 
 struct RowArgs { i64 rows, ld; int K; const void* x; void* out; uint8_t* codes; float* scales; };
 
-template <typename T, int LPR, int VPL, bool AL>
+template <typename T, int LPR, int VPL>
 __global__ __launch_bounds__(threads_of(LPR)) void qpack_kernel(RowArgs p) {
   __shared__ unsigned lds[1][16];
   constexpr int RPB = threads_of(LPR) / LPR;
@@ -63,11 +63,11 @@ __global__ __launch_bounds__(threads_of(LPR)) void qpack_kernel(RowArgs p) {
     unsigned m[1] = {0};
     if constexpr (VPL > 0) {
 #pragma unroll
-      for (int v = 0; v < VPL; ++v) f[v] = load8<T, AL>(x, (v * LPR + lane) * 8, in ? K : 0);
+      for (int v = 0; v < VPL; ++v) f[v] = load8<T>(x, (v * LPR + lane) * 8, in ? K : 0);
 #pragma unroll
       for (int v = 0; v < VPL; ++v) m[0] = max(m[0], amax8(f[v]));
     } else {
-      for (int k = lane * 8; k < K; k += LPR * 8) m[0] = max(m[0], amax8(load8<T, AL>(x, k, K)));
+      for (int k = lane * 8; k < K; k += LPR * 8) m[0] = max(m[0], amax8(load8<T>(x, k, K)));
     }
     group_max<LPR>(m, lds);
     const Scale sc = scale_of(m[0]);
@@ -80,20 +80,22 @@ __global__ __launch_bounds__(threads_of(LPR)) void qpack_kernel(RowArgs p) {
         if (k < Kp) *reinterpret_cast<uint2*>(codes + k) = codes8(f[v], sc.r);
       }
     } else {
-      for (int k = lane * 8; k < Kp; k += LPR * 8) *reinterpret_cast<uint2*>(codes + k) = codes8(load8<T, AL>(x, k, K), sc.r);
+      for (int k = lane * 8; k < Kp; k += LPR * 8) *reinterpret_cast<uint2*>(codes + k) = codes8(load8<T>(x, k, K), sc.r);
     }
   }
 }
 
-template <typename T, bool AL>
+__device__ __forceinline__ i64 row_of(i64 i, unsigned pieces) { return i >> 32 ? i / pieces : (i64)((unsigned)i / pieces); }
+
+template <typename T>
 __global__ __launch_bounds__(NT) void qunpack_kernel(RowArgs p, unsigned pieces) {
   const int K = p.K, Kp = qrow(K);
   const i64 total = p.rows * pieces;
   for (i64 i = (i64)blockIdx.x * NT + threadIdx.x; i < total; i += (i64)gridDim.x * NT) {
-    const i64 row = i / pieces;
+    const i64 row = row_of(i, pieces);
     const int k = (int)(i - row * pieces) * 8;
     const uint2 c = *reinterpret_cast<const uint2*>(p.codes + row * Kp + k);
-    store8<T, AL>(static_cast<T*>(p.out) + row * p.ld, k, K, decode8(c, p.scales[row]));
+    store8<T>(static_cast<T*>(p.out) + row * p.ld, k, K, decode8(c, p.scales[row]));
   }
 }
 
@@ -104,7 +106,7 @@ struct GateArgs {
   const void* dy; void* dh;                                                  // backward
 };
 
-template <typename T, int KIND, int LPR, int VPL, bool AL>
+template <typename T, int KIND, int LPR, int VPL>
 __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) {
   __shared__ unsigned lds_h[2][16], lds_y[1][16];
   constexpr int RPB = threads_of(LPR) / LPR, NV = VPL ? VPL : 1;
@@ -135,8 +137,8 @@ __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) 
       const int Kin = in ? K : 0;
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        g[v] = load8<T, AL>(h, (v * LPR + lane) * 8, Kin);
-        u[v] = load8<T, AL>(h + K, (v * LPR + lane) * 8, Kin);
+        g[v] = load8<T>(h, (v * LPR + lane) * 8, Kin);
+        u[v] = load8<T>(h + K, (v * LPR + lane) * 8, Kin);
       }
 #pragma unroll
       for (int v = 0; v < VPL; ++v) {
@@ -145,8 +147,8 @@ __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) 
       }
     } else {
       for (int k = lane * 8; k < K; k += LPR * 8) {
-        g[0] = load8<T, AL>(h, k, K);
-        u[0] = load8<T, AL>(h + K, k, K);
+        g[0] = load8<T>(h, k, K);
+        u[0] = load8<T>(h + K, k, K);
         look(g[0], u[0], make(g[0], u[0]));
       }
     }
@@ -165,31 +167,31 @@ __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) 
         *reinterpret_cast<uint2*>(p.hc + (2 * row + 1) * Kp + k) = codes8(b2, su.r);
       }
       if (p.yc) *reinterpret_cast<uint2*>(p.yc + row * Kp + k) = codes8(c, sy.r);
-      if (p.y) store8<T, AL>(static_cast<T*>(p.y) + row * p.ldy, k, K, c);
+      if (p.y) store8<T>(static_cast<T*>(p.y) + row * p.ldy, k, K, c);
     };
     if constexpr (VPL > 0) {
 #pragma unroll
       for (int v = 0; v < VPL; ++v) out((v * LPR + lane) * 8, g[v], u[v], y[v]);
     } else {
       for (int k = lane * 8; k < Kp; k += LPR * 8) {
-        g[0] = load8<T, AL>(h, k, K);
-        u[0] = load8<T, AL>(h + K, k, K);
+        g[0] = load8<T>(h, k, K);
+        u[0] = load8<T>(h + K, k, K);
         out(k, g[0], u[0], make(g[0], u[0]));
       }
     }
   }
 }
 
-template <typename T, int KIND, bool AL>
+template <typename T, int KIND>
 __global__ __launch_bounds__(NT) void qgate_bwd_kernel(GateArgs p, unsigned pieces) {
   const int K = p.K, Kp = qrow(K);
   const i64 total = p.rows * pieces;
   for (i64 i = (i64)blockIdx.x * NT + threadIdx.x; i < total; i += (i64)gridDim.x * NT) {
-    const i64 row = i / pieces;
+    const i64 row = row_of(i, pieces);
     const int k = (int)(i - row * pieces) * 8;
     const F8 g = decode8(*reinterpret_cast<const uint2*>(p.hc + 2 * row * Kp + k), p.hs[2 * row]);
     const F8 u = decode8(*reinterpret_cast<const uint2*>(p.hc + (2 * row + 1) * Kp + k), p.hs[2 * row + 1]);
-    const F8 dy = load8<T, AL>(static_cast<const T*>(p.dy) + row * p.ldy, k, K);
+    const F8 dy = load8<T>(static_cast<const T*>(p.dy) + row * p.ldy, k, K);
     F8 dg, du;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -199,12 +201,10 @@ __global__ __launch_bounds__(NT) void qgate_bwd_kernel(GateArgs p, unsigned piec
       du.v[e] = dy.v[e] * f;
     }
     T* dh = static_cast<T*>(p.dh) + row * p.ldh;
-    store8<T, AL>(dh, k, K, dg);
-    store8<T, AL>(dh + K, k, K, du);
+    store8<T>(dh, k, K, dg);
+    store8<T>(dh + K, k, K, du);
   }
 }
-
-bool aligned16(const void* p, i64 bytes_apart) { return ((uintptr_t)p | (uintptr_t)bytes_apart) % 16 == 0; }
 
 int blocks_of(i64 work) { return (int)(work < 1 << 20 ? work : 1 << 20); }   // (launches stay below 2^32 threads)
 
@@ -225,12 +225,11 @@ template <class F> static hipError_t by_row_length(i64 rows, int K, F&& f) {
   return f(integral_constant<int, 256>{}, integral_constant<int, 0>{});
 }
 
-template <typename T> static hipError_t pack_t(const RowArgs& a, bool al, hipStream_t st) {
+template <typename T> static hipError_t pack_t(const RowArgs& a, hipStream_t st) {
   return by_row_length(a.rows, a.K, [&](auto lpr, auto vpl) {
     constexpr int nt = threads_of(lpr.value);
     const int grid = blocks_of((a.rows + nt / lpr.value - 1) / (nt / lpr.value));
-    if (al) qpack_kernel<T, lpr.value, vpl.value, true><<<grid, nt, 0, st>>>(a);
-    else qpack_kernel<T, lpr.value, vpl.value, false><<<grid, nt, 0, st>>>(a);
+    qpack_kernel<T, lpr.value, vpl.value><<<grid, nt, 0, st>>>(a);
     return hipGetLastError();
   });
 }
@@ -238,8 +237,8 @@ template <typename T> static hipError_t pack_t(const RowArgs& a, bool al, hipStr
 hipError_t launch_qpack(int dtype, i64 rows, int K, i64 ld, const void* x, void* codes, float* scales, hipStream_t st) {
   if (!rows) return hipSuccess;
   const RowArgs a = {rows, ld, K, x, nullptr, (uint8_t*)codes, scales};
-  if (dtype == CONVBN_BF16) return pack_t<bf16_t>(a, aligned16(x, ld * 2), st);
-  return pack_t<float>(a, aligned16(x, ld * 4), st);
+  if (dtype == CONVBN_BF16) return pack_t<bf16_t>(a, st);
+  return pack_t<float>(a, st);
 }
 
 hipError_t launch_qunpack(int dtype, i64 rows, int K, i64 ld, const void* codes, const float* scales, void* x, hipStream_t st) {
@@ -247,33 +246,27 @@ hipError_t launch_qunpack(int dtype, i64 rows, int K, i64 ld, const void* codes,
   const RowArgs a = {rows, ld, K, nullptr, x, (uint8_t*)codes, (float*)scales};
   const unsigned pieces = ceil_div(K, 8);
   const int grid = blocks_of((rows * pieces + NT - 1) / NT);
-  const bool al = aligned16(x, ld * (dtype == CONVBN_BF16 ? 2 : 4));
-  if (dtype == CONVBN_BF16 && al) qunpack_kernel<bf16_t, true><<<grid, NT, 0, st>>>(a, pieces);
-  else if (dtype == CONVBN_BF16) qunpack_kernel<bf16_t, false><<<grid, NT, 0, st>>>(a, pieces);
-  else if (al) qunpack_kernel<float, true><<<grid, NT, 0, st>>>(a, pieces);
-  else qunpack_kernel<float, false><<<grid, NT, 0, st>>>(a, pieces);
+  if (dtype == CONVBN_BF16) qunpack_kernel<bf16_t><<<grid, NT, 0, st>>>(a, pieces);
+  else qunpack_kernel<float><<<grid, NT, 0, st>>>(a, pieces);
   return hipGetLastError();
 }
 
-template <typename T, int KIND, bool AL> static hipError_t gate_fwd_t(const GateArgs& a, hipStream_t st) {
+template <typename T, int KIND> static hipError_t gate_fwd_t(const GateArgs& a, hipStream_t st) {
   return by_row_length(a.rows, a.K, [&](auto lpr, auto vpl) {
     constexpr int nt = threads_of(lpr.value);
     const int grid = blocks_of((a.rows + nt / lpr.value - 1) / (nt / lpr.value));
-    qgate_fwd_kernel<T, KIND, lpr.value, vpl.value, AL><<<grid, nt, 0, st>>>(a);
+    qgate_fwd_kernel<T, KIND, lpr.value, vpl.value><<<grid, nt, 0, st>>>(a);
     return hipGetLastError();
   });
 }
-template <typename T, int KIND, bool AL> static hipError_t gate_bwd_t(const GateArgs& a, hipStream_t st) {
+template <typename T, int KIND> static hipError_t gate_bwd_t(const GateArgs& a, hipStream_t st) {
   const unsigned pieces = ceil_div(a.K, 8);
-  qgate_bwd_kernel<T, KIND, AL><<<blocks_of((a.rows * pieces + NT - 1) / NT), NT, 0, st>>>(a, pieces);
+  qgate_bwd_kernel<T, KIND><<<blocks_of((a.rows * pieces + NT - 1) / NT), NT, 0, st>>>(a, pieces);
   return hipGetLastError();
 }
-// Calls f(T, KIND, AL) with the gate's types; al: every row it touches starts on 16 bytes
-template <class F> static hipError_t by_gate(int dtype, int kind, bool al, F&& f) {
-  auto with = [&](auto t) {
-    if (kind == CONVBN_GATE_SILU) return al ? f(t, std::integral_constant<int, 0>{}, std::true_type{}) : f(t, std::integral_constant<int, 0>{}, std::false_type{});
-    return al ? f(t, std::integral_constant<int, 1>{}, std::true_type{}) : f(t, std::integral_constant<int, 1>{}, std::false_type{});
-  };
+// Calls f(T, KIND) with the gate's types
+template <class F> static hipError_t by_gate(int dtype, int kind, F&& f) {
+  auto with = [&](auto t) { return kind == CONVBN_GATE_SILU ? f(t, std::integral_constant<int, 0>{}) : f(t, std::integral_constant<int, 1>{}); };
   return dtype == CONVBN_BF16 ? with(bf16_t{}) : with(float{});
 }
 
@@ -281,17 +274,13 @@ hipError_t launch_qgate_fwd(int dtype, int kind, i64 rows, int K, i64 ldh, i64 l
                             void* y, void* y_codes, float* y_scales, hipStream_t st) {
   if (!rows) return hipSuccess;
   GateArgs a = {rows, ldh, ldy, K, h, y, (uint8_t*)h_codes, h_scales, (uint8_t*)y_codes, y_scales, nullptr, nullptr};
-  const i64 e = dtype == CONVBN_BF16 ? 2 : 4;
-  const bool al = aligned16(h, ldh * e) && K * e % 16 == 0 && (!y || aligned16(y, ldy * e));
-  return by_gate(dtype, kind, al, [&](auto t, auto k, auto v) { return gate_fwd_t<decltype(t), k.value, v.value>(a, st); });
+  return by_gate(dtype, kind, [&](auto t, auto k) { return gate_fwd_t<decltype(t), k.value>(a, st); });
 }
 hipError_t launch_qgate_bwd(int dtype, int kind, i64 rows, int K, i64 ldh, i64 ldy, const void* h_codes, const float* h_scales,
                             const void* dy, void* dh, hipStream_t st) {
   if (!rows) return hipSuccess;
   GateArgs a = {rows, ldh, ldy, K, nullptr, nullptr, (uint8_t*)h_codes, (float*)h_scales, nullptr, nullptr, dy, dh};
-  const i64 e = dtype == CONVBN_BF16 ? 2 : 4;
-  const bool al = aligned16(dh, ldh * e) && K * e % 16 == 0 && aligned16(dy, ldy * e);
-  return by_gate(dtype, kind, al, [&](auto t, auto k, auto v) { return gate_bwd_t<decltype(t), k.value, v.value>(a, st); });
+  return by_gate(dtype, kind, [&](auto t, auto k) { return gate_bwd_t<decltype(t), k.value>(a, st); });
 }
 
 }  // namespace convbn
