@@ -397,54 +397,48 @@ template <bool PARTS, class X, class W> __global__ __launch_bounds__(X::NT * X::
   else grad_body<true, PARTS, W>(w, (int)blockIdx.x - first, shared);
 }
 
-// C = the sum of the splits + add; likewise the column sums.  Four threads share eight channels (or one, where J is no multiple of 8), each
-// adds every fourth split, and the four sums meet in LDS: the order is the same in every run.
+// C = the sum of the splits + add; likewise the column sums.  Four threads share eight channels (or one column sum), each adds every fourth
+// split, and the four sums meet in LDS: the order is the same in every run.
 constexpr int JOIN = 4;
 struct JoinParams {
   i64 I, ldc;
-  int J, splits, blocks;
-  const float* part; void* C; const void* add; const float* db_part; float* db;
+  int J, splits, db_splits, blocks;   // I x J of C (either 0: none); rows of the parts lie a multiple of 8 apart
+  const float* part; void* C; const void* add;
+  i64 N; const float* db_part; float* db;
 };
 template <typename OUT> __device__ __forceinline__ void join_body(const JoinParams& p, const int wg) {
   __shared__ float meet[JOIN][8][64];
   OUT* C = static_cast<OUT*>(p.C);
   const OUT* add = static_cast<const OUT*>(p.add);
-  const int at = threadIdx.x & 63, q = threadIdx.x >> 6, J = p.J;
-  const int width = J % 8 ? 1 : 8;
-  const i64 mine = p.I * (J / width), total = mine + (p.db ? p.I : 0);   // the column sums come last, one a thread
+  const int at = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const int pieces = (p.J + 7) >> 3;
+  const i64 mine = p.I * pieces, total = mine + p.N;   // the column sums come last, one a thread
   for (i64 x0 = (i64)wg * 64; x0 < total; x0 += (i64)p.blocks * 64) {
     const i64 x = x0 + at;
     float v[8] = {};
-    if (x < mine && width == 8) {
+    if (x < mine) {
 #pragma unroll 4
       for (int s = q; s < p.splits; s += JOIN) {
-        const float4* f = reinterpret_cast<const float4*>(p.part + s * p.I * J + x * 8);
+        const float4* f = reinterpret_cast<const float4*>(p.part + (s * mine + x) * 8);
         const float4 a = f[0], b = f[1];
         v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
       }
     } else if (x < total) {
-      const float* f = x < mine ? p.part + x : p.db_part + (x - mine);
-      const i64 apart = x < mine ? p.I * J : p.I;
-#pragma unroll 4
-      for (int s = q; s < p.splits; s += JOIN) v[0] += f[s * apart];
+#pragma unroll 8
+      for (int s = q; s < p.db_splits; s += JOIN) v[0] += p.db_part[s * p.N + (x - mine)];
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) meet[q][e][at] = v[e];
     __syncthreads();
     if (q == 0 && x < total) {
+      F8 f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (meet[0][e][at] + meet[1][e][at]) + (meet[2][e][at] + meet[3][e][at]);
+      for (int e = 0; e < 8; ++e) f.v[e] = (meet[0][e][at] + meet[1][e][at]) + (meet[2][e][at] + meet[3][e][at]);
       if (x >= mine) {
-        p.db[x - mine] = v[0];
-      } else if (width == 8) {
-        const i64 row = x / (J / 8), o = row * p.ldc;
-        F8 f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f.v[e] = v[e];
-        store8_plus<OUT>(C + o, add ? add + o : nullptr, (int)(x - row * (J / 8)) * 8, J, f);
+        p.db[x - mine] = f.v[0];
       } else {
-        const i64 o = x / J * p.ldc + x % J;
-        C[o] = from_f32<OUT>(v[0] + (add ? to_f32(add[o]) : 0.f));
+        const i64 row = x / pieces, o = row * p.ldc;
+        store8_plus<OUT>(C + o, add ? add + o : nullptr, (int)(x - row * pieces) * 8, p.J, f);
       }
     }
     __syncthreads();
@@ -456,16 +450,6 @@ template <typename OUT> __global__ __launch_bounds__(256) void qjoin_kernel(Join
   else join_body<OUT>(w, (int)blockIdx.x - x.blocks);
 }
 
-// dz as the products want it: rows of a multiple of 8 channels, zeros past the last.  F32: A = dz s in three parts, s by row or by column.
-__global__ __launch_bounds__(256) void qcopy_kernel(i64 M, int N, int N8, const bf16_t* __restrict__ dz, i64 ldz, bf16_t* __restrict__ out) {
-  const unsigned pieces = N8 >> 3;
-  const i64 total = M * pieces;
-  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < total; i += (i64)gridDim.x * 256) {
-    const i64 m = i >> 32 ? i / pieces : (i64)((unsigned)i / pieces);
-    const int n = (int)(i - m * pieces) * 8;
-    store8<bf16_t>(out + m * N8, n, N8, load8<bf16_t>(dz + m * ldz, n, N));
-  }
-}
 // v in three parts of 8 bits each, which add up to it; infinities and NaN are the first whole
 __device__ __forceinline__ void split3(const F8& f, F8 (&part)[3]) {
 #pragma unroll
@@ -480,62 +464,65 @@ __device__ __forceinline__ void split3(const F8& f, F8 (&part)[3]) {
     }
   }
 }
-// by_col: dz sw, by_row: dz sx; null = not wanted
-__global__ __launch_bounds__(256) void qsplit_kernel(i64 M, int N, int N8, const float* __restrict__ dz, i64 ldz, const float* __restrict__ sw,
-                                                     const float* __restrict__ sx, bf16_t* __restrict__ by_col, bf16_t* __restrict__ by_row) {
-  const unsigned pieces = N8 >> 3;
-  const i64 total = M * pieces, plane = M * N8;
-  for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < total; i += (i64)gridDim.x * 256) {
-    const i64 m = i >> 32 ? i / pieces : (i64)((unsigned)i / pieces);
-    const int n = (int)(i - m * pieces) * 8;
-    const F8 v = load8<float>(dz + m * ldz, n, N);
-    F8 scaled, part[3];
-    if (by_col) {
-      const F8 s = load8<float>(sw, n, N);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) scaled.v[e] = n + e < N ? v.v[e] * s.v[e] : 0.f;
-      split3(scaled, part);
-#pragma unroll
-      for (int x = 0; x < 3; ++x) store8<bf16_t>(by_col + x * plane + m * N8, n, N8, part[x]);
-    }
-    if (by_row) {
-      const float s = sx[m];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) scaled.v[e] = n + e < N ? v.v[e] * s : 0.f;
-      split3(scaled, part);
-#pragma unroll
-      for (int x = 0; x < 3; ++x) store8<bf16_t>(by_row + x * plane + m * N8, n, N8, part[x]);
-    }
-  }
-}
 
-// Column sums on their own: a workgroup takes 64 columns and a slice of the rows; several slices are added in order by a second launch.
-constexpr int SUM_WAVES = 16;
-template <typename T>
-__global__ __launch_bounds__(64 * SUM_WAVES) void qcolsum_kernel(i64 M, int N, i64 per, const T* __restrict__ dz, i64 ldz, float* __restrict__ part) {
-  __shared__ float sum[SUM_WAVES][64];
-  const int n = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
-  const i64 beg = (i64)blockIdx.y * per, end = beg + per < M ? beg + per : M;
-  float s = 0.f;
-  if (n < N) {
-#pragma unroll 8
-    for (i64 m = beg + w; m < end; m += SUM_WAVES) s += to_f32(dz[m * ldz + n]);
+// One pass over dz for what the products do not take from it as it lies: its column sums, and dz as they want it, rows of a multiple of 8
+// channels with zeros past the last (f32: dz s in three parts, s by column for dx, by row for dW).  A workgroup takes 256 columns, a thread
+// eight of them and every 16th row of a slice; the sums of several slices are joined in order by a later launch.  A copy with its sums of
+// 22144 x 3841 bf16 (340 MB in and out) takes 77 us, 4.4 TB/s, bound by memory; copy and sums in two launches took 108.
+constexpr int PREP_ROWS = 16;
+struct PrepParams {
+  i64 M, ldz, per;
+  int N;
+  const void* dz; float* sums;          // [slices][N] or null
+  bf16_t* copy; bf16_t* by_row;         // copy: of bf16 dz, or of f32 dz sw; by_row: of f32 dz sx; either null
+  const float* sw; const float* sx;
+};
+template <typename T> __global__ __launch_bounds__(32 * PREP_ROWS) void qprep_kernel(PrepParams p) {
+  __shared__ float meet[PREP_ROWS][256 + 8];
+  const int c = (threadIdx.x & 31) * 8, r = threadIdx.x >> 5, n = blockIdx.x * 256 + c, N8 = (p.N + 7) & ~7;
+  const i64 beg = (i64)blockIdx.y * p.per, end = beg + p.per < p.M ? beg + p.per : p.M, plane = p.M * N8;
+  const T* dz = static_cast<const T*>(p.dz);
+  F8 sum = {}, sw = {};
+  if (n < p.N) {
+    if (sizeof(T) == 4 && p.copy) sw = load8<float>(p.sw, n, p.N);
+#pragma unroll 4
+    for (i64 m = beg + r; m < end; m += PREP_ROWS) {
+      const F8 v = load8<T>(dz + m * p.ldz, n, p.N);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum.v[e] += v.v[e];
+      if constexpr (sizeof(T) == 2) {
+        if (p.copy) store8<bf16_t>(p.copy + m * N8, n, N8, v);
+      } else {
+        F8 scaled, part[3];
+        if (p.copy) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) scaled.v[e] = n + e < p.N ? v.v[e] * sw.v[e] : 0.f;
+          split3(scaled, part);
+#pragma unroll
+          for (int x = 0; x < 3; ++x) store8<bf16_t>(p.copy + x * plane + m * N8, n, N8, part[x]);
+        }
+        if (p.by_row) {
+          const float s = p.sx[m];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) scaled.v[e] = n + e < p.N ? v.v[e] * s : 0.f;
+          split3(scaled, part);
+#pragma unroll
+          for (int x = 0; x < 3; ++x) store8<bf16_t>(p.by_row + x * plane + m * N8, n, N8, part[x]);
+        }
+      }
+    }
   }
-  sum[w][threadIdx.x & 63] = s;
+  if (!p.sums) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) meet[r][c + e] = sum.v[e];
   __syncthreads();
-  if (w == 0 && n < N) {
+  const int at = threadIdx.x, col = blockIdx.x * 256 + at;
+  if (at < 256 && col < p.N) {
     float v = 0.f;
-    for (int i = 0; i < SUM_WAVES; ++i) v += sum[i][threadIdx.x];
-    part[(i64)blockIdx.y * N + n] = v;
+#pragma unroll
+    for (int i = 0; i < PREP_ROWS; ++i) v += meet[i][at];
+    p.sums[(i64)blockIdx.y * p.N + col] = v;
   }
-}
-__global__ __launch_bounds__(256) void qcolsum_join_kernel(int N, int slices, const float* __restrict__ part, float* __restrict__ db) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
-  float s = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < slices; ++i) s += part[(i64)i * N + n];
-  db[n] = s;
 }
 
 int grid_of(i64 work) { const i64 b = (work + 255) / 256; return (int)(b < 1 ? 1 : b < 65536 ? b : 65536); }
@@ -571,10 +558,11 @@ Plan plan_of(i64 I, int J, i64 R, int planes) {
   return pl;
 }
 
-int colsum_slices(i64 M, int N) {
-  i64 s = 512 / ceil_div(N, 64);
-  if (s > M / 512) s = M / 512;
-  return (int)(s < 1 ? 1 : s);
+// Slices of dz's rows for its pass: some 2048 workgroups, of 32 rows or more (of 256 slices at most: their sums have to be joined)
+int prep_slices(i64 M, int N) {
+  i64 s = ceil_div(2048, ceil_div(N, 256));
+  if (s > M / 32) s = M / 32;
+  return (int)(s < 1 ? 1 : s < 256 ? s : 256);
 }
 
 // Whether the products read dz where it is (its first row on 16 bytes then: qgrad_reads_in_place); else a copy, or the three parts
@@ -588,10 +576,11 @@ Scratch scratch_of(const QGrad& p) {   // (for all outputs)
   if (p.dtype != CONVBN_BF16) s.copy = (size_t)6 * p.M * N8 * 2;   // three parts, for either product
   else s.copy = direct(p) ? 0 : (size_t)p.M * N8 * 2;
   const Plan dx = plan_of(p.M, p.K, p.N, planes), dw = plan_of(p.N, p.K, p.M, planes);
-  const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * p.K * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * (p.K + 1) * 4 : 0;
+  const size_t K8 = (p.K + 7) & ~7;
+  const size_t px = dx.splits > 1 ? (size_t)dx.splits * p.M * K8 * 4 : 0, pw = dw.splits > 1 ? (size_t)dw.splits * p.N * (K8 + 1) * 4 : 0;
   s.copy = align_up(s.copy, 256);
   s.part = align_up(px + pw, 256);
-  s.cols = align_up((size_t)colsum_slices(p.M, p.N) * p.N * 4, 256);
+  s.cols = align_up((size_t)prep_slices(p.M, p.N) * p.N * 4, 256);
   s.total = s.copy + s.part + s.cols;
   return s;
 }
@@ -617,7 +606,7 @@ template <bool PARTS, class X, class W> hipError_t launch_pair(const GradParams&
 }
 
 // A product as it is launched, and what joins it
-struct Product { bool on = false; int tile = 0; GradParams g; JoinParams join; };
+struct Product { bool on = false; int tile = 0; GradParams g = {}; JoinParams join = {}; };
 bool alone(const Product& r) { return r.tile <= 128 && r.g.nti * r.g.ntj * r.g.splits <= CUS; }
 
 template <bool TRANS, bool PARTS> hipError_t launch_product(const Product& r, hipStream_t st) {
@@ -648,11 +637,14 @@ template <bool TRANS> Product product(const QGrad& p, const bf16_t* A, i64 lda, 
   void* C = TRANS ? p.dW : p.dx;
   const i64 ldc = TRANS ? p.K : p.ldx;
   const void* add = TRANS ? nullptr : p.add;
-  r.join = {};
   if (pl.splits > 1) {
-    float* db_part = part + (i64)pl.splits * g.I * g.J;
-    g.C = part; g.ldc = g.J; g.db = sums ? db_part : nullptr;
-    r.join = {g.I, ldc, g.J, pl.splits, grid_of(4 * (g.I * (g.J % 8 ? g.J : g.J / 8) + (sums ? g.I : 0))), part, C, add, db_part, sums ? p.db : nullptr};
+    g.C = part; g.ldc = (g.J + 7) & ~7;
+    r.join = {g.I, ldc, g.J, pl.splits, 0, 0, part, C, add, 0, nullptr, nullptr};
+    if (sums) {
+      float* db_part = part + pl.splits * g.I * g.ldc;
+      g.db = db_part;
+      r.join.db_splits = pl.splits; r.join.N = p.N; r.join.db_part = db_part; r.join.db = p.db;
+    }
   } else {
     g.C = C; g.ldc = ldc; g.add = add; g.c_bf16 = !f32; g.db = sums ? p.db : nullptr;
   }
@@ -661,28 +653,29 @@ template <bool TRANS> Product product(const QGrad& p, const bf16_t* A, i64 lda, 
 
 template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st) {
   constexpr bool PARTS = sizeof(T) == 4;
-  const T* dz = static_cast<const T*>(p.dz);
   const Scratch sc = scratch_of(p);
   bf16_t* copy = static_cast<bf16_t*>(ws);
   float* part = reinterpret_cast<float*>(static_cast<char*>(ws) + sc.copy);
   float* cols = reinterpret_cast<float*>(static_cast<char*>(ws) + sc.copy + sc.part);
   const int N8 = (p.N + 7) & ~7;
+  const bool in_place = direct(p), copies = p.M && (p.dx || p.dW) && !in_place;
   const bf16_t* A = copy;
   i64 lda = N8;
-  if constexpr (sizeof(T) == 2) {
-    if (direct(p)) { A = dz; lda = p.ldz; }
-    else if (p.M && (p.dx || p.dW)) qcopy_kernel<<<grid_of(p.M * (N8 / 8)), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, copy);
-  }
+  if constexpr (!PARTS)
+    if (in_place) { A = static_cast<const bf16_t*>(p.dz); lda = p.ldz; }
   bf16_t* by_row = copy + 3 * p.M * N8;
-  if constexpr (sizeof(T) == 4)
-    if (p.M && (p.dx || p.dW))
-      qsplit_kernel<<<grid_of(p.M * (N8 / 8)), 256, 0, st>>>(p.M, p.N, N8, dz, p.ldz, p.sw, p.sx, p.dx ? copy : nullptr, p.dW ? by_row : nullptr);
-  // The column sums ride in the weight gradient, except with the largest tiles: the workgroups that add them up would keep the others
-  // waiting (8192 x 4096 x 4096: 26 us more, a launch of their own 14; 1568 x 2048 x 512: 1 us more, a launch 6)
-  const bool aside = p.db && p.dW && p.M && sizeof(T) == 2 && plan_of(p.N, p.K, p.M, 1).tile < 256;
+  // The column sums of dz that is read in place ride in the weight gradient, except with the largest tiles: the workgroups that add them up
+  // would keep the others waiting (8192 x 4096 x 4096: 26 us more, a launch of their own 14; 1568 x 2048 x 512: 1 us more, a launch 6)
+  const bool ride = p.db && p.dW && p.M && in_place && plan_of(p.N, p.K, p.M, 1).tile < 256;
+  const int slices = prep_slices(p.M, p.N);
+  if (copies || (p.db && !ride)) {
+    const PrepParams q = {p.M, p.ldz, (p.M + slices - 1) / slices, p.N, p.dz, !p.db ? nullptr : slices > 1 ? cols : p.db,
+                          copies && (!PARTS || p.dx) ? copy : nullptr, copies && PARTS && p.dW ? by_row : nullptr, p.sw, p.sx};
+    qprep_kernel<T><<<dim3(ceil_div(p.N, 256), slices), 32 * PREP_ROWS, 0, st>>>(q);
+  }
   Product x, w;
   if (p.dx && p.M) x = product<false>(p, A, lda, part, false);
-  if (p.dW) w = product<true>(p, sizeof(T) == 4 ? by_row : A, lda, part + (x.on && x.g.splits > 1 ? (i64)x.g.splits * x.g.I * x.g.J : 0), aside);
+  if (p.dW) w = product<true>(p, sizeof(T) == 4 ? by_row : A, lda, part + (x.on && x.g.splits > 1 ? x.g.splits * x.g.I * x.g.ldc : 0), ride);
   hipError_t e = hipSuccess;
   if (x.on && w.on && alone(x) && alone(w)) {
     if (x.tile == 64) e = w.tile == 64 ? launch_pair<PARTS, Small, Small>(x.g, w.g, st) : launch_pair<PARTS, Small, MidAlone>(x.g, w.g, st);
@@ -692,15 +685,11 @@ template <typename T> hipError_t grad_t(const QGrad& p, void* ws, hipStream_t st
     if (e == hipSuccess && w.on) e = launch_product<true, PARTS>(w, st);
   }
   if (e != hipSuccess) return e;
-  if (!x.on) x.join = {};
-  if (!w.on) w.join = {};
+  if (p.db && !ride && slices > 1) { w.join.db_splits = slices; w.join.N = p.N; w.join.db_part = cols; w.join.db = p.db; }
+  auto blocks = [](JoinParams& j) { j.blocks = j.I || j.N ? grid_of(JOIN * (j.I * ((j.J + 7) / 8) + j.N)) : 0; };
+  blocks(x.join);
+  blocks(w.join);
   if (x.join.blocks + w.join.blocks) qjoin_kernel<T><<<x.join.blocks + w.join.blocks, 256, 0, st>>>(x.join, w.join);
-  if (p.db && !aside) {
-    const int slices = colsum_slices(p.M, p.N);
-    const i64 per = (p.M + slices - 1) / slices;
-    qcolsum_kernel<T><<<dim3(ceil_div(p.N, 64), slices), 64 * SUM_WAVES, 0, st>>>(p.M, p.N, per, dz, p.ldz, slices > 1 ? cols : p.db);
-    if (slices > 1) qcolsum_join_kernel<<<ceil_div(p.N, 256), 256, 0, st>>>(p.N, slices, cols, p.db);
-  }
   return hipGetLastError();
 }
 
