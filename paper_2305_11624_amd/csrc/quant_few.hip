@@ -6,6 +6,9 @@
 // places of the reduction, its 16 columns T rows of x at the same places, and the T x T blocks on the diagonal are added up at the end.
 // That way few rows still give many workgroups, and a load takes 64 * 16 / T bytes of each weight row in a run.
 //
+// One row, 2048 -> 8192: 16.8 MB in 6.0 us, packing and launch included, 2.8 TB/s: the weights' way from memory (about 3.3 us at a copy's rate)
+// behind the row's own and its maximum.
+//
 // x that is not packed yet is packed here, by every workgroup for itself while its first weights are on the way (a launch of its own would
 // take longer than the whole product), as long as it is short.
 #include "quant_code.h"
