@@ -44,16 +44,27 @@ template <typename T> __device__ __forceinline__ F8 load8(const T* __restrict__ 
   for (int i = 0; i < 8; ++i) f.v[i] = k + i < K ? to_f32(row[k + i]) : 0.f;
   return f;
 }
-template <typename T> __device__ __forceinline__ void store8(T* __restrict__ row, int k, int K, const F8& f) {
+// STREAM: past the L2 caches
+template <typename T, bool STREAM = false> __device__ __forceinline__ void store8(T* __restrict__ row, int k, int K, const F8& f) {
   if (k + 8 <= K) {
-    *reinterpret_cast<Raw8<T>*>(row + k) = narrow<T>(f);
+    const Raw8<T> r = narrow<T>(f);
+    if constexpr (STREAM) {
+      typedef u32x4 __attribute__((aligned(2), may_alias)) Piece;
+      __builtin_nontemporal_store(r.a, reinterpret_cast<Piece*>(row + k));
+      if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(r.b, reinterpret_cast<Piece*>(row + k + 4));
+    } else {
+      *reinterpret_cast<Raw8<T>*>(row + k) = r;
+    }
     return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (k + i < K) row[k + i] = from_f32<T>(f.v[i]);
 }
-// ... a product's result: the addend, if any, comes on top (it may be the same memory)
+// ... a product's result: the addend, if any, comes on top (it may be the same memory).  Results leave the caches to the operands.  us, kept there
+// and streamed, up product, gate and down product forward and backward: 25088 x 512 -> 2 x 1024 484 and 458, 8192 x 4096 -> 2 x 8192 3913 and 3877, 1568 x
+// 2048 -> 2 x 8192 517 and 498; forward alone, where the next kernel reads them at once, 1568 x 512 -> 2 x 2048 32.3 and 30.8, 1568 x 2048 -> 2 x
+// 8192 133 and 135.
 template <typename T> __device__ __forceinline__ void store8_plus(T* row, const T* add, int k, int K, F8 f) {
   if (add) {
     if (k + 8 <= K) {
@@ -66,7 +77,7 @@ template <typename T> __device__ __forceinline__ void store8_plus(T* row, const 
         if (k + i < K) f.v[i] += to_f32(add[k + i]);
     }
   }
-  store8<T>(row, k, K, f);
+  store8<T, true>(row, k, K, f);
 }
 
 __device__ __forceinline__ unsigned amax8(const F8& f) {   // (compared as whole numbers: a NaN is the largest of all)

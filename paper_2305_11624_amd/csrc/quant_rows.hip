@@ -4,8 +4,8 @@
 // registers from the one read of the row to the store of its codes: the maximum has to be known before the first code is.  Rows that
 // are too long for that (VPL = 0) are read twice, the second time from the caches.  Many rows are bound by memory (100352 x 256: 15 us,
 // 5.1 TB/s); few rows by the way there and back, so they take as many lanes as there are pieces, up to 1024
-// (49 x 2048: 2.7 us for a launch).  The gate reads and writes 7 bytes (forward) and 8 (backward) for each element of y in bf16, memory bounds
-// it: 8192 x 8192, 4.2 TB/s in 113 us and 6.1 TB/s in 88 us (the last-level cache holds a part of what it reads).
+// (49 x 2048: 2.7 us for a launch).  The gate reads and writes 8 bytes for each bf16 element of y, forward and backward, and memory bounds
+// it: 8192 x 8192, 537 MB, forward 113 us, 4.8 TB/s, backward 88 us, 6.1 TB/s (a part of what it reads is still in the last-level cache).
 #include "quant_code.h"
 
 namespace convbn {
