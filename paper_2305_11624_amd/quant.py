@@ -107,8 +107,9 @@ class Linear:
     def _desc_with(self, bit: int, field: str, add, width: int, ld: int):
         if add is None:
             return self.desc
-        if add.dtype is not self.dtype or add.shape != (self.M, width) or self.M > 1 and add.stride() != (ld, 1):
-            raise ValueError(f"add: expected {self.dtype} [{self.M}, {width}] with rows {ld} elements apart")
+        if (add.dtype is not self.dtype or add.shape != (self.M, width) or self.M > 1 and add.stride(0) != ld
+                or self.M and width > 1 and add.stride(1) != 1 or add.device != self.z.device):
+            raise ValueError(f"add: expected {self.dtype} [{self.M}, {width}] with rows {ld} elements apart on {self.z.device}")
         d = self._add_desc
         d.act = bit
         setattr(d, field, add.data_ptr())

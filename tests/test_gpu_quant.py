@@ -500,3 +500,24 @@ def test_example_learns_and_serves():
     spec.loader.exec_module(mod)
     losses, worst, kept, whole = mod.main(images=2, steps=12)
     assert losses[-1] < 0.7 * losses[0] and worst == 0 and kept < 0.53 * whole
+
+
+@pytest.mark.parametrize("M", [1, 40])
+def test_addends_are_checked_before_anything_is_launched(M):
+    Q = _q()
+    K, N = 24, 16
+    lin = Q.Linear(M, K, N, torch.float32)
+    W, x = torch.full((N, K), 127.0, device="cuda"), torch.full((M, K), 127.0, device="cuda")      # (whole numbers: sums are exact)
+    dz = torch.ones(M, N, device="cuda")
+    lin.pack_weight(W)
+    lin.forward(x, add=torch.zeros(M, N, device="cuda"))
+    z = lin.z.clone()
+    for bad in (torch.zeros(M, N), torch.zeros(M, 2 * N, device="cuda")[:, ::2], torch.zeros(1, 1, device="cuda").expand(M, N)):
+        with pytest.raises(ValueError):
+            lin.forward(x, add=bad)
+    for bad in (torch.zeros(M, K), torch.zeros(M, 2 * K, device="cuda")[:, ::2], torch.zeros(1, 1, device="cuda").expand(M, K)):
+        with pytest.raises(ValueError):
+            lin.backward(dz, add=bad)
+    assert torch.equal(lin.z, z)
+    if M == 1:      # one row: any distance to the next
+        assert torch.equal(lin.forward(x, add=torch.ones(1, N + 3, device="cuda")[:, :N]), z + 1)

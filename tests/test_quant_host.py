@@ -192,3 +192,31 @@ def test_objects_check_their_arguments():
         lin.backward(torch.zeros(4, 8))
     with pytest.raises(AssertionError):
         lin.forward(x)                                   # right in everything, but on the host
+
+
+@pytest.mark.parametrize("M", [1, 4])
+def test_addends_are_checked_like_every_other_tensor(M):
+    """An addend goes to the kernel as an address: its type, size, strides and device are looked at first, for a single row too."""
+    from paper_2305_11624_amd import quant as Q
+    lin = Q.Linear(M, 24, 8, torch.float32, device="cpu", gap=3)
+    lin.set_weight(*Q.new_codes(8, 24, "cpu"))
+
+    def rows(width, gap=3, dtype=torch.float32, device="cpu"):
+        return torch.zeros(M, width + gap, dtype=dtype, device=device)[:, :width]
+
+    x, dz = rows(24), rows(8)
+    for call, width in ((lambda a: lin.forward(x, add=a), 8), (lambda a: lin.forward_packed(lin.codes, lin.scales, add=a), 8),
+                        (lambda a: lin.backward(dz, add=a), 24)):
+        bad = [torch.zeros(M, 2 * (width + 3))[:, :2 * width:2],      # every other element of a row
+               torch.zeros(1, 1).expand(M, width), rows(width + 1), rows(width).t(), rows(width, dtype=torch.bfloat16),
+               rows(width).view(1, M, width), rows(width, device="meta")]
+        if M > 1:
+            bad.append(rows(width, gap=0))      # (a single row is as far from the next as one likes)
+        for a in bad:
+            with pytest.raises(ValueError):
+                call(a)
+    with pytest.raises(AssertionError):
+        lin.forward(x, add=rows(8))            # right in everything, but on the host
+    if M == 1:
+        with pytest.raises(AssertionError):
+            lin.forward(x, add=rows(8, gap=0))
