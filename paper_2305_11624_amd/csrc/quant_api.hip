@@ -63,7 +63,7 @@ convbn_status check_linear(const convbn_qdesc* d, i64* ldx, i64* ldz) {
   if (d->M * d->N > most || d->M * d->K > most) return set_error(CONVBN_ERR_UNSUPPORTED, "a tensor of more than 2^38 elements");
   if (d->act & ~(CONVBN_ACT_ADD_OUT | CONVBN_ACT_ADD_IN))
     return set_error(CONVBN_ERR_UNSUPPORTED, "act %d: only the two addends", d->act);
-  if (((d->act & CONVBN_ACT_ADD_OUT) && !d->add_out) || ((d->act & CONVBN_ACT_ADD_IN) && !d->add_in))
+  if (d->M && (((d->act & CONVBN_ACT_ADD_OUT) && !d->add_out) || ((d->act & CONVBN_ACT_ADD_IN) && !d->add_in)))
     return set_error(CONVBN_ERR_NULL, "act %d asks for an addend that the descriptor does not give", d->act);
   return CONVBN_OK;
 }

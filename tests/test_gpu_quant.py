@@ -521,3 +521,13 @@ def test_addends_are_checked_before_anything_is_launched(M):
     assert torch.equal(lin.z, z)
     if M == 1:      # one row: any distance to the next
         assert torch.equal(lin.forward(x, add=torch.ones(1, N + 3, device="cuda")[:, :N]), z + 1)
+
+
+def test_a_gated_block_of_no_rows():
+    Q = _q()
+    blk = Q.GatedBlock(0, 16, 24)
+    blk.pack_weights(torch.ones(48, 16, device="cuda", dtype=torch.bfloat16), torch.ones(16, 24, device="cuda", dtype=torch.bfloat16))
+    x = torch.empty(0, 16, device="cuda", dtype=torch.bfloat16)
+    assert blk.forward(x).shape == (0, 16)
+    dx, dW_up, dW_down = blk.backward(x)
+    assert dx.shape == (0, 16) and (dW_up == 0).all() and (dW_down == 0).all()

@@ -220,3 +220,13 @@ def test_addends_are_checked_like_every_other_tensor(M):
     if M == 1:
         with pytest.raises(AssertionError):
             lin.forward(x, add=rows(8, gap=0))
+
+
+def test_no_rows_need_no_addend():
+    """M = 0 is no error, whatever the call adds: a tensor without rows has no memory either."""
+    d = _qdesc(M=0, act=4)
+    assert _fwd(d, x=None, codes=None, scales=None, z=None, work=None, nbytes=0) == B.OK
+    assert _fwd(_qdesc(act=4)) == B.ERR_NULL and _bwd(_qdesc(act=8)) == B.ERR_NULL
+    for act in (4, 8):      # (as far as the next check)
+        assert _bwd(_qdesc(M=0, act=act), dz=None, db=None, dW=None, dx=C.c_void_p(4097)) == B.ERR_UNSUPPORTED
+        assert "dx" in B.convbn_last_error()
