@@ -75,14 +75,18 @@ class Linear:
     """z = x w^T + b on M rows: x and w in 8 bits with a scale for each row of x and each output channel, integer sums.
 
     train: the codes of x are kept for `backward`, which works from them (x itself may be dropped after `forward`).
-    gap: x, dx, z and dz are rows of buffers with `gap` elements between the rows."""
+    gap: x, dx, z and dz are rows of buffers with `gap` elements between the rows.
+    packed: x always comes packed (`forward_packed`), so the layer has no codes of its own."""
 
-    def __init__(self, M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0, device="cuda"):
+    def __init__(self, M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0, device="cuda",
+                 packed: bool = False):
         self.M, self.K, self.N, self.dtype, self.train = M, K, N, dtype, train
         self.ldx, self.ldz = K + gap, N + gap
         self.desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)
         self._add_desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)   # (with an addend)
-        self.codes, self.scales = new_codes(M, K, device) if train else (None, None)
+        self.packed = packed
+        self.codes, self.scales = new_codes(M, K, device) if train and not packed else (None, None)   # what forward packs into
+        self._kept = None, None   # what backward reads: these, or those that forward_packed was given
         self.w_codes = self.w_scales = None
         self._w_desc = B.make_qdesc(N, K, dtype=_dtype(dtype))
         self.z = _new_rows(M, N, self.ldz, dtype, device)
@@ -122,18 +126,21 @@ class Linear:
     def forward(self, x: torch.Tensor, b: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None, stream=None):
         """z = x w^T + b (+ add)."""
         self._ready()
+        if self.packed:
+            raise RuntimeError("this layer takes packed rows (packed=True)")
         d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
         B.convbn_qlinear_fwd(d, x, self.codes, self.scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
+        self._kept = self.codes, self.scales
         return self.z
 
     def forward_packed(self, codes: torch.Tensor, scales: torch.Tensor, b: Optional[torch.Tensor] = None,
                        add: Optional[torch.Tensor] = None, stream=None):
-        """The same for rows that are packed already; with `train` they are what `backward` reads, so keep them until then."""
+        """The same for rows that are packed already; with `train` they are what `backward` reads, so leave them as they are until then."""
         self._ready()
         d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
         B.convbn_qlinear_fwd(d, None, codes, scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         if self.train:
-            self.codes, self.scales = codes, scales
+            self._kept = codes, scales
         return self.z
 
     def backward(self, dz: torch.Tensor, need_dx: bool = True, need_dW: bool = True, bias: bool = False,
@@ -144,12 +151,12 @@ class Linear:
         self._ready()
         d = self._desc_with(B.ACT_ADD_IN, "add_in", add, self.K, self.ldx)
         dx, dW, db = self.dx if need_dx else None, self.dW if need_dW else None, self.db if bias else None
-        B.convbn_qlinear_bwd(d, self.codes, self.scales, self.w_codes, self.w_scales, dz, dx, dW, db, self.ws, stream)
+        B.convbn_qlinear_bwd(d, *self._kept, self.w_codes, self.w_scales, dz, dx, dW, db, self.ws, stream)
         return dx, dW, db
 
     def saved_bytes(self) -> int:
         """What stays alive between forward and backward."""
-        return self.codes.numel() + 4 * self.M if self.train else 0
+        return self.M * (B.convbn_qrow_bytes(self.K) + 4) if self.train else 0
 
 
 class Gate:
@@ -189,7 +196,7 @@ class GatedBlock:
     def __init__(self, M: int, C: int, F: int, dtype=torch.bfloat16, kind: str = "silu", train: bool = True, device="cuda"):
         self.up = Linear(M, C, 2 * F, dtype, train, device=device)
         self.gate = Gate(M, F, dtype, kind, train, packed=True, device=device)
-        self.down = Linear(M, F, C, dtype, train, device=device)
+        self.down = Linear(M, F, C, dtype, train, device=device, packed=True)
 
     def pack_weights(self, W_up: torch.Tensor, W_down: torch.Tensor, stream=None):
         """W_up [2 F, C] (g's rows before u's), W_down [C, F]: once for serving, every step in training."""

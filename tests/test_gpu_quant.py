@@ -531,3 +531,40 @@ def test_a_gated_block_of_no_rows():
     assert blk.forward(x).shape == (0, 16)
     dx, dW_up, dW_down = blk.backward(x)
     assert dx.shape == (0, 16) and (dW_up == 0).all() and (dW_down == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [3, 50])
+def test_codes_that_were_handed_over_stay_the_callers(M, dtype):
+    """A training layer reads packed rows that it is given, and packs into rows of its own: two projections of one packed input, then another
+    input through one of them, leave the first's gradients and the given codes as they were."""
+    Q, dt = _q(), DT[dtype]
+    K, N = 72, 40
+    a, b = Q.Linear(M, K, N, dt), Q.Linear(M, K, N, dt)
+    x, y = torch.randn(M, K, generator=_gen(1)).to("cuda", dt), torch.randn(M, K, generator=_gen(2)).to("cuda", dt)
+    W, dz = torch.randn(N, K, generator=_gen(3)).to("cuda", dt), torch.randn(M, N, generator=_gen(4)).to("cuda", dt)
+    for lin in (a, b):
+        lin.pack_weight(W)
+    a.forward(x)
+    codes, scales = a.codes.clone(), a.scales.clone()
+    want = a.backward(dz)[1].clone()
+    b.forward_packed(a.codes, a.scales)
+    assert torch.equal(b.backward(dz)[1], want)              # from the codes that it was given
+    b.forward(y)
+    assert torch.equal(a.codes, codes) and torch.equal(a.scales, scales)
+    assert torch.equal(a.backward(dz)[1], want)
+    fresh = Q.Linear(M, K, N, dt)
+    fresh.pack_weight(W)
+    fresh.forward(y)
+    assert torch.equal(b.backward(dz)[1], fresh.backward(dz)[1])      # from its own
+
+
+def test_no_weight_gradient_before_a_forward_pass():
+    """There are no codes yet: the call refuses, and does not work from whatever the buffer holds.  dx needs none."""
+    Q = _q()
+    lin = Q.Linear(4, 24, 8, torch.float32)
+    lin.pack_weight(torch.full((8, 24), 127.0, device="cuda"))
+    dz = torch.ones(4, 8, device="cuda")
+    with pytest.raises(B.ConvBNError, match="codes"):
+        lin.backward(dz)
+    assert (lin.backward(dz, need_dW=False)[0] == 8 * 127).all()

@@ -230,3 +230,37 @@ def test_no_rows_need_no_addend():
     for act in (4, 8):      # (as far as the next check)
         assert _bwd(_qdesc(M=0, act=act), dz=None, db=None, dW=None, dx=C.c_void_p(4097)) == B.ERR_UNSUPPORTED
         assert "dx" in B.convbn_last_error()
+
+
+def test_what_a_layer_packs_into_is_its_own(monkeypatch):
+    """By the tensors that the calls get: outputs of packing are never tensors that the caller handed over."""
+    from paper_2305_11624_amd import quant as Q
+    seen = []
+    monkeypatch.setattr(B, "convbn_qlinear_fwd", lambda d, x, codes, scales, *rest: seen.append((x, codes, scales)))
+    monkeypatch.setattr(B, "convbn_qlinear_bwd", lambda d, codes, scales, *rest: seen.append((None, codes, scales)))
+    lin = Q.Linear(4, 24, 8, torch.float32, device="cpu")
+    given, w = Q.new_codes(4, 24, "cpu"), Q.new_codes(8, 24, "cpu")
+    lin.set_weight(*w)
+    x, dz = torch.zeros(4, 24), torch.zeros(4, 8)
+    lin.forward_packed(*given)
+    lin.backward(dz)
+    assert all(s[1] is given[0] and s[2] is given[1] for s in seen[-2:])
+    lin.forward(x)
+    assert seen[-1][1] is not given[0] and seen[-1][2] is not given[1]
+    own = seen[-1]
+    lin.backward(dz)
+    assert seen[-1][1] is own[1] and seen[-1][2] is own[2]
+    serve = Q.Linear(4, 24, 8, torch.float32, train=False, device="cpu")
+    serve.set_weight(*w)
+    serve.forward(x)
+    serve.forward_packed(*given)
+    serve.forward(x)
+    assert seen[-1][1] is None and seen[-1][2] is None      # nothing is kept
+    never = Q.Linear(4, 24, 8, torch.float32, packed=True, device="cpu")
+    never.set_weight(*w)
+    assert never.codes is None and never.saved_bytes() == lin.saved_bytes() == 4 * (32 + 4)
+    never.forward_packed(*given)
+    never.backward(dz)
+    assert seen[-1][1] is given[0]
+    with pytest.raises(RuntimeError):
+        never.forward(x)
