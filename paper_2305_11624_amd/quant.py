@@ -87,7 +87,8 @@ class Linear:
         self.packed = packed
         self.codes, self.scales = new_codes(M, K, device) if train and not packed else (None, None)   # what forward packs into
         self._kept = None, None   # what backward reads: these, or those that forward_packed was given
-        self.w_codes = self.w_scales = None
+        self.w_codes = self.w_scales = None   # the weight in use
+        self._own_weight = None               # what pack_weight packs into
         self._w_desc = B.make_qdesc(N, K, dtype=_dtype(dtype))
         self.z = _new_rows(M, N, self.ldz, dtype, device)
         self.dx = _new_rows(M, K, self.ldx, dtype, device) if train else None
@@ -99,14 +100,15 @@ class Linear:
         self.ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
     def set_weight(self, codes: torch.Tensor, scales: torch.Tensor):
-        """A weight that is packed already (`new_codes(N, K)`, `convbn_qpack`): kept, not copied."""
+        """A weight that is packed already (`new_codes(N, K)`, `convbn_qpack`): read where it is, never written."""
         self.w_codes, self.w_scales = _codes(codes, self.N, self.K, "codes"), _vector(scales, self.N, "scales")
 
     def pack_weight(self, W: torch.Tensor, stream=None):
-        """Pack W [N, K] by output channel."""
-        if self.w_codes is None:
-            self.w_codes, self.w_scales = new_codes(self.N, self.K, W.device)
-        B.convbn_qpack(self._w_desc, W, self.w_codes, self.w_scales, stream)
+        """Pack W [N, K] by output channel, into buffers of the layer's own."""
+        if self._own_weight is None:
+            self._own_weight = new_codes(self.N, self.K, W.device)
+        B.convbn_qpack(self._w_desc, W, *self._own_weight, stream)
+        self.w_codes, self.w_scales = self._own_weight
 
     def _desc_with(self, bit: int, field: str, add, width: int, ld: int):
         if add is None:

@@ -568,3 +568,34 @@ def test_no_weight_gradient_before_a_forward_pass():
     with pytest.raises(B.ConvBNError, match="codes"):
         lin.backward(dz)
     assert (lin.backward(dz, need_dW=False)[0] == 8 * 127).all()
+
+
+def _pair(rows, K, seed, dt):
+    """Codes and scales of random rows, and what they stand for in 64 bits."""
+    Q = _q()
+    ck = Q.Checkpoint(rows, K, dt)
+    ck.pack(torch.randn(rows, K, generator=_gen(seed)).to("cuda", dt))
+    return ck.codes, ck.scales
+
+
+@pytest.mark.parametrize("train", [True, False])
+def test_weights_that_were_handed_over_stay_the_callers(train):
+    """Packing a new weight into a layer that shares one leaves the shared one alone."""
+    Q = _q()
+    M, K, N = 5, 72, 40
+    codes, scales = _pair(N, K, 11, torch.bfloat16)
+    kept, x = (codes.clone(), scales.clone()), torch.randn(M, K, generator=_gen(12)).to("cuda", torch.bfloat16)
+    one, two = Q.Linear(M, K, N, train=train), Q.Linear(M, K, N, train=False)
+    for lin in (one, two):
+        lin.set_weight(codes, scales)
+    want = two.forward(x).clone()
+    assert torch.equal(one.forward(x), want)
+    W = torch.randn(N, K, generator=_gen(13)).to("cuda", torch.bfloat16)
+    one.pack_weight(W)
+    assert torch.equal(codes, kept[0]) and torch.equal(scales, kept[1])
+    assert torch.equal(two.forward(x), want) and not torch.equal(one.forward(x), want)
+    own = one.w_codes
+    one.set_weight(codes, scales)
+    assert torch.equal(one.forward(x), want)
+    one.pack_weight(W)
+    assert one.w_codes is own                               # its own, allocated once

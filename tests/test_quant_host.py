@@ -264,3 +264,20 @@ def test_what_a_layer_packs_into_is_its_own(monkeypatch):
     assert seen[-1][1] is given[0]
     with pytest.raises(RuntimeError):
         never.forward(x)
+
+
+def test_a_weight_is_packed_into_the_layers_own_buffers(monkeypatch):
+    from paper_2305_11624_amd import quant as Q
+    seen = []
+    monkeypatch.setattr(B, "convbn_qpack", lambda d, x, codes, scales, stream=None: seen.append((codes, scales)))
+    shared, W = Q.new_codes(8, 24, "cpu"), torch.zeros(8, 24)
+    for train in (True, False):
+        lin = Q.Linear(4, 24, 8, torch.float32, train=train, device="cpu")
+        lin.set_weight(*shared)
+        assert lin.w_codes is shared[0] and lin.w_scales is shared[1]
+        lin.pack_weight(W)
+        own = seen[-1]
+        assert own[0] is not shared[0] and own[1] is not shared[1] and lin.w_codes is own[0] and lin.w_scales is own[1]
+        lin.set_weight(*shared)
+        lin.pack_weight(W)
+        assert seen[-1][0] is own[0] and seen[-1][1] is own[1]      # allocated once
