@@ -2,9 +2,11 @@
 that way, the gate between two of them, and the gated block that they make up.
 
 Each object holds the codes, scales, outputs and workspace of one layer, allocated once; its calls enqueue on the current
-stream (or the one they are given) and allocate nothing.  What they return are the object's own buffers, overwritten by the
+stream (or the one they are given) and allocate nothing, but for the first `pack_weight` and the first `unpack` without `out`, whose
+buffers belong to the stream of that call.  What they return are the object's own buffers, overwritten by the
 next call.  Types, sizes and strides of the arguments are checked before anything is launched (ValueError).
 """
+import contextlib
 from typing import Optional
 
 import torch
@@ -37,6 +39,13 @@ def _new_rows(M, width, ld, dt, device):
     return torch.empty(M, ld, dtype=dt, device=device)[:, :width]
 
 
+def _allocating_for(stream):
+    """A context whose allocations come from the pool of the stream that a call works on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+
+
 def new_codes(rows: int, K: int, device="cuda"):
     """Buffers for `rows` packed rows of K channels: (codes, scales)."""
     return (torch.empty(rows, B.convbn_qrow_bytes(K), dtype=torch.int8, device=device),
@@ -61,7 +70,8 @@ class Checkpoint:
     def unpack(self, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         if out is None:
             if self.out is None:
-                self.out = torch.empty(self.M, self.K, dtype=self.dtype, device=self.codes.device)
+                with _allocating_for(stream):
+                    self.out = torch.empty(self.M, self.K, dtype=self.dtype, device=self.codes.device)
             out = self.out
         self.desc.ldx = out.stride(0) if self.M > 1 else self.K
         B.convbn_qunpack(self.desc, self.codes, self.scales, out, stream)
@@ -106,7 +116,8 @@ class Linear:
     def pack_weight(self, W: torch.Tensor, stream=None):
         """Pack W [N, K] by output channel, into buffers of the layer's own."""
         if self._own_weight is None:
-            self._own_weight = new_codes(self.N, self.K, W.device)
+            with _allocating_for(stream):
+                self._own_weight = new_codes(self.N, self.K, W.device)
         B.convbn_qpack(self._w_desc, W, *self._own_weight, stream)
         self.w_codes, self.w_scales = self._own_weight
 

@@ -599,3 +599,36 @@ def test_weights_that_were_handed_over_stay_the_callers(train):
     assert torch.equal(one.forward(x), want)
     one.pack_weight(W)
     assert one.w_codes is own                               # its own, allocated once
+
+
+def _stream_of(t):
+    """The stream whose pool a tensor's memory comes from."""
+    p = t.untyped_storage().data_ptr()
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= p < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+    raise AssertionError("not the allocator's")
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_what_a_call_allocates_belongs_to_its_stream(raw):
+    """Buffers of a first call on a side stream come from that stream's pool: what the current stream has just freed may still be in use there."""
+    Q = _q()
+    side = torch.cuda.Stream()
+    assert side.cuda_stream != torch.cuda.current_stream().cuda_stream
+    st = side.cuda_stream if raw else side
+    W, x = torch.randn(40, 72, generator=_gen(1)).to("cuda", torch.bfloat16), torch.randn(50, 72, generator=_gen(2)).to("cuda", torch.bfloat16)
+    lin, ck = Q.Linear(50, 72, 40, train=False), Q.Checkpoint(50, 72)
+    side.wait_stream(torch.cuda.current_stream())
+    lin.pack_weight(W, stream=st)
+    ck.pack(x, stream=st)
+    out = ck.unpack(stream=st)
+    side.synchronize()
+    assert [_stream_of(t) for t in (lin.w_codes, lin.w_scales, out)] == [side.cuda_stream] * 3
+    q, s = _pack_ref(W.float().cpu())
+    assert np.array_equal(lin.w_codes.cpu().numpy()[:, :72], q) and np.array_equal(lin.w_scales.cpu().numpy(), s)
+    assert out is ck.unpack(stream=st)
+    side.synchronize()
+    here = Q.Checkpoint(50, 72)
+    here.pack(x)
+    assert torch.equal(here.unpack(), out) and _stream_of(here.out) == torch.cuda.current_stream().cuda_stream
