@@ -3,8 +3,8 @@
     python examples/gated_head.py [--images 8] [--steps 20]
 
 The tokens are the pixels of the backbone's [N, 7, 7, 2048] output, projected to C channels by a Linear-BN block in 8 bits (its input is
-what would take the most memory to keep: 2048 channels a token).  The head learns to reproduce a random teacher head.  Between the passes the
-trained layers keep codes and scales only."""
+what would take the most memory to keep: 2048 channels a token).  The head learns to reproduce a random teacher head.  What the trained layers
+keep of the forward pass for the backward one are codes and scales."""
 import argparse
 import os
 import sys
@@ -17,7 +17,7 @@ from paper_2305_11624_amd.resnet50 import ResNet50  # noqa: E402
 
 
 def head(M, C, F, train):
-    return Q.Linear(M, 2048, C, train=train), Q.GatedBlock(M, C, F, train=train)
+    return Q.Linear(M, 2048, C, train=train, need_dx=False), Q.GatedBlock(M, C, F, train=train)
 
 
 def pack(layers, weights):
@@ -55,13 +55,13 @@ def main(images=8, steps=20, C=256, F=512, lr=0.015):
         losses.append(float(diff.square().mean()))
         dout = (diff * (2 / M)).bfloat16()
         dh, dW_up, dW_down = layers[1].backward(dout)
-        _, dW_in, _ = layers[0].backward(dh, need_dx=False)
+        _, dW_in, _ = layers[0].backward(dh)      # (the backbone is frozen: no gradient of x)
         for w, g in zip(student, (dW_in, dW_up, dW_down)):
             g = g.float()
             w -= lr * w.norm() / g.norm() * g      # a step in proportion to the weight's own size
     kept = sum(l.saved_bytes() for l in layers)
     whole = 2 * M * (2048 + C + 3 * F)
-    print("%d tokens: loss %.4f -> %.4f in %d steps; kept between the passes %.2f MB, %.2f MB in bf16"
+    print("%d tokens: loss %.4f -> %.4f in %d steps; kept for backward: codes and scales %.2f MB, the same rows in bf16 %.2f MB"
           % (M, losses[0], losses[-1], steps, kept / 1e6, whole / 1e6))
     one = head(1, C, F, train=False)
     pack(one, bf16(student))

@@ -632,3 +632,62 @@ def test_what_a_call_allocates_belongs_to_its_stream(raw):
     here = Q.Checkpoint(50, 72)
     here.pack(x)
     assert torch.equal(here.unpack(), out) and _stream_of(here.out) == torch.cuda.current_stream().cuda_stream
+
+
+@pytest.mark.parametrize("M,C,F", [(700, 128, 256), (20, 64, 96)])
+def test_a_stack_of_blocks_keeps_codes_only(M, C, F):
+    """Measured: what a further block of a stack that shares its full-width tensors adds, and that the passes add nothing.  Results and
+    gradients are those of blocks with buffers of their own."""
+    Q = _q()
+    n = 4
+    weights = [((torch.randn(2 * F, C, generator=_gen(10 + i)) * C ** -0.5).to("cuda", torch.bfloat16),
+                (torch.randn(C, F, generator=_gen(20 + i)) * F ** -0.5).to("cuda", torch.bfloat16)) for i in range(n)]
+    x, dout = (torch.randn(M, C, generator=_gen(30 + i)).to("cuda", torch.bfloat16) for i in range(2))
+    first = Q.GatedBlock(M, C, F)
+    before = torch.cuda.memory_allocated()
+    stack = [first] + [Q.GatedBlock(M, C, F, share=first) for _ in range(n - 1)]
+    each = (torch.cuda.memory_allocated() - before) / (n - 1)
+    gradients = 2 * 3 * F * C + 4 * (2 * F + C)
+    assert each <= first.saved_bytes() + gradients + 12 * 512      # (the allocator's granularity, a dozen tensors)
+    if M > 100:
+        assert each - gradients < 0.55 * 2 * M * (C + 3 * F)       # x, h and y in bf16
+    for blk, w in zip(stack, weights):
+        blk.pack_weights(*w)
+
+    def forward(blocks):
+        h = x
+        for blk in blocks:
+            h = blk.forward(h)
+        return h
+
+    def backward(blocks):
+        d = dout
+        for blk in reversed(blocks):
+            d, _, _ = blk.backward(d)
+        return d
+
+    before = torch.cuda.memory_allocated()
+    got = forward(stack)
+    assert torch.cuda.memory_allocated() == before
+    got = got.clone()
+    got_dx = backward(stack).clone()
+    alone = [Q.GatedBlock(M, C, F) for _ in range(n)]
+    for blk, w in zip(alone, weights):
+        blk.pack_weights(*w)
+    assert torch.equal(forward(alone), got) and torch.equal(backward(alone), got_dx)
+    for a, b in zip(alone, stack):
+        assert torch.equal(a.up.dW, b.up.dW) and torch.equal(a.down.dW, b.down.dW)
+
+
+def test_checkpoints_of_one_buffer():
+    Q = _q()
+    out = torch.empty(33, 72, device="cuda")
+    a, b = Q.Checkpoint(33, 72, torch.float32, out=out), Q.Checkpoint(33, 72, torch.float32, out=out)
+    x, y = torch.randn(33, 72, generator=_gen(1)).cuda(), torch.randn(33, 72, generator=_gen(2)).cuda()
+    a.pack(x)
+    b.pack(y)
+    before = torch.cuda.memory_allocated()
+    for ck, t in ((b, y), (a, x)):
+        assert ck.unpack() is out
+        assert (out - t).abs().max() <= t.abs().max() / 250
+    assert torch.cuda.memory_allocated() <= before + 3 * 33 * 72 * 4 + 4096

@@ -281,3 +281,68 @@ def test_a_weight_is_packed_into_the_layers_own_buffers(monkeypatch):
         lin.set_weight(*shared)
         lin.pack_weight(W)
         assert seen[-1][0] is own[0] and seen[-1][1] is own[1]      # allocated once
+
+
+def _held(*objects):
+    """Bytes of the distinct buffers that objects hold, themselves or in what they are made of."""
+    seen = {}
+
+    def look(o):
+        for v in vars(o).values():
+            for t in v if isinstance(v, tuple) else (v,):
+                if isinstance(t, torch.Tensor):
+                    seen[t.untyped_storage().data_ptr()] = t.untyped_storage().nbytes()
+                elif type(t).__module__ == type(o).__module__:
+                    look(t)
+
+    for o in objects:
+        look(o)
+    return sum(seen.values())
+
+
+@pytest.mark.parametrize("M,C,F,dtype", [(1568, 64, 256, torch.bfloat16), (40, 72, 136, torch.float32), (4, 64, 96, torch.bfloat16)])
+def test_a_further_block_of_a_stack_adds_codes_and_gradients_of_weights_only(M, C, F, dtype):
+    """By the buffers that the objects hold: the full-width rows and the workspace are there once for the stack."""
+    from paper_2305_11624_amd import quant as Q
+    e = torch.finfo(dtype).bits // 8
+    one = Q.GatedBlock(M, C, F, dtype, device="cpu")
+    more = [Q.GatedBlock(M, C, F, dtype, device="cpu", share=one) for _ in range(3)]
+    dW = 3 * F * C * e + 4 * (2 * F + C)      # and the biases' gradients
+    assert _held(one, *more) - _held(one) == 3 * (one.saved_bytes() + dW)
+    assert one.gate.dh is one.up.z            # h's gradient in h's place
+    assert _held(one) == one.saved_bytes() + dW + e * M * (3 * F + 2 * C) + one.up.ws.nbytes
+    assert one.up.ws is one.down.ws
+    serve = [Q.GatedBlock(M, C, F, dtype, train=False, device="cpu", share=one) for _ in range(2)]
+    assert _held(one, *serve) - _held(one) == 2 * M * (B.convbn_qrow_bytes(F) + 4)      # (y packed)
+    for bad in (dict(M=M + 1), dict(C=C + 8), dict(F=F + 8), dict(dtype=torch.float32 if e == 2 else torch.bfloat16)):
+        with pytest.raises(ValueError):
+            Q.GatedBlock(**{**dict(M=M, C=C, F=F, dtype=dtype), **bad}, device="cpu", share=one)
+    with pytest.raises(ValueError):
+        Q.GatedBlock(M, C, F, dtype, device="cpu", share=serve[0])
+
+
+def test_buffers_of_the_caller_and_gradients_that_are_not_asked_for():
+    from paper_2305_11624_amd import quant as Q
+    z, dx, ws = torch.zeros(40, 8), torch.zeros(40, 24), torch.zeros(Q.linear_workspace_bytes(40, 24, 8, torch.float32), dtype=torch.uint8)
+    lin = Q.Linear(40, 24, 8, torch.float32, device="cpu", z=z, dx=dx, ws=ws)
+    assert lin.z is z and lin.dx is dx and lin.ws is ws
+    for bad in (dict(z=z.t()), dict(z=z[:-1]), dict(dx=dx.bfloat16()), dict(z=torch.zeros(40, 9)[:, :8]), dict(z=torch.zeros(40, 16)[:, ::2]), dict(ws=ws[:-1]),
+                dict(z=torch.zeros(40, 8, device="meta"))):
+        with pytest.raises(ValueError):
+            Q.Linear(40, 24, 8, torch.float32, device="cpu", **bad)
+    first = Q.Linear(40, 24, 8, torch.float32, device="cpu", need_dx=False)
+    assert first.dx is None and first.dW is not None
+    first.set_weight(*Q.new_codes(8, 24, "cpu"))
+    with pytest.raises(RuntimeError):
+        first.backward(torch.zeros(40, 8), need_dx=True)
+    frozen = Q.Linear(40, 24, 8, torch.float32, device="cpu", need_dW=False)
+    assert frozen.dW is None and frozen.dx is not None
+    y, dh = torch.zeros(4, 8), torch.zeros(4, 16)
+    gate = Q.Gate(4, 8, torch.float32, device="cpu", y=y, dh=dh)
+    assert gate.y is y and gate.dh is dh
+    out = torch.zeros(4, 8)
+    assert Q.Checkpoint(4, 8, torch.float32, device="cpu", out=out).out is out
+    for make in (lambda: Q.Gate(4, 8, torch.float32, device="cpu", y=y[:, :7]), lambda: Q.Gate(4, 8, torch.float32, device="cpu", dh=dh[:3]),
+                 lambda: Q.Checkpoint(4, 8, torch.float32, device="cpu", out=out.bfloat16())):
+        with pytest.raises(ValueError):
+            make()
