@@ -98,6 +98,11 @@ __device__ __forceinline__ Scale scale_of(unsigned bits) {
   return {s, 127.f / a};
 }
 
+// The order of sum * s_x * s_w.  The scales' own product can leave the range where the result does not (two rows below 2^-60, a mask's value against
+// a large weight: zero sums became NaN), so the sum, a whole number below 2^31, meets one scale first: the row's, after which it is at least
+// 2^-126 and, as long as that scale is at most 2^96, finite.  Above, the row's comes last: if the sum overflows with the other, the result does.
+__device__ __forceinline__ bool scale_last(float sx) { return sx > 0x1p96f; }
+
 // 8 codes: adding 1.5 * 2^23 to |v| <= 127.0001 rounds it to a whole number, ties to even, and leaves it in the low byte.  The
 // product is rounded before that (the definition): no fused multiply-add here.
 __device__ __forceinline__ uint2 codes8(const F8& f, float r) {

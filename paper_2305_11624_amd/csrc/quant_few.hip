@@ -128,7 +128,8 @@ __global__ __launch_bounds__(1024) void qfew_kernel(FewParams p) {
     for (int wv = 0; wv < waves; ++wv)
       for (int q = 0; q < 16; q += p.T) v += sums[((wv * NB + b) * 16 + q + mm) * 16 + q + c];
     const float sx = PACK ? own_s[m] : p.m.sx[m];
-    float z = (float)v * (sx * p.m.sw[n]) + (p.m.b ? p.m.b[n] : 0.f);
+    const float sw = p.m.sw[n], bias = p.m.b ? p.m.b[n] : 0.f;
+    float z = scale_last(sx) ? (float)v * sw * sx + bias : (float)v * sx * sw + bias;
     if (p.m.add) z += to_f32(static_cast<const T*>(p.m.add)[m * p.m.ldz + n]);
     static_cast<T*>(p.m.z)[m * p.m.ldz + n] = from_f32<T>(z);
   }

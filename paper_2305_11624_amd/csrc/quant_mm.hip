@@ -30,8 +30,13 @@ struct MulParams {
 template <typename T>
 __device__ __forceinline__ void finish8(const QMul& q, i64 m, int n, const int (&acc)[8], float sx, const float (&sw)[8], const float (&b)[8]) {
   F8 f;
+  if (scale_last(sx)) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * (sx * sw[i]) + b[i];
+    for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * sw[i] * sx + b[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * sx * sw[i] + b[i];
+  }
   store8_plus<T>(static_cast<T*>(q.z) + m * q.ldz, q.add ? static_cast<const T*>(q.add) + m * q.ldz : nullptr, n, q.N, f);
 }
 

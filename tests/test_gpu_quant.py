@@ -691,3 +691,39 @@ def test_checkpoints_of_one_buffer():
         assert ck.unpack() is out
         assert (out - t).abs().max() <= t.abs().max() / 250
     assert torch.cuda.memory_allocated() <= before + 3 * 33 * 72 * 4 + 4096
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 40), (5, 300, 33), (24, 72, 64), (40, 136, 72), (70, 8192, 64), (300, 264, 512), (1100, 64, 264)])
+def test_scales_at_both_ends_of_the_range(M, K, N, dtype):
+    """Rows and weights from the smallest that are kept to the type's largest: s_x s_w alone leaves the range where the sum times both does not.
+    The sum is exact, then a conversion, two products and the result's rounding: 8 u, and the spacing of numbers below the normal range."""
+    Q, dt = _q(), DT[dtype]
+    ex, ew = [-118, -70, 0, 70, 120], [-118, -40, 0, 40, 100]
+    g = _gen(M + N)
+    x, W = torch.randn(M, K, generator=g).clamp(-4, 4), torch.randn(N, K, generator=g).clamp(-4, 4)
+    x, W = (t * torch.tensor([2.0 ** e[(i + s) % 5] for i in range(len(t))])[:, None] for t, e, s in ((x, ex, M), (W, ew, 0)))
+    x[0] *= 0
+    x[0, :2] = torch.tensor([torch.finfo(dt).max, -1.0])      # a mask's value beside codes that are zero
+    W[1] = 0
+    W[1, -1] = 2.0 ** 100                                     # its sum with that row is 0: 0 is the result, not 0 times infinity
+    x, W = x.to(dt).float(), W.to(dt).float()
+    (qx, sx), (qw, sw) = _pack_ref(x), _pack_ref(W)
+    sums = qx.astype(np.int64) @ qw.astype(np.int64).T
+    ref = sums.astype(np.float64) * sx[:, None].astype(np.float64) * sw.astype(np.float64)
+    assert sums[0, 1] == 0 and (np.abs(ref) > 1e39).any() == (M > 1 or N > 4)
+    lin = Q.Linear(M, K, N, dt)
+    lin.pack_weight(W.to("cuda", dt))
+    xd = x.to("cuda", dt)
+    results = [lin.forward(xd).clone(), lin.forward_packed(lin.codes, lin.scales).clone()]
+    serve = Q.Linear(M, K, N, dt, train=False)
+    serve.set_weight(lin.w_codes, lin.w_scales)
+    results.append(serve.forward(xd))
+    top = float(torch.finfo(dt).max)
+    half, least = (H, 2.0 ** -126) if dtype == "bf16" else (0.0, 2.0 ** -148)
+    for z in results:
+        z = _np(z)
+        assert not np.isnan(z).any()
+        over, under = np.abs(ref) > top * (1 + H), np.abs(ref) < top * (1 - H)
+        assert np.array_equal(z[over], np.sign(ref[over]) * np.inf)
+        assert (np.abs(z - ref)[under] <= (8 * U + half) * np.abs(ref)[under] + least).all()
