@@ -34,10 +34,17 @@ template <int LPR, int N> __device__ __forceinline__ void group_max(unsigned (&m
   }
 }
 
-// f(g) and f'(g)
-template <int KIND> __device__ __forceinline__ void gate_of(float g, float* f, float* df) {
-  if constexpr (KIND == CONVBN_GATE_SILU) {
-    // (the hardware's 2^x and reciprocal, 1 ulp each: p is right to |g| p ulp, at most 0.3, and a few)
+// f(g) and f'(g), for rows of T
+template <typename T, int KIND> __device__ __forceinline__ void gate_of(float g, float* f, float* df) {
+  if constexpr (KIND == CONVBN_GATE_SILU && sizeof(T) == 4) {
+    // p = 1 / (1 + e^-g) and 1 - p from e^-|g|, which neither overflows nor cancels: a few ulp each at either sign
+    const float e = expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;   // (1 ulp, between 1 and 2)
+    const float p = g < 0.f ? er : r, q = g < 0.f ? r : er;
+    *f = g * p;
+    *df = p * (1.f + g * q);
+  } else if constexpr (KIND == CONVBN_GATE_SILU) {
+    // (the hardware's 2^x and reciprocal, 1 ulp each, and an exponent that is rounded: p is right to 2^-23 (1 + |g|), 2^-16 where it is smallest,
+    // far inside the 2^-9 of the result)
     const float p = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504088896341f));
     *f = g * p;
     *df = p * (1.f + g * (1.f - p));
@@ -124,7 +131,7 @@ __global__ __launch_bounds__(threads_of(LPR)) void qgate_fwd_kernel(GateArgs p) 
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float f, df;
-        gate_of<KIND>(g.v[i], &f, &df);
+        gate_of<T, KIND>(g.v[i], &f, &df);
         y.v[i] = f * u.v[i];
       }
       return y;
@@ -198,7 +205,7 @@ __global__ __launch_bounds__(NT) void qgate_bwd_kernel(GateArgs p, unsigned piec
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float f, df;
-      gate_of<KIND>(g.v[e], &f, &df);
+      gate_of<T, KIND>(g.v[e], &f, &df);
       dg.v[e] = dy.v[e] * u.v[e] * df;
       du.v[e] = dy.v[e] * f;
     }

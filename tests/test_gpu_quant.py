@@ -727,3 +727,28 @@ def test_scales_at_both_ends_of_the_range(M, K, N, dtype):
         over, under = np.abs(ref) > top * (1 + H), np.abs(ref) < top * (1 - H)
         assert np.array_equal(z[over], np.sign(ref[over]) * np.inf)
         assert (np.abs(z - ref)[under] <= (8 * U + half) * np.abs(ref)[under] + least).all()
+
+
+@pytest.mark.parametrize("M", [2, 600])
+def test_fp32_silu_is_right_to_its_last_bits_for_negative_inputs(M):
+    """e^-|g| is right to 2 ulp; a sum, a quotient and two or three products follow: 8 u of y, and 12 u of the two terms of f'.  Below the
+    smallest normal number nothing is promised."""
+    Q = _q()
+    K = 1024
+    g = (torch.arange(M * K) % 1999 - 999).view(M, K).float() * 0.08 + torch.rand(M, K, generator=_gen(3)) * 0.07      # -80 .. 80
+    u, dy = torch.randn(M, K, generator=_gen(4)), torch.randn(M, K, generator=_gen(5))
+    h = torch.cat([g, u], 1)
+    gate = Q.Gate(M, K, torch.float32)
+    y = _np(gate.forward(h.cuda()))
+    f, _ = _act64("silu", _np(g))
+    assert (np.abs(y - f * _np(u)) <= 8 * U * np.abs(f * _np(u)) + 2.0 ** -126).all()
+    # backward from given codes: the same range of g, scale 80 / 127 apart
+    dh = _np(gate.backward(dy.cuda()))
+    q, s = _pack_ref(np.stack([g.numpy(), u.numpy()], 1).reshape(2 * M, K))
+    back = (q.astype(np.float32) * s[:, None]).astype(np.float64).reshape(M, 2, K)
+    gt, ut = back[:, 0], back[:, 1]
+    p, one_less = 1 / (1 + np.exp(-gt)), 1 / (1 + np.exp(gt))
+    f, df = gt * p, p * (1 + gt * one_less)
+    terms = np.abs(_np(dy) * ut) * p * (1 + np.abs(gt) * one_less)
+    assert (np.abs(dh[:, :K] - _np(dy) * ut * df) <= 12 * U * terms + 2.0 ** -126).all()
+    assert (np.abs(dh[:, K:] - _np(dy) * f) <= 8 * U * np.abs(_np(dy) * f) + 2.0 ** -126).all()
