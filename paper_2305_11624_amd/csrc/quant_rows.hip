@@ -49,9 +49,22 @@ template <typename T, int KIND> __device__ __forceinline__ void gate_of(float g,
     *f = g * p;
     *df = p * (1.f + g * (1.f - p));
   } else {
-    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+    // The distribution's tail beyond |g| is e^(-g^2 / 2) times a smooth function, here t Q(t) with t = 1 / (1 + 0.27 |g|) and Q the polynomial of
+    // degree 8 with the least relative error for |g| <= 16 (2.4e-8; a weighted least-squares fit in 64 bits): right to (17 + 1.5 g^2) 2^-24
+    // at either sign, where 1 + erf(g / sqrt 2) cancels for negative g (a tenth at -5).  f and f' share the exponential.
+    const float a = fabsf(g), t = __builtin_amdgcn_rcpf(fmaf(0.27f, a, 1.f)), e = __builtin_amdgcn_exp2f(a * a * -0.72134752044448170f);
+    float Q = 0.0290384758f;
+    Q = fmaf(Q, t, -0.126874059f);
+    Q = fmaf(Q, t, 0.170616165f);
+    Q = fmaf(Q, t, -0.0701961815f);
+    Q = fmaf(Q, t, 0.108534291f);
+    Q = fmaf(Q, t, 0.0717343763f);
+    Q = fmaf(Q, t, 0.101895072f);
+    Q = fmaf(Q, t, 0.107530445f);
+    Q = fmaf(Q, t, 0.107721426f);
+    const float tail = t * Q * e, p = g < 0.f ? tail : 1.f - tail;
     *f = g * p;
-    *df = p + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+    *df = p + g * e * 0.39894228040143268f;
   }
 }
 

@@ -752,3 +752,36 @@ def test_fp32_silu_is_right_to_its_last_bits_for_negative_inputs(M):
     terms = np.abs(_np(dy) * ut) * p * (1 + np.abs(gt) * one_less)
     assert (np.abs(dh[:, :K] - _np(dy) * ut * df) <= 12 * U * terms + 2.0 ** -126).all()
     assert (np.abs(dh[:, K:] - _np(dy) * f) <= 8 * U * np.abs(_np(dy) * f) + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gelu_keeps_its_relative_accuracy_for_negative_inputs(dtype):
+    """The normal distribution's tail, not 1 - (1 - tail).  It is a smooth factor times e^(-g^2 / 2), whose argument is rounded three times: 1.5 g^2 u,
+    and about 17 u for the factor, the exponential and the products.  Below the smallest normal number nothing is promised."""
+    Q, dt = _q(), DT[dtype]
+    M, K = 64, 1024
+    g = ((torch.arange(M * K) % 2603 - 1301).view(M, K).float() * 0.01 + torch.rand(M, K, generator=_gen(3)) * 0.009).to(dt).float()      # -13 .. 13
+    u, dy = (torch.randn(M, K, generator=_gen(i)).to(dt).float() for i in (4, 5))
+    half = H if dtype == "bf16" else 0.0
+
+    def parts(g):
+        return 0.5 * torch.special.erfc(torch.from_numpy(-g / math.sqrt(2))).numpy(), np.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+
+    gate = Q.Gate(M, K, dt, kind="gelu")
+    y = _np(gate.forward(torch.cat([g, u], 1).to("cuda", dt)))
+    want = _np(g) * parts(_np(g))[0] * _np(u)
+    assert (np.abs(y - want) <= ((20 + 2.5 * _np(g) ** 2) * U + half) * np.abs(want) + 2.0 ** -126).all()
+    dh = _np(gate.backward(dy.to("cuda", dt)))
+    q, s = _pack_ref(np.stack([g.numpy(), u.numpy()], 1).reshape(2 * M, K))
+    back = (q.astype(np.float32) * s[:, None]).astype(np.float64).reshape(M, 2, K)
+    gt, ut = back[:, 0], back[:, 1]
+    p, phi = parts(gt)
+    r = (20 + 2.5 * gt ** 2) * U
+    want = _np(dy) * ut * (p + gt * phi)
+    assert (np.abs(dh[:, :K] - want) <= r * np.abs(_np(dy) * ut) * (p + np.abs(gt) * phi) + half * np.abs(want) + 2.0 ** -126).all()
+    want = _np(dy) * gt * p
+    assert (np.abs(dh[:, K:] - want) <= (r + half) * np.abs(want) + 2.0 ** -126).all()
+    lowest = torch.zeros(1, 16)
+    lowest[0, :3] = torch.tensor([torch.finfo(dt).min, -40.0, torch.finfo(dt).max])      # a mask's value: 0, and nothing that is not finite
+    y = Q.Gate(1, 8, dt, kind="gelu", train=False).forward(torch.cat([lowest[:, :8], torch.ones(1, 8)], 1).to("cuda", dt)).float().cpu()
+    assert y[0, :2].abs().max() == 0 and y[0, 2] == torch.finfo(dt).max and (y[0, 3:] == 0).all()
