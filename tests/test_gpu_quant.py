@@ -785,3 +785,120 @@ def test_gelu_keeps_its_relative_accuracy_for_negative_inputs(dtype):
     lowest[0, :3] = torch.tensor([torch.finfo(dt).min, -40.0, torch.finfo(dt).max])      # a mask's value: 0, and nothing that is not finite
     y = Q.Gate(1, 8, dt, kind="gelu", train=False).forward(torch.cat([lowest[:, :8], torch.ones(1, 8)], 1).to("cuda", dt)).float().cpu()
     assert y[0, :2].abs().max() == 0 and y[0, 2] == torch.finfo(dt).max and (y[0, 3:] == 0).all()
+
+
+def _device_whole(rows, cols, most, keep, g):
+    t = torch.randint(-most, most + 1, (rows, cols), generator=g, device="cuda").float()
+    return t * (torch.rand(rows, cols, generator=g, device="cuda") < keep)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 40), (5, 40, 24), (50, 72, 33), (333, 256, 512), (2000, 136, 72), (9000, 64, 64), (9000, 72, 67), (260, 1032, 520),
+                                   (4352, 264, 4096), (4100, 128, 4101)])
+def test_every_subset_of_the_gradients(M, K, N, dtype):
+    """dx, dW and db, each asked for or not: what is asked for is exact on whole numbers, the rest stays as it was."""
+    Q, dt = _q(), DT[dtype]
+    g = torch.Generator(device="cuda").manual_seed(M + K + N)
+    x, W, dz = _device_whole(M, K, 60, 0.5, g), _device_whole(N, K, 9, 0.5, g), _device_whole(M, N, 2, 0.5, g)
+    x[torch.arange(M), torch.arange(M) % K] = 127
+    W[torch.arange(N), torch.arange(N) % K] = 127
+    lin = Q.Linear(M, K, N, dt)
+    lin.pack_weight(W.to(dt))
+    lin.forward(x.to(dt))
+    xd, gd = x.double(), dz.double()
+    want = (gd @ W.double()).to(dt), (gd.t().contiguous() @ xd).to(dt), dz.sum(0)
+    assert (gd.abs().t().contiguous() @ xd.abs()).max() < 2 ** 24
+    dzt = dz.to(dt)
+    for subset in range(1, 8):
+        asked = [bool(subset >> i & 1) for i in range(3)]
+        for t in (lin.dx, lin.dW, lin.db):
+            t.fill_(float("nan"))
+        if lin.ws is not None:
+            lin.ws.fill_(255)
+        got = lin.backward(dzt, need_dx=asked[0], need_dW=asked[1], bias=asked[2])
+        for on, have, held, ref in zip(asked, got, (lin.dx, lin.dW, lin.db), want):
+            assert (have is held and torch.equal(have, ref)) if on else (have is None and torch.isnan(held).all()), asked
+
+
+def _off(rows, width, ld, dt, by=1):
+    """Rows that start `by` elements off 16 bytes, poisoned."""
+    flat = torch.full((rows * ld + by,), float("nan"), dtype=dt, device="cuda")
+    view = flat[by:].view(rows, ld)[:, :width]
+    assert view.data_ptr() % 16 == by * flat.element_size()
+    return view
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("by", [1, 3])
+@pytest.mark.parametrize("M,K,N,gap", [(1, 64, 40, 0), (1, 2048, 33, 0), (3, 104, 24, 8), (40, 72, 136, 0), (300, 264, 65, 8), (1100, 64, 264, 0)])
+def test_rows_that_start_off_16_bytes(M, K, N, gap, by, dtype):
+    """x, z, dx and the addends of a product, h, y, dy and dh of a gate, what a checkpoint packs and reads back: all at an element's alignment, with
+    distances that are multiples of 8 too.  dz as well, where it is not read in place (fp32, odd N)."""
+    Q, dt = _q(), DT[dtype]
+
+    def put(t, ld):
+        v = _off(t.shape[0], t.shape[1], ld, dt, by)
+        v.copy_(t)
+        return v
+
+    x, W = _whole(M, K, 1), _whole(N, K, 2, 8)
+    add, add_in = torch.randint(-9, 10, (M, N), generator=_gen(6)).float(), torch.randint(-9, 10, (M, K), generator=_gen(7)).float()
+    dz = torch.randint(-2, 3, (M, N), generator=_gen(3)).float()
+    lin = Q.Linear(M, K, N, dt, gap=gap, z=_off(M, N, N + gap, dt, by), dx=_off(M, K, K + gap, dt, by))
+    lin.pack_weight(W.to("cuda", dt))
+    xd, wd, gd = x.double(), W.double(), dz.double()
+    assert torch.equal(lin.forward(put(x, K + gap), add=put(add, N + gap)).cpu(), (xd @ wd.t() + add).to(dt))
+    in_place = dtype == "bf16" and N % 8 == 0
+    dzr = _rows(dz, gap, dt) if in_place else put(dz, N + gap)
+    dx, dW, db = lin.backward(dzr, bias=True, add=put(add_in, K + gap))
+    assert torch.equal(dx.cpu(), (gd @ wd + add_in).to(dt)) and torch.equal(dW.cpu(), (gd.t() @ xd).to(dt)) and torch.equal(db.cpu(), dz.sum(0))
+    if in_place:
+        with pytest.raises(B.ConvBNError, match="16-byte"):
+            lin.backward(put(dz, N + gap))
+    serve = Q.Linear(M, K, N, dt, train=False, gap=gap, z=_off(M, N, N + gap, dt, by))
+    serve.set_weight(lin.w_codes, lin.w_scales)
+    assert torch.equal(serve.forward(put(x, K + gap)).cpu(), (xd @ wd.t()).to(dt))
+    ck = Q.Checkpoint(M, K, dt)
+    ck.pack(put(x, K + gap))
+    assert torch.equal(ck.unpack(_off(M, K, K + gap, dt, by)).cpu().float(), x)
+    h, dy = torch.randn(M, 2 * K, generator=_gen(8)).to(dt), torch.randn(M, K, generator=_gen(9)).to(dt)
+    here = Q.Gate(M, K, dt, gap=gap, y=_off(M, K, K + gap, dt, by), dh=_off(M, 2 * K, 2 * K + gap, dt, by))
+    there = Q.Gate(M, K, dt)
+    assert torch.equal(here.forward(put(h, 2 * K + gap)), there.forward(h.cuda()))
+    assert torch.equal(here.backward(put(dy, K + gap)), there.backward(dy.cuda()))
+
+
+@pytest.mark.parametrize("M,K,N,bias", [(40, 136, 72, True), (1568, 512, 264, True), (700, 1024, 2048, False), (4100, 256, 136, False)])
+def test_bf16_gradients_are_those_of_the_rows_that_a_checkpoint_reads_back(M, K, N, bias):
+    """s q in bf16, as unpack returns it, is what the gradients multiply: against 64 bits of these operands nothing but the fp32 sums and the
+    result's rounding is left."""
+    Q = _q()
+    x, W = _activations(M, K, torch.bfloat16, 11).to("cuda", torch.bfloat16), (torch.randn(N, K, generator=_gen(12)) * K ** -0.5).to("cuda", torch.bfloat16)
+    dz = (torch.randn(M, N, generator=_gen(13)) * 1e-3).to("cuda", torch.bfloat16)
+    lin = Q.Linear(M, K, N)
+    lin.pack_weight(W)
+    lin.forward(x)
+    dx, dW, db = lin.backward(dz, bias=bias)
+    rows, weight = Q.Checkpoint(M, K), Q.Checkpoint(N, K)
+    rows.codes, rows.scales, weight.codes, weight.scales = lin.codes, lin.scales, lin.w_codes, lin.w_scales
+    xr, wr, g = rows.unpack().double(), weight.unpack().double(), dz.double()
+    for got, a, b, R in ((dx, g, wr, N), (dW, g.t().contiguous(), xr, M)):
+        ref, terms = a @ b, a.abs() @ b.abs()
+        assert ((got.double() - ref).abs() <= (R + 8) * U * terms + H * ref.abs() + 1e-37).all()
+
+
+@pytest.mark.parametrize("M,K,N", [(50, 72, 136), (333, 256, 65)])
+@pytest.mark.parametrize("scale", [2.0 ** -90, 2.0 ** 60])
+def test_fp32_gradients_of_very_small_and_very_large_rows(M, K, N, scale):
+    """dz s in three parts has all its bits as long as its last one is a normal bf16 number: dz s above 2^-100."""
+    Q = _q()
+    x, W = _activations(M, K, torch.float32, 11) * scale, torch.randn(N, K, generator=_gen(12)) * scale
+    dz = torch.randn(M, N, generator=_gen(13)).sign() * torch.rand(M, N, generator=_gen(14)).add(0.5)
+    lin = Q.Linear(M, K, N, torch.float32)
+    lin.pack_weight(W.cuda())
+    lin.forward(x.cuda())
+    dx, dW, _ = lin.backward(dz.cuda())
+    (qx, sx), (qw, sw) = _pack_ref(x), _pack_ref(W)
+    xt, wt, g = qx.astype(np.float64) * sx[:, None], qw.astype(np.float64) * sw[:, None], _np(dz)
+    for got, a, b, R in ((dx, g, wt, N), (dW, g.T, xt, M)):
+        assert (np.abs(_np(got) - a @ b) <= (R + 8) * U * (np.abs(a) @ np.abs(b))).all()
