@@ -11,6 +11,12 @@ inline __host__ __device__ int qrow(int channels) { return (channels + 15) & ~15
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+constexpr unsigned OOB = 0x80000000u;   // an offset beyond any buffer: the load returns zeros
+// `bytes` (at most 2^31 - 16 of them) from p on, for loads into registers
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, i64 bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000);
+}
+
 // ---- copies from memory into LDS.  Inline asm: what the compiler knows to be such a copy it waits for before every LDS read.  Nothing is
 // returned in registers.  Five wait states in front: a vector memory instruction must not follow sooner where a vector instruction wrote one
 // of its scalar registers, and inside asm nobody else counts them (0.3 - 1 % of a pass).

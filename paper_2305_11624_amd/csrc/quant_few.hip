@@ -17,7 +17,6 @@ namespace convbn {
 
 namespace {
 
-constexpr unsigned OOB = 0x80000000u;
 constexpr int unroll_of(int NB) { return NB == 1 ? 8 : 4; }   // weight pieces a lane has in flight (and as many of each block of x)
 
 struct FewParams {
@@ -26,10 +25,6 @@ struct FewParams {
   uint8_t* codes; float* scales;    // where they go if they are kept (null: nowhere)
   int Kp, T, steps;                 // steps of 64 * 16 / T channels
 };
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, i64 bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000);
-}
 
 // NB: blocks of 16 rows of x (T == 16 where there are several).  PACK: x comes as T.
 template <typename T, int NB, bool PACK>

@@ -20,12 +20,7 @@ namespace {
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr unsigned OOB = 0x80000000u;   // beyond any buffer: the load returns zeros
 constexpr int RC = 64;                  // of the reduced index at a time
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, i64 bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(bytes > 0x7ffffff0LL ? 0x7ffffff0LL : bytes), 0x00020000);
-}
 
 struct GradParams {
   const bf16_t* A;      // [planes][rows][lda]; aligned, zeros between the last channel and a multiple of 8

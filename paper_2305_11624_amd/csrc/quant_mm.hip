@@ -16,7 +16,6 @@ namespace {
 
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr unsigned OOB = 0x80000000u;   // beyond any buffer: the load returns zeros
 constexpr int KC = 128;                 // channels at a time: a whole cache line a row
 
 struct MulParams {
