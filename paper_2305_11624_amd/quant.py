@@ -165,6 +165,8 @@ class Linear:
         self._ready()
         if self.packed:
             raise RuntimeError("this layer takes packed rows (packed=True)")
+        if x is None:
+            raise ValueError("x: expected rows")
         d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
         B.convbn_qlinear_fwd(d, x, self.codes, self.scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         self._kept = self.codes, self.scales
@@ -174,6 +176,8 @@ class Linear:
                        add: Optional[torch.Tensor] = None, stream=None):
         """The same for rows that are packed already; with `train` they are what `backward` reads, so leave them as they are until then."""
         self._ready()
+        if codes is None or scales is None:
+            raise ValueError("codes, scales: expected packed rows")
         d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
         B.convbn_qlinear_fwd(d, None, codes, scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         if self.train:

@@ -346,3 +346,17 @@ def test_buffers_of_the_caller_and_gradients_that_are_not_asked_for():
                  lambda: Q.Checkpoint(4, 8, torch.float32, device="cpu", out=out.bfloat16())):
         with pytest.raises(ValueError):
             make()
+
+
+@pytest.mark.parametrize("train", [True, False])
+def test_forward_of_no_tensor_is_refused(train, monkeypatch):
+    """The entry point reads given codes where it gets no rows; a layer's forward has rows, and never multiplies what its buffers still hold."""
+    from paper_2305_11624_amd import quant as Q
+    monkeypatch.setattr(B, "convbn_qlinear_fwd", lambda *a: pytest.fail("launched"))
+    lin = Q.Linear(4, 24, 8, torch.float32, train=train, device="cpu")
+    lin.set_weight(*Q.new_codes(8, 24, "cpu"))
+    with pytest.raises(ValueError):
+        lin.forward(None)
+    for codes, scales in ((None, None), (lin.w_codes, None)):
+        with pytest.raises(ValueError):
+            lin.forward_packed(codes, scales)
