@@ -2,7 +2,10 @@
 //
 // Both products are C[i][j] = sum_r A(i, r) s[r] q[r][j] with codes that run along j: the input gradient reduces over the output
 // channels (A = dz), the weight gradient over the rows (A = dz^T).  Codes become bf16 numbers s q on their way into LDS, once for
-// all waves of a workgroup; q alone is exact there, s q is rounded to bf16 (as the activation it stands for would be).
+// all waves of a workgroup; q alone is exact there, s q is rounded to bf16.  That is the number that a checkpoint reads back as in bf16, so that a
+// block's gradients are the same from the codes and from the rows; it takes the result from 0.0017 of its norm (its own rounding) to 0.0024
+// against unrounded operands.  A product without it takes two or three bf16 parts in place of one: fp32 rows, in three, take 723 us for dx of
+// 8192 x 4096 x 4096 and bf16 rows 231, dW 709 and 228.
 //
 // F32: A s is split into three bf16 parts that add up to all 24 bits, the codes stay whole numbers, and the three products are
 // summed in fp32: nothing is rounded below that.

@@ -29,13 +29,10 @@ struct MulParams {
 template <typename T>
 __device__ __forceinline__ void finish8(const QMul& q, i64 m, int n, const int (&acc)[8], float sx, const float (&sw)[8], const float (&b)[8]) {
   F8 f;
-  if (scale_last(sx)) {
+  // (no branch: one by the row's scale in front of a store takes 22144 x 192 -> 3840 from 66 to 68 - 70 us, wherever it stands, the third factor to 67)
+  const float first = scale_last(sx) ? 1.f : sx, last = scale_last(sx) ? sx : 1.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * sw[i] * sx + b[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * sx * sw[i] + b[i];
-  }
+  for (int i = 0; i < 8; ++i) f.v[i] = (float)acc[i] * first * sw[i] * last + b[i];
   store8_plus<T>(static_cast<T*>(q.z) + m * q.ldz, q.add ? static_cast<const T*>(q.add) + m * q.ldz : nullptr, n, q.N, f);
 }
 

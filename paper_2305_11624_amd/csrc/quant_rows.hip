@@ -5,7 +5,8 @@
 // are too long for that (VPL = 0) are read twice, the second time from the caches.  Many rows are bound by memory (100352 x 256: 15 us,
 // 5.1 TB/s); few rows by the way there and back, so they take as many lanes as there are pieces, up to 1024
 // (49 x 2048: 2.7 us for a launch).  The gate reads and writes 8 bytes for each bf16 element of y, forward and backward, and memory bounds
-// it: 8192 x 8192, 537 MB, forward 113 us, 4.8 TB/s, backward 88 us, 6.1 TB/s (a part of what it reads is still in the last-level cache).
+// it: 8192 x 8192, 537 MB, forward 113 us, 4.8 TB/s, backward 90 us, 6.0 TB/s (a part of what it reads is still in the last-level cache); GELU,
+// with twice the operations, 117 and 94.  fp32 rows: 940 MB each way, 165 us, 5.7 TB/s, with either f.
 #include "quant_code.h"
 
 namespace convbn {

@@ -186,7 +186,8 @@ class Linear:
 
     def backward(self, dz: torch.Tensor, need_dx: Optional[bool] = None, need_dW: Optional[bool] = None, bias: bool = False,
                  add: Optional[torch.Tensor] = None, stream=None):
-        """(dx (+ add), dW, db) from the kept codes; None for what is not asked for (need_dx, need_dW: as the layer was made)."""
+        """(dx (+ add), dW, db) from the kept codes; None for what is not asked for (need_dx, need_dW: as the layer was made).  bf16 dz whose N and
+        row distance are multiples of 8 is read where it is, and has to start on 16 bytes."""
         if not self.train:
             raise RuntimeError("this layer keeps no codes (train=False)")
         self._ready()
