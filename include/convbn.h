@@ -442,22 +442,23 @@ convbn_status convbn_aux_maxpool_bwd(int dtype, const void *dy, const void *idx,
  *
  * A row of channels -- a token, a pixel of a channels-last tensor, an output channel's weights -- is held as
  *     a = max |x|,   s = a / 127,   code = rint(x (127 / a))  in fp32, ties to even:  -127 .. 127,
- * so that x is about s code (s the next smaller fp32 where 127 s would overflow).  A row with a < 2^-119 (all zeros: padding) has s = 0 and codes 0; a row that holds an infinity
- * or a NaN has s = NaN and codes 0: what is computed from it is NaN.  Codes are dense rows of convbn_qrow_bytes(K)
- * bytes (K rounded up to 16; the bytes past K are zero, writers leave them so and readers rely on it), scales one fp32 a row.
+ * so that x is about s code (s the next smaller fp32 where 127 s would overflow).  A row with a < 2^-119 (all zeros: padding)
+ * has s = 0 and codes 0; a row that holds an infinity or a NaN has s = NaN and codes 0: what is computed from it is NaN.
+ * Codes are dense rows of convbn_qrow_bytes(K) bytes (K rounded up to 16; the bytes past K are zero, writers leave them so
+ * and readers rely on it), scales one fp32 a row.
  *
  *   forward    z[m,n]  = sx[m] sw[n] sum_k qx[m,k] qw[n,k] + b[n]            (the integer sum is exact)
  *   backward   dx[m,k] = sum_n dz[m,n] sw[n] qw[n,k]     dW[n,k] = sum_m dz[m,n] sx[m] qx[m,k]     db[n] = sum_m dz[m,n]
  * Backward is the gradient of the product of the two rounded operands; the rounding itself passes it on unchanged.  With dtype
- * BF16 the products s q are rounded to bf16 before they meet the bf16 gradients (sums in fp32); with F32 nothing is
- * rounded below fp32.
+ * BF16 the products s q are rounded to bf16, as convbn_qunpack returns them, before they meet the bf16 gradients (sums in fp32);
+ * with F32 nothing is rounded below fp32, as long as no dz s but zero is below 2^-100 and none overflows.
  *
  * Rows may be strided (ldx, ldz); codes, scales, W and vectors are dense.  M == 0 is no error: nothing is read, dW and db
  * become zero.  A sum over the channels is exact up to K = 131072 (longer, or N above 2^20, M above 2^30:
  * CONVBN_ERR_UNSUPPORTED).  codes and workspace are
  * 16-byte aligned; rows of x, z, dx, dz, h, y, dy, dh need the alignment of their element only (16 bytes are faster), except
  * that bf16 gradients dz whose N and ldz are multiples of 8 start on 16 bytes (they are read where they are, others from a copy
- * in the workspace).  Outputs overlap no input, but for the addends below. */
+ * in the workspace).  Outputs overlap no input, but for the addends below.  (convbn_qgate_bwd does not read h: dh may be its memory.) */
 typedef struct {
   int64_t M;                  /* rows of x, z, dx, dz (a gate: of h, y, dy, dh)                                      */
   int64_t ldx, ldz;           /* elements from a row of x / dx (a gate: h / dh) and of z / dz (y / dy) to the next;  */

@@ -11,8 +11,8 @@
 // summed in fp32: nothing is rounded below that.
 //
 // 8192 x 4096 x 4096: dx and dW 227 - 236 us each (1165 - 1210 TFLOP/s, a bf16 product of the library at 8192^3 1325 - 1392).  The matrix pipe is busy for
-// 57 - 59 % of the time; the rest goes to turning codes into bf16 numbers between the multiplies (4.9 vector instructions
-// for each matrix instruction, itself among them; the int8 product has 2.8) and to the waits at a chunk's barrier.  1568 x 2048 x 512: both in one launch of 21.7 us,
+// 58 - 59 % of the time; the rest goes to turning codes into bf16 numbers between the multiplies (4.9 vector instructions
+// for each matrix instruction, itself among them; the int8 product has 3.0) and to the waits at a chunk's barrier.  1568 x 2048 x 512: both in one launch of 21.7 us,
 // bound by the chunks' way from memory, one workgroup a compute unit.
 #include "quant_code.h"
 

@@ -5,7 +5,7 @@
 // channels that are split between workgroups stay whole numbers: any order gives the same.
 //
 // 8192 x 4096 x 8192: 233 - 252 us (2180 - 2355 TOP/s), a little faster than the library's rate at 8192^3 (2036 - 2094).  The matrix pipe is busy for
-// 57 - 59 % of the time: with one workgroup of 256 x 256 a compute unit, what is left is the copies behind each chunk's barrier, the epilogue (134 MB
+// 57 % of the time: with one workgroup of 256 x 256 a compute unit, what is left is the copies behind each chunk's barrier, the epilogue (134 MB
 // out, 26 us at a copy's rate) and the drain of the last round.  Small products (1568 x 2048 x 512: 7 us) are bound by the way to memory:
 // four waves a SIMD, each with few chunks.
 #include "quant_code.h"
