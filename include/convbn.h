@@ -509,6 +509,87 @@ convbn_status convbn_qgate_fwd(const convbn_qdesc *desc, const void *h, void *h_
 convbn_status convbn_qgate_bwd(const convbn_qdesc *desc, const void *h_codes, const float *h_scales,
                                const void *dy, void *dh, void *stream);
 
+/* ---- a head behind the backbone: 8-bit floating point, the gated product, group norm -------------------------
+ *
+ * 8-BIT FLOATING POINT.  The same calls as for the 8-bit rows above with another form of the rows: blocks of 128 channels, each held as
+ * e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest 448) and a power of two,
+ *     a = max |x| of the block,   e = the least whole number with a <= 448 2^e, at least -116,   code = e4m3(x 2^-e), ties to even,
+ * so that a loud channel costs none but its own block's, and what a code stands for, code 2^e, is a bf16 number, whatever the scale.
+ * Nothing overflows: in a block that has e = 120 codes are at most 240.  A block that holds an infinity or a NaN has NaN codes and e = 0.
+ * Codes are dense rows of convbn_qrow_bytes(K) bytes, scales dense rows of convbn_fscale_bytes(K) bytes e + 127, one a block (K
+ * rounded up to whole blocks, their number to a multiple of 4).  Bytes of codes past K are zero, bytes of scales past the last block 127:
+ * writers leave them so and readers rely on it.
+ *
+ *   forward    z[m,n]  = sum_k x8[m,k] w8[n,k] + b[n]                 x8, w8: what the codes stand for; sums in fp32
+ *   backward   dx[m,k] = sum_n dz[m,n] w8[n,k]     dW[n,k] = sum_m dz[m,n] x8[m,k]     db[n] = sum_m dz[m,n]
+ * Backward is the gradient of the product of the two rounded operands; the rounding itself passes it on unchanged.  dz is not rounded: bf16
+ * gradients meet x8 and w8 as they are, fp32 ones in three bf16 parts that add up to them.
+ *
+ * Strides, addends, alignment, limits, empty calls and the meaning of NULL are those of the 8-bit rows; scales are 4-byte aligned. */
+
+/* Bytes from one row of scales to the next (0 for channels < 1). */
+size_t convbn_fscale_bytes(int32_t channels);
+
+convbn_status convbn_fpack(const convbn_qdesc *desc, const void *x, void *codes, void *scales, void *stream);
+convbn_status convbn_funpack(const convbn_qdesc *desc, const void *codes, const void *scales, void *x, void *stream);
+
+size_t convbn_flinear_workspace_bytes(const convbn_qdesc *desc, int pass);
+convbn_status convbn_flinear_fwd(const convbn_qdesc *desc, const void *x, void *codes, void *scales,
+                                  const void *w_codes, const void *w_scales, const float *b,
+                                  void *z, void *ws, size_t ws_bytes, void *stream);
+convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, const void *scales,
+                                  const void *w_codes, const void *w_scales, const void *dz,
+                                  void *dx, void *dW, float *db, void *ws, size_t ws_bytes,
+                                  void *stream);
+
+/* GATED PRODUCT.  Both projections of a gated feed-forward block, the activation and the product in one call:
+ *     g = x Wg^T + bg,   u = x Wu^T + bu,   y = f(g) u        x [M][K] (ldx apart), y [M][N] (ldz apart), f = desc->gate
+ * W = [Wg; Wu]: dense [2 N][K] of dtype, g's rows before u's; b = [bg; bu]: [2 N] fp32, nullable.
+ * h: nullable, dense [M][2 N] of dtype: h = [g | u] as backward reads it.  Without it backward multiplies x and W again (h == NULL there):
+ * N channels are then kept of none, and g and u are not rounded to dtype on the way.
+ *   backward   dg = dy u f'(g),  du = dy f(g),  dh = [dg | du];   dx = dh W (+ add_in),   dW = dh^T x,   db = column sums of dh
+ * dx, dW, db nullable, each = not wanted.  With dtype BF16 sums are in fp32 and dh is rounded to bf16 before the products (db sums it
+ * before that); with F32 operands meet in three bf16 parts that add up to them, and nothing is rounded below fp32.
+ *
+ * Descriptor, strides, limits and empty calls (M == 0) are those of the 8-bit rows; act may be CONVBN_ACT_ADD_IN.  Rows of x, y, dx, dy and h and W
+ * need the alignment of their element, except that bf16 x whose K and ldx are multiples of 8, and bf16 W whose K is, start on 16
+ * bytes (they are read where they are, others from a copy in the workspace).  Outputs overlap no input, but for the addend. */
+size_t convbn_glu_workspace_bytes(const convbn_qdesc *desc, int pass);
+convbn_status convbn_glu_fwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, void *y,
+                             void *h, void *ws, size_t ws_bytes, void *stream);
+convbn_status convbn_glu_bwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, const void *h,
+                             const void *dy, void *dx, void *dW, float *db, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* GROUP NORM with an activation, channels last.  x, y: [M images][P pixels][C], pixels ldx / ldy elements apart.
+ *     xhat = (x - mean) / sqrt(var + eps) over the P C / groups values of a group of neighbouring channels of an image,
+ *     y = f(gamma xhat + beta)
+ * stats: [M][groups][2] fp32, mean and 1 / sqrt(var + eps): nullable in forward, what backward needs beside x.  gamma, beta: [C] fp32, NULL = ones,
+ * zeros.  (P = 1, groups = 1: a norm over each token's channels.)
+ *   backward   dx (+ add_in), dgamma, dbeta: nullable, each = not wanted; beta is read for f' alone.
+ * Sums and statistics are fp32; the variance is summed from differences to a mean.  M == 0 is no error: dgamma and dbeta become zero.  Rows need the
+ * alignment of their element (16 bytes are faster).  y may not be x where backward is to read x. */
+typedef struct {
+  int64_t M, P;               /* images, pixels of an image                                  */
+  int64_t ldx, ldy;           /* elements from a pixel of x / dx (y / dy) to the next; 0 = C */
+  int32_t C, groups;          /* channels, a multiple of groups                              */
+  int32_t dtype;              /* convbn_dtype of x, y, dx, dy                                */
+  int32_t f;                  /* convbn_norm_act                                             */
+  int32_t act;                /* CONVBN_ACT_ADD_IN or 0                                      */
+  float eps;                  /* above 0                                                     */
+  int64_t reserved;           /* 0                                                           */
+  const void *add_in;         /* CONVBN_ACT_ADD_IN: backward returns dx + add_in, laid out like dx (it may be dx) */
+} convbn_norm_desc;
+
+typedef enum { CONVBN_NORM_NONE = 0, CONVBN_NORM_RELU = 1, CONVBN_NORM_SILU = 2, CONVBN_NORM_GELU = 3 } convbn_norm_act;
+
+size_t convbn_norm_workspace_bytes(const convbn_norm_desc *desc, int pass);
+convbn_status convbn_norm_fwd(const convbn_norm_desc *desc, const void *x, const float *gamma, const float *beta,
+                              void *y, float *stats, void *ws, size_t ws_bytes, void *stream);
+convbn_status convbn_norm_bwd(const convbn_norm_desc *desc, const void *x, const float *gamma, const float *beta,
+                              const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta,
+                              void *ws, size_t ws_bytes, void *stream);
+
 /* Bytes a block must keep alive between its forward and its backward call in
  * addition to X (App. K.1): Eval keeps Y (N Cout Hout Wout elements); Tune keeps
  * w' (kH kW Cin Cout elements), or nothing when `refold` is non-zero. */

@@ -36,7 +36,10 @@ EXPORTS = ["convbn_hout", "convbn_wout", "convbn_workspace_bytes", "convbn_saved
            "convbn_tune_fwd_static", "convbn_static_workspace_limit", "convbn_fold_back_group_table_bytes",
            "convbn_fold_back_group_plan", "convbn_fold_back_group", "convbn_tune_bwd_is_fused", "convbn_tune_route",
            "convbn_qrow_bytes", "convbn_qpack", "convbn_qunpack", "convbn_qlinear_workspace_bytes", "convbn_qlinear_fwd",
-           "convbn_qlinear_bwd", "convbn_qgate_fwd", "convbn_qgate_bwd"]
+           "convbn_qlinear_bwd", "convbn_qgate_fwd", "convbn_qgate_bwd",
+           "convbn_fscale_bytes", "convbn_fpack", "convbn_funpack", "convbn_flinear_workspace_bytes", "convbn_flinear_fwd",
+           "convbn_flinear_bwd", "convbn_glu_workspace_bytes", "convbn_glu_fwd", "convbn_glu_bwd",
+           "convbn_norm_workspace_bytes", "convbn_norm_fwd", "convbn_norm_bwd"]
 
 
 class Desc(C.Structure):
@@ -54,6 +57,13 @@ class QDesc(C.Structure):
     _fields_ = [("M", C.c_int64), ("ldx", C.c_int64), ("ldz", C.c_int64), ("K", C.c_int32), ("N", C.c_int32),
                 ("dtype", C.c_int32), ("act", C.c_int32), ("gate", C.c_int32), ("reserved", C.c_int32),
                 ("add_out", C.c_void_p), ("add_in", C.c_void_p)]
+
+
+class NormDesc(C.Structure):
+    """Mirror of convbn_norm_desc."""
+    _fields_ = [("M", C.c_int64), ("P", C.c_int64), ("ldx", C.c_int64), ("ldy", C.c_int64), ("C", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("f", C.c_int32), ("act", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int64),
+                ("add_in", C.c_void_p)]
 
 
 class FoldItem(C.Structure):
@@ -77,7 +87,7 @@ class ConvBNError(RuntimeError):
 
 
 _lib = None
-_call_rows = None
+_call_rows = _call_norm = None
 _call = _at = _NO_WS = None   # the extension's `call`, the entry points' addresses by name, its "no workspace" marker
 _pointer = _stream_handle = None
 
@@ -97,7 +107,7 @@ def _load():
 
 def lib():
     """The loaded library.  Raises if it has not been built (no silent fallback)."""
-    global _lib, _call, _call_rows, _at, _NO_WS, _pointer, _stream_handle
+    global _lib, _call, _call_rows, _call_norm, _at, _NO_WS, _pointer, _stream_handle
     if _lib is None:
         missing = [p for p in (LIB_PATH, CALL_PATH) if not os.path.exists(p)]
         if missing:
@@ -207,17 +217,24 @@ def lib():
         L.convbn_static_workspace_limit.argtypes = []
         L.convbn_qrow_bytes.restype = C.c_size_t
         L.convbn_qrow_bytes.argtypes = [C.c_int32]
-        qp = C.POINTER(QDesc)
-        L.convbn_qlinear_workspace_bytes.restype = C.c_size_t
-        L.convbn_qlinear_workspace_bytes.argtypes = [qp, C.c_int]
-        for name, tensors, ws in (("convbn_qpack", 3, 0), ("convbn_qunpack", 3, 0), ("convbn_qlinear_fwd", 7, 1),
-                                  ("convbn_qlinear_bwd", 8, 1), ("convbn_qgate_fwd", 6, 0), ("convbn_qgate_bwd", 4, 0)):
+        L.convbn_fscale_bytes.restype = C.c_size_t
+        L.convbn_fscale_bytes.argtypes = [C.c_int32]
+        qp, np_ = C.POINTER(QDesc), C.POINTER(NormDesc)
+        for name, d in (("convbn_qlinear_workspace_bytes", qp), ("convbn_flinear_workspace_bytes", qp),
+                        ("convbn_glu_workspace_bytes", qp), ("convbn_norm_workspace_bytes", np_)):
+            getattr(L, name).restype = C.c_size_t
+            getattr(L, name).argtypes = [d, C.c_int]
+        for name, d, tensors, ws in (("convbn_qpack", qp, 3, 0), ("convbn_qunpack", qp, 3, 0), ("convbn_qlinear_fwd", qp, 7, 1),
+                                     ("convbn_qlinear_bwd", qp, 8, 1), ("convbn_qgate_fwd", qp, 6, 0), ("convbn_qgate_bwd", qp, 4, 0),
+                                     ("convbn_fpack", qp, 3, 0), ("convbn_funpack", qp, 3, 0), ("convbn_flinear_fwd", qp, 7, 1),
+                                     ("convbn_flinear_bwd", qp, 8, 1), ("convbn_glu_fwd", qp, 5, 1), ("convbn_glu_bwd", qp, 8, 1),
+                                     ("convbn_norm_fwd", np_, 5, 1), ("convbn_norm_bwd", np_, 8, 1)):
             getattr(L, name).restype = C.c_int
-            getattr(L, name).argtypes = [qp] + [vp] * tensors + [vp, C.c_size_t] * ws + [vp]
+            getattr(L, name).argtypes = [d] + [vp] * tensors + [vp, C.c_size_t] * ws + [vp]
         from . import _call as ext
         # another thread may be in its first call: what a call reads behind `_call` or `_lib` is there before they are
         _at, _NO_WS, _pointer, _stream_handle = _Addresses(L), ext.NO_WS, ext.pointer, ext.stream
-        _call_rows = ext.call_rows
+        _call_rows, _call_norm = ext.call_rows, ext.call_norm
         _call = ext.call
         _lib = L
     return _lib
@@ -704,6 +721,104 @@ def convbn_qgate_fwd(desc, h, h_codes, h_scales, y, y_codes, y_scales, stream=No
 
 def convbn_qgate_bwd(desc, h_codes, h_scales, dy, dh, stream=None, check=True):
     st = (_call_rows or _load_rows())(_at.convbn_qgate_bwd, desc, "etyh", h_codes, h_scales, dy, dh, _NO_WS,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+# ---- 8-bit floating point: the same calls for the other form of the rows ----------
+
+def convbn_fscale_bytes(channels: int) -> int:
+    return lib().convbn_fscale_bytes(channels)
+
+
+def convbn_flinear_workspace_bytes(desc: QDesc, pass_: int) -> int:
+    return lib().convbn_flinear_workspace_bytes(C.byref(desc), pass_)
+
+
+def convbn_fpack(desc, x, codes, scales, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_fpack, desc, "xcf", x, codes, scales, _NO_WS,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+def convbn_funpack(desc, codes, scales, x, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_funpack, desc, "cfx", codes, scales, x, _NO_WS,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+def convbn_flinear_fwd(desc, x, codes, scales, w_codes, w_scales, b, z, ws=None, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_flinear_fwd, desc, "xcfdgnz", x, codes, scales, w_codes, w_scales, b, z, ws,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+def convbn_flinear_bwd(desc, codes, scales, w_codes, w_scales, dz, dx, dW, db, ws=None, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_flinear_bwd, desc, "cfdgzxWn", codes, scales, w_codes, w_scales, dz, dx, dW, db,
+                                      ws, None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+# ---- gated product ------------------------------------------------------------
+
+def convbn_glu_workspace_bytes(desc: QDesc, pass_: int) -> int:
+    return lib().convbn_glu_workspace_bytes(C.byref(desc), pass_)
+
+
+def convbn_glu_fwd(desc, x, W, b, y, h, ws=None, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_glu_fwd, desc, "xVmzk", x, W, b, y, h, ws,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+def convbn_glu_bwd(desc, x, W, b, h, dy, dx, dW, db, ws=None, stream=None, check=True):
+    st = (_call_rows or _load_rows())(_at.convbn_glu_bwd, desc, "xVmkzxVm", x, W, b, h, dy, dx, dW, db, ws,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+# ---- group norm ---------------------------------------------------------------
+
+NORM_NONE, NORM_RELU, NORM_SILU, NORM_GELU = range(4)
+
+
+def make_norm_desc(M, P, channels, groups, dtype=BF16, ldx=0, ldy=0, f=NORM_NONE, eps=1e-5, act=0) -> NormDesc:
+    return NormDesc(M, P, ldx, ldy, channels, groups, dtype, f, act, eps)
+
+
+def convbn_norm_workspace_bytes(desc: NormDesc, pass_: int) -> int:
+    return lib().convbn_norm_workspace_bytes(C.byref(desc), pass_)
+
+
+def _load_norm():
+    lib()
+    return _call_norm
+
+
+def convbn_norm_fwd(desc, x, gamma, beta, y, stats, ws=None, stream=None, check=True):
+    st = (_call_norm or _load_norm())(_at.convbn_norm_fwd, desc, "xvvys", x, gamma, beta, y, stats, ws,
+                                      None if stream is None else _handle(stream))
+    if st and check:
+        _check(st)
+    return st
+
+
+def convbn_norm_bwd(desc, x, gamma, beta, stats, dy, dx, dgamma, dbeta, ws=None, stream=None, check=True):
+    st = (_call_norm or _load_norm())(_at.convbn_norm_bwd, desc, "xvvsyxvv", x, gamma, beta, stats, dy, dx, dgamma, dbeta, ws,
                                       None if stream is None else _handle(stream))
     if st and check:
         _check(st)

@@ -5,14 +5,18 @@
 // 5-7 us a call; here it takes well under one.
 //
 //   call(address, desc, groups, tensors..., ws, stream) -> status
-//   call_rows(address, desc, kinds, tensors..., ws, stream) -> status     (the 8-bit rows: desc is a convbn_qdesc)
+//   call_rows(address, desc, kinds, tensors..., ws, stream) -> status     (8-bit rows, gated product: desc is a convbn_qdesc)
+//   call_norm(address, desc, kinds, tensors..., ws, stream) -> status     (group norm: desc is a convbn_norm_desc)
 //
 // `address` is the entry point's address, `desc` a convbn_desc (any object with the buffer protocol), groups None
 // means that the entry point takes none; a tensor is None, a device tensor or an int (a raw address); ws is None or a
 // device tensor, passed on as pointer and size (NO_WS: the entry point takes none); stream is None (the current
 // stream) or a raw handle.  Tensors are dense.  call_rows checks each against the descriptor, by one letter of `kinds`:
 //   x z h y  rows of desc's type, [M, K] ldx apart, [M, N] ldz, [M, 2 K] ldx, [M, K] ldz;   W  a dense weight [N, K]
-//   c d e    codes of M, N, 2 M rows of K channels;   s n t  fp32 vectors of M, N, 2 M
+//   c d e    codes of M, N, 2 M rows of K channels;   s n t m  fp32 vectors of M, N, 2 M, 2 N
+//   f g      scale bytes of M, N rows of K channels in 8-bit floating point;   V k  dense [2 N, K], [M, 2 N] of desc's type
+// call_norm:
+//   x y      rows of desc's type, [M P, C], ldx or ldy apart;   v  fp32 vectors of C;   s  dense fp32 [M, groups, 2]
 #include <Python.h>
 
 #include <c10/hip/HIPStream.h>
@@ -23,7 +27,8 @@
 
 #include "../../include/convbn.h"
 
-static_assert(sizeof(convbn_desc) != sizeof(convbn_qdesc), "the calls tell the descriptors apart by their size");
+static_assert(sizeof(convbn_desc) != sizeof(convbn_qdesc) && sizeof(convbn_norm_desc) != sizeof(convbn_qdesc) &&
+                  sizeof(convbn_norm_desc) != sizeof(convbn_desc), "the calls tell the descriptors apart by their size");
 
 namespace {
 
@@ -66,36 +71,57 @@ bool pointer_of(PyObject* o, void** out, bool dense = true) {
   return false;
 }
 
-// Whether a tensor is what an entry point of the 8-bit rows reads or writes in its place; false with a Python error set.
-bool fits(PyObject* o, char kind, const convbn_qdesc* d, int at) {
+// What a letter of `kinds` stands for: rows of `width` elements ld apart, or a dense fp32 vector of `rows`.
+struct Spec {
+  int64_t rows = 0, width = 1, ld = 0;
+  bool bytes = false, vector = false;
+};
+Spec spec_of(char kind, const convbn_qdesc* d) {
+  const int64_t M = d->M, K = d->K, N = d->N, Kp = (K + 15) / 16 * 16, Sp = (K + 511) / 512 * 4;
+  switch (kind) {
+    case 'x': return {M, K, d->ldx};
+    case 'z': return {M, N, d->ldz};
+    case 'h': return {M, 2 * K, d->ldx};
+    case 'y': return {M, K, d->ldz};
+    case 'W': return {N, K};
+    case 'V': return {2 * N, K};
+    case 'k': return {M, 2 * N};
+    case 'c': return {M, Kp, 0, true};
+    case 'd': return {N, Kp, 0, true};
+    case 'e': return {2 * M, Kp, 0, true};
+    case 'f': return {M, Sp, 0, true};
+    case 'g': return {N, Sp, 0, true};
+    case 's': return {M, 1, 0, false, true};
+    case 'n': return {N, 1, 0, false, true};
+    case 't': return {2 * M, 1, 0, false, true};
+    case 'm': return {2 * N, 1, 0, false, true};
+  }
+  return {M};
+}
+int64_t times(int64_t a, int64_t b) { return (int64_t)((uint64_t)a * (uint64_t)b); }   // (the library refuses what overflows)
+Spec spec_of(char kind, const convbn_norm_desc* d) {
+  switch (kind) {
+    case 'x': return {times(d->M, d->P), d->C, d->ldx};
+    case 'y': return {times(d->M, d->P), d->C, d->ldy};
+    case 'v': return {d->C, 1, 0, false, true};
+  }
+  return {times(d->M, 2 * (int64_t)d->groups), 1, 0, false, true};
+}
+
+// Whether a tensor is what an entry point reads or writes in its place; false with a Python error set.
+bool fits(PyObject* o, Spec s, int32_t dtype, int at) {
   if (!THPVariable_Check(o)) return true;   // (None and addresses: the library's own checks)
   return guarded([&] {
     const at::Tensor& t = THPVariable_Unpack(o);
-    const int64_t M = d->M, K = d->K, N = d->N, Kp = (K + 15) / 16 * 16;
-    int64_t rows = M, width = 1, ld = 0;
-    bool bytes = false, vector = false;
-    switch (kind) {
-      case 'x': width = K; ld = d->ldx; break;
-      case 'z': width = N; ld = d->ldz; break;
-      case 'h': width = 2 * K; ld = d->ldx; break;
-      case 'y': width = K; ld = d->ldz; break;
-      case 'W': rows = N; width = K; break;
-      case 'c': width = Kp; bytes = true; break;
-      case 'd': rows = N; width = Kp; bytes = true; break;
-      case 'e': rows = 2 * M; width = Kp; bytes = true; break;
-      case 's': vector = true; break;
-      case 'n': rows = N; vector = true; break;
-      case 't': rows = 2 * M; vector = true; break;
-    }
-    if (ld == 0) ld = width;
+    const int64_t rows = s.rows, width = s.width, ld = s.ld ? s.ld : s.width;
     bool ok;
-    if (vector) ok = t.scalar_type() == at::kFloat && t.numel() == rows && t.is_contiguous();
+    if (s.vector) ok = t.scalar_type() == at::kFloat && t.numel() == rows && t.is_contiguous();
     else
-      ok = (bytes ? t.element_size() == 1 : t.scalar_type() == (d->dtype == CONVBN_BF16 ? at::kBFloat16 : at::kFloat)) && t.dim() == 2 &&
+      ok = (s.bytes ? t.element_size() == 1 : t.scalar_type() == (dtype == CONVBN_BF16 ? at::kBFloat16 : at::kFloat)) && t.dim() == 2 &&
            t.size(0) == rows && t.size(1) == width && (rows <= 1 || t.stride(0) == ld) && (width <= 1 || t.stride(1) == 1 || rows == 0);
     if (!ok)
       PyErr_Format(PyExc_ValueError, "tensor %d: expected %s%s [%lld, %lld], rows %lld elements apart", at,
-                   vector ? "float32 vector" : bytes ? "bytes" : d->dtype == CONVBN_BF16 ? "bfloat16" : "float32", vector ? ", as" : "",
+                   s.vector ? "float32 vector" : s.bytes ? "bytes" : dtype == CONVBN_BF16 ? "bfloat16" : "float32", s.vector ? ", as" : "",
                    (long long)rows, (long long)width, (long long)ld);
     return ok;
   });
@@ -122,6 +148,9 @@ int dispatch(void* f, int n, void* const* p, bool* known, const void* d, T... ta
   switch (n) {
     case 3: return invoke(f, d, p[0], p[1], p[2], tail...);
     case 4: return invoke(f, d, P4, tail...);
+    case 5:   // (always with a workspace)
+      if constexpr (sizeof...(tail) == 3) return invoke(f, d, P4, p[4], tail...);
+      break;
     case 6: return invoke(f, d, P4, p[4], p[5], tail...);
     case 7: return invoke(f, d, P4, p[4], p[5], p[6], tail...);
     case 8: return invoke(f, d, P8, tail...);
@@ -156,12 +185,9 @@ struct DescView {
   ~DescView() { if (held) PyBuffer_Release(&b); }
 };
 
-// args: `n` tensors, ws, stream
+// args: `n` tensors (kinds: which of them have been looked at), ws, stream
 PyObject* call_with(void* f, const DescView& d, const char* kinds, bool has_groups, int groups, PyObject* const* args, Py_ssize_t n) {
   void* p[kMaxPtr];
-  if (kinds)
-    for (Py_ssize_t i = 0; i < n; ++i)
-      if (!fits(args[i], kinds[i], static_cast<const convbn_qdesc*>(d.b.buf), (int)i)) return nullptr;
   for (Py_ssize_t i = 0; i < n; ++i)
     if (!pointer_of(args[i], &p[i], !kinds)) return nullptr;
   PyObject* ws_o = args[n];
@@ -203,16 +229,16 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return call_with(f, d, nullptr, has_groups, (int)groups, args + 3, n);
 }
 
-PyObject* call_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+template <class D> PyObject* call_kinds(PyObject* const* args, Py_ssize_t nargs, const char* desc, const char* usage) {
   const Py_ssize_t n = nargs - 5;
   if (n < 1 || n > kMaxPtr) {
-    PyErr_SetString(PyExc_TypeError, "call_rows(address, desc, kinds, tensors..., ws, stream)");
+    PyErr_SetString(PyExc_TypeError, usage);
     return nullptr;
   }
   void* f = PyLong_AsVoidPtr(args[0]);
   if (PyErr_Occurred()) return nullptr;
   DescView d;
-  if (!d.get(args[1], sizeof(convbn_qdesc), "convbn_qdesc")) return nullptr;
+  if (!d.get(args[1], sizeof(D), desc)) return nullptr;
   Py_ssize_t length = 0;
   const char* kinds = PyUnicode_AsUTF8AndSize(args[2], &length);
   if (!kinds) return nullptr;
@@ -220,7 +246,16 @@ PyObject* call_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     PyErr_SetString(PyExc_TypeError, "one kind for each tensor");
     return nullptr;
   }
+  const D* at = static_cast<const D*>(d.b.buf);
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (!fits(args[3 + i], spec_of(kinds[i], at), at->dtype, (int)i)) return nullptr;
   return call_with(f, d, kinds, false, 0, args + 3, n);
+}
+PyObject* call_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return call_kinds<convbn_qdesc>(args, nargs, "convbn_qdesc", "call_rows(address, desc, kinds, tensors..., ws, stream)");
+}
+PyObject* call_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return call_kinds<convbn_norm_desc>(args, nargs, "convbn_norm_desc", "call_norm(address, desc, kinds, tensors..., ws, stream)");
 }
 
 // pointer(tensor) -> address or None, stream(None or handle) -> handle: for the entry points that take no descriptor.
@@ -239,6 +274,7 @@ PyObject* stream(PyObject*, PyObject* o) {
 PyMethodDef methods[] = {
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL, nullptr},
     {"call_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call_rows)), METH_FASTCALL, nullptr},
+    {"call_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call_norm)), METH_FASTCALL, nullptr},
     {"pointer", pointer, METH_O, nullptr},
     {"stream", stream, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,5 +1,5 @@
 """The 8-bit rows for a PyTorch program: an activation kept in 8 bits, a Linear block on integer products that keeps its input
-that way, the gate between two of them, and the gated block that they make up.
+that way, the gate between two of them, and the gated block that they make up; the checkpoint and the Linear block in 8-bit floating point too.
 
 Each object holds the codes, scales, outputs and workspace of one layer, allocated once; its calls enqueue on the current
 stream (or the one they are given) and allocate nothing, but for the first `pack_weight` and the first `unpack` without `out`, whose
@@ -34,10 +34,14 @@ def _vector(t: Optional[torch.Tensor], n: int, name: str):
     return t
 
 
-def _codes(t: torch.Tensor, rows: int, K: int, name: str):
-    if t.element_size() != 1 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != B.convbn_qrow_bytes(K):
-        raise ValueError(f"{name}: expected bytes [{rows}, {B.convbn_qrow_bytes(K)}], got {t.dtype} {list(t.shape)}")
+def _bytes(t: torch.Tensor, rows: int, width: int, name: str):
+    if t.element_size() != 1 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+        raise ValueError(f"{name}: expected bytes [{rows}, {width}], got {t.dtype} {list(t.shape)}")
     return t
+
+
+def _codes(t: torch.Tensor, rows: int, K: int, name: str):
+    return _bytes(t, rows, B.convbn_qrow_bytes(K), name)
 
 
 def _rows(given: Optional[torch.Tensor], M, width, ld, dt, device, name: str):
@@ -63,6 +67,36 @@ def new_codes(rows: int, K: int, device="cuda"):
             torch.empty(rows, dtype=torch.float32, device=device))
 
 
+def new_f8_codes(rows: int, K: int, device="cuda"):
+    """Buffers for `rows` rows of K channels packed in 8-bit floating point: (codes, scales), a byte e + 127 for each block of 128 channels."""
+    return (torch.empty(rows, B.convbn_qrow_bytes(K), dtype=torch.uint8, device=device),
+            torch.empty(rows, B.convbn_fscale_bytes(K), dtype=torch.uint8, device=device))
+
+
+class _IntRows:
+    """Codes from -127 to 127, a scale for each row: the calls that work on them."""
+    new = staticmethod(lambda rows, K, device: new_codes(rows, K, device))
+    pack = staticmethod(lambda *a: B.convbn_qpack(*a))
+    unpack = staticmethod(lambda *a: B.convbn_qunpack(*a))
+    fwd = staticmethod(lambda *a: B.convbn_qlinear_fwd(*a))
+    bwd = staticmethod(lambda *a: B.convbn_qlinear_bwd(*a))
+    workspace_bytes = staticmethod(lambda desc, pass_: B.convbn_qlinear_workspace_bytes(desc, pass_))
+    scales = staticmethod(lambda t, rows, K, name: _vector(t, rows, name))
+    scale_bytes = staticmethod(lambda K: 4)   # of a row
+
+
+class _F8Rows:
+    """e4m3 codes, a power of two for each block of 128 channels of a row."""
+    new = staticmethod(lambda rows, K, device: new_f8_codes(rows, K, device))
+    pack = staticmethod(lambda *a: B.convbn_fpack(*a))
+    unpack = staticmethod(lambda *a: B.convbn_funpack(*a))
+    fwd = staticmethod(lambda *a: B.convbn_flinear_fwd(*a))
+    bwd = staticmethod(lambda *a: B.convbn_flinear_bwd(*a))
+    workspace_bytes = staticmethod(lambda desc, pass_: B.convbn_flinear_workspace_bytes(desc, pass_))
+    scales = staticmethod(lambda t, rows, K, name: _bytes(t, rows, B.convbn_fscale_bytes(K), name))
+    scale_bytes = staticmethod(lambda K: B.convbn_fscale_bytes(K))
+
+
 class Checkpoint:
     """[M, K] rows kept in 8 bits between a block's forward and its backward (a channels-last activation is [pixels,
     channels]): 1 byte a value and 4 a row in place of 2 or 4 a value.
@@ -70,16 +104,18 @@ class Checkpoint:
     out: dense rows that `unpack` writes; without it (and without `unpack(out)`) the checkpoint allocates and holds some of its own, so several
     checkpoints are better given one buffer."""
 
+    _form = _IntRows
+
     def __init__(self, M: int, K: int, dtype=torch.bfloat16, device="cuda", out: Optional[torch.Tensor] = None):
         self.M, self.K, self.dtype = M, K, dtype
         self.desc = B.make_qdesc(M, K, dtype=_dtype(dtype))
-        self.codes, self.scales = new_codes(M, K, device)
+        self.codes, self.scales = self._form.new(M, K, device)
         self.out = None if out is None else _rows(out, M, K, K, dtype, device, "out")
 
     def pack(self, x: torch.Tensor, stream=None):
         """The rows of x may be strided."""
         self.desc.ldx = x.stride(0) if self.M > 1 else self.K
-        B.convbn_qpack(self.desc, x, self.codes, self.scales, stream)
+        self._form.pack(self.desc, x, self.codes, self.scales, stream)
 
     def unpack(self, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         if out is None:
@@ -88,18 +124,30 @@ class Checkpoint:
                     self.out = torch.empty(self.M, self.K, dtype=self.dtype, device=self.codes.device)
             out = self.out
         self.desc.ldx = out.stride(0) if self.M > 1 else self.K
-        B.convbn_qunpack(self.desc, self.codes, self.scales, out, stream)
+        self._form.unpack(self.desc, self.codes, self.scales, out, stream)
         return out
 
     def saved_bytes(self) -> int:
         """Codes and scales."""
-        return self.codes.numel() + 4 * self.M
+        return self.codes.nbytes + self.scales.nbytes
 
 
-def linear_workspace_bytes(M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0) -> int:
+class F8Checkpoint(Checkpoint):
+    """The same in 8-bit floating point: e4m3 codes with a power of two for each block of 128 channels, so that a loud channel costs none but its
+    block's neighbours their bits."""
+
+    _form = _F8Rows
+
+
+def linear_workspace_bytes(M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0, form=_IntRows) -> int:
     """What `Linear` of these sizes needs as its `ws`."""
     d = B.make_qdesc(M, K, N, _dtype(dtype), K + gap, N + gap)
-    return max(B.convbn_qlinear_workspace_bytes(d, p) for p in ((B.PASS_FWD, B.PASS_BWD) if train else (B.PASS_FWD,)))
+    return max(form.workspace_bytes(d, p) for p in ((B.PASS_FWD, B.PASS_BWD) if train else (B.PASS_FWD,)))
+
+
+def f8_linear_workspace_bytes(M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0) -> int:
+    """What `F8Linear` of these sizes needs as its `ws`."""
+    return linear_workspace_bytes(M, K, N, dtype, train, gap, _F8Rows)
 
 
 class Linear:
@@ -111,6 +159,8 @@ class Linear:
     need_dx, need_dW: gradients that are ever asked for; there are buffers for these alone.
     z, dx: rows that the layer writes, ws: bytes that it works in (`linear_workspace_bytes`), where several layers share them."""
 
+    _form = _IntRows
+
     def __init__(self, M: int, K: int, N: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0, device="cuda",
                  packed: bool = False, need_dx: bool = True, need_dW: bool = True, z: Optional[torch.Tensor] = None,
                  dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
@@ -119,7 +169,7 @@ class Linear:
         self.desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)
         self._add_desc = B.make_qdesc(M, K, N, _dtype(dtype), self.ldx, self.ldz)   # (with an addend)
         self.packed = packed
-        self.codes, self.scales = new_codes(M, K, device) if train and not packed else (None, None)   # what forward packs into
+        self.codes, self.scales = self._form.new(M, K, device) if train and not packed else (None, None)   # what forward packs into
         self._kept = None, None   # what backward reads: these, or those that forward_packed was given
         self.w_codes = self.w_scales = None   # the weight in use
         self._own_weight = None               # what pack_weight packs into
@@ -128,21 +178,21 @@ class Linear:
         self.dx = _rows(dx, M, K, self.ldx, dtype, device, "dx") if train and need_dx else None
         self.dW = torch.empty(N, K, dtype=dtype, device=device) if train and need_dW else None
         self.db = torch.empty(N, dtype=torch.float32, device=device) if train else None
-        need = linear_workspace_bytes(M, K, N, dtype, train, gap)
+        need = linear_workspace_bytes(M, K, N, dtype, train, gap, self._form)
         if ws is not None and ws.nbytes < need:
             raise ValueError(f"ws: {ws.nbytes} bytes, {need} needed")
         self.ws = ws if ws is not None else torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
     def set_weight(self, codes: torch.Tensor, scales: torch.Tensor):
         """A weight that is packed already (`new_codes(N, K)`, `convbn_qpack`): read where it is, never written."""
-        self.w_codes, self.w_scales = _codes(codes, self.N, self.K, "codes"), _vector(scales, self.N, "scales")
+        self.w_codes, self.w_scales = _codes(codes, self.N, self.K, "codes"), self._form.scales(scales, self.N, self.K, "scales")
 
     def pack_weight(self, W: torch.Tensor, stream=None):
         """Pack W [N, K] by output channel, into buffers of the layer's own."""
         if self._own_weight is None:
             with _allocating_for(stream):
-                self._own_weight = new_codes(self.N, self.K, W.device)
-        B.convbn_qpack(self._w_desc, W, *self._own_weight, stream)
+                self._own_weight = self._form.new(self.N, self.K, W.device)
+        self._form.pack(self._w_desc, W, *self._own_weight, stream)
         self.w_codes, self.w_scales = self._own_weight
 
     def _desc_with(self, bit: int, field: str, add, width: int, ld: int):
@@ -168,7 +218,7 @@ class Linear:
         if x is None:
             raise ValueError("x: expected rows")
         d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
-        B.convbn_qlinear_fwd(d, x, self.codes, self.scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
+        self._form.fwd(d, x, self.codes, self.scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         self._kept = self.codes, self.scales
         return self.z
 
@@ -179,7 +229,7 @@ class Linear:
         if codes is None or scales is None:
             raise ValueError("codes, scales: expected packed rows")
         d = self._desc_with(B.ACT_ADD_OUT, "add_out", add, self.N, self.ldz)
-        B.convbn_qlinear_fwd(d, None, codes, scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
+        self._form.fwd(d, None, codes, scales, self.w_codes, self.w_scales, b, self.z, self.ws, stream)
         if self.train:
             self._kept = codes, scales
         return self.z
@@ -196,12 +246,20 @@ class Linear:
             raise RuntimeError("this layer was made without that gradient (need_dx, need_dW)")
         d = self._desc_with(B.ACT_ADD_IN, "add_in", add, self.K, self.ldx)
         dx, dW, db = self.dx if need_dx else None, self.dW if need_dW else None, self.db if bias else None
-        B.convbn_qlinear_bwd(d, *self._kept, self.w_codes, self.w_scales, dz, dx, dW, db, self.ws, stream)
+        self._form.bwd(d, *self._kept, self.w_codes, self.w_scales, dz, dx, dW, db, self.ws, stream)
         return dx, dW, db
 
     def saved_bytes(self) -> int:
         """Codes and scales: what backward needs of the forward pass."""
-        return self.M * (B.convbn_qrow_bytes(self.K) + 4) if self.train else 0
+        return self.M * (B.convbn_qrow_bytes(self.K) + self._form.scale_bytes(self.K)) if self.train else 0
+
+
+class F8Linear(Linear):
+    """The same block in 8-bit floating point: x and w as e4m3 codes with a power of two for each block of 128 channels of a row
+    (`new_f8_codes`, `convbn_fpack`; `f8_linear_workspace_bytes`), multiplied as they are held, sums in fp32.  `backward` meets unrounded
+    gradients with the values that the codes stand for, which are bf16 numbers whatever their scale."""
+
+    _form = _F8Rows
 
 
 class Gate:
