@@ -520,10 +520,12 @@ convbn_status convbn_qgate_bwd(const convbn_qdesc *desc, const void *h_codes, co
  * rounded up to whole blocks, their number to a multiple of 4).  Bytes of codes past K are zero, bytes of scales past the last block 127:
  * writers leave them so and readers rely on it.
  *
- *   forward    z[m,n]  = sum_k x8[m,k] w8[n,k] + b[n]                 x8, w8: what the codes stand for; sums in fp32
+ *   forward    z[m,n]  = sum_k x8[m,k] w8[n,k] + b[n]                 x8, w8: what the codes stand for
  *   backward   dx[m,k] = sum_n dz[m,n] w8[n,k]     dW[n,k] = sum_m dz[m,n] x8[m,k]     db[n] = sum_m dz[m,n]
  * Backward is the gradient of the product of the two rounded operands; the rounding itself passes it on unchanged.  dz is not rounded: bf16
- * gradients meet x8 and w8 as they are, fp32 ones in three bf16 parts that add up to them.
+ * gradients meet x8 and w8 as they are, fp32 ones in three bf16 parts that add up to them.  Sums are fp32, with one exception: forward with
+ * dtype BF16 and more than 32 rows adds the eight products of neighbouring channels 8 i .. 8 i + 7 with 13 bits below the leading bit of the
+ * largest (the matrix instruction for these codes; what it drops is below 7 2^-13 of that product, and 2^-15 of the sum of all sizes on average).
  *
  * Strides, addends, alignment, limits, empty calls and the meaning of NULL are those of the 8-bit rows; scales are 4-byte aligned. */
 
@@ -545,8 +547,8 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, co
 /* GATED PRODUCT.  Both projections of a gated feed-forward block, the activation and the product in one call:
  *     g = x Wg^T + bg,   u = x Wu^T + bu,   y = f(g) u        x [M][K] (ldx apart), y [M][N] (ldz apart), f = desc->gate
  * W = [Wg; Wu]: dense [2 N][K] of dtype, g's rows before u's; b = [bg; bu]: [2 N] fp32, nullable.
- * h: nullable, dense [M][2 N] of dtype: h = [g | u] as backward reads it.  Without it backward multiplies x and W again (h == NULL there):
- * N channels are then kept of none, and g and u are not rounded to dtype on the way.
+ * h: nullable, dense [M][2 N]: h = [g | u] as backward reads it, of dtype without b and fp32 with it (db adds up over the rows what is lost in
+ * rounding h).  Without h backward multiplies x and W again, and 2 N numbers a row need not be kept.
  *   backward   dg = dy u f'(g),  du = dy f(g),  dh = [dg | du];   dx = dh W (+ add_in),   dW = dh^T x,   db = column sums of dh
  * dx, dW, db nullable, each = not wanted.  With dtype BF16 sums are in fp32 and dh is rounded to bf16 before the products (db sums it
  * before that); with F32 operands meet in three bf16 parts that add up to them, and nothing is rounded below fp32.

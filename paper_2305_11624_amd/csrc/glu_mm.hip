@@ -1,0 +1,241 @@
+// The gated product y = f(x Wg^T + bg) (x Wu^T + bu) and its gradients.
+//
+// Forward is one product: a tile takes 32 rows of Wg and the same 32 of Wu in turn, so that a wave holds g and u of the same numbers of y when
+// the sum is done, and neither goes to memory unless it is kept.  Backward turns g, u and dy into dh = [dg | du] in one pass, which sums dh's columns too,
+// and multiplies it with W and with x as they lie.
+//
+// F32: operands are split into three bf16 parts that add up to all 24 bits, and the six products of parts that are not below 2^-24 of the whole are summed
+// in fp32: nothing is rounded below that.
+#include "mm_tile.h"
+#include "rows_prep.h"
+
+namespace convbn {
+
+namespace {
+
+int planes_of(int dtype) { return dtype == CONVBN_BF16 ? 1 : 3; }
+
+// ---- forward ----
+template <typename T, int KIND> struct GluOut {
+  Glu q;
+  struct Cols { F8 g, u; };
+  __device__ __forceinline__ Cols columns(int n) const {
+    return q.b ? Cols{load8<float>(q.b, n, q.N), load8<float>(q.b + q.N, n, q.N)} : Cols{};
+  }
+  __device__ __forceinline__ void operator()(i64 m, int n, const Cols& b, F8 g, F8 u) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      g.v[i] += b.g.v[i];
+      u.v[i] += b.u.v[i];
+    }
+    if (q.h) {
+      if (q.h32) {
+        float* h = static_cast<float*>(q.h) + m * 2 * q.N;
+        store8<float, true>(h, n, q.N, g);
+        store8<float, true>(h + q.N, n, q.N, u);
+      } else {
+        T* h = static_cast<T*>(q.h) + m * 2 * q.N;
+        store8<T, true>(h, n, q.N, g);
+        store8<T, true>(h + q.N, n, q.N, u);
+      }
+    }
+    if (q.y) {
+      F8 y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float f, df;
+        gate_of<T, KIND>(g.v[i], &f, &df);
+        y.v[i] = f * u.v[i];
+      }
+      store8<T, true>(static_cast<T*>(q.y) + m * q.ldz, n, q.N, y);
+    }
+  }
+};
+
+// ---- dh and its column sums ----
+// A workgroup takes 256 columns of either half, a thread eight of them and every 16th row of a slice; the sums of several slices are joined in
+// order by a later launch.
+struct DGate {
+  i64 M, ldz, per;
+  int N, W2;
+  const void* h; const void* dy;
+  bf16_t* dh; i64 plane;      // null: not wanted
+  float* sums;                // [slices][2 N] or null
+};
+template <typename T, typename H, int KIND> __global__ __launch_bounds__(32 * SUM_ROWS) void glu_dgate_kernel(DGate p) {
+  __shared__ float meet[SUM_ROWS][256 + 8];
+  const int c = (threadIdx.x & 31) * 8, r = threadIdx.x >> 5, n = blockIdx.x * 256 + c;
+  const i64 beg = (i64)blockIdx.y * p.per, end = beg + p.per < p.M ? beg + p.per : p.M;
+  F8 sum[2] = {};
+  if (n < p.N) {
+#pragma unroll 2
+    for (i64 m = beg + r; m < end; m += SUM_ROWS) {
+      const H* h = static_cast<const H*>(p.h) + m * 2 * p.N;
+      const F8 g = load8<H>(h, n, p.N), u = load8<H>(h + p.N, n, p.N), dy = load8<T>(static_cast<const T*>(p.dy) + m * p.ldz, n, p.N);
+      F8 d[2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float f, df;
+        gate_of<T, KIND>(g.v[i], &f, &df);
+        d[0].v[i] = dy.v[i] * u.v[i] * df;
+        d[1].v[i] = dy.v[i] * f;
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[x].v[i] += d[x].v[i];
+        if (!p.dh) continue;
+        bf16_t* out = p.dh + m * p.W2 + x * p.N;
+        const int width = x ? p.W2 - p.N : p.N;   // (u's last piece clears what is behind it)
+        if constexpr (sizeof(T) == 2) {
+          store8<bf16_t>(out, n, width, d[x]);
+        } else {
+          F8 part[3];
+          split3(d[x], part);
+#pragma unroll
+          for (int y = 0; y < 3; ++y) store8<bf16_t>(out + y * p.plane, n, width, part[y]);
+        }
+      }
+    }
+  }
+  if (!p.sums) return;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) meet[r][c + e] = sum[x].v[e];
+    __syncthreads();
+    const int at = threadIdx.x, col = blockIdx.x * 256 + at;
+    if (at < 256 && col < p.N) {
+      float v = 0.f;
+#pragma unroll
+      for (int i = 0; i < SUM_ROWS; ++i) v += meet[i][at];
+      p.sums[(i64)blockIdx.y * 2 * p.N + x * p.N + col] = v;
+    }
+  }
+}
+// ---- gradients ----
+// What a call needs of the workspace, in this order, and its operands
+struct Plan {
+  MmPlan fwd, dx, dw;
+  int slices;
+  size_t h, dh, x, W, part, sums, total;
+};
+Plan plan_of(const Glu& p, bool bwd) {
+  Plan s = {};
+  const int pl = planes_of(p.dtype), pairs = pl == 1 ? 1 : 6, K8 = round8(p.K), W2 = round8(2 * p.N);
+  s.fwd = mm_plan(p.M, 2 * (i64)p.N, pairs * chunks(K8));
+  s.x = glu_in_place(p.dtype, p.K, p.ldx) ? 0 : align_up((size_t)pl * p.M * K8 * 2, 256);
+  s.W = glu_in_place(p.dtype, p.K, p.K) ? 0 : align_up((size_t)pl * 2 * p.N * K8 * 2, 256);
+  s.part = mm_scratch(s.fwd, p.M, 2 * round8(p.N));
+  if (bwd) {
+    s.dx = mm_plan(p.M, p.K, pairs * chunks(2 * (i64)p.N));
+    s.dw = mm_plan(2 * (i64)p.N, p.K, pairs * chunks(p.M));
+    s.slices = row_slices(p.M, p.N);
+    s.h = align_up((size_t)p.M * 2 * p.N * 4, 256);   // (a descriptor does not say whether h is kept)
+    s.dh = align_up((size_t)pl * p.M * W2 * 2, 256);
+    const size_t both = mm_scratch(s.dx, p.M, K8) + mm_scratch(s.dw, 2 * (i64)p.N, K8);
+    s.part = s.part > both ? s.part : both;
+    s.sums = align_up((size_t)s.slices * 2 * p.N * 4, 256);
+  }
+  s.total = s.h + s.dh + s.x + s.W + s.part + s.sums;
+  return s;
+}
+
+// x and W as the products read them, after launch_rows_copies
+struct Operands { RowsOp x, W; RowsCopy cx, cw; };
+Operands operands_of(const Glu& p, const Plan& s, char* ws, bool want_x, bool want_W) {
+  Operands o = {};
+  const int K8 = round8(p.K);
+  bf16_t* const x = reinterpret_cast<bf16_t*>(ws + s.h + s.dh);
+  bf16_t* const W = reinterpret_cast<bf16_t*>(ws + s.h + s.dh + s.x);
+  if (s.x && want_x) o.cx = {p.M, p.ldx, p.K, p.x, x};
+  if (s.W && want_W) o.cw = {2 * (i64)p.N, p.K, p.K, p.W, W};
+  o.x = s.x ? RowsOp{(const uint8_t*)x, 2 * K8, 2 * p.M * K8, 2 * K8} : RowsOp{(const uint8_t*)p.x, 2 * p.ldx, 0, 2 * K8};
+  o.W = s.W ? RowsOp{(const uint8_t*)W, 2 * K8, 4 * (i64)p.N * K8, 2 * K8} : RowsOp{(const uint8_t*)p.W, 2 * K8, 0, 2 * K8};
+  return o;
+}
+
+template <typename T, int KIND> hipError_t project(const Glu& p, const Plan& s, const Operands& o, char* ws, hipStream_t st) {
+  constexpr int PAIRS = sizeof(T) == 2 ? 1 : 6;
+  MmParams m = {};
+  m.a = o.x; m.b = o.W;
+  m.I = p.M; m.J = p.N;
+  m.plane_ch = chunks(round8(p.K));
+  m.nch = PAIRS * m.plane_ch;
+  return mm_launch<OpBf16, false, false, true, PAIRS>(m, s.fwd, reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W), GluOut<T, KIND>{p}, st);
+}
+
+template <typename T, int KIND> hipError_t fwd_t(const Glu& p, char* ws, hipStream_t st) {
+  const Plan s = plan_of(p, false);
+  const Operands o = operands_of(p, s, ws, true, true);
+  const hipError_t e = launch_rows_copies(p.dtype, o.cx, o.cw, st);
+  return e == hipSuccess ? project<T, KIND>(p, s, o, ws, st) : e;
+}
+
+template <typename T, int KIND> hipError_t bwd_t(const Glu& p, char* ws, hipStream_t st) {
+  constexpr int PAIRS = sizeof(T) == 2 ? 1 : 6;
+  const Plan s = plan_of(p, true);
+  const bool again = !p.hk && p.M, want_dx = p.dx && p.M;
+  const Operands o = operands_of(p, s, ws, p.M && (again || p.dW), again || want_dx);
+  hipError_t e = launch_rows_copies(p.dtype, o.cx, o.cw, st);
+  if (e != hipSuccess) return e;
+  const void* h = p.hk;
+  if (again) {
+    Glu q = p;
+    q.y = nullptr;
+    q.h = ws;
+    q.h32 = true;
+    e = project<T, KIND>(q, s, o, ws, st);
+    if (e != hipSuccess) return e;
+    h = ws;
+  }
+  float* const part = reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W);
+  float* const sums = reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W + s.part);
+  const int W2 = round8(2 * p.N);
+  bf16_t* const dh = reinterpret_cast<bf16_t*>(ws + s.h);
+  DGate d = {p.M, p.ldz, (p.M + s.slices - 1) / s.slices, p.N, W2, h, p.dy, want_dx || p.dW ? dh : nullptr, p.M * W2,
+             !p.db ? nullptr : s.slices > 1 ? sums : p.db};
+  const dim3 grid(ceil_div(p.N, 256), s.slices);
+  if (p.b || again) glu_dgate_kernel<T, float, KIND><<<grid, 32 * SUM_ROWS, 0, st>>>(d);
+  else glu_dgate_kernel<T, T, KIND><<<grid, 32 * SUM_ROWS, 0, st>>>(d);
+  e = hipGetLastError();
+  if (e == hipSuccess && p.db && s.slices > 1) e = launch_sums(sums, s.slices, 2 * p.N, p.db, st);
+  const RowsOp rows = {(const uint8_t*)dh, 2 * W2, 2 * p.M * W2, 2 * W2};
+  if (e == hipSuccess && want_dx) {
+    MmParams m = {};
+    m.a = rows; m.b = o.W;
+    m.I = p.M; m.J = p.K; m.R = 2 * (i64)p.N;
+    m.plane_ch = chunks(m.R);
+    m.nch = PAIRS * m.plane_ch;
+    e = mm_launch<OpBf16, false, true, false, PAIRS>(m, s.dx, part, GradOut<T>{p.dx, p.add, p.ldx, p.K}, st);
+  }
+  if (e == hipSuccess && p.dW) {
+    MmParams m = {};
+    m.a = rows; m.b = o.x;
+    m.I = 2 * (i64)p.N; m.J = p.K; m.R = p.M;
+    m.plane_ch = chunks(p.M);
+    m.nch = PAIRS * m.plane_ch;
+    e = mm_launch<OpBf16, true, true, false, PAIRS>(m, s.dw, part + mm_scratch(s.dx, p.M, round8(p.K)) / 4, GradOut<T>{p.dW, nullptr, p.K, p.K}, st);
+  }
+  return e;
+}
+
+// Calls f(T, KIND) with the gate's types
+template <class F> hipError_t by_gate(const Glu& p, F&& f) {
+  auto with = [&](auto t) { return p.gate == CONVBN_GATE_SILU ? f(t, std::integral_constant<int, 0>{}) : f(t, std::integral_constant<int, 1>{}); };
+  return p.dtype == CONVBN_BF16 ? with(bf16_t{}) : with(float{});
+}
+
+}  // namespace
+
+bool glu_in_place(int dtype, int K, i64 ld) { return dtype == CONVBN_BF16 && K % 8 == 0 && ld % 8 == 0 && ld <= 1 << 20; }
+size_t glu_scratch(const Glu& p, int pass) { return plan_of(p, pass == CONVBN_PASS_BWD).total; }
+hipError_t launch_glu_fwd(const Glu& p, void* ws, hipStream_t st) {
+  return by_gate(p, [&](auto t, auto k) { return fwd_t<decltype(t), k.value>(p, static_cast<char*>(ws), st); });
+}
+hipError_t launch_glu_bwd(const Glu& p, void* ws, hipStream_t st) {
+  return by_gate(p, [&](auto t, auto k) { return bwd_t<decltype(t), k.value>(p, static_cast<char*>(ws), st); });
+}
+
+}  // namespace convbn

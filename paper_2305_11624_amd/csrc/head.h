@@ -35,7 +35,7 @@ struct Glu {
   i64 M, ldx, ldz;
   int K, N, dtype, gate;
   const void* x; const void* W; const float* b;
-  void* y; void* h;                                   // forward
+  void* y; void* h; bool h32;                         // forward (h32: h is fp32)
   const void* hk; const void* dy; const void* add;    // backward (hk: the kept h, or null)
   void* dx; void* dW; float* db;
 };

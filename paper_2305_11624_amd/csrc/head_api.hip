@@ -146,7 +146,7 @@ convbn_status convbn_glu_fwd(const convbn_qdesc* desc, const void* x, const void
   OPTIONAL(b, 4); REQUIRE_ROWS(y, elem(desc)); OPTIONAL(h, elem(desc));
   if (!desc->M) return CONVBN_OK;
   TRY_STATUS(check_ws(glu_scratch(g, CONVBN_PASS_FWD), ws, ws_bytes));
-  g.x = x; g.W = W; g.b = b; g.y = y; g.h = h;
+  g.x = x; g.W = W; g.b = b; g.y = y; g.h = h; g.h32 = b != nullptr;
   LAUNCH(launch_glu_fwd(g, ws, (hipStream_t)stream));
   return CONVBN_OK;
 }

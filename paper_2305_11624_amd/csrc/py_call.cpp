@@ -14,7 +14,7 @@
 // stream) or a raw handle.  Tensors are dense.  call_rows checks each against the descriptor, by one letter of `kinds`:
 //   x z h y  rows of desc's type, [M, K] ldx apart, [M, N] ldz, [M, 2 K] ldx, [M, K] ldz;   W  a dense weight [N, K]
 //   c d e    codes of M, N, 2 M rows of K channels;   s n t m  fp32 vectors of M, N, 2 M, 2 N
-//   f g      scale bytes of M, N rows of K channels in 8-bit floating point;   V k  dense [2 N, K], [M, 2 N] of desc's type
+//   f g      scale bytes of M, N rows of K channels in 8-bit floating point;   V k  dense [2 N, K], [M, 2 N] of desc's type;   l  dense fp32 [M, 2 N]
 // call_norm:
 //   x y      rows of desc's type, [M P, C], ldx or ldy apart;   v  fp32 vectors of C;   s  dense fp32 [M, groups, 2]
 #include <Python.h>
@@ -76,6 +76,7 @@ struct Spec {
   int64_t rows = 0, width = 1, ld = 0;
   bool bytes = false, vector = false;
 };
+int64_t times(int64_t a, int64_t b) { return (int64_t)((uint64_t)a * (uint64_t)b); }   // (the library refuses what overflows)
 Spec spec_of(char kind, const convbn_qdesc* d) {
   const int64_t M = d->M, K = d->K, N = d->N, Kp = (K + 15) / 16 * 16, Sp = (K + 511) / 512 * 4;
   switch (kind) {
@@ -86,6 +87,7 @@ Spec spec_of(char kind, const convbn_qdesc* d) {
     case 'W': return {N, K};
     case 'V': return {2 * N, K};
     case 'k': return {M, 2 * N};
+    case 'l': return {times(M, 2 * N), 1, 0, false, true};
     case 'c': return {M, Kp, 0, true};
     case 'd': return {N, Kp, 0, true};
     case 'e': return {2 * M, Kp, 0, true};
@@ -98,7 +100,6 @@ Spec spec_of(char kind, const convbn_qdesc* d) {
   }
   return {M};
 }
-int64_t times(int64_t a, int64_t b) { return (int64_t)((uint64_t)a * (uint64_t)b); }   // (the library refuses what overflows)
 Spec spec_of(char kind, const convbn_norm_desc* d) {
   switch (kind) {
     case 'x': return {times(d->M, d->P), d->C, d->ldx};

@@ -163,4 +163,33 @@ template <typename T, int KIND> __device__ __forceinline__ void gate_of(float g,
   }
 }
 
+// ---- bf16 operands whose rows lie across the reduced index: LDS, transposing loads, fp32 numbers in parts ----
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// 64-byte pieces of a row of W channels in LDS are exchanged by the row's low bits, so that the pieces of four rows that half a wave reads
+// with the transposing load lie on distinct banks
+template <int W> __device__ __forceinline__ int turn(int r) { return W >= 128 ? r & 3 : (r >> 1) & 1; }
+
+__device__ __forceinline__ bf16x8 read_tr8(const unsigned char* p, int rows4) {   // 8 rows of this lane's column; rows4: bytes of 4 rows
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + rows4));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(bf16x8, (s16x8){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+}
+
+// v in three parts of 8 bits each, which add up to it; infinities and NaN are the first whole
+__device__ __forceinline__ void split3(const F8& f, F8 (&part)[3]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float v = f.v[e];
+    const bool whole = (__float_as_uint(v) & INF) == INF;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {   // the 8 leading bits, what is left of it, and the rest of that: each exact
+      const float t = whole ? (i ? 0.f : v) : __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+      part[i].v[e] = t;
+      v -= t;
+    }
+  }
+}
+
 }  // namespace convbn

@@ -136,7 +136,7 @@ def gated(x, W, b, kind, dtype, dy=None, kept=True, add=None):
     out = dict(y=(y, ey + hs * (np.abs(y) + ey)))
     if dy is None:
         return out
-    if kept and dtype == "bf16":
+    if kept and dtype == "bf16" and b is None:      # (with b, h is kept in fp32)
         dg, du = dg + hs * (np.abs(g) + dg), du + hs * (np.abs(u) + du)
         slope = np.abs(df) + ddf * dg
         rf, rdf = act_error(kind, dtype, np.abs(g) + dg)
