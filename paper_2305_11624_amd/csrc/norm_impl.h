@@ -25,6 +25,7 @@ struct NormParams {
   Norm n;
   Team t;
   int cg, bundles;      // channels of a group, teams side by side
+  unsigned per_bundle, per_slice;   // ceil(2^32 / bundles), ceil(2^32 / slices): exact for the small numbers here; 0: divide by one
   int span, sections;   // a group of more channels than a workgroup has lanes for: sections of `span` channels, a team each
   int slices;           // workgroups along the images (each takes every slices'th team of images)
   int segs;             // segments of the pixels
@@ -35,39 +36,76 @@ struct NormParams {
 
 template <typename T, int F> __device__ __forceinline__ void act_of(float z, float* f, float* df) {
   if constexpr (F == CONVBN_NORM_NONE) { *f = z; *df = 1.f; }
-  else if constexpr (F == CONVBN_NORM_RELU) { *f = z > 0.f ? z : 0.f * z; *df = z > 0.f ? 1.f : 0.f; }
+  else if constexpr (F == CONVBN_NORM_RELU) { *f = z < 0.f ? 0.f : z; *df = z > 0.f ? 1.f : 0.f; }   // (NaN stays)
   else gate_of<T, F == CONVBN_NORM_SILU ? CONVBN_GATE_SILU : CONVBN_GATE_GELU>(z, f, df);
 }
 
-// A piece of n channels (1 to 8; zeros past them).  FULL: all pieces are whole
-template <bool FULL, typename T> __device__ __forceinline__ Raw8<T> load_piece(const T* p, int n) {
-  if (FULL || n == 8) return *reinterpret_cast<const Raw8<T>*>(p);
-  F8 f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f.v[i] = i < n ? to_f32(p[i]) : 0.f;
-  return narrow<T>(f);
-}
-template <bool FULL, typename T> __device__ __forceinline__ void store_piece(T* p, int n, const F8& f) {
-  if (FULL || n == 8) {
-    *reinterpret_cast<Raw8<T>*>(p) = narrow<T>(f);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) p[i] = from_f32<T>(f.v[i]);
-}
+// Pieces of a group's channels: whole ones of eight (EIGHTS), of eight with a shorter last one (TAIL: groups of other sizes, of some length), or single
+// channels (ONES: short groups of other sizes).  n: channels of this one.
+enum { EIGHTS, TAIL, ONES };
+template <int V> constexpr int width_of = V == ONES ? 1 : 8;
+template <typename T, int V> struct Held { Raw8<T> r; };
+template <typename T> struct Held<T, ONES> { float r; };
+template <int N> struct Vals { float v[N]; };
 
+template <typename T, int V> __device__ __forceinline__ Held<T, V> load_piece(const T* p, int n) {
+  Held<T, V> h;
+  if constexpr (V == ONES) {
+    h.r = to_f32(*p);
+  } else if (V == EIGHTS || n == 8) {
+    h.r = *reinterpret_cast<const Raw8<T>*>(p);
+  } else {
+    F8 f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.v[i] = i < n ? to_f32(p[i]) : 0.f;
+    h.r = narrow<T>(f);
+  }
+  return h;
+}
+template <typename T, int V> __device__ __forceinline__ Vals<width_of<V>> vals(const Held<T, V>& h) {
+  if constexpr (V == ONES) {
+    return {{h.r}};
+  } else {
+    const F8 f = widen(h.r);
+    return {{f.v[0], f.v[1], f.v[2], f.v[3], f.v[4], f.v[5], f.v[6], f.v[7]}};
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void store_piece(T* p, int n, const Vals<width_of<V>>& f) {
+  if constexpr (V == ONES) {
+    *p = from_f32<T>(f.v[0]);
+  } else {
+    if (V == EIGHTS || n == 8) {
+      *reinterpret_cast<Raw8<T>*>(p) = narrow<T>(F8{{f.v[0], f.v[1], f.v[2], f.v[3], f.v[4], f.v[5], f.v[6], f.v[7]}});
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = from_f32<T>(f.v[i]);
+  }
+}
 // From here on the pieces are what is in their registers: else the compiler keeps them as the eight fp32 numbers that an earlier pass made of
 // each, which take twice the room (512 lanes of 32 pieces: 142 registers to memory)
-template <typename T, int KP> __device__ __forceinline__ void as_held(Raw8<T> (&x)[KP]) {
-  if constexpr (sizeof(T) == 2) {
+template <typename T, int V, int KP> __device__ __forceinline__ void as_held(Held<T, V> (&x)[KP]) {
+  if constexpr (sizeof(T) == 2 && V != ONES) {
 #pragma unroll
     for (int k = 0; k < KP; ++k) {
-      u32x4 a = x[k].a;
+      u32x4 a = x[k].r.a;
       asm volatile("" : "+v"(a));
-      x[k].a = a;
+      x[k].r.a = a;
     }
   }
+}
+
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float across16(float v) {   // + lane ^ 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float across32(float v) {   // + lane ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // A lane's place
@@ -75,7 +113,7 @@ struct Lane {
   int wave, waves, r, RT, gl, c, n, lpr;   // waves: of the team; c: first channel, n: channels of the piece (0: none), gl: group in the team
   int g, section, team;
   bool first;                              // the group's (or its section's) first lane
-  __device__ __forceinline__ Lane(const NormParams& p, int bundle) {
+  template <int W> __device__ __forceinline__ void init(const NormParams& p, int bundle) {
     const int tid = threadIdx.x, t = tid & ((1 << p.t.ttlog) - 1), v = t & ((1 << p.t.mlog) - 1);
     team = tid >> p.t.ttlog;
     wave = tid >> 6;
@@ -86,27 +124,39 @@ struct Lane {
     RT = 1 << (p.t.ttlog - lpr);
     section = bundle % p.sections;
     g = bundle / p.sections * (1 << p.t.nblog) + gl;
-    const int at = section * p.span + v * 8;   // in the group
+    const int at = section * p.span + v * W;   // in the group
     c = g * p.cg + at;
-    n = g < p.n.groups && v < p.t.m ? max(0, min(8, p.cg - at)) : 0;
+    n = g < p.n.groups && v < p.t.m ? max(0, min(W, p.cg - at)) : 0;
     first = n && r == 0 && v == 0;
   }
   // this lane's entry of the segments' sums of image m
   __device__ __forceinline__ float* entry(const NormParams& p, i64 m, int i) const {
     return p.part + ((m * p.n.groups + g) * (p.segs * p.sections) + i) * 2;
   }
-  // Sums over a group's lanes of this wave
+  // Sums over a group's lanes of this wave.  Its pieces are the low bits of a lane; its pixels the high ones, turned within rows of 16 (a team
+  // that has several pixels side by side has 16 lanes at least) and exchanged between rows.
   template <int N> __device__ __forceinline__ void wave_sums(const Team& t, float (&s)[N]) const {
-    for (int o = 1; o < 64 && o < 1 << t.mlog; o <<= 1)
+    auto each = [&](auto f) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], o, 64);
-    for (int o = 1 << lpr; o < 64 && o < 1 << t.ttlog; o <<= 1)
-#pragma unroll
-      for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], o, 64);
+      for (int i = 0; i < N; ++i) s[i] = f(s[i]);
+    };
+    if (t.mlog > 0) each([](float v) { return v + dpp<0xb1>(v); });    // lane ^ 1
+    if (t.mlog > 1) each([](float v) { return v + dpp<0x4e>(v); });    // lane ^ 2
+    if (t.mlog > 2) each([](float v) { return v + dpp<0x141>(v); });   // 7 - lane: fours are equal by now
+    if (t.mlog > 3) each([](float v) { return v + dpp<0x140>(v); });   // 15 - lane
+    if (t.ttlog > t.lprlog) {
+      if (t.lprlog < 1) each([](float v) { return v + dpp<0x121>(v); });
+      if (t.lprlog < 2) each([](float v) { return v + dpp<0x122>(v); });
+      if (t.lprlog < 3) each([](float v) { return v + dpp<0x124>(v); });
+      if (t.lprlog < 4) each([](float v) { return v + dpp<0x128>(v); });
+    }
+    if (t.mlog > 4 || (t.lprlog < 5 && t.ttlog > 4)) each([](float v) { return across16(v); });
+    if (t.mlog > 5 || (t.lprlog < 6 && t.ttlog > 5)) each([](float v) { return across32(v); });
   }
-  // Where this wave's sums go and the team's begin; entries of N floats
-  __device__ __forceinline__ int slot(int w) const { return w * 64 + gl; }
+  // Where this wave's sums go and the team's begin
+  __device__ __forceinline__ int slot(const Team& t, int w) const { return (w << t.nblog) + gl; }
   __device__ __forceinline__ int first_wave() const { return wave & ~(waves - 1); }
+  __device__ __forceinline__ bool writes(const Team& t) const { return (int)(threadIdx.x & 63) == (gl << t.mlog & 63); }
 };
 
 struct Moments { float n, mean, m2; };
@@ -117,82 +167,109 @@ __device__ __forceinline__ void merge(Moments& a, const Moments& b) {
   a.m2 += b.m2 + d * d * a.n * q;
   a.n = n;
 }
-// A group's moments from its lanes'; every lane of the team returns them.  buf: [64 * waves of the workgroup][3]
-__device__ __forceinline__ Moments team_moments(const Lane& l, const Team& t, Moments a, float (*buf)[3]) {
-  float s[2] = {a.n, a.n * a.mean};
+// Moments of IM images' groups from their lanes'; every lane of the team returns them.  buf: [IM][waves << nblog] entries of three
+template <int IM> __device__ __forceinline__ void team_moments(const Lane& l, const Team& t, Moments (&a)[IM], float* buf, int entries) {
+  float s[2 * IM], q[IM];
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    s[2 * i] = a[i].n;
+    s[2 * i + 1] = a[i].n * a[i].mean;
+  }
   l.wave_sums(t, s);
-  const float wmean = s[0] > 0.f ? s[1] / s[0] : 0.f, d = a.mean - wmean;
-  float q[1] = {a.n > 0.f ? a.m2 + a.n * d * d : 0.f};
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    const float wmean = s[2 * i] > 0.f ? s[2 * i + 1] / s[2 * i] : 0.f, d = a[i].mean - wmean;
+    q[i] = a[i].n > 0.f ? a[i].m2 + a[i].n * d * d : 0.f;
+    a[i].n = s[2 * i];
+    a[i].mean = wmean;
+  }
   l.wave_sums(t, q);
-  Moments w = {s[0], wmean, q[0]};
-  if (t.ttlog <= 6) return w;
-  if ((threadIdx.x & 63) == (l.gl << t.mlog & 63)) {
-    float* o = buf[l.slot(l.wave)];
-    o[0] = w.n; o[1] = w.mean; o[2] = w.m2;
+#pragma unroll
+  for (int i = 0; i < IM; ++i) a[i].m2 = q[i];
+  if (t.ttlog <= 6) return;
+  if (l.writes(t)) {
+#pragma unroll
+    for (int i = 0; i < IM; ++i) {
+      float* o = buf + (i * entries + l.slot(t, l.wave)) * 3;
+      o[0] = a[i].n; o[1] = a[i].mean; o[2] = a[i].m2;
+    }
   }
   __syncthreads();
-  float n = 0.f, sum = 0.f, m2 = 0.f;
-  for (int i = 0; i < l.waves; ++i) {
-    const float* o = buf[l.slot(l.first_wave() + i)];
-    n += o[0];
-    sum += o[0] * o[1];
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    float n = 0.f, sum = 0.f, m2 = 0.f;
+    for (int w = 0; w < l.waves; ++w) {
+      const float* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
+      n += o[0];
+      sum += o[0] * o[1];
+    }
+    const float mean = n > 0.f ? sum / n : 0.f;
+    for (int w = 0; w < l.waves; ++w) {
+      const float* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
+      const float e = o[1] - mean;
+      m2 += o[2] + o[0] * e * e;
+    }
+    a[i] = {n, mean, m2};
   }
-  const float mean = sum / n;
-  for (int i = 0; i < l.waves; ++i) {
-    const float* o = buf[l.slot(l.first_wave() + i)];
-    const float e = o[1] - mean;
-    m2 += o[2] + o[0] * e * e;
-  }
-  return {n, mean, m2};
 }
-__device__ __forceinline__ void team_sums(const Lane& l, const Team& t, float (&s)[2], float (*buf)[3]) {
+// ... of pairs of sums.  buf: [waves << nblog] entries of 2 IM
+template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const Team& t, float (&s)[2 * IM], float* buf) {
   l.wave_sums(t, s);
   if (t.ttlog <= 6) return;
-  if ((threadIdx.x & 63) == (l.gl << t.mlog & 63)) {
-    float* o = buf[l.slot(l.wave)];
-    o[0] = s[0]; o[1] = s[1];
+  if (l.writes(t)) {
+#pragma unroll
+    for (int i = 0; i < 2 * IM; ++i) buf[l.slot(t, l.wave) * 2 * IM + i] = s[i];
   }
   __syncthreads();
-  s[0] = s[1] = 0.f;
-  for (int i = 0; i < l.waves; ++i) {
-    const float* o = buf[l.slot(l.first_wave() + i)];
-    s[0] += o[0];
-    s[1] += o[1];
-  }
+#pragma unroll
+  for (int i = 0; i < 2 * IM; ++i) s[i] = 0.f;
+  for (int w = 0; w < l.waves; ++w)
+#pragma unroll
+    for (int i = 0; i < 2 * IM; ++i) s[i] += buf[l.slot(t, l.first_wave() + w) * 2 * IM + i];
 }
 
 // Moments about `pivot` of KP pieces, rows of which are in
-template <bool FULL, typename T, int KP> __device__ __forceinline__ Moments moments_of(Raw8<T> (&x)[KP], int rows, int n, float pivot) {
+template <typename T, int V, int KP> __device__ __forceinline__ Moments moments_of(Held<T, V> (&x)[KP], int rows, int n, float pivot) {
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < KP; ++k)
     if (k < rows) {
-      const F8 f = widen(x[k]);
+      const auto f = vals(x[k]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s += FULL || i < n ? f.v[i] - pivot : 0.f;
+      for (int i = 0; i < width_of<V>; ++i) s += V != TAIL || i < n ? f.v[i] - pivot : 0.f;
     }
   Moments m = {(float)(rows * n), 0.f, 0.f};
   if (rows * n == 0) return m;
   m.mean = s / m.n;
   as_held(x);
+  const float c = pivot + m.mean;   // (its rounding d adds n d^2 to the sum, and nothing else: the differences to the mean add up to nothing)
 #pragma unroll
   for (int k = 0; k < KP; ++k)
     if (k < rows) {
-      const F8 f = widen(x[k]);
+      const auto f = vals(x[k]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float d = FULL || i < n ? (f.v[i] - pivot) - m.mean : 0.f;
+      for (int i = 0; i < width_of<V>; ++i) {
+        const float d = V != TAIL || i < n ? f.v[i] - c : 0.f;
         m.m2 = fmaf(d, d, m.m2);
       }
     }
   return m;
 }
 
-struct Columns { F8 ga, be; };
-__device__ __forceinline__ Columns columns_of(const Norm& p, const Lane& l) {
-  Columns o;
+template <int V> struct Columns { Vals<width_of<V>> ga, be; };
+template <int V> __device__ __forceinline__ Columns<V> columns_of(const Norm& p, const Lane& l) {
+  Columns<V> o;
+  if (V == EIGHTS && l.n) {
+    const F8 ga = p.gamma ? load8<float>(p.gamma, l.c, l.c + 8) : F8{{1, 1, 1, 1, 1, 1, 1, 1}}, be = p.beta ? load8<float>(p.beta, l.c, l.c + 8) : F8{};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < width_of<V>; ++i) {
+      o.ga.v[i] = ga.v[i];
+      o.be.v[i] = be.v[i];
+    }
+    return o;
+  }
+#pragma unroll
+  for (int i = 0; i < width_of<V>; ++i) {
     o.ga.v[i] = i < l.n ? p.gamma ? p.gamma[l.c + i] : 1.f : 0.f;
     o.be.v[i] = i < l.n && p.beta ? p.beta[l.c + i] : 0.f;
   }
@@ -201,222 +278,313 @@ __device__ __forceinline__ Columns columns_of(const Norm& p, const Lane& l) {
 
 enum { WHOLE, SUMS, OUTPUTS };   // an image at a time, or the two launches of segments
 
+// A lane's rows, one after the other.  WHOLE: 32-bit offsets from what is the same for the workgroup (plan_of sees to it), which take one register
+// for all of them.
+template <typename T, int PHASE> struct Rows {
+  char* base;      // WHOLE: of the workgroup's image; else of this lane's channels in it
+  unsigned off;
+  i64 row, hop;    // bytes from a pixel, from a row of this lane to the next
+  __device__ __forceinline__ Rows(const void* p, const Lane& l, i64 P, i64 ld, i64 m0) {
+    row = ld * sizeof(T);
+    hop = row * l.RT;
+    base = static_cast<char*>(const_cast<void*>(p)) + m0 * P * row;
+    off = (unsigned)(((l.team * P + l.r) * ld + l.c) * (int)sizeof(T));
+    if constexpr (PHASE != WHOLE) base += l.team * P * row + l.c * (i64)sizeof(T);
+  }
+  __device__ __forceinline__ void from(i64 px) {   // (WHOLE: from its first)
+    if constexpr (PHASE != WHOLE) base += px * row;
+  }
+  __device__ __forceinline__ T* next() {
+    T* at = reinterpret_cast<T*>(PHASE == WHOLE ? base + off : base);
+    base += hop;
+    return at;
+  }
+};
+
 // A workgroup's place: bundles of channels run fastest, and each XCD gets a run of them, so that neighbours share what they read in its cache
 struct Place { int bundle, slice, seg; };
 __device__ __forceinline__ bool place_of(const NormParams& p, Place* at) {
   const int total = p.bundles * p.slices * p.segs, run = (total + 7) >> 3, s = (int)blockIdx.x >> 3, id = ((int)blockIdx.x & 7) * run + s;
   if (s >= run || id >= total) return false;
-  at->bundle = id % p.bundles;
-  const int rest = id / p.bundles;
-  at->slice = rest % p.slices;
-  at->seg = rest / p.slices;
+  const int rest = p.per_bundle ? (int)__umulhi((unsigned)id, p.per_bundle) : id;
+  at->bundle = id - rest * p.bundles;
+  at->seg = p.per_slice ? (int)__umulhi((unsigned)rest, p.per_slice) : rest;
+  at->slice = rest - at->seg * p.slices;
   return true;
 }
+// Rows of a lane from px on
+template <int KP> __device__ __forceinline__ int rows_from(const Lane& l, bool live, i64 px, i64 end) {
+  const i64 n = (end - px + l.RT - 1) >> (31 - __clz(l.RT));
+  return !live || n <= 0 ? 0 : n < KP ? (int)n : KP;
+}
 
-template <typename T, int F, int NT, int KP, int PHASE, bool FULL> __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
-  __shared__ float buf[2][NT][3];
+// IM: images at a time (WHOLE)
+template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
+  extern __shared__ float lds[];   // two turns' moments
   Place at;
   if (!place_of(p, &at)) return;
-  const Lane l(p, at.bundle);
-  const int teams = NT >> p.t.ttlog;
+  Lane l;
+  l.init<width_of<V>>(p, at.bundle);
+  const int teams = NT >> p.t.ttlog, entries = NT / 64 << p.t.nblog;
   const i64 beg = at.seg * p.seg, end = beg + p.seg < p.n.P ? beg + p.seg : p.n.P;
-  const Columns col = PHASE == SUMS ? Columns{} : columns_of(p.n, l);
   const float count = (float)p.n.P * (float)p.cg;
-  int turn = 0;
-  for (i64 m0 = (i64)at.slice * teams; m0 < p.n.M; m0 += (i64)p.slices * teams, turn ^= 1) {   // (every lane of the workgroup takes part in the barrier)
-    const i64 m = m0 + l.team;
-    const bool live = m < p.n.M && l.n;
-    const T* x = static_cast<const T*>(p.n.x) + (m * p.n.P) * p.n.ldx + l.c;
-    const float pivot = live ? to_f32(x[l.g * p.cg - l.c]) : 0.f;   // (the group's first value)
-    T* y = static_cast<T*>(p.n.y) + (m * p.n.P) * p.n.ldy + l.c;
-    Raw8<T> v[KP];
-    auto load = [&](i64 px) {   // rows of this lane from px on
-      const i64 left = end - px;
-      const int rows = !live || left <= 0 ? 0 : (int)((left + l.RT - 1) / l.RT < KP ? (left + l.RT - 1) / l.RT : KP);
+  auto live_at = [&](i64 m0) { return m0 + l.team < p.n.M && l.n; };
+  auto pivot_at = [&](i64 m0) {   // the group's first value
+    return live_at(m0) ? to_f32(static_cast<const T*>(p.n.x)[(m0 + l.team) * p.n.P * p.n.ldx + l.g * p.cg]) : 0.f;
+  };
+  auto load = [&](Held<T, V> (&v)[KP], i64 m0, i64 px) {
+    Rows<T, PHASE> x(p.n.x, l, p.n.P, p.n.ldx, m0);
+    const int rows = rows_from<KP>(l, live_at(m0), px, end);
+    x.from(px);
 #pragma unroll
-      for (int k = 0; k < KP; ++k)
-        if (k < rows) v[k] = load_piece<FULL>(x + (px + (i64)k * l.RT) * p.n.ldx, l.n);
-      return rows;
-    };
-    auto put = [&](i64 px, int rows, float mean, float r) {
-      as_held(v);
+    for (int k = 0; k < KP; ++k) {
+      const T* q = x.next();
+      if (k < rows) v[k] = load_piece<T, V>(q, l.n);
+    }
+    return rows;
+  };
+  Columns<V> col;
+  if constexpr (PHASE != SUMS && IM > 1) col = columns_of<V>(p.n, l);
+  auto put = [&](Held<T, V> (&v)[KP], i64 m0, i64 px, int rows, float mean, float r) {
+    Rows<T, PHASE> y(p.n.y, l, p.n.P, p.n.ldy, m0);
+    y.from(px);
+    as_held(v);
+    const float shift = -mean * r;
 #pragma unroll
-      for (int k = 0; k < KP; ++k)
-        if (k < rows) {
-          F8 f = widen(v[k]);
+    for (int k = 0; k < KP; ++k) {
+      T* q = y.next();
+      if (k >= rows) continue;
+      auto f = vals(v[k]);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float z = fmaf((f.v[i] - mean) * r, col.ga.v[i], col.be.v[i]), df;
-            act_of<T, F>(z, &f.v[i], &df);
-          }
-          store_piece<FULL>(y + (px + (i64)k * l.RT) * p.n.ldy, l.n, f);
-        }
-    };
-    auto keep = [&](float mean, float r) {
-      if (p.n.stats && live && l.first && l.section == 0 && at.seg == 0)
-        *reinterpret_cast<float2*>(p.n.stats + (m * p.n.groups + l.g) * 2) = make_float2(mean, r);
-    };
-    if constexpr (PHASE == WHOLE) {
-      const int rows = load(beg + l.r);
-      const Moments a = team_moments(l, p.t, moments_of<FULL>(v, rows, l.n, pivot), buf[turn]);
-      const float r = 1.f / sqrtf(a.m2 / count + p.n.eps), mean = pivot + a.mean;
-      put(beg + l.r, rows, mean, r);
-      keep(mean, r);
-    } else if constexpr (PHASE == SUMS) {
-      Moments a = {0.f, 0.f, 0.f};
-      for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
-        const int rows = load(px);
-        merge(a, moments_of<FULL>(v, rows, l.n, pivot));
+      for (int i = 0; i < width_of<V>; ++i) {
+        float df;
+        act_of<T, F>(fmaf(fmaf(f.v[i], r, shift), col.ga.v[i], col.be.v[i]), &f.v[i], &df);
       }
-      a = team_moments(l, p.t, a, buf[turn]);
-      if (live && l.first) *reinterpret_cast<float2*>(l.entry(p, m, at.seg * p.sections + l.section)) = make_float2(a.mean, a.m2);
+      store_piece<T, V>(q, l.n, f);
+    }
+  };
+  auto keep = [&](i64 m0, float mean, float r) {
+    if (p.n.stats && live_at(m0) && l.first && l.section == 0 && at.seg == 0)
+      *reinterpret_cast<float2*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 2) = make_float2(mean, r);
+  };
+  const i64 stride = (i64)p.slices * teams * IM;
+  int turn = 0;   // (every lane of the workgroup takes part in the barrier of every turn)
+  for (i64 m0 = (i64)at.slice * teams * IM; m0 < p.n.M; m0 += stride, turn ^= 1) {
+    float* const buf = lds + turn * IM * entries * 3;
+    Held<T, V> v[IM][KP];
+    Moments a[IM];
+    if constexpr (PHASE == WHOLE) {
+      float pivot[IM];
+      int rows[IM];
+#pragma unroll
+      for (int i = 0; i < IM; ++i) {
+        pivot[i] = pivot_at(m0 + i * teams);
+        rows[i] = load(v[i], m0 + i * teams, l.r);
+      }
+      if constexpr (IM == 1) col = columns_of<V>(p.n, l);
+#pragma unroll
+      for (int i = 0; i < IM; ++i) a[i] = moments_of(v[i], rows[i], l.n, pivot[i]);
+      team_moments(l, p.t, a, buf, entries);
+#pragma unroll
+      for (int i = 0; i < IM; ++i) {
+        const float r = 1.f / sqrtf(a[i].m2 / count + p.n.eps), mean = pivot[i] + a[i].mean;
+        put(v[i], m0 + i * teams, l.r, rows[i], mean, r);
+        keep(m0 + i * teams, mean, r);
+      }
     } else {
-      Moments a = {0.f, 0.f, 0.f};
-      if (live)
-        for (int s = 0; s < p.segs; ++s)
-          for (int e = 0; e < p.sections; ++e) {
-            const float2 q = *reinterpret_cast<const float2*>(l.entry(p, m, s * p.sections + e));
-            const i64 px = p.n.P - s * p.seg < p.seg ? p.n.P - s * p.seg : p.seg;
-            merge(a, {(float)px * (float)min(p.span, p.cg - e * p.span), q.x, q.y});
-          }
-      const float r = 1.f / sqrtf(a.m2 / count + p.n.eps), mean = pivot + a.mean;
-      for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) put(px, load(px), mean, r);
-      keep(mean, r);
+      const i64 m = m0 + l.team;
+      const float pivot = pivot_at(m0);
+      a[0] = {0.f, 0.f, 0.f};
+      if constexpr (PHASE == SUMS) {
+        for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
+          const int rows = load(v[0], m0, px);
+          merge(a[0], moments_of(v[0], rows, l.n, pivot));
+        }
+        team_moments(l, p.t, a, buf, entries);
+        if (live_at(m0) && l.first) *reinterpret_cast<float2*>(l.entry(p, m, at.seg * p.sections + l.section)) = make_float2(a[0].mean, a[0].m2);
+      } else {
+        col = columns_of<V>(p.n, l);
+        if (live_at(m0))
+          for (int s = 0; s < p.segs; ++s)
+            for (int e = 0; e < p.sections; ++e) {
+              const float2 q = *reinterpret_cast<const float2*>(l.entry(p, m, s * p.sections + e));
+              const i64 px = p.n.P - s * p.seg < p.seg ? p.n.P - s * p.seg : p.seg;
+              merge(a[0], {(float)px * (float)min(p.span, p.cg - e * p.span), q.x, q.y});
+            }
+        const float r = 1.f / sqrtf(a[0].m2 / count + p.n.eps), mean = pivot + a[0].mean;
+        for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
+          const int rows = load(v[0], m0, px);
+          put(v[0], m0, px, rows, mean, r);
+        }
+        keep(m0, mean, r);
+      }
     }
   }
 }
 
 // dxhat = gamma dz, dz = dy f'(z);  dx = r (dxhat - mean(dxhat) - xhat mean(dxhat xhat)),  dgamma = sum dz xhat,  dbeta = sum dz
-template <typename T, int F, int NT, int KP, int PHASE, bool FULL> __global__ __launch_bounds__(NT) void norm_bwd_kernel(NormParams p) {
-  __shared__ float buf[2][NT][3];
-  extern __shared__ float cols[];   // [waves][64][16]
+template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_bwd_kernel(NormParams p) {
+  constexpr int W = width_of<V>;
+  extern __shared__ float lds[];   // two turns' sums; at the end the columns', [waves][2 W][64]
   Place at;
   if (!place_of(p, &at)) return;
-  const Lane l(p, at.bundle);
-  const int teams = NT >> p.t.ttlog;
+  Lane l;
+  l.init<W>(p, at.bundle);
+  const int teams = NT >> p.t.ttlog, entries = NT / 64 << p.t.nblog;
   const i64 beg = at.seg * p.seg, end = beg + p.seg < p.n.P ? beg + p.seg : p.n.P;
-  const Columns col = columns_of(p.n, l);
+  const Columns<V> col = columns_of<V>(p.n, l);
   const float count = (float)p.n.P * (float)p.cg;
-  F8 dga = {}, dbe = {};
-  int turn = 0;
-  for (i64 m0 = (i64)at.slice * teams; m0 < p.n.M; m0 += (i64)p.slices * teams, turn ^= 1) {
-    const i64 m = m0 + l.team;
-    const bool live = m < p.n.M && l.n;
-    const T* x = static_cast<const T*>(p.n.x) + (m * p.n.P) * p.n.ldx + l.c;
-    const T* dy = static_cast<const T*>(p.n.dy) + (m * p.n.P) * p.n.ldy + l.c;
-    const float2 st = live ? *reinterpret_cast<const float2*>(p.n.stats + (m * p.n.groups + l.g) * 2) : make_float2(0.f, 0.f);
-    const float mean = st.x, r = st.y;
-    Raw8<T> v[KP], d[KP];
-    auto load = [&](i64 px) {
-      const i64 left = end - px;
-      const int rows = !live || left <= 0 ? 0 : (int)((left + l.RT - 1) / l.RT < KP ? (left + l.RT - 1) / l.RT : KP);
+  Vals<W> dga = {}, dbe = {};
+  struct Image { Held<T, V> v[KP], d[KP]; float r, shift; int rows; };   // xhat = x r + shift
+  auto live_at = [&](i64 m0) { return m0 + l.team < p.n.M && l.n; };
+  auto stats_of = [&](Image& q, i64 m0) {
+    const float2 st = live_at(m0) ? *reinterpret_cast<const float2*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 2) : make_float2(0.f, 0.f);
+    q.r = st.y;
+    q.shift = -st.x * st.y;
+  };
+  auto load = [&](Image& q, i64 m0, i64 px) {
+    Rows<T, PHASE> x(p.n.x, l, p.n.P, p.n.ldx, m0), dy(p.n.dy, l, p.n.P, p.n.ldy, m0);
+    q.rows = rows_from<KP>(l, live_at(m0), px, end);
+    x.from(px);
+    dy.from(px);
 #pragma unroll
-      for (int k = 0; k < KP; ++k)
-        if (k < rows) {
-          v[k] = load_piece<FULL>(x + (px + (i64)k * l.RT) * p.n.ldx, l.n);
-          d[k] = load_piece<FULL>(dy + (px + (i64)k * l.RT) * p.n.ldy, l.n);
+    for (int k = 0; k < KP; ++k) {
+      const T *a = x.next(), *b = dy.next();
+      if (k >= q.rows) continue;
+      q.v[k] = load_piece<T, V>(a, l.n);
+      q.d[k] = load_piece<T, V>(b, l.n);
+    }
+  };
+  auto dz_of = [&](float xhat, float dyv, int i) {
+    if constexpr (F == CONVBN_NORM_NONE) return dyv;
+    const float z = fmaf(xhat, col.ga.v[i], col.be.v[i]);
+    if constexpr (F == CONVBN_NORM_RELU) return z > 0.f ? dyv : 0.f * dyv;   // (an infinite gradient behind a closed ReLU stays one of a kind)
+    float f, df;
+    act_of<T, F>(z, &f, &df);
+    return dyv * df;
+  };
+  // what an image adds to a lane's columns, and s: the sums of dxhat and dxhat xhat
+  auto add_up = [&](Image& q, float* s) {
+    Vals<W> sz = {}, sx = {};
+#pragma unroll
+    for (int k = 0; k < KP; ++k)
+      if (k < q.rows) {
+        const auto a = vals(q.v[k]), b = vals(q.d[k]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const float xhat = fmaf(a.v[i], q.r, q.shift), dz = V != TAIL || i < l.n ? dz_of(xhat, b.v[i], i) : 0.f;
+          sz.v[i] += dz;
+          sx.v[i] = fmaf(dz, xhat, sx.v[i]);
         }
-      return rows;
-    };
-    auto dz_of = [&](float xv, float dyv, int i, float* xhat) {
-      *xhat = (xv - mean) * r;
-      if constexpr (F == CONVBN_NORM_NONE) return dyv;
-      float f, df;
-      act_of<T, F>(fmaf(*xhat, col.ga.v[i], col.be.v[i]), &f, &df);
-      return dyv * df;
-    };
-    auto add_up = [&](int rows, float (&s)[2]) {
-#pragma unroll
-      for (int k = 0; k < KP; ++k)
-        if (k < rows) {
-          const F8 a = widen(v[k]), b = widen(d[k]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float xhat;
-            const float dz = FULL || i < l.n ? dz_of(a.v[i], b.v[i], i, &xhat) : xhat = 0.f, q = dz * xhat;
-            dbe.v[i] += dz;
-            dga.v[i] += q;
-            s[0] = fmaf(dz, col.ga.v[i], s[0]);
-            s[1] = fmaf(q, col.ga.v[i], s[1]);
-          }
-        }
-    };
-    auto put = [&](i64 px, int rows, float s0, float s1) {
-      as_held(v);
-      as_held(d);
-#pragma unroll
-      for (int k = 0; k < KP; ++k)
-        if (k < rows) {
-          const F8 a = widen(v[k]), b = widen(d[k]);
-          const i64 o = (m * p.n.P + px + (i64)k * l.RT) * p.n.ldx + l.c;
-          F8 f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float xhat;
-            const float dz = dz_of(a.v[i], b.v[i], i, &xhat);
-            f.v[i] = r * (fmaf(dz, col.ga.v[i], -s0) - xhat * s1);
-          }
-          if (p.n.add) {
-            const F8 e = widen(load_piece<FULL>(static_cast<const T*>(p.n.add) + o, l.n));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f.v[i] += e.v[i];
-          }
-          store_piece<FULL>(static_cast<T*>(p.n.dx) + o, l.n, f);
-        }
-    };
-    if constexpr (PHASE == WHOLE) {
-      float s[2] = {0.f, 0.f};
-      const int rows = load(beg + l.r);
-      add_up(rows, s);
-      if (p.n.dx) {
-        team_sums(l, p.t, s, buf[turn]);
-        put(beg + l.r, rows, s[0] / count, s[1] / count);
       }
-    } else if constexpr (PHASE == SUMS) {
-      float s[2] = {0.f, 0.f};
-      for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) add_up(load(px), s);
-      team_sums(l, p.t, s, buf[turn]);
-      if (live && l.first) *reinterpret_cast<float2*>(l.entry(p, m, at.seg * p.sections + l.section)) = make_float2(s[0], s[1]);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      dbe.v[i] += sz.v[i];
+      dga.v[i] += sx.v[i];
+      s[0] = fmaf(sz.v[i], col.ga.v[i], s[0]);
+      s[1] = fmaf(sx.v[i], col.ga.v[i], s[1]);
+    }
+  };
+  auto put = [&](Image& q, i64 m0, i64 px, float s0, float s1) {
+    Rows<T, PHASE> dx(p.n.dx, l, p.n.P, p.n.ldx, m0), add(p.n.add, l, p.n.P, p.n.ldx, m0);
+    dx.from(px);
+    add.from(px);
+    as_held(q.v);
+    as_held(q.d);
+    const float r0 = -q.r * s0, r1 = -q.r * s1;
+    Vals<W> rg;
+#pragma unroll
+    for (int i = 0; i < W; ++i) rg.v[i] = q.r * col.ga.v[i];
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+      T* o = dx.next();
+      const T* e = add.next();
+      if (k >= q.rows) continue;
+      const auto a = vals(q.v[k]), b = vals(q.d[k]);
+      Vals<W> f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float xhat = fmaf(a.v[i], q.r, q.shift), dz = dz_of(xhat, b.v[i], i);
+        f.v[i] = fmaf(dz, rg.v[i], fmaf(xhat, r1, r0));
+      }
+      if (p.n.add) {
+        const auto w = vals(load_piece<T, V>(e, l.n));
+#pragma unroll
+        for (int i = 0; i < W; ++i) f.v[i] += w.v[i];
+      }
+      store_piece<T, V>(o, l.n, f);
+    }
+  };
+  const i64 stride = (i64)p.slices * teams * IM;
+  int turn = 0;
+  for (i64 m0 = (i64)at.slice * teams * IM; m0 < p.n.M; m0 += stride, turn ^= 1) {
+    float* const buf = lds + turn * IM * entries * 2;
+    Image q[IM];
+    float s[2 * IM] = {};
+#pragma unroll
+    for (int i = 0; i < IM; ++i) stats_of(q[i], m0 + i * teams);
+    if constexpr (PHASE == WHOLE) {
+#pragma unroll
+      for (int i = 0; i < IM; ++i) load(q[i], m0 + i * teams, l.r);
+#pragma unroll
+      for (int i = 0; i < IM; ++i) add_up(q[i], s + 2 * i);
+      if (p.n.dx) {
+        team_sums<IM>(l, p.t, s, buf);
+#pragma unroll
+        for (int i = 0; i < IM; ++i) put(q[i], m0 + i * teams, l.r, s[2 * i] / count, s[2 * i + 1] / count);
+      }
     } else {
-      float s0 = 0.f, s1 = 0.f;
-      if (live)
-        for (int s = 0; s < p.segs * p.sections; ++s) {
-          const float2 q = *reinterpret_cast<const float2*>(l.entry(p, m, s));
-          s0 += q.x;
-          s1 += q.y;
+      const i64 m = m0 + l.team;
+      if constexpr (PHASE == SUMS) {
+        for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
+          load(q[0], m0, px);
+          add_up(q[0], s);
         }
-      for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) put(px, load(px), s0 / count, s1 / count);
+        team_sums<IM>(l, p.t, s, buf);
+        if (live_at(m0) && l.first) *reinterpret_cast<float2*>(l.entry(p, m, at.seg * p.sections + l.section)) = make_float2(s[0], s[1]);
+      } else {
+        if (live_at(m0))
+          for (int i = 0; i < p.segs * p.sections; ++i) {
+            const float2 e = *reinterpret_cast<const float2*>(l.entry(p, m, i));
+            s[0] += e.x;
+            s[1] += e.y;
+          }
+        for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
+          load(q[0], m0, px);
+          put(q[0], m0, px, s[0] / count, s[1] / count);
+        }
+      }
     }
   }
   if (PHASE == OUTPUTS || !p.sums) return;
   // lanes of the same channels: those of a wave by shuffles, then the waves
   for (int o = 1 << l.lpr; o < 64; o <<= 1)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < W; ++i) {
       dga.v[i] += __shfl_xor(dga.v[i], o, 64);
       dbe.v[i] += __shfl_xor(dbe.v[i], o, 64);
     }
   const int lane = threadIdx.x & 63, hop = l.lpr > 6 ? 1 << (l.lpr - 6) : 1;   // waves with the same channels are `hop` apart
   if (NT / 64 > hop) {
-    __syncthreads();
+    __syncthreads();   // (the sums' place)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      cols[(l.wave * 16 + i) * 64 + lane] = dga.v[i];
-      cols[(l.wave * 16 + 8 + i) * 64 + lane] = dbe.v[i];
+    for (int i = 0; i < W; ++i) {
+      lds[(l.wave * 2 * W + i) * 64 + lane] = dga.v[i];
+      lds[(l.wave * 2 * W + W + i) * 64 + lane] = dbe.v[i];
     }
     __syncthreads();
     if (l.wave >= hop) return;
     for (int w = l.wave + hop; w < NT / 64; w += hop)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        dga.v[i] += cols[(w * 16 + i) * 64 + lane];
-        dbe.v[i] += cols[(w * 16 + 8 + i) * 64 + lane];
+      for (int i = 0; i < W; ++i) {
+        dga.v[i] += lds[(w * 2 * W + i) * 64 + lane];
+        dbe.v[i] += lds[(w * 2 * W + W + i) * 64 + lane];
       }
   }
   if ((int)threadIdx.x < 1 << l.lpr) {
     float* out = p.sums + ((i64)(at.seg * p.slices + at.slice) * p.n.C + l.c) * 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < W; ++i)
       if (i < l.n) *reinterpret_cast<float2*>(out + 2 * i) = make_float2(dga.v[i], dbe.v[i]);
   }
 }
@@ -452,36 +620,40 @@ int log2_up(i64 v) {
   return l;
 }
 
-constexpr int CUS = 256, MAX_SPAN = 8192;   // channels of a workgroup's lanes
+constexpr int CUS = 256, MAX_LANES = 1024;   // of a group's pixel
 
 // How a call is run: workgroups of nt, the teams, one launch or two
 struct Plan {
-  int nt;
-  bool few, whole, full;   // few: at most two pieces a lane; full: pieces are
+  int nt, pieces;
+  bool few, single, whole;   // at most two pieces a lane; one; one launch
   NormParams p;
   size_t part, sums, total;
 };
 // Pieces that a lane's registers hold, of workgroups of 256 and 512
-constexpr int most_of(int size, bool bwd, int nt) { return (nt == 512 ? bwd ? 16 : 32 : bwd ? 4 : 8) * 2 / size; }
+constexpr int most_of(int size, bool bwd, int nt, int v) {
+  return v == ONES ? nt == 512 ? 32 : 8 : (nt == 512 ? bwd ? 16 : 32 : bwd ? 4 : 8) * 2 / size;
+}
 constexpr int FEW = 2, STREAM = 4;   // pieces a lane: of short parts, of a turn of the segments' launches
+constexpr int images_at_once(int size, bool bwd) { return (bwd ? 4 : 8) / size; }   // that have one piece a lane
 
 Plan plan_of(const Norm& n, bool bwd) {
   Plan s = {};
   NormParams& p = s.p;
   p.n = n;
   p.cg = n.C / n.groups;
-  s.full = p.cg % 8 == 0;
-  p.sections = ceil_div(p.cg, MAX_SPAN);
-  p.span = p.sections > 1 ? MAX_SPAN : p.cg;
+  s.pieces = p.cg % 8 == 0 ? EIGHTS : p.cg < 64 ? ONES : TAIL;
+  const int width = s.pieces == ONES ? 1 : 8;
+  p.sections = ceil_div(p.cg, MAX_LANES * width);
+  p.span = p.sections > 1 ? MAX_LANES * width : p.cg;
   const int size = n.dtype == CONVBN_BF16 ? 2 : 4;
   Team& t = p.t;
-  t.m = ceil_div(p.span, 8);
+  t.m = ceil_div(p.span, width);
   t.mlog = log2_up(t.m);
   const int glog = log2_up(n.groups);
   // groups side by side until a pixel's part is 64 bytes, or until a wave is full of pieces of few channels
   while (t.nblog < glog && t.mlog + t.nblog < 6 && (p.cg << t.nblog) * size < 64) ++t.nblog;
   auto lanes = [&](int log) { return (n.P + (1LL << (log - t.lprlog)) - 1) >> (log - t.lprlog); };   // pieces of a lane
-  auto fits = [&] { return p.sections == 1 && (t.lprlog <= 9 ? lanes(9) <= most_of(size, bwd, 512) : n.P <= FEW); };
+  auto fits = [&] { return p.sections == 1 && (t.lprlog <= 9 ? lanes(9) <= most_of(size, bwd, 512, s.pieces) : n.P <= FEW); };
   t.lprlog = t.mlog + t.nblog;
   // (backward holds twice as much: pixels' parts of 32 bytes if that keeps it in one launch)
   while (!fits() && t.nblog > 0 && (p.cg << (t.nblog - 1)) * size >= 32) {
@@ -490,15 +662,22 @@ Plan plan_of(const Norm& n, bool bwd) {
   }
   p.bundles = (int)((n.groups + (1LL << t.nblog) - 1) >> t.nblog) * p.sections;
   // one launch where the parts fit and are enough to fill a quarter of the chip, or short
-  s.whole = fits() && (n.M * p.bundles >= CUS / 4 || n.P << t.lprlog <= 4096);
+  s.whole = fits() && (n.M * p.bundles >= CUS / 8 || n.P << t.lprlog <= 4096);
   t.ttlog = t.lprlog;
   if (s.whole) {
     while (t.ttlog < 8 && lanes(t.ttlog) > FEW) ++t.ttlog;
-    if (t.ttlog == 8 && lanes(8) > most_of(size, bwd, 256)) t.ttlog = 9;
+    if (t.ttlog == 8 && lanes(8) > most_of(size, bwd, 256, s.pieces)) t.ttlog = 9;
     s.nt = t.ttlog <= 8 ? 256 : 1 << t.ttlog;
+    if (t.ttlog > t.lprlog && t.ttlog < 4) t.ttlog = 4;   // (see Lane::wave_sums)
     s.few = lanes(t.ttlog) <= FEW;
+    s.single = s.pieces == EIGHTS && s.nt <= 512 && lanes(t.ttlog) == 1 && n.M >= 4 * CUS;
     p.segs = 1;
-  } else {
+    // (32-bit offsets of the rows of a workgroup's images)
+    const i64 teams = s.nt >> t.ttlog, ld = n.ldx > n.ldy ? n.ldx : n.ldy;
+    if ((teams * n.P * ld + n.C) * size > 0x7fffffffLL) s.whole = false;
+  }
+  if (!s.whole) {
+    t.ttlog = t.lprlog;
     s.nt = 1024;
     t.ttlog = 10;
     // two workgroups a compute unit, each with two turns of its lanes at least
@@ -509,10 +688,13 @@ Plan plan_of(const Norm& n, bool bwd) {
   }
   p.seg = (n.P + p.segs - 1) / p.segs;
   p.segs = (int)((n.P + p.seg - 1) / p.seg);
-  const i64 teams = s.nt >> t.ttlog, each = (n.M + teams - 1) / teams;
+  const i64 teams = (i64)(s.nt >> t.ttlog) * (s.single ? images_at_once(size, bwd) : 1), each = (n.M + teams - 1) / teams;
   auto bounded = [&](i64 most) { return (int)(each < 1 ? 1 : each < most ? each : most < 1 ? 1 : most); };
   const i64 side = (i64)p.bundles * p.segs;
-  p.slices = bwd ? bounded((s.nt == 256 ? 8 : s.nt == 512 ? 4 : 2) * CUS / side) : bounded((1LL << 22) / side);
+  auto over = [](int d) { return d > 1 ? (unsigned)(((1ULL << 32) + d - 1) / d) : 0u; };
+  p.slices = bounded((s.nt == 256 ? 8 : s.nt == 512 ? 4 : 2) * CUS / side);
+  p.per_bundle = over(p.bundles);
+  p.per_slice = over(p.slices);
   if (bwd) s.sums = align_up((size_t)p.slices * p.segs * n.C * 8, 256);
   if (!s.whole) s.part = align_up((size_t)n.M * n.groups * p.segs * p.sections * 8, 256);
   s.total = s.part + s.sums;
@@ -534,35 +716,41 @@ template <class F> hipError_t by_type(const Norm& p, F&& f) {
 }
 int grid_of(const NormParams& p) { return (p.bundles * p.slices * p.segs + 7) / 8 * 8; }
 
-template <bool BWD, typename T, int F, int NT, int KP, int PHASE, bool FULL> hipError_t run(const NormParams& p, hipStream_t st) {
+template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V> hipError_t run(const NormParams& p, hipStream_t st) {
+  const int turns = p.t.ttlog > 6 ? 2 * IM * (BWD ? 2 : 3) * 4 * (NT / 64 << p.t.nblog) : 0;
   if constexpr (BWD) {
-    constexpr int LDS = NT * 64;
+    constexpr int COLS = NT * 8 * width_of<V>;
     static LdsLimitOnce once;
-    auto* k = &norm_bwd_kernel<T, F, NT, KP, PHASE, FULL>;
-    const hipError_t e = set_lds_limit_once(once, (const void*)k, LDS);
+    auto* k = &norm_bwd_kernel<T, F, NT, KP, IM, PHASE, V>;
+    const hipError_t e = set_lds_limit_once(once, (const void*)k, COLS > 16384 ? COLS : 16384);   // (a turn of 16 waves of 64 groups: 16384)
     if (e != hipSuccess) return e;
-    k<<<grid_of(p), NT, p.sums && PHASE != OUTPUTS ? LDS : 0, st>>>(p);
+    const int cols = p.sums && PHASE != OUTPUTS ? COLS : 0;
+    k<<<grid_of(p), NT, cols > turns ? cols : turns, st>>>(p);
   } else {
-    norm_fwd_kernel<T, F, NT, KP, PHASE, FULL><<<grid_of(p), NT, 0, st>>>(p);
+    norm_fwd_kernel<T, F, NT, KP, IM, PHASE, V><<<grid_of(p), NT, turns, st>>>(p);
   }
   return hipGetLastError();
 }
-template <bool BWD, typename T, int F, bool FULL> hipError_t run_plan(const Plan& s, hipStream_t st) {
+template <bool BWD, typename T, int F, int V> hipError_t run_plan(const Plan& s, hipStream_t st) {
   constexpr int SIZE = sizeof(T), KP = BWD ? STREAM / 2 : STREAM;
   if (!s.whole) {
-    const hipError_t e = run<BWD, T, BWD ? F : (int)CONVBN_NORM_NONE, 1024, KP, SUMS, FULL>(s.p, st);
-    return e != hipSuccess || (BWD && !s.p.n.dx) ? e : run<BWD, T, F, 1024, KP, OUTPUTS, FULL>(s.p, st);
+    const hipError_t e = run<BWD, T, BWD ? F : (int)CONVBN_NORM_NONE, 1024, KP, 1, SUMS, V>(s.p, st);
+    return e != hipSuccess || (BWD && !s.p.n.dx) ? e : run<BWD, T, F, 1024, KP, 1, OUTPUTS, V>(s.p, st);
   }
-  if (s.nt == 1024) return run<BWD, T, F, 1024, FEW, WHOLE, FULL>(s.p, st);
-  if constexpr (FULL) {   // (others are few: they do with the larger kernels)
-    if (s.few) return s.nt == 256 ? run<BWD, T, F, 256, FEW, WHOLE, FULL>(s.p, st) : run<BWD, T, F, 512, FEW, WHOLE, FULL>(s.p, st);
+  if (s.nt == 1024) return run<BWD, T, F, 1024, FEW, 1, WHOLE, V>(s.p, st);
+  if constexpr (V == EIGHTS) {   // (others are rare: they do with the larger kernels)
+    constexpr int IM = images_at_once(SIZE, BWD);
+    if (s.single) return s.nt == 256 ? run<BWD, T, F, 256, 1, IM, WHOLE, V>(s.p, st) : run<BWD, T, F, 512, 1, IM, WHOLE, V>(s.p, st);
+    if (s.few) return s.nt == 256 ? run<BWD, T, F, 256, FEW, 1, WHOLE, V>(s.p, st) : run<BWD, T, F, 512, FEW, 1, WHOLE, V>(s.p, st);
   }
-  return s.nt == 256 ? run<BWD, T, F, 256, most_of(SIZE, BWD, 256), WHOLE, FULL>(s.p, st)
-                     : run<BWD, T, F, 512, most_of(SIZE, BWD, 512), WHOLE, FULL>(s.p, st);
+  return s.nt == 256 ? run<BWD, T, F, 256, most_of(SIZE, BWD, 256, V), 1, WHOLE, V>(s.p, st)
+                     : run<BWD, T, F, 512, most_of(SIZE, BWD, 512, V), 1, WHOLE, V>(s.p, st);
 }
 template <bool BWD> hipError_t run_norm(const Plan& s, hipStream_t st) {
   return by_type(s.p.n, [&](auto t, auto f) {
-    return s.full ? run_plan<BWD, decltype(t), f.value, true>(s, st) : run_plan<BWD, decltype(t), f.value, false>(s, st);
+    using T = decltype(t);
+    return s.pieces == EIGHTS ? run_plan<BWD, T, f.value, EIGHTS>(s, st) : s.pieces == TAIL ? run_plan<BWD, T, f.value, TAIL>(s, st)
+                                                                                            : run_plan<BWD, T, f.value, ONES>(s, st);
   });
 }
 
