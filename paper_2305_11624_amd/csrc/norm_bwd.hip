@@ -11,7 +11,7 @@ hipError_t launch_norm_bwd(const Norm& n, void* ws, hipStream_t st) {
   s.p.sums = params ? sums : nullptr;
   const hipError_t e = n.M ? run_norm<true>(s, st) : hipSuccess;
   if (e != hipSuccess || !params) return e;
-  norm_join_kernel<<<ceil_div(n.C, 64), 1024, 0, st>>>(sums, n.M ? s.p.slices * s.p.segs : 0, n.C, n.dgamma, n.dbeta);
+  norm_join_kernel<<<ceil_div(n.C, 16), 1024, 0, st>>>(sums, n.M ? s.p.slices * s.p.segs : 0, n.C, n.dgamma, n.dbeta);
   return hipGetLastError();
 }
 

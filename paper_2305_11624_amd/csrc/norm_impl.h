@@ -26,6 +26,7 @@ struct NormParams {
   Team t;
   int cg, bundles;      // channels of a group, teams side by side
   unsigned per_bundle, per_slice;   // ceil(2^32 / bundles), ceil(2^32 / slices): exact for the small numbers here; 0: divide by one
+  int linelog;          // neighbouring bundles on a cache line: a power of two
   int span, sections;   // a group of more channels than a workgroup has lanes for: sections of `span` channels, a team each
   int slices;           // workgroups along the images (each takes every slices'th team of images)
   int segs;             // segments of the pixels
@@ -70,12 +71,14 @@ template <typename T, int V> __device__ __forceinline__ Vals<width_of<V>> vals(c
     return {{f.v[0], f.v[1], f.v[2], f.v[3], f.v[4], f.v[5], f.v[6], f.v[7]}};
   }
 }
+// Results leave the caches to what backward reads again: 8192 tokens of 4096 forward 38 us (44 if they stay), backward 42.8 (44.2), 32 x 56 x 56 x 256
+// 27 and 50 (23 and 57.6).
 template <typename T, int V> __device__ __forceinline__ void store_piece(T* p, int n, const Vals<width_of<V>>& f) {
   if constexpr (V == ONES) {
     *p = from_f32<T>(f.v[0]);
   } else {
     if (V == EIGHTS || n == 8) {
-      *reinterpret_cast<Raw8<T>*>(p) = narrow<T>(F8{{f.v[0], f.v[1], f.v[2], f.v[3], f.v[4], f.v[5], f.v[6], f.v[7]}});
+      store8<T, true>(p, 0, 8, F8{{f.v[0], f.v[1], f.v[2], f.v[3], f.v[4], f.v[5], f.v[6], f.v[7]}});
       return;
     }
 #pragma unroll
@@ -106,6 +109,18 @@ __device__ __forceinline__ float across16(float v) {   // + lane ^ 16
 __device__ __forceinline__ float across32(float v) {   // + lane ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Sums over 16 lanes
+template <int N> __device__ __forceinline__ void row_sums(float (&s)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] += dpp<0x121>(s[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] += dpp<0x122>(s[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] += dpp<0x124>(s[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] += dpp<0x128>(s[i]);
 }
 
 // A lane's place
@@ -195,6 +210,28 @@ template <int IM> __device__ __forceinline__ void team_moments(const Lane& l, co
     }
   }
   __syncthreads();
+  if (t.nblog == 0) {   // one group: 16 lanes read a wave's each
+    const int w = threadIdx.x & 15;
+    float mean[IM];
+#pragma unroll
+    for (int i = 0; i < IM; ++i) {
+      const float* o = buf + (i * entries + l.first_wave() + w) * 3;
+      a[i] = w < l.waves ? Moments{o[0], o[1], o[2]} : Moments{0.f, 0.f, 0.f};
+      s[2 * i] = a[i].n;
+      s[2 * i + 1] = a[i].n * a[i].mean;
+    }
+    row_sums(s);
+#pragma unroll
+    for (int i = 0; i < IM; ++i) {
+      mean[i] = s[2 * i] > 0.f ? s[2 * i + 1] / s[2 * i] : 0.f;
+      const float e = a[i].mean - mean[i];
+      q[i] = a[i].m2 + a[i].n * e * e;
+    }
+    row_sums(q);
+#pragma unroll
+    for (int i = 0; i < IM; ++i) a[i] = {s[2 * i], mean[i], q[i]};
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < IM; ++i) {
     float n = 0.f, sum = 0.f, m2 = 0.f;
@@ -221,6 +258,13 @@ template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const
     for (int i = 0; i < 2 * IM; ++i) buf[l.slot(t, l.wave) * 2 * IM + i] = s[i];
   }
   __syncthreads();
+  if (t.nblog == 0) {
+    const int w = threadIdx.x & 15;
+#pragma unroll
+    for (int i = 0; i < 2 * IM; ++i) s[i] = w < l.waves ? buf[(l.first_wave() + w) * 2 * IM + i] : 0.f;
+    row_sums(s);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 2 * IM; ++i) s[i] = 0.f;
   for (int w = 0; w < l.waves; ++w)
@@ -301,11 +345,13 @@ template <typename T, int PHASE> struct Rows {
   }
 };
 
-// A workgroup's place: bundles of channels run fastest, and each XCD gets a run of them, so that neighbours share what they read in its cache
+// A workgroup's place: bundles of channels run fastest.  Neighbours whose parts of a pixel lie on the same cache line are on the same XCD; apart from
+// that neighbours are on different ones, so that few images keep them all busy.
 struct Place { int bundle, slice, seg; };
 __device__ __forceinline__ bool place_of(const NormParams& p, Place* at) {
-  const int total = p.bundles * p.slices * p.segs, run = (total + 7) >> 3, s = (int)blockIdx.x >> 3, id = ((int)blockIdx.x & 7) * run + s;
-  if (s >= run || id >= total) return false;
+  const int total = p.bundles * p.slices * p.segs, s = (int)blockIdx.x >> 3, in = s & ((1 << p.linelog) - 1);
+  const int id = ((s - in) << 3) + (((int)blockIdx.x & 7) << p.linelog) + in;
+  if (id >= total) return false;
   const int rest = p.per_bundle ? (int)__umulhi((unsigned)id, p.per_bundle) : id;
   at->bundle = id - rest * p.bundles;
   at->seg = p.per_slice ? (int)__umulhi((unsigned)rest, p.per_slice) : rest;
@@ -589,24 +635,26 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   }
 }
 
-// dgamma and dbeta: what `rows` workgroups found, [rows][C][2], in a fixed order; 16 threads a channel
+// dgamma and dbeta: what `rows` workgroups found, [rows][C][2], in a fixed order; 64 threads a channel
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float* sums, int rows, int C, float* dgamma, float* dbeta) {
-  __shared__ float2 meet[16][64];
-  const int at = threadIdx.x & 63, q = threadIdx.x >> 6, c = blockIdx.x * 64 + at;
+  __shared__ float2 meet[16][16];
+  const int at = threadIdx.x & 15, q = threadIdx.x >> 4, c = blockIdx.x * 16 + at;
   float2 v = make_float2(0.f, 0.f);
   if (c < C) {
-#pragma unroll 4
-    for (int r = q; r < rows; r += 16) {
+#pragma unroll 8
+    for (int r = q; r < rows; r += 64) {
       const float2 w = *reinterpret_cast<const float2*>(sums + ((i64)r * C + c) * 2);
       v.x += w.x;
       v.y += w.y;
     }
   }
-  meet[q][at] = v;
+  v = make_float2(across32(across16(v.x)), across32(across16(v.y)));
+  if ((threadIdx.x & 63) < 16) meet[threadIdx.x >> 6][at] = v;
   __syncthreads();
   if (q || c >= C) return;
+  v = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int i = 1; i < 16; ++i) {
+  for (int i = 0; i < 16; ++i) {
     v.x += meet[i][at].x;
     v.y += meet[i][at].y;
   }
@@ -650,13 +698,14 @@ Plan plan_of(const Norm& n, bool bwd) {
   t.m = ceil_div(p.span, width);
   t.mlog = log2_up(t.m);
   const int glog = log2_up(n.groups);
-  // groups side by side until a pixel's part is 64 bytes, or until a wave is full of pieces of few channels
+  // groups side by side until a pixel's part is 64 bytes, or until a wave is full of pieces of few channels (32 x 56 x 56 x 256, parts of 32 bytes: forward
+  // 48.6 us instead of 24; backward in one launch 53 us, in two with parts of 64 bytes 50)
   while (t.nblog < glog && t.mlog + t.nblog < 6 && (p.cg << t.nblog) * size < 64) ++t.nblog;
   auto lanes = [&](int log) { return (n.P + (1LL << (log - t.lprlog)) - 1) >> (log - t.lprlog); };   // pieces of a lane
   auto fits = [&] { return p.sections == 1 && (t.lprlog <= 9 ? lanes(9) <= most_of(size, bwd, 512, s.pieces) : n.P <= FEW); };
   t.lprlog = t.mlog + t.nblog;
-  // (backward holds twice as much: pixels' parts of 32 bytes if that keeps it in one launch)
-  while (!fits() && t.nblog > 0 && (p.cg << (t.nblog - 1)) * size >= 32) {
+  // (few numbers, which the caches hold: one launch counts more than whole parts)
+  while (!fits() && t.nblog > 0 && n.M * n.P * n.C <= 1 << 20) {
     --t.nblog;
     --t.lprlog;
   }
@@ -692,7 +741,8 @@ Plan plan_of(const Norm& n, bool bwd) {
   auto bounded = [&](i64 most) { return (int)(each < 1 ? 1 : each < most ? each : most < 1 ? 1 : most); };
   const i64 side = (i64)p.bundles * p.segs;
   auto over = [](int d) { return d > 1 ? (unsigned)(((1ULL << 32) + d - 1) / d) : 0u; };
-  p.slices = bounded((s.nt == 256 ? 8 : s.nt == 512 ? 4 : 2) * CUS / side);
+  p.slices = bounded((s.nt == 256 ? 8 : 2) * CUS / side);
+  while (p.bundles > 1 && p.linelog < 3 && (p.span << t.nblog << p.linelog) * size < 128) ++p.linelog;
   p.per_bundle = over(p.bundles);
   p.per_slice = over(p.slices);
   if (bwd) s.sums = align_up((size_t)p.slices * p.segs * n.C * 8, 256);
@@ -714,7 +764,10 @@ template <class F> hipError_t by_type(const Norm& p, F&& f) {
   };
   return p.dtype == CONVBN_BF16 ? with(bf16_t{}) : with(float{});
 }
-int grid_of(const NormParams& p) { return (p.bundles * p.slices * p.segs + 7) / 8 * 8; }
+int grid_of(const NormParams& p) {
+  const int unit = 8 << p.linelog;
+  return (p.bundles * p.slices * p.segs + unit - 1) / unit * unit;
+}
 
 template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V> hipError_t run(const NormParams& p, hipStream_t st) {
   const int turns = p.t.ttlog > 6 ? 2 * IM * (BWD ? 2 : 3) * 4 * (NT / 64 << p.t.nblog) : 0;
