@@ -6,8 +6,8 @@
 //
 // F32: operands are split into three bf16 parts that add up to all 24 bits, and the six products of parts that are not below 2^-24 of the whole are summed
 // in fp32: nothing is rounded below that.
+#include "grads.h"
 #include "mm_tile.h"
-#include "rows_prep.h"
 
 namespace convbn {
 
@@ -52,24 +52,30 @@ template <typename T, int KIND> struct GluOut {
   }
 };
 
-// ---- dh and its column sums ----
-// A workgroup takes 256 columns of either half, a thread eight of them and every 16th row of a slice; the sums of several slices are joined in
-// order by a later launch.
+// ---- in front of the gradients: dh and its column sums, copies of x and W where they are not read in place ----
+// dh: workgroups of 256 columns of either half and a slice of the rows, a thread eight columns of every 16th row.
+constexpr int NT = 32 * SUM_ROWS;
 struct DGate {
   i64 M, ldz, per;
-  int N, W2;
+  int N, W2, across, blocks;
   const void* h; const void* dy;
   bf16_t* dh; i64 plane;      // null: not wanted
   float* sums;                // [slices][2 N] or null
 };
-template <typename T, typename H, int KIND> __global__ __launch_bounds__(32 * SUM_ROWS) void glu_dgate_kernel(DGate p) {
+template <typename T, typename H, int KIND> __global__ __launch_bounds__(NT) void glu_prep_kernel(DGate p, RowsCopy x, unsigned nx, RowsCopy w) {
   __shared__ float meet[SUM_ROWS][256 + 8];
-  const int c = (threadIdx.x & 31) * 8, r = threadIdx.x >> 5, n = blockIdx.x * 256 + c;
-  const i64 beg = (i64)blockIdx.y * p.per, end = beg + p.per < p.M ? beg + p.per : p.M;
+  if ((int)blockIdx.x >= p.blocks) {
+    const unsigned wg = blockIdx.x - p.blocks;
+    if (wg < nx) rows_copy<T, NT>(x, wg, nx);
+    else rows_copy<T, NT>(w, wg - nx, gridDim.x - p.blocks - nx);
+    return;
+  }
+  const int slice = (int)blockIdx.x / p.across, n0 = ((int)blockIdx.x - slice * p.across) * 256, n = n0 + (threadIdx.x & 31) * 8;
+  const i64 beg = (i64)slice * p.per, end = beg + p.per < p.M ? beg + p.per : p.M;
   F8 sum[2] = {};
   if (n < p.N) {
 #pragma unroll 2
-    for (i64 m = beg + r; m < end; m += SUM_ROWS) {
+    for (i64 m = beg + (threadIdx.x >> 5); m < end; m += SUM_ROWS) {
       const H* h = static_cast<const H*>(p.h) + m * 2 * p.N;
       const F8 g = load8<H>(h, n, p.N), u = load8<H>(h + p.N, n, p.N), dy = load8<T>(static_cast<const T*>(p.dy) + m * p.ldz, n, p.N);
       F8 d[2];
@@ -81,43 +87,32 @@ template <typename T, typename H, int KIND> __global__ __launch_bounds__(32 * SU
         d[1].v[i] = dy.v[i] * f;
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int y = 0; y < 2; ++y) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[x].v[i] += d[x].v[i];
+        for (int i = 0; i < 8; ++i) sum[y].v[i] += d[y].v[i];
         if (!p.dh) continue;
-        bf16_t* out = p.dh + m * p.W2 + x * p.N;
-        const int width = x ? p.W2 - p.N : p.N;   // (u's last piece clears what is behind it)
+        bf16_t* out = p.dh + m * p.W2 + y * p.N;
+        const int width = y ? p.W2 - p.N : p.N;   // (u's last piece clears what is behind it)
         if constexpr (sizeof(T) == 2) {
-          store8<bf16_t>(out, n, width, d[x]);
+          store8<bf16_t>(out, n, width, d[y]);
         } else {
           F8 part[3];
-          split3(d[x], part);
+          split3(d[y], part);
 #pragma unroll
-          for (int y = 0; y < 3; ++y) store8<bf16_t>(out + y * p.plane, n, width, part[y]);
+          for (int i = 0; i < 3; ++i) store8<bf16_t>(out + i * p.plane, n, width, part[i]);
         }
       }
     }
   }
   if (!p.sums) return;
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) meet[r][c + e] = sum[x].v[e];
-    __syncthreads();
-    const int at = threadIdx.x, col = blockIdx.x * 256 + at;
-    if (at < 256 && col < p.N) {
-      float v = 0.f;
-#pragma unroll
-      for (int i = 0; i < SUM_ROWS; ++i) v += meet[i][at];
-      p.sums[(i64)blockIdx.y * 2 * p.N + x * p.N + col] = v;
-    }
-  }
+  for (int y = 0; y < 2; ++y) meet_sums(sum[y], meet, n0, p.N, p.sums + (i64)slice * 2 * p.N + y * p.N);
 }
+
 // ---- gradients ----
 // What a call needs of the workspace, in this order, and its operands
 struct Plan {
-  MmPlan fwd, dx, dw;
+  MmPlan fwd;
   int slices;
   size_t h, dh, x, W, part, sums, total;
 };
@@ -129,12 +124,10 @@ Plan plan_of(const Glu& p, bool bwd) {
   s.W = glu_in_place(p.dtype, p.K, p.K) ? 0 : align_up((size_t)pl * 2 * p.N * K8 * 2, 256);
   s.part = mm_scratch(s.fwd, p.M, 2 * round8(p.N));
   if (bwd) {
-    s.dx = mm_plan(p.M, p.K, pairs * chunks(2 * (i64)p.N));
-    s.dw = mm_plan(2 * (i64)p.N, p.K, pairs * chunks(p.M));
     s.slices = row_slices(p.M, p.N);
     s.h = align_up((size_t)p.M * 2 * p.N * 4, 256);   // (a descriptor does not say whether h is kept)
     s.dh = align_up((size_t)pl * p.M * W2 * 2, 256);
-    const size_t both = mm_scratch(s.dx, p.M, K8) + mm_scratch(s.dw, 2 * (i64)p.N, K8);
+    const size_t both = grads_scratch(p.M, 2 * (i64)p.N, p.K, pairs);
     s.part = s.part > both ? s.part : both;
     s.sums = align_up((size_t)s.slices * 2 * p.N * 4, 256);
   }
@@ -174,51 +167,43 @@ template <typename T, int KIND> hipError_t fwd_t(const Glu& p, char* ws, hipStre
 }
 
 template <typename T, int KIND> hipError_t bwd_t(const Glu& p, char* ws, hipStream_t st) {
-  constexpr int PAIRS = sizeof(T) == 2 ? 1 : 6;
   const Plan s = plan_of(p, true);
-  const bool again = !p.hk && p.M, want_dx = p.dx && p.M;
-  const Operands o = operands_of(p, s, ws, p.M && (again || p.dW), again || want_dx);
-  hipError_t e = launch_rows_copies(p.dtype, o.cx, o.cw, st);
-  if (e != hipSuccess) return e;
+  const bool again = !p.hk && p.M, want_dx = p.dx && p.M, want_dW = p.dW && p.M;
+  const Operands o = operands_of(p, s, ws, again || want_dW, again || want_dx);
   const void* h = p.hk;
   if (again) {
     Glu q = p;
     q.y = nullptr;
     q.h = ws;
     q.h32 = true;
-    e = project<T, KIND>(q, s, o, ws, st);
+    hipError_t e = launch_rows_copies(p.dtype, o.cx, o.cw, st);
+    if (e == hipSuccess) e = project<T, KIND>(q, s, o, ws, st);
     if (e != hipSuccess) return e;
     h = ws;
   }
-  float* const part = reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W);
   float* const sums = reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W + s.part);
   const int W2 = round8(2 * p.N);
   bf16_t* const dh = reinterpret_cast<bf16_t*>(ws + s.h);
-  DGate d = {p.M, p.ldz, (p.M + s.slices - 1) / s.slices, p.N, W2, h, p.dy, want_dx || p.dW ? dh : nullptr, p.M * W2,
-             !p.db ? nullptr : s.slices > 1 ? sums : p.db};
-  const dim3 grid(ceil_div(p.N, 256), s.slices);
-  if (p.b || again) glu_dgate_kernel<T, float, KIND><<<grid, 32 * SUM_ROWS, 0, st>>>(d);
-  else glu_dgate_kernel<T, T, KIND><<<grid, 32 * SUM_ROWS, 0, st>>>(d);
-  e = hipGetLastError();
-  if (e == hipSuccess && p.db && s.slices > 1) e = launch_sums(sums, s.slices, 2 * p.N, p.db, st);
-  const RowsOp rows = {(const uint8_t*)dh, 2 * W2, 2 * p.M * W2, 2 * W2};
-  if (e == hipSuccess && want_dx) {
-    MmParams m = {};
-    m.a = rows; m.b = o.W;
-    m.I = p.M; m.J = p.K; m.R = 2 * (i64)p.N;
-    m.plane_ch = chunks(m.R);
-    m.nch = PAIRS * m.plane_ch;
-    e = mm_launch<OpBf16, false, true, false, PAIRS>(m, s.dx, part, GradOut<T>{p.dx, p.add, p.ldx, p.K}, st);
+  // (rows that are not summed go in slices of a turn each)
+  const int slices = p.db ? s.slices : (int)(p.M > SUM_ROWS << 16 ? 1 << 16 : (p.M + SUM_ROWS - 1) / SUM_ROWS);
+  DGate d = {p.M, p.ldz, slices ? (p.M + slices - 1) / slices : 0, p.N, W2, ceil_div(p.N, 256), 0, h, p.dy, want_dx || want_dW ? dh : nullptr, p.M * W2,
+             !p.db ? nullptr : slices > 1 ? sums : p.db};
+  d.blocks = d.across * slices;
+  const RowsCopy cx = again ? RowsCopy{} : o.cx, cw = again ? RowsCopy{} : o.cw;
+  const unsigned nx = piece_blocks<NT>(cx.rows, cx.width, cx.out), nw = piece_blocks<NT>(cw.rows, cw.width, cw.out), blocks = d.blocks + nx + nw;
+  if (blocks) {
+    if (p.b || again) glu_prep_kernel<T, float, KIND><<<blocks, NT, 0, st>>>(d, cx, nx, cw);
+    else glu_prep_kernel<T, T, KIND><<<blocks, NT, 0, st>>>(d, cx, nx, cw);
   }
-  if (e == hipSuccess && p.dW) {
-    MmParams m = {};
-    m.a = rows; m.b = o.x;
-    m.I = 2 * (i64)p.N; m.J = p.K; m.R = p.M;
-    m.plane_ch = chunks(p.M);
-    m.nch = PAIRS * m.plane_ch;
-    e = mm_launch<OpBf16, true, true, false, PAIRS>(m, s.dw, part + mm_scratch(s.dx, p.M, round8(p.K)) / 4, GradOut<T>{p.dW, nullptr, p.K, p.K}, st);
-  }
-  return e;
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  Grads g = {};
+  g.M = p.M; g.N = 2 * (i64)p.N; g.K = p.K; g.ldx = p.ldx; g.pairs = sizeof(T) == 2 ? 1 : 6; g.dtype = p.dtype;
+  g.a = {(const uint8_t*)dh, 2 * W2, 2 * p.M * W2, 2 * W2};
+  g.w = o.W; g.x = o.x;
+  g.dx = p.dx; g.add = p.add; g.dW = p.dW;
+  g.sum = {sums, slices, 2 * p.N, p.db && slices > 1 ? p.db : nullptr};
+  return launch_grads(g, reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W), st);
 }
 
 // Calls f(T, KIND) with the gate's types

@@ -5,7 +5,7 @@
 // pieces are exchanged by bits 1-3 of the row, so that 16 lanes reading a column of pieces meet distinct banks.  Where they run across it (TA, TB: a row
 // for each k; the gradients' operands), they pass as they lie, 64 rows of the tile's width at a time, and a transposing load turns them.
 #pragma once
-#include "f8_code.h"
+#include "rows_prep.h"
 
 namespace convbn {
 namespace {
@@ -13,9 +13,6 @@ namespace {
 constexpr int KB = 128;                 // bytes of a row at a time: a whole cache line
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-// An operand: rows of `width` bytes, a multiple of 16, `ld` bytes apart; several planes (parts of fp32 numbers) `plane` bytes apart
-struct RowsOp { const uint8_t* p; i64 ld, plane; i64 width; };
 
 struct MmParams {
   RowsOp a, b;
@@ -130,7 +127,9 @@ template <class Cfg, bool TR, bool HALVES> struct Side {
 
 // One tile.  DUAL: b's rows are two halves of J, and each wave gets the same columns of both: 32 of the first, 32 of the second, in turn.
 // out(i, j, cols, v): eight sums from column j < J of row i < I on, cols = out.columns(j); DUAL: out(i, j, cols, g, u).
-template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, bool SPLIT, class OUT>
+// SPLIT: whether the sum is, EITHER: p says (code for both: 1 % of a large product).
+enum { ENTIRE, SPLITS, EITHER };
+template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, int SPLIT, class OUT>
 __device__ __forceinline__ void mm_tile(const MmParams& p, const int wg, unsigned char* const smem, const OUT& out) {
   constexpr int TI = Cfg::TI, TJ = TI, WI = Cfg::WI, WJ = Cfg::WJ, NB = Cfg::NB, G = Cfg::G, FI = WI / 32, FJ = WJ / 32, CPH = Cfg::CPH;
   constexpr bool F8OP = Cfg::Op::SCALED;
@@ -323,7 +322,7 @@ __device__ __forceinline__ void mm_tile(const MmParams& p, const int wg, unsigne
   };
   const int c8 = (lane % LPR) * 8, col = DUAL ? (c8 >> 5) * 64 + (c8 & 31) : c8;   // (DUAL: of the first half; the second's is 32 further)
   const int n = j0 + (DUAL ? wj / 2 : wj) + c8, J8 = (p.J + 7) & ~7;
-  const auto cols = out.columns(SPLIT || n >= p.J ? 0 : n);
+  const auto cols = out.columns(n >= p.J ? 0 : n);
 #pragma unroll
   for (int i = 0; i < FI; ++i) {
 #pragma unroll
@@ -350,7 +349,7 @@ __device__ __forceinline__ void mm_tile(const MmParams& p, const int wg, unsigne
             for (int e = 0; e < 4; ++e) v[x].v[h + e] += w[e];
           }
       if (m >= p.I || n >= p.J) continue;
-      if constexpr (SPLIT) {
+      if (SPLIT == SPLITS || (SPLIT == EITHER && p.splits > 1)) {
 #pragma unroll
         for (int x = 0; x < (DUAL ? 2 : 1); ++x) store8<float>(p.part + (split * p.I + m) * (DUAL ? 2 * J8 : J8) + x * J8, n, J8, v[x]);
       } else if constexpr (DUAL) {
@@ -363,32 +362,19 @@ __device__ __forceinline__ void mm_tile(const MmParams& p, const int wg, unsigne
   }
 }
 
-template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, bool SPLIT, class OUT>
+template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, int SPLIT, class OUT>
 __global__ __launch_bounds__(Cfg::NT) void mm_kernel(MmParams p, OUT out) {
   extern __shared__ __align__(16) unsigned char smem[];
   mm_tile<Cfg, TA, TB, DUAL, PAIRS, SPLIT>(p, (int)blockIdx.x, smem, out);
 }
 
-int round8(int n) { return (n + 7) & ~7; }
 int chunks(i64 n) { return (int)((n + KB / 2 - 1) / (KB / 2)); }   // of bf16 numbers
 
-// Where a gradient goes: rows ld apart, an addend laid out like them on top
-template <typename T> struct GradOut {
-  void* c; const void* add;
-  i64 ld;
-  int J;
-  struct None {};
-  __device__ __forceinline__ None columns(int) const { return {}; }
-  __device__ __forceinline__ void operator()(i64 i, int j, const None&, const F8& v) const {
-    store8_plus<T>(static_cast<T*>(c) + i * ld, add ? static_cast<const T*>(add) + i * ld : nullptr, j, J, v);
-  }
-};
-
 // The sums of the splits, in their order, eight columns a thread
-template <bool DUAL, class OUT> __global__ __launch_bounds__(256) void mm_join_kernel(MmParams p, OUT out) {
+template <bool DUAL, class OUT> __device__ __forceinline__ void mm_join(const MmParams& p, const OUT& out, unsigned wg, unsigned wgs) {
   const int oct = (p.J + 7) >> 3, W = (DUAL ? 2 : 1) * oct * 8;
   const i64 total = p.I * oct;
-  for (i64 x = (i64)blockIdx.x * 256 + threadIdx.x; x < total; x += (i64)gridDim.x * 256) {
+  for (i64 x = (i64)wg * 256 + threadIdx.x; x < total; x += (i64)wgs * 256) {
     const i64 m = x / oct;
     const int n = (int)(x - m * oct) * 8;
     F8 v[2] = {};
@@ -405,68 +391,84 @@ template <bool DUAL, class OUT> __global__ __launch_bounds__(256) void mm_join_k
     else out(m, n, cols, v[0]);
   }
 }
+template <bool DUAL, class OUT> __global__ __launch_bounds__(256) void mm_join_kernel(MmParams p, OUT out) {
+  mm_join<DUAL>(p, out, blockIdx.x, gridDim.x);
+}
+unsigned join_blocks(const MmParams& p) {
+  const i64 n = (p.I * ((p.J + 7) >> 3) + 255) / 256;
+  return (unsigned)(n < 65536 ? n : 65536);
+}
 
 constexpr int MM_CUS = 256;
 
 // The cheapest of tiles of 64, 128 and 256, and of 1 to 64 parts of the channel sum, by what was measured in us: a launch 2, every round of
 // workgroups 2, 3 or 6 and, for each chunk, 0.18, 0.47 or 1.85 with a workgroup alone on its compute unit, 0.37 or 1.2 with two (64, 128);
-// parts cost another launch and their sums' way through memory.
-struct MmPlan { int tile, splits, per; };
+// parts cost another launch and their sums' way through memory.  us of the choice and of others: along the sum 1568 x 512, 4096 64 16.3, 128 33, in four parts
+// 20.9; 1568 x 2048, 512 128 8.5, 64 11.9, 256 16; 6272 x 1024, 1024 128 20.5, 256 26, 64 34; across it 4096 x 512, 1568 64 14.2, 128 17.3; 144 x 136, 4662 64 in
+// 15 parts 10.2, whole 18.5; both halves 6272 x 2 x 1024, 1024 256 32, 128 36; 64 x 2 x 8192, 2048 64 13.4, 128 19.
+struct MmPlan { int tile, splits, per; double us; };
+double mm_alone_us(int tile, int per) { return tile == 64 ? 2 + 0.18 * per : 3 + 0.47 * per; }   // a workgroup, alone on its compute unit
+i64 mm_tiles(i64 I, i64 J, i64 t) { return ((I + t - 1) / t) * ((J + t - 1) / t); }
 MmPlan mm_plan(i64 I, i64 J, int nch) {   // J: rows of b
-  MmPlan pl = {64, 1, nch};
+  MmPlan pl = {64, 1, nch, 0};
   if (I == 0) return pl;
-  auto tiles = [&](i64 t) { return ((I + t - 1) / t) * ((J + t - 1) / t); };
   double best = 1e30;
   for (int tile = 64; tile <= 256; tile *= 2)
     for (int s = 1; s <= 64 && s <= nch; s *= 2) {
       const int per = ceil_div(nch, s), parts = ceil_div(nch, per);
-      const double w = (double)tiles(tile) * parts;
+      const double w = (double)mm_tiles(I, J, tile) * parts;
       const bool alone = w <= MM_CUS;
       const double rounds = (double)(i64)(tile == 256 ? (w + 255) / 256 : (w + 511) / 512);
-      const double chunk = tile == 256 ? 1.85 : tile == 128 ? (alone ? 0.47 : 1.2) : alone ? 0.18 : 0.37;
-      const double us = 2 + rounds * ((tile == 256 ? 6 : tile == 128 ? 3 : 2) + chunk * per) + (parts > 1 ? 4.2 + 2e-6 * parts * (double)I * J : 0);
+      const double one = tile == 256 ? 6 + 1.85 * per : alone ? mm_alone_us(tile, per) : tile == 128 ? 3 + 1.2 * per : 2 + 0.37 * per;
+      const double us = 2 + rounds * one + (parts > 1 ? 4.2 + 2e-6 * parts * (double)I * J : 0);
       if (us < best) {
         best = us;
-        pl = {tile, parts, per};
+        pl = {tile, parts, per, us};
       }
     }
   return pl;
 }
 size_t mm_scratch(const MmPlan& pl, i64 I, i64 W) { return pl.splits > 1 ? align_up((size_t)pl.splits * I * W * 4, 256) : 0; }
 
-template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, bool SPLIT, class OUT> hipError_t mm_launch_cfg(const MmParams& p, const OUT& out, hipStream_t st) {
+int mm_grid(const MmParams& p) { return (p.nti * p.ntj * p.splits + 7) / 8 * 8; }
+bool mm_alone(const MmParams& p) { return p.nti * p.ntj * p.splits <= MM_CUS; }   // one workgroup a compute unit: its copies are all that hides the way to memory
+// The plan's tiles and splits; `part` where it has several of these
+void mm_place(MmParams* p, const MmPlan& pl, float* part, bool dual) {
+  p->splits = pl.splits; p->per = pl.per; p->part = part;
+  p->nti = (int)((p->I + pl.tile - 1) / pl.tile);
+  p->ntj = ceil_div(dual ? 2 * p->J : p->J, pl.tile);
+}
+template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, int SPLIT, class OUT> hipError_t mm_launch_as(const MmParams& p, const OUT& out, hipStream_t st) {
   static LdsLimitOnce once;
   auto* k = &mm_kernel<Cfg, TA, TB, DUAL, PAIRS, SPLIT, OUT>;
   const hipError_t e = set_lds_limit_once(once, (const void*)k, Cfg::LDS);
   if (e != hipSuccess) return e;
-  k<<<(p.nti * p.ntj * p.splits + 7) / 8 * 8, Cfg::NT, Cfg::LDS, st>>>(p, out);
+  k<<<mm_grid(p), Cfg::NT, Cfg::LDS, st>>>(p, out);
   return hipGetLastError();
 }
-template <class Op, bool TA, bool TB, bool DUAL, int PAIRS, bool SPLIT, class OUT> hipError_t mm_by_tile(int tile, const MmParams& p, const OUT& out, hipStream_t st) {
-  const bool alone = p.nti * p.ntj * p.splits <= MM_CUS;   // one workgroup a compute unit: its copies are all that hides the way to memory
+template <class Cfg, bool TA, bool TB, bool DUAL, int PAIRS, class OUT> hipError_t mm_launch_cfg(const MmParams& p, const OUT& out, hipStream_t st) {
+  return p.splits > 1 ? mm_launch_as<Cfg, TA, TB, DUAL, PAIRS, SPLITS>(p, out, st) : mm_launch_as<Cfg, TA, TB, DUAL, PAIRS, ENTIRE>(p, out, st);
+}
+template <class Op, bool TA, bool TB, bool DUAL, int PAIRS, class OUT> hipError_t mm_by_tile(int tile, const MmParams& p, const OUT& out, hipStream_t st) {
+  const bool alone = mm_alone(p);
   // (all of LDS, where scales do not need a part of it.  us, products of 8192 x 8192, 4096 with both halves and of 8192 x 16384, 4096 along and across:
   // waves of 128 x 64 with five halves 892, 834, 809; with four 915, 876, 868; of 64 x 128 924, 833, 809; four of 128 x 128 996, 896, 857; in 8-bit
   // floating point 8192 x 8192, 4096 waves of 64 x 128 228, four of 128 x 128 273.  Bound by the matrix pipe and by LDS, each busy for half of the time
   // or more, at the clock that the power allows: the library takes 793, 878 and 987 for the three.)
   constexpr int WIDTH = Op::SCALED ? 64 : 128;
-  if (tile == 256) return mm_launch_cfg<MmCfg<Op, 256, WIDTH, 192 - WIDTH, Op::SCALED ? 4 : 5, 1>, TA, TB, DUAL, PAIRS, SPLIT>(p, out, st);
+  if (tile == 256) return mm_launch_cfg<MmCfg<Op, 256, WIDTH, 192 - WIDTH, Op::SCALED ? 4 : 5, 1>, TA, TB, DUAL, PAIRS>(p, out, st);
   if (tile == 128)
-    return alone ? mm_launch_cfg<MmCfg<Op, 128, 32, 64, 8, 1>, TA, TB, DUAL, PAIRS, SPLIT>(p, out, st)
-                 : mm_launch_cfg<MmCfg<Op, 128, 64, 64, 4, 1>, TA, TB, DUAL, PAIRS, SPLIT>(p, out, st);
+    return alone ? mm_launch_cfg<MmCfg<Op, 128, 32, 64, 8, 1>, TA, TB, DUAL, PAIRS>(p, out, st)
+                 : mm_launch_cfg<MmCfg<Op, 128, 64, 64, 4, 1>, TA, TB, DUAL, PAIRS>(p, out, st);
   constexpr int WJ = DUAL ? 64 : 32;   // (32 columns of either half)
-  return alone ? mm_launch_cfg<MmCfg<Op, 64, 32, WJ, 8, 2>, TA, TB, DUAL, PAIRS, SPLIT>(p, out, st)
-               : mm_launch_cfg<MmCfg<Op, 64, 32, WJ, 8, 1>, TA, TB, DUAL, PAIRS, SPLIT>(p, out, st);
+  return alone ? mm_launch_cfg<MmCfg<Op, 64, 32, WJ, 8, 2>, TA, TB, DUAL, PAIRS>(p, out, st)
+               : mm_launch_cfg<MmCfg<Op, 64, 32, WJ, 8, 1>, TA, TB, DUAL, PAIRS>(p, out, st);
 }
-// p without tiles and splits; `part` where pl has several
 template <class Op, bool TA, bool TB, bool DUAL, int PAIRS, class OUT> hipError_t mm_launch(MmParams p, const MmPlan& pl, float* part, const OUT& out, hipStream_t st) {
-  p.splits = pl.splits; p.per = pl.per; p.part = part;
-  p.nti = (int)((p.I + pl.tile - 1) / pl.tile);
-  p.ntj = ceil_div(DUAL ? 2 * p.J : p.J, pl.tile);
-  if (pl.splits == 1) return mm_by_tile<Op, TA, TB, DUAL, PAIRS, false>(pl.tile, p, out, st);
-  const hipError_t e = mm_by_tile<Op, TA, TB, DUAL, PAIRS, true>(pl.tile, p, out, st);
-  if (e != hipSuccess) return e;
-  const i64 blocks = (p.I * ((p.J + 7) >> 3) + 255) / 256;
-  mm_join_kernel<DUAL><<<(int)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(p, out);
+  mm_place(&p, pl, part, DUAL);
+  const hipError_t e = mm_by_tile<Op, TA, TB, DUAL, PAIRS>(pl.tile, p, out, st);
+  if (e != hipSuccess || pl.splits == 1) return e;
+  mm_join_kernel<DUAL><<<join_blocks(p), 256, 0, st>>>(p, out);
   return hipGetLastError();
 }
 
