@@ -524,7 +524,7 @@ convbn_status convbn_qgate_bwd(const convbn_qdesc *desc, const void *h_codes, co
  *   backward   dx[m,k] = sum_n dz[m,n] w8[n,k]     dW[n,k] = sum_m dz[m,n] x8[m,k]     db[n] = sum_m dz[m,n]
  * Backward is the gradient of the product of the two rounded operands; the rounding itself passes it on unchanged.  dz is not rounded: bf16
  * gradients meet x8 and w8 as they are, fp32 ones in three bf16 parts that add up to them.  Sums are fp32, with one exception: forward with
- * dtype BF16 and more than 32 rows adds the eight products of neighbouring channels 8 i .. 8 i + 7 with 13 bits below the leading bit of the
+ * dtype BF16 and more than 16 rows (or fewer long ones) may add the eight products of neighbouring channels 8 i .. 8 i + 7 with 13 bits below the leading bit of the
  * largest (the matrix instruction for these codes; what it drops is below 7 2^-13 of that product, and 2^-15 of the sum of all sizes on average).
  *
  * Strides, addends, alignment, limits, empty calls and the meaning of NULL are those of the 8-bit rows; scales are 4-byte aligned. */

@@ -150,6 +150,7 @@ Operands operands_of(const Glu& p, const Plan& s, char* ws, bool want_x, bool wa
 }
 
 template <typename T, int KIND> hipError_t project(const Glu& p, const Plan& s, const Operands& o, char* ws, hipStream_t st) {
+  if (glu_few_taken(p.M, p.K, p.dtype)) return launch_glu_few(p, st);
   constexpr int PAIRS = sizeof(T) == 2 ? 1 : 6;
   MmParams m = {};
   m.a = o.x; m.b = o.W;
@@ -160,6 +161,7 @@ template <typename T, int KIND> hipError_t project(const Glu& p, const Plan& s, 
 }
 
 template <typename T, int KIND> hipError_t fwd_t(const Glu& p, char* ws, hipStream_t st) {
+  if (glu_few_taken(p.M, p.K, p.dtype)) return launch_glu_few(p, st);
   const Plan s = plan_of(p, false);
   const Operands o = operands_of(p, s, ws, true, true);
   const hipError_t e = launch_rows_copies(p.dtype, o.cx, o.cw, st);
@@ -215,7 +217,9 @@ template <class F> hipError_t by_gate(const Glu& p, F&& f) {
 }  // namespace
 
 bool glu_in_place(int dtype, int K, i64 ld) { return dtype == CONVBN_BF16 && K % 8 == 0 && ld % 8 == 0 && ld <= 1 << 20; }
-size_t glu_scratch(const Glu& p, int pass) { return plan_of(p, pass == CONVBN_PASS_BWD).total; }
+size_t glu_scratch(const Glu& p, int pass) {
+  return pass == CONVBN_PASS_FWD && glu_few_taken(p.M, p.K, p.dtype) ? 0 : plan_of(p, pass == CONVBN_PASS_BWD).total;
+}
 hipError_t launch_glu_fwd(const Glu& p, void* ws, hipStream_t st) {
   return by_gate(p, [&](auto t, auto k) { return fwd_t<decltype(t), k.value>(p, static_cast<char*>(ws), st); });
 }

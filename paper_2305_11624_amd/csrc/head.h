@@ -19,6 +19,9 @@ struct F8Mul {
 };
 size_t f8mul_scratch(i64 M, int N, int K);
 hipError_t launch_f8mul(const F8Mul& p, void* ws, hipStream_t st);
+// The same for few rows (few.hip), which it packs itself: x != null, codes and scales null = not kept
+bool f8few_taken(i64 M, int K);
+hipError_t launch_f8few(const F8Mul& p, const void* x, i64 ldx, void* codes, void* scales, hipStream_t st);
 
 // dx [M][K] = dz . w8 + add, dW [N][K] = dz^T . x8, db = column sums of dz; dx, dW, db nullable
 struct F8Grad {
@@ -40,6 +43,8 @@ struct Glu {
   void* dx; void* dW; float* db;
 };
 bool glu_in_place(int dtype, int K, i64 ld);   // bf16 rows that are read where they are, from 16 bytes on
+bool glu_few_taken(i64 M, int K, int dtype);   // few rows (few.hip): no workspace
+hipError_t launch_glu_few(const Glu& p, hipStream_t st);
 size_t glu_scratch(const Glu& p, int pass);
 hipError_t launch_glu_fwd(const Glu& p, void* ws, hipStream_t st);
 hipError_t launch_glu_bwd(const Glu& p, void* ws, hipStream_t st);

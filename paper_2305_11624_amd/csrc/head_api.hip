@@ -17,9 +17,9 @@ F8Grad grad_of(const convbn_qdesc* d, i64 ldx, i64 ldz) {
   return g;
 }
 // Forward workspace: the product's, then codes and scales that the call does not hand out
-size_t mul_ws(const convbn_qdesc* d) { return f8mul_scratch(d->M, d->N, d->K); }
+size_t mul_ws(const convbn_qdesc* d) { return f8few_taken(d->M, d->K) ? 0 : f8mul_scratch(d->M, d->N, d->K); }
 size_t codes_ws(const convbn_qdesc* d) { return align_up((size_t)d->M * qrow(d->K), 256); }
-size_t fwd_ws(const convbn_qdesc* d) { return mul_ws(d) + codes_ws(d) + align_up((size_t)d->M * f8srow(d->K), 256); }
+size_t fwd_ws(const convbn_qdesc* d) { return f8few_taken(d->M, d->K) ? 0 : mul_ws(d) + codes_ws(d) + align_up((size_t)d->M * f8srow(d->K), 256); }
 
 // ---- gated product ----
 convbn_status check_glu(const convbn_qdesc* d, Glu* g) {
@@ -103,6 +103,11 @@ convbn_status convbn_flinear_fwd(const convbn_qdesc* desc, const void* x, void* 
   m.M = desc->M; m.ldz = ldz; m.K = desc->K; m.N = desc->N; m.dtype = desc->dtype;
   m.qw = (const uint8_t*)w_codes; m.sw = (const uint8_t*)w_scales; m.b = b; m.z = z;
   m.add = (desc->act & CONVBN_ACT_ADD_OUT) ? desc->add_out : nullptr;
+  if (f8few_taken(desc->M, desc->K)) {
+    m.qx = (const uint8_t*)codes; m.sx = (const uint8_t*)scales;
+    LAUNCH(launch_f8few(m, x, ldx, codes, scales, st));
+    return CONVBN_OK;
+  }
   if (!codes) {
     codes = static_cast<char*>(ws) + mul_ws(desc);
     scales = static_cast<char*>(codes) + codes_ws(desc);

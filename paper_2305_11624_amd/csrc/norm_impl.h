@@ -710,7 +710,7 @@ Plan plan_of(const Norm& n, bool bwd) {
     --t.lprlog;
   }
   p.bundles = (int)((n.groups + (1LL << t.nblog) - 1) >> t.nblog) * p.sections;
-  // one launch where the parts fit and are enough to fill a quarter of the chip, or short
+  // one launch where the parts fit and are enough to fill an eighth of the chip, or short
   s.whole = fits() && (n.M * p.bundles >= CUS / 8 || n.P << t.lprlog <= 4096);
   t.ttlog = t.lprlog;
   if (s.whole) {
@@ -723,7 +723,7 @@ Plan plan_of(const Norm& n, bool bwd) {
     p.segs = 1;
     // (32-bit offsets of the rows of a workgroup's images)
     const i64 teams = s.nt >> t.ttlog, ld = n.ldx > n.ldy ? n.ldx : n.ldy;
-    if ((teams * n.P * ld + n.C) * size > 0x7fffffffLL) s.whole = false;
+    if ((teams * n.P * ld + n.C) * size > 0x7fffffffLL) s.whole = s.few = s.single = false;
   }
   if (!s.whole) {
     t.ttlog = t.lprlog;
