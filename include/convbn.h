@@ -547,8 +547,9 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, co
 /* GATED PRODUCT.  Both projections of a gated feed-forward block, the activation and the product in one call:
  *     g = x Wg^T + bg,   u = x Wu^T + bu,   y = f(g) u        x [M][K] (ldx apart), y [M][N] (ldz apart), f = desc->gate
  * W = [Wg; Wu]: dense [2 N][K] of dtype, g's rows before u's; b = [bg; bu]: [2 N] fp32, nullable.
- * h: nullable, dense [M][2 N]: h = [g | u] as backward reads it, of dtype without b and fp32 with it (db adds up over the rows what is lost in
- * rounding h).  Without h backward multiplies x and W again, and 2 N numbers a row need not be kept.
+ * h: nullable, dense [M][2 N] fp32: h = [g | u] as backward reads it.  Without it backward multiplies x and W again, and 2 N numbers a row
+ * need not be kept; the gradients are the same bits.  (fp32 for either dtype: gradients see dh rounded to bf16 once, and db adds up over the rows what
+ * a rounding of h would leave in it.)
  *   backward   dg = dy u f'(g),  du = dy f(g),  dh = [dg | du];   dx = dh W (+ add_in),   dW = dh^T x,   db = column sums of dh
  * dx, dW, db nullable, each = not wanted.  With dtype BF16 sums are in fp32 and dh is rounded to bf16 before the products (db sums it
  * before that); with F32 operands meet in three bf16 parts that add up to them, and nothing is rounded below fp32.
@@ -558,15 +559,16 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, co
  * bytes (they are read where they are, others from a copy in the workspace).  Outputs overlap no input, but for the addend. */
 size_t convbn_glu_workspace_bytes(const convbn_qdesc *desc, int pass);
 convbn_status convbn_glu_fwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, void *y,
-                             void *h, void *ws, size_t ws_bytes, void *stream);
-convbn_status convbn_glu_bwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, const void *h,
+                             float *h, void *ws, size_t ws_bytes, void *stream);
+convbn_status convbn_glu_bwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, const float *h,
                              const void *dy, void *dx, void *dW, float *db, void *ws, size_t ws_bytes,
                              void *stream);
 
 /* GROUP NORM with an activation, channels last.  x, y: [M images][P pixels][C], pixels ldx / ldy elements apart.
  *     xhat = (x - mean) / sqrt(var + eps) over the P C / groups values of a group of neighbouring channels of an image,
  *     y = f(gamma xhat + beta)
- * stats: [M][groups][2] fp32, mean and 1 / sqrt(var + eps): nullable in forward, what backward needs beside x.  gamma, beta: [C] fp32, NULL = ones,
+ * stats: [M][groups][4] fp32, mean and 1 / sqrt(var + eps), each as a number and what that leaves of it (behind a ReLU backward decides with all of their
+ * bits which values next to its border passed; 0 for the other activations): nullable in forward, what backward needs beside x.  gamma, beta: [C] fp32, NULL = ones,
  * zeros.  (P = 1, groups = 1: a norm over each token's channels.)
  *   backward   dx (+ add_in), dgamma, dbeta: nullable, each = not wanted; beta is read for f' alone.
  * Sums and statistics are fp32; the variance is summed from differences to a mean.  M == 0 is no error: dgamma and dbeta become zero.  Rows need the

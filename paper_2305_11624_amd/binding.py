@@ -776,7 +776,7 @@ def convbn_glu_workspace_bytes(desc: QDesc, pass_: int) -> int:
 
 
 def convbn_glu_fwd(desc, x, W, b, y, h, ws=None, stream=None, check=True):
-    st = (_call_rows or _load_rows())(_at.convbn_glu_fwd, desc, "xVmzk" if b is None else "xVmzl", x, W, b, y, h, ws,
+    st = (_call_rows or _load_rows())(_at.convbn_glu_fwd, desc, "xVmzl", x, W, b, y, h, ws,
                                       None if stream is None else _handle(stream))
     if st and check:
         _check(st)
@@ -784,7 +784,7 @@ def convbn_glu_fwd(desc, x, W, b, y, h, ws=None, stream=None, check=True):
 
 
 def convbn_glu_bwd(desc, x, W, b, h, dy, dx, dW, db, ws=None, stream=None, check=True):
-    st = (_call_rows or _load_rows())(_at.convbn_glu_bwd, desc, "xVmkzxVm" if b is None else "xVmlzxVm", x, W, b, h, dy, dx, dW, db, ws,
+    st = (_call_rows or _load_rows())(_at.convbn_glu_bwd, desc, "xVmlzxVm", x, W, b, h, dy, dx, dW, db, ws,
                                       None if stream is None else _handle(stream))
     if st and check:
         _check(st)

@@ -172,13 +172,8 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
       const float g = v[0] + (p.g.b ? p.g.b[j] : 0.f), u = v[S - 1] + (p.g.b ? p.g.b[p.N + j] : 0.f);
       if (p.g.h) {
         const i64 at = (i64)m * 2 * p.N + j;
-        if (p.g.h32) {
-          static_cast<float*>(p.g.h)[at] = g;
-          static_cast<float*>(p.g.h)[at + p.N] = u;
-        } else {
-          static_cast<T*>(p.g.h)[at] = from_f32<T>(g);
-          static_cast<T*>(p.g.h)[at + p.N] = from_f32<T>(u);
-        }
+        p.g.h[at] = g;
+        p.g.h[at + p.N] = u;
       }
       float f, df;
       gate_of<T, KIND>(g, &f, &df);

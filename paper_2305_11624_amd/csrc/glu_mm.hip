@@ -29,15 +29,9 @@ template <typename T, int KIND> struct GluOut {
       u.v[i] += b.u.v[i];
     }
     if (q.h) {
-      if (q.h32) {
-        float* h = static_cast<float*>(q.h) + m * 2 * q.N;
-        store8<float, true>(h, n, q.N, g);
-        store8<float, true>(h + q.N, n, q.N, u);
-      } else {
-        T* h = static_cast<T*>(q.h) + m * 2 * q.N;
-        store8<T, true>(h, n, q.N, g);
-        store8<T, true>(h + q.N, n, q.N, u);
-      }
+      float* h = q.h + m * 2 * q.N;   // (halves of a lane's 32 bytes are two stores: the caches make lines of them)
+      store8<float>(h, n, q.N, g);
+      store8<float>(h + q.N, n, q.N, u);
     }
     if (q.y) {
       F8 y;
@@ -58,11 +52,11 @@ constexpr int NT = 32 * SUM_ROWS;
 struct DGate {
   i64 M, ldz, per;
   int N, W2, across, blocks;
-  const void* h; const void* dy;
+  const float* h; const void* dy;
   bf16_t* dh; i64 plane;      // null: not wanted
   float* sums;                // [slices][2 N] or null
 };
-template <typename T, typename H, int KIND> __global__ __launch_bounds__(NT) void glu_prep_kernel(DGate p, RowsCopy x, unsigned nx, RowsCopy w) {
+template <typename T, int KIND> __global__ __launch_bounds__(NT) void glu_prep_kernel(DGate p, RowsCopy x, unsigned nx, RowsCopy w) {
   __shared__ float meet[SUM_ROWS][256 + 8];
   if ((int)blockIdx.x >= p.blocks) {
     const unsigned wg = blockIdx.x - p.blocks;
@@ -76,8 +70,8 @@ template <typename T, typename H, int KIND> __global__ __launch_bounds__(NT) voi
   if (n < p.N) {
 #pragma unroll 2
     for (i64 m = beg + (threadIdx.x >> 5); m < end; m += SUM_ROWS) {
-      const H* h = static_cast<const H*>(p.h) + m * 2 * p.N;
-      const F8 g = load8<H>(h, n, p.N), u = load8<H>(h + p.N, n, p.N), dy = load8<T>(static_cast<const T*>(p.dy) + m * p.ldz, n, p.N);
+      const float* h = p.h + m * 2 * p.N;
+      const F8 g = load8<float>(h, n, p.N), u = load8<float>(h + p.N, n, p.N), dy = load8<T>(static_cast<const T*>(p.dy) + m * p.ldz, n, p.N);
       F8 d[2];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -172,16 +166,15 @@ template <typename T, int KIND> hipError_t bwd_t(const Glu& p, char* ws, hipStre
   const Plan s = plan_of(p, true);
   const bool again = !p.hk && p.M, want_dx = p.dx && p.M, want_dW = p.dW && p.M;
   const Operands o = operands_of(p, s, ws, again || want_dW, again || want_dx);
-  const void* h = p.hk;
+  const float* h = p.hk;
   if (again) {
     Glu q = p;
     q.y = nullptr;
-    q.h = ws;
-    q.h32 = true;
+    q.h = reinterpret_cast<float*>(ws);
     hipError_t e = launch_rows_copies(p.dtype, o.cx, o.cw, st);
     if (e == hipSuccess) e = project<T, KIND>(q, s, o, ws, st);
     if (e != hipSuccess) return e;
-    h = ws;
+    h = q.h;
   }
   float* const sums = reinterpret_cast<float*>(ws + s.h + s.dh + s.x + s.W + s.part);
   const int W2 = round8(2 * p.N);
@@ -193,10 +186,7 @@ template <typename T, int KIND> hipError_t bwd_t(const Glu& p, char* ws, hipStre
   d.blocks = d.across * slices;
   const RowsCopy cx = again ? RowsCopy{} : o.cx, cw = again ? RowsCopy{} : o.cw;
   const unsigned nx = piece_blocks<NT>(cx.rows, cx.width, cx.out), nw = piece_blocks<NT>(cw.rows, cw.width, cw.out), blocks = d.blocks + nx + nw;
-  if (blocks) {
-    if (p.b || again) glu_prep_kernel<T, float, KIND><<<blocks, NT, 0, st>>>(d, cx, nx, cw);
-    else glu_prep_kernel<T, T, KIND><<<blocks, NT, 0, st>>>(d, cx, nx, cw);
-  }
+  if (blocks) glu_prep_kernel<T, KIND><<<blocks, NT, 0, st>>>(d, cx, nx, cw);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   Grads g = {};

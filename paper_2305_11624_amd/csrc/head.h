@@ -38,8 +38,8 @@ struct Glu {
   i64 M, ldx, ldz;
   int K, N, dtype, gate;
   const void* x; const void* W; const float* b;
-  void* y; void* h; bool h32;                         // forward (h32: h is fp32)
-  const void* hk; const void* dy; const void* add;    // backward (hk: the kept h, or null)
+  void* y; float* h;                                  // forward
+  const float* hk; const void* dy; const void* add;    // backward (hk: the kept h, or null)
   void* dx; void* dW; float* db;
 };
 bool glu_in_place(int dtype, int K, i64 ld);   // bf16 rows that are read where they are, from 16 bytes on

@@ -142,27 +142,27 @@ size_t convbn_glu_workspace_bytes(const convbn_qdesc* desc, int pass) {
   return check_glu(desc, &g) == CONVBN_OK ? glu_scratch(g, pass) : 0;
 }
 
-convbn_status convbn_glu_fwd(const convbn_qdesc* desc, const void* x, const void* W, const float* b, void* y, void* h, void* ws,
+convbn_status convbn_glu_fwd(const convbn_qdesc* desc, const void* x, const void* W, const float* b, void* y, float* h, void* ws,
                              size_t ws_bytes, void* stream) {
   Glu g = {};
   TRY_STATUS(check_glu(desc, &g));
   REQUIRE_ROWS(x, glu_in_place(g.dtype, g.K, g.ldx) ? 16 : elem(desc));
   REQUIRE(W, glu_in_place(g.dtype, g.K, g.K) ? 16 : elem(desc));
-  OPTIONAL(b, 4); REQUIRE_ROWS(y, elem(desc)); OPTIONAL(h, elem(desc));
+  OPTIONAL(b, 4); REQUIRE_ROWS(y, elem(desc)); OPTIONAL(h, 4);
   if (!desc->M) return CONVBN_OK;
   TRY_STATUS(check_ws(glu_scratch(g, CONVBN_PASS_FWD), ws, ws_bytes));
-  g.x = x; g.W = W; g.b = b; g.y = y; g.h = h; g.h32 = b != nullptr;
+  g.x = x; g.W = W; g.b = b; g.y = y; g.h = h;
   LAUNCH(launch_glu_fwd(g, ws, (hipStream_t)stream));
   return CONVBN_OK;
 }
 
-convbn_status convbn_glu_bwd(const convbn_qdesc* desc, const void* x, const void* W, const float* b, const void* h, const void* dy,
+convbn_status convbn_glu_bwd(const convbn_qdesc* desc, const void* x, const void* W, const float* b, const float* h, const void* dy,
                              void* dx, void* dW, float* db, void* ws, size_t ws_bytes, void* stream) {
   Glu g = {};
   TRY_STATUS(check_glu(desc, &g));
   REQUIRE_ROWS(x, glu_in_place(g.dtype, g.K, g.ldx) ? 16 : elem(desc));
   REQUIRE(W, glu_in_place(g.dtype, g.K, g.K) ? 16 : elem(desc));
-  OPTIONAL(b, 4); OPTIONAL(h, elem(desc)); REQUIRE_ROWS(dy, elem(desc));
+  OPTIONAL(b, 4); OPTIONAL(h, 4); REQUIRE_ROWS(dy, elem(desc));
   OPTIONAL(dx, elem(desc)); OPTIONAL(dW, elem(desc)); OPTIONAL(db, 4);
   if (!dx && !dW && !db && desc->M) return set_error(CONVBN_ERR_NULL, "no output is asked for");
   OPTIONAL(desc->add_in, elem(desc));

@@ -8,7 +8,7 @@ size_t norm_scratch(const Norm& p, int pass) { return plan_of(p, pass == CONVBN_
 hipError_t launch_norm_fwd(const Norm& n, void* ws, hipStream_t st) {
   if (!n.M) return hipSuccess;
   Plan s = plan_of(n, false);
-  s.p.part = static_cast<float*>(ws);
+  s.p.part = static_cast<double2*>(ws);
   return run_norm<false>(s, st);
 }
 

@@ -5,7 +5,7 @@ namespace convbn {
 
 hipError_t launch_norm_bwd(const Norm& n, void* ws, hipStream_t st) {
   Plan s = plan_of(n, true);
-  s.p.part = static_cast<float*>(ws);
+  s.p.part = static_cast<double2*>(ws);
   const bool params = n.dgamma || n.dbeta;
   float* const sums = reinterpret_cast<float*>(static_cast<char*>(ws) + s.part);
   s.p.sums = params ? sums : nullptr;

@@ -31,7 +31,7 @@ struct NormParams {
   int slices;           // workgroups along the images (each takes every slices'th team of images)
   int segs;             // segments of the pixels
   i64 seg;              // pixels of one
-  float* part;          // sums of the segments, [M][groups][segs * sections][2]
+  double2* part;        // sums of the segments, [M][groups][segs * sections]
   float* sums;          // [slices * segs][C][2]: dgamma, dbeta; null: not wanted
 };
 
@@ -111,8 +111,23 @@ __device__ __forceinline__ float across32(float v) {   // + lane ^ 32
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// ... and for 64 bits, as two halves
+template <int CTRL> __device__ __forceinline__ double dpp(double v) {
+  const int2 q = __builtin_bit_cast(int2, v);
+  return __builtin_bit_cast(double, make_int2(__builtin_amdgcn_update_dpp(0, q.x, CTRL, 0xf, 0xf, false), __builtin_amdgcn_update_dpp(0, q.y, CTRL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ double across16(double v) {
+  const uint2 q = __builtin_bit_cast(uint2, v);
+  const auto x = __builtin_amdgcn_permlane16_swap(q.x, q.x, false, false), y = __builtin_amdgcn_permlane16_swap(q.y, q.y, false, false);
+  return __builtin_bit_cast(double, make_uint2(x[0], y[0])) + __builtin_bit_cast(double, make_uint2(x[1], y[1]));
+}
+__device__ __forceinline__ double across32(double v) {
+  const uint2 q = __builtin_bit_cast(uint2, v);
+  const auto x = __builtin_amdgcn_permlane32_swap(q.x, q.x, false, false), y = __builtin_amdgcn_permlane32_swap(q.y, q.y, false, false);
+  return __builtin_bit_cast(double, make_uint2(x[0], y[0])) + __builtin_bit_cast(double, make_uint2(x[1], y[1]));
+}
 // Sums over 16 lanes
-template <int N> __device__ __forceinline__ void row_sums(float (&s)[N]) {
+template <int N, typename A> __device__ __forceinline__ void row_sums(A (&s)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] += dpp<0x121>(s[i]);
 #pragma unroll
@@ -145,28 +160,28 @@ struct Lane {
     first = n && r == 0 && v == 0;
   }
   // this lane's entry of the segments' sums of image m
-  __device__ __forceinline__ float* entry(const NormParams& p, i64 m, int i) const {
-    return p.part + ((m * p.n.groups + g) * (p.segs * p.sections) + i) * 2;
+  __device__ __forceinline__ double2* entry(const NormParams& p, i64 m, int i) const {
+    return p.part + (m * p.n.groups + g) * (p.segs * p.sections) + i;
   }
   // Sums over a group's lanes of this wave.  Its pieces are the low bits of a lane; its pixels the high ones, turned within rows of 16 (a team
   // that has several pixels side by side has 16 lanes at least) and exchanged between rows.
-  template <int N> __device__ __forceinline__ void wave_sums(const Team& t, float (&s)[N]) const {
+  template <int N, typename A> __device__ __forceinline__ void wave_sums(const Team& t, A (&s)[N]) const {
     auto each = [&](auto f) {
 #pragma unroll
       for (int i = 0; i < N; ++i) s[i] = f(s[i]);
     };
-    if (t.mlog > 0) each([](float v) { return v + dpp<0xb1>(v); });    // lane ^ 1
-    if (t.mlog > 1) each([](float v) { return v + dpp<0x4e>(v); });    // lane ^ 2
-    if (t.mlog > 2) each([](float v) { return v + dpp<0x141>(v); });   // 7 - lane: fours are equal by now
-    if (t.mlog > 3) each([](float v) { return v + dpp<0x140>(v); });   // 15 - lane
+    if (t.mlog > 0) each([](A v) { return v + dpp<0xb1>(v); });    // lane ^ 1
+    if (t.mlog > 1) each([](A v) { return v + dpp<0x4e>(v); });    // lane ^ 2
+    if (t.mlog > 2) each([](A v) { return v + dpp<0x141>(v); });   // 7 - lane: fours are equal by now
+    if (t.mlog > 3) each([](A v) { return v + dpp<0x140>(v); });   // 15 - lane
     if (t.ttlog > t.lprlog) {
-      if (t.lprlog < 1) each([](float v) { return v + dpp<0x121>(v); });
-      if (t.lprlog < 2) each([](float v) { return v + dpp<0x122>(v); });
-      if (t.lprlog < 3) each([](float v) { return v + dpp<0x124>(v); });
-      if (t.lprlog < 4) each([](float v) { return v + dpp<0x128>(v); });
+      if (t.lprlog < 1) each([](A v) { return v + dpp<0x121>(v); });
+      if (t.lprlog < 2) each([](A v) { return v + dpp<0x122>(v); });
+      if (t.lprlog < 3) each([](A v) { return v + dpp<0x124>(v); });
+      if (t.lprlog < 4) each([](A v) { return v + dpp<0x128>(v); });
     }
-    if (t.mlog > 4 || (t.lprlog < 5 && t.ttlog > 4)) each([](float v) { return across16(v); });
-    if (t.mlog > 5 || (t.lprlog < 6 && t.ttlog > 5)) each([](float v) { return across32(v); });
+    if (t.mlog > 4 || (t.lprlog < 5 && t.ttlog > 4)) each([](A v) { return across16(v); });
+    if (t.mlog > 5 || (t.lprlog < 6 && t.ttlog > 5)) each([](A v) { return across32(v); });
   }
   // Where this wave's sums go and the team's begin
   __device__ __forceinline__ int slot(const Team& t, int w) const { return (w << t.nblog) + gl; }
@@ -174,17 +189,19 @@ struct Lane {
   __device__ __forceinline__ bool writes(const Team& t) const { return (int)(threadIdx.x & 63) == (gl << t.mlog & 63); }
 };
 
-struct Moments { float n, mean, m2; };
-__device__ __forceinline__ void merge(Moments& a, const Moments& b) {
-  if (b.n == 0.f) return;
-  const float n = a.n + b.n, d = b.mean - a.mean, q = b.n / n;
+// What is merged of the lanes' sums: fp32, or, in front of a ReLU, 64 bits (what is left to err is then a lane's own sums, some 6e-9 of a deviation)
+template <int F> using Sum = std::conditional_t<F == CONVBN_NORM_RELU, double, float>;
+template <typename A> struct Moments { A n, mean, m2; };
+template <typename A> __device__ __forceinline__ void merge(Moments<A>& a, const Moments<A>& b) {
+  if (b.n == A(0)) return;
+  const A n = a.n + b.n, d = b.mean - a.mean, q = b.n / n;
   a.mean += d * q;
   a.m2 += b.m2 + d * d * a.n * q;
   a.n = n;
 }
 // Moments of IM images' groups from their lanes'; every lane of the team returns them.  buf: [IM][waves << nblog] entries of three
-template <int IM> __device__ __forceinline__ void team_moments(const Lane& l, const Team& t, Moments (&a)[IM], float* buf, int entries) {
-  float s[2 * IM], q[IM];
+template <int IM, typename A> __device__ __forceinline__ void team_moments(const Lane& l, const Team& t, Moments<A> (&a)[IM], A* buf, int entries) {
+  A s[2 * IM], q[IM];
 #pragma unroll
   for (int i = 0; i < IM; ++i) {
     s[2 * i] = a[i].n;
@@ -193,8 +210,8 @@ template <int IM> __device__ __forceinline__ void team_moments(const Lane& l, co
   l.wave_sums(t, s);
 #pragma unroll
   for (int i = 0; i < IM; ++i) {
-    const float wmean = s[2 * i] > 0.f ? s[2 * i + 1] / s[2 * i] : 0.f, d = a[i].mean - wmean;
-    q[i] = a[i].n > 0.f ? a[i].m2 + a[i].n * d * d : 0.f;
+    const A wmean = s[2 * i] > A(0) ? s[2 * i + 1] / s[2 * i] : A(0), d = a[i].mean - wmean;
+    q[i] = a[i].n > A(0) ? a[i].m2 + a[i].n * d * d : A(0);
     a[i].n = s[2 * i];
     a[i].mean = wmean;
   }
@@ -205,26 +222,26 @@ template <int IM> __device__ __forceinline__ void team_moments(const Lane& l, co
   if (l.writes(t)) {
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
-      float* o = buf + (i * entries + l.slot(t, l.wave)) * 3;
+      A* o = buf + (i * entries + l.slot(t, l.wave)) * 3;
       o[0] = a[i].n; o[1] = a[i].mean; o[2] = a[i].m2;
     }
   }
   __syncthreads();
   if (t.nblog == 0) {   // one group: 16 lanes read a wave's each
     const int w = threadIdx.x & 15;
-    float mean[IM];
+    A mean[IM];
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
-      const float* o = buf + (i * entries + l.first_wave() + w) * 3;
-      a[i] = w < l.waves ? Moments{o[0], o[1], o[2]} : Moments{0.f, 0.f, 0.f};
+      const A* o = buf + (i * entries + l.first_wave() + w) * 3;
+      a[i] = w < l.waves ? Moments<A>{o[0], o[1], o[2]} : Moments<A>{A(0), A(0), A(0)};
       s[2 * i] = a[i].n;
       s[2 * i + 1] = a[i].n * a[i].mean;
     }
     row_sums(s);
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
-      mean[i] = s[2 * i] > 0.f ? s[2 * i + 1] / s[2 * i] : 0.f;
-      const float e = a[i].mean - mean[i];
+      mean[i] = s[2 * i] > A(0) ? s[2 * i + 1] / s[2 * i] : A(0);
+      const A e = a[i].mean - mean[i];
       q[i] = a[i].m2 + a[i].n * e * e;
     }
     row_sums(q);
@@ -234,20 +251,26 @@ template <int IM> __device__ __forceinline__ void team_moments(const Lane& l, co
   }
 #pragma unroll
   for (int i = 0; i < IM; ++i) {
-    float n = 0.f, sum = 0.f, m2 = 0.f;
+    A n = A(0), sum = A(0), m2 = A(0);
     for (int w = 0; w < l.waves; ++w) {
-      const float* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
+      const A* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
       n += o[0];
       sum += o[0] * o[1];
     }
-    const float mean = n > 0.f ? sum / n : 0.f;
+    const A mean = n > A(0) ? sum / n : A(0);
     for (int w = 0; w < l.waves; ++w) {
-      const float* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
-      const float e = o[1] - mean;
+      const A* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
+      const A e = o[1] - mean;
       m2 += o[2] + o[0] * e * e;
     }
     a[i] = {n, mean, m2};
   }
+}
+// A group's statistics from its moments about `pivot`
+template <typename A> struct Stats { A mean, r; };
+template <typename A> __device__ __forceinline__ Stats<A> stats_of(const Moments<A>& a, float pivot, A count, float eps) {
+  if constexpr (sizeof(A) == 8) return {a.mean + pivot, 1. / sqrt(a.m2 / count + eps)};
+  else return {a.mean + pivot, 1.f / sqrtf(a.m2 / count + eps)};
 }
 // ... of pairs of sums.  buf: [waves << nblog] entries of 2 IM
 template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const Team& t, float (&s)[2 * IM], float* buf) {
@@ -273,7 +296,7 @@ template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const
 }
 
 // Moments about `pivot` of KP pieces, rows of which are in
-template <typename T, int V, int KP> __device__ __forceinline__ Moments moments_of(Held<T, V> (&x)[KP], int rows, int n, float pivot) {
+template <typename A, typename T, int V, int KP> __device__ __forceinline__ Moments<A> moments_of(Held<T, V> (&x)[KP], int rows, int n, float pivot) {
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < KP; ++k)
@@ -282,11 +305,11 @@ template <typename T, int V, int KP> __device__ __forceinline__ Moments moments_
 #pragma unroll
       for (int i = 0; i < width_of<V>; ++i) s += V != TAIL || i < n ? f.v[i] - pivot : 0.f;
     }
-  Moments m = {(float)(rows * n), 0.f, 0.f};
-  if (rows * n == 0) return m;
-  m.mean = s / m.n;
+  if (rows * n == 0) return {A(0), A(0), A(0)};
+  const float mean = s / (float)(rows * n);
+  float m2 = 0.f;
   as_held(x);
-  const float c = pivot + m.mean;   // (its rounding d adds n d^2 to the sum, and nothing else: the differences to the mean add up to nothing)
+  const float c = pivot + mean;   // (its rounding d adds n d^2 to the sum, and nothing else: the differences to the mean add up to nothing)
 #pragma unroll
   for (int k = 0; k < KP; ++k)
     if (k < rows) {
@@ -294,10 +317,14 @@ template <typename T, int V, int KP> __device__ __forceinline__ Moments moments_
 #pragma unroll
       for (int i = 0; i < width_of<V>; ++i) {
         const float d = V != TAIL || i < n ? f.v[i] - c : 0.f;
-        m.m2 = fmaf(d, d, m.m2);
+        m2 = fmaf(d, d, m2);
       }
     }
-  return m;
+  if constexpr (sizeof(A) == 8) {   // the mean with all of its bits, and the sum about it
+    const A exact = (A)s / (rows * n), e = (A)c - pivot - exact;
+    return {(A)(rows * n), exact, (A)m2 - e * e * (rows * n)};
+  }
+  return {(A)(rows * n), mean, m2};
 }
 
 template <int V> struct Columns { Vals<width_of<V>> ga, be; };
@@ -366,14 +393,15 @@ template <int KP> __device__ __forceinline__ int rows_from(const Lane& l, bool l
 
 // IM: images at a time (WHOLE)
 template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
-  extern __shared__ float lds[];   // two turns' moments
+  using A = Sum<F>;
+  extern __shared__ __align__(16) unsigned char lds[];   // two turns' moments
   Place at;
   if (!place_of(p, &at)) return;
   Lane l;
   l.init<width_of<V>>(p, at.bundle);
   const int teams = NT >> p.t.ttlog, entries = NT / 64 << p.t.nblog;
   const i64 beg = at.seg * p.seg, end = beg + p.seg < p.n.P ? beg + p.seg : p.n.P;
-  const float count = (float)p.n.P * (float)p.cg;
+  const A count = (A)p.n.P * (A)p.cg;
   auto live_at = [&](i64 m0) { return m0 + l.team < p.n.M && l.n; };
   auto pivot_at = [&](i64 m0) {   // the group's first value
     return live_at(m0) ? to_f32(static_cast<const T*>(p.n.x)[(m0 + l.team) * p.n.P * p.n.ldx + l.g * p.cg]) : 0.f;
@@ -391,11 +419,11 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   };
   Columns<V> col;
   if constexpr (PHASE != SUMS && IM > 1) col = columns_of<V>(p.n, l);
-  auto put = [&](Held<T, V> (&v)[KP], i64 m0, i64 px, int rows, float mean, float r) {
+  auto put = [&](Held<T, V> (&v)[KP], i64 m0, i64 px, int rows, const Stats<A>& z) {
     Rows<T, PHASE> y(p.n.y, l, p.n.P, p.n.ldy, m0);
     y.from(px);
     as_held(v);
-    const float shift = -mean * r;
+    const float r = (float)z.r, shift = (float)(-z.mean * z.r);
 #pragma unroll
     for (int k = 0; k < KP; ++k) {
       T* q = y.next();
@@ -409,16 +437,18 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       store_piece<T, V>(q, l.n, f);
     }
   };
-  auto keep = [&](i64 m0, float mean, float r) {
-    if (p.n.stats && live_at(m0) && l.first && l.section == 0 && at.seg == 0)
-      *reinterpret_cast<float2*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 2) = make_float2(mean, r);
+  auto keep = [&](i64 m0, const Stats<A>& z) {
+    if (p.n.stats && live_at(m0) && l.first && l.section == 0 && at.seg == 0) {
+      const float mean = (float)z.mean, r = (float)z.r;
+      *reinterpret_cast<float4*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 4) = make_float4(mean, (float)(z.mean - mean), r, (float)(z.r - r));
+    }
   };
   const i64 stride = (i64)p.slices * teams * IM;
   int turn = 0;   // (every lane of the workgroup takes part in the barrier of every turn)
   for (i64 m0 = (i64)at.slice * teams * IM; m0 < p.n.M; m0 += stride, turn ^= 1) {
-    float* const buf = lds + turn * IM * entries * 3;
+    A* const buf = reinterpret_cast<A*>(lds) + turn * IM * entries * 3;
     Held<T, V> v[IM][KP];
-    Moments a[IM];
+    Moments<A> a[IM];
     if constexpr (PHASE == WHOLE) {
       float pivot[IM];
       int rows[IM];
@@ -429,40 +459,40 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       }
       if constexpr (IM == 1) col = columns_of<V>(p.n, l);
 #pragma unroll
-      for (int i = 0; i < IM; ++i) a[i] = moments_of(v[i], rows[i], l.n, pivot[i]);
+      for (int i = 0; i < IM; ++i) a[i] = moments_of<A>(v[i], rows[i], l.n, pivot[i]);
       team_moments(l, p.t, a, buf, entries);
 #pragma unroll
       for (int i = 0; i < IM; ++i) {
-        const float r = 1.f / sqrtf(a[i].m2 / count + p.n.eps), mean = pivot[i] + a[i].mean;
-        put(v[i], m0 + i * teams, l.r, rows[i], mean, r);
-        keep(m0 + i * teams, mean, r);
+        const Stats<A> z = stats_of(a[i], pivot[i], count, p.n.eps);
+        put(v[i], m0 + i * teams, l.r, rows[i], z);
+        keep(m0 + i * teams, z);
       }
     } else {
       const i64 m = m0 + l.team;
       const float pivot = pivot_at(m0);
-      a[0] = {0.f, 0.f, 0.f};
+      a[0] = {A(0), A(0), A(0)};
       if constexpr (PHASE == SUMS) {
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           const int rows = load(v[0], m0, px);
-          merge(a[0], moments_of(v[0], rows, l.n, pivot));
+          merge(a[0], moments_of<A>(v[0], rows, l.n, pivot));
         }
         team_moments(l, p.t, a, buf, entries);
-        if (live_at(m0) && l.first) *reinterpret_cast<float2*>(l.entry(p, m, at.seg * p.sections + l.section)) = make_float2(a[0].mean, a[0].m2);
+        if (live_at(m0) && l.first) *l.entry(p, m, at.seg * p.sections + l.section) = make_double2(a[0].mean, a[0].m2);
       } else {
         col = columns_of<V>(p.n, l);
         if (live_at(m0))
           for (int s = 0; s < p.segs; ++s)
             for (int e = 0; e < p.sections; ++e) {
-              const float2 q = *reinterpret_cast<const float2*>(l.entry(p, m, s * p.sections + e));
+              const double2 q = *l.entry(p, m, s * p.sections + e);
               const i64 px = p.n.P - s * p.seg < p.seg ? p.n.P - s * p.seg : p.seg;
-              merge(a[0], {(float)px * (float)min(p.span, p.cg - e * p.span), q.x, q.y});
+              merge(a[0], {(A)px * (A)min(p.span, p.cg - e * p.span), (A)q.x, (A)q.y});
             }
-        const float r = 1.f / sqrtf(a[0].m2 / count + p.n.eps), mean = pivot + a[0].mean;
+        const Stats<A> z = stats_of(a[0], pivot, count, p.n.eps);
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           const int rows = load(v[0], m0, px);
-          put(v[0], m0, px, rows, mean, r);
+          put(v[0], m0, px, rows, z);
         }
-        keep(m0, mean, r);
+        keep(m0, z);
       }
     }
   }
@@ -471,7 +501,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
 // dxhat = gamma dz, dz = dy f'(z);  dx = r (dxhat - mean(dxhat) - xhat mean(dxhat xhat)),  dgamma = sum dz xhat,  dbeta = sum dz
 template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_bwd_kernel(NormParams p) {
   constexpr int W = width_of<V>;
-  extern __shared__ float lds[];   // two turns' sums; at the end the columns', [waves][2 W][64]
+  extern __shared__ float cols[];   // two turns' sums; at the end the columns', [waves][2 W][64]
   Place at;
   if (!place_of(p, &at)) return;
   Lane l;
@@ -481,12 +511,15 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   const Columns<V> col = columns_of<V>(p.n, l);
   const float count = (float)p.n.P * (float)p.cg;
   Vals<W> dga = {}, dbe = {};
-  struct Image { Held<T, V> v[KP], d[KP]; float r, shift; int rows; };   // xhat = x r + shift
+  struct Image { Held<T, V> v[KP], d[KP]; float r, shift, mean, mean_l, r_l; int rows; };   // xhat = x r + shift; RELU: the rest of the statistics
   auto live_at = [&](i64 m0) { return m0 + l.team < p.n.M && l.n; };
   auto stats_of = [&](Image& q, i64 m0) {
-    const float2 st = live_at(m0) ? *reinterpret_cast<const float2*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 2) : make_float2(0.f, 0.f);
-    q.r = st.y;
-    q.shift = -st.x * st.y;
+    const float4 st = live_at(m0) ? *reinterpret_cast<const float4*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    q.r = st.z;
+    q.shift = -st.x * st.z;
+    q.mean = st.x;
+    q.mean_l = st.y;
+    q.r_l = st.w;
   };
   auto load = [&](Image& q, i64 m0, i64 px) {
     Rows<T, PHASE> x(p.n.x, l, p.n.P, p.n.ldx, m0), dy(p.n.dy, l, p.n.P, p.n.ldy, m0);
@@ -501,12 +534,45 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       q.d[k] = load_piece<T, V>(b, l.n);
     }
   };
-  auto dz_of = [&](float xhat, float dyv, int i) {
+  // RELU: which of a piece's values passed, a bit each.  Values next to the border are looked at again with all bits: each that falls on the wrong side is off
+  // by a whole gradient (2e-4 of dbeta's norm at 32 x 56 x 56 x 256).
+  // (next to zero z is off by less than 2^-22 of beta and of gamma mean r, what it is the difference of)
+  float edge = 1.f, steep = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    edge = fmaxf(edge, fabsf(col.be.v[i]));
+    steep = fmaxf(steep, fabsf(col.ga.v[i]));
+  }
+  edge *= 1e-6f;
+  steep *= 1e-6f;
+  auto passed = [&](const Image& q, const Vals<W>& x) {
+    unsigned open = 0;
+    if constexpr (F == CONVBN_NORM_RELU) {
+      float near = INFINITY;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float z = fmaf(fmaf(x.v[i], q.r, q.shift), col.ga.v[i], col.be.v[i]);
+        open |= z > 0.f ? 1u << i : 0u;
+        near = fminf(near, fabsf(z));
+      }
+      if (near < fmaf(steep, fabsf(q.shift), edge)) {
+        // (x - mean) r with what each rounding leaves, in `dl` and `el`; the last product and its sum are rounded once, relative to a result next to 0
+        open = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          const float d = x.v[i] - q.mean, back = d - x.v[i], dl = (x.v[i] - (d - back)) - (q.mean + back) - q.mean_l;
+          const float e = d * q.r, el = fmaf(d, q.r, -e) + fmaf(d, q.r_l, dl * q.r);
+          open |= fmaf(el, col.ga.v[i], fmaf(e, col.ga.v[i], col.be.v[i])) > 0.f ? 1u << i : 0u;
+        }
+      }
+    }
+    return open;
+  };
+  auto dz_of = [&](unsigned open, float xhat, float dyv, int i) {
     if constexpr (F == CONVBN_NORM_NONE) return dyv;
-    const float z = fmaf(xhat, col.ga.v[i], col.be.v[i]);
-    if constexpr (F == CONVBN_NORM_RELU) return z > 0.f ? dyv : 0.f * dyv;   // (an infinite gradient behind a closed ReLU stays one of a kind)
+    if constexpr (F == CONVBN_NORM_RELU) return open >> i & 1 ? dyv : 0.f * dyv;   // (an infinite gradient behind a closed ReLU is none)
     float f, df;
-    act_of<T, F>(z, &f, &df);
+    act_of<T, F>(fmaf(xhat, col.ga.v[i], col.be.v[i]), &f, &df);
     return dyv * df;
   };
   // what an image adds to a lane's columns, and s: the sums of dxhat and dxhat xhat
@@ -516,9 +582,10 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
     for (int k = 0; k < KP; ++k)
       if (k < q.rows) {
         const auto a = vals(q.v[k]), b = vals(q.d[k]);
+        const unsigned open = passed(q, a);
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          const float xhat = fmaf(a.v[i], q.r, q.shift), dz = V != TAIL || i < l.n ? dz_of(xhat, b.v[i], i) : 0.f;
+          const float xhat = fmaf(a.v[i], q.r, q.shift), dz = V != TAIL || i < l.n ? dz_of(open, xhat, b.v[i], i) : 0.f;
           sz.v[i] += dz;
           sx.v[i] = fmaf(dz, xhat, sx.v[i]);
         }
@@ -547,10 +614,11 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       const T* e = add.next();
       if (k >= q.rows) continue;
       const auto a = vals(q.v[k]), b = vals(q.d[k]);
+      const unsigned open = passed(q, a);
       Vals<W> f;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const float xhat = fmaf(a.v[i], q.r, q.shift), dz = dz_of(xhat, b.v[i], i);
+        const float xhat = fmaf(a.v[i], q.r, q.shift), dz = dz_of(open, xhat, b.v[i], i);
         f.v[i] = fmaf(dz, rg.v[i], fmaf(xhat, r1, r0));
       }
       if (p.n.add) {
@@ -564,7 +632,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   const i64 stride = (i64)p.slices * teams * IM;
   int turn = 0;
   for (i64 m0 = (i64)at.slice * teams * IM; m0 < p.n.M; m0 += stride, turn ^= 1) {
-    float* const buf = lds + turn * IM * entries * 2;
+    float* const buf = cols + turn * IM * entries * 2;
     Image q[IM];
     float s[2 * IM] = {};
 #pragma unroll
@@ -587,13 +655,13 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
           add_up(q[0], s);
         }
         team_sums<IM>(l, p.t, s, buf);
-        if (live_at(m0) && l.first) *reinterpret_cast<float2*>(l.entry(p, m, at.seg * p.sections + l.section)) = make_float2(s[0], s[1]);
+        if (live_at(m0) && l.first) *l.entry(p, m, at.seg * p.sections + l.section) = make_double2(s[0], s[1]);
       } else {
         if (live_at(m0))
           for (int i = 0; i < p.segs * p.sections; ++i) {
-            const float2 e = *reinterpret_cast<const float2*>(l.entry(p, m, i));
-            s[0] += e.x;
-            s[1] += e.y;
+            const double2 e = *l.entry(p, m, i);
+            s[0] += (float)e.x;
+            s[1] += (float)e.y;
           }
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           load(q[0], m0, px);
@@ -615,16 +683,16 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
     __syncthreads();   // (the sums' place)
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-      lds[(l.wave * 2 * W + i) * 64 + lane] = dga.v[i];
-      lds[(l.wave * 2 * W + W + i) * 64 + lane] = dbe.v[i];
+      cols[(l.wave * 2 * W + i) * 64 + lane] = dga.v[i];
+      cols[(l.wave * 2 * W + W + i) * 64 + lane] = dbe.v[i];
     }
     __syncthreads();
     if (l.wave >= hop) return;
     for (int w = l.wave + hop; w < NT / 64; w += hop)
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        dga.v[i] += lds[(w * 2 * W + i) * 64 + lane];
-        dbe.v[i] += lds[(w * 2 * W + W + i) * 64 + lane];
+        dga.v[i] += cols[(w * 2 * W + i) * 64 + lane];
+        dbe.v[i] += cols[(w * 2 * W + W + i) * 64 + lane];
       }
   }
   if ((int)threadIdx.x < 1 << l.lpr) {
@@ -746,7 +814,7 @@ Plan plan_of(const Norm& n, bool bwd) {
   p.per_bundle = over(p.bundles);
   p.per_slice = over(p.slices);
   if (bwd) s.sums = align_up((size_t)p.slices * p.segs * n.C * 8, 256);
-  if (!s.whole) s.part = align_up((size_t)n.M * n.groups * p.segs * p.sections * 8, 256);
+  if (!s.whole) s.part = align_up((size_t)n.M * n.groups * p.segs * p.sections * 16, 256);
   s.total = s.part + s.sums;
   return s;
 }
@@ -770,7 +838,7 @@ int grid_of(const NormParams& p) {
 }
 
 template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V> hipError_t run(const NormParams& p, hipStream_t st) {
-  const int turns = p.t.ttlog > 6 ? 2 * IM * (BWD ? 2 : 3) * 4 * (NT / 64 << p.t.nblog) : 0;
+  const int turns = p.t.ttlog > 6 ? 2 * IM * (BWD ? 2 * 4 : 3 * (int)sizeof(Sum<F>)) * (NT / 64 << p.t.nblog) : 0;
   if constexpr (BWD) {
     constexpr int COLS = NT * 8 * width_of<V>;
     static LdsLimitOnce once;
@@ -780,14 +848,18 @@ template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V>
     const int cols = p.sums && PHASE != OUTPUTS ? COLS : 0;
     k<<<grid_of(p), NT, cols > turns ? cols : turns, st>>>(p);
   } else {
-    norm_fwd_kernel<T, F, NT, KP, IM, PHASE, V><<<grid_of(p), NT, turns, st>>>(p);
+    static LdsLimitOnce once;
+    auto* k = &norm_fwd_kernel<T, F, NT, KP, IM, PHASE, V>;
+    const hipError_t e = set_lds_limit_once(once, (const void*)k, 2 * IM * 3 * (int)sizeof(Sum<F>) * NT);   // (64 groups a wave)
+    if (e != hipSuccess) return e;
+    k<<<grid_of(p), NT, turns, st>>>(p);
   }
   return hipGetLastError();
 }
 template <bool BWD, typename T, int F, int V> hipError_t run_plan(const Plan& s, hipStream_t st) {
   constexpr int SIZE = sizeof(T), KP = BWD ? STREAM / 2 : STREAM;
   if (!s.whole) {
-    const hipError_t e = run<BWD, T, BWD ? F : (int)CONVBN_NORM_NONE, 1024, KP, 1, SUMS, V>(s.p, st);
+    const hipError_t e = run<BWD, T, BWD || F == CONVBN_NORM_RELU ? F : (int)CONVBN_NORM_NONE, 1024, KP, 1, SUMS, V>(s.p, st);
     return e != hipSuccess || (BWD && !s.p.n.dx) ? e : run<BWD, T, F, 1024, KP, 1, OUTPUTS, V>(s.p, st);
   }
   if (s.nt == 1024) return run<BWD, T, F, 1024, FEW, 1, WHOLE, V>(s.p, st);

@@ -14,9 +14,9 @@
 // stream) or a raw handle.  Tensors are dense.  call_rows checks each against the descriptor, by one letter of `kinds`:
 //   x z h y  rows of desc's type, [M, K] ldx apart, [M, N] ldz, [M, 2 K] ldx, [M, K] ldz;   W  a dense weight [N, K]
 //   c d e    codes of M, N, 2 M rows of K channels;   s n t m  fp32 vectors of M, N, 2 M, 2 N
-//   f g      scale bytes of M, N rows of K channels in 8-bit floating point;   V k  dense [2 N, K], [M, 2 N] of desc's type;   l  dense fp32 [M, 2 N]
+//   f g      scale bytes of M, N rows of K channels in 8-bit floating point;   V  dense [2 N, K] of desc's type;   l  dense fp32 [M, 2 N]
 // call_norm:
-//   x y      rows of desc's type, [M P, C], ldx or ldy apart;   v  fp32 vectors of C;   s  dense fp32 [M, groups, 2]
+//   x y      rows of desc's type, [M P, C], ldx or ldy apart;   v  fp32 vectors of C;   s  dense fp32 [M, groups, 4]
 #include <Python.h>
 
 #include <c10/hip/HIPStream.h>
@@ -86,7 +86,6 @@ Spec spec_of(char kind, const convbn_qdesc* d) {
     case 'y': return {M, K, d->ldz};
     case 'W': return {N, K};
     case 'V': return {2 * N, K};
-    case 'k': return {M, 2 * N};
     case 'l': return {times(M, 2 * N), 1, 0, false, true};
     case 'c': return {M, Kp, 0, true};
     case 'd': return {N, Kp, 0, true};
@@ -106,7 +105,7 @@ Spec spec_of(char kind, const convbn_norm_desc* d) {
     case 'y': return {times(d->M, d->P), d->C, d->ldy};
     case 'v': return {d->C, 1, 0, false, true};
   }
-  return {times(d->M, 2 * (int64_t)d->groups), 1, 0, false, true};
+  return {times(d->M, 4 * (int64_t)d->groups), 1, 0, false, true};
 }
 
 // Whether a tensor is what an entry point reads or writes in its place; false with a Python error set.

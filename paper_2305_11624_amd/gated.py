@@ -23,22 +23,17 @@ class Gated:
     """y = f(x Wg^T + bg) (x Wu^T + bu) on M rows of C channels, F out: both projections, f = "silu" or "gelu" and the product in one call.
     W = [Wg; Wu] is [2 F, C] (g's rows first), b = [bg; bu] float32 [2 F] or None.
 
-    train: there are buffers for `backward`, which reads x and W again.  keep: h = [g | u] is kept for it, of dtype without b and float32 with it;
-    without, it multiplies x and W once more and 2 F numbers a row need not be kept.  bias: b is ever given; else h needs room in dtype alone.  gap: x, dx, y and dy are rows of buffers with `gap` elements between the rows.  y, dx: rows that the
+    train: there are buffers for `backward`, which reads x and W again.  keep: h = [g | u] is kept for it, in float32; without, it multiplies x and W
+    once more, with the same result, and 2 F numbers a row need not be kept.  gap: x, dx, y and dy are rows of buffers with `gap` elements between the rows.  y, dx: rows that the
     layer writes, ws: bytes that it works in (`workspace_bytes`), where several layers share them."""
 
-    def __init__(self, M: int, C: int, F: int, dtype=torch.bfloat16, kind: str = "silu", train: bool = True, keep: bool = True, bias: bool = True,
-                 gap: int = 0, device="cuda", y: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    def __init__(self, M: int, C: int, F: int, dtype=torch.bfloat16, kind: str = "silu", train: bool = True, keep: bool = True, gap: int = 0,
+                 device="cuda", y: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
         self.M, self.C, self.F, self.dtype, self.train = M, C, F, dtype, train
         self.ldx, self.ldy = C + gap, F + gap
         self.desc, self._add_desc = (B.make_qdesc(M, C, F, _dtype(dtype), self.ldx, self.ldy, gate=_GATES[kind]) for _ in range(2))
         self.y = _rows(y, M, F, self.ldy, dtype, device, "y")
-        self.h = self._h_bias = None      # the same memory, as it is kept without b and with it
-        if train and keep:
-            room = torch.empty(M, 2 * F, dtype=torch.float32 if bias else dtype, device=device)
-            self.h = room if room.dtype is dtype else room.view(dtype).view(-1)[:M * 2 * F].view(M, 2 * F)
-            self._h_bias = room if bias else None
-        self._bias = bias
+        self.h = torch.empty(M, 2 * F, dtype=torch.float32, device=device) if train and keep else None
         self.dx = _rows(dx, M, C, self.ldx, dtype, device, "dx") if train else None
         self.dW = torch.empty(2 * F, C, dtype=dtype, device=device) if train else None
         self.db = torch.empty(2 * F, dtype=torch.float32, device=device) if train else None
@@ -47,15 +42,10 @@ class Gated:
             raise ValueError(f"ws: {ws.nbytes} bytes, {need} needed")
         self.ws = ws if ws is not None else torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
-    def _kept(self, b):
-        if b is not None and not self._bias:
-            raise RuntimeError("this layer was made without b (bias=False)")
-        return self.h if b is None else self._h_bias
-
     def forward(self, x: torch.Tensor, W: torch.Tensor, b: Optional[torch.Tensor] = None, stream=None):
         if x is None or W is None:
             raise ValueError("x, W: expected rows and a weight")
-        B.convbn_glu_fwd(self.desc, x, W, b, self.y, self._kept(b), self.ws, stream)
+        B.convbn_glu_fwd(self.desc, x, W, b, self.y, self.h, self.ws, stream)
         return self.y
 
     def backward(self, x: torch.Tensor, W: torch.Tensor, dy: torch.Tensor, b: Optional[torch.Tensor] = None, need_dx: bool = True,
@@ -73,12 +63,12 @@ class Gated:
             d = self._add_desc
             d.act, d.add_in = B.ACT_ADD_IN, add.data_ptr()
         dx, dW, db = self.dx if need_dx else None, self.dW if need_dW else None, self.db if b is not None else None
-        B.convbn_glu_bwd(d, x, W, b, self._kept(b), dy, dx, dW, db, self.ws, stream)
+        B.convbn_glu_bwd(d, x, W, b, self.h, dy, dx, dW, db, self.ws, stream)
         return dx, dW, db
 
     def saved_bytes(self) -> int:
         """h: what backward needs of the forward pass beside x and W."""
-        return 0 if self.h is None else (self.h if self._h_bias is None else self._h_bias).nbytes
+        return 0 if self.h is None else self.h.nbytes
 
 
 class NormGatedBlock:
@@ -101,7 +91,7 @@ class NormGatedBlock:
                 raise ValueError("share: a block that is not trained has no gradients to share")
             ws, y, dy, dn, dx = share.gated.ws, share.gated.y, share.down.dx, share.gated.dx, share.norm.dx
         self.norm = _norm.GroupNorm(images, pixels, C, groups, dtype, eps=eps, train=train, device=device, dx=dx, ws=ws)
-        self.gated = Gated(M, C, F, dtype, kind, train, keep, bias=False, device=device, y=y, dx=dn, ws=ws)
+        self.gated = Gated(M, C, F, dtype, kind, train, keep, device=device, y=y, dx=dn, ws=ws)
         self.down = Q.F8Linear(M, F, C, dtype, train, device=device, dx=dy, ws=ws)
 
     def pack_weight(self, W_down: torch.Tensor, stream=None):

@@ -37,7 +37,7 @@ class GroupNorm:
                                      for _ in range(2))   # (the second with an addend)
         self.y = _rows(y, self.rows, C, self.ld, dtype, device, "y")
         self.dx = _rows(dx, self.rows, C, self.ld, dtype, device, "dx") if train else None
-        self.stats = torch.empty(images * groups * 2, dtype=torch.float32, device=device) if train else None
+        self.stats = torch.empty(images * groups * 4, dtype=torch.float32, device=device) if train else None
         self.dgamma, self.dbeta = (torch.empty(C, dtype=torch.float32, device=device) if train else None for _ in range(2))
         need = workspace_bytes(images, pixels, C, groups, dtype, train, gap)
         if ws is not None and ws.nbytes < need:

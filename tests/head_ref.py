@@ -119,7 +119,7 @@ def act_error(kind, dtype, g):
 
 # ---- gated product -------------------------------------------------------------------------------------------------
 
-def gated(x, W, b, kind, dtype, dy=None, kept=True, add=None):
+def gated(x, W, b, kind, dtype, dy=None, add=None):
     """Results and how far each may be off: {name: (value, allowed)}.  Sums of R terms t: (R + 8) U sum |t|; each rounding half a step."""
     M, K = x.shape
     F, hs = W.shape[0] // 2, half(dtype)
@@ -136,11 +136,6 @@ def gated(x, W, b, kind, dtype, dy=None, kept=True, add=None):
     out = dict(y=(y, ey + hs * (np.abs(y) + ey)))
     if dy is None:
         return out
-    if kept and dtype == "bf16" and b is None:      # (with b, h is kept in fp32)
-        dg, du = dg + hs * (np.abs(g) + dg), du + hs * (np.abs(u) + du)
-        slope = np.abs(df) + ddf * dg
-        rf, rdf = act_error(kind, dtype, np.abs(g) + dg)
-        ef = slope * dg + rf * (np.abs(f) + slope * dg)
     edf = ddf * dg + rdf
     gu = np.concatenate([dy * u * df, dy * f], 1)
     e = np.concatenate([np.abs(dy) * ((np.abs(u) + du) * edf + np.abs(df) * du), np.abs(dy) * ef], 1) + 3 * U * np.abs(gu)

@@ -223,7 +223,7 @@ def test_gated_product(M, K, F, dtype, kind, bias, gap, keep):
     xd, Wd, bd, dyd = on_device(x, gap, dt), W.to("cuda", dt), b.cuda() if bias else None, on_device(dy, gap, dt)
     y = lay.forward(xd, Wd, bd)
     dx, dW, db = lay.backward(xd, Wd, dyd, bd, add=on_device(add, gap, dt))
-    want = R.gated(*(np64(t) for t in (x, W)), np64(b) if bias else None, kind, dtype, np64(dy), keep, np64(add))
+    want = R.gated(*(np64(t) for t in (x, W)), np64(b) if bias else None, kind, dtype, np64(dy), np64(add))
     within(y, *want["y"], "y")
     within(dx, *want["dx"], "dx")
     within(dW, *want["dW"], "dW")
@@ -242,11 +242,10 @@ def test_gated_product_gives_what_is_asked_for(dtype):
     lay = G.Gated(M, K, F, dt)
     lay.forward(x, W, b)
     full = [t.clone() for t in lay.backward(x, W, dy, b)]
-    h = lay._kept(b)
     for need_dx, need_dW, bias in [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1), (0, 1, 1), (1, 1, 0)]:
         for t in (lay.dx, lay.dW, lay.db):
             t.fill_(7)
-        st = B.convbn_glu_bwd(lay.desc, x, W, b, h, dy, lay.dx if need_dx else None, lay.dW if need_dW else None, lay.db if bias else None, lay.ws)
+        st = B.convbn_glu_bwd(lay.desc, x, W, b, lay.h, dy, lay.dx if need_dx else None, lay.dW if need_dW else None, lay.db if bias else None, lay.ws)
         assert st == B.OK
         for got, want, asked in zip((lay.dx, lay.dW, lay.db), full, (need_dx, need_dW, bias)):
             assert torch.equal(got, want) if asked else (got == 7).all()
@@ -325,9 +324,9 @@ def test_group_norm(images, P, C, G, act, gap, affine, dtype):
     want = R.norm(np64(x), images, G, act, dtype, np64(ga) if affine else None, np64(be) if affine else None, 1e-5, np64(dy))
     y = lay.forward(xd, gd, bd)
     within(y, *want["y"], "y")
-    stats = lay.stats.view(-1, 2)
-    within(stats[:, 0], *want["mean"], "mean")
-    within(stats[:, 1], *want["rstd"], "rstd")
+    stats = lay.stats.view(-1, 4).double()      # each as a number and what it leaves
+    within(stats[:, 0] + stats[:, 1], *want["mean"], "mean")
+    within(stats[:, 2] + stats[:, 3], *want["rstd"], "rstd")
     dx, dgamma, dbeta = lay.backward(xd, gd, bd, dyd)
     for got, name in ((dx, "dx"), (dgamma, "dgamma"), (dbeta, "dbeta")):
         within(got, *want[name], name)
@@ -454,7 +453,7 @@ def test_block_is_its_parts(images, P, C, F, groups, keep):
     dy = np64(blk.down.dx)
     within(blk.down.dx, d @ w8, (C + 10) * U * (np.abs(d) @ np.abs(w8)), "dy")
     within(dWd, d.T @ y8, (images * P + 10) * U * (np.abs(d).T @ np.abs(y8)), "dW_down")
-    gb = R.gated(np64(blk.norm.y), np64(Wu), None, "silu", "f32", dy, keep)
+    gb = R.gated(np64(blk.norm.y), np64(Wu), None, "silu", "f32", dy)
     within(blk.gated.dx, *gb["dx"], "dn")
     within(dWu, *gb["dW"], "dW_up")
     nb = R.norm(np64(x), images, groups, "none", "f32", np64(ga), np64(be), 1e-5, np64(blk.gated.dx), d)
