@@ -533,3 +533,112 @@ def test_results_do_not_change_from_run_to_run():
         got = [t.clone() for t in [blk.forward(x, Wu, ga, be)] + list(blk.backward(x, Wu, ga, be, dout))]
         first = first or got
         assert all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+# ---- every tile, split and launch of the products, every walk of group norm ------------------------------------------
+
+# Tiles of 128 and 256 with one and with two workgroups a compute unit, entire sums and parts of them, products in one launch and in two, each with
+# tails in every direction
+LARGE = [(2000, 130, 3001), (3001, 200, 3500), (3500, 3001, 200), (200, 3001, 3500), (600, 8200, 600), (1000, 4096, 1030), (1568, 2048, 520), (5000, 72, 4100)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", LARGE)
+def test_large_f8_linear_of_whole_numbers_is_exact(M, K, N, dtype):
+    dt = DT[dtype]
+    x, W, dz, addx = (_whole(*s, M + i, m) for i, (s, m) in enumerate([((M, K), 8), ((N, K), 8), ((M, N), 3), ((M, K), 50)]))
+    lay = _f8_layer(M, K, N, dtype)
+    lay.pack_weight(W.to("cuda", dt))
+    z = lay.forward(x.to("cuda", dt))
+    assert torch.equal(z.cpu(), (x.double() @ W.double().T).float().to(dt))
+    # (the three ways to ask: both products, each alone)
+    want_x, want_W = (dz.double() @ W.double() + addx.double()).float().to(dt), (dz.double().T @ x.double()).float().to(dt)
+    for need in ((True, True), (True, False), (False, True)):
+        lay.dx.fill_(7)
+        lay.dW.fill_(7)
+        dx, dW, _ = lay.backward(dz.to("cuda", dt), need_dx=need[0], need_dW=need[1], add=addx.to("cuda", dt) if need[0] else None)
+        assert dx is None or torch.equal(dx.cpu(), want_x)
+        assert dW is None or torch.equal(dW.cpu(), want_W)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,F", [(2000, 130, 1501), (3001, 200, 1750), (2060, 2048, 1026), (600, 4100, 300), (1568, 520, 1024), (5000, 72, 2050)])
+def test_large_gated_product(M, K, F, dtype):
+    G, dt = _mods()[1], DT[dtype]
+    x, W, b, dy = _glu_case(M, K, F, dtype, M + K + F)
+    lay = G.Gated(M, K, F, dt, "silu", keep=True)
+    xd, Wd, bd, dyd = x.to("cuda", dt), W.to("cuda", dt), b.cuda(), dy.to("cuda", dt)
+    y = lay.forward(xd, Wd, bd)
+    want = R.gated(*(np64(t) for t in (x, W)), np64(b), "silu", dtype, np64(dy))
+    within(y, *want["y"], "y")
+    got = [t.clone() for t in lay.backward(xd, Wd, dyd, bd)]
+    for t, name in zip(got, ("dx", "dW", "db")):
+        within(t, *want[name], name)
+    again = G.Gated(M, K, F, dt, "silu", keep=False)      # the projections a second time: the same bits
+    assert torch.equal(again.forward(xd, Wd, bd), y)
+    assert all(torch.equal(a, b) for a, b in zip(again.backward(xd, Wd, dyd, bd), got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("images,P,C,G", [(32, 3136, 64, 8), (8, 3136, 256, 32), (40, 49, 2048, 32), (5, 891, 72, 8), (2000, 1, 4096, 1), (1, 40000, 8, 1), (3, 5000, 100, 4)])
+def test_group_norm_decides_every_value_next_to_the_border(images, P, C, G, dtype):
+    """dy = 1: dbeta is the number of values that passed, which 32 bits hold."""
+    N, dt = _mods()[2], DT[dtype]
+    for seed in range(3):
+        x, ga, be, _ = _norm_case(images, P, C, dtype, 50 + seed)
+        lay = N.GroupNorm(images, P, C, G, dt, act="relu")
+        xd, gd, bd = x.to("cuda", dt), ga.cuda(), be.cuda()
+        lay.forward(xd, gd, bd)
+        dbeta = lay.backward(xd, gd, bd, torch.ones_like(xd))[2]
+        g4 = xd.double().view(images, P, G, C // G)
+        mean = g4.mean((1, 3), keepdim=True)
+        r = ((g4 - mean).square().mean((1, 3), keepdim=True) + float(np.float32(1e-5))).rsqrt()
+        z = (g4 - mean) * r * gd.double().view(G, -1) + bd.double().view(G, -1)
+        assert torch.equal(dbeta.double(), (z > 0).sum((0, 1)).double().view(-1)), seed
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_a_wide_buffer_are_copied_where_they_cannot_be_read_in_place(dtype):
+    """Rows 2^21 elements apart, and rows that start off a 16-byte border: the same bits as from rows next to each other."""
+    G, dt, M, K, F = _mods()[1], DT[dtype], 40, 64, 48
+    x, W, b, dy = _glu_case(M, K, F, dtype, 3)
+    results = []
+    for gap in (0, (1 << 21) - K, 3):
+        lay = G.Gated(M, K, F, dt, "silu", gap=gap)
+        xd, dyd = on_device(x, gap, dt), on_device(dy, gap, dt)
+        y = lay.forward(xd, W.to("cuda", dt), b.cuda())
+        results.append([y.clone()] + [t.clone() for t in lay.backward(xd, W.to("cuda", dt), dyd, b.cuda())])
+    for r in results[1:]:
+        assert all(torch.equal(p, q) for p, q in zip(r, results[0]))
+
+
+def test_two_graphs_of_one_block_take_turns():
+    """Two captured graphs on one workspace, replayed one after the other, and an eager call between them."""
+    sizes = (2, 49, 64, 136, 8, torch.bfloat16)
+    blk = _block(*sizes)
+    ins = [[t.clone() for t in _block_inputs(*sizes[:4], torch.bfloat16)] for _ in range(2)]
+    ins[1][0].mul_(-0.5)
+
+    def step(x, Wu, Wd, ga, be, dout):
+        blk.pack_weight(Wd)
+        return [t.clone() for t in [blk.forward(x, Wu, ga, be)] + list(blk.backward(x, Wu, ga, be, dout))]
+
+    want = [step(*i) for i in ins]
+    graphs, outs = [], []
+    for i in ins:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            step(*i)
+        torch.cuda.current_stream().wait_stream(side)
+        with torch.cuda.graph(graph):
+            outs.append(step(*i))
+        graphs.append(graph)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        step(*ins[0])
+        for o, w in zip(outs, want):
+            assert all(torch.equal(a, b) for a, b in zip(o, w))
