@@ -391,6 +391,15 @@ template <int KP> __device__ __forceinline__ int rows_from(const Lane& l, bool l
   return !live || n <= 0 ? 0 : n < KP ? (int)n : KP;
 }
 
+// Calls f for each of a group's segments, a lane of each wave for a part of them, and sums what they add to s (1 x 2289 x 1472, one group: the
+// outputs' launch 13 us; every lane all of them, one after the other, 34).
+template <int N, typename A, class F> __device__ __forceinline__ void over_entries(const NormParams& p, const Lane& l, A (&s)[N], F&& f) {
+  const int lane = threadIdx.x & 63, of = p.t.nblog ? (lane >> l.lpr << p.t.mlog) | (lane & ((1 << p.t.mlog) - 1)) : lane;   // (groups side by side fit a wave)
+  if (l.g < p.n.groups)
+    for (int i = of; i < p.segs * p.sections; i += 64 >> p.t.nblog) f(i);
+  l.wave_sums(p.t, s);
+}
+
 // IM: images at a time (WHOLE)
 template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
   using A = Sum<F>;
@@ -480,13 +489,24 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
         if (live_at(m0) && l.first) *l.entry(p, m, at.seg * p.sections + l.section) = make_double2(a[0].mean, a[0].m2);
       } else {
         col = columns_of<V>(p.n, l);
-        if (live_at(m0))
-          for (int s = 0; s < p.segs; ++s)
-            for (int e = 0; e < p.sections; ++e) {
-              const double2 q = *l.entry(p, m, s * p.sections + e);
-              const i64 px = p.n.P - s * p.seg < p.seg ? p.n.P - s * p.seg : p.seg;
-              merge(a[0], {(A)px * (A)min(p.span, p.cg - e * p.span), (A)q.x, (A)q.y});
-            }
+        auto part = [&](int i) {
+          const int s = i / p.sections, e = i - s * p.sections;
+          const i64 px = p.n.P - s * p.seg < p.seg ? p.n.P - s * p.seg : p.seg;
+          const double2 q = *l.entry(p, m, i);
+          return Moments<A>{(A)px * (A)min(p.span, p.cg - e * p.span), (A)q.x, (A)q.y};
+        };
+        A sum[1] = {A(0)}, m2[1] = {A(0)};
+        over_entries(p, l, sum, [&](int i) {
+          const Moments<A> b = part(i);
+          sum[0] += b.n * b.mean;
+        });
+        const A mean = sum[0] / count;
+        over_entries(p, l, m2, [&](int i) {
+          const Moments<A> b = part(i);
+          const A d = b.mean - mean;
+          m2[0] += b.m2 + b.n * d * d;
+        });
+        a[0] = {count, mean, m2[0]};
         const Stats<A> z = stats_of(a[0], pivot, count, p.n.eps);
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           const int rows = load(v[0], m0, px);
@@ -657,12 +677,11 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
         team_sums<IM>(l, p.t, s, buf);
         if (live_at(m0) && l.first) *l.entry(p, m, at.seg * p.sections + l.section) = make_double2(s[0], s[1]);
       } else {
-        if (live_at(m0))
-          for (int i = 0; i < p.segs * p.sections; ++i) {
-            const double2 e = *l.entry(p, m, i);
-            s[0] += (float)e.x;
-            s[1] += (float)e.y;
-          }
+        over_entries(p, l, s, [&](int i) {
+          const double2 e = *l.entry(p, m, i);
+          s[0] += (float)e.x;
+          s[1] += (float)e.y;
+        });
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           load(q[0], m0, px);
           put(q[0], m0, px, s[0] / count, s[1] / count);
@@ -737,6 +756,7 @@ int log2_up(i64 v) {
 }
 
 constexpr int CUS = 256, MAX_LANES = 1024;   // of a group's pixel
+constexpr int SEGS = 256;   // of an image, at most: the join and every workgroup of the outputs read one number of each
 
 // How a call is run: workgroups of nt, the teams, one launch or two
 struct Plan {
@@ -747,7 +767,7 @@ struct Plan {
 };
 // Pieces that a lane's registers hold, of workgroups of 256 and 512
 constexpr int most_of(int size, bool bwd, int nt, int v) {
-  return v == ONES ? nt == 512 ? 32 : 8 : (nt == 512 ? bwd ? 16 : 32 : bwd ? 4 : 8) * 2 / size;
+  return v == ONES ? nt == 512 ? 32 : 16 : (nt == 512 ? bwd ? 16 : 32 : bwd ? 4 : 8) * 2 / size;
 }
 constexpr int FEW = 2, STREAM = 4;   // pieces a lane: of short parts, of a turn of the segments' launches
 constexpr int images_at_once(int size, bool bwd) { return (bwd ? 4 : 8) / size; }   // that have one piece a lane
@@ -767,8 +787,10 @@ Plan plan_of(const Norm& n, bool bwd) {
   t.mlog = log2_up(t.m);
   const int glog = log2_up(n.groups);
   // groups side by side until a pixel's part is 64 bytes, or until a wave is full of pieces of few channels (32 x 56 x 56 x 256, parts of 32 bytes: forward
-  // 48.6 us instead of 24; backward in one launch 53 us, in two with parts of 64 bytes 50)
-  while (t.nblog < glog && t.mlog + t.nblog < 6 && (p.cg << t.nblog) * size < 64) ++t.nblog;
+  // 48.6 us instead of 24; backward in one launch 53 us, in two with parts of 64 bytes 50).  Single 16-bit channels of rows that begin inside such a part: 128
+  // bytes (groups of one channel, forward and backward, 3 x 1884 x 3123 174 us, with 64 bytes 235; 8 x 3136 x 256 89 and 76; 52 x 132 x 472 fp32 50 and 34)
+  const int part = s.pieces == ONES && size == 2 && n.ldx % 32 ? 128 : 64;
+  while (t.nblog < glog && t.mlog + t.nblog < 6 && (p.cg << t.nblog) * size < part) ++t.nblog;
   auto lanes = [&](int log) { return (n.P + (1LL << (log - t.lprlog)) - 1) >> (log - t.lprlog); };   // pieces of a lane
   auto fits = [&] { return p.sections == 1 && (t.lprlog <= 9 ? lanes(9) <= most_of(size, bwd, 512, s.pieces) : n.P <= FEW); };
   t.lprlog = t.mlog + t.nblog;
@@ -797,11 +819,13 @@ Plan plan_of(const Norm& n, bool bwd) {
     t.ttlog = t.lprlog;
     s.nt = 1024;
     t.ttlog = 10;
-    // two workgroups a compute unit, each with two turns of its lanes at least
+    // two workgroups a compute unit, each with a turn of its lanes at least, or with two where there is one for each of them anyway (32 x 56 x 56 x 256 88
+    // us; with one turn 98)
     const i64 turn = (i64)STREAM << (10 - t.lprlog);
     i64 segs = n.M ? 2 * CUS / (n.M * p.bundles) : 1;
-    if (segs > n.P / (2 * turn)) segs = n.P / (2 * turn);
-    p.segs = (int)(segs < 1 ? 1 : segs < 64 ? segs : 64);
+    const i64 most = n.P / (n.M * p.bundles < CUS ? turn : 2 * turn);
+    if (segs > most) segs = most;
+    p.segs = (int)(segs < 1 ? 1 : segs < SEGS ? segs : SEGS);
   }
   p.seg = (n.P + p.segs - 1) / p.segs;
   p.segs = (int)((n.P + p.seg - 1) / p.seg);
