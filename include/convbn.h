@@ -524,7 +524,7 @@ convbn_status convbn_qgate_bwd(const convbn_qdesc *desc, const void *h_codes, co
  *   backward   dx[m,k] = sum_n dz[m,n] w8[n,k]     dW[n,k] = sum_m dz[m,n] x8[m,k]     db[n] = sum_m dz[m,n]
  * Backward is the gradient of the product of the two rounded operands; the rounding itself passes it on unchanged.  dz is not rounded: bf16
  * gradients meet x8 and w8 as they are, fp32 ones in three bf16 parts that add up to them.  Sums are fp32, with one exception: forward with
- * dtype BF16 and more than 16 rows (or fewer long ones) may add the eight products of neighbouring channels 8 i .. 8 i + 7 with 13 bits below the leading bit of the
+ * dtype BF16 and more than 16 rows (or fewer whose channels do not fit LDS) may add the eight products of neighbouring channels 8 i .. 8 i + 7 with 13 bits below the leading bit of the
  * largest (the matrix instruction for these codes; what it drops is below 7 2^-13 of that product, and 2^-15 of the sum of all sizes on average).
  *
  * Strides, addends, alignment, limits, empty calls and the meaning of NULL are those of the 8-bit rows; scales are 4-byte aligned. */
@@ -571,8 +571,9 @@ convbn_status convbn_glu_bwd(const convbn_qdesc *desc, const void *x, const void
  * bits which values next to its border passed; 0 for the other activations): nullable in forward, what backward needs beside x.  gamma, beta: [C] fp32, NULL = ones,
  * zeros.  (P = 1, groups = 1: a norm over each token's channels.)
  *   backward   dx (+ add_in), dgamma, dbeta: nullable, each = not wanted; beta is read for f' alone.
- * Sums and statistics are fp32; the variance is summed from differences to a mean.  M == 0 is no error: dgamma and dbeta become zero.  Rows need the
- * alignment of their element (16 bytes are faster).  y may not be x where backward is to read x. */
+ * Sums and statistics are fp32, in front of a ReLU what lanes found is merged in 64 bits; the variance is summed from differences to a mean.
+ * M == 0 is no error: dgamma and dbeta become zero.  Rows need the alignment of their element (16 bytes are faster).  Outputs overlap no input, but for the
+ * addend; y that is x is refused. */
 typedef struct {
   int64_t M, P;               /* images, pixels of an image                                  */
   int64_t ldx, ldy;           /* elements from a pixel of x / dx (y / dy) to the next; 0 = C */

@@ -184,6 +184,7 @@ convbn_status convbn_norm_fwd(const convbn_norm_desc* desc, const void* x, const
   const uintptr_t elem = n.dtype == CONVBN_BF16 ? 2 : 4;
   REQUIRE_ROWS(x, elem); OPTIONAL(gamma, 4); OPTIONAL(beta, 4); REQUIRE_ROWS(y, elem); OPTIONAL(stats, 4);
   if (!n.M) return CONVBN_OK;
+  if (x == y) return set_error(CONVBN_ERR_UNSUPPORTED, "y is x: other workgroups read a group's first value when its outputs are written");
   TRY_STATUS(check_ws(norm_scratch(n, CONVBN_PASS_FWD), ws, ws_bytes));
   n.x = x; n.gamma = gamma; n.beta = beta; n.y = y; n.stats = stats;
   LAUNCH(launch_norm_fwd(n, ws, (hipStream_t)stream));

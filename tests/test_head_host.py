@@ -208,3 +208,9 @@ def test_native_call_takes_the_norm_descriptor_only():
             B._call_norm(at, bad, "xvvys", None, None, None, None, None, None, 0)
     with pytest.raises(TypeError):
         B._call_rows(at, _ndesc(), "xvvys", None, None, None, None, None, None, 0)
+
+
+def test_group_norm_in_place_is_refused():
+    """Large parts take two launches, the second of which reads every group's first value again."""
+    assert nfwd(_ndesc()) == nfwd(_ndesc(M=1, P=5000, groups=1)) == B.ERR_UNSUPPORTED and "y is x" in B.convbn_last_error()
+    assert nfwd(_ndesc(M=0), p0=None, p3=None) == B.OK
