@@ -4,9 +4,9 @@
 // the sum is done, and neither goes to memory unless it is kept.  Backward turns g, u and dy into dh = [dg | du] in one pass, which sums dh's columns too,
 // and multiplies it with W and with x as they lie.
 //
-// Bound by the matrix pipe and by LDS (mm_tile.h): 8192 x 4096 -> 8192 forward 955 us, 1150 TFLOP/s; dx and dW 848 and 857, 1300 each; dh in front of them 177,
-// of 805 MB read and written at 4.5 TB/s.  The projections are kept in 32 bits: kept in bf16 they cost 122 us instead, and the gradients a third of their bits
-// (relative 2-norm of dW against 64 bits 0.003 instead of 0.002).
+// Bound by the matrix pipe (mm_tile.h): 8192 x 4096 -> 8192 forward 955 us, 1150 TFLOP/s; dx and dW 848 and 857, 1300 each; dh in front of them 172, 940 MB read
+// and written at 5.4 TB/s.  The projections are kept in 32 bits: kept in bf16 that pass takes 122, and the gradients are off by a third more
+// (relative 2-norm against 64 bits 0.003 instead of 0.0023, where dh in bf16 and the result's own rounding make 0.0023).
 //
 // F32: operands are split into three bf16 parts that add up to all 24 bits, and the six products of parts that are not below 2^-24 of the whole are summed
 // in fp32: nothing is rounded below that.

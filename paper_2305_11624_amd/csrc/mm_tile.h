@@ -453,8 +453,8 @@ template <class Op, bool TA, bool TB, bool DUAL, int PAIRS, class OUT> hipError_
   const bool alone = mm_alone(p);
   // (all of LDS, where scales do not need a part of it.  us, products of 8192 x 8192, 4096 with both halves and of 8192 x 16384, 4096 along and across:
   // waves of 128 x 64 with five halves 892, 834, 809; with four 915, 876, 868; of 64 x 128 924, 833, 809; four of 128 x 128 996, 896, 857; in 8-bit
-  // floating point 8192 x 8192, 4096 waves of 64 x 128 228, four of 128 x 128 273.  Bound by the matrix pipe and by LDS, each busy for half of the time
-  // or more, at the clock that the power allows: the library takes 793, 878 and 987 for the three.)
+  // floating point 8192 x 8192, 4096 waves of 64 x 128 228, four of 128 x 128 273.  The matrix pipe is busy for 66 - 74 % of the
+  // time, in 8 bits 47 - 52 %, LDS for 22 - 29 %; the rest is waiting at chunks and in the epilogue.  The library takes 793, 878 and 987 for the three.)
   constexpr int WIDTH = Op::SCALED ? 64 : 128;
   if (tile == 256) return mm_launch_cfg<MmCfg<Op, 256, WIDTH, 192 - WIDTH, Op::SCALED ? 4 : 5, 1>, TA, TB, DUAL, PAIRS>(p, out, st);
   if (tile == 128)
