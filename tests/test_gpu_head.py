@@ -642,3 +642,10 @@ def test_two_graphs_of_one_block_take_turns():
         step(*ins[0])
         for o, w in zip(outs, want):
             assert all(torch.equal(a, b) for a, b in zip(o, w))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("images,P,C,G,gap", [(1, 2289, 1472, 1, 8), (1, 676, 2872, 4, 5), (1, 6000, 512, 16, 0), (2, 2000, 300, 300, 3), (3, 700, 130, 65, 0)])
+def test_group_norm_of_few_images_in_many_segments(images, P, C, G, gap, act, dtype):
+    test_group_norm(images, P, C, G, act, gap, True, dtype)
