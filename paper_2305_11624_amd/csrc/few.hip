@@ -83,7 +83,7 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
         const int e = f8_exp(bits);
         if (p.codes && blockIdx.x == 0) {
           if (k < Kp) *reinterpret_cast<uint2*>(p.codes + (i64)m * Kp + k) = c;
-          if ((k & (BLK - 1)) == 0 && k / BLK < Sp) p.scales[(i64)m * Sp + k / BLK] = k < K ? (uint8_t)(e + 127) : (uint8_t)127;
+          if ((k & (BLK - 1)) == 0) p.scales[(i64)m * Sp + k / BLK] = (uint8_t)(e + 127);
         }
         v = f8_decode8(c, two_to(e));
       } else if (k < Kp) {
@@ -101,6 +101,10 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
         for (int y = 0; y < 3; ++y) put(y * M + m, k, q[y]);
       }
     }
+  }
+  if (W::F8 && p.x && p.codes && blockIdx.x == 0) {   // scales past the last block, as packing leaves them
+    const int blocks = wide / BLK, pad = Sp - blocks;
+    for (int i = tid; i < M * pad; i += blockDim.x) p.scales[(i64)(i / pad) * Sp + blocks + i % pad] = 127;
   }
   __syncthreads();
 
