@@ -2,9 +2,9 @@
 //
 // A team of lanes takes some neighbouring groups of an image.  A lane holds pieces of eight channels of one group: v counts the pieces of a
 // group's pixel, then come the groups of the team, then the pixels, so that neighbouring lanes read neighbouring memory and a group's lanes meet by
-// exchanging along the bits of v and of the pixel: within a wave by shuffles, between waves through LDS, one barrier an image.  Means are taken
-// relative to the group's first value and variances merged from what each lane finds about its own mean, so neither loses bits to values that lie
-// far from zero.
+// exchanging along the bits of v and of the pixel: within a wave by shuffles, between waves through LDS, one barrier an image.  A wave takes its values
+// twice: for a number near their mean, and for the sums of the differences to that number and of their squares.  So neither the mean nor the variance loses
+// bits to values that lie far from zero, nor to one that lies far from the others.
 //
 // Where a team's part of an image fits the registers (x forward, x and dy backward) it is read once: one launch that reads and writes
 // each number once.  Larger parts, and images that are too few to fill the chip, go in two launches: the sums of segments of the
@@ -186,57 +186,53 @@ struct Lane {
     if (t.mlog > 4 || (t.lprlog < 5 && t.ttlog > 4)) each([](A v) { return across16(v); });
     if (t.mlog > 5 || (t.lprlog < 6 && t.ttlog > 5)) each([](A v) { return across32(v); });
   }
+  // One number for all of a group's lanes of this wave from what wave_sums left in them: turned within rows they add in different orders
+  __device__ __forceinline__ float same(const Team& t, float v) const {
+    return t.ttlog > t.lprlog && t.lprlog < 4 ? __shfl(v, (threadIdx.x & 63 & ~((1u << t.ttlog) - 1)) + (gl << t.mlog), 64) : v;
+  }
   // Where this wave's sums go and the team's begin
   __device__ __forceinline__ int slot(const Team& t, int w) const { return (w << t.nblog) + gl; }
   __device__ __forceinline__ int first_wave() const { return wave & ~(waves - 1); }
   __device__ __forceinline__ bool writes(const Team& t) const { return (int)(threadIdx.x & 63) == (gl << t.mlog & 63); }
 };
 
-// What is merged of the lanes' sums: fp32, or, in front of a ReLU, 64 bits (what is left to err is then a lane's own sums, some 6e-9 of a deviation)
+// What lanes' sums are added up in: fp32, or, in front of a ReLU, 64 bits (what is left to err is then a lane's own sums, some 6e-9 of a deviation)
 template <int F> using Sum = std::conditional_t<F == CONVBN_NORM_RELU, double, float>;
+// Moments about a number that is kept beside them
 template <typename A> struct Moments { A n, mean, m2; };
-template <typename A> __device__ __forceinline__ void merge(Moments<A>& a, const Moments<A>& b) {
-  if (b.n == A(0)) return;
-  const A n = a.n + b.n, d = b.mean - a.mean, q = b.n / n;
+__device__ __forceinline__ void merge(Moments<double>& a, const Moments<double>& b) {
+  if (b.n == 0.) return;
+  const double n = a.n + b.n, d = b.mean - a.mean, q = b.n / n;
   a.mean += d * q;
   a.m2 += b.m2 + d * d * a.n * q;
   a.n = n;
 }
-// Moments of IM images' groups from their lanes'; every lane of the team returns them.  buf: [IM][waves << nblog] entries of three
-template <int IM, typename A> __device__ __forceinline__ void team_moments(const Lane& l, const Team& t, Moments<A> (&a)[IM], A* buf, int entries) {
-  A s[2 * IM], q[IM];
-#pragma unroll
-  for (int i = 0; i < IM; ++i) {
-    s[2 * i] = a[i].n;
-    s[2 * i + 1] = a[i].n * a[i].mean;
-  }
-  l.wave_sums(t, s);
-#pragma unroll
-  for (int i = 0; i < IM; ++i) {
-    const A wmean = s[2 * i] > A(0) ? s[2 * i + 1] / s[2 * i] : A(0), d = a[i].mean - wmean;
-    q[i] = a[i].n > A(0) ? a[i].m2 + a[i].n * d * d : A(0);
-    a[i].n = s[2 * i];
-    a[i].mean = wmean;
-  }
-  l.wave_sums(t, q);
-#pragma unroll
-  for (int i = 0; i < IM; ++i) a[i].m2 = q[i];
+// Moments of IM images' groups: in, of the wave's lanes, about c; out, of the team, about the first wave's c.  That one's distance to the others' is at most
+// some deviations of the values, so that fp32 keeps what counts (about one value of the group it would not: that may lie as many deviations away as the root of the
+// group's size).  buf: [IM][waves << nblog] entries of four
+template <int IM, typename A> __device__ __forceinline__ void join_waves(const Lane& l, const Team& t, Moments<A> (&a)[IM], float (&c)[IM], A* buf, int entries) {
   if (t.ttlog <= 6) return;
   if (l.writes(t)) {
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
-      A* o = buf + (i * entries + l.slot(t, l.wave)) * 3;
-      o[0] = a[i].n; o[1] = a[i].mean; o[2] = a[i].m2;
+      A* o = buf + (i * entries + l.slot(t, l.wave)) * 4;
+      o[0] = a[i].n; o[1] = a[i].mean; o[2] = a[i].m2; o[3] = (A)c[i];
     }
   }
   __syncthreads();
+  // wave w's, about the first one's c
+  auto of = [&](int i, int w) {
+    const A* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 4;
+    return Moments<A>{o[0], o[3] - (A)c[i] + o[1], o[2]};
+  };
+#pragma unroll
+  for (int i = 0; i < IM; ++i) c[i] = (float)buf[(i * entries + l.slot(t, l.first_wave())) * 4 + 3];
   if (t.nblog == 0) {   // one group: 16 lanes read a wave's each
     const int w = threadIdx.x & 15;
-    A mean[IM];
+    A mean[IM], s[2 * IM], q[IM];
 #pragma unroll
     for (int i = 0; i < IM; ++i) {
-      const A* o = buf + (i * entries + l.first_wave() + w) * 3;
-      a[i] = w < l.waves ? Moments<A>{o[0], o[1], o[2]} : Moments<A>{A(0), A(0), A(0)};
+      a[i] = w < l.waves ? of(i, w) : Moments<A>{A(0), A(0), A(0)};
       s[2 * i] = a[i].n;
       s[2 * i + 1] = a[i].n * a[i].mean;
     }
@@ -256,24 +252,35 @@ template <int IM, typename A> __device__ __forceinline__ void team_moments(const
   for (int i = 0; i < IM; ++i) {
     A n = A(0), sum = A(0), m2 = A(0);
     for (int w = 0; w < l.waves; ++w) {
-      const A* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
-      n += o[0];
-      sum += o[0] * o[1];
+      const Moments<A> o = of(i, w);
+      n += o.n;
+      sum += o.n * o.mean;
     }
     const A mean = n > A(0) ? sum / n : A(0);
     for (int w = 0; w < l.waves; ++w) {
-      const A* o = buf + (i * entries + l.slot(t, l.first_wave() + w)) * 3;
-      const A e = o[1] - mean;
-      m2 += o[2] + o[0] * e * e;
+      const Moments<A> o = of(i, w);
+      const A e = o.mean - mean;
+      m2 += o.m2 + o.n * e * e;
     }
     a[i] = {n, mean, m2};
   }
 }
-// A group's statistics from its moments about `pivot`
-template <typename A> struct Stats { A mean, r; };
-template <typename A> __device__ __forceinline__ Stats<A> stats_of(const Moments<A>& a, float pivot, A count, float eps) {
-  if constexpr (sizeof(A) == 8) return {a.mean + pivot, 1. / sqrt(a.m2 / count + eps)};
-  else return {a.mean + pivot, 1.f / sqrtf(a.m2 / count + eps)};
+// ... of lanes' that have each their own, about c
+__device__ __forceinline__ void team_moments(const Lane& l, const Team& t, Moments<double> (&a)[1], float c, double* buf, int entries) {
+  double s[2] = {a[0].n, a[0].n * a[0].mean};
+  l.wave_sums(t, s);
+  const double mean = s[0] > 0. ? s[1] / s[0] : 0., d = a[0].mean - mean;
+  double q[1] = {a[0].n > 0. ? a[0].m2 + a[0].n * d * d : 0.};
+  l.wave_sums(t, q);
+  a[0] = {s[0], mean, q[0]};
+  float about[1] = {c};
+  join_waves(l, t, a, about, buf, entries);
+}
+// A group's statistics from its moments about c
+struct Stats { double mean, r; };
+template <typename A> __device__ __forceinline__ Stats stats_of(const Moments<A>& a, float c, A count, float eps) {
+  if constexpr (sizeof(A) == 8) return {c + a.mean, 1. / sqrt(a.m2 / count + eps)};
+  else return {(double)c + a.mean, 1.f / sqrtf(a.m2 / count + eps)};
 }
 // ... of pairs of sums.  buf: [waves << nblog] entries of 2 IM
 template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const Team& t, float (&s)[2 * IM], float* buf) {
@@ -298,8 +305,8 @@ template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const
     for (int i = 0; i < 2 * IM; ++i) s[i] += buf[l.slot(t, l.first_wave() + w) * 2 * IM + i];
 }
 
-// Moments about `pivot` of KP pieces, rows of which are in
-template <typename A, typename T, int V, int KP> __device__ __forceinline__ Moments<A> moments_of(Held<T, V> (&x)[KP], int rows, int n, float pivot) {
+// Of KP pieces, rows of which are in: the sum of the differences to `pivot`
+template <typename T, int V, int KP> __device__ __forceinline__ float sum_about(const Held<T, V> (&x)[KP], int rows, int n, float pivot) {
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < KP; ++k)
@@ -308,11 +315,13 @@ template <typename A, typename T, int V, int KP> __device__ __forceinline__ Mome
 #pragma unroll
       for (int i = 0; i < width_of<V>; ++i) s += V != TAIL || i < n ? f.v[i] - pivot : 0.f;
     }
-  if (rows * n == 0) return {A(0), A(0), A(0)};
-  const float mean = s / (float)(rows * n);
-  float m2 = 0.f;
+  return s;
+}
+// ... and of their squares
+struct Sums { float m1, m2; };
+template <typename T, int V, int KP> __device__ __forceinline__ Sums sums_about(Held<T, V> (&x)[KP], int rows, int n, float c) {
   as_held(x);
-  const float c = pivot + mean;   // (its rounding d adds n d^2 to the sum, and nothing else: the differences to the mean add up to nothing)
+  Sums s = {0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < KP; ++k)
     if (k < rows) {
@@ -320,14 +329,46 @@ template <typename A, typename T, int V, int KP> __device__ __forceinline__ Mome
 #pragma unroll
       for (int i = 0; i < width_of<V>; ++i) {
         const float d = V != TAIL || i < n ? f.v[i] - c : 0.f;
-        m2 = fmaf(d, d, m2);
+        s.m1 += d;
+        s.m2 = fmaf(d, d, s.m2);
       }
     }
-  if constexpr (sizeof(A) == 8) {   // the mean with all of its bits, and the sum about it
-    const A exact = (A)s / (rows * n), e = (A)c - pivot - exact;
-    return {(A)(rows * n), exact, (A)m2 - e * e * (rows * n)};
+  return s;
+}
+// A lane's moments about `pivot`.  What c is off by (2^-24 of the distance to `pivot` for each addition) is in the sum of the differences to it.
+template <typename T, int V, int KP> __device__ __forceinline__ Moments<double> lane_moments(Held<T, V> (&x)[KP], int rows, int n, float pivot) {
+  const float s = sum_about(x, rows, n, pivot);
+  if (rows * n == 0) return {0., 0., 0.};
+  const float c = pivot + s / (float)(rows * n);
+  const Sums q = sums_about(x, rows, n, c);
+  const double count = rows * n, e = q.m1 / count;
+  return {count, (double)c - pivot + e, q.m2 - e * q.m1};
+}
+// The team's moments of IM images' pieces; c: in, a value of each group, out, what they are about
+template <typename A, int IM, typename T, int V, int KP>
+__device__ __forceinline__ void whole_moments(const Lane& l, const Team& t, Held<T, V> (&x)[IM][KP], const int (&rows)[IM], Moments<A> (&a)[IM], float (&c)[IM], A* buf, int entries) {
+  float s[2 * IM];
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    s[2 * i] = (float)(rows[i] * l.n);
+    s[2 * i + 1] = sum_about(x[i], rows[i], l.n, c[i]);
   }
-  return {(A)(rows * n), mean, m2};
+  l.wave_sums(t, s);
+  A q[2 * IM];
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    c[i] = l.same(t, s[2 * i] > 0.f ? c[i] + s[2 * i + 1] / s[2 * i] : c[i]);
+    const Sums w = sums_about(x[i], rows[i], l.n, c[i]);
+    q[2 * i] = w.m1;
+    q[2 * i + 1] = w.m2;
+  }
+  l.wave_sums(t, q);
+#pragma unroll
+  for (int i = 0; i < IM; ++i) {
+    const A n = s[2 * i], mean = n > A(0) ? q[2 * i] / n : A(0);
+    a[i] = {n, mean, q[2 * i + 1] - mean * q[2 * i]};
+  }
+  join_waves(l, t, a, c, buf, entries);
 }
 
 template <int V> struct Columns { Vals<width_of<V>> ga, be; };
@@ -405,7 +446,7 @@ template <int N, typename A, class F> __device__ __forceinline__ void over_entri
 
 // IM: images at a time (WHOLE)
 template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
-  using A = Sum<F>;
+  using A = std::conditional_t<PHASE == WHOLE, Sum<F>, double>;
   extern __shared__ __align__(16) unsigned char lds[];   // two turns' moments
   Place at;
   if (!place_of(p, &at)) return;
@@ -431,7 +472,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   };
   Columns<V> col;
   if constexpr (PHASE != SUMS && IM > 1) col = columns_of<V>(p.n, l);
-  auto put = [&](Held<T, V> (&v)[KP], i64 m0, i64 px, int rows, const Stats<A>& z) {
+  auto put = [&](Held<T, V> (&v)[KP], i64 m0, i64 px, int rows, const Stats& z) {
     Rows<T, PHASE> y(p.n.y, l, p.n.P, p.n.ldy, m0);
     y.from(px);
     as_held(v);
@@ -449,7 +490,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       store_piece<T, V>(q, l.n, f);
     }
   };
-  auto keep = [&](i64 m0, const Stats<A>& z) {
+  auto keep = [&](i64 m0, const Stats& z) {
     if (p.n.stats && live_at(m0) && l.first && l.section == 0 && at.seg == 0) {
       const float mean = (float)z.mean, r = (float)z.r;
       *reinterpret_cast<float4*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 4) = make_float4(mean, (float)(z.mean - mean), r, (float)(z.r - r));
@@ -458,24 +499,22 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   const i64 stride = (i64)p.slices * teams * IM;
   int turn = 0;   // (every lane of the workgroup takes part in the barrier of every turn)
   for (i64 m0 = (i64)at.slice * teams * IM; m0 < p.n.M; m0 += stride, turn ^= 1) {
-    A* const buf = reinterpret_cast<A*>(lds) + turn * IM * entries * 3;
+    A* const buf = reinterpret_cast<A*>(lds) + turn * IM * entries * 4;
     Held<T, V> v[IM][KP];
     Moments<A> a[IM];
     if constexpr (PHASE == WHOLE) {
-      float pivot[IM];
+      float c[IM];
       int rows[IM];
 #pragma unroll
       for (int i = 0; i < IM; ++i) {
-        pivot[i] = pivot_at(m0 + i * teams);
+        c[i] = pivot_at(m0 + i * teams);
         rows[i] = load(v[i], m0 + i * teams, l.r);
       }
       if constexpr (IM == 1) col = columns_of<V>(p.n, l);
-#pragma unroll
-      for (int i = 0; i < IM; ++i) a[i] = moments_of<A>(v[i], rows[i], l.n, pivot[i]);
-      team_moments(l, p.t, a, buf, entries);
+      whole_moments(l, p.t, v, rows, a, c, buf, entries);
 #pragma unroll
       for (int i = 0; i < IM; ++i) {
-        const Stats<A> z = stats_of(a[i], pivot[i], count, p.n.eps);
+        const Stats z = stats_of(a[i], c[i], count, p.n.eps);
         put(v[i], m0 + i * teams, l.r, rows[i], z);
         keep(m0 + i * teams, z);
       }
@@ -486,9 +525,9 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       if constexpr (PHASE == SUMS) {
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           const int rows = load(v[0], m0, px);
-          merge(a[0], moments_of<A>(v[0], rows, l.n, pivot));
+          merge(a[0], lane_moments(v[0], rows, l.n, pivot));
         }
-        team_moments(l, p.t, a, buf, entries);
+        team_moments(l, p.t, a, pivot, buf, entries);
         if (live_at(m0) && l.first) *l.entry(p, m, at.seg * p.sections + l.section) = make_double2(a[0].mean, a[0].m2);
       } else {
         col = columns_of<V>(p.n, l);
@@ -510,7 +549,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
           m2[0] += b.m2 + b.n * d * d;
         });
         a[0] = {count, mean, m2[0]};
-        const Stats<A> z = stats_of(a[0], pivot, count, p.n.eps);
+        const Stats z = stats_of(a[0], pivot, count, p.n.eps);
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           const int rows = load(v[0], m0, px);
           put(v[0], m0, px, rows, z);
@@ -865,7 +904,7 @@ int grid_of(const NormParams& p) {
 }
 
 template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V> hipError_t run(const NormParams& p, hipStream_t st) {
-  const int turns = p.t.ttlog > 6 ? 2 * IM * (BWD ? 2 * 4 : 3 * (int)sizeof(Sum<F>)) * (NT / 64 << p.t.nblog) : 0;
+  const int turns = p.t.ttlog > 6 ? 2 * IM * (BWD ? 2 * 4 : 4 * (int)(PHASE == WHOLE ? sizeof(Sum<F>) : 8)) * (NT / 64 << p.t.nblog) : 0;
   if constexpr (BWD) {
     constexpr int COLS = NT * 8 * width_of<V>;
     static LdsLimitOnce once;
@@ -877,7 +916,7 @@ template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V>
   } else {
     static LdsLimitOnce once;
     auto* k = &norm_fwd_kernel<T, F, NT, KP, IM, PHASE, V>;
-    const hipError_t e = set_lds_limit_once(once, (const void*)k, 2 * IM * 3 * (int)sizeof(Sum<F>) * NT);   // (64 groups a wave)
+    const hipError_t e = set_lds_limit_once(once, (const void*)k, 2 * IM * 4 * 8 * NT);   // (64 groups a wave)
     if (e != hipSuccess) return e;
     k<<<grid_of(p), NT, turns, st>>>(p);
   }
@@ -886,7 +925,7 @@ template <bool BWD, typename T, int F, int NT, int KP, int IM, int PHASE, int V>
 template <bool BWD, typename T, int F, int V> hipError_t run_plan(const Plan& s, hipStream_t st) {
   constexpr int SIZE = sizeof(T), KP = BWD ? STREAM / 2 : STREAM;
   if (!s.whole) {
-    const hipError_t e = run<BWD, T, BWD || F == CONVBN_NORM_RELU ? F : (int)CONVBN_NORM_NONE, 1024, KP, 1, SUMS, V>(s.p, st);
+    const hipError_t e = run<BWD, T, BWD ? F : (int)CONVBN_NORM_NONE, 1024, KP, 1, SUMS, V>(s.p, st);
     return e != hipSuccess || (BWD && !s.p.n.dx) ? e : run<BWD, T, F, 1024, KP, 1, OUTPUTS, V>(s.p, st);
   }
   if (s.nt == 1024) return run<BWD, T, F, 1024, FEW, 1, WHOLE, V>(s.p, st);

@@ -1,9 +1,12 @@
-"""Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows."""
+"""Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm behind an outlying first value.
+
+Bounds are those of head_ref.py, with U = 2^-24."""
+import numpy as np
 import pytest
 import torch
 
 import head_ref as R
-from head_ref import DT
+from head_ref import DT, np64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +31,40 @@ def test_rows_that_forward_keeps_are_those_of_pack(K, M, dtype):
     ck.pack(x)
     assert torch.equal(lay.codes, ck.codes) and torch.equal(lay.scales, ck.scales)
     assert (lay.scales[:, -(-K // 128):] == 127).all()
+
+
+# ---- group norm -----------------------------------------------------------------------------------------------------
+
+# images, pixels, channels, groups: pieces of eight, with tails and single channels, in one launch and in segments
+WALKS = [(2, 64, 64, 1), (3, 1, 4096, 1), (2, 300, 32, 4), (3, 100, 65, 1), (2, 33, 65, 5), (5, 891, 72, 8), (1, 30000, 16, 2), (2, 5000, 24, 3), (1, 2289, 1472, 1),
+         (40, 9, 32, 4), (300, 1, 40, 1)]
+
+
+def _norm_within(x, images, G, act, dtype, centre, params=True):
+    """Forward and backward of x against the formulas on x - centre, a number for each group, which gives the same results, but with bounds
+    that know nothing of the centre's size."""
+    from paper_2305_11624_amd import norm as N
+    C, dt = x.shape[1], DT[dtype]
+    P = x.shape[0] // images
+    ga, be = 1 + 0.3 * torch.randn(C, generator=R.gen(1)), 0.3 * torch.randn(C, generator=R.gen(2))
+    dy = torch.randn(x.shape, generator=R.gen(3)).to(dt).float()
+    lay = N.GroupNorm(images, P, C, G, dt, act=act)
+    xd, gd, bd = x.to("cuda", dt), ga.cuda(), be.cuda()
+    x64 = np64(xd).reshape(images, P, G, C // G)
+    near = (x64 - centre(x64)).reshape(x.shape)
+    want = R.norm(near, images, G, act, dtype, np64(ga), np64(be), 1e-5, np64(dy))
+    within(lay.forward(xd, gd, bd), *want["y"], "y")
+    dx, dgamma, dbeta = lay.backward(xd, gd, bd, dy.to("cuda", dt))
+    within(dx, *want["dx"], "dx")
+    within(dgamma, *want["dgamma"], "dgamma")
+    within(dbeta, *want["dbeta"], "dbeta")
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("first,rest", [(1e3, 0), (-1e5, 0)])
+@pytest.mark.parametrize("images,P,C,G", WALKS)
+def test_group_norm_behind_an_outlying_first_value(images, P, C, G, first, rest, act):
+    """The first value of each group far from all others: a loud channel."""
+    x = torch.randn(images, P, G, C // G, generator=R.gen(7)) + rest
+    x[:, 0, :, 0] = first
+    _norm_within(x.reshape(images * P, C), images, G, act, "f32", lambda v: np.median(v, axis=(1, 3), keepdims=True))
