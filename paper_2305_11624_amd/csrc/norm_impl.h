@@ -200,13 +200,6 @@ struct Lane {
 template <int F> using Sum = std::conditional_t<F == CONVBN_NORM_RELU, double, float>;
 // Moments about a number that is kept beside them
 template <typename A> struct Moments { A n, mean, m2; };
-__device__ __forceinline__ void merge(Moments<double>& a, const Moments<double>& b) {
-  if (b.n == 0.) return;
-  const double n = a.n + b.n, d = b.mean - a.mean, q = b.n / n;
-  a.mean += d * q;
-  a.m2 += b.m2 + d * d * a.n * q;
-  a.n = n;
-}
 // Moments of IM images' groups: in, of the wave's lanes, about c; out, of the team, about the first wave's c.  That one's distance to the others' is at most
 // some deviations of the values, so that fp32 keeps what counts (about one value of the group it would not: that may lie as many deviations away as the root of the
 // group's size).  buf: [IM][waves << nblog] entries of four
@@ -335,15 +328,30 @@ template <typename T, int V, int KP> __device__ __forceinline__ Sums sums_about(
     }
   return s;
 }
-// A lane's moments about `pivot`.  What c is off by (2^-24 of the distance to `pivot` for each addition) is in the sum of the differences to it.
-template <typename T, int V, int KP> __device__ __forceinline__ Moments<double> lane_moments(Held<T, V> (&x)[KP], int rows, int n, float pivot) {
-  const float s = sum_about(x, rows, n, pivot);
-  if (rows * n == 0) return {0., 0., 0.};
-  const float c = pivot + s / (float)(rows * n);
-  const Sums q = sums_about(x, rows, n, c);
-  const double count = rows * n, e = q.m1 / count;
-  return {count, (double)c - pivot + e, q.m2 - e * q.m1};
-}
+// A lane's sums, turn by turn: each turn's about a number near its own mean, in fp32, and these about the first turn's in 64 bits.  What such a number is off by
+// (2^-24 of the distance to `pivot` for each addition) is in the sum of the differences to it.
+struct Turns {
+  float c = 0.f;
+  int n = 0;
+  double m1 = 0., m2 = 0.;
+  template <typename T, int V, int KP> __device__ __forceinline__ void add(Held<T, V> (&x)[KP], int rows, int channels, float pivot) {
+    const int many = rows * channels;
+    const float s = sum_about(x, rows, channels, pivot);
+    if (many == 0) return;
+    const float near = pivot + s / (float)many;
+    const Sums q = sums_about(x, rows, channels, near);
+    if (n == 0) c = near;
+    const double e = (double)near - c;
+    m1 += many * e + q.m1;
+    m2 += q.m2 + e * (2. * q.m1 + many * e);
+    n += many;
+  }
+  __device__ __forceinline__ Moments<double> about(float pivot) const {
+    if (n == 0) return {0., 0., 0.};
+    const double mean = m1 / n;
+    return {(double)n, (double)c - pivot + mean, m2 - mean * m1};
+  }
+};
 // The team's moments of IM images' pieces; c: in, a value of each group, out, what they are about
 template <typename A, int IM, typename T, int V, int KP>
 __device__ __forceinline__ void whole_moments(const Lane& l, const Team& t, Held<T, V> (&x)[IM][KP], const int (&rows)[IM], Moments<A> (&a)[IM], float (&c)[IM], A* buf, int entries) {
@@ -392,6 +400,16 @@ template <int V> __device__ __forceinline__ Columns<V> columns_of(const Norm& p,
 }
 
 enum { WHOLE, SUMS, OUTPUTS };   // an image at a time, or the two launches of segments
+
+// Waves a SIMD that kernels shall have registers for which need about as many as that leaves: one more halves what is in flight (8192 tokens of 4096 backward
+// 44 us with 128 registers, 63 with 129; sums of single channels, 64 registers, 8 x 3136 x 256 in groups of one)
+constexpr int least_waves(bool bwd, int f, int size, int kp, int im, int phase, int v) {
+  const bool relu = f == CONVBN_NORM_RELU;
+  if (phase == SUMS && v == ONES) return bwd ? 1 : 8;
+  if (phase != WHOLE || v != EIGHTS || kp > 2) return 1;
+  if (!bwd) return !relu ? 1 : im == 1 ? 4 : 3;
+  return f == CONVBN_NORM_NONE || (im == 1 && kp * size <= 4) ? 4 : relu && im == 1 ? 3 : 1;
+}
 
 // A lane's rows, one after the other.  WHOLE: 32-bit offsets from what is the same for the workgroup (plan_of sees to it), which take one register
 // for all of them.
@@ -445,7 +463,8 @@ template <int N, typename A, class F> __device__ __forceinline__ void over_entri
 }
 
 // IM: images at a time (WHOLE)
-template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
+template <typename T, int F, int NT, int KP, int IM, int PHASE, int V>
+__global__ __launch_bounds__(NT, least_waves(false, F, sizeof(T), KP, IM, PHASE, V)) void norm_fwd_kernel(NormParams p) {
   using A = std::conditional_t<PHASE == WHOLE, Sum<F>, double>;
   extern __shared__ __align__(16) unsigned char lds[];   // two turns' moments
   Place at;
@@ -476,7 +495,8 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
     Rows<T, PHASE> y(p.n.y, l, p.n.P, p.n.ldy, m0);
     y.from(px);
     as_held(v);
-    const float r = (float)z.r, shift = (float)(-z.mean * z.r);
+    // (x - c) r + shift, c the mean and shift what rounding c leaves of it: x r - mean r would keep 2^-24 of mean r
+    const float r = (float)z.r, c = (float)z.mean, shift = (float)((c - z.mean) * z.r);
 #pragma unroll
     for (int k = 0; k < KP; ++k) {
       T* q = y.next();
@@ -485,7 +505,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
 #pragma unroll
       for (int i = 0; i < width_of<V>; ++i) {
         float df;
-        act_of<T, F>(fmaf(fmaf(f.v[i], r, shift), col.ga.v[i], col.be.v[i]), &f.v[i], &df);
+        act_of<T, F>(fmaf(fmaf(f.v[i] - c, r, shift), col.ga.v[i], col.be.v[i]), &f.v[i], &df);
       }
       store_piece<T, V>(q, l.n, f);
     }
@@ -521,12 +541,13 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
     } else {
       const i64 m = m0 + l.team;
       const float pivot = pivot_at(m0);
-      a[0] = {A(0), A(0), A(0)};
       if constexpr (PHASE == SUMS) {
+        Turns sums;
         for (i64 px = beg + l.r; px < end; px += (i64)KP * l.RT) {
           const int rows = load(v[0], m0, px);
-          merge(a[0], lane_moments(v[0], rows, l.n, pivot));
+          sums.add(v[0], rows, l.n, pivot);
         }
+        a[0] = sums.about(pivot);
         team_moments(l, p.t, a, pivot, buf, entries);
         if (live_at(m0) && l.first) *l.entry(p, m, at.seg * p.sections + l.section) = make_double2(a[0].mean, a[0].m2);
       } else {
@@ -561,7 +582,8 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
 }
 
 // dxhat = gamma dz, dz = dy f'(z);  dx = r (dxhat - mean(dxhat) - xhat mean(dxhat xhat)),  dgamma = sum dz xhat,  dbeta = sum dz
-template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global__ __launch_bounds__(NT) void norm_bwd_kernel(NormParams p) {
+template <typename T, int F, int NT, int KP, int IM, int PHASE, int V>
+__global__ __launch_bounds__(NT, least_waves(true, F, sizeof(T), KP, IM, PHASE, V)) void norm_bwd_kernel(NormParams p) {
   constexpr int W = width_of<V>;
   extern __shared__ float cols[];   // two turns' sums; at the end the columns', [waves][2 W][64]
   Place at;
@@ -573,12 +595,12 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   const Columns<V> col = columns_of<V>(p.n, l);
   const float count = (float)p.n.P * (float)p.cg;
   Vals<W> dga = {}, dbe = {};
-  struct Image { Held<T, V> v[KP], d[KP]; float r, shift, mean, mean_l, r_l; int rows; };   // xhat = x r + shift; RELU: the rest of the statistics
+  struct Image { Held<T, V> v[KP], d[KP]; float r, shift, mean, mean_l, r_l; int rows; };   // xhat = (x - mean) r + shift; RELU: the rest of the statistics
   auto live_at = [&](i64 m0) { return m0 + l.team < p.n.M && l.n; };
   auto stats_of = [&](Image& q, i64 m0) {
     const float4 st = live_at(m0) ? *reinterpret_cast<const float4*>(p.n.stats + ((m0 + l.team) * p.n.groups + l.g) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
     q.r = st.z;
-    q.shift = -st.x * st.z;
+    q.shift = -st.y * st.z;
     q.mean = st.x;
     q.mean_l = st.y;
     q.r_l = st.w;
@@ -598,7 +620,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
   };
   // RELU: which of a piece's values passed, a bit each.  Values next to the border are looked at again with all bits: each that falls on the wrong side is off
   // by a whole gradient (2e-4 of dbeta's norm at 32 x 56 x 56 x 256).
-  // (next to zero z is off by less than 2^-22 of beta and of gamma mean r, what it is the difference of)
+  // (next to zero z is off by less than 2^-22 of beta, with which gamma xhat cancels, and 2^-21 of gamma times what rounding the mean left of xhat)
   float edge = 1.f, steep = 0.f;
 #pragma unroll
   for (int i = 0; i < W; ++i) {
@@ -613,7 +635,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       float near = INFINITY;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const float z = fmaf(fmaf(x.v[i], q.r, q.shift), col.ga.v[i], col.be.v[i]);
+        const float z = fmaf(fmaf(x.v[i] - q.mean, q.r, q.shift), col.ga.v[i], col.be.v[i]);
         open |= z > 0.f ? 1u << i : 0u;
         near = fminf(near, fabsf(z));
       }
@@ -647,13 +669,14 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
         const unsigned open = passed(q, a);
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          const float xhat = fmaf(a.v[i], q.r, q.shift), dz = V != TAIL || i < l.n ? dz_of(open, xhat, b.v[i], i) : 0.f;
+          const float d = a.v[i] - q.mean, xhat = fmaf(d, q.r, q.shift), dz = V != TAIL || i < l.n ? dz_of(open, xhat, b.v[i], i) : 0.f;
           sz.v[i] += dz;
-          sx.v[i] = fmaf(dz, xhat, sx.v[i]);
+          sx.v[i] = fmaf(dz, PHASE == SUMS ? d : xhat, sx.v[i]);
         }
       }
 #pragma unroll
     for (int i = 0; i < W; ++i) {
+      if constexpr (PHASE == SUMS) sx.v[i] = fmaf(sx.v[i], q.r, sz.v[i] * q.shift);   // (of dz (x - mean) until here: 28.7 us for 30.5 at 32 x 56 x 56 x 256)
       dbe.v[i] += sz.v[i];
       dga.v[i] += sx.v[i];
       s[0] = fmaf(sz.v[i], col.ga.v[i], s[0]);
@@ -680,7 +703,7 @@ template <typename T, int F, int NT, int KP, int IM, int PHASE, int V> __global_
       Vals<W> f;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const float xhat = fmaf(a.v[i], q.r, q.shift), dz = dz_of(open, xhat, b.v[i], i);
+        const float xhat = fmaf(a.v[i] - q.mean, q.r, q.shift), dz = dz_of(open, xhat, b.v[i], i);
         f.v[i] = fmaf(dz, rg.v[i], fmaf(xhat, r1, r0));
       }
       if (p.n.add) {

@@ -1,4 +1,5 @@
-"""Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm behind an outlying first value.
+"""Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm of values far from zero and behind an
+outlying first value.
 
 Bounds are those of head_ref.py, with U = 2^-24."""
 import numpy as np
@@ -61,10 +62,19 @@ def _norm_within(x, images, G, act, dtype, centre, params=True):
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "gelu"])
-@pytest.mark.parametrize("first,rest", [(1e3, 0), (-1e5, 0)])
+@pytest.mark.parametrize("first,rest", [(1e3, 0), (-1e5, 0), (0, 1e4)])
 @pytest.mark.parametrize("images,P,C,G", WALKS)
 def test_group_norm_behind_an_outlying_first_value(images, P, C, G, first, rest, act):
-    """The first value of each group far from all others: a loud channel."""
+    """The first value of each group far from all others: a loud channel, a zero of padding in front of a map whose mean is not zero."""
     x = torch.randn(images, P, G, C // G, generator=R.gen(7)) + rest
     x[:, 0, :, 0] = first
     _norm_within(x.reshape(images * P, C), images, G, act, "f32", lambda v: np.median(v, axis=(1, 3), keepdims=True))
+
+
+@pytest.mark.parametrize("dtype,mean", [("bf16", 200), ("f32", 1e4)])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("images,P,C,G", WALKS)
+def test_group_norm_of_a_mean_far_from_zero(images, P, C, G, act, dtype, mean):
+    """Results have the bits that the differences to the mean have, not those that the values leave."""
+    x = torch.randn(images * P, C, generator=R.gen(8)) + mean
+    _norm_within(x, images, G, act, dtype, lambda v: mean)
