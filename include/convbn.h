@@ -571,6 +571,7 @@ convbn_status convbn_glu_bwd(const convbn_qdesc *desc, const void *x, const void
  * bits which values next to its border passed): nullable in forward, what backward needs beside x.  gamma, beta: [C] fp32, NULL = ones,
  * zeros.  (P = 1, groups = 1: a norm over each token's channels.)
  *   backward   dx (+ add_in), dgamma, dbeta: nullable, each = not wanted; beta is read for f' alone.
+ * Where a ReLU is closed the gradient counts as zero, whatever dy holds there.
  * Sums and statistics are fp32, between launches and in front of a ReLU what lanes found is merged in 64 bits; mean and variance are summed from differences
  * to a number near the mean, so that neither a mean far from zero nor a value far from the others costs them bits.
  * M == 0 is no error: dgamma and dbeta become zero.  Rows need the alignment of their element (16 bytes are faster).  Outputs overlap no input, but for the

@@ -654,7 +654,7 @@ __global__ __launch_bounds__(NT, least_waves(true, F, sizeof(T), KP, IM, PHASE, 
   };
   auto dz_of = [&](unsigned open, float xhat, float dyv, int i) {
     if constexpr (F == CONVBN_NORM_NONE) return dyv;
-    if constexpr (F == CONVBN_NORM_RELU) return open >> i & 1 ? dyv : 0.f * dyv;   // (an infinite gradient behind a closed ReLU is none)
+    if constexpr (F == CONVBN_NORM_RELU) return open >> i & 1 ? dyv : 0.f;   // (an infinite gradient behind a closed ReLU is none)
     float f, df;
     act_of<T, F>(fmaf(xhat, col.ga.v[i], col.be.v[i]), &f, &df);
     return dyv * df;

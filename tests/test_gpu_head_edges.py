@@ -1,5 +1,5 @@
 """Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm of values far from zero and behind an
-outlying first value.
+outlying first value, infinite gradients behind a closed ReLU.
 
 Bounds are those of head_ref.py, with U = 2^-24."""
 import numpy as np
@@ -78,3 +78,19 @@ def test_group_norm_of_a_mean_far_from_zero(images, P, C, G, act, dtype, mean):
     """Results have the bits that the differences to the mean have, not those that the values leave."""
     x = torch.randn(images * P, C, generator=R.gen(8)) + mean
     _norm_within(x, images, G, act, dtype, lambda v: mean)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("images,P,C,G", [(2, 49, 64, 8), (300, 1, 40, 1), (2, 33, 65, 5), (1, 20000, 8, 1)])
+def test_infinite_gradients_behind_a_closed_relu_are_none(images, P, C, G, dtype):
+    from paper_2305_11624_amd import norm as N
+    dt = DT[dtype]
+    x, dy = (torch.randn(images * P, C, generator=R.gen(i)).to("cuda", dt) for i in (1, 2))
+    lay = N.GroupNorm(images, P, C, G, dt, act="relu")
+    closed = lay.forward(x) == 0
+    results = []
+    for v in (0.0, float("inf"), float("-inf"), float("nan")):
+        d = torch.where(closed, torch.full_like(dy, v), dy)
+        results.append([t.clone() for t in lay.backward(x, None, None, d)])
+    for r in results:
+        assert all(torch.isfinite(t).all() and torch.equal(t, z) for t, z in zip(r, results[0]))
