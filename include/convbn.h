@@ -552,7 +552,8 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, co
  * a rounding of h would leave in it.)
  *   backward   dg = dy u f'(g),  du = dy f(g),  dh = [dg | du];   dx = dh W (+ add_in),   dW = dh^T x,   db = column sums of dh
  * dx, dW, db nullable, each = not wanted.  With dtype BF16 sums are in fp32 and dh is rounded to bf16 before the products (db sums it
- * before that); with F32 operands meet in three bf16 parts that add up to them, and nothing is rounded below fp32.
+ * before that); with F32 operands meet in three bf16 parts that add up to them: what is left out of a product is at most 2^-24 of it, of either sign, and sums
+ * are in fp32.
  *
  * Descriptor, strides, limits and empty calls (M == 0) are those of the 8-bit rows; act may be CONVBN_ACT_ADD_IN.  Rows of x, y, dx, dy and h and W
  * need the alignment of their element, except that bf16 x whose K and ldx are multiples of 8, and bf16 W whose K is, start on 16

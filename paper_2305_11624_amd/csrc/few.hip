@@ -96,7 +96,7 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
         put(m, k, f);
       } else {
         F8 q[3];
-        split3(f, q);
+        split3_near(f, q);
 #pragma unroll
         for (int y = 0; y < 3; ++y) put(y * M + m, k, q[y]);
       }
@@ -137,7 +137,7 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
 #pragma unroll
         for (int x = 0; x < S; ++x) {
           F8 q[3];
-          split3(widen(w[x][u]), q);
+          split3_near(widen(w[x][u]), q);
           bf16x8 wv[3];
 #pragma unroll
           for (int y = 0; y < 3; ++y) {

@@ -8,8 +8,8 @@
 // and written at 5.4 TB/s.  The projections are kept in 32 bits: kept in bf16 that pass takes 122, and the gradients are off by a third more
 // (relative 2-norm against 64 bits 0.003 instead of 0.0023, where dh in bf16 and the result's own rounding make 0.0023).
 //
-// F32: operands are split into three bf16 parts that add up to all 24 bits, and the six products of parts that are not below 2^-24 of the whole are summed
-// in fp32: nothing is rounded below that.
+// F32: operands are split into three bf16 parts that add up to all 24 bits, and six products of parts are summed in fp32; the others add up to at most 2^-24 of
+// a product, of either sign.
 #include "grads.h"
 #include "mm_tile.h"
 
@@ -95,7 +95,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(NT) void glu_prep_k
           store8<bf16_t>(out, n, width, d[y]);
         } else {
           F8 part[3];
-          split3(d[y], part);
+          split3_near(d[y], part);
 #pragma unroll
           for (int i = 0; i < 3; ++i) store8<bf16_t>(out + i * p.plane, n, width, part[i]);
         }

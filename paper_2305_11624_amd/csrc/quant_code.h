@@ -192,4 +192,25 @@ __device__ __forceinline__ void split3(const F8& f, F8 (&part)[3]) {
   }
 }
 
+// ... for products of two such numbers, of whose pairs of parts the last three are left out.  The first two parts are rounded to nearest: of numbers in [1, 2) the others
+// are at most 2^-8 and 2^-17, and what is left out of a product is at most 2^-24 of it, of either sign (leading bits would leave out 2^-21, always towards zero).
+__device__ __forceinline__ void split3_near(const F8& f, F8 (&part)[3]) {
+  constexpr float MOST = 0x1.fep127f;   // (bf16's largest number: what lies above it stays finite)
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    float v[2] = {f.v[e], f.v[e + 1]};
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {   // (each difference is exact, and the last a bf16 number)
+      const unsigned near = pack_bf16x2(fminf(fmaxf(v[0], -MOST), MOST), fminf(fmaxf(v[1], -MOST), MOST));
+      const float t[2] = {bf16_lo(near), bf16_hi(near)};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool whole = (__float_as_uint(f.v[e + h]) & INF) == INF;
+        part[i].v[e + h] = !whole ? t[h] : i ? 0.f : f.v[e + h];
+        v[h] -= t[h];
+      }
+    }
+  }
+}
+
 }  // namespace convbn

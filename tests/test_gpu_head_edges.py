@@ -1,5 +1,5 @@
 """Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm of values far from zero and behind an
-outlying first value, infinite gradients behind a closed ReLU.
+outlying first value, infinite gradients behind a closed ReLU, what fp32 operands in parts leave out.
 
 Bounds are those of head_ref.py, with U = 2^-24."""
 import numpy as np
@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import head_ref as R
-from head_ref import DT, np64, within
+from head_ref import DT, U, np64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,52 @@ def test_infinite_gradients_behind_a_closed_relu_are_none(images, P, C, G, dtype
         results.append([t.clone() for t in lay.backward(x, None, None, d)])
     for r in results:
         assert all(torch.isfinite(t).all() and torch.equal(t, z) for t, z in zip(r, results[0]))
+
+
+# ---- fp32 operands of the gated product in parts --------------------------------------------------------------------
+
+def _gated(M, K, F, dtype, **kw):
+    from paper_2305_11624_amd import gated as G
+    return G.Gated(M, K, F, DT[dtype], **kw)
+
+
+def _shrinks(got, want):
+    """The mean of what got lies nearer to zero than want, in units of U |want|."""
+    got, want = np64(got), np64(want)
+    return float((np.sign(want) * (want - got) / np.abs(want)).mean() / U)
+
+
+@pytest.mark.parametrize("M,F", [(16, 4096), (300, 512)])
+def test_products_of_fp32_numbers_in_parts_are_not_drawn_to_zero(M, F):
+    """Products of one term each, of either sign.  What is left out of such a product, and each rounding of its sum, is at most some U of it and as often up as
+    down: over 10^5 of them the mean is below 0.1 U (parts that are cut off rather than rounded make 0.7).  Either is at most 7 U in one."""
+    x, W = (torch.randn(n, 1, generator=R.gen(n)) for n in (M, 2 * F))
+    lay = _gated(M, 1, F, "f32")
+    lay.forward(x.cuda(), W.cuda())
+    want = x.double() @ W.double().T
+    assert abs(_shrinks(lay.h.view(M, 2 * F), want)) < 0.1
+    within(lay.h.view(M, 2 * F), np64(want), 12 * U * np.abs(np64(want)), "h")
+
+
+def test_gradients_of_fp32_numbers_in_parts_are_not_drawn_to_zero():
+    """One row: db is dh, and each number of dW one product of it."""
+    K, F = 700, 600
+    x, W = torch.randn(1, K, generator=R.gen(1)), torch.randn(2 * F, K, generator=R.gen(2)) * K ** -0.5
+    lay = _gated(1, K, F, "f32")
+    b, dy = torch.zeros(2 * F, device="cuda"), torch.randn(1, F, generator=R.gen(3)).cuda()
+    lay.forward(x.cuda(), W.cuda(), b)
+    _, dW, db = lay.backward(x.cuda(), W.cuda(), dy, b)
+    want = db.cpu().double()[:, None] * x.double()
+    assert abs(_shrinks(dW, want)) < 0.1
+    within(dW, np64(want), 12 * U * np.abs(np64(want)), "dW")
+
+
+@pytest.mark.parametrize("M", [2, 40])
+def test_largest_fp32_numbers_in_parts_stay_finite(M):
+    """Numbers above bf16's largest, and fp32's largest itself: one term each, so that what is left out and six roundings are at most 7 U of it."""
+    x = torch.tensor([torch.finfo(torch.float32).max, -3.4e38]).repeat(M // 2)[:, None]
+    W = torch.tensor([0.5, -0.25, 1 / 3, 0.9])[:, None]
+    lay = _gated(M, 1, 2, "f32")
+    lay.forward(x.cuda(), W.cuda())
+    want = np64(x) @ np64(W).T
+    within(lay.h.view(M, 4), want, 7 * U * np.abs(want), "h")
