@@ -90,14 +90,19 @@ template <typename T, int KIND> __global__ __launch_bounds__(NT) void glu_prep_k
         for (int i = 0; i < 8; ++i) sum[y].v[i] += d[y].v[i];
         if (!p.dh) continue;
         bf16_t* out = p.dh + m * p.W2 + y * p.N;
-        const int width = y ? p.W2 - p.N : p.N;   // (u's last piece clears what is behind it)
+        const int width = y ? p.W2 - p.N : p.N;   // (u's last piece clears what is behind it: products read whole rows)
+        const int behind = y && n + 8 >= p.N ? width : 0;
         if constexpr (sizeof(T) == 2) {
           store8<bf16_t>(out, n, width, d[y]);
+          for (int c = n + 8; c < behind; ++c) out[c] = bf16_t(0.f);
         } else {
           F8 part[3];
           split3_near(d[y], part);
 #pragma unroll
-          for (int i = 0; i < 3; ++i) store8<bf16_t>(out + i * p.plane, n, width, part[i]);
+          for (int i = 0; i < 3; ++i) {
+            store8<bf16_t>(out + i * p.plane, n, width, part[i]);
+            for (int c = n + 8; c < behind; ++c) out[i * p.plane + c] = bf16_t(0.f);
+          }
         }
       }
     }

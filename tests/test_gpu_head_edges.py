@@ -34,6 +34,53 @@ def test_rows_that_forward_keeps_are_those_of_pack(K, M, dtype):
     assert (lay.scales[:, -(-K // 128):] == 127).all()
 
 
+# ---- what workspaces and outputs hold before a call ------------------------------------------------------------------
+
+@pytest.mark.parametrize("keep", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 20, 64, 300])
+@pytest.mark.parametrize("F", [1, 2, 3, 4, 5, 6, 7, 8, 9, 29, 62, 70, 71, 261])
+def test_gated_product_of_any_width_reads_nothing_that_it_has_not_written(F, M, dtype, keep):
+    """Buffers full of NaN in front of each call change no bit."""
+    from paper_2305_11624_amd import gated as G
+    K, dt = 40, DT[dtype]
+    x, W, dy = (torch.randn(*s, generator=R.gen(i)).to("cuda", dt) for i, s in enumerate([(M, K), (2 * F, K), (M, F)]))
+    b = torch.randn(2 * F, generator=R.gen(4)).cuda()
+    results = []
+    for value in (0, 255):
+        lay = G.Gated(M, K, F, dt, keep=keep)
+        for t in (lay.ws, lay.h, lay.y, lay.dx, lay.dW, lay.db):
+            if t is not None:
+                t.view(torch.uint8).fill_(value)
+        y = lay.forward(x, W, b).clone()
+        if lay.ws is not None:
+            lay.ws.fill_(value)
+        results.append([y] + [t.clone() for t in lay.backward(x, W, dy, b)])
+    assert all(torch.isfinite(a).all() and torch.equal(a, c) for a, c in zip(*results))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 20, 300])
+@pytest.mark.parametrize("K,N", [(1, 1), (3, 5), (40, 29), (130, 70), (300, 261), (513, 6), (129, 127)])
+def test_f8_linear_of_any_width_reads_nothing_that_it_has_not_written(K, N, M, dtype):
+    from paper_2305_11624_amd import quant as Q
+    dt = DT[dtype]
+    x, W, dz = (torch.randn(*s, generator=R.gen(i)).to("cuda", dt) for i, s in enumerate([(M, K), (N, K), (M, N)]))
+    results = []
+    for value in (0, 255):
+        lay = Q.F8Linear(M, K, N, dt)
+        lay.pack_weight(W)
+        for t in (lay.w_codes, lay.w_scales, lay.codes, lay.scales, lay.ws, lay.z, lay.dx, lay.dW, lay.db):
+            if t is not None:
+                t.view(torch.uint8).fill_(value)
+        lay.pack_weight(W)
+        z = lay.forward(x).clone()
+        if lay.ws is not None:
+            lay.ws.fill_(value)
+        results.append([z] + [t.clone() for t in lay.backward(dz, bias=True)])
+    assert all(torch.isfinite(a).all() and torch.equal(a, c) for a, c in zip(*results))
+
+
 # ---- group norm -----------------------------------------------------------------------------------------------------
 
 # images, pixels, channels, groups: pieces of eight, with tails and single channels, in one launch and in segments
@@ -94,6 +141,27 @@ def test_infinite_gradients_behind_a_closed_relu_are_none(images, P, C, G, dtype
         results.append([t.clone() for t in lay.backward(x, None, None, d)])
     for r in results:
         assert all(torch.isfinite(t).all() and torch.equal(t, z) for t, z in zip(r, results[0]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("images,P,C,G", WALKS)
+def test_group_norm_reads_nothing_that_it_has_not_written(images, P, C, G, act, dtype):
+    from paper_2305_11624_amd import norm as N
+    dt = DT[dtype]
+    x, dy = (torch.randn(images * P, C, generator=R.gen(i)).to("cuda", dt) for i in (1, 2))
+    ga, be = (torch.randn(C, generator=R.gen(i)).cuda() for i in (3, 4))
+    results = []
+    for value in (0, 255):
+        lay = N.GroupNorm(images, P, C, G, dt, act=act)
+        for t in (lay.ws, lay.stats, lay.y, lay.dx, lay.dgamma, lay.dbeta):
+            if t is not None:
+                t.view(torch.uint8).fill_(value)
+        y = lay.forward(x, ga, be).clone()
+        if lay.ws is not None:
+            lay.ws.fill_(value)
+        results.append([y] + [t.clone() for t in lay.backward(x, ga, be, dy)])
+    assert all(torch.isfinite(a).all() and torch.equal(a, c) for a, c in zip(*results))
 
 
 # ---- fp32 operands of the gated product in parts --------------------------------------------------------------------
