@@ -8,7 +8,7 @@
 // copy; in 8 bits 17 MB in 7.2 us, 2.4 TB/s, of which a launch is 2 - 3.
 //
 // x lies in LDS as bf16 numbers, put there by every workgroup for itself while its first weights are on the way (a launch of its own would take longer
-// than the whole product): rounded to 8 bits as the packed form is, as it is, or, fp32, in three parts that add up to it.  e4m3 weights become bf16 numbers in
+// than the whole product): rounded to 8 bits as the packed form is, as it is, or, fp32, in three parts that add up to it (and the first once more, where it is finite).  e4m3 weights become bf16 numbers in
 // registers, fp32 ones three parts, and sums are fp32 throughout.
 #include "f8_code.h"
 #include "mm_tile.h"
@@ -20,7 +20,7 @@ namespace {
 // What the weight is held as: bytes and channels of a lane's piece, streams (the gated product has two), parts
 struct F8Weight { static constexpr bool F8 = true; static constexpr int CH = 16, STREAMS = 1, PARTS = 1, UNROLL = 8; };
 struct BfWeight { static constexpr bool F8 = false; static constexpr int CH = 8, STREAMS = 2, PARTS = 1, UNROLL = 6; using T = bf16_t; };
-struct FpWeight { static constexpr bool F8 = false; static constexpr int CH = 8, STREAMS = 2, PARTS = 3, UNROLL = 4; using T = float; };
+struct FpWeight { static constexpr bool F8 = false; static constexpr int CH = 8, STREAMS = 2, PARTS = 4, UNROLL = 4; using T = float; };
 
 struct FewParams {
   F8Mul f; Glu g;                   // one of them
@@ -95,10 +95,9 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
       if constexpr (PARTS == 1) {
         put(m, k, f);
       } else {
-        F8 q[3];
-        split3_near(f, q);
+        const Parts4 q = split3_near(f);
 #pragma unroll
-        for (int y = 0; y < 3; ++y) put(y * M + m, k, q[y]);
+        for (int y = 0; y < PARTS; ++y) *reinterpret_cast<u32x4*>(xs + (y * M + m) * p.pitch + k) = q.p[y];
       }
     }
   }
@@ -133,17 +132,13 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
           acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), xv, acc[x], 0, 0, 0);
         }
       } else {
-        const bf16x8 xv[3] = {rows(0, 0), rows(1, 0), rows(2, 0)};
+        const bf16x8 xv[PARTS] = {rows(0, 0), rows(1, 0), rows(2, 0), rows(3, 0)};
 #pragma unroll
         for (int x = 0; x < S; ++x) {
-          F8 q[3];
-          split3_near(widen(w[x][u]), q);
-          bf16x8 wv[3];
+          const Parts4 q = split3_near(widen(w[x][u]));
+          bf16x8 wv[PARTS];
 #pragma unroll
-          for (int y = 0; y < 3; ++y) {
-            const u32x4 a = narrow<bf16_t>(q[y]).a;
-            wv[y] = __builtin_bit_cast(bf16x8, a);
-          }
+          for (int y = 0; y < PARTS; ++y) wv[y] = __builtin_bit_cast(bf16x8, q.p[y]);
 #pragma unroll
           for (int pr = 0; pr < 6; ++pr)
             acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[Parts<6>::B >> (2 * pr) & 3], xv[Parts<6>::A >> (2 * pr) & 3], acc[x], 0, 0, 0);
@@ -186,11 +181,11 @@ template <class W, typename T, int KIND> __global__ __launch_bounds__(512) void 
   }
 }
 
-// Rows this way, as long as every workgroup's own x takes no more LDS than this; fp32 rows, which the tiles want copies of, twice as much.  us, this and
+// Rows this way, as long as every workgroup's own x takes no more LDS than this; fp32 rows, which the tiles want copies of, more.  us, this and
 // the tiles, gated and 8 bits: one row 2048 -> 8192 12.6 and 12.8, 7.2 and 9.6; one row 4096 -> 1024 7.0 and 12.6, 5.9 and 10.2; 16 rows 512 -> 4096 5.0 and 5.7, 5.9
 // and 6.9; with twice as much 8 rows 4096 -> 4096 17.3 and 16.6, 14.4 and 12.8.
 constexpr int MOST = 16;
-constexpr int lds_x(int parts) { return (parts == 1 ? 34 : 68) * 1024; }
+constexpr int lds_x(int parts) { return (parts == 1 ? 34 : 90) * 1024; }
 int pitch_of(int K, bool f8) { return (f8 ? (K + BLK - 1) / BLK * BLK : (K + 15) & ~15) + 8; }   // (8 more: rows on other banks)
 bool fits(i64 M, int K, int parts, bool f8) { return M > 0 && M <= MOST && (i64)M * pitch_of(K, f8) * 2 * parts <= lds_x(parts); }
 
@@ -207,7 +202,7 @@ template <class W, typename T, int KIND> hipError_t launch(FewParams p, hipStrea
   const int x = (int)p.M * p.pitch * 2 * W::PARTS, sums = waves * W::STREAMS * 1024;
   static LdsLimitOnce once;
   auto* k = &few_kernel<W, T, KIND>;
-  const hipError_t e = set_lds_limit_once(once, (const void*)k, 68 * 1024);
+  const hipError_t e = set_lds_limit_once(once, (const void*)k, lds_x(W::PARTS) < 64 * 1024 ? 64 * 1024 : lds_x(W::PARTS));
   if (e != hipSuccess) return e;
   k<<<grid, waves * 64, x > sums ? x : sums, st>>>(p);
   return hipGetLastError();
@@ -223,7 +218,7 @@ hipError_t launch_f8few(const F8Mul& f, const void* x, i64 ldx, void* codes, voi
   return f.dtype == CONVBN_BF16 ? launch<F8Weight, bf16_t, 0>(p, st) : launch<F8Weight, float, 0>(p, st);
 }
 
-bool glu_few_taken(i64 M, int K, int dtype) { return fits(M, K, dtype == CONVBN_BF16 ? 1 : 3, false); }
+bool glu_few_taken(i64 M, int K, int dtype) { return fits(M, K, dtype == CONVBN_BF16 ? 1 : FpWeight::PARTS, false); }
 hipError_t launch_glu_few(const Glu& g, hipStream_t st) {
   FewParams p = {};
   p.g = g; p.x = g.x; p.ldx = g.ldx;

@@ -17,7 +17,7 @@ namespace convbn {
 
 namespace {
 
-int planes_of(int dtype) { return dtype == CONVBN_BF16 ? 1 : 3; }
+int planes_of(int dtype) { return dtype == CONVBN_BF16 ? 1 : 4; }
 
 // ---- forward ----
 template <typename T, int KIND> struct GluOut {
@@ -96,11 +96,10 @@ template <typename T, int KIND> __global__ __launch_bounds__(NT) void glu_prep_k
           store8<bf16_t>(out, n, width, d[y]);
           for (int c = n + 8; c < behind; ++c) out[c] = bf16_t(0.f);
         } else {
-          F8 part[3];
-          split3_near(d[y], part);
+          const Parts4 part = split3_near(d[y]);
 #pragma unroll
-          for (int i = 0; i < 3; ++i) {
-            store8<bf16_t>(out + i * p.plane, n, width, part[i]);
+          for (int i = 0; i < 4; ++i) {
+            store8<bf16_t>(out + i * p.plane, n, width, widen(Raw8<bf16_t>{part.p[i]}));
             for (int c = n + 8; c < behind; ++c) out[i * p.plane + c] = bf16_t(0.f);
           }
         }

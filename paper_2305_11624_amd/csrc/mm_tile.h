@@ -27,11 +27,11 @@ struct MmParams {
   float* part;                // [splits][I][W], where there are several: W = J8 or 2 J8, J8 = J rounded up to 8
 };
 
-// fp32 numbers in three bf16 parts: the pairs of parts but for those whose products are at most 2^-24 of the whole (PAIRS = 6; split3_near); or a's three
-// parts with b as it is (PAIRS = 3)
+// fp32 numbers in three bf16 parts: the pairs of parts but for those whose products are at most 2^-24 of the whole (PAIRS = 6; split3_near, plane 3 the first
+// part where it is finite); or a's three parts with b as it is (PAIRS = 3)
 template <int PAIRS> struct Parts {
-  static constexpr unsigned A = PAIRS == 6 ? 0u | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 2 << 10 : 0u | 1 << 2 | 2 << 4;
-  static constexpr unsigned B = PAIRS == 6 ? 0u | 1 << 2 | 0 << 4 | 1 << 6 | 2 << 8 | 0 << 10 : 0u;
+  static constexpr unsigned A = PAIRS == 6 ? 0u | 3 << 2 | 1 << 4 | 1 << 6 | 3 << 8 | 2 << 10 : 0u | 1 << 2 | 2 << 4;
+  static constexpr unsigned B = PAIRS == 6 ? 0u | 1 << 2 | 3 << 4 | 1 << 6 | 2 << 8 | 3 << 10 : 0u;
 };
 
 // What meets: bf16 numbers; e4m3 codes on their own instruction, which adds groups of eight products with 13 bits below the largest one's

@@ -194,23 +194,44 @@ __device__ __forceinline__ void split3(const F8& f, F8 (&part)[3]) {
 
 // ... for products of two such numbers, of whose pairs of parts the last three are left out.  The first two parts are rounded to nearest: of numbers in [1, 2) the others
 // are at most 2^-8 and 2^-17, and what is left out of a product is at most 2^-24 of it, of either sign (leading bits would leave out 2^-21, always towards zero).
-__device__ __forceinline__ void split3_near(const F8& f, F8 (&part)[3]) {
-  constexpr float MOST = 0x1.fep127f;   // (bf16's largest number: what lies above it stays finite)
+// The fourth is the first once more, zero in place of infinities and NaN: lower parts meet it, whose zeros would make NaN of an infinity.
+struct Parts4 { u32x4 p[4]; };   // eight bf16 numbers each
+__device__ __forceinline__ Parts4 split3_near(const F8& f) {
+  constexpr float MOST = 0x1.fep127f;   // bf16's largest number
+  Parts4 o;
+  float sum = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    float v[2] = {f.v[e], f.v[e + 1]};
+  for (int e = 0; e < 8; ++e) sum += fabsf(f.v[e]);
+  const bool plain = sum <= MOST;   // (no infinity, no NaN, nothing that is rounded to an infinity)
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float v[2] = {f.v[2 * e], f.v[2 * e + 1]};
 #pragma unroll
     for (int i = 0; i < 3; ++i) {   // (each difference is exact, and the last a bf16 number)
-      const unsigned near = pack_bf16x2(fminf(fmaxf(v[0], -MOST), MOST), fminf(fmaxf(v[1], -MOST), MOST));
-      const float t[2] = {bf16_lo(near), bf16_hi(near)};
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool whole = (__float_as_uint(f.v[e + h]) & INF) == INF;
-        part[i].v[e + h] = !whole ? t[h] : i ? 0.f : f.v[e + h];
-        v[h] -= t[h];
-      }
+      o.p[i][e] = pack_bf16x2(v[0], v[1]);
+      v[0] -= bf16_lo(o.p[i][e]);
+      v[1] -= bf16_hi(o.p[i][e]);
     }
   }
+  o.p[3] = o.p[0];
+  if (!plain) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float v = f.v[e];
+      const bool whole = (__float_as_uint(v) & INF) == INF;
+      unsigned t[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const unsigned near = pack_bf16x2(fminf(fmaxf(v, -MOST), MOST), 0.f) & 0xffffu;
+        t[i] = !whole ? near : i ? 0u : pack_bf16x2(f.v[e], 0.f) & 0xffffu;
+        v -= bf16_lo(near);
+        if (i == 0) t[3] = whole ? 0u : near;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o.p[i][e / 2] = e & 1 ? (o.p[i][e / 2] & 0xffffu) | t[i] << 16 : (o.p[i][e / 2] & 0xffff0000u) | t[i];
+    }
+  }
+  return o;
 }
 
 }  // namespace convbn

@@ -8,8 +8,8 @@ namespace convbn {
 // An operand: rows of `width` bytes, a multiple of 16, `ld` bytes apart; several planes (parts of fp32 numbers) `plane` bytes apart
 struct RowsOp { const uint8_t* p; i64 ld, plane; i64 width; };
 
-// Rows of whole 16-byte pieces with zeros past the last number, for operands that are not read where they are; fp32 numbers in three planes, for products
-// with others in three
+// Rows of whole 16-byte pieces with zeros past the last number, for operands that are not read where they are; fp32 numbers in four planes, for
+// products with others in four
 struct RowsCopy { i64 rows, ld; int width; const void* x; bf16_t* out; };   // (out null: none)
 hipError_t launch_rows_copies(int dtype, const RowsCopy& a, const RowsCopy& b, hipStream_t st);
 
@@ -43,10 +43,9 @@ template <typename T, int NT> __device__ __forceinline__ void rows_copy(const Ro
     if constexpr (sizeof(T) == 2) {
       store8<bf16_t>(p.out + row * W8, k, W8, v);
     } else {
-      F8 part[3];
-      split3_near(v, part);
+      const Parts4 part = split3_near(v);
 #pragma unroll
-      for (int x = 0; x < 3; ++x) store8<bf16_t>(p.out + x * plane + row * W8, k, W8, part[x]);
+      for (int x = 0; x < 4; ++x) *reinterpret_cast<u32x4*>(p.out + x * plane + row * W8 + k) = part.p[x];
     }
   }
 }

@@ -1,5 +1,5 @@
 """Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm of values far from zero and behind an
-outlying first value, infinite gradients behind a closed ReLU, what fp32 operands in parts leave out.
+outlying first value, infinite gradients behind a closed ReLU, what fp32 operands in parts leave out, infinite operands.
 
 Bounds are those of head_ref.py, with U = 2^-24."""
 import numpy as np
@@ -211,3 +211,46 @@ def test_largest_fp32_numbers_in_parts_stay_finite(M):
     lay.forward(x.cuda(), W.cuda())
     want = np64(x) @ np64(W).T
     within(lay.h.view(M, 4), want, 7 * U * np.abs(want), "h")
+
+
+def _same_kind(got, want, name):
+    """Infinities of the same sign, NaN, and finite numbers in the same places."""
+    got, want = np64(got), np.asarray(want)
+    for kind in (np.isnan, np.isposinf, np.isneginf):
+        assert np.array_equal(kind(got), kind(want)), (name, kind.__name__)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [3, 70])
+def test_infinite_operands_of_the_gated_product(M, dtype):
+    """An infinity meets numbers that bf16 holds (whose lower parts are zero), others, and a zero."""
+    K, F, dt = 40, 24, DT[dtype]
+    x, W = torch.randn(M, K, generator=R.gen(1)).to(dt).float(), torch.randn(2 * F, K, generator=R.gen(2)).to(dt).float()
+    W[::2] = W[::2].bfloat16().float()
+    x[::2] = x[::2].bfloat16().float()
+    x[0, 3], x[1, 39], x[2, 5] = float("inf"), float("-inf"), 0
+    W[7, 5], W[30, 11], W[4, 3] = float("inf"), float("-inf"), 0
+    lay = _gated(M, K, F, dtype)
+    lay.forward(x.to("cuda", dt), W.to("cuda", dt))
+    with np.errstate(invalid="ignore"):
+        _same_kind(lay.h.view(M, 2 * F), np64(x) @ np64(W).T, "h")
+
+
+@pytest.mark.parametrize("M", [3, 70])
+def test_infinite_gradients_of_the_gated_product(M):
+    K, F = 40, 24
+    x, W = torch.randn(M, K, generator=R.gen(1)), torch.randn(2 * F, K, generator=R.gen(2)) * K ** -0.5
+    x[::2], W[::2] = x[::2].bfloat16().float(), W[::2].bfloat16().float()
+    dy = torch.randn(M, F, generator=R.gen(3))
+    dy[1, 4], dy[2, 9] = float("inf"), float("-inf")
+    lay = _gated(M, K, F, "f32")
+    b = torch.zeros(2 * F)
+    lay.forward(x.cuda(), W.cuda(), b.cuda())
+    dx, dW, db = lay.backward(x.cuda(), W.cuda(), dy.cuda(), b.cuda())
+    with np.errstate(invalid="ignore"):
+        h = np64(x) @ np64(W).T
+        f, df, _ = R.act("silu", h[:, :F])
+        dh = np.concatenate([np64(dy) * h[:, F:] * df, np64(dy) * f], 1)
+        _same_kind(db, dh.sum(0), "db")
+        _same_kind(dx, dh @ np64(W), "dx")
+        _same_kind(dW, dh.T @ np64(x), "dW")
