@@ -29,6 +29,8 @@ class Gated:
 
     def __init__(self, M: int, C: int, F: int, dtype=torch.bfloat16, kind: str = "silu", train: bool = True, keep: bool = True, gap: int = 0,
                  device="cuda", y: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+        if kind not in _GATES:
+            raise ValueError(f"kind: {kind!r}, expected one of {sorted(_GATES)}")
         self.M, self.C, self.F, self.dtype, self.train = M, C, F, dtype, train
         self.ldx, self.ldy = C + gap, F + gap
         self.desc, self._add_desc = (B.make_qdesc(M, C, F, _dtype(dtype), self.ldx, self.ldy, gate=_GATES[kind]) for _ in range(2))
