@@ -527,7 +527,8 @@ convbn_status convbn_qgate_bwd(const convbn_qdesc *desc, const void *h_codes, co
  * dtype BF16 and more than 16 rows (or fewer whose channels do not fit LDS) may add the eight products of neighbouring channels 8 i .. 8 i + 7 with 13 bits below the leading bit of the
  * largest (the matrix instruction for these codes; what it drops is below 7 2^-13 of that product, and 2^-15 of the sum of all sizes on average).
  *
- * Strides, addends, alignment, limits, empty calls and the meaning of NULL are those of the 8-bit rows; scales are 4-byte aligned. */
+ * Strides, addends, alignment, limits, empty calls and the meaning of NULL are those of the 8-bit rows; scales are 4-byte aligned.  z that is x and dx that is
+ * dz are refused. */
 
 /* Bytes from one row of scales to the next (0 for channels < 1). */
 size_t convbn_fscale_bytes(int32_t channels);
@@ -557,7 +558,8 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, co
  *
  * Descriptor, strides, limits and empty calls (M == 0) are those of the 8-bit rows; act may be CONVBN_ACT_ADD_IN.  Rows of x, y, dx, dy and h and W
  * need the alignment of their element, except that bf16 x whose K and ldx are multiples of 8, and bf16 W whose K is, start on 16
- * bytes (they are read where they are, others from a copy in the workspace).  Outputs overlap no input, but for the addend. */
+ * bytes (they are read where they are, others from a copy in the workspace).  Outputs overlap no input, but for the addend;
+ * y or dx that is x is refused. */
 size_t convbn_glu_workspace_bytes(const convbn_qdesc *desc, int pass);
 convbn_status convbn_glu_fwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, void *y,
                              float *h, void *ws, size_t ws_bytes, void *stream);

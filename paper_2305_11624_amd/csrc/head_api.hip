@@ -58,6 +58,11 @@ convbn_status check_norm(const convbn_norm_desc* d, Norm* n) {
   return CONVBN_OK;
 }
 
+// The rows that a kernel reads while others of its workgroups write theirs
+convbn_status apart(const char* names, const void* out, const void* in) {
+  return out == in ? set_error(CONVBN_ERR_UNSUPPORTED, "%s: other workgroups read what this output overwrites", names) : CONVBN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -98,6 +103,7 @@ convbn_status convbn_flinear_fwd(const convbn_qdesc* desc, const void* x, void* 
   OPTIONAL(desc->add_out, elem(desc));
   if (!desc->M) return CONVBN_OK;
   TRY_STATUS(check_ws(codes ? mul_ws(desc) : fwd_ws(desc), ws, ws_bytes));
+  TRY_STATUS(apart("z is x", z, x));
   const hipStream_t st = (hipStream_t)stream;
   F8Mul m = {};
   m.M = desc->M; m.ldz = ldz; m.K = desc->K; m.N = desc->N; m.dtype = desc->dtype;
@@ -133,6 +139,7 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc* desc, const void* codes, co
   g.qx = (const uint8_t*)codes; g.sx = (const uint8_t*)scales; g.qw = (const uint8_t*)w_codes; g.sw = (const uint8_t*)w_scales;
   g.dz = dz; g.dx = dx; g.dW = dW; g.db = db;
   TRY_STATUS(check_ws(f8grad_scratch(g), ws, ws_bytes));
+  if (dx && desc->M) TRY_STATUS(apart("dx is dz", dx, dz));
   LAUNCH(launch_f8grad(g, ws, (hipStream_t)stream));
   return CONVBN_OK;
 }
@@ -151,6 +158,7 @@ convbn_status convbn_glu_fwd(const convbn_qdesc* desc, const void* x, const void
   OPTIONAL(b, 4); REQUIRE_ROWS(y, elem(desc)); OPTIONAL(h, 4);
   if (!desc->M) return CONVBN_OK;
   TRY_STATUS(check_ws(glu_scratch(g, CONVBN_PASS_FWD), ws, ws_bytes));
+  TRY_STATUS(apart("y is x", y, x));
   g.x = x; g.W = W; g.b = b; g.y = y; g.h = h;
   LAUNCH(launch_glu_fwd(g, ws, (hipStream_t)stream));
   return CONVBN_OK;
@@ -167,6 +175,7 @@ convbn_status convbn_glu_bwd(const convbn_qdesc* desc, const void* x, const void
   if (!dx && !dW && !db && desc->M) return set_error(CONVBN_ERR_NULL, "no output is asked for");
   OPTIONAL(desc->add_in, elem(desc));
   TRY_STATUS(check_ws(glu_scratch(g, CONVBN_PASS_BWD), ws, ws_bytes));
+  if (dx && desc->M) TRY_STATUS(apart("dx is x", dx, x));
   g.x = x; g.W = W; g.b = b; g.hk = h; g.dy = dy; g.dx = dx; g.dW = dW; g.db = db;
   LAUNCH(launch_glu_bwd(g, ws, (hipStream_t)stream));
   return CONVBN_OK;
@@ -184,7 +193,7 @@ convbn_status convbn_norm_fwd(const convbn_norm_desc* desc, const void* x, const
   const uintptr_t elem = n.dtype == CONVBN_BF16 ? 2 : 4;
   REQUIRE_ROWS(x, elem); OPTIONAL(gamma, 4); OPTIONAL(beta, 4); REQUIRE_ROWS(y, elem); OPTIONAL(stats, 4);
   if (!n.M) return CONVBN_OK;
-  if (x == y) return set_error(CONVBN_ERR_UNSUPPORTED, "y is x: other workgroups read a group's first value when its outputs are written");
+  TRY_STATUS(apart("y is x", y, x));
   TRY_STATUS(check_ws(norm_scratch(n, CONVBN_PASS_FWD), ws, ws_bytes));
   n.x = x; n.gamma = gamma; n.beta = beta; n.y = y; n.stats = stats;
   LAUNCH(launch_norm_fwd(n, ws, (hipStream_t)stream));
