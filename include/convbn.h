@@ -556,10 +556,11 @@ convbn_status convbn_flinear_bwd(const convbn_qdesc *desc, const void *codes, co
  * before that); with F32 operands meet in three bf16 parts that add up to them: what is left out of a product is at most 2^-24 of it, of either sign, and sums
  * are in fp32.
  *
- * Descriptor, strides, limits and empty calls (M == 0) are those of the 8-bit rows; act may be CONVBN_ACT_ADD_IN.  Rows of x, y, dx, dy and h and W
+ * Descriptor, strides, limits and empty calls (M == 0) are those of the 8-bit rows; act may hold CONVBN_ACT_ADD_IN and CONVBN_ACT_H_KEPT.  Rows of x, y, dx, dy and h and W
  * need the alignment of their element, except that bf16 x whose K and ldx are multiples of 8, and bf16 W whose K is, start on 16
  * bytes (they are read where they are, others from a copy in the workspace).  Outputs overlap no input, but for the addend;
  * y or dx that is x is refused. */
+enum { CONVBN_ACT_H_KEPT = 32 };   /* a bit of desc->act: backward is given h, and its workspace (8 N bytes a row less) has no room for it */
 size_t convbn_glu_workspace_bytes(const convbn_qdesc *desc, int pass);
 convbn_status convbn_glu_fwd(const convbn_qdesc *desc, const void *x, const void *W, const float *b, void *y,
                              float *h, void *ws, size_t ws_bytes, void *stream);

@@ -771,6 +771,9 @@ def convbn_flinear_bwd(desc, codes, scales, w_codes, w_scales, dz, dx, dW, db, w
 
 # ---- gated product ------------------------------------------------------------
 
+ACT_H_KEPT = 32
+
+
 def convbn_glu_workspace_bytes(desc: QDesc, pass_: int) -> int:
     return lib().convbn_glu_workspace_bytes(C.byref(desc), pass_)
 

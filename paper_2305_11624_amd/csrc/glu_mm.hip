@@ -127,7 +127,7 @@ Plan plan_of(const Glu& p, bool bwd) {
   s.part = mm_scratch(s.fwd, p.M, 2 * round8(p.N));
   if (bwd) {
     s.slices = row_slices(p.M, p.N);
-    s.h = align_up((size_t)p.M * 2 * p.N * 4, 256);   // (a descriptor does not say whether h is kept)
+    s.h = p.kept ? 0 : align_up((size_t)p.M * 2 * p.N * 4, 256);
     s.dh = align_up((size_t)pl * p.M * W2 * 2, 256);
     const size_t both = grads_scratch(p.M, 2 * (i64)p.N, p.K, pairs);
     s.part = s.part > both ? s.part : both;

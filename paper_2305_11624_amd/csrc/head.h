@@ -37,6 +37,7 @@ hipError_t launch_f8grad(const F8Grad& p, void* ws, hipStream_t st);
 struct Glu {
   i64 M, ldx, ldz;
   int K, N, dtype, gate;
+  bool kept;                                          // backward is given h: the workspace has no room for it
   const void* x; const void* W; const float* b;
   void* y; float* h;                                  // forward
   const float* hk; const void* dy; const void* add;    // backward (hk: the kept h, or null)

@@ -23,11 +23,13 @@ size_t fwd_ws(const convbn_qdesc* d) { return f8few_taken(d->M, d->K) ? 0 : mul_
 
 // ---- gated product ----
 convbn_status check_glu(const convbn_qdesc* d, Glu* g) {
-  TRY_STATUS(check_linear(d, &g->ldx, &g->ldz));
-  if (d->act & ~CONVBN_ACT_ADD_IN) return set_error(CONVBN_ERR_UNSUPPORTED, "act %d: only CONVBN_ACT_ADD_IN", d->act);
+  TRY_STATUS(check_linear(d, &g->ldx, &g->ldz, CONVBN_ACT_H_KEPT));
+  if (d->act & ~(CONVBN_ACT_ADD_IN | CONVBN_ACT_H_KEPT))
+    return set_error(CONVBN_ERR_UNSUPPORTED, "act %d: only CONVBN_ACT_ADD_IN and CONVBN_ACT_H_KEPT", d->act);
   if (d->gate != CONVBN_GATE_SILU && d->gate != CONVBN_GATE_GELU) return set_error(CONVBN_ERR_UNSUPPORTED, "gate %d is unknown", d->gate);
   g->M = d->M; g->K = d->K; g->N = d->N; g->dtype = d->dtype; g->gate = d->gate;
   g->add = (d->act & CONVBN_ACT_ADD_IN) ? d->add_in : nullptr;
+  g->kept = d->act & CONVBN_ACT_H_KEPT;
   return CONVBN_OK;
 }
 
@@ -170,7 +172,9 @@ convbn_status convbn_glu_bwd(const convbn_qdesc* desc, const void* x, const void
   TRY_STATUS(check_glu(desc, &g));
   REQUIRE_ROWS(x, glu_in_place(g.dtype, g.K, g.ldx) ? 16 : elem(desc));
   REQUIRE(W, glu_in_place(g.dtype, g.K, g.K) ? 16 : elem(desc));
-  OPTIONAL(b, 4); OPTIONAL(h, 4); REQUIRE_ROWS(dy, elem(desc));
+  OPTIONAL(b, 4); REQUIRE_ROWS(dy, elem(desc));
+  if (g.kept) REQUIRE_ROWS(h, 4);
+  OPTIONAL(h, 4);
   OPTIONAL(dx, elem(desc)); OPTIONAL(dW, elem(desc)); OPTIONAL(db, 4);
   if (!dx && !dW && !db && desc->M) return set_error(CONVBN_ERR_NULL, "no output is asked for");
   OPTIONAL(desc->add_in, elem(desc));

@@ -53,7 +53,7 @@ convbn_status check(const convbn_qdesc* d, i64 wx, i64 wz, i64* ldx, i64* ldz) {
   return CONVBN_OK;
 }
 
-convbn_status check_linear(const convbn_qdesc* d, i64* ldx, i64* ldz) {
+convbn_status check_linear(const convbn_qdesc* d, i64* ldx, i64* ldz, int32_t more_acts = 0) {
   if (!d) return set_error(CONVBN_ERR_NULL, "descriptor is NULL");
   if (d->N < 1) return set_error(CONVBN_ERR_SHAPE, "N must be >= 1");
   TRY_STATUS(check(d, d->K, d->N, ldx, ldz));
@@ -61,7 +61,7 @@ convbn_status check_linear(const convbn_qdesc* d, i64* ldx, i64* ldz) {
   if (d->N > MAX_OUT) return set_error(CONVBN_ERR_UNSUPPORTED, "more than %d output channels", (int)MAX_OUT);
   const i64 most = 1LL << 38;   // (more than the card holds; tile counts stay far below 2^31)
   if (d->M * d->N > most || d->M * d->K > most) return set_error(CONVBN_ERR_UNSUPPORTED, "a tensor of more than 2^38 elements");
-  if (d->act & ~(CONVBN_ACT_ADD_OUT | CONVBN_ACT_ADD_IN))
+  if (d->act & ~(CONVBN_ACT_ADD_OUT | CONVBN_ACT_ADD_IN | more_acts))
     return set_error(CONVBN_ERR_UNSUPPORTED, "act %d: only the two addends", d->act);
   if (d->M && (((d->act & CONVBN_ACT_ADD_OUT) && !d->add_out) || ((d->act & CONVBN_ACT_ADD_IN) && !d->add_in)))
     return set_error(CONVBN_ERR_NULL, "act %d asks for an addend that the descriptor does not give", d->act);

@@ -13,9 +13,9 @@ from . import quant as Q
 from .quant import _GATES, _dtype, _rows
 
 
-def workspace_bytes(M: int, C: int, F: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0) -> int:
-    """What `Gated` of these sizes needs as its `ws`."""
-    d = B.make_qdesc(M, C, F, _dtype(dtype), C + gap, F + gap)
+def workspace_bytes(M: int, C: int, F: int, dtype=torch.bfloat16, train: bool = True, gap: int = 0, keep: bool = False) -> int:
+    """What `Gated` of these sizes needs as its `ws`; keep: one that keeps h, which needs less."""
+    d = B.make_qdesc(M, C, F, _dtype(dtype), C + gap, F + gap, act=B.ACT_H_KEPT if keep else 0)
     return max(B.convbn_glu_workspace_bytes(d, p) for p in ((B.PASS_FWD, B.PASS_BWD) if train else (B.PASS_FWD,)))
 
 
@@ -33,13 +33,14 @@ class Gated:
             raise ValueError(f"kind: {kind!r}, expected one of {sorted(_GATES)}")
         self.M, self.C, self.F, self.dtype, self.train = M, C, F, dtype, train
         self.ldx, self.ldy = C + gap, F + gap
-        self.desc, self._add_desc = (B.make_qdesc(M, C, F, _dtype(dtype), self.ldx, self.ldy, gate=_GATES[kind]) for _ in range(2))
+        self._act = B.ACT_H_KEPT if train and keep else 0
+        self.desc, self._add_desc = (B.make_qdesc(M, C, F, _dtype(dtype), self.ldx, self.ldy, self._act, _GATES[kind]) for _ in range(2))
         self.y = _rows(y, M, F, self.ldy, dtype, device, "y")
         self.h = torch.empty(M, 2 * F, dtype=torch.float32, device=device) if train and keep else None
         self.dx = _rows(dx, M, C, self.ldx, dtype, device, "dx") if train else None
         self.dW = torch.empty(2 * F, C, dtype=dtype, device=device) if train else None
         self.db = torch.empty(2 * F, dtype=torch.float32, device=device) if train else None
-        need = workspace_bytes(M, C, F, dtype, train, gap)
+        need = workspace_bytes(M, C, F, dtype, train, gap, keep)
         if ws is not None and ws.nbytes < need:
             raise ValueError(f"ws: {ws.nbytes} bytes, {need} needed")
         self.ws = ws if ws is not None else torch.empty(need, dtype=torch.uint8, device=device) if need else None
@@ -63,7 +64,7 @@ class Gated:
                     or self.M and self.C > 1 and add.stride(1) != 1 or add.device != self.y.device):
                 raise ValueError(f"add: expected {self.dtype} [{self.M}, {self.C}] with rows {self.ldx} elements apart on {self.y.device}")
             d = self._add_desc
-            d.act, d.add_in = B.ACT_ADD_IN, add.data_ptr()
+            d.act, d.add_in = self._act | B.ACT_ADD_IN, add.data_ptr()
         dx, dW, db = self.dx if need_dx else None, self.dW if need_dW else None, self.db if b is not None else None
         B.convbn_glu_bwd(d, x, W, b, self.h, dy, dx, dW, db, self.ws, stream)
         return dx, dW, db
@@ -84,7 +85,7 @@ class NormGatedBlock:
                  train: bool = True, keep: bool = True, device="cuda", share: Optional["NormGatedBlock"] = None):
         M = images * pixels
         if share is None:
-            need = max(_norm.workspace_bytes(images, pixels, C, groups, dtype, train), workspace_bytes(M, C, F, dtype, train),
+            need = max(_norm.workspace_bytes(images, pixels, C, groups, dtype, train), workspace_bytes(M, C, F, dtype, train, keep=keep),
                        Q.f8_linear_workspace_bytes(M, F, C, dtype, train))
             ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
             y = dy = dn = dx = None

@@ -37,3 +37,31 @@ def test_no_rows_may_lie_anywhere(dtype):
     d, L = B.make_qdesc(0, 64, 64, dtype), B.lib()
     assert L.convbn_flinear_fwd(C.byref(d), None, None, None, C.c_void_p(4096), C.c_void_p(4096), None, None, None, 0, None) == B.OK
     assert L.convbn_glu_fwd(C.byref(d), None, C.c_void_p(4096), None, None, None, None, 0, None) == B.OK
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 40), (100, 64, 40), (8192, 64, 128), (300, 72, 29)])
+def test_a_kept_h_has_no_second_place_in_the_workspace(M, K, N, dtype):
+    from paper_2305_11624_amd import gated as G
+    h = -(-M * 2 * N * 4 // 256) * 256
+    full, less = G.workspace_bytes(M, K, N, dtype), G.workspace_bytes(M, K, N, dtype, keep=True)
+    assert full - less == h
+    assert G.Gated(M, K, N, dtype, device="cpu").ws.nbytes == less and G.Gated(M, K, N, dtype, device="cpu", keep=False).ws.nbytes == full
+    assert G.workspace_bytes(M, K, N, dtype, train=False) == G.workspace_bytes(M, K, N, dtype, train=False, keep=True)
+    d = B.make_qdesc(M, K, N, {torch.bfloat16: B.BF16, torch.float32: B.F32}[dtype], act=B.ACT_H_KEPT)
+    at = [C.c_void_p(4096 * i) for i in range(1, 9)]
+    call = lambda h, work, n: B.lib().convbn_glu_bwd(C.byref(d), at[0], at[1], None, h, at[3], at[4], at[5], None, work, n, None)
+    assert call(None, at[7], full) == B.ERR_NULL and "'h'" in B.convbn_last_error()
+    assert call(at[2], at[7], less - 1) == B.ERR_WORKSPACE
+    for f in (B.lib().convbn_flinear_fwd, B.lib().convbn_qlinear_fwd):      # (the bit is the gated product's)
+        assert f(C.byref(d), *[at[0]] * 7, at[7], full, None) == B.ERR_UNSUPPORTED
+
+
+def test_blocks_that_keep_h_have_the_smaller_workspace():
+    from paper_2305_11624_amd.gated import NormGatedBlock
+    sizes = (4, 25, 64, 256)
+    kept, again = (NormGatedBlock(*sizes, keep=k, device="cpu") for k in (True, False))
+    assert again.gated.ws.nbytes - kept.gated.ws.nbytes > 0
+    NormGatedBlock(*sizes, keep=True, device="cpu", share=again)
+    with pytest.raises(ValueError, match="ws"):
+        NormGatedBlock(*sizes, keep=False, device="cpu", share=kept)
