@@ -1,5 +1,6 @@
 """Edges of the operators for a head on the GPU: every byte of kept 8-bit floating-point rows, group norm of values far from zero and behind an
-outlying first value, infinite gradients behind a closed ReLU, what fp32 operands in parts leave out, infinite operands.
+outlying first value, infinite gradients behind a closed ReLU, what fp32 operands in parts leave out, infinite operands, a
+stack on shared buffers, buffers that hold NaN before a call.
 
 Bounds are those of head_ref.py, with U = 2^-24."""
 import numpy as np
@@ -254,3 +255,34 @@ def test_infinite_gradients_of_the_gated_product(M):
         _same_kind(db, dh.sum(0), "db")
         _same_kind(dx, dh @ np64(W), "dx")
         _same_kind(dW, dh.T @ np64(x), "dW")
+
+
+# ---- a stack ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("images,P,C,F,G", [(2, 49, 64, 136, 8), (1, 20000, 8, 24, 1), (300, 1, 72, 40, 1)])
+def test_gradient_of_a_stack_on_shared_buffers(images, P, C, F, G):
+    """Three blocks on one set of buffers: each block's gradient is handed on as it comes, in the buffer that the next one writes, and gives what blocks with
+    buffers of their own give."""
+    from paper_2305_11624_amd.gated import NormGatedBlock
+    g = R.gen(11)
+    dt = torch.bfloat16
+    x, dout = (torch.randn(images * P, C, generator=g).to("cuda", dt) for _ in range(2))
+    Wu = (torch.randn(2 * F, C, generator=g) * C ** -0.5).to("cuda", dt)
+    Wd = (torch.randn(C, F, generator=g) * F ** -0.5).to("cuda", dt)
+    ga, be = (1 + 0.2 * torch.randn(C, generator=g)).cuda(), (0.2 * torch.randn(C, generator=g)).cuda()
+    results = []
+    for shared in (False, True):
+        blocks = [NormGatedBlock(images, P, C, F, G, dt)]
+        blocks += [NormGatedBlock(images, P, C, F, G, dt, share=blocks[0] if shared else None) for _ in range(2)]
+        assert not shared or len({b.norm.dx.data_ptr() for b in blocks}) == 1
+        ins, v = [], x
+        for b in blocks:
+            b.pack_weight(Wd)
+            ins.append(v)
+            v = b.forward(v, Wu, ga, be)
+        found, d = [v.clone()], dout
+        for b, i in zip(blocks[::-1], ins[::-1]):
+            d, *params = b.backward(i, Wu, ga, be, d)
+            found += [t.clone() for t in params]
+        results.append(found + [d.clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
