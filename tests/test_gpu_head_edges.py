@@ -7,6 +7,8 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2305_11624_amd import binding as B
+
 import head_ref as R
 from head_ref import DT, U, np64, within
 
@@ -286,3 +288,96 @@ def test_gradient_of_a_stack_on_shared_buffers(images, P, C, F, G):
             found += [t.clone() for t in params]
         results.append(found + [d.clone()])
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+# ---- more than 2^31 elements -------------------------------------------------------------------------------------------
+
+def _some_rows(M):
+    return [0, 1, M // 2, M - 2, M - 1]
+
+
+def test_group_norm_of_tokens_past_2_31_elements():
+    """The last tokens like the first: what a layer of these tokens alone gives.  dy is zero but for them, so that dgamma and dbeta are theirs."""
+    from paper_2305_11624_amd import norm as N
+    C, dt = 4104, torch.bfloat16
+    M = (1 << 31) // C + 7
+    some = _some_rows(M)
+    x, dy = torch.zeros(M, C, dtype=dt, device="cuda"), torch.zeros(M, C, dtype=dt, device="cuda")
+    rows = [torch.randn(len(some), C, generator=R.gen(i)).to("cuda", dt) for i in (1, 2)]
+    x[some], dy[some] = rows
+    ga, be = (1 + 0.3 * torch.randn(C, generator=R.gen(3))).cuda(), (0.3 * torch.randn(C, generator=R.gen(4))).cuda()
+    big, small = (N.GroupNorm(n, 1, C, 1, dt, act="silu") for n in (M, len(some)))
+    assert torch.equal(big.forward(x, ga, be)[some], small.forward(rows[0], ga, be))
+    dx, dgamma, dbeta = big.backward(x, ga, be, dy)
+    want = small.backward(rows[0], ga, be, rows[1])
+    assert torch.equal(dx[some], want[0])
+    for got, ref in ((dgamma, want[1]), (dbeta, want[2])):      # (five terms, added in another order)
+        assert ((got - ref).abs() <= 16 * U * (rows[1].float().abs() * 6).sum(0)).all()
+
+
+def test_group_norm_of_an_image_past_2_31_elements():
+    """Values +-1 in equal number, but for a last pixel of another kind: mean 0 and variance 1 to 2^-18."""
+    from paper_2305_11624_amd import norm as N
+    C, dt = 2056, torch.bfloat16
+    P = (1 << 31) // C + 8
+    x = torch.ones(P, C, dtype=dt, device="cuda")
+    x[1::2] = -1
+    x[-1], x[-2] = 2.0, -2.0
+    lay = N.GroupNorm(1, P, C, 2, dt)
+    y = lay.forward(x)
+    for row in _some_rows(P):
+        assert torch.equal(y[row], x[row]), row      # (bf16: half a step is 2^-9)
+    dy = torch.zeros_like(x)
+    dy[-1, -1] = 1.0
+    dx, dgamma, dbeta = lay.backward(x, None, None, dy)
+    assert float(dx[-1, -1]) == 1.0 and float(dgamma[-1]) == pytest.approx(2.0, rel=1e-4) and float(dbeta[-1]) == 1.0
+    assert not dgamma[:-1].any() and not dbeta[:-1].any()
+
+
+def test_f8_rows_past_2_31_elements():
+    from paper_2305_11624_amd import quant as Q
+    K, dt = 4104, torch.bfloat16
+    M = (1 << 31) // K + 7
+    some = _some_rows(M)
+    x = torch.zeros(M, K, dtype=dt, device="cuda")
+    x[some] = rows = torch.randn(len(some), K, generator=R.gen(1)).to("cuda", dt)
+    big, small = Q.F8Checkpoint(M, K, dt), Q.F8Checkpoint(len(some), K, dt)
+    big.pack(x)
+    small.pack(rows)
+    assert torch.equal(big.codes[some], small.codes) and torch.equal(big.scales[some], small.scales)
+    out = big.unpack(x.fill_(3))
+    assert torch.equal(out[some], small.unpack()) and not out[2:M // 2].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_products_of_rows_that_lie_past_2_31_elements(dtype):
+    """Rows 2^20 (read in place, where they can be) and 2^21 elements apart, 2^31 of them in all: the bits of rows next to each other."""
+    from paper_2305_11624_amd import quant as Q
+    dt, K, F = DT[dtype], 64, 48
+    for M, ld in ((2100, 1 << 20), (1030, 1 << 21)):
+        x, dy = (torch.randn(M, n, generator=R.gen(n)).to("cuda", dt) for n in (K, F))
+        W = torch.randn(2 * F, K, generator=R.gen(1)).to("cuda", dt)
+        buf = [torch.empty(M * ld, dtype=dt, device="cuda") for _ in range(2)]      # of inputs and of outputs: x and dy, y and dx side by side
+        far = lambda i, at, n: buf[i].as_strided((M, n), (ld, 1), at)
+        xf, dyf, yf, dxf = far(0, 0, K), far(0, 4096, F), far(1, 0, F), far(1, 4096, K)
+        xf.copy_(x)
+        dyf.copy_(dy)
+        near = _gated(M, K, F, dtype)
+        want = [near.forward(x, W).clone()] + [t.clone() for t in near.backward(x, W, dy)[:2]]
+        lay = _gated(M, K, F, dtype)
+        lay.desc.ldx = lay._add_desc.ldx = lay.desc.ldz = lay._add_desc.ldz = ld
+        lay.y, lay.dx = yf, dxf
+        lay.ws = torch.empty(max(B.convbn_glu_workspace_bytes(lay.desc, p) for p in (B.PASS_FWD, B.PASS_BWD)), dtype=torch.uint8, device="cuda")
+        got = [lay.forward(xf, W).clone()] + [t.clone() for t in lay.backward(xf, W, dyf)[:2]]
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), ld
+        near = Q.F8Linear(M, K, F, dt)
+        near.pack_weight(W[:F])
+        want = [near.forward(x).clone()] + [t.clone() for t in near.backward(dy)[:2]]
+        lay = Q.F8Linear(M, K, F, dt)
+        lay.ldx = lay.ldz = lay.desc.ldx = lay.desc.ldz = lay._add_desc.ldx = lay._add_desc.ldz = ld
+        lay.z, lay.dx = yf, dxf
+        lay.ws = torch.empty(max(B.convbn_flinear_workspace_bytes(lay.desc, p) for p in (B.PASS_FWD, B.PASS_BWD)), dtype=torch.uint8, device="cuda")
+        lay.pack_weight(W[:F])
+        got = [lay.forward(xf).clone()] + [t.clone() for t in lay.backward(dyf)[:2]]
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), ld
+        del buf
