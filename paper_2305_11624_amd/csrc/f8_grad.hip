@@ -2,8 +2,8 @@
 //
 // What a code stands for is a bf16 number, so the codes are written out as such, once, and the products are plain ones of bf16 operands that lie across
 // the sum; fp32 dz meets them in three bf16 parts that add up to it.  One pass does all that comes in front: the codes of x and of the weight, a copy of dz
-// where it is not read in place, its column sums.  That pass is bound by memory (8192 x 4096 and 4096 x 4096 codes 31 us), the products as mm_tile.h says (227 us
-// each, 1210 TFLOP/s); 1568 x 2048 -> 512, all three gradients, is four launches' worth of waiting.
+// where it is not read in place, its column sums.  That pass is bound by memory (8192 x 4096 and 4096 x 4096 codes 25 us, 154 MB), the products as mm_tile.h says (214 and
+// 208 us, 1280 and 1320 TFLOP/s; fp32 dz, three products each, 1320 in all); 1568 x 2048 -> 512, all three gradients, is four launches' worth of waiting.
 #include "grads.h"
 
 namespace convbn {

@@ -13,8 +13,8 @@
 //
 // Backward walks several images with the same channels, so that dgamma and dbeta gather in registers; a launch joins what the workgroups found.
 //
-// Bound by memory where it is large: 8192 tokens of 4096 forward 38 us (134 MB, 3.5 TB/s) and backward 43 (201 MB, 4.7); 32 x 56 x 56 x 256, whose 51 MB the
-// last-level cache holds, forward 27, backward 28 + 28 and the join 5.  Small calls are bound by their launches: 49 x 2048 in one of 4.2 us.
+// Bound by memory where it is large: 8192 tokens of 4096 forward 41 us (134 MB, 3.3 TB/s) and backward 44 (201 MB, 4.6); 32 x 56 x 56 x 256, whose 51 MB the
+// last-level cache holds, forward 27, backward 28 + 29 and the join 5.  Small calls are bound by their launches: 49 x 2048 in one of 4.2 us.
 #pragma once
 #include "f8_code.h"
 
@@ -74,8 +74,8 @@ template <typename T, int V> __device__ __forceinline__ Vals<width_of<V>> vals(c
     return {{f.v[0], f.v[1], f.v[2], f.v[3], f.v[4], f.v[5], f.v[6], f.v[7]}};
   }
 }
-// Results leave the caches to what backward reads again: 8192 tokens of 4096 forward 38 us (44 if they stay), backward 42.8 (44.2), 32 x 56 x 56 x 256
-// 27 and 50 (23 and 57.6).
+// Results go past the L2 caches, which leaves them to what is read again.  us, each call over and over, in brackets if they stay: 8192 tokens of 4096 forward 40 (41), backward
+// 47 (46), fp32 51 (49) and 77 (83); 32 x 28 x 28 x 512 18 (20) and 24 (26); 32 x 56 x 56 x 256 27 (23) and 52 (52).
 template <typename T, int V> __device__ __forceinline__ void store_piece(T* p, int n, const Vals<width_of<V>>& f) {
   if constexpr (V == ONES) {
     *p = from_f32<T>(f.v[0]);
@@ -275,7 +275,7 @@ template <typename A> __device__ __forceinline__ Stats stats_of(const Moments<A>
   if constexpr (sizeof(A) == 8) return {c + a.mean, 1. / sqrt(a.m2 / count + eps)};
   else return {(double)c + a.mean, 1.f / sqrtf(a.m2 / count + eps)};
 }
-// ... of pairs of sums.  buf: [waves << nblog] entries of 2 IM
+// The team's sums of IM pairs.  buf: [waves << nblog] entries of 2 IM
 template <int IM> __device__ __forceinline__ void team_sums(const Lane& l, const Team& t, float (&s)[2 * IM], float* buf) {
   l.wave_sums(t, s);
   if (t.ttlog <= 6) return;
